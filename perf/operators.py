@@ -1,0 +1,631 @@
+"""The attention block on quaternion maps, as calls to be timed and compared:
+what each stands for, its inputs, one pass in plain torch operations or through
+the public entry points, the work it cannot do without and its result in 64
+bits.
+
+A block works on the pixels of a map [N, 4, C, H, W] as tokens of 4 C reals.
+Its parts, each with its own cases:
+
+- attention between the pixels (heads take Dq = C / heads quaternion channels
+  of all four components; the score is the real part of conj(q) k, the inner
+  product of 4 Dq reals) with a learned bias by buckets of the relative
+  position (dy, dx): "attention_train" is forward and backward of a training
+  step, "attention_forward" the same at inference, "attention_token" one query
+  per image against a long map or cache of keys;
+- the block's residual step with the norms before and after it, its gate, its
+  residual scale and its dropout: "residual_forward" and "residual_backward";
+- dropout by itself, its mask computed from a counter: "dropout".
+
+A case is a dict of plain values: "h", "w" is the map of keys, "hq", "wq" that
+of queries (the same in training), "kv_heads" the heads that keys and values
+have, "ny", "nx" the buckets per axis and "ry", "rx" the distances beyond which
+offsets share the last bucket, "ragged" images of differing numbers of keys,
+one of them without any.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+EPS = 1e-6
+DTYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
+
+
+# ------------------------------------------------------------------ the cases
+
+def _attention(name, kind, dtype, n, h, w, heads, dq, kv_heads=None, hq=None, wq=None, ny=1, nx=16, ry=0, rx=64,
+               ragged=False):
+    d = {"name": name} if name else {}
+    d.update(kind=kind, dtype=dtype, n=n, h=h, w=w, hq=hq or h, wq=wq or w, heads=heads, dq=dq,
+             kv_heads=kv_heads or heads, ny=ny, nx=nx, ry=ry, rx=rx, ragged=ragged)
+    return d
+
+
+def _rows(name, kind, dtype, n, h, w, c, p, gate=True, post=True, scale=True, following=True):
+    d = {"name": name} if name else {}
+    d.update(kind=kind, dtype=dtype, n=n, h=h, w=w, c=c, p=p)
+    if kind != "dropout":
+        d.update(gate=gate, post=post, scale=scale, following=following)
+    return d
+
+
+def listed():
+    return [
+        # the library's smallest layer (2 x 16 x 16, 4 channels, fp32): launch
+        # latency, heads of 8 reals
+        _attention("train_tiny_fp32", "attention_train", "fp32", 2, 16, 16, 2, 2, ny=31, nx=31, ry=15, rx=15),
+        # a deep stage's 14 x 14 maps with 256 channels, a bucket per offset
+        _attention("train_deep_stage", "attention_train", "bf16", 32, 14, 14, 16, 16, ny=27, nx=27, ry=13, rx=13),
+        # a detection backbone's 40 x 40 maps, buckets that widen with distance
+        _attention("train_detection", "attention_train", "bf16", 16, 40, 40, 8, 16, ny=16, nx=16, ry=32, rx=32),
+        # detection at 80 x 80, inference: 6400 tokens, wide heads that share
+        # keys in pairs
+        _attention("forward_detection", "attention_forward", "bf16", 2, 80, 80, 4, 32, kv_heads=2, ny=16, nx=16, ry=64,
+                   rx=64),
+        # one query per image that pools a 20 x 20 map: attention pooling at
+        # the end of a classifier
+        _attention("pool_token", "attention_token", "bf16", 64, 20, 20, 4, 16, hq=1, wq=1, ny=8, nx=8, ry=16, rx=16),
+        # a cache of 65536 tokens in a row, ragged, its heads shared in fours
+        _attention("cache_token", "attention_token", "bf16", 4, 1, 65536, 8, 16, kv_heads=2, hq=1, wq=1, nx=32, rx=128,
+                   ragged=True),
+        # the residual step of an ImageNet stage (64 channels, 64 x 56 x 56)
+        _rows("residual_imagenet", "residual_forward", "bf16", 64, 56, 56, 64, 0.1),
+        _rows("residual_imagenet_backward", "residual_backward", "bf16", 64, 56, 56, 64, 0.1),
+        # a single token at inference: latency alone
+        _rows("residual_token", "residual_forward", "bf16", 1, 1, 1, 256, 0.0),
+        # odd everywhere: 37 channels, no following norm
+        _rows("residual_odd_backward", "residual_backward", "fp32", 3, 17, 23, 37, 0.25, following=False),
+        # dropout on CIFAR maps, and on maps of rows that are no whole chunks
+        _rows("dropout_cifar", "dropout", "bf16", 128, 32, 32, 16, 0.2),
+        _rows("dropout_odd", "dropout", "fp32", 16, 20, 21, 13, 0.5),
+    ]
+
+
+_MAX_SCORES = 16 * 8 * 1600 * 1600  # of the listed training case
+_MAX_MAP = 64 * 56 * 56 * 256       # reals of the listed residual case
+
+
+def _log(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def _draw_attention(rng, kind):
+    dtype = rng.choice(["bf16", "bf16", "bf16", "fp32"])
+    kv_heads = rng.choice([1, 2, 4])
+    heads = kv_heads * rng.choice([1, 1, 1, 2, 4])
+    dq = rng.choice([2, 5, 8, 8, 12, 16, 16, 16, 16, 24, 32])
+    ragged = rng.random() < 0.4
+    if kind == "attention_token":
+        n = _log(rng, 1, 64)
+        most = max(1, min(65536, 4 * 65536 * 2 * 16 // (n * kv_heads * dq * (2 if dtype == "fp32" else 1))))
+    else:
+        n = _log(rng, 1, 32)
+        per = heads * n * max(1.0, dq / 16) * (4 if dtype == "fp32" else 1)
+        most = max(1, min(6400, int(math.sqrt(_MAX_SCORES / per))))
+    tokens = _log(rng, 1, most)
+    if rng.random() < 0.3:
+        h, w = 1, tokens
+    else:
+        w = max(1, min(tokens, int(math.sqrt(tokens) * rng.uniform(0.7, 1.4))))
+        h = max(1, tokens // w)
+    ry, rx = (min(v - 1, rng.choice([v - 1, 32, 64])) if v > 1 else 0 for v in (h, w))
+    ny, nx = (1 if r == 0 else min(2 * r + 1, 31, rng.choice([2 * r + 1, 8, 16])) for r in (ry, rx))
+    hq, wq = (1, 1) if kind == "attention_token" else (h, w)
+    return _attention(None, kind, dtype, n, h, w, heads, dq, kv_heads, hq, wq, ny, nx, ry, rx, ragged)
+
+
+def _draw_rows(rng, kind):
+    dtype = rng.choice(["bf16", "bf16", "fp32"])
+    c = rng.choice([4, 13, 16, 37, 64, 64, 100, 256])
+    pixels = _log(rng, 1, _MAX_MAP // (4 * c * (2 if dtype == "fp32" else 1)))
+    n = min(pixels, _log(rng, 1, 64))
+    w = max(1, min(224, int(math.sqrt(pixels / n) * rng.uniform(0.8, 1.25))))
+    h = max(1, pixels // (n * w))
+    p = rng.choice([0.05, 0.1, 0.2, 0.5]) if kind == "dropout" else rng.choice([0.0, 0.1, 0.25])
+    return _rows(None, kind, dtype, n, h, w, c, p, rng.random() < 0.6, rng.random() < 0.7, rng.random() < 0.7,
+                 rng.random() < 0.7)
+
+
+def draw(rng):
+    kind = rng.choice(["attention_train", "attention_train", "attention_forward", "attention_token", "attention_token",
+                       "residual_forward", "residual_backward", "residual_backward", "dropout"])
+    return _draw_attention(rng, kind) if kind.startswith("attention") else _draw_rows(rng, kind)
+
+
+# ------------------------------------------------------------------ the inputs
+
+def _bucket_map(radius, buckets):
+    """Bucket of every offset -radius..radius of an axis: one each where there
+    are enough, else half the buckets for each sign, the nearer offsets one
+    each and the others in steps that widen by a constant factor."""
+    if buckets >= 2 * radius + 1:
+        return list(range(2 * radius + 1))
+    half = buckets // 2
+    if half < 1:
+        return [0] * (2 * radius + 1)
+    near = max(1, half // 2)
+    out = []
+    for d in range(-radius, radius + 1):
+        a = abs(d)
+        if a >= near and radius > near:
+            a = near + int(math.log(a / near) / math.log(radius / near) * (half - near))
+        out.append(min(a, half - 1) + (half if d > 0 else 0))
+    return out
+
+
+def _lengths(case, gen):
+    """Keys of every image: all, or spread from none to all in an order from
+    the seed."""
+    total = case["h"] * case["w"]
+    n = case["n"]
+    if not case["ragged"]:
+        return None
+    lens = torch.tensor([total * (i + (n == 1)) // max(1, n - 1 + (n == 1)) for i in range(n)], dtype=torch.int32)
+    return lens[torch.randperm(n, generator=gen)]
+
+
+def _map(gen, dev, n, c, h, w, dtype):
+    """A map [N, 4, C, H, W] channels-last by component."""
+    return torch.randn((n, h, w, 4, c), generator=gen, device=dev, dtype=torch.float32).to(dtype).permute(0, 3, 4, 1, 2)
+
+
+def prepare(case, seed):
+    dev = torch.device("cuda")
+    gen = torch.Generator(device=dev).manual_seed(seed)
+    host = torch.Generator().manual_seed(seed)
+    dt = DTYPES[case["dtype"]]
+    n, h, w = case["n"], case["h"], case["w"]
+    st = {"case": case}
+    if case["kind"].startswith("attention"):
+        c, ckv = case["heads"] * case["dq"], case["kv_heads"] * case["dq"]
+        if case["kind"] == "attention_token":
+            st["q"] = _map(gen, dev, n, c, 1, 1, dt)
+            kv = _map(gen, dev, n, 2 * ckv, h, w, dt)
+            st["k"], st["v"] = kv[:, :, :ckv], kv[:, :, ckv:]
+        else:  # one map from one 1x1 convolution
+            qkv = _map(gen, dev, n, c + 2 * ckv, h, w, dt)
+            st["q"], st["k"], st["v"] = qkv[:, :, :c], qkv[:, :, c:c + ckv], qkv[:, :, c + ckv:]
+        st["table"] = 0.5 * torch.randn((case["heads"], case["ny"] * case["nx"]), generator=gen, device=dev)
+        st["by"] = torch.tensor(_bucket_map(case["ry"], case["ny"]), dtype=torch.int32, device=dev)
+        st["bx"] = torch.tensor(_bucket_map(case["rx"], case["nx"]), dtype=torch.int32, device=dev)
+        lens = _lengths(case, host)
+        st["kv_len"] = None if lens is None else lens.to(dev)
+        st["pos"] = None
+        if case["kind"] == "attention_token":
+            # the query's place: the middle of the map, or the cache's end
+            last = torch.full((n,), h * w, dtype=torch.int32) if lens is None else lens
+            at = torch.clamp(last - 1, min=0)
+            pos = torch.stack([at // w, at % w], 1) if h == 1 else torch.tensor([[h // 2, w // 2]]).expand(n, 2)
+            st["pos"] = pos.to(torch.int32).contiguous().to(dev)
+        if case["kind"] == "attention_train":
+            st["dout"] = _map(gen, dev, n, c, h, w, dt)
+        return st
+    c = case["c"]
+    st["rng"] = torch.randint(0, 1 << 40, (2,), generator=host).to(dev)
+    if case["kind"] == "dropout":
+        st["x"] = _map(gen, dev, n, c, h, w, dt)
+        return st
+
+    def param(flag, spread=0.2):
+        return 1.0 + spread * torch.randn((4, c), generator=gen, device=dev) if flag else None
+
+    st["gamma"], st["next_gamma"] = param(case["post"]), param(case["following"])
+    st["scale"] = None if not case["scale"] else 0.5 * param(True)
+    st["gate"] = _map(gen, dev, n, c, 1, 1, dt) if case["gate"] else None
+    st["y"] = _map(gen, dev, n, c, h, w, dt)
+    if case["kind"] == "residual_forward":
+        st["x"] = _map(gen, dev, n, c, h, w, dt)
+    else:
+        st["dout"] = _map(gen, dev, n, c, h, w, dt)
+        st["out"] = _map(gen, dev, n, c, h, w, dt) if case["following"] else None
+        st["dh"] = _map(gen, dev, n, c, h, w, dt) if case["following"] else None
+    return st
+
+
+def _keys(case):
+    """Keys that the images have together."""
+    total, n = case["h"] * case["w"], case["n"]
+    if not case["ragged"]:
+        return n * total
+    return sum(total * (i + (n == 1)) // max(1, n - 1 + (n == 1)) for i in range(n))
+
+
+def work(case):
+    es = 4 if case["dtype"] == "fp32" else 2
+    kind = case["kind"]
+    if kind.startswith("attention"):
+        d = 4 * case["dq"]
+        queries, keys = case["n"] * case["hq"] * case["wq"], _keys(case)
+        q_bytes, kv_bytes = queries * case["heads"] * d * es, keys * case["kv_heads"] * d * es
+        table = 4 * case["heads"] * case["ny"] * case["nx"]
+        products = 2 * keys * case["hq"] * case["wq"] * case["heads"] * d  # flops of one product
+        if kind == "attention_train":
+            # q, dout, out, dq; k, v and their gradients (whole, zeros behind the keys)
+            whole = case["n"] * case["h"] * case["w"] * case["kv_heads"] * d * es
+            return {"bytes": 4 * q_bytes + 2 * kv_bytes + 2 * whole + 2 * table, "flops": 7 * products}
+        return {"bytes": 2 * q_bytes + 2 * kv_bytes + table, "flops": 2 * products}
+    reals = case["n"] * case["h"] * case["w"] * 4 * case["c"]
+    if kind == "dropout":
+        return {"bytes": 2 * reals * es, "flops": reals}
+    maps = (4 if case["following"] else 3) if kind == "residual_forward" else (6 if case["following"] else 4)
+    return {"bytes": maps * reals * es, "flops": (10 if kind == "residual_forward" else 24) * reals}
+
+
+# ------------------------------------------------------------- the plain forms
+
+def _tokens(x, heads):
+    """[B, 4, C, H, W] -> [B, heads, H W, 4 Dq] in 32 bits."""
+    b, _, c, h, w = x.shape
+    x = x.permute(0, 3, 4, 1, 2).reshape(b, h * w, 4, heads, c // heads).permute(0, 3, 1, 2, 4)
+    return x.reshape(b, heads, h * w, 4 * (c // heads)).float()
+
+
+def _untokens(t, h, w, like):
+    """[B, heads, H W, 4 Dq] -> [B, 4, C, H, W] of like's type."""
+    b, heads, _, d = t.shape
+    t = t.reshape(b, heads, h * w, 4, d // 4).permute(0, 2, 3, 1, 4).reshape(b, h, w, 4, heads * (d // 4))
+    return t.to(like.dtype).permute(0, 3, 4, 1, 2)
+
+
+def _axis_buckets(n_keys, n_queries, at, buckets):
+    """[len(at), queries, keys]: bucket of key - (query + at) on one axis."""
+    r = (buckets.numel() - 1) // 2
+    keys = torch.arange(n_keys, device=buckets.device)
+    queries = torch.arange(n_queries, device=buckets.device)
+    d = keys[None, None, :] - (queries[None, :, None] + at[:, None, None])
+    return buckets.long()[torch.clamp(d, -r, r) + r]
+
+
+def _bias(st):
+    """[1 or N, heads, queries, keys]"""
+    case = st["case"]
+    at = st["pos"].long() if st["pos"] is not None else torch.zeros((1, 2), dtype=torch.long, device=st["by"].device)
+    iy = _axis_buckets(case["h"], case["hq"], at[:, 0], st["by"])
+    ix = _axis_buckets(case["w"], case["wq"], at[:, 1], st["bx"])
+    idx = iy[:, :, None, :, None] * case["nx"] + ix[:, None, :, None, :]
+    idx = idx.reshape(at.shape[0], case["hq"] * case["wq"], case["h"] * case["w"])
+    return st["table"][:, idx].transpose(0, 1)
+
+
+def _offset_sums(t):
+    """[..., queries, keys] of one axis -> sums by key - query, from the
+    lowest: every row shifted behind the next one's."""
+    q, k = t.shape[-2:]
+    width = q + k - 1
+    t = torch.nn.functional.pad(t.flip(-2), (0, q))
+    t = t.reshape(*t.shape[:-2], q * (width + 1))[..., :q * width]
+    return t.reshape(*t.shape[:-1], q, width).sum(-2)
+
+
+def _one_hot(n_keys, n_queries, buckets, n):
+    r = (buckets.numel() - 1) // 2
+    d = torch.arange(-(n_queries - 1), n_keys, device=buckets.device)
+    b = buckets.long()[torch.clamp(d, -r, r) + r]
+    return (b[:, None] == torch.arange(n, device=b.device)[None, :]).float()
+
+
+def _table_gradient(ds, case, st):
+    """[heads, queries, keys] -> [heads, ny nx]"""
+    t = ds.reshape(case["heads"], case["hq"], case["wq"], case["h"], case["w"]).permute(0, 1, 3, 2, 4)
+    t = _offset_sums(t)                               # [heads, hq, h, dx]
+    t = _offset_sums(t.permute(0, 3, 1, 2))           # [heads, dx, dy]
+    t = t @ _one_hot(case["h"], case["hq"], st["by"], case["ny"])
+    t = t.transpose(1, 2) @ _one_hot(case["w"], case["wq"], st["bx"], case["nx"])
+    return t.reshape(case["heads"], -1)
+
+
+def _plain_attention(st):
+    case = st["case"]
+    n, heads, kv_heads = case["n"], case["heads"], case["kv_heads"]
+    group, dq = heads // kv_heads, case["dq"]
+    lq, lk = case["hq"] * case["wq"], case["h"] * case["w"]
+    scale = 1.0 / math.sqrt(4 * dq)
+    bias = _bias(st)
+    train = case["kind"] == "attention_train"
+    some = max(1, min(n, (1 << 28) // (heads * lq * lk)))
+    outs, grads, table = [], [], 0.0
+    for a in range(0, n, some):
+        z = slice(a, min(n, a + some))
+        q, k, v = _tokens(st["q"][z], heads), _tokens(st["k"][z], kv_heads), _tokens(st["v"][z], kv_heads)
+        b = q.shape[0]
+        ke, ve = k.repeat_interleave(group, 1), v.repeat_interleave(group, 1)
+        s = torch.matmul(q, ke.transpose(2, 3).contiguous()) * scale + (bias if bias.shape[0] == 1 else bias[z])
+        if st["kv_len"] is not None:
+            gone = torch.arange(lk, device=s.device)[None, :] >= st["kv_len"][z][:, None]
+            s = s.masked_fill(gone[:, None, None, :], float("-inf"))
+        top = s.amax(-1, keepdim=True)
+        p = torch.exp(s - torch.where(torch.isinf(top), torch.zeros_like(top), top))
+        total = p.sum(-1, keepdim=True)
+        p = p / torch.where(total == 0, torch.ones_like(total), total)
+        outs.append(_untokens(torch.matmul(p, ve), case["hq"], case["wq"], st["q"]))
+        if not train:
+            continue
+        do = _tokens(st["dout"][z], heads)
+        dv = torch.matmul(p.transpose(2, 3).contiguous(), do)
+        dp = torch.matmul(do, ve.transpose(2, 3).contiguous())
+        ds = p * (dp - (p * dp).sum(-1, keepdim=True))
+        dqs = torch.matmul(ds, ke) * scale
+        dk = torch.matmul(ds.transpose(2, 3).contiguous(), q) * scale
+        dk, dv = (t.reshape(b, kv_heads, group, lk, 4 * dq).sum(2) for t in (dk, dv))
+        table = table + _table_gradient(ds.sum(0), case, st)
+        grads.append(torch.cat([_untokens(t, case["h"], case["w"], st["q"]) for t in (dqs, dk, dv)], 2))
+    out = torch.cat(outs)
+    return {"out": out, "dqkv": torch.cat(grads), "dtable": table} if train else {"out": out}
+
+
+_MUL = (0xD2511F53, 0xCD9E8D57)
+_WEYL = (0x9E3779B9, 0xBB67AE85)
+_ROUNDS = 7
+
+
+def _mul32(m, x):
+    """High and low halves of the product of 32-bit values held in int64."""
+    low = m * (x & 0xFFFF)
+    high = m * (x >> 16) + (low >> 16)
+    return high >> 16, ((high & 0xFFFF) << 16) | (low & 0xFFFF)
+
+
+def _keep(case, rng):
+    """[pixels, 4 C] truth values: element j of a pixel's row is kept where the
+    16 bits j % 8 of the Philox 4x32 output (7 rounds; Salmon et al. 2011) for
+    counter (j / 8, pixel, offset) and key seed reach round(65536 p)."""
+    pixels, row = case["n"] * case["h"] * case["w"], 4 * case["c"]
+    chunks = (row + 7) // 8
+    k0, k1 = rng[0] & 0xFFFFFFFF, (rng[0] >> 32) & 0xFFFFFFFF
+    c0 = torch.arange(chunks, device=rng.device)[None, :].expand(pixels, chunks)
+    c1 = torch.arange(pixels, device=rng.device)[:, None].expand(pixels, chunks)
+    c2, c3 = (rng[1] & 0xFFFFFFFF).expand_as(c0), ((rng[1] >> 32) & 0xFFFFFFFF).expand_as(c0)
+    for _ in range(_ROUNDS):
+        h0, l0 = _mul32(_MUL[0], c0)
+        h1, l1 = _mul32(_MUL[1], c2)
+        c0, c1, c2, c3 = h1 ^ c1 ^ k0, l1, h0 ^ c3 ^ k1, l0
+        k0, k1 = (k0 + _WEYL[0]) & 0xFFFFFFFF, (k1 + _WEYL[1]) & 0xFFFFFFFF
+    words = torch.stack([c0 & 0xFFFF, c0 >> 16, c1 & 0xFFFF, c1 >> 16, c2 & 0xFFFF, c2 >> 16, c3 & 0xFFFF, c3 >> 16], -1)
+    return words.reshape(pixels, chunks * 8)[:, :row] >= int(round(case["p"] * 65536))
+
+
+def _drop(t, case, rng):
+    """Dropout of [N, pixels, 4 C]"""
+    cut = int(round(case["p"] * 65536))
+    if cut == 0:
+        return t
+    return torch.where(_keep(case, rng).reshape(t.shape), t * (65536.0 / (65536 - cut)), torch.zeros_like(t))
+
+
+def _plain_rows(st):
+    case = st["case"]
+    n, h, w, c = case["n"], case["h"], case["w"], case["c"]
+
+    def rows(name):
+        t = st.get(name)
+        return None if t is None else t.permute(0, 3, 4, 1, 2).reshape(n, -1, 4 * c).float()
+
+    def unrows(t):
+        return t.reshape(n, h, w, 4, c).to(DTYPES[case["dtype"]]).permute(0, 3, 4, 1, 2)
+
+    def vec(name):
+        return None if st.get(name) is None else st[name].reshape(4 * c)
+
+    def normed(t):
+        r = torch.rsqrt((t * t).mean(-1, keepdim=True) + EPS)
+        return t * r, r
+
+    def norm_gradient(that, r, u):
+        return r * (u - that * (u * that).mean(-1, keepdim=True))
+
+    if case["kind"] == "dropout":
+        return {"out": unrows(_drop(rows("x"), case, st["rng"]))}
+    y, gate, gamma, scale, following = rows("y"), rows("gate"), vec("gamma"), vec("scale"), vec("next_gamma")
+    one = torch.ones((), device=y.device)
+    f = (one if gate is None else gate) * (one if scale is None else scale)
+    if case["kind"] == "residual_forward":
+        z = y if gamma is None else normed(y)[0] * gamma
+        out = rows("x") + f * _drop(z, case, st["rng"])
+        res = {"out": unrows(out)}
+        if following is not None:
+            res["h"] = unrows(normed(out)[0] * following)
+        return res
+    g = rows("dout")
+    res = {}
+    if following is not None:
+        dh = rows("dh")
+        that, r = normed(rows("out"))
+        res["dnext_gamma"] = (dh * that).sum((0, 1)).reshape(4, c)
+        g = g + norm_gradient(that, r, dh * following)
+    res["dx"] = unrows(g)
+    g = _drop(g, case, st["rng"])  # the mask of the forward pass
+    that, r = (y, one) if gamma is None else normed(y)
+    sums = (g * that).sum(1, keepdim=True)
+    gm = one if gamma is None else gamma
+    if gamma is not None:
+        res["dgamma"] = (sums * f).sum((0, 1)).reshape(4, c)
+    if gate is not None:
+        res["dgate"] = (sums * gm * (one if scale is None else scale)).reshape(n, 1, 1, 4, c).to(
+            st["gate"].dtype).permute(0, 3, 4, 1, 2)
+    if scale is not None:
+        res["dscale"] = (sums * gm * (one if gate is None else gate)).sum((0, 1)).reshape(4, c)
+    u = g * f * gm
+    res["dy"] = unrows(u if gamma is None else norm_gradient(that, r, u))
+    return res
+
+
+# -------------------------------------------------------------- the framework's
+
+def _own_attention(st):
+    from paper_2509_05512_amd import quan
+    case = st["case"]
+    relpos = (st["table"], st["by"], st["bx"])
+    kw = dict(relpos=relpos, kv_len=st["kv_len"], pos=st["pos"])
+    if case["kind"] != "attention_train":
+        return {"out": quan.quan_attention_forward(st["q"], st["k"], st["v"], case["heads"], **kw)}
+    out, lse, rest = quan.quan_attention_forward(st["q"], st["k"], st["v"], case["heads"], save=True, **kw)
+    c, ckv = st["q"].shape[2], st["k"].shape[2]
+    dqkv = quan.empty_qmap(case["n"], c + 2 * ckv, case["h"], case["w"], st["q"].dtype, st["q"].device)
+    dtable = quan.quan_attention_backward(st["q"], st["k"], st["v"], out, lse, rest, st["dout"], case["heads"],
+                                          dq=dqkv[:, :, :c], dk=dqkv[:, :, c:c + ckv], dv=dqkv[:, :, c + ckv:], **kw)[3]
+    return {"out": out, "dqkv": dqkv, "dtable": dtable}
+
+
+def _own_rows(st):
+    from paper_2509_05512_amd import quan
+    case = st["case"]
+    if case["kind"] == "dropout":
+        return {"out": quan.quan_dropout(st["x"], case["p"], st["rng"])}
+    kw = dict(gamma=st["gamma"], gate=st["gate"], scale=st["scale"], next_gamma=st["next_gamma"], p=case["p"],
+              rng=st["rng"], eps=EPS)
+    if case["kind"] == "residual_forward":
+        out, h = quan.quan_residual_forward(st["x"], st["y"], **kw)
+        return {"out": out} if h is None else {"out": out, "h": h}
+    g = quan.quan_residual_backward(st["y"], st["dout"], out=st["out"], dh=st["dh"], **kw)
+    res = {"dnext_gamma": g.dnext_gamma, "dx": g.dx, "dgamma": g.dgamma, "dgate": g.dgate, "dscale": g.dscale, "dy": g.dy}
+    return {k: v for k, v in res.items() if v is not None}
+
+
+def run(st):
+    if st["case"]["kind"].startswith("attention"):
+        return _own_attention(st) if own else _plain_attention(st)
+    return _own_rows(st) if own else _plain_rows(st)
+
+
+# ---------------------------------------------------------------- in 64 bits
+
+def _exact_attention(st):
+    """Image by image and head by head; the bias by a table lookup per pair of
+    pixels, its gradient by additions to the looked-up places."""
+    case = st["case"]
+    heads, dq, h, w, hq, wq = (case[k] for k in ("heads", "dq", "h", "w", "hq", "wq"))
+    group = heads // case["kv_heads"]
+    train = case["kind"] == "attention_train"
+    dev = st["table"].device
+    at_key, at_query = torch.arange(h * w, device=dev), torch.arange(hq * wq, device=dev)
+    table = st["table"].double()
+    q, k, v = (st[name].double() for name in ("q", "k", "v"))
+    out = torch.zeros_like(q)
+    grads = {name: torch.zeros_like(t) for name, t in (("dq", q), ("dk", k), ("dv", v))}
+    dtable = torch.zeros_like(table)
+
+    def idx(pos):
+        dy = (at_key // w)[None, :] - (at_query // wq)[:, None] - pos[0]
+        dx = (at_key % w)[None, :] - (at_query % wq)[:, None] - pos[1]
+        iy = st["by"].long()[dy.clamp(-case["ry"], case["ry"]) + case["ry"]]
+        return iy * case["nx"] + st["bx"].long()[dx.clamp(-case["rx"], case["rx"]) + case["rx"]]
+
+    def part(t, i, head):
+        return t[i, :, head * dq:(head + 1) * dq].reshape(4 * dq, -1)  # [reals, pixels]
+
+    same = idx((0, 0)) if st["pos"] is None else None
+    lens = [h * w] * case["n"] if st["kv_len"] is None else st["kv_len"].tolist()
+    positions = None if st["pos"] is None else st["pos"].tolist()
+    ds_all = [0.0] * heads
+    for i in range(case["n"]):
+        m = lens[i]
+        if m == 0:
+            continue
+        where = same if same is not None else idx(positions[i])
+        for head in range(heads):
+            kv = head // group
+            qh, kh, vh = part(q, i, head), part(k, i, kv)[:, :m], part(v, i, kv)[:, :m]
+            s = qh.t().contiguous() @ kh / math.sqrt(4 * dq) + table[head][where[:, :m]]
+            p = torch.exp(s - torch.logsumexp(s, 1, keepdim=True))
+            oh = vh @ p.t().contiguous()
+            part_shape = (4, dq)
+            out[i, :, head * dq:(head + 1) * dq] = oh.reshape(*part_shape, hq, wq)
+            if not train:
+                continue
+            go = part(st["dout"][i:i + 1].double(), 0, head)
+            dp = go.t().contiguous() @ vh
+            ds = p * (dp - (go * oh).sum(0)[:, None])
+            full = torch.zeros((hq * wq, h * w), dtype=torch.float64, device=dev)
+            full[:, :m] = ds
+            ds_all[head] = ds_all[head] + full
+            grads["dq"][i, :, head * dq:(head + 1) * dq] += (kh @ ds.t().contiguous() / math.sqrt(4 * dq)).reshape(
+                *part_shape, hq, wq)
+            for name, g in (("dk", qh @ ds / math.sqrt(4 * dq)), ("dv", go @ p)):
+                g = torch.cat([g, torch.zeros((4 * dq, h * w - m), dtype=g.dtype, device=dev)], 1)
+                grads[name][i, :, kv * dq:(kv + 1) * dq] += g.reshape(*part_shape, h, w)
+    if not train:
+        return {"out": out}
+    for head in range(heads):
+        if torch.is_tensor(ds_all[head]):
+            dtable[head].index_add_(0, same.reshape(-1), ds_all[head].reshape(-1))
+    return {"out": out, "dqkv": torch.cat([grads[k] for k in ("dq", "dk", "dv")], 2), "dtable": dtable}
+
+
+def _exact_factor(case, rng):
+    """Dropout's factors [N, 4, C, H, W]: 0 or 1 / (1 - p), the generator in
+    numpy's unsigned integers."""
+    n, h, w, c = (case[k] for k in ("n", "h", "w", "c"))
+    cut = int(round(case["p"] * 65536))
+    if cut == 0:
+        return 1.0
+    seed, offset = (int(v) for v in rng.tolist())
+    chunks, low = -(-4 * c // 8), np.uint64(0xFFFFFFFF)
+    full = (n * h * w, chunks)
+    ctr = [np.broadcast_to(np.arange(chunks, dtype=np.uint64)[None, :], full),
+           np.broadcast_to(np.arange(n * h * w, dtype=np.uint64)[:, None], full),
+           np.full(full, offset & 0xFFFFFFFF, np.uint64), np.full(full, offset >> 32 & 0xFFFFFFFF, np.uint64)]
+    key = [seed & 0xFFFFFFFF, seed >> 32 & 0xFFFFFFFF]
+    for _ in range(_ROUNDS):
+        a, b = ctr[0] * np.uint64(_MUL[0]), ctr[2] * np.uint64(_MUL[1])
+        ctr = [(b >> np.uint64(32)) ^ ctr[1] ^ np.uint64(key[0]), b & low,
+               (a >> np.uint64(32)) ^ ctr[3] ^ np.uint64(key[1]), a & low]
+        key = [(key[i] + _WEYL[i]) & 0xFFFFFFFF for i in range(2)]
+    words = np.stack([v.astype(np.uint32) for v in ctr], -1).view(np.uint16)  # low half first
+    kept = (words.reshape(n * h * w, chunks * 8)[:, :4 * c] >= cut).astype(np.float64) * (65536.0 / (65536 - cut))
+    return torch.from_numpy(kept).to(rng.device).reshape(n, h, w, 4, c).permute(0, 3, 4, 1, 2)
+
+
+def _exact_rows(st):
+    case = st["case"]
+    n, c = case["n"], case["c"]
+    m = _exact_factor(case, st["rng"])
+
+    def get(name):
+        t = st.get(name)
+        return None if t is None else (t.double() if t.dim() == 5 else t.double().reshape(1, 4, c, 1, 1))
+
+    def times(*ts):
+        out = 1.0
+        for t in ts:
+            out = out if t is None else out * t
+        return out
+
+    if case["kind"] == "dropout":
+        return {"out": get("x") * m}
+    y, gate, gamma, scale, following = (get(k) for k in ("y", "gate", "gamma", "scale", "next_gamma"))
+
+    def root(t):
+        return torch.sqrt((t * t).mean((1, 2), keepdim=True) + EPS)
+
+    yhat = y if gamma is None else y / root(y)
+    if case["kind"] == "residual_forward":
+        out = get("x") + times(gate, scale, gamma) * yhat * m
+        return {"out": out} if following is None else {"out": out, "h": out / root(out) * following}
+    g, res = get("dout"), {}
+    if following is not None:
+        out, dh = get("out"), get("dh")
+        r = root(out)
+        res["dnext_gamma"] = (dh * out / r).sum((0, 3, 4))
+        u = dh * following
+        g = g + u / r - out * (u * out).mean((1, 2), keepdim=True) / r ** 3
+    res["dx"] = g
+    gm = g * m
+    if gamma is not None:
+        res["dgamma"] = (gm * yhat * times(gate, scale)).sum((0, 3, 4))
+    if gate is not None:
+        res["dgate"] = (gm * yhat * times(gamma, scale)).sum((3, 4), keepdim=True)
+    if scale is not None:
+        res["dscale"] = (gm * yhat * times(gamma, gate)).sum((0, 3, 4))
+    u = gm * times(gate, scale, gamma)
+    if gamma is not None:
+        r = root(y)
+        u = u / r - y * (u * y).mean((1, 2), keepdim=True) / r ** 3
+    res["dy"] = u
+    return res
+
+
+def exact(case, seed):
+    st = prepare(case, seed)
+    return _exact_attention(st) if case["kind"].startswith("attention") else _exact_rows(st)
