@@ -456,7 +456,7 @@ def _plain_rows(st):
 def _own_attention(st):
     from paper_2509_05512_amd import quan
     case = st["case"]
-    relpos = (st["table"], st["by"], st["bx"])
+    relpos = (st["table"].view(case["heads"], case["ny"], case["nx"]), st["by"], st["bx"])
     kw = dict(relpos=relpos, kv_len=st["kv_len"], pos=st["pos"])
     if case["kind"] != "attention_train":
         return {"out": quan.quan_attention_forward(st["q"], st["k"], st["v"], case["heads"], **kw)}
@@ -465,7 +465,7 @@ def _own_attention(st):
     dqkv = quan.empty_qmap(case["n"], c + 2 * ckv, case["h"], case["w"], st["q"].dtype, st["q"].device)
     dtable = quan.quan_attention_backward(st["q"], st["k"], st["v"], out, lse, rest, st["dout"], case["heads"],
                                           dq=dqkv[:, :, :c], dk=dqkv[:, :, c:c + ckv], dv=dqkv[:, :, c + ckv:], **kw)[3]
-    return {"out": out, "dqkv": dqkv, "dtable": dtable}
+    return {"out": out, "dqkv": dqkv, "dtable": dtable.view(case["heads"], -1)}
 
 
 def _own_rows(st):
