@@ -545,6 +545,191 @@ QUAN_API int quan_iqbn_backward(const void *x, const void *dout, const void *y,
                                 int32_t n, int32_t c, int32_t h, int32_t w,
                                 int32_t dtype, void *stream);
 
+/*
+ * The attention block on quaternion maps
+ * --------------------------------------
+ * A block takes the pixels of a map as tokens of 4*C reals.  Its projections
+ * are 1x1 quaternion convolutions; the parts below are what stands between
+ * them: attention between pixels, the norms before and after the block with
+ * its gate, residual scale and dropout.  Maps of these entry points may hold
+ * 2^31 elements and more; an image may hold 2^24 pixels, a call 2^31 - 1.
+ */
+
+/*
+ * Learned bias of attention by buckets of the relative position (dy, dx) =
+ * place of the key - place of the query.  Offsets -radius..radius of an axis
+ * have the buckets bucket[0 .. 2*radius], those beyond take the ends' (entries
+ * outside 0..buckets-1 count as the nearest bucket).
+ *
+ *   table      [heads][buckets_y * buckets_x] fp32 on the device, the bias of
+ *              head h being table[h][by * buckets_x + bx]; -infinity keeps a
+ *              pair of pixels apart
+ *   bucket_y, bucket_x   int32 [2*radius + 1] on the device; NULL puts the
+ *              whole axis into bucket 0
+ *   buckets_*  1..1024; radius_* >= 0
+ */
+typedef struct quan_relpos {
+    const float *table;
+    const int32_t *bucket_y, *bucket_x;
+    int32_t buckets_y, buckets_x;
+    int32_t radius_y, radius_x;
+} quan_relpos;
+
+/*
+ * A bucket map for quan_relpos, written to host memory: one bucket per offset
+ * where buckets >= 2*radius + 1; else buckets/2 for each sign (an offset of 0
+ * counts as negative), the nearer half of them one per distance and the others
+ * in steps that widen by a constant factor up to `radius`.  map holds 2*radius
+ * + 1 entries.
+ */
+QUAN_API int quan_relpos_buckets(int32_t radius, int32_t buckets, int32_t *map);
+
+/*
+ * Attention between pixels.  With head h taking the dq = C / heads quaternion
+ * channels h*dq.. of q, and of k and v those of kv head g = h / (heads /
+ * kv_heads), over the keys j < kv_len of image n,
+ *
+ *   s_ij = scale * Re(sum_c conj(q_ic) k_jc) + bias[h][bucket(i, j)]
+ *   P_ij = exp(s_ij) / sum_j exp(s_ij),   out_i = sum_j P_ij v_j;
+ *
+ * the real part is the inner product of the 4*dq reals.  A query without a key
+ * (kv_len 0, or every bias -infinity) has out 0.
+ *
+ *   q, out     descriptors [N, 4, C, Hq, Wq]; k, v [N, 4, kv_heads*dq, Hk, Wk]
+ *              of the same dtype.  Channels lie side by side and pixels in row
+ *              order at one stride; the strides of components, pixels and
+ *              images are free as long as they ascend (a channel slice of a
+ *              wider map in the library's layout, as one convolution for q, k
+ *              and v gives them).  Anything else returns QUAN_ERR_LAYOUT.
+ *              Pointers are aligned to their element; 16-byte aligned pointers
+ *              and strides with dq a multiple of 8 run faster.
+ *   relpos     the bias, or NULL for none.
+ *   kv_len     int32 [N] on the device, or NULL: keys of each image in row
+ *              order (clamped to 0..Hk*Wk).  What lies behind them is not read.
+ *   pos        int32 [N][2] on the device, or NULL for (0, 0): the place (y,
+ *              x) of query (0, 0) in the keys' map, for the bias alone.
+ *   scale      finite.
+ *   heads      divides C; dq <= 32, and dq must divide k's channels into a
+ *              number of heads that divides `heads`.
+ *   rest       NULL, or (bf16) a 16-byte aligned dense map like out's that
+ *              receives bf16(out before rounding - out).
+ *   stats      NULL, or fp32 [N][heads][Hq*Wq][2]: each row's maximum in units
+ *              of log 2 (0 for a row without a key) and the sum of
+ *              2^(score - maximum).
+ *
+ * rest and stats are what quan_attention_backward takes.  With a bias, maps of
+ * more than one row may be 1792 pixels wide.  out may overlap no input; it may
+ * be a slice of a map that holds inputs in other channels.  Probabilities are
+ * rounded to dtype before they meet v; everything else is fp32.  Calls with
+ * few queries split the keys over work-groups where a workspace can be had
+ * (at most 64 MiB); a captured call that cannot have it sums them in one piece,
+ * and so may differ in rounding.
+ */
+QUAN_API int quan_attention_forward(const quan_tensor *q, const quan_tensor *k, const quan_tensor *v,
+                                    const quan_relpos *relpos, const int32_t *kv_len, const int32_t *pos,
+                                    float scale, int32_t heads, quan_tensor *out, void *rest, float *stats,
+                                    void *stream);
+
+/*
+ * Gradients of quan_attention_forward for dL/dout = dout, from what it was
+ * given and gave:
+ *
+ *   dP = dout v^T,  dS = P (dP - rowsum(dout out)),  dv = P^T dout,
+ *   dq = scale dS k,  dk = scale dS^T q,
+ *   dtable[h][b] = sum of dS over the images and pairs of pixels in bucket b.
+ *
+ *   rest       the forward's, or NULL: row sums then take the rounded out.
+ *   dq, dk, dv descriptors like q, k, v (strides of their own; slices of one
+ *              map may be passed), overlapping nothing else.  dk and dv are
+ *              sums over the heads that share them, and zero behind kv_len.
+ *   dtable     fp32 [heads][buckets_y * buckets_x], or NULL.
+ * Every other argument is the forward's.  Sums have a fixed order (dtable's in
+ * fp32 within a tile of queries, in fp64 beyond): deterministic.  Uses a
+ * workspace per (device, stream), with dtable of about 4 * N * heads *
+ * (Hq*Wq / 128) * (offsets of a map) bytes.
+ */
+QUAN_API int quan_attention_backward(const quan_tensor *q, const quan_tensor *k, const quan_tensor *v,
+                                     const quan_relpos *relpos, const int32_t *kv_len, const int32_t *pos,
+                                     float scale, int32_t heads, const quan_tensor *out, const void *rest,
+                                     const float *stats, const quan_tensor *dout, quan_tensor *dq,
+                                     quan_tensor *dk, quan_tensor *dv, float *dtable, void *stream);
+
+/*
+ * The norm of a pixel's 4*c reals: out = gamma x / sqrt(mean(x^2) + eps).
+ * x, out   [n, 4, c, h, w] in the library's layout, c <= 1024; out may be x.
+ * gamma    [4, c] fp32.
+ */
+QUAN_API int quan_rmsnorm_forward(const void *x, const float *gamma, float eps, void *out, int32_t n,
+                                  int32_t c, int32_t h, int32_t w, int32_t dtype, void *stream);
+
+/* Its gradients for dL/dout = dout: dx = dres + r (gamma dout - xhat
+ * mean(gamma dout xhat)), r = 1 / sqrt(mean(x^2) + eps), xhat = r x, and dgamma
+ * = sum of dout xhat over pixels ([4, c] fp32, added up in fp64 in a fixed
+ * order).  dres, like x, is a gradient that reaches x past the norm, or NULL;
+ * dx may be dres or dout but may not otherwise overlap an input. */
+QUAN_API int quan_rmsnorm_backward(const void *x, const void *dout, const float *gamma, const void *dres,
+                                   float eps, void *dx, float *dgamma, int32_t n, int32_t c, int32_t h,
+                                   int32_t w, int32_t dtype, void *stream);
+
+/*
+ * A block's residual step with the norm behind the block and the one before
+ * the next:
+ *
+ *   z   = gamma y / sqrt(mean(y^2) + eps)        (gamma NULL: z = y)
+ *   out = x + scale gate dropout(z)              (scale, gate NULL: 1)
+ *   h   = next_gamma out / sqrt(mean(out^2) + eps)   (next_gamma NULL: none)
+ *
+ *   x, y, out, h  [n, 4, c, h, w] in the library's layout, c <= 1024; out may
+ *                 be x or y, h overlaps nothing.  h is NULL with next_gamma.
+ *   gate          one map pixel per image, [n, 4, c, 1, 1] (dtype, 16-byte
+ *                 aligned): factors from outside the block.
+ *   gamma, scale, next_gamma  [4, c] fp32.
+ *   p, rng        dropout, as quan_dropout.
+ * The norm of out takes it before its rounding.
+ */
+QUAN_API int quan_residual_forward(const void *x, const void *y, const void *gate, const float *gamma,
+                                   const float *scale, const float *next_gamma, float p,
+                                   const uint64_t *rng, float eps, void *out, void *h, int32_t n,
+                                   int32_t c, int32_t height, int32_t w, int32_t dtype, void *stream);
+
+/*
+ * Its gradients for dL/dout = dout and dL/dh = dh (out and dh are NULL with
+ * next_gamma).  With G = dout + the norm's gradient of dh at out, m the
+ * dropout's factors (its mask computed anew), yhat = y / sqrt(mean(y^2) + eps)
+ * (y without gamma) and Q[n] = sum over an image's pixels of G m yhat,
+ *
+ *   dx = G,   dy = the norm's gradient of scale gate m G at y,
+ *   dgate[n] = scale gamma Q[n],   dgamma = sum_n gate scale Q,
+ *   dscale = sum_n gate gamma Q,   dnext_gamma = sum of dh out / sqrt(...).
+ *
+ * dgate (dtype), dgamma, dscale and dnext_gamma (fp32 [4, c]) are NULL exactly
+ * where their parameter is.  dx may be dout or dh, dy may be y; other overlaps
+ * are refused.  Sums are added in fp64 in a fixed order: deterministic.  Uses
+ * a workspace per (device, stream).
+ */
+QUAN_API int quan_residual_backward(const void *y, const void *dout, const void *out, const void *dh,
+                                    const void *gate, const float *gamma, const float *scale,
+                                    const float *next_gamma, float p, const uint64_t *rng, float eps,
+                                    void *dx, void *dy, void *dgate, float *dgamma, float *dscale,
+                                    float *dnext_gamma, int32_t n, int32_t c, int32_t h, int32_t w,
+                                    int32_t dtype, void *stream);
+
+/*
+ * Dropout whose mask is computed, never stored: out = x / (1 - p') where kept,
+ * else 0, p' = round(65536 p) / 65536.  Real j of pixel m (its row of 4*c
+ * reals, component-major; m counts n, h, w) is kept where the 16 bits j % 8
+ * (low half of word 0 first) of Philox 4x32 with 7 rounds reach 65536 p', its
+ * counter being (j / 8, m, offset low, offset high) and its key seed.  The same
+ * call on a gradient is the backward pass.
+ *
+ *   x, out  [n, 4, c, h, w] in the library's layout; out may be x.
+ *   p       0 <= p < 1.
+ *   rng     {seed, offset}, two uint64 on the device (so that a replayed graph
+ *           may see new ones), 8-byte aligned; NULL is allowed with p = 0.
+ */
+QUAN_API int quan_dropout(const void *x, float p, const uint64_t *rng, void *out, int32_t n, int32_t c,
+                          int32_t h, int32_t w, int32_t dtype, void *stream);
+
 /* Message describing the last failure of a quan_* call on this thread
  * ("" if none).  The pointer stays valid until the next call on the thread. */
 QUAN_API const char *quan_last_error(void);

@@ -1,0 +1,641 @@
+// Attention between the pixels of quaternion maps on gfx950, forward.
+//
+// A work-group takes NW x 32 queries of one head and image and walks over the
+// keys in tiles of LDS with the running maximum and sum of a softmax; a wave
+// holds its 32 queries' rows, and the transposed scores S^T = K Q^T leave a
+// query's scores in two lanes (see attention_tile.h), so that maxima and sums
+// are taken in registers and the probabilities are the next product's operand.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "attention_tile.h"
+
+namespace quan {
+namespace {
+
+// What a forward launch computes, and where its partial results go.
+struct Forward {
+    AttnCall a;
+    Offsets o;
+    AttnMap out;
+    void *rest;
+    float *stats;
+    int blocks, splits, tiles_per_split;  // of queries per head; of the keys; tiles of a split
+    float *part, *part_stats;             // [split][row][D], [split][row][2] (splits > 1)
+};
+
+// The scores of two half-waves' quads with their bias.  MODE 0: no bias; 1: 4
+// keys of a quad lie in one row of the map; 2: any.
+template <int MODE>
+__device__ __forceinline__ void add_bias(f32x16 &s, float c, const float *bias, const int *place, int at, int sub,
+                                         int half)
+{
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        if (MODE == 0) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                s[4 * g + t] *= c;
+        } else if (MODE == 1) {
+            const float *b = bias + at + place[32 * sub + 8 * g + 4 * half];
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                s[4 * g + t] = fmaf(s[4 * g + t], c, b[t]);
+        } else {
+            const i32x4 p = *reinterpret_cast<const i32x4 *>(place + 32 * sub + 8 * g + 4 * half);
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                s[4 * g + t] = fmaf(s[4 * g + t], c, bias[at + p[t]]);
+        }
+    }
+}
+
+template <typename T, int DQP, int MODE, int NW>
+__global__ void __launch_bounds__(64 * NW) attention_forward_kernel(Forward f)
+{
+    constexpr int DP = 4 * DQP, kThreads = 64 * NW, kQueries = 32 * NW;
+    typedef Stage<T, DP, kThreads> Tile;
+    typedef typename Elem<T>::frag frag;
+    constexpr int KT = Tile::kTokens, SUBS = KT / 32, ROW = Tile::kRow;
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
+    T *k_lds = reinterpret_cast<T *>(lds_raw), *v_lds = k_lds + 2 * Tile::kElems;
+    int *place = reinterpret_cast<int *>(v_lds + 2 * Tile::kElems);
+    float *bias = reinterpret_cast<float *>(place + 2 * KT);
+
+    const AttnGeom &g = f.a.g;
+    const int lq = g.lq(), lk = g.lk();
+    const int total = g.n * g.heads * f.splits * f.blocks;
+    int id = xcd_order(total);
+    if (id >= total)
+        return;
+    const int block = id % f.blocks;
+    id /= f.blocks;
+    const int split = id % f.splits;
+    id /= f.splits;
+    const int head = id % g.heads, img = id / g.heads;
+    const int kv_head = head / (g.heads / g.kv_heads);
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int q0 = block * kQueries;
+    const int query = q0 + 32 * wave + (lane & 31);
+    const bool q_here = query < lq;
+    const int len = f.a.kv_len != nullptr ? min(max(f.a.kv_len[img], 0), lk) : lk;
+    const int first = split * f.tiles_per_split * KT;
+    const int end = min(len, first + f.tiles_per_split * KT);
+
+    const HeadMap<const T, DQP> qm(f.a.q, img, head, g.dq), km(f.a.k, img, kv_head, g.dq), vm(f.a.v, img, kv_head, g.dq);
+    frag q[DP / 16];
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i)
+        q[i] = qm.load(query, 16 * i + 8 * half, q_here);
+
+    f32x16 o[DP / 32];
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i)
+        o[i] = 0.0f;
+    float top = -INFINITY, sum = 0.0f;
+    const float c = g.scale * kLog2e;
+
+    // offsets of this work-group's queries
+    int pos_y = 0, pos_x = 0, lane_at = 0, low_q = 0, high_q = 0, segment = -1;
+    const float *table = nullptr;
+    if (MODE != 0) {
+        if (f.a.pos != nullptr) {
+            pos_y = f.a.pos[2 * img];
+            pos_x = f.a.pos[2 * img + 1];
+        }
+        table = f.a.bias.table + int64_t(head) * f.a.bias.ny * f.a.bias.nx;
+        low_q = f.o.origin - place_q(f.o, min(q0 + kQueries, lq) - 1);
+        high_q = f.o.origin - place_q(f.o, q0);
+        lane_at = f.o.origin - place_q(f.o, min(query, lq - 1));
+    }
+    const int high = MODE != 0 ? high_q + place_k(f.o, max(end, 1) - 1) + 4 : 0;  // past the last offset
+
+    Tile kt, vt;
+    if (first < end) {
+        kt.fetch(km, first, end);
+        vt.fetch(vm, first, end);
+    }
+    int buf = 0;
+    for (int j0 = first; j0 < end; j0 += KT, buf ^= 1) {
+        T *kb = k_lds + buf * Tile::kElems, *vb = v_lds + buf * Tile::kElems;
+        int *pl = place + buf * KT;
+        kt.put(kb);
+        vt.put(vb);
+        if (MODE != 0) {
+            if (threadIdx.x < KT)
+                pl[threadIdx.x] = place_k(f.o, min(j0 + int(threadIdx.x), lk - 1));
+            const int lo = low_q + place_k(f.o, j0), hi = high_q + place_k(f.o, min(j0 + KT, lk) - 1) + 3;
+            if (segment < 0 || hi >= segment + f.o.cap) {
+                if (segment >= 0)
+                    __syncthreads();  // the last segment has been read
+                segment = lo;
+                stage_bias(bias, f.o, f.a.bias, table, segment, min(f.o.cap, high - segment), pos_y, pos_x);
+            }
+        }
+        __syncthreads();
+        if (j0 + KT < end) {
+            kt.fetch(km, j0 + KT, end);
+            vt.fetch(vm, j0 + KT, end);
+        }
+        f32x16 s[SUBS];
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub) {
+            s[sub] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < DP / 16; ++i)
+                s[sub] = mma(row_frag<T, ROW>(kb, sub, i), q[i], s[sub]);
+        }
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub)
+            add_bias<MODE>(s[sub], c, bias, pl, lane_at - segment, sub, half);
+        if (j0 + KT > end) {
+#pragma unroll
+            for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (j0 + 32 * sub + 8 * (r / 4) + 4 * half + r % 4 >= end)
+                        s[sub][r] = -INFINITY;
+        }
+        float t = s[0][0];
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                t = fmaxf(t, s[sub][r]);
+        t = half_max(t);
+        if (__any(t > top)) {
+            const float now = fmaxf(top, t);
+            const float back = exp2_fast(top - (now == -INFINITY ? 0.0f : now));
+            top = now;
+            sum *= back;
+#pragma unroll
+            for (int i = 0; i < DP / 32; ++i)
+                o[i] *= back;
+        }
+        const float m = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[sub][r] = exp2_fast(s[sub][r] - m);
+                sum += s[sub][r];
+            }
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                const frag p = acc_frag<T>(s[sub], st);
+#pragma unroll
+                for (int i = 0; i < DP / 32; ++i)
+                    o[i] = mma(col_frag<ROW>(vb, sub, st, i), p, o[i]);
+            }
+    }
+    sum = half_sum(sum);
+
+    const int64_t row = (int64_t(img) * g.heads + head) * lq + query;
+    if (f.splits > 1) {
+        const int64_t rows = int64_t(g.n) * g.heads * lq;
+        if (q_here) {
+            float *dst = f.part + (split * rows + row) * DP;
+#pragma unroll
+            for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+                for (int gq = 0; gq < 4; ++gq) {
+                    const f32x4 v = {o[i][4 * gq], o[i][4 * gq + 1], o[i][4 * gq + 2], o[i][4 * gq + 3]};
+                    *reinterpret_cast<f32x4 *>(dst + 32 * i + 8 * gq + 4 * half) = v;
+                }
+            if (half == 0) {
+                f.part_stats[(split * rows + row) * 2] = top;
+                f.part_stats[(split * rows + row) * 2 + 1] = sum;
+            }
+        }
+        return;
+    }
+    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+    const HeadMap<T, DQP> om(f.out, img, head, g.dq);
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i) {
+        o[i] *= inv;
+        om.store(query, i, half, o[i], q_here);
+    }
+    if (f.rest != nullptr && sizeof(T) == 2) {
+        const int64_t c_all = int64_t(g.heads) * g.dq;
+        const AttnMap dense{f.rest, lq * 4 * c_all, 4 * c_all, c_all, f.out.vec && g.dq % 8 == 0};
+        const HeadMap<T, DQP> rm(dense, img, head, g.dq);
+#pragma unroll
+        for (int i = 0; i < DP / 32; ++i) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                o[i][r] -= float(T(o[i][r]));
+            rm.store(query, i, half, o[i], q_here);
+        }
+    }
+    if (f.stats != nullptr && half == 0 && q_here) {
+        f.stats[2 * row] = top == -INFINITY ? 0.0f : top;
+        f.stats[2 * row + 1] = sum;
+    }
+}
+
+// The splits' partial results joined: one thread per 8 reals of a row.
+template <typename T, int DQP>
+__global__ void __launch_bounds__(256) attention_join_kernel(Forward f)
+{
+    constexpr int DP = 4 * DQP, kChunks = DP / 8;
+    const AttnGeom &g = f.a.g;
+    const int lq = g.lq();
+    const int64_t rows = int64_t(g.n) * g.heads * lq;
+    const int64_t id = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    const int64_t row = id / kChunks;
+    const int d = 8 * int(id % kChunks);
+    if (row >= rows)
+        return;
+    float top = -INFINITY;
+    for (int s = 0; s < f.splits; ++s)
+        top = fmaxf(top, f.part_stats[(s * rows + row) * 2]);
+    const float m = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f;
+    f32x8 o = 0.0f;
+    for (int s = 0; s < f.splits; ++s) {
+        const float w = exp2_fast(f.part_stats[(s * rows + row) * 2] - m);
+        sum = fmaf(w, f.part_stats[(s * rows + row) * 2 + 1], sum);
+        const f32x8 v = *reinterpret_cast<const f32x8 *>(f.part + (s * rows + row) * DP + d);
+        o += v * w;
+    }
+    o *= sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+    const int query = int(row % lq), head = int(row / lq % g.heads), img = int(row / lq / g.heads);
+    const HeadMap<T, DQP> om(f.out, img, head, g.dq);
+    store_chunk(om.at(query, d), o, om.valid(d, 8), om.vec);
+    if (f.rest != nullptr && sizeof(T) == 2) {
+        const int64_t c_all = int64_t(g.heads) * g.dq;
+        const AttnMap dense{f.rest, lq * 4 * c_all, 4 * c_all, c_all, f.out.vec && g.dq % 8 == 0};
+        const HeadMap<T, DQP> rm(dense, img, head, g.dq);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            o[e] -= float(T(o[e]));
+        store_chunk(rm.at(query, d), o, rm.valid(d, 8), rm.vec);
+    }
+    if (f.stats != nullptr && d == 0) {
+        f.stats[2 * row] = m;
+        f.stats[2 * row + 1] = sum;
+    }
+}
+
+// ------------------------------------------------------- one query per image
+
+// A chunk of 8 reals per lane: G = D / 8 neighbouring lanes hold a key of one
+// head for GRP of the query heads that share it, and a work-group's lanes hold
+// as many heads of a token as there are, so that they read whole rows of the
+// map.  Each such set of lanes walks over every `slots`-th key with a softmax
+// of its own; they are joined in LDS, and those of several splits of the keys
+// by attention_join_kernel.  Bound by reading keys and values once.
+struct Token {
+    int heads_per_block, slots, kv_blocks, group_blocks;
+};
+constexpr int kTokenChunk = 512;  // keys whose buckets are looked up at a time
+
+// Sum over the 4, 8 or 16 lanes of a row.
+template <int G> __device__ __forceinline__ float lanes_sum(float x)
+{
+#define QUAN_DPP_ADD(ctrl) \
+    x += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), ctrl, 0xf, 0xf, false))
+    QUAN_DPP_ADD(0xB1);  // lane ^ 1
+    QUAN_DPP_ADD(0x4E);  // lane ^ 2
+    if (G >= 8)
+        QUAN_DPP_ADD(0x141);  // 7 - lane of 8: the other four's sum
+    if (G >= 16)
+        QUAN_DPP_ADD(0x140);  // 15 - lane of 16
+#undef QUAN_DPP_ADD
+    return x;
+}
+
+template <typename T, int DQP, int GRP, bool BIAS>
+__global__ void __launch_bounds__(256) attention_token_kernel(Forward f, Token tk)
+{
+    constexpr int DP = 4 * DQP, G = DP / 8, kPairs = 256 / G, U = 4;
+    typedef typename Elem<T>::frag frag;
+    __shared__ float acc_lds[kPairs * GRP * DP];
+    __shared__ float stat_lds[kPairs * GRP * 2];
+    __shared__ int bucket[BIAS ? kTokenChunk : 1];
+    const AttnGeom &g = f.a.g;
+    const int lk = g.lk(), group = g.heads / g.kv_heads;
+    int id = blockIdx.x;
+    const int split = id % f.splits;
+    id /= f.splits;
+    const int gb = id % tk.group_blocks;
+    id /= tk.group_blocks;
+    const int kvb = id % tk.kv_blocks, img = id / tk.kv_blocks;
+    const int pair = threadIdx.x / G, d = 8 * (threadIdx.x % G);
+    const int slot = pair / tk.heads_per_block, kv_head = kvb * tk.heads_per_block + pair % tk.heads_per_block;
+    const bool active = slot < tk.slots && kv_head < g.kv_heads;
+    const int len = f.a.kv_len != nullptr ? min(max(f.a.kv_len[img], 0), lk) : lk;
+    const int first = split * f.tiles_per_split * kTokenChunk;
+    const int end = min(len, first + f.tiles_per_split * kTokenChunk);
+    const int head0 = kv_head * group + gb * GRP;  // of GRP query heads
+    const int heads_here = min(GRP, group - gb * GRP);
+
+    const HeadMap<const T, DQP> km(f.a.k, img, active ? kv_head : 0, g.dq), vm(f.a.v, img, active ? kv_head : 0, g.dq);
+    f32x8 q[GRP], o[GRP];
+    float top[GRP], sum[GRP];
+    const float *table[GRP];
+    const float c = g.scale * kLog2e;
+#pragma unroll
+    for (int i = 0; i < GRP; ++i) {
+        const bool here = active && i < heads_here;
+        const HeadMap<const T, DQP> qm(f.a.q, img, here ? head0 + i : 0, g.dq);
+        q[i] = to_f32(qm.load(0, d, here)) * c;
+        o[i] = 0.0f;
+        top[i] = -INFINITY;
+        sum[i] = 0.0f;
+        if (BIAS)
+            table[i] = f.a.bias.table + int64_t(here ? head0 + i : 0) * f.a.bias.ny * f.a.bias.nx;
+    }
+    const int valid = active ? km.valid(d, 8) : 0;
+    int pos_y = 0, pos_x = 0;
+    if (BIAS && f.a.pos != nullptr) {
+        pos_y = f.a.pos[2 * img];
+        pos_x = f.a.pos[2 * img + 1];
+    }
+    for (int c0 = first; c0 < end; c0 += kTokenChunk) {
+        const int c1 = min(c0 + kTokenChunk, end);
+        if (BIAS) {
+            __syncthreads();  // the last chunk's buckets have been read
+            for (int j = c0 + int(threadIdx.x); j < c1; j += 256)
+                bucket[j - c0] = bucket_of(f.o, f.a.bias, place_k(f.o, j), pos_y, pos_x);
+            __syncthreads();
+        }
+        if (!active)
+            continue;
+        for (int j = c0 + slot; j < c1; j += U * tk.slots) {
+            frag k[U], v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int t = j + u * tk.slots;
+                const int n = t < c1 ? valid : 0;
+                k[u] = load_chunk<T>(n > 0 ? km.at(t, d) : km.p, n, km.vec);
+                v[u] = load_chunk<T>(n > 0 ? vm.at(t, d) : vm.p, n, vm.vec);
+            }
+            float s[U][GRP];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const f32x8 kf = to_f32(k[u]);
+#pragma unroll
+                for (int i = 0; i < GRP; ++i) {
+                    float x = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        x = fmaf(kf[e], q[i][e], x);
+                    s[u][i] = lanes_sum<G>(x);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int t = j + u * tk.slots;
+                const int b = BIAS ? bucket[min(t, c1 - 1) - c0] : 0;
+#pragma unroll
+                for (int i = 0; i < GRP; ++i) {
+                    if (BIAS)
+                        s[u][i] += in_log2(table[i][b]);
+                    if (t >= c1)
+                        s[u][i] = -INFINITY;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < GRP; ++i) {
+                float now = top[i];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    now = fmaxf(now, s[u][i]);
+                const float m = now == -INFINITY ? 0.0f : now;
+                const float back = exp2_fast(top[i] - m);
+                top[i] = now;
+                sum[i] *= back;
+                o[i] *= back;
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    s[u][i] = exp2_fast(s[u][i] - m);
+                    sum[i] += s[u][i];
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const f32x8 vf = to_f32(v[u]);
+#pragma unroll
+                for (int i = 0; i < GRP; ++i)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        o[i][e] = fmaf(s[u][i], vf[e], o[i][e]);
+            }
+        }
+    }
+    // the slots' results joined, a thread per real of a head
+#pragma unroll
+    for (int i = 0; i < GRP; ++i) {
+        const int at = pair * GRP + i;
+        *reinterpret_cast<f32x8 *>(acc_lds + at * DP + d) = o[i];
+        if (d == 0) {
+            stat_lds[2 * at] = top[i];
+            stat_lds[2 * at + 1] = sum[i];
+        }
+    }
+    __syncthreads();
+    const int64_t rows = int64_t(g.n) * g.heads;
+    for (int e = threadIdx.x; e < tk.heads_per_block * GRP * DP; e += 256) {
+        const int real = e % DP, i = e / DP % GRP, h = e / DP / GRP;
+        const int kvh = kvb * tk.heads_per_block + h, head = kvh * group + gb * GRP + i;
+        if (kvh >= g.kv_heads || i >= heads_here)
+            continue;
+        float m = -INFINITY;
+        for (int w = 0; w < tk.slots; ++w)
+            m = fmaxf(m, stat_lds[2 * ((w * tk.heads_per_block + h) * GRP + i)]);
+        const float base = m == -INFINITY ? 0.0f : m;
+        float total = 0.0f, value = 0.0f;
+        for (int w = 0; w < tk.slots; ++w) {
+            const int at = (w * tk.heads_per_block + h) * GRP + i;
+            const float x = exp2_fast(stat_lds[2 * at] - base);
+            total = fmaf(x, stat_lds[2 * at + 1], total);
+            value = fmaf(x, acc_lds[at * DP + real], value);
+        }
+        const int64_t row = int64_t(img) * g.heads + head;
+        if (f.splits > 1) {
+            f.part[(split * rows + row) * DP + real] = value;
+            if (real == 0) {
+                f.part_stats[(split * rows + row) * 2] = m;
+                f.part_stats[(split * rows + row) * 2 + 1] = total;
+            }
+            continue;
+        }
+        value *= total > 0.0f || total != total ? 1.0f / total : 0.0f;
+        const HeadMap<T, DQP> om(f.out, img, head, g.dq);
+        if (om.valid(real, 1) > 0) {
+            const T rounded = T(value);
+            *om.at(0, real) = rounded;
+            if (f.rest != nullptr && sizeof(T) == 2) {
+                const int64_t c_all = int64_t(g.heads) * g.dq;
+                static_cast<T *>(f.rest)[(int64_t(img) * 4 + real / DQP) * c_all + int64_t(head) * g.dq + real % DQP] =
+                    T(value - float(rounded));
+            }
+        }
+        if (f.stats != nullptr && real == 0) {
+            f.stats[2 * row] = base;
+            f.stats[2 * row + 1] = total;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------- host
+
+int padded_dq(int dq)
+{
+    return dq <= 8 ? 8 : dq <= 16 ? 16 : 32;
+}
+
+struct Plan {
+    int waves, blocks, splits, tiles_per_split, cap;
+    size_t lds;
+    Token token;  // one query
+    int grp;
+};
+
+// may_split: there is memory for partial results.
+Plan forward_plan(const AttnCall &a, DType dt, bool may_split = true)
+{
+    const AttnGeom &g = a.g;
+    const int es = dt == DType::BF16 ? 2 : 4, tile = dt == DType::BF16 ? 64 : 32, dp = 4 * padded_dq(g.dq);
+    Plan p{};
+    const int lq = g.lq();
+    if (lq == 1) {
+        // one query: heads of a token side by side, splits of whole chunks of
+        // keys until two rounds of the chip have work
+        const int pairs = 256 / (dp / 8), group = g.heads / g.kv_heads;
+        p.grp = group == 1 ? 1 : group == 2 ? 2 : 4;
+        p.token.heads_per_block = std::min(g.kv_heads, pairs);
+        p.token.slots = pairs / p.token.heads_per_block;
+        p.token.kv_blocks = (g.kv_heads + p.token.heads_per_block - 1) / p.token.heads_per_block;
+        p.token.group_blocks = (group + p.grp - 1) / p.grp;
+        p.blocks = 1;
+        const int64_t groups = int64_t(g.n) * p.token.kv_blocks * p.token.group_blocks;
+        const int chunks = (g.lk() + kTokenChunk - 1) / kTokenChunk;
+        p.splits = may_split ? int(std::max<int64_t>(1, std::min<int64_t>(1024 / groups, chunks))) : 1;
+        p.tiles_per_split = (chunks + p.splits - 1) / p.splits;
+        p.splits = (chunks + p.tiles_per_split - 1) / p.tiles_per_split;
+        return p;
+    }
+    // half work-groups where whole ones would leave half of their queries empty
+    p.waves = (lq + 63) / 64 % 2 == 1 && lq <= 320 ? 2 : 4;
+    const int queries = 32 * p.waves;
+    p.blocks = (lq + queries - 1) / queries;
+    const int64_t groups = int64_t(g.n) * g.heads * p.blocks;
+    const int tiles = (g.lk() + tile - 1) / tile;
+    // fewer work-groups than two rounds of the chip: the keys are dealt out too,
+    // four tiles at least to each
+    p.splits = 1;
+    if (groups < 256 && may_split)
+        p.splits = int(std::max<int64_t>(1, std::min<int64_t>(512 / groups, tiles / 4)));
+    p.tiles_per_split = (tiles + p.splits - 1) / p.splits;
+    p.splits = (tiles + p.tiles_per_split - 1) / p.tiles_per_split;
+    p.cap = 0;
+    if (a.bias.table != nullptr) {
+        const Offsets o = make_offsets(g);
+        // the widest range of offsets that a tile of queries and one of keys have
+        const int span_q = std::min(queries, lq) - 1 + std::min((queries - 1) / g.wq + 1, g.hq - 1) * o.skip_q;
+        const int span_k = tile + ((tile - 1) / g.wk + 1) * (g.hk > 1 ? o.skip_k : 0);
+        const int window = span_q + span_k + 5;
+        p.cap = 1024;
+        while (p.cap < window)
+            p.cap *= 2;
+        if (p.cap < o.total && p.cap < 2048)
+            p.cap = 2048;
+    }
+    p.lds = size_t(4) * tile * (dp + (es == 2 ? 8 : 4)) * es + size_t(2) * tile * 4 + size_t(p.cap) * 4;
+    return p;
+}
+
+template <typename T, int DQP, int MODE>
+hipError_t forward_launch(const Forward &f, const Plan &p, hipStream_t s)
+{
+    const AttnGeom &g = f.a.g;
+    const unsigned grid = xcd_grid(int64_t(g.n) * g.heads * p.splits * p.blocks);
+    if (p.waves == 4)
+        attention_forward_kernel<T, DQP, MODE, 4><<<grid, 256, p.lds, s>>>(f);
+    else
+        attention_forward_kernel<T, DQP, MODE, 2><<<grid, 128, p.lds, s>>>(f);
+    if (hipError_t e = hipGetLastError())
+        return e;
+    if (p.splits > 1) {
+        const int64_t threads = int64_t(g.n) * g.heads * g.lq() * (DQP / 2);
+        attention_join_kernel<T, DQP><<<unsigned((threads + 255) / 256), 256, 0, s>>>(f);
+    }
+    return hipGetLastError();
+}
+template <typename T, int DQP, int GRP> hipError_t token_launch(const Forward &f, const Plan &p, hipStream_t s)
+{
+    const AttnGeom &g = f.a.g;
+    const unsigned grid = unsigned(int64_t(g.n) * p.token.kv_blocks * p.token.group_blocks * p.splits);
+    if (f.a.bias.table != nullptr)
+        attention_token_kernel<T, DQP, GRP, true><<<grid, 256, 0, s>>>(f, p.token);
+    else
+        attention_token_kernel<T, DQP, GRP, false><<<grid, 256, 0, s>>>(f, p.token);
+    if (hipError_t e = hipGetLastError())
+        return e;
+    if (p.splits > 1) {
+        const int64_t threads = int64_t(g.n) * g.heads * (DQP / 2);
+        attention_join_kernel<T, DQP><<<unsigned((threads + 255) / 256), 256, 0, s>>>(f);
+    }
+    return hipGetLastError();
+}
+template <typename T, int DQP> hipError_t forward_mode(const Forward &f, const Plan &p, hipStream_t s)
+{
+    if (f.a.g.lq() == 1)
+        return p.grp == 1 ? token_launch<T, DQP, 1>(f, p, s)
+                          : p.grp == 2 ? token_launch<T, DQP, 2>(f, p, s) : token_launch<T, DQP, 4>(f, p, s);
+    if (f.a.bias.table == nullptr)
+        return forward_launch<T, DQP, 0>(f, p, s);
+    if (f.a.g.hk == 1 || f.a.g.wk % 4 == 0)
+        return forward_launch<T, DQP, 1>(f, p, s);
+    return forward_launch<T, DQP, 2>(f, p, s);
+}
+template <typename T> hipError_t forward_dq(const Forward &f, const Plan &p, hipStream_t s)
+{
+    switch (padded_dq(f.a.g.dq)) {
+    case 8:
+        return forward_mode<T, 8>(f, p, s);
+    case 16:
+        return forward_mode<T, 16>(f, p, s);
+    default:
+        return forward_mode<T, 32>(f, p, s);
+    }
+}
+
+}  // namespace
+
+size_t attention_forward_work_bytes(const AttnCall &a, DType dt)
+{
+    const Plan p = forward_plan(a, dt);
+    if (p.splits == 1)
+        return 0;
+    const size_t rows = size_t(a.g.n) * a.g.heads * a.g.lq();
+    return size_t(p.splits) * rows * (4 * padded_dq(a.g.dq) + 2) * sizeof(float);
+}
+
+hipError_t attention_forward_run(const AttnCall &a, DType dt, const AttnMap &out, void *rest, float *stats, void *work,
+                                 hipStream_t s)
+{
+    const Plan p = forward_plan(a, dt, work != nullptr);
+    Forward f;
+    f.a = a;
+    f.o = make_offsets(a.g);
+    f.o.cap = p.cap;
+    f.out = out;
+    f.rest = rest;
+    f.stats = stats;
+    f.blocks = p.blocks;
+    f.splits = p.splits;
+    f.tiles_per_split = p.tiles_per_split;
+    f.part = static_cast<float *>(work);
+    f.part_stats = f.part + (p.splits > 1 ? size_t(p.splits) * a.g.n * a.g.heads * a.g.lq() * 4 * padded_dq(a.g.dq) : 0);
+    return dt == DType::BF16 ? forward_dq<__bf16>(f, p, s) : forward_dq<float>(f, p, s);
+}
+
+}  // namespace quan

@@ -1,0 +1,368 @@
+// Device helpers shared by the attention kernels (gfx950): element types and
+// their matrix products, chunks of a head's row, tiles in LDS and the position
+// bias of a tile.
+//
+// A head's row is D = 4 DQP reals, component-major, DQP = 8, 16 or 32 the
+// quaternion channels dq of a head rounded up (the added ones are zero).
+//
+// Products are 32 x 32 tiles over 16 reals of depth.  Lane l of a wave holds
+// row (or column) l % 32 and 8 values of the depth; its accumulators are
+// column l % 32 and the rows 8 (r / 4) + 4 (l / 32) + r % 4, r < 16.  The depth
+// may be dealt to lanes in any order that both operands share, so 8
+// accumulators of a tile, r = 8 s .. 8 s + 7, are at once the operand of depths
+// 16 s + 4 (l / 32) + e % 4 + 8 (e / 4), e < 8: probabilities go from one
+// product to the next without leaving their lanes.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "gfx950_dma.h"
+#include "quan_block.h"
+
+namespace quan {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLowest = -3.402823466e38f;
+
+template <typename T> struct Elem;
+template <> struct Elem<__bf16> {
+    typedef bf16x8 frag;
+    static constexpr int kTile = 64;  // tokens of a tile in LDS
+    static constexpr int kPad = 8;    // elements between rows in LDS (16 bytes: no bank conflicts)
+};
+template <> struct Elem<float> {
+    typedef f32x8 frag;
+    static constexpr int kTile = 32;
+    static constexpr int kPad = 4;
+};
+
+__device__ __forceinline__ f32x16 mma(const bf16x8 &a, const bf16x8 &b, const f32x16 &c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+// fp32: 8 products over two reals of depth, one of each half-wave.
+__device__ __forceinline__ f32x16 mma(const f32x8 &a, const f32x8 &b, f32x16 c)
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+}
+
+template <typename T> __device__ __forceinline__ typename Elem<T>::frag to_frag(const f32x8 &v);
+template <> __device__ __forceinline__ bf16x8 to_frag<__bf16>(const f32x8 &v)
+{
+    return __builtin_convertvector(v, bf16x8);
+}
+template <> __device__ __forceinline__ f32x8 to_frag<float>(const f32x8 &v)
+{
+    return v;
+}
+__device__ __forceinline__ f32x8 to_f32(const bf16x8 &v)
+{
+    return __builtin_convertvector(v, f32x8);
+}
+__device__ __forceinline__ f32x8 to_f32(const f32x8 &v)
+{
+    return v;
+}
+
+// Accumulators 8 s .. 8 s + 7 as an operand.
+template <typename T> __device__ __forceinline__ typename Elem<T>::frag acc_frag(const f32x16 &v, int s)
+{
+    f32x8 t;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        t[e] = v[8 * s + e];
+    return to_frag<T>(t);
+}
+
+// Values of the two half-waves joined: the lane's own and lane ^ 32's.
+__device__ __forceinline__ float half_max(float x)
+{
+    const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
+}
+__device__ __forceinline__ float half_sum(float x)
+{
+    const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(w[0]) + __uint_as_float(w[1]);
+}
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    return __builtin_amdgcn_exp2f(x);
+}
+
+// 8 reals of a row that has `valid` of them from p on, zeros behind.  vec: p is
+// 16-byte aligned and valid is 0 or 8.
+template <typename T> __device__ __forceinline__ typename Elem<T>::frag load_chunk(const T *p, int valid, bool vec)
+{
+    typename Elem<T>::frag v = {};
+    if (vec) {
+        if (valid > 0)
+            v = *reinterpret_cast<const typename Elem<T>::frag *>(p);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < valid)
+                v[e] = p[e];
+    }
+    return v;
+}
+template <typename T> __device__ __forceinline__ void store_chunk(T *p, const f32x8 &v, int valid, bool vec)
+{
+    const typename Elem<T>::frag f = to_frag<T>(v);
+    if (vec) {
+        if (valid > 0)
+            *reinterpret_cast<typename Elem<T>::frag *>(p) = f;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < valid)
+                p[e] = f[e];
+    }
+}
+// 4 reals (a quad of accumulators): aligned to 4 elements where vec.
+__device__ __forceinline__ void store_quad(__bf16 *p, const f32x4 &v, int valid, bool vec)
+{
+    const bf16x4 f = __builtin_convertvector(v, bf16x4);
+    if (vec) {
+        if (valid > 0)
+            *reinterpret_cast<bf16x4 *>(p) = f;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < valid)
+                p[e] = f[e];
+    }
+}
+__device__ __forceinline__ void store_quad(float *p, const f32x4 &v, int valid, bool vec)
+{
+    if (vec) {
+        if (valid > 0)
+            *reinterpret_cast<f32x4 *>(p) = v;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < valid)
+                p[e] = v[e];
+    }
+}
+
+// A head of one image in a map: element d = component * DQP + channel of a
+// token at at(token, d).
+template <typename T, int DQP> struct HeadMap {
+    T *p;
+    int64_t s_t, s_p;
+    int dq;
+    bool vec;
+    __device__ __forceinline__ HeadMap(const AttnMap &m, int64_t img, int head, int dq_)
+        : p(static_cast<T *>(const_cast<void *>(m.data)) + img * m.s_n + int64_t(head) * dq_), s_t(m.s_t), s_p(m.s_p),
+          dq(dq_), vec(m.vec)
+    {
+    }
+    __device__ __forceinline__ T *at(int64_t token, int d) const
+    {
+        return p + token * s_t + (d / DQP) * s_p + d % DQP;
+    }
+    __device__ __forceinline__ int valid(int d, int most) const { return max(0, min(most, dq - d % DQP)); }
+    __device__ __forceinline__ typename Elem<T>::frag load(int64_t token, int d, bool here) const
+    {
+        return load_chunk<T>(at(here ? token : 0, d), here ? valid(d, 8) : 0, vec);
+    }
+    // Accumulators of a D x 32 tile, transposed: column = token.
+    __device__ __forceinline__ void store(int64_t token, int tile, int half, const f32x16 &v, bool here) const
+    {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int d = 32 * tile + 8 * g + 4 * half;
+            const f32x4 q = {v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
+            if (here)
+                store_quad(at(token, d), q, valid(d, 4), vec);
+        }
+    }
+};
+
+// ------------------------------------------------------------- tiles in LDS
+
+// A tile of kTile tokens x D reals, staged by THREADS threads: fetch() loads
+// this thread's chunks of the tile at `token`, put() writes them to LDS.
+template <typename T, int DP, int THREADS> struct Stage {
+    typedef typename Elem<T>::frag frag;
+    static constexpr int kTokens = Elem<T>::kTile, kRow = DP + Elem<T>::kPad;
+    static constexpr int kChunks = DP / 8, kStep = THREADS / kChunks;
+    static constexpr int kCount = kTokens > kStep ? kTokens / kStep : 1;  // (more threads than chunks: some idle)
+    static_assert(THREADS % kChunks == 0 && kCount * kStep >= kTokens, "whole rows per step");
+    static constexpr int kElems = kTokens * kRow;
+    frag r[kCount];
+    template <int DQP> __device__ __forceinline__ void fetch(const HeadMap<const T, DQP> &m, int token, int end)
+    {
+        const int row = threadIdx.x / kChunks, d = 8 * (threadIdx.x % kChunks);
+        const int valid = m.valid(d, 8);
+        const T *p = m.at(token + row, d);  // (dereferenced below `end` only)
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) {
+            const bool here = token + row + i * kStep < end && (kStep <= kTokens || row < kTokens);
+            r[i] = load_chunk<T>(here ? p + int64_t(i * kStep) * m.s_t : m.p, here ? valid : 0, m.vec);
+        }
+    }
+    __device__ __forceinline__ void put(T *lds) const
+    {
+        const int row = threadIdx.x / kChunks, d = 8 * (threadIdx.x % kChunks);
+        if (kStep > kTokens && row >= kTokens)
+            return;
+#pragma unroll
+        for (int i = 0; i < kCount; ++i)
+            *reinterpret_cast<frag *>(lds + (row + i * kStep) * kRow + d) = r[i];
+    }
+};
+template <typename T, int DQP> struct HeadMap<const T, DQP> {
+    const T *p;
+    int64_t s_t, s_p;
+    int dq;
+    bool vec;
+    __device__ __forceinline__ HeadMap(const AttnMap &m, int64_t img, int head, int dq_)
+        : p(static_cast<const T *>(m.data) + img * m.s_n + int64_t(head) * dq_), s_t(m.s_t), s_p(m.s_p), dq(dq_),
+          vec(m.vec)
+    {
+    }
+    __device__ __forceinline__ const T *at(int64_t token, int d) const
+    {
+        return p + token * s_t + (d / DQP) * s_p + d % DQP;
+    }
+    __device__ __forceinline__ int valid(int d, int most) const { return max(0, min(most, dq - d % DQP)); }
+    __device__ __forceinline__ typename Elem<T>::frag load(int64_t token, int d, bool here) const
+    {
+        return load_chunk<T>(here ? at(token, d) : p, here ? valid(d, 8) : 0, vec);
+    }
+};
+
+// Operand whose rows are the tile's tokens (32 sub + lane % 32) and whose depth
+// is reals 16 f + 8 (lane / 32) ..+7 of a row.
+template <typename T, int ROW> __device__ __forceinline__ typename Elem<T>::frag row_frag(const T *tile, int sub, int f)
+{
+    const int lane = threadIdx.x & 63;
+    return *reinterpret_cast<const typename Elem<T>::frag *>(tile + (32 * sub + (lane & 31)) * ROW + 16 * f +
+                                                             8 * (lane >> 5));
+}
+
+// Operand whose rows are reals 32 mt + lane % 32 and whose depth is the tile's
+// tokens 32 sub + 16 s + 4 (lane / 32) + e % 4 + 8 (e / 4): acc_frag's order.
+// In bf16 four tokens of one real come from one transposing read, in which 16
+// lanes give the addresses of 4 rows of 16 reals.
+template <int ROW> __device__ __forceinline__ bf16x8 col_frag(const __bf16 *tile, int sub, int s, int mt)
+{
+    typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+    const int lane = threadIdx.x & 63, i = lane & 15;
+    const __bf16 *p = tile + (32 * sub + 16 * s + 4 * (lane >> 5) + (i >> 2)) * ROW + 32 * mt + (lane & 16) + 4 * (i & 3);
+    const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(p));
+    const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(p + 8 * ROW));
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+template <int ROW> __device__ __forceinline__ f32x8 col_frag(const float *tile, int sub, int s, int mt)
+{
+    const int lane = threadIdx.x & 63;
+    const float *p = tile + (32 * sub + 16 * s + 4 * (lane >> 5)) * ROW + 32 * mt + (lane & 31);
+    f32x8 v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        v[e] = p[((e & 3) + 8 * (e >> 2)) * ROW];
+    return v;
+}
+
+// ------------------------------------------------------- the position bias
+
+// Offsets in one number: A = place(key) - place(query) + origin with place(t)
+// = (t / w) * pitch + t % w, pitch = wk + wq - 1 and origin = place of the last
+// query, so that A / pitch and A % pitch are dy + hq - 1 and dx + wq - 1.  Of a
+// tile of queries and keys A lies in a range not much longer than the tile's
+// sides and the rows' ends between them; biases of a range (a segment) are
+// looked up once into LDS, as table * log2 e.
+struct Offsets {
+    int pitch, origin, hq1, wq1;  // hq - 1, wq - 1
+    int total;                    // A < total
+    FastDiv by_pitch, by_wq, by_wk;
+    int skip_q, skip_k;  // pitch - wq, pitch - wk
+    int cap;             // entries of a segment
+};
+inline Offsets make_offsets(const AttnGeom &g)
+{
+    Offsets o;
+    o.pitch = g.wk + g.wq - 1;
+    o.hq1 = g.hq - 1;
+    o.wq1 = g.wq - 1;
+    o.origin = o.hq1 * o.pitch + o.wq1;
+    o.total = (g.hk + g.hq - 1) * o.pitch;
+    o.by_pitch = FastDiv(o.pitch);
+    o.by_wq = FastDiv(g.wq);
+    o.by_wk = FastDiv(g.wk);
+    o.skip_q = o.pitch - g.wq;
+    o.skip_k = o.pitch - g.wk;
+    o.cap = 0;
+    return o;
+}
+__device__ __host__ __forceinline__ int host_place(int t, int w, int skip)
+{
+    return t + t / w * skip;
+}
+__device__ __forceinline__ int place_q(const Offsets &o, int t)
+{
+    return t + fast_div(t, o.by_wq) * o.skip_q;
+}
+__device__ __forceinline__ int place_k(const Offsets &o, int t)
+{
+    return t + fast_div(t, o.by_wk) * o.skip_k;
+}
+
+// Bucket (by * nx + bx) of offset A for an image whose queries start at (y, x).
+__device__ __forceinline__ int bucket_of(const Offsets &o, const AttnBias &b, int a, int y, int x)
+{
+    const int qy = fast_div(a, o.by_pitch);
+    int dy = qy - o.hq1 - y, dx = a - qy * o.pitch - o.wq1 - x;
+    dy = min(max(dy, -b.ry), b.ry);
+    dx = min(max(dx, -b.rx), b.rx);
+    const int iy = b.by != nullptr ? min(max(b.by[dy + b.ry], 0), b.ny - 1) : 0;
+    const int ix = b.bx != nullptr ? min(max(b.bx[dx + b.rx], 0), b.nx - 1) : 0;
+    return iy * b.nx + ix;
+}
+// A bias in units of log 2; finite ones stay finite, so that rows whose every
+// bias is the type's lowest value keep a softmax.
+__device__ __forceinline__ float in_log2(float t)
+{
+    const float v = t * kLog2e;
+    return fabsf(t) <= -kLowest ? fminf(fmaxf(v, kLowest), -kLowest) : v;
+}
+// Entries [first, first + count) of offsets into lds.
+__device__ __forceinline__ void stage_bias(float *lds, const Offsets &o, const AttnBias &b, const float *table,
+                                           int first, int count, int y, int x)
+{
+    for (int e = threadIdx.x; e < count; e += blockDim.x) {
+        const int a = first + e;
+        lds[e] = a < o.total ? in_log2(table[bucket_of(o, b, a, y, x)]) : 0.0f;
+    }
+}
+
+// The work-group's place among `total` in an order in which neighbours run on
+// the same XCD (work-groups go to the 8 XCDs in turn), so that those that read
+// the same keys share an L2.
+__device__ __forceinline__ int xcd_order(int total)
+{
+    const int per = (total + 7) / 8;
+    return (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+}
+inline unsigned xcd_grid(int64_t total)
+{
+    return unsigned((total + 7) / 8 * 8);
+}
+
+}  // namespace
+}  // namespace quan

@@ -9,6 +9,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <exception>
 #include <map>
 #include <mutex>
 #include <shared_mutex>
@@ -17,6 +18,7 @@
 #include <vector>
 
 #include "quan.h"
+#include "quan_block.h"
 #include "quan_launch.h"
 
 namespace {
@@ -66,7 +68,8 @@ enum Purpose {
     kIqbnMask = 8,     // sign bits of the saved ReLU output, IQBN gradient (optional)
     kConvSplit = 9,    // partial tiles of a convolution that splits K (optional)
     kConvFold = 11,    // folded maps, one per work-group (optional)
-    kConvPad = 10      // a convolution's input padded to whole chunks (optional)
+    kConvPad = 10,     // a convolution's input padded to whole chunks (optional)
+    kBlock = 12        // the attention block's row sums, offsets and partial results
 };
 
 // A call on (current device, stream).  Held from its first look at the buffers
@@ -354,6 +357,23 @@ int report(int code, const char *fmt, ...)
     va_end(ap);
     g_last_error = buf;
     return code;
+}
+
+int run_on_stream(void *stream, size_t bytes, bool optional, hipError_t (*launch)(void *, void *, hipStream_t),
+                  void *args, const char *what)
+{
+    try {
+        const StreamCall call(stream);
+        void *work = nullptr;
+        if (optional)
+            work = bytes > 0 ? optional_workspace(call, kBlock, bytes) : nullptr;
+        else if (int rc = workspace(call, kBlock, bytes, &work))
+            return rc;
+        const hipError_t e = launch(args, work, static_cast<hipStream_t>(stream));
+        return e == hipSuccess ? QUAN_OK : fail_hip(e, what);
+    } catch (const std::exception &e) {
+        return fail(QUAN_ERR_NOMEM, "%s: %s", what, e.what());
+    }
 }
 
 int iqbn_validate(const void *x, const float *gamma, const float *beta, float eps, const void *out,

@@ -12,8 +12,10 @@ Quaternion feature maps are tensors of logical shape [N, 4, C, H, W]
 allocates it.
 """
 import ctypes
+import math
 import os
 import struct
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -31,6 +33,13 @@ class QuanTensor(ctypes.Structure):
     in elements) axes."""
     _fields_ = [("data", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("ndim", ctypes.c_int32),
                 ("shape", ctypes.c_int64 * 5), ("strides", ctypes.c_int64 * 5)]
+
+
+class QuanRelpos(ctypes.Structure):
+    """struct quan_relpos: the attention bias's table and bucket maps."""
+    _fields_ = [("table", ctypes.c_void_p), ("bucket_y", ctypes.c_void_p), ("bucket_x", ctypes.c_void_p),
+                ("buckets_y", ctypes.c_int32), ("buckets_x", ctypes.c_int32),
+                ("radius_y", ctypes.c_int32), ("radius_x", ctypes.c_int32)]
 
 
 _PACK_DESC = struct.Struct("=Qii10q").pack  # the fields of QuanTensor in order (no padding)
@@ -76,6 +85,14 @@ SIGNATURES = {
     "quan_iqbn_forward": (ctypes.c_int, [_vp, _vp, _vp, _f32, _vp, _vp, _vp] + [_i32] * 5 + [_vp]),
     "quan_iqbn_relu_forward": (ctypes.c_int, [_vp, _vp, _vp, _f32, _vp, _vp, _vp] + [_i32] * 5 + [_vp]),
     "quan_iqbn_forward_noalloc": (ctypes.c_int, [_vp, _vp, _vp, _f32, _vp, _vp, _vp] + [_i32] * 5 + [_vp]),
+    "quan_relpos_buckets": (ctypes.c_int, [_i32, _i32, ctypes.POINTER(ctypes.c_int32)]),
+    "quan_attention_forward": (ctypes.c_int, [_vp] * 6 + [_f32, _i32] + [_vp] * 4),
+    "quan_attention_backward": (ctypes.c_int, [_vp] * 6 + [_f32, _i32] + [_vp] * 9),
+    "quan_rmsnorm_forward": (ctypes.c_int, [_vp] * 2 + [_f32, _vp] + [_i32] * 5 + [_vp]),
+    "quan_rmsnorm_backward": (ctypes.c_int, [_vp] * 4 + [_f32] + [_vp] * 2 + [_i32] * 5 + [_vp]),
+    "quan_residual_forward": (ctypes.c_int, [_vp] * 6 + [_f32, _vp, _f32] + [_vp] * 2 + [_i32] * 5 + [_vp]),
+    "quan_residual_backward": (ctypes.c_int, [_vp] * 8 + [_f32, _vp, _f32] + [_vp] * 6 + [_i32] * 5 + [_vp]),
+    "quan_dropout": (ctypes.c_int, [_vp, _f32, _vp, _vp] + [_i32] * 5 + [_vp]),
     "quan_last_error": (ctypes.c_char_p, []),
     "quan_release": (ctypes.c_int, []),
     "quan_version": (ctypes.c_char_p, []),
@@ -633,6 +650,281 @@ def quan_iqbn_forward_noalloc(x, gamma, beta, eps=1e-5, out=None, mean=None, var
     array (no device allocation by the call; out, mean and var must then be
     passed in for an allocation-free call).  Returns (out, mean, var)."""
     return _iqbn("quan_iqbn_forward_noalloc", x, gamma, beta, eps, out, mean, var)
+
+
+# ---------------------------------------------------- the attention block
+
+def quan_relpos_buckets(radius, buckets, device="cpu"):
+    """Bucket map int32 [2 radius + 1] of the offsets -radius..radius of one
+    axis: one bucket per offset where there are enough, else half of them for
+    each sign, the near distances one each, the others in widening steps."""
+    size = 2 * int(radius) + 1
+    host = (ctypes.c_int32 * max(size, 1))()
+    _check(load_library().quan_relpos_buckets(int(radius), int(buckets), host))
+    return torch.tensor(list(host), dtype=torch.int32, device=device)
+
+
+def _relpos(relpos, heads, device):
+    """(struct quan_relpos, table's shape) of (table, bucket_y, bucket_x)."""
+    table, by, bx = relpos
+    if table.dtype != torch.float32 or not table.is_contiguous() or table.device != device:
+        raise ValueError("relpos's table must be a contiguous float32 tensor on q's device")
+    radii, buckets = [], []
+    for name, t in (("bucket_y", by), ("bucket_x", bx)):
+        if t is None:
+            radii.append(0)
+            continue
+        if t.dtype != torch.int32 or t.dim() != 1 or t.numel() % 2 != 1 or not t.is_contiguous() or t.device != device:
+            raise ValueError(f"relpos's {name} must be a contiguous int32 tensor of odd length on q's device")
+        radii.append(t.numel() // 2)
+    if table.dim() == 3:
+        buckets = [table.shape[1], table.shape[2]]
+    elif table.dim() == 2 and by is None:
+        buckets = [1, table.shape[1]]
+    elif table.dim() == 2 and bx is None:
+        buckets = [table.shape[1], 1]
+    else:
+        raise ValueError("relpos's table must be [heads, buckets_y, buckets_x] (or [heads, buckets] with one axis's map)")
+    if table.shape[0] != heads:
+        raise ValueError("relpos's table must have a row per head")
+    return QuanRelpos(_ptr(table), _ptr(by), _ptr(bx), buckets[0], buckets[1], radii[0], radii[1]), table
+
+
+def _attention_args(q, k, v, heads, relpos, kv_len, pos, scale):
+    if q.dim() != 5 or k.dim() != 5 or v.dim() != 5:
+        raise ValueError("q, k and v must be [N, 4, C, H, W]")
+    for t in (k, v, kv_len, pos):
+        if t is not None and t.device != q.device:
+            raise ValueError("all tensors must be on q's device")
+    n = q.shape[0]
+    if kv_len is not None and (tuple(kv_len.shape) != (n,) or kv_len.dtype != torch.int32 or not kv_len.is_contiguous()):
+        raise ValueError("kv_len must be a contiguous int32 [N] tensor")
+    if pos is not None and (tuple(pos.shape) != (n, 2) or pos.dtype != torch.int32 or not pos.is_contiguous()):
+        raise ValueError("pos must be a contiguous int32 [N, 2] tensor")
+    heads = int(heads)
+    if scale is None:
+        scale = 1.0 / math.sqrt(max(1, 4 * (q.shape[2] // heads))) if heads > 0 else 1.0
+    bias, table = (None, None) if relpos is None else _relpos(relpos, heads, q.device)
+    return [describe(t) for t in (q, k, v)], bias, table, float(scale), heads
+
+
+def quan_attention_forward(q, k, v, heads, relpos=None, kv_len=None, pos=None, scale=None, out=None, save=False):
+    """Attention between the pixels of quaternion maps.
+
+    q: [N, 4, C, Hq, Wq]; k, v: [N, 4, Ckv, Hk, Wk] with Ckv = C / heads times
+    the heads of keys and values; channel slices of wider maps are taken as
+    they are.  relpos: (table, bucket_y, bucket_x), the learned bias by buckets
+    of the relative position: table float32 [heads, buckets_y, buckets_x],
+    bucket maps int32 of odd length (quan_relpos_buckets) or None for one bucket
+    along that axis.  kv_len: int32 [N], keys of each image; pos: int32 [N, 2],
+    (y, x) of query (0, 0) among the keys; scale: 1 / sqrt(4 C / heads) by
+    default.  Returns out, or with save (out, stats, rest) for
+    quan_attention_backward."""
+    lib = load_library()
+    descs, bias, _, scale, heads = _attention_args(q, k, v, heads, relpos, kv_len, pos, scale)
+    n, _, c, h, w = q.shape
+    if out is None:
+        out = empty_qmap(n, c, h, w, q.dtype, q.device)
+    elif out.dim() != 5 or out.device != q.device:
+        raise ValueError("out must be [N, 4, C, Hq, Wq] on q's device")
+    stats = rest = None
+    if save:
+        stats = torch.empty((n, heads, h * w, 2), dtype=torch.float32, device=q.device)
+        if q.dtype == torch.bfloat16:
+            rest = empty_qmap(n, c, h, w, q.dtype, q.device)
+    with _on(q.device):
+        rc = lib.quan_attention_forward(_ref(descs[0]), _ref(descs[1]), _ref(descs[2]), _ref(bias), _ptr(kv_len),
+                                        _ptr(pos), scale, heads, _ref(describe(out)), _ptr(rest), _ptr(stats),
+                                        _stream(q.device))
+    _check(rc)
+    return (out, stats, rest) if save else out
+
+
+def quan_attention_backward(q, k, v, out, stats, rest, dout, heads, relpos=None, kv_len=None, pos=None, scale=None,
+                            dq=None, dk=None, dv=None):
+    """Gradients of quan_attention_forward for dL/dout = dout, with what it
+    saved.  dq, dk, dv may be slices of one map.  Returns (dq, dk, dv, dtable),
+    dtable float32 like relpos's table (None without one)."""
+    lib = load_library()
+    descs, bias, table, scale, heads = _attention_args(q, k, v, heads, relpos, kv_len, pos, scale)
+    n, _, c, h, w = q.shape
+    if stats is None or tuple(stats.shape) != (n, heads, h * w, 2) or stats.dtype != torch.float32 \
+            or not stats.is_contiguous():
+        raise ValueError("stats must be the forward's, float32 [N, heads, Hq Wq, 2]")
+    if rest is not None and (rest.shape != q.shape or rest.dtype != q.dtype or not is_device_layout(rest)):
+        raise ValueError("rest must be the forward's, in device layout like out")
+    grads = []
+    for t, like in ((dq, q), (dk, k), (dv, v)):
+        if t is None:
+            t = empty_qmap(like.shape[0], like.shape[2], like.shape[3], like.shape[4], like.dtype, like.device)
+        grads.append(t)
+    for t in (out, stats, rest, dout, *grads):
+        if t is not None and t.device != q.device:
+            raise ValueError("all tensors must be on q's device")
+    dtable = None if table is None else torch.empty_like(table)
+    descs += [describe(t) for t in (out, dout, *grads)]
+    with _on(q.device):
+        rc = lib.quan_attention_backward(_ref(descs[0]), _ref(descs[1]), _ref(descs[2]), _ref(bias), _ptr(kv_len),
+                                         _ptr(pos), scale, heads, _ref(descs[3]), _ptr(rest), _ptr(stats),
+                                         _ref(descs[4]), _ref(descs[5]), _ref(descs[6]), _ref(descs[7]), _ptr(dtable),
+                                         _stream(q.device))
+    _check(rc)
+    return (*grads, dtable)
+
+
+def _check_map(name, t, like):
+    if not is_device_layout(t) or t.shape != like.shape or t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"{name} must be [N, 4, C, H, W] in device layout like the others")
+
+
+def _check_param(name, t, c, device):
+    if t is not None and (tuple(t.shape) != (4, c) or t.dtype != torch.float32 or not t.is_contiguous()
+                          or t.device != device):
+        raise ValueError(f"{name} must be a contiguous float32 [4, C] tensor")
+
+
+def _check_gate(name, t, like):
+    n, _, c = like.shape[:3]
+    if t is not None and (tuple(t.shape) != (n, 4, c, 1, 1) or not is_device_layout(t) or t.dtype != like.dtype
+                          or t.device != like.device):
+        raise ValueError(f"{name} must be [N, 4, C, 1, 1] in device layout like the maps")
+
+
+def _check_rng(rng, p, device):
+    if rng is None:
+        if p > 0:
+            raise ValueError("rng, an int64 tensor (seed, offset), is needed with p > 0")
+    elif tuple(rng.shape) != (2,) or rng.dtype != torch.int64 or not rng.is_contiguous() or rng.device != device:
+        raise ValueError("rng must be a contiguous int64 tensor (seed, offset) on the maps' device")
+
+
+def _like_map(t):
+    n, _, c, h, w = t.shape
+    return empty_qmap(n, c, h, w, t.dtype, t.device)
+
+
+def _first_map(name, t):
+    if not is_device_layout(t):
+        raise ValueError(f"{name} must be [N, 4, C, H, W] stored channels-last by component")
+    return t.shape
+
+
+def quan_rmsnorm_forward(x, gamma, eps=1e-6, out=None):
+    """The norm of a pixel's 4 C reals: gamma x / sqrt(mean(x^2) + eps)."""
+    lib = load_library()
+    n, _, c, h, w = _first_map("x", x)
+    if out is None:
+        out = _like_map(x)
+    _check_map("out", out, x)
+    _check_param("gamma", gamma, c, x.device)
+    with _on(x.device):
+        rc = lib.quan_rmsnorm_forward(_ptr(x), _ptr(gamma), float(eps), _ptr(out), n, c, h, w, _dtype_code(x),
+                                      _stream(x.device))
+    _check(rc)
+    return out
+
+
+def quan_rmsnorm_backward(x, dout, gamma, dres=None, eps=1e-6, dx=None):
+    """Gradients of quan_rmsnorm_forward; dres, a gradient that reaches x past
+    the norm, is added to dx.  Returns (dx, dgamma)."""
+    lib = load_library()
+    n, _, c, h, w = _first_map("x", x)
+    if dx is None:
+        dx = _like_map(x)
+    for name, t in (("dout", dout), ("dx", dx)) + ((("dres", dres),) if dres is not None else ()):
+        _check_map(name, t, x)
+    _check_param("gamma", gamma, c, x.device)
+    dgamma = torch.empty((4, c), dtype=torch.float32, device=x.device)
+    with _on(x.device):
+        rc = lib.quan_rmsnorm_backward(_ptr(x), _ptr(dout), _ptr(gamma), _ptr(dres), float(eps), _ptr(dx),
+                                       _ptr(dgamma), n, c, h, w, _dtype_code(x), _stream(x.device))
+    _check(rc)
+    return dx, dgamma
+
+
+def quan_residual_forward(x, y, gamma=None, gate=None, scale=None, next_gamma=None, p=0.0, rng=None, eps=1e-6,
+                          out=None, h=None):
+    """A block's residual step: out = x + scale gate dropout(norm(y) gamma) and
+    h = norm(out) next_gamma, the norms over a pixel's 4 C reals.
+
+    gate: [N, 4, C, 1, 1] like x; gamma, scale, next_gamma: float32 [4, C]; each
+    may be None (gamma None: no norm of y).  p, rng: see quan_dropout.  Returns
+    (out, h), h None without next_gamma."""
+    lib = load_library()
+    n, _, c, height, w = _first_map("x", x)
+    if out is None:
+        out = _like_map(x)
+    if next_gamma is not None and h is None:
+        h = _like_map(x)
+    if next_gamma is None and h is not None:
+        raise ValueError("h without next_gamma")
+    for name, t in (("y", y), ("out", out)) + ((("h", h),) if h is not None else ()):
+        _check_map(name, t, x)
+    for name, t in (("gamma", gamma), ("scale", scale), ("next_gamma", next_gamma)):
+        _check_param(name, t, c, x.device)
+    _check_gate("gate", gate, x)
+    _check_rng(rng, p, x.device)
+    with _on(x.device):
+        rc = lib.quan_residual_forward(_ptr(x), _ptr(y), _ptr(gate), _ptr(gamma), _ptr(scale), _ptr(next_gamma),
+                                       float(p), _ptr(rng), float(eps), _ptr(out), _ptr(h), n, c, height, w,
+                                       _dtype_code(x), _stream(x.device))
+    _check(rc)
+    return out, h
+
+
+class ResidualGradients(NamedTuple):
+    """Of quan_residual_forward's inputs; None where the input was."""
+    dx: torch.Tensor
+    dy: torch.Tensor
+    dgamma: Optional[torch.Tensor]
+    dgate: Optional[torch.Tensor]
+    dscale: Optional[torch.Tensor]
+    dnext_gamma: Optional[torch.Tensor]
+
+
+def quan_residual_backward(y, dout, gamma=None, gate=None, scale=None, next_gamma=None, out=None, dh=None, p=0.0,
+                           rng=None, eps=1e-6, dx=None, dy=None):
+    """Gradients of quan_residual_forward for dL/dout = dout and dL/dh = dh (out
+    and dh with next_gamma), the dropout's mask computed anew from the same p
+    and rng.  Returns ResidualGradients."""
+    lib = load_library()
+    n, _, c, h, w = _first_map("y", y)
+    if (next_gamma is None) != (out is None) or (next_gamma is None) != (dh is None):
+        raise ValueError("out, dh and next_gamma come together")
+    dx = _like_map(y) if dx is None else dx
+    dy = _like_map(y) if dy is None else dy
+    for name, t in (("dout", dout), ("out", out), ("dh", dh), ("dx", dx), ("dy", dy)):
+        if t is not None:
+            _check_map(name, t, y)
+    for name, t in (("gamma", gamma), ("scale", scale), ("next_gamma", next_gamma)):
+        _check_param(name, t, c, y.device)
+    _check_gate("gate", gate, y)
+    _check_rng(rng, p, y.device)
+    dgamma, dscale, dnext = (None if t is None else torch.empty((4, c), dtype=torch.float32, device=y.device)
+                             for t in (gamma, scale, next_gamma))
+    dgate = None if gate is None else empty_qmap(n, c, 1, 1, y.dtype, y.device)
+    with _on(y.device):
+        rc = lib.quan_residual_backward(_ptr(y), _ptr(dout), _ptr(out), _ptr(dh), _ptr(gate), _ptr(gamma),
+                                        _ptr(scale), _ptr(next_gamma), float(p), _ptr(rng), float(eps), _ptr(dx),
+                                        _ptr(dy), _ptr(dgate), _ptr(dgamma), _ptr(dscale), _ptr(dnext), n, c, h, w,
+                                        _dtype_code(y), _stream(y.device))
+    _check(rc)
+    return ResidualGradients(dx, dy, dgamma, dgate, dscale, dnext)
+
+
+def quan_dropout(x, p, rng=None, out=None):
+    """Dropout with a mask computed from rng = (seed, offset), an int64 tensor
+    on the device; the same call on a gradient is its backward pass."""
+    lib = load_library()
+    n, _, c, h, w = _first_map("x", x)
+    if out is None:
+        out = _like_map(x)
+    _check_map("out", out, x)
+    _check_rng(rng, p, x.device)
+    with _on(x.device):
+        rc = lib.quan_dropout(_ptr(x), float(p), _ptr(rng), _ptr(out), n, c, h, w, _dtype_code(x), _stream(x.device))
+    _check(rc)
+    return out
 
 
 def quan_last_error() -> str:
