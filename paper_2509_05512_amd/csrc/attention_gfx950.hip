@@ -112,6 +112,11 @@ __global__ void __launch_bounds__(64 * NW) attention_forward_kernel(Forward f)
     }
     const int high = MODE != 0 ? high_q + place_k(f.o, max(end, 1) - 1) + 4 : 0;  // past the last offset
 
+    // A training step's bf16 probabilities meet v in two parts, the rounded one
+    // and what it leaves: the gradient of the bias, which is fp32, goes by the
+    // rows' sums of dout out, and with probabilities of 8 bits alone it had
+    // 3e-4 of its norm wrong.
+    const bool exact = sizeof(T) == 2 && f.rest != nullptr;
     Tile kt, vt;
     if (first < end) {
         kt.fetch(km, first, end);
@@ -190,6 +195,12 @@ __global__ void __launch_bounds__(64 * NW) attention_forward_kernel(Forward f)
 #pragma unroll
                 for (int i = 0; i < DP / 32; ++i)
                     o[i] = mma(col_frag<ROW>(vb, sub, st, i), p, o[i]);
+                if (exact) {
+                    const frag r = rest_frag<T>(s[sub], st, p);
+#pragma unroll
+                    for (int i = 0; i < DP / 32; ++i)
+                        o[i] = mma(col_frag<ROW>(vb, sub, st, i), r, o[i]);
+                }
             }
     }
     sum = half_sum(sum);

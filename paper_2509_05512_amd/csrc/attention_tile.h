@@ -86,6 +86,18 @@ template <typename T> __device__ __forceinline__ typename Elem<T>::frag acc_frag
     return to_frag<T>(t);
 }
 
+// What the rounding of accumulators 8 s .. 8 s + 7 to `rounded` left.
+template <typename T>
+__device__ __forceinline__ typename Elem<T>::frag rest_frag(const f32x16 &v, int s, const typename Elem<T>::frag &rounded)
+{
+    const f32x8 r = to_f32(rounded);
+    f32x8 t;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        t[e] = v[8 * s + e] - r[e];
+    return to_frag<T>(t);
+}
+
 // Values of the two half-waves joined: the lane's own and lane ^ 32's.
 __device__ __forceinline__ float half_max(float x)
 {
