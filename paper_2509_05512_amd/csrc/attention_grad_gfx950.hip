@@ -30,12 +30,61 @@ struct Backward {
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves, kQueries = 32 * kWaves;
 
-// The launch of the queries' side.  The sums of dS by offset are gathered in
-// LDS, one array per wave (a wave's additions have a fixed order) over the
-// segment whose biases are staged: lanes of one addition hold neighbouring
-// queries and the same key, so their offsets differ and lie side by side.  As
-// the walk leaves a segment its sums go, over the waves, to the work-group's
-// own row of `offsets`.
+// Sums of dS by offset in 64-bit fixed point: integer additions in LDS take 7
+// clocks a wave where those of floats take 194 (measured), and their order
+// changes nothing.  Each wave has an array of its own in units of 2^-k, k so
+// that its largest term so far lies below 2^kSumTop: 128 terms of an offset
+// (one per query) stay below 2^62, and a term's last place is 2^-31 of the
+// first tile's largest or less.  A term that is larger takes the array to
+// coarser units.  What rows with NaN or infinity give is NaN.
+constexpr int kSumFirst = 44, kSumTop = 54;
+struct FixedSums {
+    long long *sums;
+    int k;        // 127: nothing added yet
+    float limit;  // terms below it fit: 2^(kSumTop - k)
+    float unit;   // 2^(k - 32)
+    bool bad;
+    __device__ __forceinline__ void start(long long *array, bool bad_)
+    {
+        sums = array;
+        bad = bad_;
+        k = 127;
+        limit = 0.0f;
+        unit = 0.0f;
+    }
+    // Units for a wave whose largest term is `most`, the array's entries shifted.
+    __device__ __forceinline__ void rescale(float most, int entries)
+    {
+        for (int m = 1; m < 64; m <<= 1)
+            most = fmaxf(most, __shfl_xor(most, m, 64));
+        if (!(most <= -kLowest)) {
+            bad = true;
+            limit = INFINITY;
+            return;
+        }
+        int e = 0;
+        (void)frexpf(most, &e);  // most < 2^e
+        const int now = min(kSumFirst - e, 126);
+        if (k != 127)
+            for (int i = threadIdx.x & 63; i < entries; i += 64)
+                sums[i] >>= min(k - now, 63);
+        k = now;
+        limit = ldexpf(1.0f, kSumTop - k);
+        unit = ldexpf(1.0f, k - 32);
+    }
+    __device__ __forceinline__ void add(int at, float v) const
+    {
+        const float t = v * unit, whole = floorf(t);
+        const unsigned low = unsigned((t - whole) * 4294967296.0f);
+        const unsigned long long term = (unsigned long long)(unsigned)(int(whole)) << 32 | low;
+        __hip_atomic_fetch_add(reinterpret_cast<unsigned long long *>(sums) + at, term, __ATOMIC_RELAXED,
+                               __HIP_MEMORY_SCOPE_WORKGROUP);
+    }
+};
+
+// The launch of the queries' side.  Sums of dS by offset are gathered over the
+// segment whose biases are staged; as the walk leaves it they go, over the
+// waves, to the work-group's own row of `offsets`.
 template <typename T, int DQP, int MODE>
 __global__ void __launch_bounds__(kThreads) attention_dq_kernel(Backward f)
 {
@@ -47,7 +96,8 @@ __global__ void __launch_bounds__(kThreads) attention_dq_kernel(Backward f)
     T *k_lds = reinterpret_cast<T *>(lds_raw), *v_lds = k_lds + 2 * Tile::kElems;
     int *place = reinterpret_cast<int *>(v_lds + 2 * Tile::kElems);
     float *bias = reinterpret_cast<float *>(place + 2 * KT);
-    float *sums = bias + f.o.cap;
+    long long *sums = reinterpret_cast<long long *>(bias + f.o.cap);
+    __shared__ int sum_units[kWaves];
 
     const AttnGeom &g = f.a.g;
     const int lq = g.lq(), lk = g.lk();
@@ -113,7 +163,8 @@ __global__ void __launch_bounds__(kThreads) attention_dq_kernel(Backward f)
         done = low_q;
     }
     const int past = MODE != 0 ? high_q + place_k(f.o, lk - 1) + 1 : 0;  // past the last offset
-    float *my_sums = sums + wave * f.o.cap;
+    FixedSums my_sums;
+    my_sums.start(sums + wave * f.o.cap, __any(!(fabsf(delta) <= -kLowest) || !(sum <= -kLowest)));
     // The segment's sums over the waves, added to the entries that an earlier
     // one has written; a thread has the same entries modulo kThreads of every
     // segment.
@@ -124,11 +175,13 @@ __global__ void __launch_bounds__(kThreads) attention_dq_kernel(Backward f)
             a += kThreads;
         for (; a < last; a += kThreads) {
             const int e = a - segment;
-            float v = 0.0f;
+            double v = 0.0;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w)
-                v += sums[w * f.o.cap + e];
-            offsets[a] = a < done ? offsets[a] + v : v;
+            for (int w = 0; w < kWaves; ++w) {
+                const int k = sum_units[w];
+                v += k == 128 ? double(NAN) : k == 127 ? 0.0 : ldexp(double(sums[w * f.o.cap + e]), -k);
+            }
+            offsets[a] = a < done ? offsets[a] + float(v) : float(v);
         }
         done = max(done, last);
     };
@@ -154,6 +207,8 @@ __global__ void __launch_bounds__(kThreads) attention_dq_kernel(Backward f)
             const int lo = low_q + place_k(f.o, j0), hi = high_q + place_k(f.o, min(j0 + KT, lk) - 1) + 3;
             if (segment < 0 || hi >= segment + f.o.cap) {
                 if (segment >= 0) {
+                    if (lane == 0)
+                        sum_units[wave] = my_sums.bad ? 128 : my_sums.k;
                     __syncthreads();  // the last segment has been read and added to
                     if (offsets != nullptr)
                         flush();
@@ -163,7 +218,7 @@ __global__ void __launch_bounds__(kThreads) attention_dq_kernel(Backward f)
                 stage_bias(bias, f.o, f.a.bias, table, segment, f.o.cap, pos_y, pos_x);
                 if (offsets != nullptr)
                     for (int e = threadIdx.x; e < kWaves * f.o.cap; e += kThreads)
-                        sums[e] = 0.0f;
+                        sums[e] = 0;
             }
         }
         __syncthreads();
@@ -201,8 +256,30 @@ __global__ void __launch_bounds__(kThreads) attention_dq_kernel(Backward f)
                     if (j0 + KT > end && j0 + first + t >= end)
                         p = 0.0f;
                     s[r] = p * fmaf(dp[r], inv, shift);
-                    if (MODE != 0 && offsets != nullptr)
-                        unsafeAtomicAdd(my_sums + at + p4[t], s[r]);
+                }
+            }
+            if (MODE != 0 && offsets != nullptr) {
+                float most = 0.0f;
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    most = fmaxf(most, fabsf(s[r]));
+                if (__any(!(most < my_sums.limit)))
+                    my_sums.rescale(most, f.o.cap);
+                if (!my_sums.bad) {
+#pragma unroll
+                    for (int gq = 0; gq < 4; ++gq) {
+                        const int first = 32 * sub + 8 * gq + 4 * half;
+                        i32x4 p4 = 0;
+                        if (MODE == 1) {
+                            const int p0 = pl[first];
+                            p4 = i32x4{p0, p0 + 1, p0 + 2, p0 + 3};
+                        } else {
+                            p4 = *reinterpret_cast<const i32x4 *>(pl + first);
+                        }
+#pragma unroll
+                        for (int t = 0; t < 4; ++t)
+                            my_sums.add(at + p4[t], s[4 * gq + t]);
+                    }
                 }
             }
 #pragma unroll
@@ -222,6 +299,8 @@ __global__ void __launch_bounds__(kThreads) attention_dq_kernel(Backward f)
     }
     if (MODE != 0 && offsets != nullptr) {
         if (segment >= 0) {
+            if (lane == 0)
+                sum_units[wave] = my_sums.bad ? 128 : my_sums.k;
             __syncthreads();
             flush();
         }
@@ -483,14 +562,11 @@ Plan backward_plan(const AttnCall &a, DType dt, bool table)
     if (a.bias.table != nullptr) {
         const Offsets o = make_offsets(g);
         auto span = [](int count, int w, int h, int skip) { return count + std::min((count - 1) / w + 1, h - 1) * skip; };
-        // a segment holds the widest tile's offsets; where that leaves room for
-        // few tiles more, twice that
+        // a segment holds the widest tile's offsets
         auto cap = [&](int window) {
             int c = 1024;
             while (c < window)
                 c *= 2;
-            if (c < o.total && c < 2 * window && c < 2048)
-                c = 2048;
             return c;
         };
         const int block_q = span(std::min(kQueries, lq), g.wq, g.hq, o.skip_q);
@@ -505,7 +581,7 @@ Plan backward_plan(const AttnCall &a, DType dt, bool table)
         }
     }
     const size_t tiles = size_t(4) * tile * (dp + (es == 2 ? 8 : 4)) * es + size_t(2) * tile * 4;
-    p.q_lds = tiles + size_t(p.q_cap) * 4 * (table && a.bias.table != nullptr ? 1 + kWaves : 1);
+    p.q_lds = tiles + size_t(p.q_cap) * 4 * (table && a.bias.table != nullptr ? 1 + 2 * kWaves : 1);
     p.k_lds = tiles + size_t(6) * tile * 4 + size_t(p.k_cap) * 4;
     return p;
 }
