@@ -25,34 +25,8 @@ struct Forward {
     float *part, *part_stats;             // [split][row][D], [split][row][2] (splits > 1)
 };
 
-// The scores of two half-waves' quads with their bias.  MODE 0: no bias; 1: 4
-// keys of a quad lie in one row of the map; 2: any.
-template <int MODE>
-__device__ __forceinline__ void add_bias(f32x16 &s, float c, const float *bias, const int *place, int at, int sub,
-                                         int half)
-{
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-        if (MODE == 0) {
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-                s[4 * g + t] *= c;
-        } else if (MODE == 1) {
-            const float *b = bias + at + place[32 * sub + 8 * g + 4 * half];
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-                s[4 * g + t] = fmaf(s[4 * g + t], c, b[t]);
-        } else {
-            const i32x4 p = *reinterpret_cast<const i32x4 *>(place + 32 * sub + 8 * g + 4 * half);
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-                s[4 * g + t] = fmaf(s[4 * g + t], c, bias[at + p[t]]);
-        }
-    }
-}
-
 template <typename T, int DQP, int MODE, int NW>
-__global__ void __launch_bounds__(64 * NW) attention_forward_kernel(Forward f)
+__global__ void __launch_bounds__(64 * NW, DQP <= 16 ? 2 : 1) attention_forward_kernel(Forward f)
 {
     constexpr int DP = 4 * DQP, kThreads = 64 * NW, kQueries = 32 * NW;
     typedef Stage<T, DP, kThreads> Tile;
@@ -154,15 +128,9 @@ __global__ void __launch_bounds__(64 * NW) attention_forward_kernel(Forward f)
         }
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub)
-            add_bias<MODE>(s[sub], c, bias, pl, lane_at - segment, sub, half);
-        if (j0 + KT > end) {
-#pragma unroll
-            for (int sub = 0; sub < SUBS; ++sub)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (j0 + 32 * sub + 8 * (r / 4) + 4 * half + r % 4 >= end)
-                        s[sub][r] = -INFINITY;
-        }
+            add_bias<MODE, 1>(s[sub], c, bias, pl, lane_at - segment, sub, half);
+        if (j0 + KT > end)
+            clear_behind(s, j0, end, half, -INFINITY);
         float t = s[0][0];
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub)

@@ -33,60 +33,54 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves, kQueries = 32 * kWaves;
 // Sums of dS by offset in 64-bit fixed point: integer additions in LDS take 7
 // clocks a wave where those of floats take 194 (measured), and their order
 // changes nothing.  Each wave has an array of its own in units of 2^-k, k so
-// that its largest term so far lies below 2^kSumTop: 128 terms of an offset
-// (one per query) stay below 2^62, and a term's last place is 2^-31 of the
-// first tile's largest or less.  A term that is larger takes the array to
+// that its largest term so far lies below 2^kSumTop (an offset has one term per
+// query, 32 of a wave, so sums stay below 2^55), and a term's last place is
+// 2^-40 of the first tile's largest or less.  A larger term takes the array to
 // coarser units.  What rows with NaN or infinity give is NaN.
-constexpr int kSumFirst = 44, kSumTop = 54;
+constexpr int kSumFirst = 40, kSumTop = 50;
 struct FixedSums {
-    long long *sums;
-    int k;        // 127: nothing added yet
-    float limit;  // terms below it fit: 2^(kSumTop - k)
-    float unit;   // 2^(k - 32)
+    int k;         // 127: nothing added yet
+    float limit;   // terms below it fit: 2^(kSumTop - k)
+    double scale;  // 2^k
     bool bad;
-    __device__ __forceinline__ void start(long long *array, bool bad_)
-    {
-        sums = array;
-        bad = bad_;
-        k = 127;
-        limit = 0.0f;
-        unit = 0.0f;
-    }
-    // Units for a wave whose largest term is `most`, the array's entries shifted.
-    __device__ __forceinline__ void rescale(float most, int entries)
-    {
-        for (int m = 1; m < 64; m <<= 1)
-            most = fmaxf(most, __shfl_xor(most, m, 64));
-        if (!(most <= -kLowest)) {
-            bad = true;
-            limit = INFINITY;
-            return;
-        }
-        int e = 0;
-        (void)frexpf(most, &e);  // most < 2^e
-        const int now = min(kSumFirst - e, 126);
-        if (k != 127)
-            for (int i = threadIdx.x & 63; i < entries; i += 64)
-                sums[i] >>= min(k - now, 63);
-        k = now;
-        limit = ldexpf(1.0f, kSumTop - k);
-        unit = ldexpf(1.0f, k - 32);
-    }
-    __device__ __forceinline__ void add(int at, float v) const
-    {
-        const float t = v * unit, whole = floorf(t);
-        const unsigned low = unsigned((t - whole) * 4294967296.0f);
-        const unsigned long long term = (unsigned long long)(unsigned)(int(whole)) << 32 | low;
-        __hip_atomic_fetch_add(reinterpret_cast<unsigned long long *>(sums) + at, term, __ATOMIC_RELAXED,
-                               __HIP_MEMORY_SCOPE_WORKGROUP);
-    }
 };
+constexpr double kRound = 6755399441055744.0;  // 1.5 * 2^52: to add it rounds to an integer in the low bits
+// Units for a wave whose largest term is `most`, the array's entries shifted.
+// (Not inlined: it runs a few times per launch.)
+__device__ __attribute__((noinline)) FixedSums rescaled(FixedSums f, long long *sums, float most, int entries)
+{
+    for (int m = 1; m < 64; m <<= 1)
+        most = fmaxf(most, __shfl_xor(most, m, 64));
+    if (!(most <= -kLowest)) {
+        f.bad = true;
+        f.limit = INFINITY;
+        f.scale = 0.0;
+        return f;
+    }
+    int e = 0;
+    (void)frexpf(most, &e);  // most < 2^e
+    const int now = min(kSumFirst - e, 126);
+    if (f.k != 127)
+        for (int i = threadIdx.x & 63; i < entries; i += 64)
+            sums[i] >>= min(f.k - now, 63);
+    f.k = now;
+    f.limit = ldexpf(1.0f, kSumTop - now);
+    f.scale = ldexp(1.0, now);
+    return f;
+}
+__device__ __forceinline__ void add_fixed(long long *entry, float v, double scale)
+{
+    const double t = fma(double(v), scale, kRound);
+    const long long term = __builtin_bit_cast(long long, t) - __builtin_bit_cast(long long, kRound);
+    __hip_atomic_fetch_add(reinterpret_cast<unsigned long long *>(entry), (unsigned long long)term, __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_WORKGROUP);
+}
 
 // The launch of the queries' side.  Sums of dS by offset are gathered over the
 // segment whose biases are staged; as the walk leaves it they go, over the
 // waves, to the work-group's own row of `offsets`.
 template <typename T, int DQP, int MODE>
-__global__ void __launch_bounds__(kThreads) attention_dq_kernel(Backward f)
+__global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dq_kernel(Backward f)
 {
     constexpr int DP = 4 * DQP;
     typedef Stage<T, DP, kThreads> Tile;
@@ -163,8 +157,8 @@ __global__ void __launch_bounds__(kThreads) attention_dq_kernel(Backward f)
         done = low_q;
     }
     const int past = MODE != 0 ? high_q + place_k(f.o, lk - 1) + 1 : 0;  // past the last offset
-    FixedSums my_sums;
-    my_sums.start(sums + wave * f.o.cap, __any(!(fabsf(delta) <= -kLowest) || !(sum <= -kLowest)));
+    long long *my_array = sums + wave * f.o.cap;
+    FixedSums my_sums{127, 0.0f, 0.0, __any(!(fabsf(delta) <= -kLowest) || !(sum <= -kLowest)) != 0};
     // The segment's sums over the waves, added to the entries that an earlier
     // one has written; a thread has the same entries modulo kThreads of every
     // segment.
@@ -226,70 +220,57 @@ __global__ void __launch_bounds__(kThreads) attention_dq_kernel(Backward f)
             kt.fetch(km, j0 + KT, end);
             vt.fetch(vm, j0 + KT, end);
         }
+        f32x16 s[SUBS], dp[SUBS];
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub) {
-            f32x16 s = 0.0f, dp = 0.0f;
+            s[sub] = 0.0f;
+            dp[sub] = 0.0f;
+        }
 #pragma unroll
-            for (int i = 0; i < DP / 16; ++i)
-                s = mma(row_frag<T, ROW>(kb, sub, i), q[i], s);
+        for (int i = 0; i < DP / 16; ++i)
 #pragma unroll
-            for (int i = 0; i < DP / 16; ++i)
-                dp = mma(row_frag<T, ROW>(vb, sub, i), go[i], dp);
-            const int at = lane_at - segment;
-#pragma unroll
-            for (int gq = 0; gq < 4; ++gq) {
-                const int first = 32 * sub + 8 * gq + 4 * half;
-                i32x4 p4 = 0;
-                if (MODE == 1) {
-                    const int p0 = pl[first];
-                    p4 = i32x4{p0, p0 + 1, p0 + 2, p0 + 3};
-                } else if (MODE == 2) {
-                    p4 = *reinterpret_cast<const i32x4 *>(pl + first);
-                }
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const int r = 4 * gq + t;
-                    float x = s[r] * c;
-                    if (MODE != 0)
-                        x = fmaf(s[r], c, bias[at + p4[t]]);
-                    float p = exp2_fast(x - top);
-                    if (j0 + KT > end && j0 + first + t >= end)
-                        p = 0.0f;
-                    s[r] = p * fmaf(dp[r], inv, shift);
-                }
+            for (int sub = 0; sub < SUBS; ++sub) {
+                s[sub] = mma(row_frag<T, ROW>(kb, sub, i), q[i], s[sub]);
+                dp[sub] = mma(row_frag<T, ROW>(vb, sub, i), go[i], dp[sub]);
             }
-            if (MODE != 0 && offsets != nullptr) {
-                float most = 0.0f;
+        const int at = lane_at - segment;
+        float most = 0.0f;
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub) {
+            add_bias<MODE, 1>(s[sub], c, bias, pl, at, sub, half);
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                s[sub][r] = exp2_fast(s[sub][r] - top) * fmaf(dp[sub][r], inv, shift);
+        }
+        if (j0 + KT > end)
+            clear_behind(s, j0, end, half, 0.0f);
+        if (MODE != 0 && offsets != nullptr) {
+#pragma unroll
+            for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    most = fmaxf(most, fabsf(s[r]));
-                if (__any(!(most < my_sums.limit)))
-                    my_sums.rescale(most, f.o.cap);
-                if (!my_sums.bad) {
+                    most = fmaxf(most, fabsf(s[sub][r]));
+            if (__any(!(most < my_sums.limit)))
+                my_sums = rescaled(my_sums, my_array, most, f.o.cap);
 #pragma unroll
-                    for (int gq = 0; gq < 4; ++gq) {
-                        const int first = 32 * sub + 8 * gq + 4 * half;
-                        i32x4 p4 = 0;
-                        if (MODE == 1) {
-                            const int p0 = pl[first];
-                            p4 = i32x4{p0, p0 + 1, p0 + 2, p0 + 3};
-                        } else {
-                            p4 = *reinterpret_cast<const i32x4 *>(pl + first);
-                        }
+            for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
-                        for (int t = 0; t < 4; ++t)
-                            my_sums.add(at + p4[t], s[4 * gq + t]);
-                    }
+                for (int gq = 0; gq < 4; ++gq) {
+                    const i32x4 p4 = places<MODE>(pl, sub, gq, half);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+                        add_fixed(my_array + at + p4[t], s[sub][4 * gq + t], my_sums.scale);
                 }
-            }
+        }
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
-                const frag p = acc_frag<T>(s, st);
+                const frag p = acc_frag<T>(s[sub], st);
 #pragma unroll
                 for (int i = 0; i < DP / 32; ++i)
                     dq[i] = mma(col_frag<ROW>(kb, sub, st, i), p, dq[i]);
             }
-        }
     }
     const HeadMap<T, DQP> om(f.dq, img, head, g.dq);
 #pragma unroll
@@ -315,7 +296,7 @@ __global__ void __launch_bounds__(kThreads) attention_dq_kernel(Backward f)
 
 // The launch of the keys' side: lanes hold keys, registers queries.
 template <typename T, int DQP, int MODE>
-__global__ void __launch_bounds__(kThreads) attention_dkv_kernel(Backward f)
+__global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dkv_kernel(Backward f)
 {
     constexpr int DP = 4 * DQP;
     typedef Stage<T, DP, kThreads> Tile;
@@ -407,50 +388,48 @@ __global__ void __launch_bounds__(kThreads) attention_dkv_kernel(Backward f)
                 qt.fetch(qm, i0 - QT, lq);
                 gt.fetch(gm, i0 - QT, lq);
             }
+            f32x16 s[SUBS], dp[SUBS];
 #pragma unroll
             for (int sub = 0; sub < SUBS; ++sub) {
-                f32x16 s = 0.0f, dp = 0.0f;
+                s[sub] = 0.0f;
+                dp[sub] = 0.0f;
+            }
 #pragma unroll
-                for (int i = 0; i < DP / 16; ++i)
-                    s = mma(row_frag<T, ROW>(qb, sub, i), k[i], s);
+            for (int i = 0; i < DP / 16; ++i)
 #pragma unroll
-                for (int i = 0; i < DP / 16; ++i)
-                    dp = mma(row_frag<T, ROW>(gb, sub, i), v[i], dp);
-                const int at = lane_at - segment;
+                for (int sub = 0; sub < SUBS; ++sub) {
+                    s[sub] = mma(row_frag<T, ROW>(qb, sub, i), k[i], s[sub]);
+                    dp[sub] = mma(row_frag<T, ROW>(gb, sub, i), v[i], dp[sub]);
+                }
+#pragma unroll
+            for (int sub = 0; sub < SUBS; ++sub) {
+                add_bias<MODE, -1>(s[sub], c, bias, pl, lane_at - segment, sub, half);
 #pragma unroll
                 for (int gq = 0; gq < 4; ++gq) {
                     const int first = 32 * sub + 8 * gq + 4 * half;
                     const f32x4 top = *reinterpret_cast<const f32x4 *>(rw + first);
                     const f32x4 inv = *reinterpret_cast<const f32x4 *>(rw + QT + first);
                     const f32x4 shift = *reinterpret_cast<const f32x4 *>(rw + 2 * QT + first);
-                    i32x4 p4 = 0;
-                    if (MODE == 1) {
-                        const int p0 = pl[first];
-                        p4 = i32x4{p0, p0 + 1, p0 + 2, p0 + 3};
-                    } else if (MODE == 2) {
-                        p4 = *reinterpret_cast<const i32x4 *>(pl + first);
-                    }
 #pragma unroll
                     for (int t = 0; t < 4; ++t) {
                         const int r = 4 * gq + t;
-                        float x = s[r] * c;
-                        if (MODE != 0)
-                            x = fmaf(s[r], c, bias[max(at - p4[t], 0)]);
-                        const float p = exp2_fast(x - top[t]) * inv[t];
-                        s[r] = p;
-                        dp[r] = p * (dp[r] + shift[t]);
+                        const float p = exp2_fast(s[sub][r] - top[t]) * inv[t];
+                        s[sub][r] = p;
+                        dp[sub][r] = p * (dp[sub][r] + shift[t]);
                     }
                 }
+            }
+#pragma unroll
+            for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
                 for (int st = 0; st < 2; ++st) {
-                    const frag p = acc_frag<T>(s, st), ds = acc_frag<T>(dp, st);
+                    const frag p = acc_frag<T>(s[sub], st), ds = acc_frag<T>(dp[sub], st);
 #pragma unroll
                     for (int i = 0; i < DP / 32; ++i) {
                         dv[i] = mma(col_frag<ROW>(gb, sub, st, i), p, dv[i]);
                         dk[i] = mma(col_frag<ROW>(qb, sub, st, i), ds, dk[i]);
                     }
                 }
-            }
         }
     }
     // keys behind the image's last have no gradient

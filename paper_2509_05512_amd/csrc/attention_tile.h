@@ -114,19 +114,20 @@ __device__ __forceinline__ float exp2_fast(float x)
     return __builtin_amdgcn_exp2f(x);
 }
 
-// 8 reals of a row that has `valid` of them from p on, zeros behind.  vec: p is
-// 16-byte aligned and valid is 0 or 8.
+// 8 reals of a row that has `valid` of them from p on, zeros behind; p can be
+// read where valid is 0 too.  vec: p is 16-byte aligned and valid is 0 or 8.
 template <typename T> __device__ __forceinline__ typename Elem<T>::frag load_chunk(const T *p, int valid, bool vec)
 {
     typename Elem<T>::frag v = {};
     if (vec) {
-        if (valid > 0)
-            v = *reinterpret_cast<const typename Elem<T>::frag *>(p);
+        const typename Elem<T>::frag t = *reinterpret_cast<const typename Elem<T>::frag *>(p);
+        v = valid > 0 ? t : v;
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < valid)
-                v[e] = p[e];
+        for (int e = 0; e < 8; ++e) {
+            const T t = p[max(min(e, valid - 1), 0)];
+            v[e] = e < valid ? t : v[e];
+        }
     }
     return v;
 }
@@ -189,7 +190,8 @@ template <typename T, int DQP> struct HeadMap {
     __device__ __forceinline__ int valid(int d, int most) const { return max(0, min(most, dq - d % DQP)); }
     __device__ __forceinline__ typename Elem<T>::frag load(int64_t token, int d, bool here) const
     {
-        return load_chunk<T>(at(here ? token : 0, d), here ? valid(d, 8) : 0, vec);
+        const int n = here ? valid(d, 8) : 0;
+        return load_chunk<T>(n > 0 ? at(token, d) : p, n, vec);
     }
     // Accumulators of a D x 32 tile, transposed: column = token.
     __device__ __forceinline__ void store(int64_t token, int tile, int half, const f32x16 &v, bool here) const
@@ -219,11 +221,17 @@ template <typename T, int DP, int THREADS> struct Stage {
     template <int DQP> __device__ __forceinline__ void fetch(const HeadMap<const T, DQP> &m, int token, int end)
     {
         const int row = threadIdx.x / kChunks, d = 8 * (threadIdx.x % kChunks);
+        const T *p = m.at(token + row, d);  // (dereferenced below `end` and within the head only)
+        if (kStep <= kTokens && m.vec && m.dq == DQP && token + kTokens <= end) {  // whole tiles
+#pragma unroll
+            for (int i = 0; i < kCount; ++i)
+                r[i] = *reinterpret_cast<const frag *>(p + int64_t(i * kStep) * m.s_t);
+            return;
+        }
         const int valid = m.valid(d, 8);
-        const T *p = m.at(token + row, d);  // (dereferenced below `end` only)
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
-            const bool here = token + row + i * kStep < end && (kStep <= kTokens || row < kTokens);
+            const bool here = valid > 0 && token + row + i * kStep < end && (kStep <= kTokens || row < kTokens);
             r[i] = load_chunk<T>(here ? p + int64_t(i * kStep) * m.s_t : m.p, here ? valid : 0, m.vec);
         }
     }
@@ -254,7 +262,8 @@ template <typename T, int DQP> struct HeadMap<const T, DQP> {
     __device__ __forceinline__ int valid(int d, int most) const { return max(0, min(most, dq - d % DQP)); }
     __device__ __forceinline__ typename Elem<T>::frag load(int64_t token, int d, bool here) const
     {
-        return load_chunk<T>(here ? at(token, d) : p, here ? valid(d, 8) : 0, vec);
+        const int n = here ? valid(d, 8) : 0;
+        return load_chunk<T>(n > 0 ? at(token, d) : p, n, vec);
     }
 };
 
@@ -360,6 +369,59 @@ __device__ __forceinline__ void stage_bias(float *lds, const Offsets &o, const A
     for (int e = threadIdx.x; e < count; e += blockDim.x) {
         const int a = first + e;
         lds[e] = a < o.total ? in_log2(table[bucket_of(o, b, a, y, x)]) : 0.0f;
+    }
+}
+
+// Places of the 4 tokens of a quad of accumulators.  MODE 1: they lie in one row
+// of the map; 2: anywhere.
+template <int MODE> __device__ __forceinline__ i32x4 places(const int *place, int sub, int quad, int half)
+{
+    const int *p = place + 32 * sub + 8 * quad + 4 * half;
+    if (MODE == 2)
+        return *reinterpret_cast<const i32x4 *>(p);
+    const int p0 = MODE == 1 ? p[0] : 0;
+    return i32x4{p0, p0 + 1, p0 + 2, p0 + 3};
+}
+// Scores in units of log 2: c times the products plus the bias of the lane's
+// offset `at` + SIGN * place (MODE 0: no bias).  Behind the last token of the
+// queries' side a place may pass the lane's offset: such scores count nowhere.
+template <int MODE, int SIGN>
+__device__ __forceinline__ void add_bias(f32x16 &s, float c, const float *bias, const int *place, int at, int sub,
+                                         int half)
+{
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        if (MODE == 0) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                s[4 * g + t] *= c;
+        } else if (MODE == 1) {
+            const int p0 = place[32 * sub + 8 * g + 4 * half];
+            const float *b = bias + (SIGN > 0 ? at + p0 : max(at - p0 - 3, 0));
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                s[4 * g + t] = fmaf(s[4 * g + t], c, b[SIGN > 0 ? t : 3 - t]);
+        } else {
+            const i32x4 p = places<MODE>(place, sub, g, half);
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                s[4 * g + t] = fmaf(s[4 * g + t], c, bias[SIGN > 0 ? at + p[t] : max(at - p[t], 0)]);
+        }
+    }
+}
+// `value` in the places of a tile's tokens (rows of accumulators) at or behind
+// `end`.  The empty statements keep the compiler from doing this to every tile
+// with selects.
+template <int SUBS>
+__device__ __forceinline__ void clear_behind(f32x16 (&s)[SUBS], int first, int end, int half, float value)
+{
+#pragma unroll
+    for (int sub = 0; sub < SUBS; ++sub) {
+        asm volatile("" : "+v"(s[sub]));
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            if (first + 32 * sub + 8 * (r / 4) + 4 * half + r % 4 >= end)
+                s[sub][r] = value;
     }
 }
 
