@@ -25,13 +25,17 @@ struct Forward {
     float *part, *part_stats;             // [split][row][D], [split][row][2] (splits > 1)
 };
 
-template <typename T, int DQP, int MODE, int NW>
+// EXACT (a training step in bf16): the probabilities meet v in two parts, the
+// rounded one and what it leaves.  The gradient of the bias, which is fp32, goes
+// by the rows' sums of dout out, and with probabilities of 8 bits alone 3e-4 of
+// its norm was wrong (1e-6 with both parts).
+template <typename T, int DQP, int MODE, int NW, bool EXACT>
 __global__ void __launch_bounds__(64 * NW, DQP <= 16 ? 2 : 1) attention_forward_kernel(Forward f)
 {
     constexpr int DP = 4 * DQP, kThreads = 64 * NW, kQueries = 32 * NW;
     typedef Stage<T, DP, kThreads> Tile;
     typedef typename Elem<T>::frag frag;
-    constexpr int KT = Tile::kTokens, SUBS = KT / 32, ROW = Tile::kRow;
+    constexpr int KT = Tile::kTokens, SUBS = KT / 32;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
     T *k_lds = reinterpret_cast<T *>(lds_raw), *v_lds = k_lds + 2 * Tile::kElems;
     int *place = reinterpret_cast<int *>(v_lds + 2 * Tile::kElems);
@@ -86,11 +90,6 @@ __global__ void __launch_bounds__(64 * NW, DQP <= 16 ? 2 : 1) attention_forward_
     }
     const int high = MODE != 0 ? high_q + place_k(f.o, max(end, 1) - 1) + 4 : 0;  // past the last offset
 
-    // A training step's bf16 probabilities meet v in two parts, the rounded one
-    // and what it leaves: the gradient of the bias, which is fp32, goes by the
-    // rows' sums of dout out, and with probabilities of 8 bits alone it had
-    // 3e-4 of its norm wrong.
-    const bool exact = sizeof(T) == 2 && f.rest != nullptr;
     Tile kt, vt;
     if (first < end) {
         kt.fetch(km, first, end);
@@ -124,7 +123,7 @@ __global__ void __launch_bounds__(64 * NW, DQP <= 16 ? 2 : 1) attention_forward_
             s[sub] = 0.0f;
 #pragma unroll
             for (int i = 0; i < DP / 16; ++i)
-                s[sub] = mma(row_frag<T, ROW>(kb, sub, i), q[i], s[sub]);
+                s[sub] = mma(row_frag<T, DP>(kb, sub, i), q[i], s[sub]);
         }
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub)
@@ -162,12 +161,12 @@ __global__ void __launch_bounds__(64 * NW, DQP <= 16 ? 2 : 1) attention_forward_
                 const frag p = acc_frag<T>(s[sub], st);
 #pragma unroll
                 for (int i = 0; i < DP / 32; ++i)
-                    o[i] = mma(col_frag<ROW>(vb, sub, st, i), p, o[i]);
-                if (exact) {
+                    o[i] = mma(col_frag<DP>(vb, sub, st, i), p, o[i]);
+                if (EXACT) {
                     const frag r = rest_frag<T>(s[sub], st, p);
 #pragma unroll
                     for (int i = 0; i < DP / 32; ++i)
-                        o[i] = mma(col_frag<ROW>(vb, sub, st, i), r, o[i]);
+                        o[i] = mma(col_frag<DP>(vb, sub, st, i), r, o[i]);
                 }
             }
     }
@@ -527,7 +526,7 @@ Plan forward_plan(const AttnCall &a, DType dt, bool may_split = true)
         if (p.cap < o.total && p.cap < 2048)
             p.cap = 2048;
     }
-    p.lds = size_t(4) * tile * (dp + (es == 2 ? 8 : 4)) * es + size_t(2) * tile * 4 + size_t(p.cap) * 4;
+    p.lds = size_t(4) * tile * (dp + (es == 2 ? 0 : 4)) * es + size_t(2) * tile * 4 + size_t(p.cap) * 4;
     return p;
 }
 
@@ -536,10 +535,15 @@ hipError_t forward_launch(const Forward &f, const Plan &p, hipStream_t s)
 {
     const AttnGeom &g = f.a.g;
     const unsigned grid = xcd_grid(int64_t(g.n) * g.heads * p.splits * p.blocks);
-    if (p.waves == 4)
-        attention_forward_kernel<T, DQP, MODE, 4><<<grid, 256, p.lds, s>>>(f);
+    const bool exact = sizeof(T) == 2 && f.rest != nullptr;
+    if (p.waves == 4 && exact)
+        attention_forward_kernel<T, DQP, MODE, 4, sizeof(T) == 2><<<grid, 256, p.lds, s>>>(f);
+    else if (p.waves == 4)
+        attention_forward_kernel<T, DQP, MODE, 4, false><<<grid, 256, p.lds, s>>>(f);
+    else if (exact)
+        attention_forward_kernel<T, DQP, MODE, 2, sizeof(T) == 2><<<grid, 128, p.lds, s>>>(f);
     else
-        attention_forward_kernel<T, DQP, MODE, 2><<<grid, 128, p.lds, s>>>(f);
+        attention_forward_kernel<T, DQP, MODE, 2, false><<<grid, 128, p.lds, s>>>(f);
     if (hipError_t e = hipGetLastError())
         return e;
     if (p.splits > 1) {

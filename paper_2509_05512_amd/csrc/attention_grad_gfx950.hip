@@ -32,42 +32,16 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves, kQueries = 32 * kWaves;
 
 // Sums of dS by offset in 64-bit fixed point: integer additions in LDS take 7
 // clocks a wave where those of floats take 194 (measured), and their order
-// changes nothing.  Each wave has an array of its own in units of 2^-k, k so
-// that its largest term so far lies below 2^kSumTop (an offset has one term per
-// query, 32 of a wave, so sums stay below 2^55), and a term's last place is
-// 2^-40 of the first tile's largest or less.  A larger term takes the array to
-// coarser units.  What rows with NaN or infinity give is NaN.
-constexpr int kSumFirst = 40, kSumTop = 50;
-struct FixedSums {
-    int k;         // 127: nothing added yet
-    float limit;   // terms below it fit: 2^(kSumTop - k)
-    double scale;  // 2^k
-    bool bad;
-};
+// changes nothing, so that the waves share one array.  Its units 2^-k follow
+// from a bound of the terms known before they are: |dS| <= |dP - delta| <=
+// |dO| |v| + |delta|, with the work-group's largest |dO| and |delta| and the
+// tile's largest element of v.  k = 50 - e for a bound below 2^e: a term is
+// below 2^51, an offset's terms (one per query, 128) stay below 2^58, and a
+// term's last place is 2^-50 of the bound.  A tile with a larger bound takes the
+// array to coarser units.  What NaN or infinity is in the work-group's rows or
+// in v gives NaN.
+constexpr int kSumBits = 50, kNoUnits = 127, kBadUnits = 128;
 constexpr double kRound = 6755399441055744.0;  // 1.5 * 2^52: to add it rounds to an integer in the low bits
-// Units for a wave whose largest term is `most`, the array's entries shifted.
-// (Not inlined: it runs a few times per launch.)
-__device__ __attribute__((noinline)) FixedSums rescaled(FixedSums f, long long *sums, float most, int entries)
-{
-    for (int m = 1; m < 64; m <<= 1)
-        most = fmaxf(most, __shfl_xor(most, m, 64));
-    if (!(most <= -kLowest)) {
-        f.bad = true;
-        f.limit = INFINITY;
-        f.scale = 0.0;
-        return f;
-    }
-    int e = 0;
-    (void)frexpf(most, &e);  // most < 2^e
-    const int now = min(kSumFirst - e, 126);
-    if (f.k != 127)
-        for (int i = threadIdx.x & 63; i < entries; i += 64)
-            sums[i] >>= min(f.k - now, 63);
-    f.k = now;
-    f.limit = ldexpf(1.0f, kSumTop - now);
-    f.scale = ldexp(1.0, now);
-    return f;
-}
 __device__ __forceinline__ void add_fixed(long long *entry, float v, double scale)
 {
     const double t = fma(double(v), scale, kRound);
@@ -75,23 +49,56 @@ __device__ __forceinline__ void add_fixed(long long *entry, float v, double scal
     __hip_atomic_fetch_add(reinterpret_cast<unsigned long long *>(entry), (unsigned long long)term, __ATOMIC_RELAXED,
                            __HIP_MEMORY_SCOPE_WORKGROUP);
 }
+// The larger of two values >= 0; as unsigned numbers such floats keep their
+// order, and NaN is above infinity.
+__device__ __forceinline__ float bits_max(float a, float b)
+{
+    return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b)));
+}
+// Largest |value| of a wave, in all its lanes.
+__device__ __forceinline__ float wave_top(float x)
+{
+    unsigned v = __float_as_uint(x) & 0x7fffffffu;
+#define QUAN_DPP_MAX(ctrl) v = max(v, unsigned(__builtin_amdgcn_update_dpp(0, int(v), ctrl, 0xf, 0xf, false)))
+    QUAN_DPP_MAX(0xB1);   // lane ^ 1
+    QUAN_DPP_MAX(0x4E);   // lane ^ 2
+    QUAN_DPP_MAX(0x141);  // 7 - lane of 8
+    QUAN_DPP_MAX(0x140);  // 15 - lane of 16
+#undef QUAN_DPP_MAX
+    v = max(v, unsigned(__shfl_xor(int(v), 16, 64)));
+    v = max(v, unsigned(__shfl_xor(int(v), 32, 64)));
+    return __uint_as_float(v);
+}
+// |largest| of this thread's chunks of a tile, as wave_top takes it.
+template <typename F, int N> __device__ __forceinline__ float chunk_top(const F (&r)[N])
+{
+    unsigned v = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const f32x8 t = to_f32(r[i]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            v = max(v, __float_as_uint(t[e]) & 0x7fffffffu);
+    }
+    return __uint_as_float(v);
+}
 
 // The launch of the queries' side.  Sums of dS by offset are gathered over the
 // segment whose biases are staged; as the walk leaves it they go, over the
 // waves, to the work-group's own row of `offsets`.
 template <typename T, int DQP, int MODE>
-__global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dq_kernel(Backward f)
+__global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kernel(Backward f)
 {
     constexpr int DP = 4 * DQP;
     typedef Stage<T, DP, kThreads> Tile;
     typedef typename Elem<T>::frag frag;
-    constexpr int KT = Tile::kTokens, SUBS = KT / 32, ROW = Tile::kRow;
+    constexpr int KT = Tile::kTokens, SUBS = KT / 32;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
     T *k_lds = reinterpret_cast<T *>(lds_raw), *v_lds = k_lds + 2 * Tile::kElems;
     int *place = reinterpret_cast<int *>(v_lds + 2 * Tile::kElems);
     float *bias = reinterpret_cast<float *>(place + 2 * KT);
     long long *sums = reinterpret_cast<long long *>(bias + f.o.cap);
-    __shared__ int sum_units[kWaves];
+    __shared__ float tops[2 * kWaves];  // of a tile's v, by buffer and wave
 
     const AttnGeom &g = f.a.g;
     const int lq = g.lq(), lk = g.lk();
@@ -157,10 +164,36 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dq_kern
         done = low_q;
     }
     const int past = MODE != 0 ? high_q + place_k(f.o, lk - 1) + 1 : 0;  // past the last offset
-    long long *my_array = sums + wave * f.o.cap;
-    FixedSums my_sums{127, 0.0f, 0.0, __any(!(fabsf(delta) <= -kLowest) || !(sum <= -kLowest)) != 0};
-    // The segment's sums over the waves, added to the entries that an earlier
-    // one has written; a thread has the same entries modulo kThreads of every
+    // the bound's parts from the work-group's rows: |dO| and |delta|; a row whose
+    // sum is no number has NaN
+    float top_go = 0.0f, top_delta = 0.0f;
+    if (MODE != 0 && offsets != nullptr) {
+        float n2 = 0.0f;
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) {
+            const f32x8 w = to_f32(go[i]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                n2 = fmaf(w[e], w[e], n2);
+        }
+        top_go = wave_top(sum <= -kLowest ? sqrtf(half_sum(n2)) : NAN);
+        top_delta = wave_top(delta);
+        if (lane == 0) {
+            tops[wave] = top_go;
+            tops[kWaves + wave] = top_delta;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            top_go = bits_max(top_go, tops[w]);
+            top_delta = bits_max(top_delta, tops[kWaves + w]);
+        }
+        top_go *= sqrtf(float(DP));
+        __syncthreads();
+    }
+    int units = kNoUnits;  // k of the array's units 2^-k
+    double unit = 0.0;     // 2^k
+    // The segment's sums, added to the entries that an earlier one has written; a thread has the same entries modulo kThreads of every
     // segment.
     auto flush = [&]() {
         const int last = min(segment + f.o.cap, past);
@@ -169,13 +202,8 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dq_kern
             a += kThreads;
         for (; a < last; a += kThreads) {
             const int e = a - segment;
-            double v = 0.0;
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                const int k = sum_units[w];
-                v += k == 128 ? double(NAN) : k == 127 ? 0.0 : ldexp(double(sums[w * f.o.cap + e]), -k);
-            }
-            offsets[a] = a < done ? offsets[a] + float(v) : float(v);
+            const float v = units == kBadUnits ? NAN : units == kNoUnits ? 0.0f : float(ldexp(double(sums[e]), -units));
+            offsets[a] = a < done ? offsets[a] + v : v;
         }
         done = max(done, last);
     };
@@ -195,14 +223,17 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dq_kern
         int *pl = place + buf * KT;
         kt.put(kb);
         vt.put(vb);
+        if (MODE != 0 && offsets != nullptr) {
+            const float most = wave_top(chunk_top(vt.r));
+            if (lane == 0)
+                tops[buf * kWaves + wave] = most;
+        }
         if (MODE != 0) {
             if (threadIdx.x < KT)
                 pl[threadIdx.x] = place_k(f.o, min(j0 + int(threadIdx.x), lk - 1));
             const int lo = low_q + place_k(f.o, j0), hi = high_q + place_k(f.o, min(j0 + KT, lk) - 1) + 3;
             if (segment < 0 || hi >= segment + f.o.cap) {
                 if (segment >= 0) {
-                    if (lane == 0)
-                        sum_units[wave] = my_sums.bad ? 128 : my_sums.k;
                     __syncthreads();  // the last segment has been read and added to
                     if (offsets != nullptr)
                         flush();
@@ -211,7 +242,7 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dq_kern
                 segment = lo;
                 stage_bias(bias, f.o, f.a.bias, table, segment, f.o.cap, pos_y, pos_x);
                 if (offsets != nullptr)
-                    for (int e = threadIdx.x; e < kWaves * f.o.cap; e += kThreads)
+                    for (int e = threadIdx.x; e < f.o.cap; e += kThreads)
                         sums[e] = 0;
             }
         }
@@ -220,57 +251,63 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dq_kern
             kt.fetch(km, j0 + KT, end);
             vt.fetch(vm, j0 + KT, end);
         }
-        f32x16 s[SUBS], dp[SUBS];
+        if (MODE != 0 && offsets != nullptr) {
+            float most = 0.0f;
 #pragma unroll
-        for (int sub = 0; sub < SUBS; ++sub) {
-            s[sub] = 0.0f;
-            dp[sub] = 0.0f;
-        }
-#pragma unroll
-        for (int i = 0; i < DP / 16; ++i)
-#pragma unroll
-            for (int sub = 0; sub < SUBS; ++sub) {
-                s[sub] = mma(row_frag<T, ROW>(kb, sub, i), q[i], s[sub]);
-                dp[sub] = mma(row_frag<T, ROW>(vb, sub, i), go[i], dp[sub]);
+            for (int w = 0; w < kWaves; ++w)
+                most = bits_max(most, tops[buf * kWaves + w]);
+            most = fmaf(most, top_go, top_delta);
+            if (!(most <= -kLowest)) {
+                units = kBadUnits;
+                unit = 0.0;
+            } else if (units != kBadUnits) {
+                const int e = int(__float_as_uint(most) >> 23) - 126;  // most < 2^e
+                const int now = min(kSumBits - e, kNoUnits - 1);
+                if (now < units) {
+                    if (units != kNoUnits) {  // (what other waves add meanwhile waits for the barriers)
+                        __syncthreads();
+                        for (int i = threadIdx.x; i < f.o.cap; i += kThreads)
+                            sums[i] >>= min(units - now, 63);
+                        __syncthreads();
+                    }
+                    units = now;
+                    unit = ldexp(1.0, now);
+                }
             }
+        }
         const int at = lane_at - segment;
-        float most = 0.0f;
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub) {
-            add_bias<MODE, 1>(s[sub], c, bias, pl, at, sub, half);
+            f32x16 s[1], dp = 0.0f;
+            s[0] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < DP / 16; ++i) {
+                s[0] = mma(row_frag<T, DP>(kb, sub, i), q[i], s[0]);
+                dp = mma(row_frag<T, DP>(vb, sub, i), go[i], dp);
+            }
+            add_bias<MODE, 1>(s[0], c, bias, pl, at, sub, half);
 #pragma unroll
             for (int r = 0; r < 16; ++r)
-                s[sub][r] = exp2_fast(s[sub][r] - top) * fmaf(dp[sub][r], inv, shift);
-        }
-        if (j0 + KT > end)
-            clear_behind(s, j0, end, half, 0.0f);
-        if (MODE != 0 && offsets != nullptr) {
-#pragma unroll
-            for (int sub = 0; sub < SUBS; ++sub)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    most = fmaxf(most, fabsf(s[sub][r]));
-            if (__any(!(most < my_sums.limit)))
-                my_sums = rescaled(my_sums, my_array, most, f.o.cap);
-#pragma unroll
-            for (int sub = 0; sub < SUBS; ++sub)
+                s[0][r] = exp2_fast(s[0][r] - top) * fmaf(dp[r], inv, shift);
+            if (j0 + KT > end)
+                clear_behind(s, j0 + 32 * sub, end, half, 0.0f);
+            if (MODE != 0 && offsets != nullptr) {
 #pragma unroll
                 for (int gq = 0; gq < 4; ++gq) {
                     const i32x4 p4 = places<MODE>(pl, sub, gq, half);
 #pragma unroll
                     for (int t = 0; t < 4; ++t)
-                        add_fixed(my_array + at + p4[t], s[sub][4 * gq + t], my_sums.scale);
+                        add_fixed(sums + at + p4[t], s[0][4 * gq + t], unit);
                 }
-        }
-#pragma unroll
-        for (int sub = 0; sub < SUBS; ++sub)
+            }
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
-                const frag p = acc_frag<T>(s[sub], st);
+                const frag p = acc_frag<T>(s[0], st);
 #pragma unroll
                 for (int i = 0; i < DP / 32; ++i)
-                    dq[i] = mma(col_frag<ROW>(kb, sub, st, i), p, dq[i]);
+                    dq[i] = mma(col_frag<DP>(kb, sub, st, i), p, dq[i]);
             }
+        }
     }
     const HeadMap<T, DQP> om(f.dq, img, head, g.dq);
 #pragma unroll
@@ -280,8 +317,6 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dq_kern
     }
     if (MODE != 0 && offsets != nullptr) {
         if (segment >= 0) {
-            if (lane == 0)
-                sum_units[wave] = my_sums.bad ? 128 : my_sums.k;
             __syncthreads();
             flush();
         }
@@ -301,7 +336,7 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dkv_ker
     constexpr int DP = 4 * DQP;
     typedef Stage<T, DP, kThreads> Tile;
     typedef typename Elem<T>::frag frag;
-    constexpr int QT = Tile::kTokens, SUBS = QT / 32, ROW = Tile::kRow;
+    constexpr int QT = Tile::kTokens, SUBS = QT / 32;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
     T *q_lds = reinterpret_cast<T *>(lds_raw), *g_lds = q_lds + 2 * Tile::kElems;
     float *rows = reinterpret_cast<float *>(g_lds + 2 * Tile::kElems);  // [2][top, inv, shift][QT]
@@ -398,8 +433,8 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dkv_ker
             for (int i = 0; i < DP / 16; ++i)
 #pragma unroll
                 for (int sub = 0; sub < SUBS; ++sub) {
-                    s[sub] = mma(row_frag<T, ROW>(qb, sub, i), k[i], s[sub]);
-                    dp[sub] = mma(row_frag<T, ROW>(gb, sub, i), v[i], dp[sub]);
+                    s[sub] = mma(row_frag<T, DP>(qb, sub, i), k[i], s[sub]);
+                    dp[sub] = mma(row_frag<T, DP>(gb, sub, i), v[i], dp[sub]);
                 }
 #pragma unroll
             for (int sub = 0; sub < SUBS; ++sub) {
@@ -426,8 +461,8 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dkv_ker
                     const frag p = acc_frag<T>(s[sub], st), ds = acc_frag<T>(dp[sub], st);
 #pragma unroll
                     for (int i = 0; i < DP / 32; ++i) {
-                        dv[i] = mma(col_frag<ROW>(gb, sub, st, i), p, dv[i]);
-                        dk[i] = mma(col_frag<ROW>(qb, sub, st, i), ds, dk[i]);
+                        dv[i] = mma(col_frag<DP>(gb, sub, st, i), p, dv[i]);
+                        dk[i] = mma(col_frag<DP>(qb, sub, st, i), ds, dk[i]);
                     }
                 }
         }
@@ -559,8 +594,8 @@ Plan backward_plan(const AttnCall &a, DType dt, bool table)
             p.sum_bytes = size_t(p.slices) * g.heads * o.total * sizeof(double);
         }
     }
-    const size_t tiles = size_t(4) * tile * (dp + (es == 2 ? 8 : 4)) * es + size_t(2) * tile * 4;
-    p.q_lds = tiles + size_t(p.q_cap) * 4 * (table && a.bias.table != nullptr ? 1 + 2 * kWaves : 1);
+    const size_t tiles = size_t(4) * tile * (dp + (es == 2 ? 0 : 4)) * es + size_t(2) * tile * 4;
+    p.q_lds = tiles + size_t(p.q_cap) * 4 * (table && a.bias.table != nullptr ? 3 : 1);
     p.k_lds = tiles + size_t(6) * tile * 4 + size_t(p.k_cap) * 4;
     return p;
 }

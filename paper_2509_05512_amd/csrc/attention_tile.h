@@ -37,12 +37,10 @@ template <typename T> struct Elem;
 template <> struct Elem<__bf16> {
     typedef bf16x8 frag;
     static constexpr int kTile = 64;  // tokens of a tile in LDS
-    static constexpr int kPad = 8;    // elements between rows in LDS (16 bytes: no bank conflicts)
 };
 template <> struct Elem<float> {
     typedef f32x8 frag;
     static constexpr int kTile = 32;
-    static constexpr int kPad = 4;
 };
 
 __device__ __forceinline__ f32x16 mma(const bf16x8 &a, const bf16x8 &b, const f32x16 &c)
@@ -208,11 +206,33 @@ template <typename T, int DQP> struct HeadMap {
 
 // ------------------------------------------------------------- tiles in LDS
 
+// A tile is read by rows, 16 bytes of 16 neighbouring rows at a time, and in
+// bf16 by columns, 64 bytes of 4 neighbouring rows (tr reads).  Its chunks of
+// 16 bytes change places within a row by a number that the row gives, so that
+// both fall into different banks: rows of 64 bytes (4 in a line of the 64
+// banks) by bits 2 and 3 of the row, of 128 bytes by bit 1 (to the other half of
+// the row) and bits 2, 3, of 256 bytes by bits 0, 1 and 2, 3.  fp32 tiles, read
+// by columns real by real, have 16 bytes between their rows instead.
+template <typename T, int DP> struct Lds;
+template <int DP> struct Lds<__bf16, DP> {
+    static constexpr int kRow = DP;
+    static __device__ __forceinline__ int turn(int row)
+    {
+        const int q = row >> 2 & 3;
+        return DP == 32 ? q : DP == 64 ? (row << 1 & 4) | q : (row << 2 & 12) | q;
+    }
+    static __device__ __forceinline__ int at(int row, int chunk) { return row * DP + ((chunk ^ turn(row)) << 3); }
+};
+template <int DP> struct Lds<float, DP> {
+    static constexpr int kRow = DP + 4;
+    static __device__ __forceinline__ int at(int row, int chunk) { return row * kRow + (chunk << 3); }
+};
+
 // A tile of kTile tokens x D reals, staged by THREADS threads: fetch() loads
 // this thread's chunks of the tile at `token`, put() writes them to LDS.
 template <typename T, int DP, int THREADS> struct Stage {
     typedef typename Elem<T>::frag frag;
-    static constexpr int kTokens = Elem<T>::kTile, kRow = DP + Elem<T>::kPad;
+    static constexpr int kTokens = Elem<T>::kTile, kRow = Lds<T, DP>::kRow;
     static constexpr int kChunks = DP / 8, kStep = THREADS / kChunks;
     static constexpr int kCount = kTokens > kStep ? kTokens / kStep : 1;  // (more threads than chunks: some idle)
     static_assert(THREADS % kChunks == 0 && kCount * kStep >= kTokens, "whole rows per step");
@@ -242,7 +262,7 @@ template <typename T, int DP, int THREADS> struct Stage {
             return;
 #pragma unroll
         for (int i = 0; i < kCount; ++i)
-            *reinterpret_cast<frag *>(lds + (row + i * kStep) * kRow + d) = r[i];
+            *reinterpret_cast<frag *>(lds + Lds<T, DP>::at(row + i * kStep, d / 8)) = r[i];
     }
 };
 template <typename T, int DQP> struct HeadMap<const T, DQP> {
@@ -269,34 +289,37 @@ template <typename T, int DQP> struct HeadMap<const T, DQP> {
 
 // Operand whose rows are the tile's tokens (32 sub + lane % 32) and whose depth
 // is reals 16 f + 8 (lane / 32) ..+7 of a row.
-template <typename T, int ROW> __device__ __forceinline__ typename Elem<T>::frag row_frag(const T *tile, int sub, int f)
+template <typename T, int DP> __device__ __forceinline__ typename Elem<T>::frag row_frag(const T *tile, int sub, int f)
 {
     const int lane = threadIdx.x & 63;
-    return *reinterpret_cast<const typename Elem<T>::frag *>(tile + (32 * sub + (lane & 31)) * ROW + 16 * f +
-                                                             8 * (lane >> 5));
+    return *reinterpret_cast<const typename Elem<T>::frag *>(tile + Lds<T, DP>::at(lane & 31, 2 * f + (lane >> 5)) +
+                                                             32 * sub * Lds<T, DP>::kRow);
 }
 
 // Operand whose rows are reals 32 mt + lane % 32 and whose depth is the tile's
 // tokens 32 sub + 16 s + 4 (lane / 32) + e % 4 + 8 (e / 4): acc_frag's order.
 // In bf16 four tokens of one real come from one transposing read, in which 16
-// lanes give the addresses of 4 rows of 16 reals.
-template <int ROW> __device__ __forceinline__ bf16x8 col_frag(const __bf16 *tile, int sub, int s, int mt)
+// lanes give the addresses of 4 rows of 16 reals.  (Rows 16 apart have the same
+// turn of chunks.)
+template <int DP> __device__ __forceinline__ bf16x8 col_frag(const __bf16 *tile, int sub, int s, int mt)
 {
     typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
     const int lane = threadIdx.x & 63, i = lane & 15;
-    const __bf16 *p = tile + (32 * sub + 16 * s + 4 * (lane >> 5) + (i >> 2)) * ROW + 32 * mt + (lane & 16) + 4 * (i & 3);
-    const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(p));
-    const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(p + 8 * ROW));
+    const int row = 4 * (lane >> 5) + (i >> 2), chunk = 4 * mt + (lane >> 3 & 2) + (i >> 1 & 1), at = 4 * (i & 1);
+    const __bf16 *p = tile + (32 * sub + 16 * s) * DP + at;
+    const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(p + Lds<__bf16, DP>::at(row, chunk)));
+    const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(p + Lds<__bf16, DP>::at(row + 8, chunk)));
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
-template <int ROW> __device__ __forceinline__ f32x8 col_frag(const float *tile, int sub, int s, int mt)
+template <int DP> __device__ __forceinline__ f32x8 col_frag(const float *tile, int sub, int s, int mt)
 {
+    constexpr int kRow = Lds<float, DP>::kRow;
     const int lane = threadIdx.x & 63;
-    const float *p = tile + (32 * sub + 16 * s + 4 * (lane >> 5)) * ROW + 32 * mt + (lane & 31);
+    const float *p = tile + (32 * sub + 16 * s + 4 * (lane >> 5)) * kRow + 32 * mt + (lane & 31);
     f32x8 v;
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-        v[e] = p[((e & 3) + 8 * (e >> 2)) * ROW];
+        v[e] = p[((e & 3) + 8 * (e >> 2)) * kRow];
     return v;
 }
 
@@ -410,19 +433,18 @@ __device__ __forceinline__ void add_bias(f32x16 &s, float c, const float *bias, 
     }
 }
 // `value` in the places of a tile's tokens (rows of accumulators) at or behind
-// `end`.  The empty statements keep the compiler from doing this to every tile
-// with selects.
+// `end`.  (The empty statement ties the comparisons to this branch: the compiler
+// would else make selects of them for every tile.)
 template <int SUBS>
 __device__ __forceinline__ void clear_behind(f32x16 (&s)[SUBS], int first, int end, int half, float value)
 {
+    int left = end - first - 4 * half;
+    asm volatile("" : "+v"(left));
 #pragma unroll
-    for (int sub = 0; sub < SUBS; ++sub) {
-        asm volatile("" : "+v"(s[sub]));
+    for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-            if (first + 32 * sub + 8 * (r / 4) + 4 * half + r % 4 >= end)
-                s[sub][r] = value;
-    }
+            s[sub][r] = 32 * sub + 8 * (r / 4) + r % 4 >= left ? value : s[sub][r];
 }
 
 // The work-group's place among `total` in an order in which neighbours run on
