@@ -216,48 +216,76 @@ __global__ void __launch_bounds__(64 * NW, DQP <= 16 ? 2 : 1) attention_forward_
     }
 }
 
-// The splits' partial results joined: one thread per 8 reals of a row.
+// One real of a row's output from its sum over the keys.
+template <typename T, int DQP>
+__device__ __forceinline__ void finish_real(const Forward &f, int64_t row, int real, float value, float top, float sum)
+{
+    const AttnGeom &g = f.a.g;
+    const int lq = g.lq();
+    const int query = int(row % lq), head = int(row / lq % g.heads);
+    const int64_t img = row / lq / g.heads;
+    value *= sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+    const HeadMap<T, DQP> om(f.out, img, head, g.dq);
+    if (om.valid(real, 1) > 0) {
+        const T rounded = T(value);
+        *om.at(query, real) = rounded;
+        if (f.rest != nullptr && sizeof(T) == 2) {
+            const int64_t c_all = int64_t(g.heads) * g.dq;
+            static_cast<T *>(f.rest)[((img * lq + query) * 4 + real / DQP) * c_all + int64_t(head) * g.dq + real % DQP] =
+                T(value - float(rounded));
+        }
+    }
+    if (f.stats != nullptr && real == 0) {
+        f.stats[2 * row] = top;
+        f.stats[2 * row + 1] = sum;
+    }
+}
+
+// The splits' partial results joined: a work-group per row, its lanes in sets
+// of D / 4 (4 reals each) that take the splits in turn and meet in LDS.
 template <typename T, int DQP>
 __global__ void __launch_bounds__(256) attention_join_kernel(Forward f)
 {
-    constexpr int DP = 4 * DQP, kChunks = DP / 8;
+    constexpr int DP = 4 * DQP, kLanes = DP / 4, kSets = 256 / kLanes;
+    __shared__ float acc_lds[kSets * DP];
+    __shared__ float stat_lds[2 * kSets];
     const AttnGeom &g = f.a.g;
     const int lq = g.lq();
-    const int64_t rows = int64_t(g.n) * g.heads * lq;
-    const int64_t id = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    const int64_t row = id / kChunks;
-    const int d = 8 * int(id % kChunks);
-    if (row >= rows)
+    const int64_t rows = int64_t(g.n) * g.heads * lq, row = blockIdx.x;
+    const int set = threadIdx.x / kLanes, d = 4 * (threadIdx.x % kLanes);
+    float top = -INFINITY, sum = 0.0f;
+    f32x4 o = 0.0f;
+#pragma unroll 4
+    for (int s = set; s < f.splits; s += kSets) {
+        const float t = f.part_stats[(s * rows + row) * 2], l = f.part_stats[(s * rows + row) * 2 + 1];
+        const f32x4 v = *reinterpret_cast<const f32x4 *>(f.part + (s * rows + row) * DP + d);
+        const float now = fmaxf(top, t), m = now == -INFINITY ? 0.0f : now;
+        const float back = exp2_fast(top - m), w = exp2_fast(t - m);
+        top = now;
+        sum = sum * back + l * w;
+        o = o * back + v * w;
+    }
+    *reinterpret_cast<f32x4 *>(acc_lds + set * DP + d) = o;
+    if (d == 0) {
+        stat_lds[2 * set] = top;
+        stat_lds[2 * set + 1] = sum;
+    }
+    __syncthreads();
+    if (threadIdx.x >= DP)
         return;
-    float top = -INFINITY;
-    for (int s = 0; s < f.splits; ++s)
-        top = fmaxf(top, f.part_stats[(s * rows + row) * 2]);
+    const int real = threadIdx.x;
+    top = -INFINITY;
+    for (int s = 0; s < kSets; ++s)
+        top = fmaxf(top, stat_lds[2 * s]);
     const float m = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f;
-    f32x8 o = 0.0f;
-    for (int s = 0; s < f.splits; ++s) {
-        const float w = exp2_fast(f.part_stats[(s * rows + row) * 2] - m);
-        sum = fmaf(w, f.part_stats[(s * rows + row) * 2 + 1], sum);
-        const f32x8 v = *reinterpret_cast<const f32x8 *>(f.part + (s * rows + row) * DP + d);
-        o += v * w;
+    float value = 0.0f;
+    sum = 0.0f;
+    for (int s = 0; s < kSets; ++s) {
+        const float w = exp2_fast(stat_lds[2 * s] - m);
+        sum = fmaf(w, stat_lds[2 * s + 1], sum);
+        value = fmaf(w, acc_lds[s * DP + real], value);
     }
-    o *= sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-    const int query = int(row % lq), head = int(row / lq % g.heads), img = int(row / lq / g.heads);
-    const HeadMap<T, DQP> om(f.out, img, head, g.dq);
-    store_chunk(om.at(query, d), o, om.valid(d, 8), om.vec);
-    if (f.rest != nullptr && sizeof(T) == 2) {
-        const int64_t c_all = int64_t(g.heads) * g.dq;
-        const AttnMap dense{f.rest, lq * 4 * c_all, 4 * c_all, c_all, f.out.vec && g.dq % 8 == 0};
-        const HeadMap<T, DQP> rm(dense, img, head, g.dq);
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            o[e] -= float(T(o[e]));
-        store_chunk(rm.at(query, d), o, rm.valid(d, 8), rm.vec);
-    }
-    if (f.stats != nullptr && d == 0) {
-        f.stats[2 * row] = m;
-        f.stats[2 * row + 1] = sum;
-    }
+    finish_real<T, DQP>(f, row, real, value, m, sum);
 }
 
 // ------------------------------------------------------- one query per image
@@ -266,12 +294,15 @@ __global__ void __launch_bounds__(256) attention_join_kernel(Forward f)
 // head for GRP of the query heads that share it, and a work-group's lanes hold
 // as many heads of a token as there are, so that they read whole rows of the
 // map.  Each such set of lanes walks over every `slots`-th key with a softmax
-// of its own; they are joined in LDS, and those of several splits of the keys
-// by attention_join_kernel.  Bound by reading keys and values once.
+// of its own; they are joined in LDS, and those of several splits of an image's
+// keys (equal shares of what the image has) by attention_join_kernel.  Biases of
+// a chunk of keys are looked up into LDS at a time.  Bound by reading keys and
+// values once.
 struct Token {
-    int heads_per_block, slots, kv_blocks, group_blocks;
+    int heads_per_block, slots, kv_blocks, group_blocks, chunk;
 };
-constexpr int kTokenChunk = 512;  // keys whose buckets are looked up at a time
+constexpr int kTokenBias = 4096;  // biases in LDS: keys of a chunk x query heads of the work-group
+constexpr int kTokenUnroll = 4;   // keys that a set of lanes reads at a time
 
 // Sum over the 4, 8 or 16 lanes of a row.
 template <int G> __device__ __forceinline__ float lanes_sum(float x)
@@ -291,11 +322,11 @@ template <int G> __device__ __forceinline__ float lanes_sum(float x)
 template <typename T, int DQP, int GRP, bool BIAS>
 __global__ void __launch_bounds__(256) attention_token_kernel(Forward f, Token tk)
 {
-    constexpr int DP = 4 * DQP, G = DP / 8, kPairs = 256 / G, U = 4;
+    constexpr int DP = 4 * DQP, G = DP / 8, kPairs = 256 / G, U = kTokenUnroll;
     typedef typename Elem<T>::frag frag;
     __shared__ float acc_lds[kPairs * GRP * DP];
     __shared__ float stat_lds[kPairs * GRP * 2];
-    __shared__ int bucket[BIAS ? kTokenChunk : 1];
+    __shared__ float bias_lds[BIAS ? kTokenBias : 1];
     const AttnGeom &g = f.a.g;
     const int lk = g.lk(), group = g.heads / g.kv_heads;
     int id = blockIdx.x;
@@ -308,15 +339,14 @@ __global__ void __launch_bounds__(256) attention_token_kernel(Forward f, Token t
     const int slot = pair / tk.heads_per_block, kv_head = kvb * tk.heads_per_block + pair % tk.heads_per_block;
     const bool active = slot < tk.slots && kv_head < g.kv_heads;
     const int len = f.a.kv_len != nullptr ? min(max(f.a.kv_len[img], 0), lk) : lk;
-    const int first = split * f.tiles_per_split * kTokenChunk;
-    const int end = min(len, first + f.tiles_per_split * kTokenChunk);
+    const int round = U * tk.slots, share = ((len + f.splits - 1) / f.splits + round - 1) / round * round;
+    const int first = int(min(int64_t(split) * share, int64_t(len))), end = min(len, first + share);
     const int head0 = kv_head * group + gb * GRP;  // of GRP query heads
     const int heads_here = min(GRP, group - gb * GRP);
 
     const HeadMap<const T, DQP> km(f.a.k, img, active ? kv_head : 0, g.dq), vm(f.a.v, img, active ? kv_head : 0, g.dq);
     f32x8 q[GRP], o[GRP];
     float top[GRP], sum[GRP];
-    const float *table[GRP];
     const float c = g.scale * kLog2e;
 #pragma unroll
     for (int i = 0; i < GRP; ++i) {
@@ -326,8 +356,6 @@ __global__ void __launch_bounds__(256) attention_token_kernel(Forward f, Token t
         o[i] = 0.0f;
         top[i] = -INFINITY;
         sum[i] = 0.0f;
-        if (BIAS)
-            table[i] = f.a.bias.table + int64_t(here ? head0 + i : 0) * f.a.bias.ny * f.a.bias.nx;
     }
     const int valid = active ? km.valid(d, 8) : 0;
     int pos_y = 0, pos_x = 0;
@@ -335,12 +363,22 @@ __global__ void __launch_bounds__(256) attention_token_kernel(Forward f, Token t
         pos_y = f.a.pos[2 * img];
         pos_x = f.a.pos[2 * img + 1];
     }
-    for (int c0 = first; c0 < end; c0 += kTokenChunk) {
-        const int c1 = min(c0 + kTokenChunk, end);
+    const int nb = f.a.bias.ny * f.a.bias.nx;
+    const int chunk = BIAS ? tk.chunk : max(end - first, 1);
+    for (int c0 = first; c0 < end; c0 += chunk) {
+        const int c1 = min(c0 + chunk, end);
         if (BIAS) {
-            __syncthreads();  // the last chunk's buckets have been read
-            for (int j = c0 + int(threadIdx.x); j < c1; j += 256)
-                bucket[j - c0] = bucket_of(f.o, f.a.bias, place_k(f.o, j), pos_y, pos_x);
+            __syncthreads();  // the last chunk's biases have been read
+            for (int j = c0 + int(threadIdx.x); j < c1; j += 256) {
+                const float *row = f.a.bias.table + bucket_of(f.o, f.a.bias, place_k(f.o, j), pos_y, pos_x);
+                for (int h = 0; h < tk.heads_per_block; ++h)
+#pragma unroll
+                    for (int i = 0; i < GRP; ++i) {
+                        const int head = (kvb * tk.heads_per_block + h) * group + gb * GRP + i;
+                        if (i < heads_here && head < g.heads)
+                            bias_lds[(h * GRP + i) * tk.chunk + j - c0] = in_log2(row[int64_t(head) * nb]);
+                    }
+            }
             __syncthreads();
         }
         if (!active)
@@ -370,11 +408,10 @@ __global__ void __launch_bounds__(256) attention_token_kernel(Forward f, Token t
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int t = j + u * tk.slots;
-                const int b = BIAS ? bucket[min(t, c1 - 1) - c0] : 0;
 #pragma unroll
                 for (int i = 0; i < GRP; ++i) {
                     if (BIAS)
-                        s[u][i] += in_log2(table[i][b]);
+                        s[u][i] += bias_lds[(pair % tk.heads_per_block * GRP + i) * tk.chunk + min(t, c1 - 1) - c0];
                     if (t >= c1)
                         s[u][i] = -INFINITY;
                 }
@@ -444,21 +481,7 @@ __global__ void __launch_bounds__(256) attention_token_kernel(Forward f, Token t
             }
             continue;
         }
-        value *= total > 0.0f || total != total ? 1.0f / total : 0.0f;
-        const HeadMap<T, DQP> om(f.out, img, head, g.dq);
-        if (om.valid(real, 1) > 0) {
-            const T rounded = T(value);
-            *om.at(0, real) = rounded;
-            if (f.rest != nullptr && sizeof(T) == 2) {
-                const int64_t c_all = int64_t(g.heads) * g.dq;
-                static_cast<T *>(f.rest)[(int64_t(img) * 4 + real / DQP) * c_all + int64_t(head) * g.dq + real % DQP] =
-                    T(value - float(rounded));
-            }
-        }
-        if (f.stats != nullptr && real == 0) {
-            f.stats[2 * row] = base;
-            f.stats[2 * row + 1] = total;
-        }
+        finish_real<T, DQP>(f, row, real, value, base, total);
     }
 }
 
@@ -484,8 +507,7 @@ Plan forward_plan(const AttnCall &a, DType dt, bool may_split = true)
     Plan p{};
     const int lq = g.lq();
     if (lq == 1) {
-        // one query: heads of a token side by side, splits of whole chunks of
-        // keys until two rounds of the chip have work
+        // one query: heads of a token side by side
         const int pairs = 256 / (dp / 8), group = g.heads / g.kv_heads;
         p.grp = group == 1 ? 1 : group == 2 ? 2 : 4;
         p.token.heads_per_block = std::min(g.kv_heads, pairs);
@@ -493,11 +515,12 @@ Plan forward_plan(const AttnCall &a, DType dt, bool may_split = true)
         p.token.kv_blocks = (g.kv_heads + p.token.heads_per_block - 1) / p.token.heads_per_block;
         p.token.group_blocks = (group + p.grp - 1) / p.grp;
         p.blocks = 1;
+        // (biases of a work-group's heads for a chunk of keys fill the LDS array)
+        p.token.chunk = kTokenBias / (p.token.heads_per_block * p.grp);
+        // four work-groups per compute unit, two rounds of keys at least to each
         const int64_t groups = int64_t(g.n) * p.token.kv_blocks * p.token.group_blocks;
-        const int chunks = (g.lk() + kTokenChunk - 1) / kTokenChunk;
-        p.splits = may_split ? int(std::max<int64_t>(1, std::min<int64_t>(1024 / groups, chunks))) : 1;
-        p.tiles_per_split = (chunks + p.splits - 1) / p.splits;
-        p.splits = (chunks + p.tiles_per_split - 1) / p.tiles_per_split;
+        const int rounds = (g.lk() + 2 * kTokenUnroll * p.token.slots - 1) / (2 * kTokenUnroll * p.token.slots);
+        p.splits = may_split ? int(std::max<int64_t>(1, std::min<int64_t>(1024 / groups, rounds))) : 1;
         return p;
     }
     // half work-groups where whole ones would leave half of their queries empty
@@ -547,8 +570,7 @@ hipError_t forward_launch(const Forward &f, const Plan &p, hipStream_t s)
     if (hipError_t e = hipGetLastError())
         return e;
     if (p.splits > 1) {
-        const int64_t threads = int64_t(g.n) * g.heads * g.lq() * (DQP / 2);
-        attention_join_kernel<T, DQP><<<unsigned((threads + 255) / 256), 256, 0, s>>>(f);
+        attention_join_kernel<T, DQP><<<unsigned(int64_t(g.n) * g.heads * g.lq()), 256, 0, s>>>(f);
     }
     return hipGetLastError();
 }
@@ -563,8 +585,7 @@ template <typename T, int DQP, int GRP> hipError_t token_launch(const Forward &f
     if (hipError_t e = hipGetLastError())
         return e;
     if (p.splits > 1) {
-        const int64_t threads = int64_t(g.n) * g.heads * (DQP / 2);
-        attention_join_kernel<T, DQP><<<unsigned((threads + 255) / 256), 256, 0, s>>>(f);
+        attention_join_kernel<T, DQP><<<unsigned(int64_t(g.n) * g.heads), 256, 0, s>>>(f);
     }
     return hipGetLastError();
 }
