@@ -614,8 +614,8 @@ QUAN_API int quan_relpos_buckets(int32_t radius, int32_t buckets, int32_t *map);
  *   rest       NULL, or (bf16) a 16-byte aligned dense map like out's that
  *              receives bf16(out before rounding - out).
  *   stats      NULL, or fp32 [N][heads][Hq*Wq][2]: each row's maximum in units
- *              of log 2 (0 for a row without a key) and the sum of
- *              2^(score - maximum).
+ *              of log 2 (at least the type's lowest; 0 for a row without a
+ *              key) and the sum of 2^(score - maximum).
  *
  * rest and stats are what quan_attention_backward takes.  With a bias, maps of
  * more than one row may be 1792 pixels wide.  out may overlap no input; it may

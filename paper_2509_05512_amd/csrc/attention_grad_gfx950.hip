@@ -330,6 +330,7 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
 }
 
 // The launch of the keys' side: lanes hold keys, registers queries.
+constexpr int kNoSegment = -(1 << 30);
 template <typename T, int DQP, int MODE>
 __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dkv_kernel(Backward f)
 {
@@ -385,7 +386,7 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dkv_ker
         const HeadMap<const T, DQP> qm(f.a.q, img, head, g.dq), gm(f.dout, img, head, g.dq);
         const float *table = MODE != 0 ? f.a.bias.table + int64_t(head) * f.a.bias.ny * f.a.bias.nx : nullptr;
         const int64_t row0 = (int64_t(img) * g.heads + head) * lq;
-        int segment = -1, buf = 0;
+        int segment = kNoSegment, buf = 0;
         Tile qt, gt;
         __syncthreads();  // the last head's tiles and segment have been read
         qt.fetch(qm, (tiles - 1) * QT, lq);
@@ -411,10 +412,10 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dkv_ker
             }
             if (MODE != 0) {
                 const int lo = low_k - place_q(f.o, min(i0 + QT, lq) - 1) - 3, hi = high_k - place_q(f.o, i0);
-                if (segment < 0 || hi >= segment + f.o.cap) {
-                    if (segment >= 0)
+                if (segment == kNoSegment || hi >= segment + f.o.cap) {
+                    if (segment != kNoSegment)
                         __syncthreads();
-                    segment = max(lo, 0);
+                    segment = lo;  // (down to -3)
                     stage_bias(bias, f.o, f.a.bias, table, segment, f.o.cap, pos_y, pos_x);
                 }
             }
@@ -486,30 +487,34 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dkv_ker
 __global__ void __launch_bounds__(256) offset_sums_kernel(Backward f, int slices, double *__restrict__ out)
 {
     const AttnGeom &g = f.a.g;
-    const int a = blockIdx.x * 256 + threadIdx.x, head = blockIdx.y, slice = blockIdx.z;
+    const int a = blockIdx.x * 256 + threadIdx.x, head = blockIdx.y;
     if (a >= f.o.total)
         return;
     const int lq = g.lq(), last_k = place_k(f.o, g.lk() - 1);
-    double s = 0.0;
-    for (int b = 0; b < f.blocks; ++b) {
-        const int low = f.o.origin - place_q(f.o, min((b + 1) * kQueries, lq) - 1);
-        const int past = f.o.origin - place_q(f.o, b * kQueries) + last_k + 1;
-        if (a < low || a >= past)
-            continue;
-        const float *p = f.offsets + (int64_t(head) * f.blocks + b) * f.range + (a - low);
-        for (int img = slice; img < g.n; img += slices)
-            s += double(p[int64_t(img) * g.heads * f.blocks * f.range]);
+    for (int slice = blockIdx.z; slice < slices; slice += gridDim.z) {
+        double s = 0.0;
+        for (int b = 0; b < f.blocks; ++b) {
+            const int low = f.o.origin - place_q(f.o, min((b + 1) * kQueries, lq) - 1);
+            const int past = f.o.origin - place_q(f.o, b * kQueries) + last_k + 1;
+            if (a < low || a >= past)
+                continue;
+            const float *p = f.offsets + (int64_t(head) * f.blocks + b) * f.range + (a - low);
+            for (int img = slice; img < g.n; img += slices)
+                s += double(p[int64_t(img) * g.heads * f.blocks * f.range]);
+        }
+        out[(int64_t(slice) * g.heads + head) * f.o.total + a] = s;
     }
-    out[(int64_t(slice) * g.heads + head) * f.o.total + a] = s;
 }
 
 // dtable from the sums by offset: a work-group per row of buckets (head, by).
 // Its threads add up the rows dy of offsets in that bucket, column by column,
-// then its waves the columns dx of each bucket bx.
+// then its waves the columns dx of each bucket bx.  The slices have their
+// offsets' buckets in common, but where queries have places of their own (pos):
+// there a slice is an image, and they are taken one by one.
 constexpr int kTableThreads = 512, kTableCols = 2048;
 __global__ void __launch_bounds__(kTableThreads)
-table_gradient_kernel(AttnBias b, Offsets o, int heads, int rows, int slices, const double *__restrict__ sums,
-                      float *__restrict__ dtable)
+table_gradient_kernel(AttnBias b, Offsets o, int heads, int rows, int slices, const int *__restrict__ pos,
+                      const double *__restrict__ sums, float *__restrict__ dtable)
 {
     __shared__ double cols[kTableCols];
     __shared__ short bucket[kTableCols];
@@ -518,32 +523,36 @@ table_gradient_kernel(AttnBias b, Offsets o, int heads, int rows, int slices, co
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int x = threadIdx.x; x < b.nx; x += kTableThreads)
         tot[x] = 0.0;
-    for (int x0 = 0; x0 < o.pitch; x0 += kTableCols) {
-        const int width = min(kTableCols, o.pitch - x0);
-        __syncthreads();  // cols has been read
-        for (int x = threadIdx.x; x < width; x += kTableThreads) {
-            double s = 0.0;
-            for (int y = 0; y < rows; ++y) {
-                const int dy = min(max(y - o.hq1, -b.ry), b.ry);
-                if ((b.by != nullptr ? min(max(b.by[dy + b.ry], 0), b.ny - 1) : 0) != iy)
-                    continue;
-                for (int sl = 0; sl < slices; ++sl)
-                    s += sums[(int64_t(sl) * heads + head) * o.total + int64_t(y) * o.pitch + x0 + x];
+    const int groups = pos != nullptr ? slices : 1, per = slices / groups;
+    for (int group = 0; group < groups; ++group) {
+        const int pos_y = pos != nullptr ? pos[2 * group] : 0, pos_x = pos != nullptr ? pos[2 * group + 1] : 0;
+        for (int x0 = 0; x0 < o.pitch; x0 += kTableCols) {
+            const int width = min(kTableCols, o.pitch - x0);
+            __syncthreads();  // cols has been read
+            for (int x = threadIdx.x; x < width; x += kTableThreads) {
+                double s = 0.0;
+                for (int y = 0; y < rows; ++y) {
+                    const int dy = min(max(y - o.hq1 - pos_y, -b.ry), b.ry);
+                    if ((b.by != nullptr ? min(max(b.by[dy + b.ry], 0), b.ny - 1) : 0) != iy)
+                        continue;
+                    for (int sl = group * per; sl < (group + 1) * per; ++sl)
+                        s += sums[(int64_t(sl) * heads + head) * o.total + int64_t(y) * o.pitch + x0 + x];
+                }
+                cols[x] = s;
+                const int dx = min(max(x0 + x - o.wq1 - pos_x, -b.rx), b.rx);
+                bucket[x] = short(b.bx != nullptr ? min(max(b.bx[dx + b.rx], 0), b.nx - 1) : 0);
             }
-            cols[x] = s;
-            const int dx = min(max(x0 + x - o.wq1, -b.rx), b.rx);
-            bucket[x] = short(b.bx != nullptr ? min(max(b.bx[dx + b.rx], 0), b.nx - 1) : 0);
-        }
-        __syncthreads();
-        for (int ix = wave; ix < b.nx; ix += kTableThreads / 64) {
-            double s = 0.0;
-            for (int x = lane; x < width; x += 64)
-                if (bucket[x] == ix)
-                    s += cols[x];
-            for (int m = 1; m < 64; m <<= 1)
-                s += __shfl_xor(s, m, 64);
-            if (lane == 0)
-                tot[ix] += s;
+            __syncthreads();
+            for (int ix = wave; ix < b.nx; ix += kTableThreads / 64) {
+                double s = 0.0;
+                for (int x = lane; x < width; x += 64)
+                    if (bucket[x] == ix)
+                        s += cols[x];
+                for (int m = 1; m < 64; m <<= 1)
+                    s += __shfl_xor(s, m, 64);
+                if (lane == 0)
+                    tot[ix] += s;
+            }
         }
     }
     __syncthreads();
@@ -590,7 +599,8 @@ Plan backward_plan(const AttnCall &a, DType dt, bool table)
         if (table) {
             p.range = block_q + host_place(lk - 1, g.wk, o.skip_k) + 1;
             p.offset_bytes = (size_t(g.n) * g.heads * p.blocks * p.range * sizeof(float) + 255) & ~size_t(255);
-            p.slices = std::min(g.n, std::max(1, 1024 / std::max(1, (o.total + 255) / 256 * g.heads)));
+            // (images whose queries have places of their own have slices of their own)
+            p.slices = a.pos != nullptr ? g.n : std::min(g.n, std::max(1, 1024 / std::max(1, (o.total + 255) / 256 * g.heads)));
             p.sum_bytes = size_t(p.slices) * g.heads * o.total * sizeof(double);
         }
     }
@@ -668,11 +678,11 @@ hipError_t attention_backward_run(const AttnCall &a, DType dt, const AttnMap &ou
     if (!table)
         return hipSuccess;
     double *sums = reinterpret_cast<double *>(w + p.delta_bytes + p.offset_bytes);
-    offset_sums_kernel<<<dim3((f.o.total + 255) / 256, a.g.heads, p.slices), 256, 0, s>>>(f, p.slices, sums);
+    offset_sums_kernel<<<dim3((f.o.total + 255) / 256, a.g.heads, std::min(p.slices, 65535)), 256, 0, s>>>(f, p.slices, sums);
     if (hipError_t e = hipGetLastError())
         return e;
     table_gradient_kernel<<<a.g.heads * a.bias.ny, kTableThreads, 0, s>>>(a.bias, f.o, a.g.heads, a.g.hk + a.g.hq - 1,
-                                                                        p.slices, sums, dtable);
+                                                                        p.slices, a.pos, sums, dtable);
     return hipGetLastError();
 }
 

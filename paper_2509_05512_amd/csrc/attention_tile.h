@@ -385,13 +385,14 @@ __device__ __forceinline__ float in_log2(float t)
     const float v = t * kLog2e;
     return fabsf(t) <= -kLowest ? fminf(fmaxf(v, kLowest), -kLowest) : v;
 }
-// Entries [first, first + count) of offsets into lds.
+// Entries [first, first + count) of offsets into lds; those that no pair of
+// pixels has (a quad's tokens may pass the last one) are zero.
 __device__ __forceinline__ void stage_bias(float *lds, const Offsets &o, const AttnBias &b, const float *table,
                                            int first, int count, int y, int x)
 {
     for (int e = threadIdx.x; e < count; e += blockDim.x) {
         const int a = first + e;
-        lds[e] = a < o.total ? in_log2(table[bucket_of(o, b, a, y, x)]) : 0.0f;
+        lds[e] = a >= 0 && a < o.total ? in_log2(table[bucket_of(o, b, a, y, x)]) : 0.0f;
     }
 }
 
@@ -406,8 +407,7 @@ template <int MODE> __device__ __forceinline__ i32x4 places(const int *place, in
     return i32x4{p0, p0 + 1, p0 + 2, p0 + 3};
 }
 // Scores in units of log 2: c times the products plus the bias of the lane's
-// offset `at` + SIGN * place (MODE 0: no bias).  Behind the last token of the
-// queries' side a place may pass the lane's offset: such scores count nowhere.
+// offset `at` + SIGN * place (MODE 0: no bias).
 template <int MODE, int SIGN>
 __device__ __forceinline__ void add_bias(f32x16 &s, float c, const float *bias, const int *place, int at, int sub,
                                          int half)
@@ -420,7 +420,7 @@ __device__ __forceinline__ void add_bias(f32x16 &s, float c, const float *bias, 
                 s[4 * g + t] *= c;
         } else if (MODE == 1) {
             const int p0 = place[32 * sub + 8 * g + 4 * half];
-            const float *b = bias + (SIGN > 0 ? at + p0 : max(at - p0 - 3, 0));
+            const float *b = bias + (SIGN > 0 ? at + p0 : at - p0 - 3);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
                 s[4 * g + t] = fmaf(s[4 * g + t], c, b[SIGN > 0 ? t : 3 - t]);
@@ -428,7 +428,7 @@ __device__ __forceinline__ void add_bias(f32x16 &s, float c, const float *bias, 
             const i32x4 p = places<MODE>(place, sub, g, half);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-                s[4 * g + t] = fmaf(s[4 * g + t], c, bias[SIGN > 0 ? at + p[t] : max(at - p[t], 0)]);
+                s[4 * g + t] = fmaf(s[4 * g + t], c, bias[at + SIGN * p[t]]);
         }
     }
 }

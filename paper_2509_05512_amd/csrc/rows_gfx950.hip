@@ -18,64 +18,63 @@
 namespace quan {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;         // of a work-group whose rows are held by waves or parts of them
+constexpr int kBlockThreads = 512;     // at most, of one that holds a row together
 constexpr int kWaves = kThreads / 64;
+constexpr int kBlockWaves = kBlockThreads / 64;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// 8 reals of a row from `p`, of which the first `valid` (0, 4 or 8: rows are
-// whole quaternions per channel, 4C reals) exist.  `whole` rows are multiples
-// of 8 reals, so that every chunk is 16-byte aligned; others are aligned to 4
-// reals.
-__device__ __forceinline__ f32x8 load8(const __bf16 *p, int valid, bool whole)
+// 8 reals of a row as they lie in memory.
+template <typename T> struct Raw;
+template <> struct Raw<__bf16> {
+    bf16x8 v;
+    __device__ __forceinline__ f32x8 get() const { return __builtin_convertvector(v, f32x8); }
+};
+template <> struct Raw<float> {
+    f32x8 v;
+    __device__ __forceinline__ f32x8 get() const { return v; }
+};
+// Those from element `at` of a map, of which the first `valid` (0, 4 or 8: rows
+// are whole quaternions per channel, 4C reals) exist; zeros behind.  `whole` rows
+// are multiples of 8 reals, so that every chunk is 16-byte aligned; others are
+// aligned to 4 reals.
+template <typename T> __device__ __forceinline__ Raw<T> load_raw(const T *map, int64_t at, int valid, bool whole)
 {
-    f32x8 v = 0.0f;
+    typedef T half __attribute__((ext_vector_type(4)));
+    Raw<T> r;
     if (whole) {
-        if (valid == 8)
-            v = __builtin_convertvector(*reinterpret_cast<const bf16x8 *>(p), f32x8);
-        return v;
+        const Raw<T> t = *reinterpret_cast<const Raw<T> *>(map + (valid > 0 ? at : 0));
+        r.v = valid > 0 ? t.v : T(0.0f);
+        return r;
     }
-    if (valid >= 4) {
-        const f32x4 a = __builtin_convertvector(*reinterpret_cast<const bf16x4 *>(p), f32x4);
-        v.lo = a;
-    }
-    if (valid == 8) {
-        const f32x4 a = __builtin_convertvector(*reinterpret_cast<const bf16x4 *>(p + 4), f32x4);
-        v.hi = a;
-    }
-    return v;
+    const half lo = *reinterpret_cast<const half *>(map + (valid > 0 ? at : 0));
+    const half hi = *reinterpret_cast<const half *>(map + (valid > 4 ? at + 4 : 0));
+    r.v.lo = valid > 0 ? lo : half(T(0.0f));
+    r.v.hi = valid > 4 ? hi : half(T(0.0f));
+    return r;
 }
-__device__ __forceinline__ f32x8 load8(const float *p, int valid, bool)
+template <typename T> __device__ __forceinline__ f32x8 load8(const T *map, int64_t at, int valid, bool whole)
 {
-    f32x8 v = 0.0f;
-    if (valid >= 4)
-        v.lo = *reinterpret_cast<const f32x4 *>(p);
-    if (valid == 8)
-        v.hi = *reinterpret_cast<const f32x4 *>(p + 4);
-    return v;
+    return load_raw(map, at, valid, whole).get();
 }
-__device__ __forceinline__ void store8(__bf16 *p, const f32x8 &v, int valid, bool whole)
+template <typename T> __device__ __forceinline__ void store8(T *p, const f32x8 &v, int valid, bool whole)
 {
-    const bf16x8 b = __builtin_convertvector(v, bf16x8);
+    typedef T half __attribute__((ext_vector_type(4)));
+    typedef T full __attribute__((ext_vector_type(8)));
+    const full b = __builtin_convertvector(v, full);
     if (whole) {
-        if (valid == 8)
-            *reinterpret_cast<bf16x8 *>(p) = b;
+        if (valid > 0)
+            __builtin_nontemporal_store(b, reinterpret_cast<full *>(p));
         return;
     }
-    if (valid >= 4)
-        *reinterpret_cast<bf16x4 *>(p) = b.lo;
-    if (valid == 8)
-        *reinterpret_cast<bf16x4 *>(p + 4) = b.hi;
-}
-__device__ __forceinline__ void store8(float *p, const f32x8 &v, int valid, bool)
-{
-    if (valid >= 4)
-        *reinterpret_cast<f32x4 *>(p) = v.lo;
-    if (valid == 8)
-        *reinterpret_cast<f32x4 *>(p + 4) = v.hi;
+    if (valid > 0)
+        __builtin_nontemporal_store(b.lo, reinterpret_cast<half *>(p));
+    if (valid > 4)
+        __builtin_nontemporal_store(b.hi, reinterpret_cast<half *>(p + 4));
 }
 
 // Parameters are aligned to their element only.
@@ -90,18 +89,9 @@ __device__ __forceinline__ f32x8 param8(const float *p, int col, int valid)
     return v;
 }
 
-// The 8 factors (0 or 1 / (1 - p)) of a chunk: see Drop.
-struct Mask {
-    unsigned w[4];
-    unsigned cut;
-    float factor;
-    __device__ __forceinline__ float apply(float v, int e) const
-    {
-        const unsigned bits = e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu;
-        return bits >= cut ? v * factor : 0.0f;
-    }
-};
-__device__ __forceinline__ Mask mask8(unsigned chunk, unsigned pixel, uint64_t seed, uint64_t offset, const Drop &d)
+// Dropout of a chunk: see Drop.
+__device__ __forceinline__ void drop8(f32x8 &v, unsigned chunk, unsigned pixel, uint64_t seed, uint64_t offset,
+                                      const Drop &d)
 {
     unsigned c0 = chunk, c1 = pixel, c2 = unsigned(offset), c3 = unsigned(offset >> 32);
     unsigned k0 = unsigned(seed), k1 = unsigned(seed >> 32);
@@ -115,32 +105,80 @@ __device__ __forceinline__ Mask mask8(unsigned chunk, unsigned pixel, uint64_t s
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
     }
-    return {{c0, c1, c2, c3}, d.cut, d.factor};
+    const unsigned w[4] = {c0, c1, c2, c3};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const unsigned bits = e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu;
+        v[e] = bits >= d.cut ? v[e] * d.factor : 0.0f;
+    }
+}
+__device__ __forceinline__ float dot8(const f32x8 &a, const f32x8 &b)
+{
+    float s = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        s = fmaf(a[e], b[e], s);
+    return s;
 }
 
 // Sums over the lanes of a row; BLOCK: over the work-group.
+template <int CTRL> __device__ __forceinline__ float dpp_add(float x)
+{
+    return x + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xf, 0xf, false));
+}
 template <bool BLOCK, int N>
 __device__ __forceinline__ void row_sums(float (&s)[N], int lpr, float *lds)
 {
-    for (int m = 1; m < lpr; m <<= 1)
+    // (lane ^ 1, ^ 2, then the mirrors of 8 and of 16 lanes, whose halves hold
+    // equal sums by then, and the other half of 32 and of 64)
+    if (lpr >= 2)
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            s[i] += __shfl_xor(s[i], m, 64);
+            s[i] = dpp_add<0xB1>(s[i]);
+    if (lpr >= 4)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            s[i] = dpp_add<0x4E>(s[i]);
+    if (lpr >= 8)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            s[i] = dpp_add<0x141>(s[i]);
+    if (lpr >= 16)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            s[i] = dpp_add<0x140>(s[i]);
+    if (lpr >= 32)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(s[i]), __float_as_uint(s[i]), false, false);
+            s[i] = __uint_as_float(w[0]) + __uint_as_float(w[1]);
+        }
+    if (lpr >= 64)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(s[i]), __float_as_uint(s[i]), false, false);
+            s[i] = __uint_as_float(w[0]) + __uint_as_float(w[1]);
+        }
     if (BLOCK) {
         __syncthreads();  // the last sums have been read
         if ((threadIdx.x & 63) == 0)
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                lds[i * kWaves + (threadIdx.x >> 6)] = s[i];
+                lds[i * kBlockWaves + (threadIdx.x >> 6)] = s[i];
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             s[i] = 0.0f;
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w)
-                s[i] += lds[i * kWaves + w];
+            for (int w = 0; w < int(blockDim.x >> 6); ++w)
+                s[i] += lds[i * kBlockWaves + w];
         }
     }
+}
+
+// 1 / sqrt(x) of x > 0.
+__device__ __forceinline__ float inv_sqrt(float x)
+{
+    return __builtin_amdgcn_rsqf(fmaxf(x, 1.17549435e-38f));
 }
 
 // The three sums of a gradient's row, those of absent parts left out.
@@ -160,30 +198,29 @@ __device__ __forceinline__ void row_sums3(float (&s)[3], int lpr, float *lds)
     }
 }
 
-// A lane's place in its row.
+// A lane's place: its chunk of the row, the work-group's row.
 struct Lane {
-    int at, row, lpr;  // among the row's lanes; the work-group's row; lanes that hold a row
-    int step;          // lanes between chunks of a lane
-    __device__ __forceinline__ Lane(int lpr_, bool block)
-        : at(block ? threadIdx.x : threadIdx.x & (lpr_ - 1)), row(block ? 0 : threadIdx.x / lpr_), lpr(lpr_),
-          step(block ? kThreads : lpr_)
+    int chunk, row;
+    __device__ __forceinline__ Lane(int lpr, bool block)
+        : chunk(block ? threadIdx.x : threadIdx.x & (lpr - 1)), row(block ? 0 : threadIdx.x / lpr)
     {
     }
-    __device__ __forceinline__ int chunk(int k) const { return at + k * step; }
-    __device__ __forceinline__ int valid(int k, int reals) const { return max(0, min(8, reals - 8 * chunk(k))); }
+    __device__ __forceinline__ int valid(int reals) const { return max(0, min(8, reals - 8 * chunk)); }
 };
 
 // ------------------------------------------------------------------- forward
 
-// Bound by HBM: two maps read and two written, 8 bytes per real in bf16.
-template <typename T, int CH, bool BLOCK, bool HAS_Y, bool HAS_H>
-__global__ void __launch_bounds__(kThreads)
+// Bound by HBM: two maps read and two written, 8 bytes per real in bf16.  The
+// work-groups walk over the rows side by side, so that at any time few DRAM
+// pages are in use, and what they write goes past the caches.
+template <typename T, bool BLOCK, bool HAS_Y, bool HAS_H>
+__global__ void __launch_bounds__(BLOCK ? kBlockThreads : kThreads)
 residual_forward_kernel(int64_t rows, FastDiv by_hw, int reals, int lpr, bool whole, ResidualForward a, Drop drop,
                         float eps)
 {
-    __shared__ float lds[kWaves];
+    __shared__ float lds[kBlockWaves];
     const Lane l(lpr, BLOCK);
-    const int per = BLOCK ? 1 : kThreads / lpr;
+    const int per = BLOCK ? 1 : kThreads / lpr, col = 8 * l.chunk, valid = l.valid(reals);
     const float mean = 1.0f / float(reals);
     const bool normed = HAS_Y && a.gamma != nullptr;
     uint64_t seed = 0, offset = 0;
@@ -191,73 +228,52 @@ residual_forward_kernel(int64_t rows, FastDiv by_hw, int reals, int lpr, bool wh
         seed = drop.rng[0];
         offset = drop.rng[1];
     }
-    f32x8 f[CH], next[CH];
-    int valid[CH];
-#pragma unroll
-    for (int k = 0; k < CH; ++k) {
-        valid[k] = l.valid(k, reals);
-        const int col = 8 * l.chunk(k);
-        if (HAS_Y)
-            f[k] = param8(a.gamma, col, valid[k]) * param8(a.scale, col, valid[k]);
-        if (HAS_H)
-            next[k] = param8(a.next_gamma, col, valid[k]);
-    }
+    f32x8 f, next;
+    if (HAS_Y)
+        f = param8(a.gamma, col, valid) * param8(a.scale, col, valid);
+    if (HAS_H)
+        next = param8(a.next_gamma, col, valid);
     const T *x = static_cast<const T *>(a.x), *y = static_cast<const T *>(a.y), *gate = static_cast<const T *>(a.gate);
     T *out = static_cast<T *>(a.out), *h = static_cast<T *>(a.h);
-    for (int64_t base = int64_t(blockIdx.x) * per; base < rows; base += int64_t(gridDim.x) * per) {
+    // the next row's maps are on their way while this one's are summed
+    Raw<T> nx, ny;
+    auto fetch = [&](int64_t row) {
+        const int v = row < rows ? valid : 0;
+        nx = load_raw(x, row * reals + col, v, whole);
+        if (HAS_Y)
+            ny = load_raw(y, row * reals + col, v, whole);
+    };
+    const int64_t step = int64_t(gridDim.x) * per;
+    fetch(int64_t(blockIdx.x) * per + l.row);
+    for (int64_t base = int64_t(blockIdx.x) * per; base < rows; base += step) {
         const int64_t row = base + l.row;
-        const bool here = row < rows;
-        const int64_t at = (here ? row : 0) * reals;
-        f32x8 xv[CH], yv[CH];
-#pragma unroll
-        for (int k = 0; k < CH; ++k) {
-            const int v = here ? valid[k] : 0;
-            xv[k] = load8(x + at + 8 * l.chunk(k), v, whole);
-            if (HAS_Y)
-                yv[k] = load8(y + at + 8 * l.chunk(k), v, whole);
-        }
+        const int v = row < rows ? valid : 0;
+        const int64_t at = row * reals + col;
+        f32x8 xv = nx.get(), yv;
+        if (HAS_Y)
+            yv = ny.get();
+        fetch(row + step);
         if (HAS_Y) {
             float r = 1.0f;
             if (normed) {
-                float s[1] = {0.0f};
-#pragma unroll
-                for (int k = 0; k < CH; ++k)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        s[0] = fmaf(yv[k][e], yv[k][e], s[0]);
+                float s[1] = {dot8(yv, yv)};
                 row_sums<BLOCK>(s, lpr, lds);
-                r = 1.0f / sqrtf(fmaf(s[0], mean, eps));
+                r = inv_sqrt(fmaf(s[0], mean, eps));
             }
-#pragma unroll
-            for (int k = 0; k < CH; ++k) {
-                const int v = here ? valid[k] : 0;
-                f32x8 z = yv[k] * r * f[k];
-                if (drop.cut) {
-                    const Mask m = mask8(unsigned(l.chunk(k)), unsigned(row), seed, offset, drop);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        z[e] = m.apply(z[e], e);
-                }
-                if (gate != nullptr) {
-                    const int64_t img = here ? fast_div(int(row), by_hw) : 0;
-                    z *= load8(gate + img * reals + 8 * l.chunk(k), v, whole);
-                }
-                xv[k] += z;
-                store8(out + at + 8 * l.chunk(k), xv[k], v, whole);
+            f32x8 z = yv * r * f;
+            if (drop.cut)
+                drop8(z, unsigned(l.chunk), unsigned(row), seed, offset, drop);
+            if (gate != nullptr) {
+                const int64_t img = row < rows ? fast_div(int(row), by_hw) : 0;
+                z *= load8(gate, img * reals + col, v, whole);
             }
+            xv += z;
+            store8(out + at, xv, v, whole);
         }
         if (HAS_H) {
-            float s[1] = {0.0f};
-#pragma unroll
-            for (int k = 0; k < CH; ++k)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    s[0] = fmaf(xv[k][e], xv[k][e], s[0]);
+            float s[1] = {dot8(xv, xv)};
             row_sums<BLOCK>(s, lpr, lds);
-            const float r = 1.0f / sqrtf(fmaf(s[0], mean, eps));
-#pragma unroll
-            for (int k = 0; k < CH; ++k)
-                store8(h + at + 8 * l.chunk(k), xv[k] * r * next[k], here ? valid[k] : 0, whole);
+            store8(h + at, xv * inv_sqrt(fmaf(s[0], mean, eps)) * next, v, whole);
         }
     }
 }
@@ -266,12 +282,12 @@ residual_forward_kernel(int64_t rows, FastDiv by_hw, int reals, int lpr, bool wh
 
 // How a gradient's rows are dealt to work-groups: `bpi` work-groups share each
 // image (of `n` with `hw` rows; all rows are one image where no gate asks for
-// sums by image), or a work-group takes `ipb` images.  Each writes the sums of
-// its rows, image by image, to part[(image * bpi + b) * 2 * reals].
+// sums by image) and take its rows in turn, or a work-group takes `ipb` images.
+// Each writes the sums of its rows, image by image, to part[(image * bpi + b) *
+// 2 * reals].
 struct Deal {
     int64_t n, hw;
     int bpi, ipb, grid;
-    int64_t rows;  // of a work-group in an image
 };
 
 // With G the whole gradient at out (dout and the norm's of dh), m dropout's
@@ -280,15 +296,15 @@ struct Deal {
 //   Q[image] = sum over rows of G m yhat,  N = sum over rows of dh out / rms(out);
 // Q carries the gradients of gate, scale and gamma, N that of next_gamma.
 // Bound by HBM: four maps read and two written, 12 bytes per real in bf16.
-template <typename T, int CH, bool BLOCK, bool HAS_Y, bool HAS_H>
-__global__ void __launch_bounds__(kThreads)
+template <typename T, bool BLOCK, bool HAS_Y, bool HAS_H>
+__global__ void __launch_bounds__(BLOCK ? kBlockThreads : kThreads)
 residual_backward_kernel(Deal deal, int reals, int lpr, bool whole, ResidualBackward a, Drop drop, float eps,
                          float *__restrict__ part)
 {
-    __shared__ float lds[2 * kWaves];
-    __shared__ float cols[BLOCK ? 1 : kWaves * CH * 512];
+    __shared__ float lds[2 * kBlockWaves];
+    __shared__ float cols[BLOCK ? 1 : kWaves * 512];
     const Lane l(lpr, BLOCK);
-    const int per = BLOCK ? 1 : kThreads / lpr;
+    const int per = BLOCK ? 1 : kThreads / lpr, col = 8 * l.chunk, valid = l.valid(reals);
     const float mean = 1.0f / float(reals);
     const bool normed = HAS_Y && a.gamma != nullptr;
     uint64_t seed = 0, offset = 0;
@@ -296,17 +312,11 @@ residual_backward_kernel(Deal deal, int reals, int lpr, bool whole, ResidualBack
         seed = drop.rng[0];
         offset = drop.rng[1];
     }
-    f32x8 f[CH], next[CH];
-    int valid[CH];
-#pragma unroll
-    for (int k = 0; k < CH; ++k) {
-        valid[k] = l.valid(k, reals);
-        const int col = 8 * l.chunk(k);
-        if (HAS_Y)
-            f[k] = param8(a.gamma, col, valid[k]) * param8(a.scale, col, valid[k]);
-        if (HAS_H)
-            next[k] = param8(a.next_gamma, col, valid[k]);
-    }
+    f32x8 f, next;
+    if (HAS_Y)
+        f = param8(a.gamma, col, valid) * param8(a.scale, col, valid);
+    if (HAS_H)
+        next = param8(a.next_gamma, col, valid);
     const T *y = static_cast<const T *>(a.y), *dout = static_cast<const T *>(a.dout);
     const T *out = static_cast<const T *>(a.out), *dh = static_cast<const T *>(a.dh);
     const T *gate = static_cast<const T *>(a.gate);
@@ -315,96 +325,51 @@ residual_backward_kernel(Deal deal, int reals, int lpr, bool whole, ResidualBack
     const int64_t img0 = int64_t(blockIdx.x) / deal.bpi * deal.ipb;
     const int64_t b = int64_t(blockIdx.x) % deal.bpi;
     for (int64_t img = img0; img < img0 + deal.ipb && img < deal.n; ++img) {
-        f32x8 acc_q[CH], acc_n[CH], fg[CH];
-#pragma unroll
-        for (int k = 0; k < CH; ++k) {
-            acc_q[k] = 0.0f;
-            acc_n[k] = 0.0f;
-            if (HAS_Y) {
-                fg[k] = f[k];
-                if (gate != nullptr)
-                    fg[k] *= load8(gate + img * reals + 8 * l.chunk(k), valid[k], whole);
-            }
+        f32x8 acc_q = 0.0f, acc_n = 0.0f, fg = 1.0f;
+        if (HAS_Y) {
+            fg = f;
+            if (gate != nullptr)
+                fg *= load8(gate, img * reals + col, valid, whole);
         }
-        const int64_t last = min((b + 1) * deal.rows, deal.hw);
-        for (int64_t base = b * deal.rows; base < last; base += per) {
-            const bool here = base + l.row < last;
-            const int64_t row = img * deal.hw + (here ? base + l.row : 0);
-            const int64_t at = row * reals;
-            f32x8 yv[CH], g[CH], ov[CH], hv[CH];
-#pragma unroll
-            for (int k = 0; k < CH; ++k) {
-                const int v = here ? valid[k] : 0;
-                const int64_t p = at + 8 * l.chunk(k);
-                if (HAS_H) {
-                    ov[k] = load8(out + p, v, whole);
-                    hv[k] = load8(dh + p, v, whole);
-                }
-                if (HAS_Y)
-                    yv[k] = load8(y + p, v, whole);
-                if (dout != nullptr)
-                    g[k] = load8(dout + p, v, whole);
-                else
-                    g[k] = 0.0f;
+        for (int64_t base = b * per; base < deal.hw; base += int64_t(deal.bpi) * per) {
+            const int v = base + l.row < deal.hw ? valid : 0;
+            const int64_t row = img * deal.hw + base + l.row, at = row * reals + col;
+            f32x8 yv, g = 0.0f, ov, hv;
+            if (HAS_H) {
+                ov = load8(out, at, v, whole);
+                hv = load8(dh, at, v, whole);
             }
+            if (HAS_Y)
+                yv = load8(y, at, v, whole);
+            if (dout != nullptr)
+                g = load8(dout, at, v, whole);
             float s[3] = {0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int k = 0; k < CH; ++k)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    if (HAS_Y)
-                        s[0] = fmaf(yv[k][e], yv[k][e], s[0]);
-                    if (HAS_H) {
-                        s[1] = fmaf(ov[k][e], ov[k][e], s[1]);
-                        s[2] = fmaf(hv[k][e] * next[k][e], ov[k][e], s[2]);
-                    }
-                }
+            if (HAS_Y)
+                s[0] = dot8(yv, yv);
+            if (HAS_H) {
+                s[1] = dot8(ov, ov);
+                s[2] = dot8(hv * next, ov);
+            }
             row_sums3<BLOCK, HAS_Y, HAS_H>(s, lpr, lds);
             if (HAS_H) {
-                const float r = 1.0f / sqrtf(fmaf(s[1], mean, eps));
-                const float t = s[2] * mean * r * r;
-#pragma unroll
-                for (int k = 0; k < CH; ++k)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float hat = ov[k][e] * r;
-                        acc_n[k][e] = fmaf(hv[k][e], hat, acc_n[k][e]);
-                        g[k][e] += r * hv[k][e] * next[k][e] - hat * t;
-                    }
+                const float r = inv_sqrt(fmaf(s[1], mean, eps));
+                const f32x8 hat = ov * r;
+                acc_n += hv * hat;
+                g += hv * next * r - hat * (s[2] * mean * r * r);
             }
-#pragma unroll
-            for (int k = 0; k < CH; ++k)
-                store8(dx + at + 8 * l.chunk(k), g[k], here ? valid[k] : 0, whole);
+            store8(dx + at, g, v, whole);
             if (HAS_Y) {
-                const float r = normed ? 1.0f / sqrtf(fmaf(s[0], mean, eps)) : 1.0f;
-                float t[1] = {0.0f};
-#pragma unroll
-                for (int k = 0; k < CH; ++k) {
-                    if (drop.cut) {
-                        const Mask m = mask8(unsigned(l.chunk(k)), unsigned(row), seed, offset, drop);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            g[k][e] = m.apply(g[k][e], e);
-                    }
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        acc_q[k][e] = fmaf(g[k][e], yv[k][e] * r, acc_q[k][e]);
-                        g[k][e] *= fg[k][e];
-                        t[0] = fmaf(g[k][e], yv[k][e], t[0]);
-                    }
-                }
+                const float r = normed ? inv_sqrt(fmaf(s[0], mean, eps)) : 1.0f;
+                if (drop.cut)
+                    drop8(g, unsigned(l.chunk), unsigned(row), seed, offset, drop);
+                acc_q += g * (yv * r);
+                g *= fg;
                 if (normed) {
+                    float t[1] = {dot8(g, yv)};
                     row_sums<BLOCK>(t, lpr, lds);
-                    const float c = t[0] * mean * r * r * r;
-#pragma unroll
-                    for (int k = 0; k < CH; ++k)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            g[k][e] = r * g[k][e] - yv[k][e] * c;
+                    g = g * r - yv * (t[0] * mean * r * r * r);
                 }
-#pragma unroll
-                for (int k = 0; k < CH; ++k)
-                    store8(dy + at + 8 * l.chunk(k), g[k], here ? valid[k] : 0, whole);
+                store8(dy + at, g, v, whole);
             }
         }
         // the work-group's sums of the image, in a fixed order
@@ -413,32 +378,29 @@ residual_backward_kernel(Deal deal, int reals, int lpr, bool whole, ResidualBack
         for (int which = 0; which < 2; ++which) {
             if (which == 0 ? !HAS_Y : !HAS_H)
                 continue;
+            const f32x8 acc = which == 0 ? acc_q : acc_n;
             if (BLOCK) {
 #pragma unroll
-                for (int k = 0; k < CH; ++k)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (e < valid[k])
-                            dst[which * reals + 8 * l.chunk(k) + e] = which == 0 ? acc_q[k][e] : acc_n[k][e];
+                for (int e = 0; e < 8; ++e)
+                    if (e < valid)
+                        dst[which * reals + col + e] = acc[e];
                 continue;
             }
             __syncthreads();  // cols has been read
 #pragma unroll
-            for (int k = 0; k < CH; ++k)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float v = which == 0 ? acc_q[k][e] : acc_n[k][e];
-                    for (int m = lpr; m < 64; m <<= 1)
-                        v += __shfl_xor(v, m, 64);
-                    if ((threadIdx.x & 63) < unsigned(lpr))
-                        cols[(threadIdx.x >> 6) * CH * 512 + 8 * l.chunk(k) + e] = v;
-                }
+            for (int e = 0; e < 8; ++e) {
+                float v = acc[e];
+                for (int m = lpr; m < 64; m <<= 1)
+                    v += __shfl_xor(v, m, 64);
+                if ((threadIdx.x & 63) < unsigned(lpr))
+                    cols[(threadIdx.x >> 6) * 512 + col + e] = v;
+            }
             __syncthreads();
             for (int c = threadIdx.x; c < reals; c += kThreads) {
                 float v = 0.0f;
 #pragma unroll
                 for (int w = 0; w < kWaves; ++w)
-                    v += cols[w * CH * 512 + c];
+                    v += cols[w * 512 + c];
                 dst[which * reals + c] = v;
             }
         }
@@ -525,20 +487,16 @@ template <typename T>
 __global__ void __launch_bounds__(kThreads)
 dropout_kernel(int64_t rows, int reals, int lpr, bool whole, const T *__restrict__ x, T *__restrict__ out, Drop drop)
 {
-    const Lane l(lpr, false);
+    const int first = threadIdx.x & (lpr - 1);
     const int per = kThreads / lpr, chunks = (reals + 7) / 8;
     const uint64_t seed = drop.cut ? drop.rng[0] : 0, offset = drop.cut ? drop.rng[1] : 0;
-    for (int64_t row = int64_t(blockIdx.x) * per + l.row; row < rows; row += int64_t(gridDim.x) * per)
-        for (int c = l.at; c < chunks; c += lpr) {
+    for (int64_t row = int64_t(blockIdx.x) * per + threadIdx.x / lpr; row < rows; row += int64_t(gridDim.x) * per)
+        for (int c = first; c < chunks; c += lpr) {
             const int v = min(8, reals - 8 * c);
             const int64_t p = row * reals + 8 * c;
-            f32x8 t = load8(x + p, v, whole);
-            if (drop.cut) {
-                const Mask m = mask8(unsigned(c), unsigned(row), seed, offset, drop);
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    t[e] = m.apply(t[e], e);
-            }
+            f32x8 t = load8(x, p, v, whole);
+            if (drop.cut)
+                drop8(t, unsigned(c), unsigned(row), seed, offset, drop);
             store8(out + p, t, v, whole);
         }
 }
@@ -554,29 +512,37 @@ int lanes_per_row(int reals)
     return l;
 }
 
-// Rows of up to 1024 reals are a wave's, wider ones a work-group's.
+// Rows of up to 512 reals are a wave's or a part of one's, wider ones a
+// work-group's of as many waves as they have chunks for.
 bool block_rows(int reals)
 {
-    return reals > 1024;
+    return reals > 512;
 }
+int group_threads(int reals)
+{
+    return !block_rows(reals) ? kThreads : reals <= 1024 ? 128 : reals <= 2048 ? 256 : kBlockThreads;
+}
+static_assert(4 * kRowsMaxChannels <= 8 * kBlockThreads, "a work-group holds the widest row");
 
-// The work-groups that the chip holds at once, several times over, so that
-// the last round is short.
+// The work-groups that the chip holds at once, forward several times over, so
+// that the last round is short.  (A gradient's have partial sums to write: one
+// time over.)
 constexpr int kForwardGroups = 256 * 8;
-constexpr int kBackwardGroups = 256 * 4;
+int backward_groups(int reals)
+{
+    return 256 * 1024 / group_threads(reals);
+}
 
 Deal deal_rows(const RowsGeom &g, bool by_image)
 {
     Deal d;
     d.n = by_image ? g.n : 1;
     d.hw = by_image ? g.hw : g.n * g.hw;
-    const int reals = 4 * g.c;
+    const int reals = 4 * g.c, groups = backward_groups(reals);
     const int per = block_rows(reals) ? 1 : kThreads / lanes_per_row(reals);
     const int64_t most = (d.hw + per - 1) / per;
-    d.bpi = int(std::max<int64_t>(1, std::min<int64_t>(kBackwardGroups / std::max<int64_t>(1, d.n), most)));
-    d.ipb = int((d.n + kBackwardGroups - 1) / kBackwardGroups);
-    d.rows = ((most + d.bpi - 1) / d.bpi) * per;
-    d.bpi = int((d.hw + d.rows - 1) / d.rows);
+    d.bpi = int(std::max<int64_t>(1, std::min<int64_t>(groups / d.n, most)));
+    d.ipb = int((d.n + groups - 1) / groups);
     d.grid = int((d.n + d.ipb - 1) / d.ipb) * d.bpi;
     return d;
 }
@@ -590,14 +556,10 @@ hipError_t forward_launch(const RowsGeom &g, const ResidualForward &a, const Dro
     const int per = block_rows(reals) ? 1 : kThreads / lpr;
     const dim3 grid(unsigned(std::min<int64_t>((rows + per - 1) / per, kForwardGroups)));
     const FastDiv by(int(g.hw));
-    if (reals <= 512)
-        residual_forward_kernel<T, 1, false, HAS_Y, HAS_H><<<grid, kThreads, 0, s>>>(rows, by, reals, lpr, whole, a, drop, eps);
-    else if (reals <= 1024)
-        residual_forward_kernel<T, 2, false, HAS_Y, HAS_H><<<grid, kThreads, 0, s>>>(rows, by, reals, lpr, whole, a, drop, eps);
-    else if (reals <= 2048)
-        residual_forward_kernel<T, 1, true, HAS_Y, HAS_H><<<grid, kThreads, 0, s>>>(rows, by, reals, lpr, whole, a, drop, eps);
+    if (block_rows(reals))
+        residual_forward_kernel<T, true, HAS_Y, HAS_H><<<grid, group_threads(reals), 0, s>>>(rows, by, reals, lpr, whole, a, drop, eps);
     else
-        residual_forward_kernel<T, 2, true, HAS_Y, HAS_H><<<grid, kThreads, 0, s>>>(rows, by, reals, lpr, whole, a, drop, eps);
+        residual_forward_kernel<T, false, HAS_Y, HAS_H><<<grid, kThreads, 0, s>>>(rows, by, reals, lpr, whole, a, drop, eps);
     return hipGetLastError();
 }
 
@@ -609,14 +571,10 @@ hipError_t backward_launch(const RowsGeom &g, const ResidualBackward &a, const D
     const bool whole = reals % 8 == 0;
     const Deal d = deal_rows(g, a.gate != nullptr);
     float *part = static_cast<float *>(work);
-    if (reals <= 512)
-        residual_backward_kernel<T, 1, false, HAS_Y, HAS_H><<<d.grid, kThreads, 0, s>>>(d, reals, lpr, whole, a, drop, eps, part);
-    else if (reals <= 1024)
-        residual_backward_kernel<T, 2, false, HAS_Y, HAS_H><<<d.grid, kThreads, 0, s>>>(d, reals, lpr, whole, a, drop, eps, part);
-    else if (reals <= 2048)
-        residual_backward_kernel<T, 1, true, HAS_Y, HAS_H><<<d.grid, kThreads, 0, s>>>(d, reals, lpr, whole, a, drop, eps, part);
+    if (block_rows(reals))
+        residual_backward_kernel<T, true, HAS_Y, HAS_H><<<d.grid, group_threads(reals), 0, s>>>(d, reals, lpr, whole, a, drop, eps, part);
     else
-        residual_backward_kernel<T, 2, true, HAS_Y, HAS_H><<<d.grid, kThreads, 0, s>>>(d, reals, lpr, whole, a, drop, eps, part);
+        residual_backward_kernel<T, false, HAS_Y, HAS_H><<<d.grid, kThreads, 0, s>>>(d, reals, lpr, whole, a, drop, eps, part);
     if (hipError_t e = hipGetLastError())
         return e;
     if (a.dgate == nullptr && a.dgamma == nullptr && a.dscale == nullptr && a.dnext_gamma == nullptr)
@@ -624,7 +582,7 @@ hipError_t backward_launch(const RowsGeom &g, const ResidualBackward &a, const D
     const int64_t entries = a.gate != nullptr ? d.n : d.bpi;
     const dim3 grid(unsigned((reals + kCols - 1) / kCols));
     if (a.gate != nullptr && d.bpi > 1) {
-        // (bpi > 1 only where n < kBackwardGroups: n fits the grid)
+        // (bpi > 1 only where n < backward_groups: n fits the grid)
         double *sums = reinterpret_cast<double *>(part + d.n * d.bpi * 2 * reals);
         image_sums_kernel<<<dim3(unsigned((2 * reals + kCols - 1) / kCols), unsigned(d.n)), kThreads, 0, s>>>(
             part, sums, d.bpi, reals);
@@ -655,10 +613,10 @@ hipError_t residual_forward_run(const RowsGeom &g, DType dt, const ResidualForwa
 size_t residual_backward_work_bytes(const RowsGeom &g, const ResidualBackward &a)
 {
     // enough for every smaller batch and map: n images take at most
-    // max(n, kBackwardGroups) rows of partial sums, and of sums by image
+    // max(n, backward_groups) rows of partial sums, and of sums by image
     const size_t row = size_t(8) * g.c, n = a.gate != nullptr ? size_t(g.n) : 1;
-    return (std::max<size_t>(n, kBackwardGroups) * sizeof(float) +
-            std::min<size_t>(n, kBackwardGroups) * sizeof(double)) * row;
+    const size_t groups = size_t(backward_groups(4 * g.c));
+    return (std::max(n, groups) * sizeof(float) + std::min(n, groups) * sizeof(double)) * row;
 }
 
 hipError_t residual_backward_run(const RowsGeom &g, DType dt, const ResidualBackward &a, const Drop &drop, float eps,
