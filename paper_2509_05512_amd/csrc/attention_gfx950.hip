@@ -30,7 +30,7 @@ struct Forward {
 // by the rows' sums of dout out, and with probabilities of 8 bits alone 3e-4 of
 // its norm was wrong (1e-6 with both parts).
 template <typename T, int DQP, int MODE, int NW, bool EXACT>
-__global__ void __launch_bounds__(64 * NW, DQP <= 16 ? 2 : 1) attention_forward_kernel(Forward f)
+__global__ void __launch_bounds__(64 * NW, 2) attention_forward_kernel(Forward f)
 {
     constexpr int DP = 4 * DQP, kThreads = 64 * NW, kQueries = 32 * NW;
     typedef Stage<T, DP, kThreads> Tile;
@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(64 * NW, DQP <= 16 ? 2 : 1) attention_forward_
     const int first = split * f.tiles_per_split * KT;
     const int end = min(len, first + f.tiles_per_split * KT);
 
-    const HeadMap<const T, DQP> qm(f.a.q, img, head, g.dq), km(f.a.k, img, kv_head, g.dq), vm(f.a.v, img, kv_head, g.dq);
+    const WholeMap<T, DQP> qm(f.a.q, img, head), km(f.a.k, img, kv_head), vm(f.a.v, img, kv_head);
     frag q[DP / 16];
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i)
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(64 * NW, DQP <= 16 ? 2 : 1) attention_forward_
     }
     if (f.rest != nullptr && sizeof(T) == 2) {
         const int64_t c_all = int64_t(g.heads) * g.dq;
-        const AttnMap dense{f.rest, lq * 4 * c_all, 4 * c_all, c_all, f.out.vec && g.dq % 8 == 0};
+        const AttnMap dense{f.rest, lq * 4 * c_all, 4 * c_all, c_all, g.dq % 8 == 0, g.dq};
         const HeadMap<T, DQP> rm(dense, img, head, g.dq);
 #pragma unroll
         for (int i = 0; i < DP / 32; ++i) {
@@ -344,14 +344,14 @@ __global__ void __launch_bounds__(256) attention_token_kernel(Forward f, Token t
     const int head0 = kv_head * group + gb * GRP;  // of GRP query heads
     const int heads_here = min(GRP, group - gb * GRP);
 
-    const HeadMap<const T, DQP> km(f.a.k, img, active ? kv_head : 0, g.dq), vm(f.a.v, img, active ? kv_head : 0, g.dq);
+    const HeadMap<T, DQP> km(f.a.k, img, active ? kv_head : 0, g.dq), vm(f.a.v, img, active ? kv_head : 0, g.dq);
     f32x8 q[GRP], o[GRP];
     float top[GRP], sum[GRP];
     const float c = g.scale * kLog2e;
 #pragma unroll
     for (int i = 0; i < GRP; ++i) {
         const bool here = active && i < heads_here;
-        const HeadMap<const T, DQP> qm(f.a.q, img, here ? head0 + i : 0, g.dq);
+        const HeadMap<T, DQP> qm(f.a.q, img, here ? head0 + i : 0, g.dq);
         q[i] = to_f32(qm.load(0, d, here)) * c;
         o[i] = 0.0f;
         top[i] = -INFINITY;
@@ -487,11 +487,6 @@ __global__ void __launch_bounds__(256) attention_token_kernel(Forward f, Token t
 
 // ---------------------------------------------------------------------- host
 
-int padded_dq(int dq)
-{
-    return dq <= 8 ? 8 : dq <= 16 ? 16 : 32;
-}
-
 struct Plan {
     int waves, blocks, splits, tiles_per_split, cap;
     size_t lds;
@@ -612,9 +607,74 @@ template <typename T> hipError_t forward_dq(const Forward &f, const Plan &p, hip
     }
 }
 
+// One chunk of 8 reals per thread of the maps that are copied.
+template <typename T, int DQP> __global__ void __launch_bounds__(256) attention_pack_kernel(AttnPack p, int n, int dq)
+{
+    constexpr int DP = 4 * DQP, kChunks = DP / 8;
+    int64_t id = int64_t(blockIdx.x) * 256 + threadIdx.x;
+#pragma unroll
+    for (int m = 0; m < AttnPack::kMaps; ++m) {
+        if (m >= p.maps)
+            return;
+        const int64_t count = int64_t(n) * p.heads[m] * p.tokens[m] * kChunks;
+        if (id < count) {
+            const int d = 8 * int(id % kChunks);
+            const int64_t row = id / kChunks;
+            const int token = int(row % p.tokens[m]), head = int(row / p.tokens[m] % p.heads[m]);
+            const HeadMap<T, DQP> src(p.src[m], row / p.tokens[m] / p.heads[m], head, dq);
+            *reinterpret_cast<typename Elem<T>::frag *>(static_cast<T *>(p.dst[m]) + row * DP + d) = src.load(token, d, true);
+            return;
+        }
+        id -= count;
+    }
+}
+
+size_t packed_bytes(int n, int heads, int tokens, int dq, DType dt)
+{
+    return size_t(n) * heads * tokens * 4 * padded_dq(dq) * (dt == DType::BF16 ? 2 : 4);
+}
+
+bool whole_maps(const AttnCall &a)
+{
+    return a.q.vec && a.k.vec && a.v.vec && padded_dq(a.g.dq) == a.g.dq;
+}
+
 }  // namespace
 
+hipError_t attention_pack_run(const AttnPack &p, int n, int dq, DType dt, hipStream_t s)
+{
+    const int dqp = padded_dq(dq);
+    int64_t chunks = 0;
+    for (int m = 0; m < p.maps; ++m)
+        chunks += int64_t(n) * p.heads[m] * p.tokens[m] * (dqp / 2);
+    const unsigned grid = unsigned((chunks + 255) / 256);
+    if (dt == DType::BF16) {
+        if (dqp == 8)
+            attention_pack_kernel<__bf16, 8><<<grid, 256, 0, s>>>(p, n, dq);
+        else if (dqp == 16)
+            attention_pack_kernel<__bf16, 16><<<grid, 256, 0, s>>>(p, n, dq);
+        else
+            attention_pack_kernel<__bf16, 32><<<grid, 256, 0, s>>>(p, n, dq);
+    } else {
+        if (dqp == 8)
+            attention_pack_kernel<float, 8><<<grid, 256, 0, s>>>(p, n, dq);
+        else if (dqp == 16)
+            attention_pack_kernel<float, 16><<<grid, 256, 0, s>>>(p, n, dq);
+        else
+            attention_pack_kernel<float, 32><<<grid, 256, 0, s>>>(p, n, dq);
+    }
+    return hipGetLastError();
+}
+
 size_t attention_forward_work_bytes(const AttnCall &a, DType dt)
+{
+    const AttnGeom &g = a.g;
+    if (g.lq() == 1 || whole_maps(a))
+        return 0;
+    return packed_bytes(g.n, g.heads, g.lq(), g.dq, dt) + 2 * packed_bytes(g.n, g.kv_heads, g.lk(), g.dq, dt);
+}
+
+size_t attention_forward_extra_bytes(const AttnCall &a, DType dt)
 {
     const Plan p = forward_plan(a, dt);
     if (p.splits == 1)
@@ -624,12 +684,31 @@ size_t attention_forward_work_bytes(const AttnCall &a, DType dt)
 }
 
 hipError_t attention_forward_run(const AttnCall &a, DType dt, const AttnMap &out, void *rest, float *stats, void *work,
-                                 hipStream_t s)
+                                 void *extra, hipStream_t s)
 {
-    const Plan p = forward_plan(a, dt, work != nullptr);
+    const Plan p = forward_plan(a, dt, extra != nullptr);
+    const AttnGeom &g = a.g;
     Forward f;
     f.a = a;
-    f.o = make_offsets(a.g);
+    if (work != nullptr) {
+        AttnPack pack;
+        unsigned char *at = static_cast<unsigned char *>(work);
+        pack.maps = 0;
+        for (AttnMap *m : {&f.a.q, &f.a.k, &f.a.v}) {
+            const bool q = m == &f.a.q;
+            const int i = pack.maps++;
+            pack.src[i] = *m;
+            pack.heads[i] = q ? g.heads : g.kv_heads;
+            pack.tokens[i] = q ? g.lq() : g.lk();
+            pack.dst[i] = at;
+            const int64_t d = 4 * padded_dq(g.dq);
+            *m = {at, pack.heads[i] * pack.tokens[i] * d, d, d / 4, true, pack.tokens[i] * d};
+            at += packed_bytes(g.n, pack.heads[i], pack.tokens[i], g.dq, dt);
+        }
+        if (hipError_t e = attention_pack_run(pack, g.n, g.dq, dt, s))
+            return e;
+    }
+    f.o = make_offsets(g);
     f.o.cap = p.cap;
     f.out = out;
     f.rest = rest;
@@ -637,8 +716,8 @@ hipError_t attention_forward_run(const AttnCall &a, DType dt, const AttnMap &out
     f.blocks = p.blocks;
     f.splits = p.splits;
     f.tiles_per_split = p.tiles_per_split;
-    f.part = static_cast<float *>(work);
-    f.part_stats = f.part + (p.splits > 1 ? size_t(p.splits) * a.g.n * a.g.heads * a.g.lq() * 4 * padded_dq(a.g.dq) : 0);
+    f.part = static_cast<float *>(extra);
+    f.part_stats = f.part + (p.splits > 1 ? size_t(p.splits) * g.n * g.heads * g.lq() * 4 * padded_dq(g.dq) : 0);
     return dt == DType::BF16 ? forward_dq<__bf16>(f, p, s) : forward_dq<float>(f, p, s);
 }
 

@@ -6,8 +6,10 @@
 //   dtable[head][b] = sum of dS over the pairs of pixels in bucket b.
 // Two launches, so that every sum has one owner and a fixed order: the first
 // takes blocks of queries and walks over the keys (dQ, delta, and the sums of
-// dS by offset), the second blocks of keys and walks over the queries (dK, dV).
-// Two more small ones bring the sums by offset to buckets, in fp64.
+// dS by offset), the second blocks of keys and walks over the queries of the
+// heads that share them (dK, dV).  Where there are few blocks, several
+// work-groups share a block's walk, and a third launch adds up their results.
+// One or two more bring the sums by offset to buckets, in fp64.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -20,12 +22,14 @@ namespace {
 struct Backward {
     AttnCall a;
     Offsets o;
-    AttnMap out, dout, dq, dk, dv;
-    const void *rest;
+    AttnMap out, rest, dout, dq, dk, dv;  // (rest.data may be NULL)
     const float *stats;
     float *delta;    // [n][heads][lq]
-    float *offsets;  // [n * heads * blocks][range] sums of dS by offset, NULL: none asked for
+    float *offsets;  // [n * heads * blocks][q_splits][range] sums of dS by offset, NULL: none asked for
     int blocks, range;
+    // work-groups that share a block of queries, of keys; the tiles of each
+    int q_splits, k_splits, q_tiles, k_tiles;
+    float *part_q, *part_k, *part_v;  // [split][row][D] where shared
 };
 
 constexpr int kWaves = 4, kThreads = 64 * kWaves, kQueries = 32 * kWaves;
@@ -83,6 +87,21 @@ template <typename F, int N> __device__ __forceinline__ float chunk_top(const F 
     return __uint_as_float(v);
 }
 
+// A D x 32 tile of accumulators, transposed, to a row of fp32.
+template <int DP>
+__device__ __forceinline__ void store_part(float *dst, const f32x16 (&v)[DP / 32], int half, bool here)
+{
+    if (!here)
+        return;
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4 t = {v[i][4 * g], v[i][4 * g + 1], v[i][4 * g + 2], v[i][4 * g + 3]};
+            *reinterpret_cast<f32x4 *>(dst + 32 * i + 8 * g + 4 * half) = t;
+        }
+}
+
 // The launch of the queries' side.  Sums of dS by offset are gathered over the
 // segment whose biases are staged; as the walk leaves it they go, over the
 // waves, to the work-group's own row of `offsets`.
@@ -102,33 +121,35 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
 
     const AttnGeom &g = f.a.g;
     const int lq = g.lq(), lk = g.lk();
-    const int total = g.n * g.heads * f.blocks;
-    const int id = xcd_order(total);
+    const int total = g.n * g.heads * f.blocks * f.q_splits;
+    int id = xcd_order(total);
     if (id >= total)
         return;
-    const int block = id % f.blocks, head = id / f.blocks % g.heads, img = id / f.blocks / g.heads;
+    const int block = id % f.blocks;
+    id /= f.blocks;
+    const int split = id % f.q_splits;
+    id /= f.q_splits;
+    const int head = id % g.heads, img = id / g.heads;
     const int kv_head = head / (g.heads / g.kv_heads);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
     const int q0 = block * kQueries, query = q0 + 32 * wave + (lane & 31);
     const bool q_here = query < lq;
-    const int end = f.a.kv_len != nullptr ? min(max(f.a.kv_len[img], 0), lk) : lk;
+    const int len = f.a.kv_len != nullptr ? min(max(f.a.kv_len[img], 0), lk) : lk;
+    const int begin = split * f.q_tiles * KT, end = min(len, begin + f.q_tiles * KT);
     const int64_t row = (int64_t(img) * g.heads + head) * lq + query;
 
-    const HeadMap<const T, DQP> qm(f.a.q, img, head, g.dq), km(f.a.k, img, kv_head, g.dq), vm(f.a.v, img, kv_head, g.dq);
+    const WholeMap<T, DQP> qm(f.a.q, img, head), km(f.a.k, img, kv_head), vm(f.a.v, img, kv_head);
     frag q[DP / 16], go[DP / 16];
     float delta = 0.0f;
     {
-        const HeadMap<const T, DQP> gm(f.dout, img, head, g.dq), om(f.out, img, head, g.dq);
-        const int64_t c_all = int64_t(g.heads) * g.dq;
-        const AttnMap dense{f.rest, lq * 4 * c_all, 4 * c_all, c_all, f.out.vec && g.dq % 8 == 0};
-        const HeadMap<const T, DQP> rm(dense, img, head, g.dq);
+        const WholeMap<T, DQP> gm(f.dout, img, head), om(f.out, img, head), rm(f.rest, img, head);
 #pragma unroll
         for (int i = 0; i < DP / 16; ++i) {
             const int d = 16 * i + 8 * half;
             q[i] = qm.load(query, d, q_here);
             go[i] = gm.load(query, d, q_here);
             f32x8 o = to_f32(om.load(query, d, q_here));
-            if (f.rest != nullptr)
+            if (f.rest.data != nullptr)
                 o += to_f32(rm.load(query, d, q_here));
             const f32x8 w = to_f32(go[i]);
 #pragma unroll
@@ -136,7 +157,7 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
                 delta = fmaf(w[e], o[e], delta);
         }
         delta = half_sum(delta);
-        if (q_here && half == 0)
+        if (q_here && half == 0 && split == 0)
             f.delta[row] = delta;
     }
     // P = 2^(s - top) inv; rows without a key, and none, have P = 0
@@ -160,7 +181,7 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
         high_q = f.o.origin - place_q(f.o, q0);
         lane_at = f.o.origin - place_q(f.o, min(query, lq - 1));
         if (f.offsets != nullptr)
-            offsets = f.offsets + ((int64_t(img) * g.heads + head) * f.blocks + block) * f.range - low_q;
+            offsets = f.offsets + (((int64_t(img) * g.heads + head) * f.blocks + block) * f.q_splits + split) * f.range - low_q;
         done = low_q;
     }
     const int past = MODE != 0 ? high_q + place_k(f.o, lk - 1) + 1 : 0;  // past the last offset
@@ -193,32 +214,43 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
     }
     int units = kNoUnits;  // k of the array's units 2^-k
     double unit = 0.0;     // 2^k
-    // The segment's sums, added to the entries that an earlier one has written; a thread has the same entries modulo kThreads of every
-    // segment.
+    // Zeros to entries [from, to), and the segment's sums, added to the entries
+    // that an earlier one has written: a thread has the same entries modulo
+    // kThreads each time.
+    auto own = [&](int from) {
+        const int a = from - from % kThreads + int(threadIdx.x);
+        return a < from ? a + kThreads : a;
+    };
+    auto clear = [&](int from, int to) {
+        for (int a = own(from); a < to; a += kThreads)
+            offsets[a] = 0.0f;
+    };
     auto flush = [&]() {
         const int last = min(segment + f.o.cap, past);
-        int a = segment - segment % kThreads + int(threadIdx.x);
-        if (a < segment)
-            a += kThreads;
-        for (; a < last; a += kThreads) {
-            const int e = a - segment;
-            const float v = units == kBadUnits ? NAN : units == kNoUnits ? 0.0f : float(ldexp(double(sums[e]), -units));
+        const double back = __longlong_as_double((long long)(1023 - units) << 52);  // 2^-units
+        for (int a = own(segment); a < last; a += kThreads) {
+            const float v = units == kBadUnits ? NAN : units == kNoUnits ? 0.0f : float(double(sums[a - segment]) * back);
             offsets[a] = a < done ? offsets[a] + v : v;
         }
         done = max(done, last);
     };
+    // (entries of the keys before this work-group's)
+    if (MODE != 0 && offsets != nullptr && begin > 0) {
+        done = begin < end ? low_q + place_k(f.o, begin) : past;
+        clear(low_q, done);
+    }
 
     f32x16 dq[DP / 32];
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i)
         dq[i] = 0.0f;
     Tile kt, vt;
-    if (0 < end) {
-        kt.fetch(km, 0, end);
-        vt.fetch(vm, 0, end);
+    if (begin < end) {
+        kt.fetch(km, begin, end);
+        vt.fetch(vm, begin, end);
     }
     int buf = 0;
-    for (int j0 = 0; j0 < end; j0 += KT, buf ^= 1) {
+    for (int j0 = begin; j0 < end; j0 += KT, buf ^= 1) {
         T *kb = k_lds + buf * Tile::kElems, *vb = v_lds + buf * Tile::kElems;
         int *pl = place + buf * KT;
         kt.put(kb);
@@ -240,9 +272,10 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
                     __syncthreads();
                 }
                 segment = lo;
-                stage_bias(bias, f.o, f.a.bias, table, segment, f.o.cap, pos_y, pos_x);
+                const int count = min(f.o.cap, past + 3 - segment);  // (a quad may pass the last offset)
+                stage_bias(bias, f.o, f.a.bias, table, segment, count, pos_y, pos_x);
                 if (offsets != nullptr)
-                    for (int e = threadIdx.x; e < f.o.cap; e += kThreads)
+                    for (int e = threadIdx.x; e < count; e += kThreads)
                         sums[e] = 0;
             }
         }
@@ -271,7 +304,7 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
                         __syncthreads();
                     }
                     units = now;
-                    unit = ldexp(1.0, now);
+                    unit = __longlong_as_double((long long)(1023 + now) << 52);
                 }
             }
         }
@@ -309,23 +342,23 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
             }
         }
     }
-    const HeadMap<T, DQP> om(f.dq, img, head, g.dq);
+    if (f.q_splits > 1) {
+        const int64_t rows = int64_t(g.n) * g.heads * lq;
+        store_part<DP>(f.part_q + (split * rows + row) * DP, dq, half, q_here);
+    } else {
+        const HeadMap<T, DQP> om(f.dq, img, head, g.dq);
 #pragma unroll
-    for (int i = 0; i < DP / 32; ++i) {
-        dq[i] *= g.scale;
-        om.store(query, i, half, dq[i], q_here);
+        for (int i = 0; i < DP / 32; ++i) {
+            dq[i] *= g.scale;
+            om.store(query, i, half, dq[i], q_here);
+        }
     }
     if (MODE != 0 && offsets != nullptr) {
         if (segment >= 0) {
             __syncthreads();
             flush();
         }
-        // entries of offsets to keys that the image lacks
-        int a = done - done % kThreads + int(threadIdx.x);
-        if (a < done)
-            a += kThreads;
-        for (; a < past; a += kThreads)
-            offsets[a] = 0.0f;
+        clear(done, past);  // entries of keys that this work-group has not
     }
 }
 
@@ -347,17 +380,21 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dkv_ker
     const AttnGeom &g = f.a.g;
     const int lq = g.lq(), lk = g.lk(), group = g.heads / g.kv_heads;
     const int blocks = (lk + kQueries - 1) / kQueries;
-    const int total = g.n * g.kv_heads * blocks;
-    const int id = xcd_order(total);
+    const int total = g.n * g.kv_heads * blocks * f.k_splits;
+    int id = xcd_order(total);
     if (id >= total)
         return;
-    const int block = id % blocks, kv_head = id / blocks % g.kv_heads, img = id / blocks / g.kv_heads;
+    const int block = id % blocks;
+    id /= blocks;
+    const int split = id % f.k_splits;
+    id /= f.k_splits;
+    const int kv_head = id % g.kv_heads, img = id / g.kv_heads;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
     const int k0 = block * kQueries, key = k0 + 32 * wave + (lane & 31);
     const int end = f.a.kv_len != nullptr ? min(max(f.a.kv_len[img], 0), lk) : lk;
     const bool k_here = key < end;
 
-    const HeadMap<const T, DQP> km(f.a.k, img, kv_head, g.dq), vm(f.a.v, img, kv_head, g.dq);
+    const WholeMap<T, DQP> km(f.a.k, img, kv_head), vm(f.a.v, img, kv_head);
     frag k[DP / 16], v[DP / 16];
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i) {
@@ -381,177 +418,256 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dkv_ker
         high_k = f.o.origin + place_k(f.o, min(k0 + kQueries, lk) - 1);
         lane_at = f.o.origin + place_k(f.o, min(key, lk - 1));
     }
-    const int tiles = k0 < end ? (lq + QT - 1) / QT : 0;
-    for (int head = kv_head * group; head < (kv_head + 1) * group && tiles > 0; ++head) {
-        const HeadMap<const T, DQP> qm(f.a.q, img, head, g.dq), gm(f.dout, img, head, g.dq);
+    // The walk: tile by tile from the last, so that offsets ascend, head by head.
+    const int tiles = (lq + QT - 1) / QT, first = split * f.k_tiles;
+    const int last = k0 < end ? min(group * tiles, first + f.k_tiles) : first;
+    Tile qt, gt;
+    auto fetch = [&](int item) {
+        const int head = kv_head * group + item / tiles, i0 = (tiles - 1 - item % tiles) * QT;
+        qt.fetch(WholeMap<T, DQP>(f.a.q, img, head), i0, lq);
+        gt.fetch(WholeMap<T, DQP>(f.dout, img, head), i0, lq);
+    };
+    if (first < last)
+        fetch(first);
+    int segment = kNoSegment, buf = 0;
+    for (int item = first; item < last; ++item, buf ^= 1) {
+        const int head = kv_head * group + item / tiles, i0 = (tiles - 1 - item % tiles) * QT;
         const float *table = MODE != 0 ? f.a.bias.table + int64_t(head) * f.a.bias.ny * f.a.bias.nx : nullptr;
         const int64_t row0 = (int64_t(img) * g.heads + head) * lq;
-        int segment = kNoSegment, buf = 0;
-        Tile qt, gt;
-        __syncthreads();  // the last head's tiles and segment have been read
-        qt.fetch(qm, (tiles - 1) * QT, lq);
-        gt.fetch(gm, (tiles - 1) * QT, lq);
-        // from the last tile, so that offsets ascend
-        for (int tile = tiles - 1; tile >= 0; --tile, buf ^= 1) {
-            const int i0 = tile * QT;
-            T *qb = q_lds + buf * Tile::kElems, *gb = g_lds + buf * Tile::kElems;
-            int *pl = place + buf * QT;
-            float *rw = rows + buf * 3 * QT;
-            qt.put(qb);
-            gt.put(gb);
-            if (threadIdx.x < QT) {
-                const int i = i0 + threadIdx.x;
-                const float sum = i < lq ? f.stats[2 * (row0 + i) + 1] : 0.0f;
-                const bool empty = sum == 0.0f;
-                const float inv = empty ? 0.0f : 1.0f / sum;
-                rw[threadIdx.x] = empty ? INFINITY : f.stats[2 * (row0 + i)];
-                rw[QT + threadIdx.x] = inv;
-                rw[2 * QT + threadIdx.x] = empty ? 0.0f : -f.delta[row0 + i];
-                if (MODE != 0)
-                    pl[threadIdx.x] = place_q(f.o, min(i, lq - 1));
-            }
-            if (MODE != 0) {
-                const int lo = low_k - place_q(f.o, min(i0 + QT, lq) - 1) - 3, hi = high_k - place_q(f.o, i0);
-                if (segment == kNoSegment || hi >= segment + f.o.cap) {
-                    if (segment != kNoSegment)
-                        __syncthreads();
-                    segment = lo;  // (down to -3)
-                    stage_bias(bias, f.o, f.a.bias, table, segment, f.o.cap, pos_y, pos_x);
-                }
-            }
-            __syncthreads();
-            if (tile > 0) {
-                qt.fetch(qm, i0 - QT, lq);
-                gt.fetch(gm, i0 - QT, lq);
-            }
-            f32x16 s[SUBS], dp[SUBS];
-#pragma unroll
-            for (int sub = 0; sub < SUBS; ++sub) {
-                s[sub] = 0.0f;
-                dp[sub] = 0.0f;
-            }
-#pragma unroll
-            for (int i = 0; i < DP / 16; ++i)
-#pragma unroll
-                for (int sub = 0; sub < SUBS; ++sub) {
-                    s[sub] = mma(row_frag<T, DP>(qb, sub, i), k[i], s[sub]);
-                    dp[sub] = mma(row_frag<T, DP>(gb, sub, i), v[i], dp[sub]);
-                }
-#pragma unroll
-            for (int sub = 0; sub < SUBS; ++sub) {
-                add_bias<MODE, -1>(s[sub], c, bias, pl, lane_at - segment, sub, half);
-#pragma unroll
-                for (int gq = 0; gq < 4; ++gq) {
-                    const int first = 32 * sub + 8 * gq + 4 * half;
-                    const f32x4 top = *reinterpret_cast<const f32x4 *>(rw + first);
-                    const f32x4 inv = *reinterpret_cast<const f32x4 *>(rw + QT + first);
-                    const f32x4 shift = *reinterpret_cast<const f32x4 *>(rw + 2 * QT + first);
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        const int r = 4 * gq + t;
-                        const float p = exp2_fast(s[sub][r] - top[t]) * inv[t];
-                        s[sub][r] = p;
-                        dp[sub][r] = p * (dp[sub][r] + shift[t]);
-                    }
-                }
-            }
-#pragma unroll
-            for (int sub = 0; sub < SUBS; ++sub)
-#pragma unroll
-                for (int st = 0; st < 2; ++st) {
-                    const frag p = acc_frag<T>(s[sub], st), ds = acc_frag<T>(dp[sub], st);
-#pragma unroll
-                    for (int i = 0; i < DP / 32; ++i) {
-                        dv[i] = mma(col_frag<DP>(gb, sub, st, i), p, dv[i]);
-                        dk[i] = mma(col_frag<DP>(qb, sub, st, i), ds, dk[i]);
-                    }
-                }
+        T *qb = q_lds + buf * Tile::kElems, *gb = g_lds + buf * Tile::kElems;
+        int *pl = place + buf * QT;
+        float *rw = rows + buf * 3 * QT;
+        qt.put(qb);
+        gt.put(gb);
+        if (threadIdx.x < QT) {
+            const int i = i0 + threadIdx.x;
+            const float sum = i < lq ? f.stats[2 * (row0 + i) + 1] : 0.0f;
+            const bool empty = sum == 0.0f;
+            const float inv = empty ? 0.0f : 1.0f / sum;
+            rw[threadIdx.x] = empty ? INFINITY : f.stats[2 * (row0 + i)];
+            rw[QT + threadIdx.x] = inv;
+            rw[2 * QT + threadIdx.x] = empty ? 0.0f : -f.delta[row0 + i];
+            if (MODE != 0)
+                pl[threadIdx.x] = place_q(f.o, min(i, lq - 1));
         }
+        if (MODE != 0) {
+            const int lo = low_k - place_q(f.o, min(i0 + QT, lq) - 1) - 3, hi = high_k - place_q(f.o, i0);
+            if (segment == kNoSegment || hi >= segment + f.o.cap || item % tiles == 0) {
+                if (segment != kNoSegment)
+                    __syncthreads();
+                segment = lo;  // (down to -3)
+                stage_bias(bias, f.o, f.a.bias, table, segment, min(f.o.cap, high_k + 1 - segment), pos_y, pos_x);
+            }
+        }
+        __syncthreads();
+        if (item + 1 < last)
+            fetch(item + 1);
+        f32x16 s[SUBS], dp[SUBS];
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub) {
+            s[sub] = 0.0f;
+            dp[sub] = 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i)
+#pragma unroll
+            for (int sub = 0; sub < SUBS; ++sub) {
+                s[sub] = mma(row_frag<T, DP>(qb, sub, i), k[i], s[sub]);
+                dp[sub] = mma(row_frag<T, DP>(gb, sub, i), v[i], dp[sub]);
+            }
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub) {
+            add_bias<MODE, -1>(s[sub], c, bias, pl, lane_at - segment, sub, half);
+#pragma unroll
+            for (int gq = 0; gq < 4; ++gq) {
+                const int first = 32 * sub + 8 * gq + 4 * half;
+                const f32x4 top = *reinterpret_cast<const f32x4 *>(rw + first);
+                const f32x4 inv = *reinterpret_cast<const f32x4 *>(rw + QT + first);
+                const f32x4 shift = *reinterpret_cast<const f32x4 *>(rw + 2 * QT + first);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const int r = 4 * gq + t;
+                    const float p = exp2_fast(s[sub][r] - top[t]) * inv[t];
+                    s[sub][r] = p;
+                    dp[sub][r] = p * (dp[sub][r] + shift[t]);
+                }
+            }
+        }
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                const frag p = acc_frag<T>(s[sub], st), ds = acc_frag<T>(dp[sub], st);
+#pragma unroll
+                for (int i = 0; i < DP / 32; ++i) {
+                    dv[i] = mma(col_frag<DP>(gb, sub, st, i), p, dv[i]);
+                    dk[i] = mma(col_frag<DP>(qb, sub, st, i), ds, dk[i]);
+                }
+            }
     }
     // keys behind the image's last have no gradient
+    if (!k_here)
+#pragma unroll
+        for (int i = 0; i < DP / 32; ++i) {
+            dk[i] = 0.0f;
+            dv[i] = 0.0f;
+        }
+    if (f.k_splits > 1) {
+        const int64_t at = (split * int64_t(g.n) * g.kv_heads * lk + (int64_t(img) * g.kv_heads + kv_head) * lk + key) * DP;
+        store_part<DP>(f.part_k + at, dk, half, key < lk);
+        store_part<DP>(f.part_v + at, dv, half, key < lk);
+        return;
+    }
     const HeadMap<T, DQP> okm(f.dk, img, kv_head, g.dq), ovm(f.dv, img, kv_head, g.dq);
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i) {
         dk[i] *= g.scale;
-        if (!k_here) {
-            dk[i] = 0.0f;
-            dv[i] = 0.0f;
-        }
         okm.store(key, i, half, dk[i], key < lk);
         ovm.store(key, i, half, dv[i], key < lk);
     }
 }
 
-// Sums by offset over the work-groups of a head, in fp64 and a fixed order:
-// slice s takes every slices-th image.  out [slices][heads][total].
-__global__ void __launch_bounds__(256) offset_sums_kernel(Backward f, int slices, double *__restrict__ out)
+// The results of work-groups that shared a block, added up in order: a thread
+// per quad of reals.
+template <typename T, int DQP> __global__ void __launch_bounds__(256) gradient_join_kernel(Backward f)
 {
+    constexpr int DP = 4 * DQP;
     const AttnGeom &g = f.a.g;
-    const int a = blockIdx.x * 256 + threadIdx.x, head = blockIdx.y;
-    if (a >= f.o.total)
-        return;
-    const int lq = g.lq(), last_k = place_k(f.o, g.lk() - 1);
-    for (int slice = blockIdx.z; slice < slices; slice += gridDim.z) {
-        double s = 0.0;
-        for (int b = 0; b < f.blocks; ++b) {
-            const int low = f.o.origin - place_q(f.o, min((b + 1) * kQueries, lq) - 1);
-            const int past = f.o.origin - place_q(f.o, b * kQueries) + last_k + 1;
-            if (a < low || a >= past)
-                continue;
-            const float *p = f.offsets + (int64_t(head) * f.blocks + b) * f.range + (a - low);
-            for (int img = slice; img < g.n; img += slices)
-                s += double(p[int64_t(img) * g.heads * f.blocks * f.range]);
+    int64_t id = int64_t(blockIdx.x) * 256 + threadIdx.x;
+#pragma unroll
+    for (int which = 0; which < 3; ++which) {
+        const int splits = which == 0 ? f.q_splits : f.k_splits, heads = which == 0 ? g.heads : g.kv_heads;
+        const int tokens = which == 0 ? g.lq() : g.lk();
+        const int64_t rows = int64_t(g.n) * heads * tokens, quads = splits > 1 ? rows * (DP / 4) : 0;
+        if (id < quads) {
+            const float *p = (which == 0 ? f.part_q : which == 1 ? f.part_k : f.part_v) + id * 4;
+            f32x4 s = 0.0f;
+#pragma unroll 4
+            for (int i = 0; i < splits; ++i)
+                s += *reinterpret_cast<const f32x4 *>(p + i * rows * DP);
+            if (which < 2)
+                s *= g.scale;
+            const int64_t row = id / (DP / 4);
+            const int d = 4 * int(id % (DP / 4)), token = int(row % tokens), head = int(row / tokens % heads);
+            const HeadMap<T, DQP> m(which == 0 ? f.dq : which == 1 ? f.dk : f.dv, row / tokens / heads, head, g.dq);
+            store_quad(m.at(token, d), s, m.valid(d, 4), m.vec);
+            return;
         }
-        out[(int64_t(slice) * g.heads + head) * f.o.total + a] = s;
+        id -= quads;
     }
 }
 
-// dtable from the sums by offset: a work-group per row of buckets (head, by).
-// Its threads add up the rows dy of offsets in that bucket, column by column,
-// then its waves the columns dx of each bucket bx.  The slices have their
-// offsets' buckets in common, but where queries have places of their own (pos):
-// there a slice is an image, and they are taken one by one.
-constexpr int kTableThreads = 512, kTableCols = 2048;
-__global__ void __launch_bounds__(kTableThreads)
-table_gradient_kernel(AttnBias b, Offsets o, int heads, int rows, int slices, const int *__restrict__ pos,
-                      const double *__restrict__ sums, float *__restrict__ dtable)
+// Sum over images slice, slice + slices, .. and their work-groups of what offset
+// `a` has in them, in a fixed order.
+__device__ __forceinline__ double offset_sum(const Backward &f, int head, int a, int slice, int slices, int last_k)
 {
-    __shared__ double cols[kTableCols];
-    __shared__ short bucket[kTableCols];
+    const AttnGeom &g = f.a.g;
+    const int lq = g.lq();
+    const int64_t image = int64_t(g.heads) * f.blocks * f.q_splits * f.range;
+    double s = 0.0;
+    for (int b = 0; b < f.blocks; ++b) {
+        const int low = f.o.origin - place_q(f.o, min((b + 1) * kQueries, lq) - 1);
+        const int past = f.o.origin - place_q(f.o, b * kQueries) + last_k + 1;
+        if (a < low || a >= past)
+            continue;
+        for (int sp = 0; sp < f.q_splits; ++sp) {
+            const float *p = f.offsets + ((int64_t(head) * f.blocks + b) * f.q_splits + sp) * f.range + (a - low);
+#pragma unroll 4
+            for (int img = slice; img < g.n; img += slices)
+                s += double(p[img * image]);
+        }
+    }
+    return s;
+}
+
+// Sums by offset of each slice of the images, in fp64: out [slices][heads][total].
+__global__ void __launch_bounds__(256) offset_sums_kernel(Backward f, int slices, double *__restrict__ out)
+{
+    const int a = blockIdx.x * 256 + threadIdx.x, head = blockIdx.y;
+    if (a >= f.o.total)
+        return;
+    const int last_k = place_k(f.o, f.a.g.lk() - 1);
+    for (int slice = blockIdx.z; slice < slices; slice += gridDim.z)
+        out[(int64_t(slice) * f.a.g.heads + head) * f.o.total + a] = offset_sum(f, head, a, slice, slices, last_k);
+}
+
+// dtable from the sums by offset: a work-group per row of buckets (head, by),
+// which takes columns dx of offsets in turn.  Its waves share the rows dy of that
+// bucket out among them, a lane per column; then each wave adds up the columns of
+// its buckets bx.  The slices have their offsets' buckets in common, but where
+// queries have places of their own (pos): there a slice is an image, and they are
+// taken one by one.  DIRECT: from the work-groups' sums themselves (few of them),
+// one slice.
+constexpr int kTableThreads = 512, kTableWaves = kTableThreads / 64, kTableCols = 128;
+template <bool DIRECT>
+__global__ void __launch_bounds__(kTableThreads)
+table_gradient_kernel(Backward f, int rows, int slices, const double *__restrict__ sums, float *__restrict__ dtable)
+{
+    constexpr int kCols = kTableCols / 64;
+    __shared__ double parts[kTableWaves][kTableCols];
+    __shared__ unsigned char takes[kTableThreads];
     __shared__ double tot[kAttnMaxBuckets];
-    const int iy = blockIdx.x % b.ny, head = blockIdx.x / b.ny;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const AttnBias &b = f.a.bias;
+    const Offsets &o = f.o;
+    const int *pos = f.a.pos;
+    const int heads = f.a.g.heads, iy = blockIdx.x % b.ny, head = blockIdx.x / b.ny;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, last_k = place_k(o, f.a.g.lk() - 1);
     for (int x = threadIdx.x; x < b.nx; x += kTableThreads)
         tot[x] = 0.0;
     const int groups = pos != nullptr ? slices : 1, per = slices / groups;
     for (int group = 0; group < groups; ++group) {
         const int pos_y = pos != nullptr ? pos[2 * group] : 0, pos_x = pos != nullptr ? pos[2 * group + 1] : 0;
         for (int x0 = 0; x0 < o.pitch; x0 += kTableCols) {
-            const int width = min(kTableCols, o.pitch - x0);
-            __syncthreads();  // cols has been read
-            for (int x = threadIdx.x; x < width; x += kTableThreads) {
-                double s = 0.0;
-                for (int y = 0; y < rows; ++y) {
-                    const int dy = min(max(y - o.hq1 - pos_y, -b.ry), b.ry);
-                    if ((b.by != nullptr ? min(max(b.by[dy + b.ry], 0), b.ny - 1) : 0) != iy)
+            double s[kCols] = {};
+            for (int y0 = 0; y0 < rows; y0 += kTableThreads) {
+                __syncthreads();  // the last rows' and columns' have been read
+                const int y = y0 + threadIdx.x, dy = min(max(y - o.hq1 - pos_y, -b.ry), b.ry);
+                takes[threadIdx.x] =
+                    y < rows && (b.by != nullptr ? min(max(b.by[dy + b.ry], 0), b.ny - 1) : 0) == iy;
+                __syncthreads();
+                // (row, slice) pairs in turn
+                const int count = min(rows - y0, kTableThreads) * per;
+                for (int i = wave; i < count; i += kTableWaves) {
+                    const int r = i / per, sl = group * per + i % per;
+                    if (!takes[r])
                         continue;
-                    for (int sl = group * per; sl < (group + 1) * per; ++sl)
-                        s += sums[(int64_t(sl) * heads + head) * o.total + int64_t(y) * o.pitch + x0 + x];
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c) {
+                        const int x = x0 + 64 * c + lane, a = (y0 + r) * o.pitch + x;
+                        if (x < o.pitch)
+                            s[c] += DIRECT ? offset_sum(f, head, a, sl, slices, last_k)
+                                           : sums[(int64_t(sl) * heads + head) * o.total + a];
+                    }
                 }
-                cols[x] = s;
-                const int dx = min(max(x0 + x - o.wq1 - pos_x, -b.rx), b.rx);
-                bucket[x] = short(b.bx != nullptr ? min(max(b.bx[dx + b.rx], 0), b.nx - 1) : 0);
+            }
+            int bucket[kCols];
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) {
+                parts[wave][64 * c + lane] = s[c];
+                const int dx = min(max(x0 + 64 * c + lane - o.wq1 - pos_x, -b.rx), b.rx);
+                bucket[c] = b.bx != nullptr ? min(max(b.bx[dx + b.rx], 0), b.nx - 1) : 0;
             }
             __syncthreads();
-            for (int ix = wave; ix < b.nx; ix += kTableThreads / 64) {
-                double s = 0.0;
-                for (int x = lane; x < width; x += 64)
-                    if (bucket[x] == ix)
-                        s += cols[x];
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) {
+                s[c] = 0.0;
+                for (int w = 0; w < kTableWaves; ++w)
+                    s[c] += parts[w][64 * c + lane];
+            }
+            for (int ix = wave; ix < b.nx; ix += kTableWaves) {
+                double t = 0.0;
+                bool any = false;
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) {
+                    any = any || bucket[c] == ix;
+                    t += bucket[c] == ix ? s[c] : 0.0;
+                }
+                if (!__any(any))
+                    continue;
                 for (int m = 1; m < 64; m <<= 1)
-                    s += __shfl_xor(s, m, 64);
+                    t += __shfl_xor(t, m, 64);
                 if (lane == 0)
-                    tot[ix] += s;
+                    tot[ix] += t;
             }
         }
     }
@@ -562,26 +678,57 @@ table_gradient_kernel(AttnBias b, Offsets o, int heads, int rows, int slices, co
 
 // ---------------------------------------------------------------------- host
 
-int padded_dq(int dq)
-{
-    return dq <= 8 ? 8 : dq <= 16 ? 16 : 32;
-}
-
 struct Plan {
     int blocks, range, slices, q_cap, k_cap;
+    int q_splits, k_splits, q_tiles, k_tiles;
+    bool copies, direct;
     size_t q_lds, k_lds;
-    size_t delta_bytes, offset_bytes, sum_bytes;
+    // workspace: copies of q, dout, out and rest, of k and v; delta; sums by
+    // work-group and by slice; partial gradients
+    size_t q_copy, k_copy, delta_bytes, offset_bytes, sum_bytes, part_q, part_k;
 };
 
-Plan backward_plan(const AttnCall &a, DType dt, bool table)
+size_t round_up(size_t bytes)
+{
+    return (bytes + 255) & ~size_t(255);
+}
+
+// Work-groups that share a walk of `tiles` where there are only `groups` walks
+// for 256 compute units: two rounds of the chip, four tiles at least to each.
+int share(int64_t groups, int tiles)
+{
+    return groups >= 256 ? 1 : int(std::max<int64_t>(1, std::min<int64_t>(512 / groups, tiles / 4)));
+}
+
+Plan backward_plan(const AttnCall &a, DType dt, const AttnGradients &gr)
 {
     const AttnGeom &g = a.g;
     const int es = dt == DType::BF16 ? 2 : 4, tile = dt == DType::BF16 ? 64 : 32, dp = 4 * padded_dq(g.dq);
     const int lq = g.lq(), lk = g.lk();
+    const bool table = gr.dtable != nullptr && a.bias.table != nullptr;
     Plan p{};
+    p.copies = padded_dq(g.dq) != g.dq || !(a.q.vec && a.k.vec && a.v.vec && gr.out.vec && gr.dout.vec);
+    if (p.copies) {
+        p.q_copy = round_up(size_t(g.n) * g.heads * lq * dp * es);
+        p.k_copy = round_up(size_t(g.n) * g.kv_heads * lk * dp * es);
+    }
     p.blocks = (lq + kQueries - 1) / kQueries;
+    const int key_blocks = (lk + kQueries - 1) / kQueries;
+    const int q_walk = (lk + tile - 1) / tile, k_walk = (lq + tile - 1) / tile * (g.heads / g.kv_heads);
+    const int64_t q_groups = int64_t(g.n) * g.heads * p.blocks, k_groups = int64_t(g.n) * g.kv_heads * key_blocks;
+    p.q_splits = share(q_groups, q_walk);
+    p.q_tiles = (q_walk + p.q_splits - 1) / p.q_splits;
+    p.q_splits = (q_walk + p.q_tiles - 1) / p.q_tiles;
+    p.k_splits = share(k_groups, k_walk);
+    p.k_tiles = (k_walk + p.k_splits - 1) / p.k_splits;
+    p.k_splits = (k_walk + p.k_tiles - 1) / p.k_tiles;
+    // (room for what smaller batches share: at most 512 work-groups)
+    if (q_walk >= 8)
+        p.part_q = round_up(size_t(512) * kQueries * dp * sizeof(float));
+    if (k_walk >= 8)
+        p.part_k = round_up(size_t(512) * kQueries * dp * sizeof(float));
     p.slices = 1;
-    p.delta_bytes = (size_t(g.n) * g.heads * lq * sizeof(float) + 255) & ~size_t(255);
+    p.delta_bytes = round_up(size_t(g.n) * g.heads * lq * sizeof(float));
     if (a.bias.table != nullptr) {
         const Offsets o = make_offsets(g);
         auto span = [](int count, int w, int h, int skip) { return count + std::min((count - 1) / w + 1, h - 1) * skip; };
@@ -598,14 +745,17 @@ Plan backward_plan(const AttnCall &a, DType dt, bool table)
         p.k_cap = cap(block_k + span(tile, g.wq, g.hq, o.skip_q) + 8);
         if (table) {
             p.range = block_q + host_place(lk - 1, g.wk, o.skip_k) + 1;
-            p.offset_bytes = (size_t(g.n) * g.heads * p.blocks * p.range * sizeof(float) + 255) & ~size_t(255);
-            // (images whose queries have places of their own have slices of their own)
-            p.slices = a.pos != nullptr ? g.n : std::min(g.n, std::max(1, 1024 / std::max(1, (o.total + 255) / 256 * g.heads)));
-            p.sum_bytes = size_t(p.slices) * g.heads * o.total * sizeof(double);
+            p.offset_bytes = round_up(size_t(std::max<int64_t>(q_groups, q_walk >= 8 ? 512 : 0)) * p.range * sizeof(float));
+            // few sums are taken to their buckets directly; images whose queries
+            // have places of their own have slices of their own
+            p.direct = int64_t(g.n) * p.blocks * p.q_splits <= 16;
+            p.slices = a.pos != nullptr ? g.n : p.direct ? 1
+                     : std::min(g.n, std::max(1, 2048 / std::max(1, (o.total + 255) / 256 * g.heads)));
+            p.sum_bytes = round_up(size_t(p.slices) * g.heads * o.total * sizeof(double));
         }
     }
     const size_t tiles = size_t(4) * tile * (dp + (es == 2 ? 0 : 4)) * es + size_t(2) * tile * 4;
-    p.q_lds = tiles + size_t(p.q_cap) * 4 * (table && a.bias.table != nullptr ? 3 : 1);
+    p.q_lds = tiles + size_t(p.q_cap) * 4 * (table ? 3 : 1);
     p.k_lds = tiles + size_t(6) * tile * 4 + size_t(p.k_cap) * 4;
     return p;
 }
@@ -614,12 +764,20 @@ template <typename T, int DQP, int QMODE, int KMODE> hipError_t launch(Backward 
 {
     const AttnGeom &g = f.a.g;
     f.o.cap = p.q_cap;
-    attention_dq_kernel<T, DQP, QMODE><<<xcd_grid(int64_t(g.n) * g.heads * p.blocks), kThreads, p.q_lds, s>>>(f);
+    attention_dq_kernel<T, DQP, QMODE>
+        <<<xcd_grid(int64_t(g.n) * g.heads * p.blocks * p.q_splits), kThreads, p.q_lds, s>>>(f);
     if (hipError_t e = hipGetLastError())
         return e;
     f.o.cap = p.k_cap;
     const int64_t blocks = (g.lk() + kQueries - 1) / kQueries;
-    attention_dkv_kernel<T, DQP, KMODE><<<xcd_grid(g.n * g.kv_heads * blocks), kThreads, p.k_lds, s>>>(f);
+    attention_dkv_kernel<T, DQP, KMODE>
+        <<<xcd_grid(g.n * g.kv_heads * blocks * p.k_splits), kThreads, p.k_lds, s>>>(f);
+    if (hipError_t e = hipGetLastError())
+        return e;
+    const int64_t quads = DQP * int64_t(g.n) * ((p.q_splits > 1 ? int64_t(g.heads) * g.lq() : 0) +
+                                                (p.k_splits > 1 ? 2 * int64_t(g.kv_heads) * g.lk() : 0));
+    if (quads > 0)
+        gradient_join_kernel<T, DQP><<<unsigned((quads + 255) / 256), 256, 0, s>>>(f);
     return hipGetLastError();
 }
 template <typename T, int DQP> hipError_t launch_mode(const Backward &f, const Plan &p, hipStream_t s)
@@ -646,43 +804,79 @@ template <typename T> hipError_t launch_dq(const Backward &f, const Plan &p, hip
 
 }  // namespace
 
-size_t attention_backward_work_bytes(const AttnCall &a, DType dt, bool table)
+size_t attention_backward_work_bytes(const AttnCall &a, DType dt, const AttnGradients &gr)
 {
-    const Plan p = backward_plan(a, dt, table);
-    return p.delta_bytes + p.offset_bytes + p.sum_bytes;
+    const Plan p = backward_plan(a, dt, gr);
+    return 4 * p.q_copy + 2 * p.k_copy + p.delta_bytes + p.offset_bytes + p.sum_bytes + p.part_q + 2 * p.part_k;
 }
 
-hipError_t attention_backward_run(const AttnCall &a, DType dt, const AttnMap &out, const void *rest,
-                                  const float *stats, const AttnMap &dout, const AttnMap &dq, const AttnMap &dk,
-                                  const AttnMap &dv, float *dtable, void *work, hipStream_t s)
+hipError_t attention_backward_run(const AttnCall &a, DType dt, const AttnGradients &gr, void *work, hipStream_t s)
 {
-    const bool table = dtable != nullptr && a.bias.table != nullptr;
-    const Plan p = backward_plan(a, dt, table);
-    unsigned char *w = static_cast<unsigned char *>(work);
+    const Plan p = backward_plan(a, dt, gr);
+    const AttnGeom &g = a.g;
+    unsigned char *at = static_cast<unsigned char *>(work);
+    auto take = [&](size_t bytes) {
+        void *r = at;
+        at += bytes;
+        return r;
+    };
     Backward f;
     f.a = a;
-    f.o = make_offsets(a.g);
-    f.out = out;
-    f.dout = dout;
-    f.dq = dq;
-    f.dk = dk;
-    f.dv = dv;
-    f.rest = rest;
-    f.stats = stats;
-    f.delta = reinterpret_cast<float *>(w);
-    f.offsets = table ? reinterpret_cast<float *>(w + p.delta_bytes) : nullptr;
+    f.o = make_offsets(g);
+    f.out = gr.out;
+    f.dout = gr.dout;
+    f.dq = gr.dq;
+    f.dk = gr.dk;
+    f.dv = gr.dv;
+    const int64_t c_all = int64_t(g.heads) * g.dq;
+    f.rest = {gr.rest, g.lq() * 4 * c_all, 4 * c_all, c_all, true, g.dq};
+    f.stats = gr.stats;
+    if (p.copies) {
+        AttnPack pack;
+        pack.maps = 0;
+        const int64_t d = 4 * padded_dq(g.dq);
+        for (AttnMap *m : {&f.a.q, &f.dout, &f.out, &f.rest, &f.a.k, &f.a.v}) {
+            if (m->data == nullptr)
+                continue;
+            const bool keys = m == &f.a.k || m == &f.a.v;
+            const int i = pack.maps++;
+            pack.src[i] = *m;
+            // (rest is dense and aligned, but its rows may not be whole chunks)
+            pack.src[i].vec = m->vec && g.dq % 8 == 0;
+            pack.heads[i] = keys ? g.kv_heads : g.heads;
+            pack.tokens[i] = keys ? g.lk() : g.lq();
+            pack.dst[i] = take(keys ? p.k_copy : p.q_copy);
+            *m = {pack.dst[i], pack.heads[i] * pack.tokens[i] * d, d, d / 4, true, pack.tokens[i] * d};
+        }
+        if (hipError_t e = attention_pack_run(pack, g.n, g.dq, dt, s))
+            return e;
+    }
+    const bool table = gr.dtable != nullptr && a.bias.table != nullptr;
+    f.delta = static_cast<float *>(take(p.delta_bytes));
+    f.offsets = table ? static_cast<float *>(take(p.offset_bytes)) : nullptr;
+    double *sums = static_cast<double *>(take(p.sum_bytes));
+    f.part_q = static_cast<float *>(take(p.part_q));
+    f.part_k = static_cast<float *>(take(p.part_k));
+    f.part_v = static_cast<float *>(take(p.part_k));
     f.blocks = p.blocks;
     f.range = p.range;
+    f.q_splits = p.q_splits;
+    f.k_splits = p.k_splits;
+    f.q_tiles = p.q_tiles;
+    f.k_tiles = p.k_tiles;
     if (hipError_t e = dt == DType::BF16 ? launch_dq<__bf16>(f, p, s) : launch_dq<float>(f, p, s))
         return e;
     if (!table)
         return hipSuccess;
-    double *sums = reinterpret_cast<double *>(w + p.delta_bytes + p.offset_bytes);
-    offset_sums_kernel<<<dim3((f.o.total + 255) / 256, a.g.heads, std::min(p.slices, 65535)), 256, 0, s>>>(f, p.slices, sums);
+    const int rows = g.hk + g.hq - 1, groups = g.heads * a.bias.ny;
+    if (p.direct) {
+        table_gradient_kernel<true><<<groups, kTableThreads, 0, s>>>(f, rows, p.slices, nullptr, gr.dtable);
+        return hipGetLastError();
+    }
+    offset_sums_kernel<<<dim3((f.o.total + 255) / 256, g.heads, std::min(p.slices, 65535)), 256, 0, s>>>(f, p.slices, sums);
     if (hipError_t e = hipGetLastError())
         return e;
-    table_gradient_kernel<<<a.g.heads * a.bias.ny, kTableThreads, 0, s>>>(a.bias, f.o, a.g.heads, a.g.hk + a.g.hq - 1,
-                                                                        p.slices, a.pos, sums, dtable);
+    table_gradient_kernel<false><<<groups, kTableThreads, 0, s>>>(f, rows, p.slices, sums, gr.dtable);
     return hipGetLastError();
 }
 

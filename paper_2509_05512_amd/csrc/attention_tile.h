@@ -170,14 +170,14 @@ __device__ __forceinline__ void store_quad(float *p, const f32x4 &v, int valid, 
 }
 
 // A head of one image in a map: element d = component * DQP + channel of a
-// token at at(token, d).
+// token at at(token, d); channels dq and beyond do not exist.
 template <typename T, int DQP> struct HeadMap {
     T *p;
     int64_t s_t, s_p;
     int dq;
     bool vec;
     __device__ __forceinline__ HeadMap(const AttnMap &m, int64_t img, int head, int dq_)
-        : p(static_cast<T *>(const_cast<void *>(m.data)) + img * m.s_n + int64_t(head) * dq_), s_t(m.s_t), s_p(m.s_p),
+        : p(static_cast<T *>(const_cast<void *>(m.data)) + img * m.s_n + head * m.s_h), s_t(m.s_t), s_p(m.s_p),
           dq(dq_), vec(m.vec)
     {
     }
@@ -201,6 +201,25 @@ template <typename T, int DQP> struct HeadMap {
             if (here)
                 store_quad(at(token, d), q, valid(d, 4), vec);
         }
+    }
+};
+// One whose rows are whole chunks, aligned (see AttnPack), to be read.
+template <typename T, int DQP> struct WholeMap {
+    typedef typename Elem<T>::frag frag;
+    const T *p;
+    int64_t s_t, s_p;
+    __device__ __forceinline__ WholeMap(const AttnMap &m, int64_t img, int head)
+        : p(static_cast<const T *>(m.data) + img * m.s_n + head * m.s_h), s_t(m.s_t), s_p(m.s_p)
+    {
+    }
+    __device__ __forceinline__ const T *at(int64_t token, int d) const
+    {
+        return p + token * s_t + (d / DQP) * s_p + d % DQP;
+    }
+    __device__ __forceinline__ frag load(int64_t token, int d, bool here) const
+    {
+        const frag v = *reinterpret_cast<const frag *>(at(here ? token : 0, d));
+        return here ? v : frag{};
     }
 };
 
@@ -238,21 +257,21 @@ template <typename T, int DP, int THREADS> struct Stage {
     static_assert(THREADS % kChunks == 0 && kCount * kStep >= kTokens, "whole rows per step");
     static constexpr int kElems = kTokens * kRow;
     frag r[kCount];
-    template <int DQP> __device__ __forceinline__ void fetch(const HeadMap<const T, DQP> &m, int token, int end)
+    template <int DQP> __device__ __forceinline__ void fetch(const WholeMap<T, DQP> &m, int token, int end)
     {
         const int row = threadIdx.x / kChunks, d = 8 * (threadIdx.x % kChunks);
-        const T *p = m.at(token + row, d);  // (dereferenced below `end` and within the head only)
-        if (kStep <= kTokens && m.vec && m.dq == DQP && token + kTokens <= end) {  // whole tiles
+        const T *p = m.at(token + row, d);  // (dereferenced below `end` only)
+        if (kStep <= kTokens && token + kTokens <= end) {
 #pragma unroll
             for (int i = 0; i < kCount; ++i)
                 r[i] = *reinterpret_cast<const frag *>(p + int64_t(i * kStep) * m.s_t);
             return;
         }
-        const int valid = m.valid(d, 8);
 #pragma unroll
         for (int i = 0; i < kCount; ++i) {
-            const bool here = valid > 0 && token + row + i * kStep < end && (kStep <= kTokens || row < kTokens);
-            r[i] = load_chunk<T>(here ? p + int64_t(i * kStep) * m.s_t : m.p, here ? valid : 0, m.vec);
+            const bool here = token + row + i * kStep < end && (kStep <= kTokens || row < kTokens);
+            const frag v = *reinterpret_cast<const frag *>(here ? p + int64_t(i * kStep) * m.s_t : m.p);
+            r[i] = here ? v : frag{};
         }
     }
     __device__ __forceinline__ void put(T *lds) const
@@ -265,28 +284,6 @@ template <typename T, int DP, int THREADS> struct Stage {
             *reinterpret_cast<frag *>(lds + Lds<T, DP>::at(row + i * kStep, d / 8)) = r[i];
     }
 };
-template <typename T, int DQP> struct HeadMap<const T, DQP> {
-    const T *p;
-    int64_t s_t, s_p;
-    int dq;
-    bool vec;
-    __device__ __forceinline__ HeadMap(const AttnMap &m, int64_t img, int head, int dq_)
-        : p(static_cast<const T *>(m.data) + img * m.s_n + int64_t(head) * dq_), s_t(m.s_t), s_p(m.s_p), dq(dq_),
-          vec(m.vec)
-    {
-    }
-    __device__ __forceinline__ const T *at(int64_t token, int d) const
-    {
-        return p + token * s_t + (d / DQP) * s_p + d % DQP;
-    }
-    __device__ __forceinline__ int valid(int d, int most) const { return max(0, min(most, dq - d % DQP)); }
-    __device__ __forceinline__ typename Elem<T>::frag load(int64_t token, int d, bool here) const
-    {
-        const int n = here ? valid(d, 8) : 0;
-        return load_chunk<T>(n > 0 ? at(token, d) : p, n, vec);
-    }
-};
-
 // Operand whose rows are the tile's tokens (32 sub + lane % 32) and whose depth
 // is reals 16 f + 8 (lane / 32) ..+7 of a row.
 template <typename T, int DP> __device__ __forceinline__ typename Elem<T>::frag row_frag(const T *tile, int sub, int f)

@@ -69,7 +69,8 @@ enum Purpose {
     kConvSplit = 9,    // partial tiles of a convolution that splits K (optional)
     kConvFold = 11,    // folded maps, one per work-group (optional)
     kConvPad = 10,     // a convolution's input padded to whole chunks (optional)
-    kBlock = 12        // the attention block's row sums, offsets and partial results
+    kBlock = 12,       // the attention block's copies, row sums, offsets and partial gradients
+    kBlockSplit = 13   // partial results of an attention that splits its keys (optional)
 };
 
 // A call on (current device, stream).  Held from its first look at the buffers
@@ -359,17 +360,17 @@ int report(int code, const char *fmt, ...)
     return code;
 }
 
-int run_on_stream(void *stream, size_t bytes, bool optional, hipError_t (*launch)(void *, void *, hipStream_t),
-                  void *args, const char *what)
+int run_on_stream(void *stream, size_t bytes, size_t extra_bytes,
+                  hipError_t (*launch)(void *, void *, void *, hipStream_t), void *args, const char *what)
 {
     try {
         const StreamCall call(stream);
         void *work = nullptr;
-        if (optional)
-            work = bytes > 0 ? optional_workspace(call, kBlock, bytes) : nullptr;
-        else if (int rc = workspace(call, kBlock, bytes, &work))
-            return rc;
-        const hipError_t e = launch(args, work, static_cast<hipStream_t>(stream));
+        if (bytes > 0)
+            if (int rc = workspace(call, kBlock, bytes, &work))
+                return rc;
+        void *extra = extra_bytes > 0 ? optional_workspace(call, kBlockSplit, extra_bytes) : nullptr;
+        const hipError_t e = launch(args, work, extra, static_cast<hipStream_t>(stream));
         return e == hipSuccess ? QUAN_OK : fail_hip(e, what);
     } catch (const std::exception &e) {
         return fail(QUAN_ERR_NOMEM, "%s: %s", what, e.what());

@@ -12,11 +12,11 @@
 
 namespace quan {
 
-// launch(args, work, stream) as one call on the stream: with `bytes` of the
-// block's workspace there, or (optional) NULL where that cannot be had or none
-// is asked for.  Returns a QUAN_* code.
-int run_on_stream(void *stream, size_t bytes, bool optional, hipError_t (*launch)(void *, void *, hipStream_t),
-                  void *args, const char *what);
+// launch(args, work, extra, stream) as one call on the stream, with `bytes` of
+// the block's workspace, and `extra_bytes` of another or NULL where that cannot
+// be had (or no bytes are asked for).  Returns a QUAN_* code.
+int run_on_stream(void *stream, size_t bytes, size_t extra_bytes,
+                  hipError_t (*launch)(void *, void *, void *, hipStream_t), void *args, const char *what);
 
 // Dropout's mask: element j of pixel m's row of 4C reals is kept where the 16
 // bits j % 8 of Philox 4x32-7 (J. Salmon, M. Moraes, R. Dror, D. Shaw,
@@ -67,12 +67,13 @@ hipError_t dropout_run(const RowsGeom &g, DType dt, const void *x, void *out, co
 // Attention between the pixels of maps, heads of dq quaternion channels:
 //   s_ij = scale Re<q_i, k_j> + table[head][by][bx],  P = softmax over the
 //   image's keys j < kv_len,  out_i = sum_j P_ij v_j;  rows without a key: 0.
-// A map: element (n, token, component, channel) at n s_n + token s_t +
-// component s_p + channel.
+// A map: element (n, head, token, component, channel) at n s_n + head s_h +
+// token s_t + component s_p + channel.
 struct AttnMap {
     const void *data;
     int64_t s_n, s_t, s_p;
-    bool vec;  // 16-byte aligned everywhere
+    bool vec;     // 16-byte aligned everywhere
+    int64_t s_h;  // the head's channels: dq
 };
 // The bias.  by, bx: buckets of the offsets -r..r of key - (query + pos) per
 // axis, offsets beyond them taking the end's (by NULL: one bucket).
@@ -98,17 +99,35 @@ struct AttnCall {
     const int32_t *kv_len;  // [n] or NULL
     const int32_t *pos;     // [n][2] (y, x) of query 0 in the keys' map, or NULL
 };
+// Heads are read as 16-byte chunks of whole rows of D = 4 * padded_dq reals;
+// maps that do not lie so (unaligned slices, other dq) are copied first, head by
+// head ([n][head][token][D], zeros in the added channels).
+constexpr int padded_dq(int dq) { return dq <= 8 ? 8 : dq <= 16 ? 16 : 32; }
+struct AttnPack {
+    static constexpr int kMaps = 6;
+    AttnMap src[kMaps];
+    int heads[kMaps], tokens[kMaps];
+    void *dst[kMaps];
+    int maps;
+};
+hipError_t attention_pack_run(const AttnPack &p, int n, int dq, DType dt, hipStream_t stream);
+
 // out, and where given its remainder to 16 more bits (dense [n][lq][4][c]) and
 // stats [n][heads][lq][2]: the row's maximum in units of log 2 and the sum of
-// 2^(score - maximum).  `work`: attention_forward_work_bytes(...), partial
-// results of a call with few queries.
+// 2^(score - maximum).  `work` holds the copies that the call needs, `extra`
+// (or NULL) partial results of a call with few queries.
 size_t attention_forward_work_bytes(const AttnCall &a, DType dt);
+size_t attention_forward_extra_bytes(const AttnCall &a, DType dt);
 hipError_t attention_forward_run(const AttnCall &a, DType dt, const AttnMap &out, void *rest, float *stats, void *work,
-                                 hipStream_t stream);
-// `work`: attention_backward_work_bytes(...).  dtable [heads][ny * nx] or NULL.
-size_t attention_backward_work_bytes(const AttnCall &a, DType dt, bool table);
-hipError_t attention_backward_run(const AttnCall &a, DType dt, const AttnMap &out, const void *rest,
-                                  const float *stats, const AttnMap &dout, const AttnMap &dq, const AttnMap &dk,
-                                  const AttnMap &dv, float *dtable, void *work, hipStream_t stream);
+                                 void *extra, hipStream_t stream);
+// dtable [heads][ny * nx] or NULL.
+struct AttnGradients {
+    AttnMap out, dout, dq, dk, dv;
+    const void *rest;
+    const float *stats;
+    float *dtable;
+};
+size_t attention_backward_work_bytes(const AttnCall &a, DType dt, const AttnGradients &g);
+hipError_t attention_backward_run(const AttnCall &a, DType dt, const AttnGradients &g, void *work, hipStream_t stream);
 
 }  // namespace quan

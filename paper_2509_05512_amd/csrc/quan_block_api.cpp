@@ -147,7 +147,7 @@ struct BackwardRows {
     quan::Drop drop;
     float eps;
 };
-hipError_t run_backward_rows(void *args, void *work, hipStream_t s)
+hipError_t run_backward_rows(void *args, void *work, void *, hipStream_t s)
 {
     const BackwardRows &r = *static_cast<BackwardRows *>(args);
     return quan::residual_backward_run(r.g, r.dt, r.a, r.drop, r.eps, work, s);
@@ -202,7 +202,7 @@ int check_map(const char *fn, const char *what, const quan_tensor *t, int32_t dt
         return report(QUAN_ERR_ALIGN, "%s: %s must be aligned to its element", fn, what);
     const int64_t chunk = 16 / int64_t(es);
     *m = {t->data, s_n, s_t, s_p,
-          !misaligned(t->data, 16) && s_n % chunk == 0 && s_t % chunk == 0 && s_p % chunk == 0};
+          !misaligned(t->data, 16) && s_n % chunk == 0 && s_t % chunk == 0 && s_p % chunk == 0, 0};
     const int64_t last = (n - 1) * s_n + (h * w - 1) * s_t + 3 * s_p + c;
     *span = {what, t->data, size_t(last) * es};
     if ((n == 1 || s_n % s_p == 0) && s_t % s_p == 0) {
@@ -210,6 +210,13 @@ int check_map(const char *fn, const char *what, const quan_tensor *t, int32_t dt
         span->width = c * int64_t(es);
     }
     return QUAN_OK;
+}
+
+// A lane takes 8 reals of a head at a time.
+void for_heads(quan::AttnMap *m, int dq)
+{
+    m->s_h = dq;
+    m->vec = m->vec && dq % 8 == 0;
 }
 
 struct Spans {
@@ -258,10 +265,8 @@ int check_call(const char *fn, const quan_tensor *q, const quan_tensor *k, const
     const int64_t blocks = (std::max(g.lq(), g.lk()) + 63) / 64;
     if (blocks * g.n > kMaxPixels / 2 / heads)
         return report(QUAN_ERR_UNSUPPORTED, "%s: too many work-groups", fn);
-    // a lane takes 8 reals of a head at a time
-    a->q.vec = a->q.vec && dq % 8 == 0;
-    a->k.vec = a->k.vec && dq % 8 == 0;
-    a->v.vec = a->v.vec && dq % 8 == 0;
+    for (quan::AttnMap *m : {&a->q, &a->k, &a->v})
+        for_heads(m, g.dq);
     a->kv_len = kv_len;
     a->pos = pos;
     a->bias = {};
@@ -300,24 +305,21 @@ struct ForwardCall {
     void *rest;
     float *stats;
 };
-hipError_t run_forward(void *args, void *work, hipStream_t s)
+hipError_t run_forward(void *args, void *work, void *extra, hipStream_t s)
 {
     const ForwardCall &c = *static_cast<ForwardCall *>(args);
-    return quan::attention_forward_run(c.a, c.dt, c.out, c.rest, c.stats, work, s);
+    return quan::attention_forward_run(c.a, c.dt, c.out, c.rest, c.stats, work, extra, s);
 }
 
 struct BackwardCall {
     quan::AttnCall a;
     quan::DType dt;
-    quan::AttnMap out, dout, dq, dk, dv;
-    const void *rest;
-    const float *stats;
-    float *dtable;
+    quan::AttnGradients g;
 };
-hipError_t run_backward(void *args, void *work, hipStream_t s)
+hipError_t run_backward(void *args, void *work, void *, hipStream_t s)
 {
     const BackwardCall &c = *static_cast<BackwardCall *>(args);
-    return quan::attention_backward_run(c.a, c.dt, c.out, c.rest, c.stats, c.dout, c.dq, c.dk, c.dv, c.dtable, work, s);
+    return quan::attention_backward_run(c.a, c.dt, c.g, work, s);
 }
 
 size_t dense_bytes(const quan_tensor *t)
@@ -387,14 +389,15 @@ QUAN_API int quan_attention_forward(const quan_tensor *q, const quan_tensor *k, 
         return rc;
     if (int rc = check_alias(fn, rest_span, {stats_span}))
         return rc;
-    c.out.vec = c.out.vec && c.a.g.dq % 8 == 0;
+    for_heads(&c.out, c.a.g.dq);
     c.dt = to_dt(q->dtype);
     c.rest = rest;
     c.stats = stats;
     const size_t bytes = quan::attention_forward_work_bytes(c.a, c.dt);
-    if (bytes == 0)
-        return launched(run_forward(&c, nullptr, static_cast<hipStream_t>(stream)), fn);
-    return quan::run_on_stream(stream, bytes, true, run_forward, &c, fn);
+    const size_t extra = quan::attention_forward_extra_bytes(c.a, c.dt);
+    if (bytes == 0 && extra == 0)
+        return launched(run_forward(&c, nullptr, nullptr, static_cast<hipStream_t>(stream)), fn);
+    return quan::run_on_stream(stream, bytes, extra, run_forward, &c, fn);
 }
 
 QUAN_API int quan_attention_backward(const quan_tensor *q, const quan_tensor *k, const quan_tensor *v,
@@ -410,15 +413,15 @@ QUAN_API int quan_attention_backward(const quan_tensor *q, const quan_tensor *k,
     if (int rc = check_call(fn, q, k, v, relpos, kv_len, pos, scale, heads, &c.a, &s))
         return rc;
     Span out_span, dout_span, dq_span, dk_span, dv_span;
-    if (int rc = check_map(fn, "out", out, q->dtype, q->shape, &c.out, &out_span))
+    if (int rc = check_map(fn, "out", out, q->dtype, q->shape, &c.g.out, &out_span))
         return rc;
-    if (int rc = check_map(fn, "dout", dout, q->dtype, q->shape, &c.dout, &dout_span))
+    if (int rc = check_map(fn, "dout", dout, q->dtype, q->shape, &c.g.dout, &dout_span))
         return rc;
-    if (int rc = check_map(fn, "dq", dq, q->dtype, q->shape, &c.dq, &dq_span))
+    if (int rc = check_map(fn, "dq", dq, q->dtype, q->shape, &c.g.dq, &dq_span))
         return rc;
-    if (int rc = check_map(fn, "dk", dk, q->dtype, k->shape, &c.dk, &dk_span))
+    if (int rc = check_map(fn, "dk", dk, q->dtype, k->shape, &c.g.dk, &dk_span))
         return rc;
-    if (int rc = check_map(fn, "dv", dv, q->dtype, k->shape, &c.dv, &dv_span))
+    if (int rc = check_map(fn, "dv", dv, q->dtype, k->shape, &c.g.dv, &dv_span))
         return rc;
     if (stats == nullptr)
         return report(QUAN_ERR_NULL, "%s: stats must be non-NULL", fn);
@@ -443,14 +446,13 @@ QUAN_API int quan_attention_backward(const quan_tensor *q, const quan_tensor *k,
         return rc;
     if (int rc = check_alias(fn, dv_span, {dtable_span}))
         return rc;
-    for (quan::AttnMap *m : {&c.out, &c.dout, &c.dq, &c.dk, &c.dv})
-        m->vec = m->vec && c.a.g.dq % 8 == 0;
+    for (quan::AttnMap *m : {&c.g.out, &c.g.dout, &c.g.dq, &c.g.dk, &c.g.dv})
+        for_heads(m, c.a.g.dq);
     c.dt = to_dt(q->dtype);
-    c.rest = rest;
-    c.stats = stats;
-    c.dtable = dtable;
-    return quan::run_on_stream(stream, quan::attention_backward_work_bytes(c.a, c.dt, dtable != nullptr), false,
-                               run_backward, &c, fn);
+    c.g.rest = rest;
+    c.g.stats = stats;
+    c.g.dtable = dtable;
+    return quan::run_on_stream(stream, quan::attention_backward_work_bytes(c.a, c.dt, c.g), 0, run_backward, &c, fn);
 }
 
 QUAN_API int quan_rmsnorm_forward(const void *x, const float *gamma, float eps, void *out, int32_t n, int32_t c,
@@ -509,7 +511,7 @@ QUAN_API int quan_rmsnorm_backward(const void *x, const void *dout, const float 
     r.a.dx = dx;
     r.a.dnext_gamma = dgamma;
     r.eps = eps;
-    return quan::run_on_stream(stream, quan::residual_backward_work_bytes(r.g, r.a), false, run_backward_rows, &r, fn);
+    return quan::run_on_stream(stream, quan::residual_backward_work_bytes(r.g, r.a), 0, run_backward_rows, &r, fn);
 }
 
 QUAN_API int quan_residual_forward(const void *x, const void *y, const void *gate, const float *gamma,
@@ -593,7 +595,7 @@ QUAN_API int quan_residual_backward(const void *y, const void *dout, const void 
     r.dt = to_dt(dtype);
     r.a = {y, dout, out, dh, gamma, scale, next_gamma, gate, dx, dy, dgate, dgamma, dscale, dnext_gamma};
     r.eps = eps;
-    return quan::run_on_stream(stream, quan::residual_backward_work_bytes(r.g, r.a), false, run_backward_rows, &r, fn);
+    return quan::run_on_stream(stream, quan::residual_backward_work_bytes(r.g, r.a), 0, run_backward_rows, &r, fn);
 }
 
 QUAN_API int quan_dropout(const void *x, float p, const uint64_t *rng, void *out, int32_t n, int32_t c, int32_t h,
