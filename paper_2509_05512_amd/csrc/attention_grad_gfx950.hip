@@ -605,7 +605,8 @@ table_gradient_kernel(Backward f, int rows, int slices, const double *__restrict
 {
     constexpr int kCols = kTableCols / 64;
     __shared__ double parts[kTableWaves][kTableCols];
-    __shared__ unsigned char takes[kTableThreads];
+    __shared__ short taken[kTableThreads];  // rows of that bucket among kTableThreads, in order
+    __shared__ int counts[kTableWaves];
     __shared__ double tot[kAttnMaxBuckets];
     const AttnBias &b = f.a.bias;
     const Offsets &o = f.o;
@@ -620,20 +621,28 @@ table_gradient_kernel(Backward f, int rows, int slices, const double *__restrict
         for (int x0 = 0; x0 < o.pitch; x0 += kTableCols) {
             double s[kCols] = {};
             for (int y0 = 0; y0 < rows; y0 += kTableThreads) {
-                __syncthreads();  // the last rows' and columns' have been read
                 const int y = y0 + threadIdx.x, dy = min(max(y - o.hq1 - pos_y, -b.ry), b.ry);
-                takes[threadIdx.x] =
-                    y < rows && (b.by != nullptr ? min(max(b.by[dy + b.ry], 0), b.ny - 1) : 0) == iy;
+                const bool here = y < rows && (b.by != nullptr ? min(max(b.by[dy + b.ry], 0), b.ny - 1) : 0) == iy;
+                const unsigned long long mine = __ballot(here);
+                __syncthreads();  // the last rows and columns have been read
+                if (lane == 0)
+                    counts[wave] = __popcll(mine);
+                __syncthreads();
+                int before = 0, all = 0;
+                for (int w = 0; w < kTableWaves; ++w) {
+                    before += w < wave ? counts[w] : 0;
+                    all += counts[w];
+                }
+                if (here)
+                    taken[before + __popcll(mine & ((1ull << lane) - 1))] = short(threadIdx.x);
                 __syncthreads();
                 // (row, slice) pairs in turn
-                const int count = min(rows - y0, kTableThreads) * per;
-                for (int i = wave; i < count; i += kTableWaves) {
-                    const int r = i / per, sl = group * per + i % per;
-                    if (!takes[r])
-                        continue;
+#pragma unroll 4
+                for (int i = wave; i < all * per; i += kTableWaves) {
+                    const int r = i / per, sl = group * per + (i - r * per);
 #pragma unroll
                     for (int c = 0; c < kCols; ++c) {
-                        const int x = x0 + 64 * c + lane, a = (y0 + r) * o.pitch + x;
+                        const int x = x0 + 64 * c + lane, a = (y0 + taken[r]) * o.pitch + x;
                         if (x < o.pitch)
                             s[c] += DIRECT ? offset_sum(f, head, a, sl, slices, last_k)
                                            : sums[(int64_t(sl) * heads + head) * o.total + a];
@@ -750,7 +759,7 @@ Plan backward_plan(const AttnCall &a, DType dt, const AttnGradients &gr)
             // have places of their own have slices of their own
             p.direct = int64_t(g.n) * p.blocks * p.q_splits <= 16;
             p.slices = a.pos != nullptr ? g.n : p.direct ? 1
-                     : std::min(g.n, std::max(1, 2048 / std::max(1, (o.total + 255) / 256 * g.heads)));
+                     : std::min(g.n, std::max(1, 1024 / std::max(1, (o.total + 255) / 256 * g.heads)));
             p.sum_bytes = round_up(size_t(p.slices) * g.heads * o.total * sizeof(double));
         }
     }

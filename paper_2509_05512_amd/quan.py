@@ -35,13 +35,6 @@ class QuanTensor(ctypes.Structure):
                 ("shape", ctypes.c_int64 * 5), ("strides", ctypes.c_int64 * 5)]
 
 
-class QuanRelpos(ctypes.Structure):
-    """struct quan_relpos: the attention bias's table and bucket maps."""
-    _fields_ = [("table", ctypes.c_void_p), ("bucket_y", ctypes.c_void_p), ("bucket_x", ctypes.c_void_p),
-                ("buckets_y", ctypes.c_int32), ("buckets_x", ctypes.c_int32),
-                ("radius_y", ctypes.c_int32), ("radius_x", ctypes.c_int32)]
-
-
 _PACK_DESC = struct.Struct("=Qii10q").pack  # the fields of QuanTensor in order (no padding)
 
 
@@ -158,7 +151,8 @@ def to_device_layout(t: torch.Tensor) -> torch.Tensor:
 
 
 def empty_qmap(n, c, h, w, dtype, device):
-    return torch.empty((n, h, w, 4, c), dtype=dtype, device=device).permute(0, 3, 4, 1, 2)
+    row = 4 * c
+    return torch.empty_strided((n, 4, c, h, w), (h * w * row, c, 1, w * row, row), dtype=dtype, device=device)
 
 
 # Host work per call matters where the kernels are short (a training step of a
@@ -664,48 +658,65 @@ def quan_relpos_buckets(radius, buckets, device="cpu"):
     return torch.tensor(list(host), dtype=torch.int32, device=device)
 
 
+# quan_relpos and the quan_tensors of 5-axis maps go to the library as bytes
+# (it only reads them): the structures' own construction cost 1 us each.
+_PACK_RELPOS = struct.Struct("@PPPiiii").pack
+_PACK_MAP = struct.Struct("=Qii10q").pack
+_CODES = {torch.bfloat16: QUAN_BF16, torch.float32: QUAN_F32}
+
+
+def _map_desc(t):
+    code = _CODES.get(t.dtype)
+    if code is None:
+        _dtype_code(t)
+    return _PACK_MAP(t.data_ptr(), code, 5, *t.shape, *t.stride())
+
+
+def _bucket_map(name, t, device):
+    if t.dtype != torch.int32 or t.dim() != 1 or t.numel() % 2 != 1 or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"relpos's {name} must be a contiguous int32 tensor of odd length on q's device")
+    return t.data_ptr(), t.numel() // 2
+
+
 def _relpos(relpos, heads, device):
-    """(struct quan_relpos, table's shape) of (table, bucket_y, bucket_x)."""
+    """struct quan_relpos of (table, bucket_y, bucket_x)."""
     table, by, bx = relpos
     if table.dtype != torch.float32 or not table.is_contiguous() or table.device != device:
         raise ValueError("relpos's table must be a contiguous float32 tensor on q's device")
-    radii, buckets = [], []
-    for name, t in (("bucket_y", by), ("bucket_x", bx)):
-        if t is None:
-            radii.append(0)
-            continue
-        if t.dtype != torch.int32 or t.dim() != 1 or t.numel() % 2 != 1 or not t.is_contiguous() or t.device != device:
-            raise ValueError(f"relpos's {name} must be a contiguous int32 tensor of odd length on q's device")
-        radii.append(t.numel() // 2)
-    if table.dim() == 3:
-        buckets = [table.shape[1], table.shape[2]]
-    elif table.dim() == 2 and by is None:
-        buckets = [1, table.shape[1]]
-    elif table.dim() == 2 and bx is None:
-        buckets = [table.shape[1], 1]
+    at_y, ry = (0, 0) if by is None else _bucket_map("bucket_y", by, device)
+    at_x, rx = (0, 0) if bx is None else _bucket_map("bucket_x", bx, device)
+    shape = table.shape
+    if len(shape) == 3:
+        ny, nx = shape[1:]
+    elif len(shape) == 2 and by is None:
+        ny, nx = 1, shape[1]
+    elif len(shape) == 2 and bx is None:
+        ny, nx = shape[1], 1
     else:
         raise ValueError("relpos's table must be [heads, buckets_y, buckets_x] (or [heads, buckets] with one axis's map)")
-    if table.shape[0] != heads:
+    if shape[0] != heads:
         raise ValueError("relpos's table must have a row per head")
-    return QuanRelpos(_ptr(table), _ptr(by), _ptr(bx), buckets[0], buckets[1], radii[0], radii[1]), table
+    return _PACK_RELPOS(table.data_ptr(), at_y, at_x, ny, nx, ry, rx)
 
 
 def _attention_args(q, k, v, heads, relpos, kv_len, pos, scale):
+    """The arguments that both directions start with."""
     if q.dim() != 5 or k.dim() != 5 or v.dim() != 5:
         raise ValueError("q, k and v must be [N, 4, C, H, W]")
-    for t in (k, v, kv_len, pos):
-        if t is not None and t.device != q.device:
-            raise ValueError("all tensors must be on q's device")
-    n = q.shape[0]
-    if kv_len is not None and (tuple(kv_len.shape) != (n,) or kv_len.dtype != torch.int32 or not kv_len.is_contiguous()):
-        raise ValueError("kv_len must be a contiguous int32 [N] tensor")
-    if pos is not None and (tuple(pos.shape) != (n, 2) or pos.dtype != torch.int32 or not pos.is_contiguous()):
-        raise ValueError("pos must be a contiguous int32 [N, 2] tensor")
+    dev, n = q.device, q.shape[0]
+    if k.device != dev or v.device != dev:
+        raise ValueError("all tensors must be on q's device")
+    if kv_len is not None and (kv_len.shape != (n,) or kv_len.dtype != torch.int32 or not kv_len.is_contiguous()
+                               or kv_len.device != dev):
+        raise ValueError("kv_len must be a contiguous int32 [N] tensor on q's device")
+    if pos is not None and (pos.shape != (n, 2) or pos.dtype != torch.int32 or not pos.is_contiguous()
+                            or pos.device != dev):
+        raise ValueError("pos must be a contiguous int32 [N, 2] tensor on q's device")
     heads = int(heads)
     if scale is None:
         scale = 1.0 / math.sqrt(max(1, 4 * (q.shape[2] // heads))) if heads > 0 else 1.0
-    bias, table = (None, None) if relpos is None else _relpos(relpos, heads, q.device)
-    return [describe(t) for t in (q, k, v)], bias, table, float(scale), heads
+    return (_map_desc(q), _map_desc(k), _map_desc(v), None if relpos is None else _relpos(relpos, heads, dev),
+            _ptr(kv_len), _ptr(pos), float(scale), heads)
 
 
 def quan_attention_forward(q, k, v, heads, relpos=None, kv_len=None, pos=None, scale=None, out=None, save=False):
@@ -721,22 +732,22 @@ def quan_attention_forward(q, k, v, heads, relpos=None, kv_len=None, pos=None, s
     default.  Returns out, or with save (out, stats, rest) for
     quan_attention_backward."""
     lib = load_library()
-    descs, bias, _, scale, heads = _attention_args(q, k, v, heads, relpos, kv_len, pos, scale)
+    args = _attention_args(q, k, v, heads, relpos, kv_len, pos, scale)
     n, _, c, h, w = q.shape
+    dev, dtype = q.device, q.dtype
     if out is None:
-        out = empty_qmap(n, c, h, w, q.dtype, q.device)
-    elif out.dim() != 5 or out.device != q.device:
+        out = empty_qmap(n, c, h, w, dtype, dev)
+    elif out.dim() != 5 or out.device != dev:
         raise ValueError("out must be [N, 4, C, Hq, Wq] on q's device")
     stats = rest = None
     if save:
-        stats = torch.empty((n, heads, h * w, 2), dtype=torch.float32, device=q.device)
-        if q.dtype == torch.bfloat16:
-            rest = empty_qmap(n, c, h, w, q.dtype, q.device)
-    with _on(q.device):
-        rc = lib.quan_attention_forward(_ref(descs[0]), _ref(descs[1]), _ref(descs[2]), _ref(bias), _ptr(kv_len),
-                                        _ptr(pos), scale, heads, _ref(describe(out)), _ptr(rest), _ptr(stats),
-                                        _stream(q.device))
-    _check(rc)
+        stats = torch.empty((n, args[-1], h * w, 2), dtype=torch.float32, device=dev)
+        if dtype == torch.bfloat16:
+            rest = empty_qmap(n, c, h, w, dtype, dev)
+    with _on(dev):
+        rc = lib.quan_attention_forward(*args, _map_desc(out), _ptr(rest), _ptr(stats), _stream(dev))
+    if rc:
+        _check(rc)
     return (out, stats, rest) if save else out
 
 
@@ -746,46 +757,46 @@ def quan_attention_backward(q, k, v, out, stats, rest, dout, heads, relpos=None,
     saved.  dq, dk, dv may be slices of one map.  Returns (dq, dk, dv, dtable),
     dtable float32 like relpos's table (None without one)."""
     lib = load_library()
-    descs, bias, table, scale, heads = _attention_args(q, k, v, heads, relpos, kv_len, pos, scale)
+    args = _attention_args(q, k, v, heads, relpos, kv_len, pos, scale)
     n, _, c, h, w = q.shape
-    if stats is None or tuple(stats.shape) != (n, heads, h * w, 2) or stats.dtype != torch.float32 \
+    dev = q.device
+    if stats is None or stats.shape != (n, args[-1], h * w, 2) or stats.dtype != torch.float32 \
             or not stats.is_contiguous():
         raise ValueError("stats must be the forward's, float32 [N, heads, Hq Wq, 2]")
     if rest is not None and (rest.shape != q.shape or rest.dtype != q.dtype or not is_device_layout(rest)):
         raise ValueError("rest must be the forward's, in device layout like out")
-    grads = []
-    for t, like in ((dq, q), (dk, k), (dv, v)):
-        if t is None:
-            t = empty_qmap(like.shape[0], like.shape[2], like.shape[3], like.shape[4], like.dtype, like.device)
-        grads.append(t)
-    for t in (out, stats, rest, dout, *grads):
-        if t is not None and t.device != q.device:
+    dq, dk, dv = (_like_map(like) if t is None else t for t, like in ((dq, q), (dk, k), (dv, v)))
+    for t in (out, stats, rest, dout, dq, dk, dv):
+        if t is not None and t.device != dev:
             raise ValueError("all tensors must be on q's device")
-    dtable = None if table is None else torch.empty_like(table)
-    descs += [describe(t) for t in (out, dout, *grads)]
-    with _on(q.device):
-        rc = lib.quan_attention_backward(_ref(descs[0]), _ref(descs[1]), _ref(descs[2]), _ref(bias), _ptr(kv_len),
-                                         _ptr(pos), scale, heads, _ref(descs[3]), _ptr(rest), _ptr(stats),
-                                         _ref(descs[4]), _ref(descs[5]), _ref(descs[6]), _ref(descs[7]), _ptr(dtable),
-                                         _stream(q.device))
-    _check(rc)
-    return (*grads, dtable)
+    for t in (out, dout, dq, dk, dv):
+        if t.dim() != 5:
+            raise ValueError("out, dout and the gradients must be [N, 4, C, H, W]")
+    dtable = None if relpos is None else torch.empty_like(relpos[0])
+    with _on(dev):
+        rc = lib.quan_attention_backward(*args, _map_desc(out), _ptr(rest), stats.data_ptr(), _map_desc(dout),
+                                         _map_desc(dq), _map_desc(dk), _map_desc(dv), _ptr(dtable), _stream(dev))
+    if rc:
+        _check(rc)
+    return dq, dk, dv, dtable
 
 
 def _check_map(name, t, like):
-    if not is_device_layout(t) or t.shape != like.shape or t.dtype != like.dtype or t.device != like.device:
+    """t is like `like`, a map whose layout has been checked."""
+    if t.shape != like.shape or t.dtype != like.dtype or t.device != like.device \
+            or (t.stride() != like.stride() and not is_device_layout(t)):
         raise ValueError(f"{name} must be [N, 4, C, H, W] in device layout like the others")
 
 
 def _check_param(name, t, c, device):
-    if t is not None and (tuple(t.shape) != (4, c) or t.dtype != torch.float32 or not t.is_contiguous()
+    if t is not None and (t.shape != (4, c) or t.dtype != torch.float32 or not t.is_contiguous()
                           or t.device != device):
         raise ValueError(f"{name} must be a contiguous float32 [4, C] tensor")
 
 
 def _check_gate(name, t, like):
     n, _, c = like.shape[:3]
-    if t is not None and (tuple(t.shape) != (n, 4, c, 1, 1) or not is_device_layout(t) or t.dtype != like.dtype
+    if t is not None and (t.shape != (n, 4, c, 1, 1) or not is_device_layout(t) or t.dtype != like.dtype
                           or t.device != like.device):
         raise ValueError(f"{name} must be [N, 4, C, 1, 1] in device layout like the maps")
 
@@ -794,7 +805,7 @@ def _check_rng(rng, p, device):
     if rng is None:
         if p > 0:
             raise ValueError("rng, an int64 tensor (seed, offset), is needed with p > 0")
-    elif tuple(rng.shape) != (2,) or rng.dtype != torch.int64 or not rng.is_contiguous() or rng.device != device:
+    elif rng.shape != (2,) or rng.dtype != torch.int64 or not rng.is_contiguous() or rng.device != device:
         raise ValueError("rng must be a contiguous int64 tensor (seed, offset) on the maps' device")
 
 

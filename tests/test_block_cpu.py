@@ -31,10 +31,16 @@ def desc(data, n=2, c=16, h=4, w=6, dtype=1, strides=None, ndim=5, comp=4, c_all
     return quan.QuanTensor(data, dtype, ndim, (ctypes.c_int64 * 5)(n, comp, c, h, w), (ctypes.c_int64 * 5)(*s))
 
 
+class QuanRelpos(ctypes.Structure):
+    """struct quan_relpos"""
+    _fields_ = [(m, ctypes.c_void_p) for m in ("table", "bucket_y", "bucket_x")] \
+        + [(m, ctypes.c_int32) for m in ("buckets_y", "buckets_x", "radius_y", "radius_x")]
+
+
 def relpos(**kw):
     a = dict(table=addr(20), bucket_y=addr(21), bucket_x=addr(22), buckets_y=4, buckets_x=5, radius_y=3, radius_x=5)
     a.update(kw)
-    return quan.QuanRelpos(*a.values())
+    return QuanRelpos(*a.values())
 
 
 def attention(lib, back=False, **kw):
