@@ -37,9 +37,9 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_forward_kernel(Forward f
     typedef typename Elem<T>::frag frag;
     constexpr int KT = Tile::kTokens, SUBS = KT / 32;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
-    T *k_lds = reinterpret_cast<T *>(lds_raw), *v_lds = k_lds + 2 * Tile::kElems;
-    int *place = reinterpret_cast<int *>(v_lds + 2 * Tile::kElems);
-    float *bias = reinterpret_cast<float *>(place + 2 * KT);
+    float *bias = reinterpret_cast<float *>(lds_raw);  // (at 0: its reads then have their offsets in the instruction)
+    int *place = reinterpret_cast<int *>(bias + f.o.cap);
+    T *k_lds = reinterpret_cast<T *>(place + 2 * KT), *v_lds = k_lds + 2 * Tile::kElems;
 
     const AttnGeom &g = f.a.g;
     const int lq = g.lq(), lk = g.lk();
@@ -55,6 +55,7 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_forward_kernel(Forward f
     const int kv_head = head / (g.heads / g.kv_heads);
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int half_at = KT / 2 * half;  // the lane's half of a tile
     const int q0 = block * kQueries;
     const int query = q0 + 32 * wave + (lane & 31);
     const bool q_here = query < lq;
@@ -127,9 +128,12 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_forward_kernel(Forward f
         }
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub)
-            add_bias<MODE, 1>(s[sub], c, bias, pl, lane_at - segment, sub, half);
-        if (j0 + KT > end)
-            clear_behind(s, j0, end, half, -INFINITY);
+            add_bias<MODE, 1>(s[sub], c, bias, pl, lane_at - segment, half_at, sub);
+        if (j0 + KT > end) {
+#pragma unroll
+            for (int sub = 0; sub < SUBS; ++sub)
+                clear_behind(s[sub], end - j0 - half_at, sub, -INFINITY);
+        }
         float t = s[0][0];
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub)

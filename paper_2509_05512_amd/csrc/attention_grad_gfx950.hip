@@ -39,19 +39,25 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves, kQueries = 32 * kWaves;
 // changes nothing, so that the waves share one array.  Its units 2^-k follow
 // from a bound of the terms known before they are: |dS| <= |dP - delta| <=
 // |dO| |v| + |delta|, with the work-group's largest |dO| and |delta| and the
-// tile's largest element of v.  k = 50 - e for a bound below 2^e: a term is
-// below 2^51, an offset's terms (one per query, 128) stay below 2^58, and a
-// term's last place is 2^-50 of the bound.  A tile with a larger bound takes the
-// array to coarser units.  What NaN or infinity is in the work-group's rows or
-// in v gives NaN.
-constexpr int kSumBits = 50, kNoUnits = 127, kBadUnits = 128;
-constexpr double kRound = 6755399441055744.0;  // 1.5 * 2^52: to add it rounds to an integer in the low bits
+// tile's largest element of v.  k = kSumBits - e for a bound below 2^e: an
+// offset's terms (one per query, 128) stay below 2^50, and a term's last place
+// is 2^-42 of the bound.  A tile with a larger bound takes the array to coarser
+// units.  What NaN or infinity is in the work-group's rows or in v gives NaN.
+//
+// Adding 1.5 * 2^52 to a term brings it, rounded, to the low bits of a double;
+// those bits are added as they are, the constant with them: it is a multiple of
+// 2^51, so that the sum is what its low 51 bits say.
+constexpr int kSumBits = 42, kNoUnits = 127, kBadUnits = 128;
+constexpr double kRound = 6755399441055744.0;
 __device__ __forceinline__ void add_fixed(long long *entry, float v, double scale)
 {
     const double t = fma(double(v), scale, kRound);
-    const long long term = __builtin_bit_cast(long long, t) - __builtin_bit_cast(long long, kRound);
-    __hip_atomic_fetch_add(reinterpret_cast<unsigned long long *>(entry), (unsigned long long)term, __ATOMIC_RELAXED,
-                           __HIP_MEMORY_SCOPE_WORKGROUP);
+    __hip_atomic_fetch_add(reinterpret_cast<unsigned long long *>(entry), __builtin_bit_cast(unsigned long long, t),
+                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
+__device__ __forceinline__ long long fixed_sum(long long entry)
+{
+    return (long long)((unsigned long long)entry << 13) >> 13;
 }
 // The larger of two values >= 0; as unsigned numbers such floats keep their
 // order, and NaN is above infinity.
@@ -113,10 +119,10 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
     typedef typename Elem<T>::frag frag;
     constexpr int KT = Tile::kTokens, SUBS = KT / 32;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
-    T *k_lds = reinterpret_cast<T *>(lds_raw), *v_lds = k_lds + 2 * Tile::kElems;
-    int *place = reinterpret_cast<int *>(v_lds + 2 * Tile::kElems);
-    float *bias = reinterpret_cast<float *>(place + 2 * KT);
+    float *bias = reinterpret_cast<float *>(lds_raw);  // (at 0: its reads then have their offsets in the instruction)
     long long *sums = reinterpret_cast<long long *>(bias + f.o.cap);
+    int *place = reinterpret_cast<int *>(sums + (f.offsets != nullptr ? f.o.cap : 0));
+    T *k_lds = reinterpret_cast<T *>(place + 2 * KT), *v_lds = k_lds + 2 * Tile::kElems;
     __shared__ float tops[2 * kWaves];  // of a tile's v, by buffer and wave
 
     const AttnGeom &g = f.a.g;
@@ -132,6 +138,7 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
     const int head = id % g.heads, img = id / g.heads;
     const int kv_head = head / (g.heads / g.kv_heads);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int half_at = KT / 2 * half;  // the lane's half of a tile
     const int q0 = block * kQueries, query = q0 + 32 * wave + (lane & 31);
     const bool q_here = query < lq;
     const int len = f.a.kv_len != nullptr ? min(max(f.a.kv_len[img], 0), lk) : lk;
@@ -229,7 +236,7 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
         const int last = min(segment + f.o.cap, past);
         const double back = __longlong_as_double((long long)(1023 - units) << 52);  // 2^-units
         for (int a = own(segment); a < last; a += kThreads) {
-            const float v = units == kBadUnits ? NAN : units == kNoUnits ? 0.0f : float(double(sums[a - segment]) * back);
+            const float v = units == kBadUnits ? NAN : units == kNoUnits ? 0.0f : float(double(fixed_sum(sums[a - segment])) * back);
             offsets[a] = a < done ? offsets[a] + v : v;
         }
         done = max(done, last);
@@ -300,7 +307,7 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
                     if (units != kNoUnits) {  // (what other waves add meanwhile waits for the barriers)
                         __syncthreads();
                         for (int i = threadIdx.x; i < f.o.cap; i += kThreads)
-                            sums[i] >>= min(units - now, 63);
+                            sums[i] = fixed_sum(sums[i]) >> min(units - now, 63);
                         __syncthreads();
                     }
                     units = now;
@@ -311,31 +318,30 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
         const int at = lane_at - segment;
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub) {
-            f32x16 s[1], dp = 0.0f;
-            s[0] = 0.0f;
+            f32x16 s = 0.0f, dp = 0.0f;
 #pragma unroll
             for (int i = 0; i < DP / 16; ++i) {
-                s[0] = mma(row_frag<T, DP>(kb, sub, i), q[i], s[0]);
+                s = mma(row_frag<T, DP>(kb, sub, i), q[i], s);
                 dp = mma(row_frag<T, DP>(vb, sub, i), go[i], dp);
             }
-            add_bias<MODE, 1>(s[0], c, bias, pl, at, sub, half);
+            add_bias<MODE, 1>(s, c, bias, pl, at, half_at, sub);
 #pragma unroll
             for (int r = 0; r < 16; ++r)
-                s[0][r] = exp2_fast(s[0][r] - top) * fmaf(dp[r], inv, shift);
+                s[r] = exp2_fast(s[r] - top) * fmaf(dp[r], inv, shift);
             if (j0 + KT > end)
-                clear_behind(s, j0 + 32 * sub, end, half, 0.0f);
+                clear_behind(s, end - j0 - half_at, sub, 0.0f);
             if (MODE != 0 && offsets != nullptr) {
 #pragma unroll
                 for (int gq = 0; gq < 4; ++gq) {
-                    const i32x4 p4 = places<MODE>(pl, sub, gq, half);
+                    const i32x4 p4 = places<MODE>(pl, half_at, sub, gq);
 #pragma unroll
                     for (int t = 0; t < 4; ++t)
-                        add_fixed(sums + at + p4[t], s[0][4 * gq + t], unit);
+                        add_fixed(sums + at + p4[t], s[4 * gq + t], unit);
                 }
             }
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
-                const frag p = acc_frag<T>(s[0], st);
+                const frag p = acc_frag<T>(s, st);
 #pragma unroll
                 for (int i = 0; i < DP / 32; ++i)
                     dq[i] = mma(col_frag<DP>(kb, sub, st, i), p, dq[i]);
@@ -364,6 +370,19 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
 
 // The launch of the keys' side: lanes hold keys, registers queries.
 constexpr int kNoSegment = -(1 << 30);
+// A value of each row of a tile, as accumulators have them.
+__device__ __forceinline__ f32x16 row_values(const float *values, int first, int sub)
+{
+    f32x16 v;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const f32x4 t = *reinterpret_cast<const f32x4 *>(values + first + 16 * sub + 4 * g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            v[4 * g + e] = t[e];
+    }
+    return v;
+}
 template <typename T, int DQP, int MODE>
 __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dkv_kernel(Backward f)
 {
@@ -372,10 +391,10 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dkv_ker
     typedef typename Elem<T>::frag frag;
     constexpr int QT = Tile::kTokens, SUBS = QT / 32;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
-    T *q_lds = reinterpret_cast<T *>(lds_raw), *g_lds = q_lds + 2 * Tile::kElems;
-    float *rows = reinterpret_cast<float *>(g_lds + 2 * Tile::kElems);  // [2][top, inv, shift][QT]
+    float *bias = reinterpret_cast<float *>(lds_raw);  // (at 0: its reads then have their offsets in the instruction)
+    float *rows = bias + f.o.cap;                      // [2][top, inv, -delta][QT]
     int *place = reinterpret_cast<int *>(rows + 6 * QT);
-    float *bias = reinterpret_cast<float *>(place + 2 * QT);
+    T *q_lds = reinterpret_cast<T *>(place + 2 * QT), *g_lds = q_lds + 2 * Tile::kElems;
 
     const AttnGeom &g = f.a.g;
     const int lq = g.lq(), lk = g.lk(), group = g.heads / g.kv_heads;
@@ -390,6 +409,7 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dkv_ker
     id /= f.k_splits;
     const int kv_head = id % g.kv_heads, img = id / g.kv_heads;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int half_at = QT / 2 * half;  // the lane's half of a tile
     const int k0 = block * kQueries, key = k0 + 32 * wave + (lane & 31);
     const int end = f.a.kv_len != nullptr ? min(max(f.a.kv_len[img], 0), lk) : lk;
     const bool k_here = key < end;
@@ -466,7 +486,7 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dkv_ker
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub) {
             s[sub] = 0.0f;
-            dp[sub] = 0.0f;
+            dp[sub] = row_values(rw + 2 * QT, half_at, sub);  // dP - delta starts from -delta
         }
 #pragma unroll
         for (int i = 0; i < DP / 16; ++i)
@@ -477,20 +497,12 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dkv_ker
             }
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub) {
-            add_bias<MODE, -1>(s[sub], c, bias, pl, lane_at - segment, sub, half);
+            add_bias<MODE, -1>(s[sub], c, bias, pl, lane_at - segment, half_at, sub);
+            const f32x16 top = row_values(rw, half_at, sub), inv = row_values(rw + QT, half_at, sub);
 #pragma unroll
-            for (int gq = 0; gq < 4; ++gq) {
-                const int first = 32 * sub + 8 * gq + 4 * half;
-                const f32x4 top = *reinterpret_cast<const f32x4 *>(rw + first);
-                const f32x4 inv = *reinterpret_cast<const f32x4 *>(rw + QT + first);
-                const f32x4 shift = *reinterpret_cast<const f32x4 *>(rw + 2 * QT + first);
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const int r = 4 * gq + t;
-                    const float p = exp2_fast(s[sub][r] - top[t]) * inv[t];
-                    s[sub][r] = p;
-                    dp[sub][r] = p * (dp[sub][r] + shift[t]);
-                }
+            for (int r = 0; r < 16; ++r) {
+                s[sub][r] = exp2_fast(s[sub][r] - top[r]) * inv[r];
+                dp[sub][r] *= s[sub][r];
             }
         }
 #pragma unroll

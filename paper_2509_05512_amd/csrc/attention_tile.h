@@ -7,11 +7,15 @@
 //
 // Products are 32 x 32 tiles over 16 reals of depth.  Lane l of a wave holds
 // row (or column) l % 32 and 8 values of the depth; its accumulators are
-// column l % 32 and the rows 8 (r / 4) + 4 (l / 32) + r % 4, r < 16.  The depth
-// may be dealt to lanes in any order that both operands share, so 8
-// accumulators of a tile, r = 8 s .. 8 s + 7, are at once the operand of depths
-// 16 s + 4 (l / 32) + e % 4 + 8 (e / 4), e < 8: probabilities go from one
-// product to the next without leaving their lanes.
+// column l % 32 and the rows 8 (r / 4) + 4 (l / 32) + r % 4, r < 16.  Rows and
+// depth may be any tokens that both operands agree on.  Row m of the products of
+// part `sub` of a tile of kTile tokens stands for token
+//   kTile / 2 * (m / 4 % 2) + 16 sub + 4 (m / 8) + m % 4,
+// so that accumulator r of a lane is token 16 sub + r of its half-wave's half of
+// the tile.  Then 8 accumulators, r = 8 s .. 8 s + 7, are at once the operand of
+// 8 tokens of depth (the probabilities go from one product to the next without
+// leaving their lanes), and the two half-waves' tokens are 32 apart in bf16: of
+// the 32 neighbouring queries that they hold, none has the same offset to both.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -225,19 +229,19 @@ template <typename T, int DQP> struct WholeMap {
 
 // ------------------------------------------------------------- tiles in LDS
 
-// A tile is read by rows, 16 bytes of 16 neighbouring rows at a time, and in
-// bf16 by columns, 64 bytes of 4 neighbouring rows (tr reads).  Its chunks of
-// 16 bytes change places within a row by a number that the row gives, so that
-// both fall into different banks: rows of 64 bytes (4 in a line of the 64
-// banks) by bits 2 and 3 of the row, of 128 bytes by bit 1 (to the other half of
-// the row) and bits 2, 3, of 256 bytes by bits 0, 1 and 2, 3.  fp32 tiles, read
-// by columns real by real, have 16 bytes between their rows instead.
+// A tile is read by rows, 16 bytes of 16 rows (8 neighbouring ones of each half)
+// at a time, and in bf16 by columns, 64 bytes of 4 neighbouring rows (tr reads).
+// Its chunks of 16 bytes change places within a row by a number that the row
+// gives, so that both fall into different banks: rows of 64 bytes (4 in a line
+// of the 64 banks) by bits 2 and 5 of the row, of 128 bytes by bit 1 (to the
+// other half of the row) and bits 2, 5, of 256 bytes by bits 0, 1 and 2, 5.  fp32
+// tiles, read by columns real by real, have 16 bytes between their rows instead.
 template <typename T, int DP> struct Lds;
 template <int DP> struct Lds<__bf16, DP> {
     static constexpr int kRow = DP;
     static __device__ __forceinline__ int turn(int row)
     {
-        const int q = row >> 2 & 3;
+        const int q = (row >> 2 & 1) | (row >> 4 & 2);
         return DP == 32 ? q : DP == 64 ? (row << 1 & 4) | q : (row << 2 & 12) | q;
     }
     static __device__ __forceinline__ int at(int row, int chunk) { return row * DP + ((chunk ^ turn(row)) << 3); }
@@ -284,39 +288,41 @@ template <typename T, int DP, int THREADS> struct Stage {
             *reinterpret_cast<frag *>(lds + Lds<T, DP>::at(row + i * kStep, d / 8)) = r[i];
     }
 };
-// Operand whose rows are the tile's tokens (32 sub + lane % 32) and whose depth
-// is reals 16 f + 8 (lane / 32) ..+7 of a row.
+// Operand whose rows are the tokens of a tile's part `sub` and whose depth is
+// reals 16 f + 8 (lane / 32) ..+7 of a row.
 template <typename T, int DP> __device__ __forceinline__ typename Elem<T>::frag row_frag(const T *tile, int sub, int f)
 {
-    const int lane = threadIdx.x & 63;
-    return *reinterpret_cast<const typename Elem<T>::frag *>(tile + Lds<T, DP>::at(lane & 31, 2 * f + (lane >> 5)) +
-                                                             32 * sub * Lds<T, DP>::kRow);
+    const int lane = threadIdx.x & 63, m = lane & 31;
+    const int row = Elem<T>::kTile / 2 * (m >> 2 & 1) + 4 * (m >> 3) + (m & 3);
+    // (16 rows on, a row's turn of chunks is the same)
+    return *reinterpret_cast<const typename Elem<T>::frag *>(tile + Lds<T, DP>::at(row, 2 * f + (lane >> 5)) +
+                                                             16 * sub * Lds<T, DP>::kRow);
 }
 
-// Operand whose rows are reals 32 mt + lane % 32 and whose depth is the tile's
-// tokens 32 sub + 16 s + 4 (lane / 32) + e % 4 + 8 (e / 4): acc_frag's order.
-// In bf16 four tokens of one real come from one transposing read, in which 16
-// lanes give the addresses of 4 rows of 16 reals.  (Rows 16 apart have the same
-// turn of chunks.)
+// Operand whose rows are reals 32 mt + lane % 32 and whose depth is the tokens
+// that acc_frag(., s) of part `sub` stands for: 16 sub + 8 s ..+7 of the lane's
+// half of the tile.  In bf16 four tokens of one real come from one transposing
+// read, in which 16 lanes give the addresses of 4 rows of 16 reals.
 template <int DP> __device__ __forceinline__ bf16x8 col_frag(const __bf16 *tile, int sub, int s, int mt)
 {
     typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
     const int lane = threadIdx.x & 63, i = lane & 15;
-    const int row = 4 * (lane >> 5) + (i >> 2), chunk = 4 * mt + (lane >> 3 & 2) + (i >> 1 & 1), at = 4 * (i & 1);
-    const __bf16 *p = tile + (32 * sub + 16 * s) * DP + at;
+    const int row = Elem<__bf16>::kTile / 2 * (lane >> 5) + (i >> 2), at = 4 * (i & 1);
+    const int chunk = 4 * mt + (lane >> 3 & 2) + (i >> 1 & 1);
+    const __bf16 *p = tile + (16 * sub + 8 * s) * DP + at;
     const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(p + Lds<__bf16, DP>::at(row, chunk)));
-    const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(p + Lds<__bf16, DP>::at(row + 8, chunk)));
+    const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(p + Lds<__bf16, DP>::at(row + 4, chunk)));
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 template <int DP> __device__ __forceinline__ f32x8 col_frag(const float *tile, int sub, int s, int mt)
 {
     constexpr int kRow = Lds<float, DP>::kRow;
     const int lane = threadIdx.x & 63;
-    const float *p = tile + (32 * sub + 16 * s + 4 * (lane >> 5)) * kRow + 32 * mt + (lane & 31);
+    const float *p = tile + (Elem<float>::kTile / 2 * (lane >> 5) + 16 * sub + 8 * s) * kRow + 32 * mt + (lane & 31);
     f32x8 v;
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-        v[e] = p[((e & 3) + 8 * (e >> 2)) * kRow];
+        v[e] = p[e * kRow];
     return v;
 }
 
@@ -395,9 +401,10 @@ __device__ __forceinline__ void stage_bias(float *lds, const Offsets &o, const A
 
 // Places of the 4 tokens of a quad of accumulators.  MODE 1: they lie in one row
 // of the map; 2: anywhere.
-template <int MODE> __device__ __forceinline__ i32x4 places(const int *place, int sub, int quad, int half)
+// (`first`: the lane's half of the tile's first token.)
+template <int MODE> __device__ __forceinline__ i32x4 places(const int *place, int first, int sub, int quad)
 {
-    const int *p = place + 32 * sub + 8 * quad + 4 * half;
+    const int *p = place + first + 16 * sub + 4 * quad;
     if (MODE == 2)
         return *reinterpret_cast<const i32x4 *>(p);
     const int p0 = MODE == 1 ? p[0] : 0;
@@ -406,8 +413,8 @@ template <int MODE> __device__ __forceinline__ i32x4 places(const int *place, in
 // Scores in units of log 2: c times the products plus the bias of the lane's
 // offset `at` + SIGN * place (MODE 0: no bias).
 template <int MODE, int SIGN>
-__device__ __forceinline__ void add_bias(f32x16 &s, float c, const float *bias, const int *place, int at, int sub,
-                                         int half)
+__device__ __forceinline__ void add_bias(f32x16 &s, float c, const float *bias, const int *place, int at, int first,
+                                         int sub)
 {
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
@@ -416,32 +423,28 @@ __device__ __forceinline__ void add_bias(f32x16 &s, float c, const float *bias, 
             for (int t = 0; t < 4; ++t)
                 s[4 * g + t] *= c;
         } else if (MODE == 1) {
-            const int p0 = place[32 * sub + 8 * g + 4 * half];
+            const int p0 = place[first + 16 * sub + 4 * g];
             const float *b = bias + (SIGN > 0 ? at + p0 : at - p0 - 3);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
                 s[4 * g + t] = fmaf(s[4 * g + t], c, b[SIGN > 0 ? t : 3 - t]);
         } else {
-            const i32x4 p = places<MODE>(place, sub, g, half);
+            const i32x4 p = places<MODE>(place, first, sub, g);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
                 s[4 * g + t] = fmaf(s[4 * g + t], c, bias[at + SIGN * p[t]]);
         }
     }
 }
-// `value` in the places of a tile's tokens (rows of accumulators) at or behind
-// `end`.  (The empty statement ties the comparisons to this branch: the compiler
-// would else make selects of them for every tile.)
-template <int SUBS>
-__device__ __forceinline__ void clear_behind(f32x16 (&s)[SUBS], int first, int end, int half, float value)
+// `value` in the accumulators of part `sub` whose tokens are at or behind `left`
+// of the lane's half of the tile.  (The empty statement ties the comparisons to
+// this branch: the compiler would else make selects of them for every tile.)
+__device__ __forceinline__ void clear_behind(f32x16 &s, int left, int sub, float value)
 {
-    int left = end - first - 4 * half;
     asm volatile("" : "+v"(left));
 #pragma unroll
-    for (int sub = 0; sub < SUBS; ++sub)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-            s[sub][r] = 32 * sub + 8 * (r / 4) + r % 4 >= left ? value : s[sub][r];
+    for (int r = 0; r < 16; ++r)
+        s[r] = 16 * sub + r >= left ? value : s[r];
 }
 
 // The work-group's place among `total` in an order in which neighbours run on
