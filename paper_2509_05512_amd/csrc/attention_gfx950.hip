@@ -64,6 +64,11 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_forward_kernel(Forward f
     const int end = min(len, first + f.tiles_per_split * KT);
 
     const WholeMap<T, DQP> qm(f.a.q, img, head), km(f.a.k, img, kv_head), vm(f.a.v, img, kv_head);
+    Tile kt, vt;
+    if (first < end) {
+        kt.fetch(km, first, end);
+        vt.fetch(vm, first, end);
+    }
     frag q[DP / 16];
 #pragma unroll
     for (int i = 0; i < DP / 16; ++i)
@@ -91,11 +96,6 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_forward_kernel(Forward f
     }
     const int high = MODE != 0 ? high_q + place_k(f.o, max(end, 1) - 1) + 4 : 0;  // past the last offset
 
-    Tile kt, vt;
-    if (first < end) {
-        kt.fetch(km, first, end);
-        vt.fetch(vm, first, end);
-    }
     int buf = 0;
     for (int j0 = first; j0 < end; j0 += KT, buf ^= 1) {
         T *kb = k_lds + buf * Tile::kElems, *vb = v_lds + buf * Tile::kElems;
@@ -305,8 +305,9 @@ __global__ void __launch_bounds__(256) attention_join_kernel(Forward f)
 struct Token {
     int heads_per_block, slots, kv_blocks, group_blocks, chunk;
 };
-constexpr int kTokenBias = 4096;  // biases in LDS: keys of a chunk x query heads of the work-group
+constexpr int kTokenBias = 8192;  // biases in LDS: keys of a chunk x query heads of the work-group
 constexpr int kTokenUnroll = 4;   // keys that a set of lanes reads at a time
+constexpr int kTokenThreads = 256;
 
 // Sum over the 4, 8 or 16 lanes of a row.
 template <int G> __device__ __forceinline__ float lanes_sum(float x)
@@ -324,13 +325,15 @@ template <int G> __device__ __forceinline__ float lanes_sum(float x)
 }
 
 template <typename T, int DQP, int GRP, bool BIAS>
-__global__ void __launch_bounds__(256) attention_token_kernel(Forward f, Token tk)
+__global__ void __launch_bounds__(kTokenThreads) attention_token_kernel(Forward f, Token tk)
 {
-    constexpr int DP = 4 * DQP, G = DP / 8, kPairs = 256 / G, U = kTokenUnroll;
+    constexpr int DP = 4 * DQP, G = DP / 8, kThreads = kTokenThreads, kPairs = kThreads / G, U = kTokenUnroll;
     typedef typename Elem<T>::frag frag;
-    __shared__ float acc_lds[kPairs * GRP * DP];
+    // (a chunk's biases are done with when the results are joined)
+    constexpr int kLds = kPairs * GRP * DP > kTokenBias ? kPairs * GRP * DP : kTokenBias;
+    __shared__ __attribute__((aligned(16))) float acc_lds[kLds];
     __shared__ float stat_lds[kPairs * GRP * 2];
-    __shared__ float bias_lds[BIAS ? kTokenBias : 1];
+    float *bias_lds = acc_lds;
     const AttnGeom &g = f.a.g;
     const int lk = g.lk(), group = g.heads / g.kv_heads;
     int id = blockIdx.x;
@@ -373,7 +376,7 @@ __global__ void __launch_bounds__(256) attention_token_kernel(Forward f, Token t
         const int c1 = min(c0 + chunk, end);
         if (BIAS) {
             __syncthreads();  // the last chunk's biases have been read
-            for (int j = c0 + int(threadIdx.x); j < c1; j += 256) {
+            for (int j = c0 + int(threadIdx.x); j < c1; j += kThreads) {
                 const float *row = f.a.bias.table + bucket_of(f.o, f.a.bias, place_k(f.o, j), pos_y, pos_x);
                 for (int h = 0; h < tk.heads_per_block; ++h)
 #pragma unroll
@@ -387,7 +390,7 @@ __global__ void __launch_bounds__(256) attention_token_kernel(Forward f, Token t
         }
         if (!active)
             continue;
-        for (int j = c0 + slot; j < c1; j += U * tk.slots) {
+        for (int j = c0 + slot; j < c1; j += round) {
             frag k[U], v[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -449,6 +452,7 @@ __global__ void __launch_bounds__(256) attention_token_kernel(Forward f, Token t
         }
     }
     // the slots' results joined, a thread per real of a head
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < GRP; ++i) {
         const int at = pair * GRP + i;
@@ -460,7 +464,7 @@ __global__ void __launch_bounds__(256) attention_token_kernel(Forward f, Token t
     }
     __syncthreads();
     const int64_t rows = int64_t(g.n) * g.heads;
-    for (int e = threadIdx.x; e < tk.heads_per_block * GRP * DP; e += 256) {
+    for (int e = threadIdx.x; e < tk.heads_per_block * GRP * DP; e += kThreads) {
         const int real = e % DP, i = e / DP % GRP, h = e / DP / GRP;
         const int kvh = kvb * tk.heads_per_block + h, head = kvh * group + gb * GRP + i;
         if (kvh >= g.kv_heads || i >= heads_here)
@@ -507,8 +511,9 @@ Plan forward_plan(const AttnCall &a, DType dt, bool may_split = true)
     const int lq = g.lq();
     if (lq == 1) {
         // one query: heads of a token side by side
-        const int pairs = 256 / (dp / 8), group = g.heads / g.kv_heads;
+        const int group = g.heads / g.kv_heads;
         p.grp = group == 1 ? 1 : group == 2 ? 2 : 4;
+        const int pairs = kTokenThreads / (dp / 8);
         p.token.heads_per_block = std::min(g.kv_heads, pairs);
         p.token.slots = pairs / p.token.heads_per_block;
         p.token.kv_blocks = (g.kv_heads + p.token.heads_per_block - 1) / p.token.heads_per_block;
@@ -516,10 +521,12 @@ Plan forward_plan(const AttnCall &a, DType dt, bool may_split = true)
         p.blocks = 1;
         // (biases of a work-group's heads for a chunk of keys fill the LDS array)
         p.token.chunk = kTokenBias / (p.token.heads_per_block * p.grp);
-        // four work-groups per compute unit, two rounds of keys at least to each
+        // up to four rounds of keys in one work-group; beyond that, or where
+        // the chip has room, two rounds at least to each of several
         const int64_t groups = int64_t(g.n) * p.token.kv_blocks * p.token.group_blocks;
-        const int rounds = (g.lk() + 2 * kTokenUnroll * p.token.slots - 1) / (2 * kTokenUnroll * p.token.slots);
-        p.splits = may_split ? int(std::max<int64_t>(1, std::min<int64_t>(1024 / groups, rounds))) : 1;
+        const int rounds = (g.lk() + kTokenUnroll * p.token.slots - 1) / (kTokenUnroll * p.token.slots);
+        const int64_t room = 1024 / groups;
+        p.splits = may_split && rounds > 4 ? int(std::max<int64_t>(1, std::min<int64_t>(room, (rounds + 1) / 2))) : 1;
         return p;
     }
     // half work-groups where whole ones would leave half of their queries empty
@@ -578,9 +585,9 @@ template <typename T, int DQP, int GRP> hipError_t token_launch(const Forward &f
     const AttnGeom &g = f.a.g;
     const unsigned grid = unsigned(int64_t(g.n) * p.token.kv_blocks * p.token.group_blocks * p.splits);
     if (f.a.bias.table != nullptr)
-        attention_token_kernel<T, DQP, GRP, true><<<grid, 256, 0, s>>>(f, p.token);
+        attention_token_kernel<T, DQP, GRP, true><<<grid, kTokenThreads, 0, s>>>(f, p.token);
     else
-        attention_token_kernel<T, DQP, GRP, false><<<grid, 256, 0, s>>>(f, p.token);
+        attention_token_kernel<T, DQP, GRP, false><<<grid, kTokenThreads, 0, s>>>(f, p.token);
     if (hipError_t e = hipGetLastError())
         return e;
     if (p.splits > 1) {

@@ -146,6 +146,11 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
     const int64_t row = (int64_t(img) * g.heads + head) * lq + query;
 
     const WholeMap<T, DQP> qm(f.a.q, img, head), km(f.a.k, img, kv_head), vm(f.a.v, img, kv_head);
+    Tile kt, vt;
+    if (begin < end) {
+        kt.fetch(km, begin, end);
+        vt.fetch(vm, begin, end);
+    }
     frag q[DP / 16], go[DP / 16];
     float delta = 0.0f;
     {
@@ -192,6 +197,16 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
         done = low_q;
     }
     const int past = MODE != 0 ? high_q + place_k(f.o, lk - 1) + 1 : 0;  // past the last offset
+    auto start_segment = [&](int lo) {
+        segment = lo;
+        const int count = min(f.o.cap, past + 3 - segment);  // (a quad may pass the last offset)
+        stage_bias(bias, f.o, f.a.bias, table, segment, count, pos_y, pos_x);
+        if (offsets != nullptr)
+            for (int e = threadIdx.x; e < count; e += kThreads)
+                sums[e] = 0;
+    };
+    if (MODE != 0 && begin < end)
+        start_segment(low_q + place_k(f.o, begin));
     // the bound's parts from the work-group's rows: |dO| and |delta|; a row whose
     // sum is no number has NaN
     float top_go = 0.0f, top_delta = 0.0f;
@@ -251,11 +266,6 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i)
         dq[i] = 0.0f;
-    Tile kt, vt;
-    if (begin < end) {
-        kt.fetch(km, begin, end);
-        vt.fetch(vm, begin, end);
-    }
     int buf = 0;
     for (int j0 = begin; j0 < end; j0 += KT, buf ^= 1) {
         T *kb = k_lds + buf * Tile::kElems, *vb = v_lds + buf * Tile::kElems;
@@ -271,19 +281,12 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
             if (threadIdx.x < KT)
                 pl[threadIdx.x] = place_k(f.o, min(j0 + int(threadIdx.x), lk - 1));
             const int lo = low_q + place_k(f.o, j0), hi = high_q + place_k(f.o, min(j0 + KT, lk) - 1) + 3;
-            if (segment < 0 || hi >= segment + f.o.cap) {
-                if (segment >= 0) {
-                    __syncthreads();  // the last segment has been read and added to
-                    if (offsets != nullptr)
-                        flush();
-                    __syncthreads();
-                }
-                segment = lo;
-                const int count = min(f.o.cap, past + 3 - segment);  // (a quad may pass the last offset)
-                stage_bias(bias, f.o, f.a.bias, table, segment, count, pos_y, pos_x);
+            if (hi >= segment + f.o.cap) {
+                __syncthreads();  // the last segment has been read and added to
                 if (offsets != nullptr)
-                    for (int e = threadIdx.x; e < count; e += kThreads)
-                        sums[e] = 0;
+                    flush();
+                __syncthreads();
+                start_segment(lo);
             }
         }
         __syncthreads();
