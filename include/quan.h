@@ -612,7 +612,8 @@ QUAN_API int quan_relpos_buckets(int32_t radius, int32_t buckets, int32_t *map);
  *   heads      divides C; dq <= 32, and dq must divide k's channels into a
  *              number of heads that divides `heads`.
  *   rest       NULL, or (bf16) a 16-byte aligned dense map like out's that
- *              receives bf16(out before rounding - out).
+ *              receives, for the backward pass, what the rounding of out
+ *              left (16 bits a real; out and rest give the fp32 results).
  *   stats      NULL, or fp32 [N][heads][Hq*Wq][2]: each row's maximum in units
  *              of log 2 (at least the type's lowest; 0 for a row without a
  *              key) and the sum of 2^(score - maximum).

@@ -25,11 +25,13 @@ struct Forward {
     float *part, *part_stats;             // [split][row][D], [split][row][2] (splits > 1)
 };
 
-// EXACT (a training step in bf16): the probabilities meet v in two parts, the
-// rounded one and what it leaves.  The gradient of the bias, which is fp32, goes
-// by the rows' sums of dout out, and with probabilities of 8 bits alone 3e-4 of
-// its norm was wrong (1e-6 with both parts).
-template <typename T, int DQP, int MODE, int NW, bool EXACT>
+// PARTS (3 in a training step in bf16, else 1): bf16 numbers that a probability
+// meets v in, each what the ones before leave of it.  The gradient of the bias,
+// which is fp32, goes by the rows' sums of dout out: with probabilities of 8 bits
+// 3e-4 of its norm was wrong, of 16 bits 1e-6 to 7e-6, of 24 bits what fp32
+// leaves, 1e-7 to 4e-7.  The third part is 45 us of the 270 at 1600 queries and
+// keys, 16 images, 8 heads of 64 reals.
+template <typename T, int DQP, int MODE, int NW, int PARTS>
 __global__ void __launch_bounds__(64 * NW, 2) attention_forward_kernel(Forward f)
 {
     constexpr int DP = 4 * DQP, kThreads = 64 * NW, kQueries = 32 * NW;
@@ -118,6 +120,8 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_forward_kernel(Forward f
             kt.fetch(km, j0 + KT, end);
             vt.fetch(vm, j0 + KT, end);
         }
+        if (q0 + 32 * wave >= lq)
+            continue;  // (none of the wave's queries is there)
         f32x16 s[SUBS];
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub) {
@@ -162,15 +166,19 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_forward_kernel(Forward f
         for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
-                const frag p = acc_frag<T>(s[sub], st);
+                frag p[PARTS];
 #pragma unroll
-                for (int i = 0; i < DP / 32; ++i)
-                    o[i] = mma(col_frag<DP>(vb, sub, st, i), p, o[i]);
-                if (EXACT) {
-                    const frag r = rest_frag<T>(s[sub], st, p);
+                for (int part = 0; part < PARTS; ++part) {
+                    if (part > 0)
+                        take_from(s[sub], st, p[part - 1]);
+                    p[part] = acc_frag<T>(s[sub], st);
+                }
 #pragma unroll
-                    for (int i = 0; i < DP / 32; ++i)
-                        o[i] = mma(col_frag<DP>(vb, sub, st, i), r, o[i]);
+                for (int i = 0; i < DP / 32; ++i) {
+                    const frag column = col_frag<DP>(vb, sub, st, i);
+#pragma unroll
+                    for (int part = 0; part < PARTS; ++part)
+                        o[i] = mma(column, p[part], o[i]);
                 }
             }
     }
@@ -202,17 +210,20 @@ __global__ void __launch_bounds__(64 * NW, 2) attention_forward_kernel(Forward f
         o[i] *= inv;
         om.store(query, i, half, o[i], q_here);
     }
-    if (f.rest != nullptr && sizeof(T) == 2) {
+    if constexpr (sizeof(T) == 2)
+        if (f.rest != nullptr) {
         const int64_t c_all = int64_t(g.heads) * g.dq;
         const AttnMap dense{f.rest, lq * 4 * c_all, 4 * c_all, c_all, g.dq % 8 == 0, g.dq};
         const HeadMap<T, DQP> rm(dense, img, head, g.dq);
 #pragma unroll
-        for (int i = 0; i < DP / 32; ++i) {
+        for (int i = 0; i < DP / 32; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                o[i][r] -= float(T(o[i][r]));
-            rm.store(query, i, half, o[i], q_here);
-        }
+            for (int gq = 0; gq < 4; ++gq) {
+                const int d = 32 * i + 8 * gq + 4 * half;
+                const f32x4 v = {o[i][4 * gq], o[i][4 * gq + 1], o[i][4 * gq + 2], o[i][4 * gq + 3]};
+                if (q_here)
+                    store_rest(rm.at(query, d), v, rm.valid(d, 4), rm.vec);
+            }
     }
     if (f.stats != nullptr && half == 0 && q_here) {
         f.stats[2 * row] = top == -INFINITY ? 0.0f : top;
@@ -233,10 +244,11 @@ __device__ __forceinline__ void finish_real(const Forward &f, int64_t row, int r
     if (om.valid(real, 1) > 0) {
         const T rounded = T(value);
         *om.at(query, real) = rounded;
-        if (f.rest != nullptr && sizeof(T) == 2) {
+        if constexpr (sizeof(T) == 2)
+            if (f.rest != nullptr) {
             const int64_t c_all = int64_t(g.heads) * g.dq;
-            static_cast<T *>(f.rest)[((img * lq + query) * 4 + real / DQP) * c_all + int64_t(head) * g.dq + real % DQP] =
-                T(value - float(rounded));
+            static_cast<short *>(f.rest)[((img * lq + query) * 4 + real / DQP) * c_all + int64_t(head) * g.dq + real % DQP] =
+                rest_of(value, rounded);
         }
     }
     if (f.stats != nullptr && real == 0) {
@@ -564,15 +576,16 @@ hipError_t forward_launch(const Forward &f, const Plan &p, hipStream_t s)
 {
     const AttnGeom &g = f.a.g;
     const unsigned grid = xcd_grid(int64_t(g.n) * g.heads * p.splits * p.blocks);
-    const bool exact = sizeof(T) == 2 && f.rest != nullptr;
-    if (p.waves == 4 && exact)
-        attention_forward_kernel<T, DQP, MODE, 4, sizeof(T) == 2><<<grid, 256, p.lds, s>>>(f);
+    constexpr int kParts = sizeof(T) == 2 ? 3 : 1;
+    const bool train = f.rest != nullptr;
+    if (p.waves == 4 && train)
+        attention_forward_kernel<T, DQP, MODE, 4, kParts><<<grid, 256, p.lds, s>>>(f);
     else if (p.waves == 4)
-        attention_forward_kernel<T, DQP, MODE, 4, false><<<grid, 256, p.lds, s>>>(f);
-    else if (exact)
-        attention_forward_kernel<T, DQP, MODE, 2, sizeof(T) == 2><<<grid, 128, p.lds, s>>>(f);
+        attention_forward_kernel<T, DQP, MODE, 4, 1><<<grid, 256, p.lds, s>>>(f);
+    else if (train)
+        attention_forward_kernel<T, DQP, MODE, 2, kParts><<<grid, 128, p.lds, s>>>(f);
     else
-        attention_forward_kernel<T, DQP, MODE, 2, false><<<grid, 128, p.lds, s>>>(f);
+        attention_forward_kernel<T, DQP, MODE, 2, 1><<<grid, 128, p.lds, s>>>(f);
     if (hipError_t e = hipGetLastError())
         return e;
     if (p.splits > 1) {

@@ -160,9 +160,8 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
             const int d = 16 * i + 8 * half;
             q[i] = qm.load(query, d, q_here);
             go[i] = gm.load(query, d, q_here);
-            f32x8 o = to_f32(om.load(query, d, q_here));
-            if (f.rest.data != nullptr)
-                o += to_f32(rm.load(query, d, q_here));
+            const frag rounded = om.load(query, d, q_here);
+            const f32x8 o = f.rest.data != nullptr ? with_rest(rounded, rm.load(query, d, q_here)) : to_f32(rounded);
             const f32x8 w = to_f32(go[i]);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -318,9 +317,13 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
                 }
             }
         }
+        if (q0 + 32 * wave >= lq)
+            continue;  // (none of the wave's queries is there)
         const int at = lane_at - segment;
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub) {
+            if (16 * sub >= end - j0)
+                break;
             f32x16 s = 0.0f, dp = 0.0f;
 #pragma unroll
             for (int i = 0; i < DP / 16; ++i) {
@@ -333,7 +336,9 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
                 s[r] = exp2_fast(s[r] - top) * fmaf(dp[r], inv, shift);
             if (j0 + KT > end)
                 clear_behind(s, end - j0 - half_at, sub, 0.0f);
-            if (MODE != 0 && offsets != nullptr) {
+            // (lanes without a query would all add to the last one's offsets, and
+            // such additions take their turns: 5 of a small launch's 17 us)
+            if (MODE != 0 && offsets != nullptr && q_here) {
 #pragma unroll
                 for (int gq = 0; gq < 4; ++gq) {
                     const i32x4 p4 = places<MODE>(pl, half_at, sub, gq);
@@ -445,10 +450,18 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dkv_ker
     const int tiles = (lq + QT - 1) / QT, first = split * f.k_tiles;
     const int last = k0 < end ? min(group * tiles, first + f.k_tiles) : first;
     Tile qt, gt;
+    float row_top = 0.0f, row_sum = 0.0f, row_delta = 0.0f;  // of thread t < QT's query of a tile
     auto fetch = [&](int item) {
         const int head = kv_head * group + item / tiles, i0 = (tiles - 1 - item % tiles) * QT;
         qt.fetch(WholeMap<T, DQP>(f.a.q, img, head), i0, lq);
         gt.fetch(WholeMap<T, DQP>(f.dout, img, head), i0, lq);
+        if (threadIdx.x < QT) {
+            const int i = i0 + threadIdx.x;
+            const int64_t row = (int64_t(img) * g.heads + head) * lq + min(i, lq - 1);
+            row_top = f.stats[2 * row];
+            row_sum = i < lq ? f.stats[2 * row + 1] : 0.0f;
+            row_delta = f.delta[row];
+        }
     };
     if (first < last)
         fetch(first);
@@ -456,22 +469,18 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dkv_ker
     for (int item = first; item < last; ++item, buf ^= 1) {
         const int head = kv_head * group + item / tiles, i0 = (tiles - 1 - item % tiles) * QT;
         const float *table = MODE != 0 ? f.a.bias.table + int64_t(head) * f.a.bias.ny * f.a.bias.nx : nullptr;
-        const int64_t row0 = (int64_t(img) * g.heads + head) * lq;
         T *qb = q_lds + buf * Tile::kElems, *gb = g_lds + buf * Tile::kElems;
         int *pl = place + buf * QT;
         float *rw = rows + buf * 3 * QT;
         qt.put(qb);
         gt.put(gb);
         if (threadIdx.x < QT) {
-            const int i = i0 + threadIdx.x;
-            const float sum = i < lq ? f.stats[2 * (row0 + i) + 1] : 0.0f;
-            const bool empty = sum == 0.0f;
-            const float inv = empty ? 0.0f : 1.0f / sum;
-            rw[threadIdx.x] = empty ? INFINITY : f.stats[2 * (row0 + i)];
-            rw[QT + threadIdx.x] = inv;
-            rw[2 * QT + threadIdx.x] = empty ? 0.0f : -f.delta[row0 + i];
+            const bool empty = row_sum == 0.0f;
+            rw[threadIdx.x] = empty ? INFINITY : row_top;
+            rw[QT + threadIdx.x] = empty ? 0.0f : 1.0f / row_sum;
+            rw[2 * QT + threadIdx.x] = empty ? 0.0f : -row_delta;
             if (MODE != 0)
-                pl[threadIdx.x] = place_q(f.o, min(i, lq - 1));
+                pl[threadIdx.x] = place_q(f.o, min(i0 + int(threadIdx.x), lq - 1));
         }
         if (MODE != 0) {
             const int lo = low_k - place_q(f.o, min(i0 + QT, lq) - 1) - 3, hi = high_k - place_q(f.o, i0);
@@ -485,6 +494,8 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dkv_ker
         __syncthreads();
         if (item + 1 < last)
             fetch(item + 1);
+        if (k0 + 32 * wave >= end)
+            continue;  // (none of the wave's keys is there)
         f32x16 s[SUBS], dp[SUBS];
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub) {

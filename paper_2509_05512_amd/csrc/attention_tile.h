@@ -28,6 +28,9 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -88,16 +91,37 @@ template <typename T> __device__ __forceinline__ typename Elem<T>::frag acc_frag
     return to_frag<T>(t);
 }
 
-// What the rounding of accumulators 8 s .. 8 s + 7 to `rounded` left.
-template <typename T>
-__device__ __forceinline__ typename Elem<T>::frag rest_frag(const f32x16 &v, int s, const typename Elem<T>::frag &rounded)
+// Takes from accumulators 8 s .. 8 s + 7 what they were rounded to.
+template <typename F> __device__ __forceinline__ void take_from(f32x16 &v, int s, const F &rounded)
 {
     const f32x8 r = to_f32(rounded);
-    f32x8 t;
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-        t[e] = v[8 * s + e] - r[e];
-    return to_frag<T>(t);
+        v[8 * s + e] -= r[e];
+}
+
+// What the rounding of a result to bf16 leaves, in 16 bits: by how much the bits
+// of the fp32 value are above those of the rounded one, at most half of its last
+// place (a tie, the one distance that does not fit, is cut by 2^-24 of the value).
+__device__ __forceinline__ short rest_of(float value, __bf16 rounded)
+{
+    const int above = int(__float_as_uint(value) - (unsigned(__builtin_bit_cast(unsigned short, rounded)) << 16));
+    return short(max(min(above, 32767), -32768));
+}
+// The fp32 values again.
+__device__ __forceinline__ f32x8 with_rest(const bf16x8 &rounded, const bf16x8 &rest)
+{
+    const auto high = __builtin_bit_cast(u16x8, rounded);
+    const auto low = __builtin_bit_cast(s16x8, rest);
+    f32x8 v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        v[e] = __uint_as_float((unsigned(high[e]) << 16) + unsigned(int(low[e])));
+    return v;
+}
+__device__ __forceinline__ f32x8 with_rest(const f32x8 &value, const f32x8 &)
+{
+    return value;
 }
 
 // Values of the two half-waves joined: the lane's own and lane ^ 32's.
@@ -170,6 +194,24 @@ __device__ __forceinline__ void store_quad(float *p, const f32x4 &v, int valid, 
         for (int e = 0; e < 4; ++e)
             if (e < valid)
                 p[e] = v[e];
+    }
+}
+
+__device__ __forceinline__ void store_rest(__bf16 *to, const f32x4 &v, int valid, bool vec)
+{
+    s16x4 f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        f[e] = rest_of(v[e], __bf16(v[e]));
+    short *p = reinterpret_cast<short *>(to);
+    if (vec) {
+        if (valid > 0)
+            *reinterpret_cast<s16x4 *>(p) = f;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < valid)
+                p[e] = f[e];
     }
 }
 
