@@ -644,8 +644,9 @@ QUAN_API int quan_attention_forward(const quan_tensor *q, const quan_tensor *k, 
  *              map may be passed), overlapping nothing else.  dk and dv are
  *              sums over the heads that share them, and zero behind kv_len.
  *   dtable     fp32 [heads][buckets_y * buckets_x], or NULL.
- * Every other argument is the forward's.  Sums have a fixed order (dtable's in
- * fp32 within a tile of queries, in fp64 beyond): deterministic.  Uses a
+ * Every other argument is the forward's.  Sums have a fixed order (dtable's are
+ * whole numbers of 2^-42 of a bound of their terms within a block of 128
+ * queries, fp64 beyond): deterministic.  Uses a
  * workspace per (device, stream), with dtable of about 4 * N * heads *
  * (Hq*Wq / 128) * (offsets of a map) bytes.
  */

@@ -1,10 +1,14 @@
 // Attention between the pixels of quaternion maps on gfx950, forward.
 //
-// A work-group takes NW x 32 queries of one head and image and walks over the
-// keys in tiles of LDS with the running maximum and sum of a softmax; a wave
-// holds its 32 queries' rows, and the transposed scores S^T = K Q^T leave a
+// A work-group of four waves takes 128 queries of one head and image and walks
+// over the keys in tiles of LDS with the running maximum and sum of a softmax; a
+// wave holds its 32 queries' rows, and the transposed scores S^T = K Q^T leave a
 // query's scores in two lanes (see attention_tile.h), so that maxima and sums
 // are taken in registers and the probabilities are the next product's operand.
+// What bounds it is what a wave issues between two products: 16 exponentials,
+// sums and biases of a lane's scores, and the tiles' way out of LDS.  2 images of
+// 80 x 80, 4 heads of 128 reals: 255 us, 660 TFLOP/s; 16 of 40 x 40, 8 heads of
+// 64, in training 271 us, 620 TFLOP/s (matrix units busy 25 and 29 % of the time).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -13,6 +17,8 @@
 
 namespace quan {
 namespace {
+
+constexpr int kThreads = 256, kQueries = 128;  // of a work-group: a wave per 32 queries
 
 // What a forward launch computes, and where its partial results go.
 struct Forward {
@@ -31,10 +37,10 @@ struct Forward {
 // 3e-4 of its norm was wrong, of 16 bits 1e-6 to 7e-6, of 24 bits what fp32
 // leaves, 1e-7 to 4e-7.  The third part is 45 us of the 270 at 1600 queries and
 // keys, 16 images, 8 heads of 64 reals.
-template <typename T, int DQP, int MODE, int NW, int PARTS>
-__global__ void __launch_bounds__(64 * NW, 2) attention_forward_kernel(Forward f)
+template <typename T, int DQP, int MODE, int PARTS>
+__global__ void __launch_bounds__(kThreads, 2) attention_forward_kernel(Forward f)
 {
-    constexpr int DP = 4 * DQP, kThreads = 64 * NW, kQueries = 32 * NW;
+    constexpr int DP = 4 * DQP;
     typedef Stage<T, DP, kThreads> Tile;
     typedef typename Elem<T>::frag frag;
     constexpr int KT = Tile::kTokens, SUBS = KT / 32;
@@ -313,13 +319,14 @@ __global__ void __launch_bounds__(256) attention_join_kernel(Forward f)
 // of its own; they are joined in LDS, and those of several splits of an image's
 // keys (equal shares of what the image has) by attention_join_kernel.  Biases of
 // a chunk of keys are looked up into LDS at a time.  Bound by reading keys and
-// values once.
+// values once, and below that by a first key's way from memory: a cache of 4 x
+// 65536 keys (half of them there), 8 heads of 64 reals on 2 of keys: 27 us, 2.5
+// TB/s, and 4 us of joining; 64 maps of 20 x 20, 4 heads of 64: 12 and 3 us.
 struct Token {
     int heads_per_block, slots, kv_blocks, group_blocks, chunk;
 };
 constexpr int kTokenBias = 8192;  // biases in LDS: keys of a chunk x query heads of the work-group
 constexpr int kTokenUnroll = 4;   // keys that a set of lanes reads at a time
-constexpr int kTokenThreads = 256;
 
 // Sum over the 4, 8 or 16 lanes of a row.
 template <int G> __device__ __forceinline__ float lanes_sum(float x)
@@ -337,9 +344,9 @@ template <int G> __device__ __forceinline__ float lanes_sum(float x)
 }
 
 template <typename T, int DQP, int GRP, bool BIAS>
-__global__ void __launch_bounds__(kTokenThreads) attention_token_kernel(Forward f, Token tk)
+__global__ void __launch_bounds__(kThreads) attention_token_kernel(Forward f, Token tk)
 {
-    constexpr int DP = 4 * DQP, G = DP / 8, kThreads = kTokenThreads, kPairs = kThreads / G, U = kTokenUnroll;
+    constexpr int DP = 4 * DQP, G = DP / 8, kPairs = kThreads / G, U = kTokenUnroll;
     typedef typename Elem<T>::frag frag;
     // (a chunk's biases are done with when the results are joined)
     constexpr int kLds = kPairs * GRP * DP > kTokenBias ? kPairs * GRP * DP : kTokenBias;
@@ -508,7 +515,7 @@ __global__ void __launch_bounds__(kTokenThreads) attention_token_kernel(Forward 
 // ---------------------------------------------------------------------- host
 
 struct Plan {
-    int waves, blocks, splits, tiles_per_split, cap;
+    int blocks, splits, tiles_per_split, cap;
     size_t lds;
     Token token;  // one query
     int grp;
@@ -525,7 +532,7 @@ Plan forward_plan(const AttnCall &a, DType dt, bool may_split = true)
         // one query: heads of a token side by side
         const int group = g.heads / g.kv_heads;
         p.grp = group == 1 ? 1 : group == 2 ? 2 : 4;
-        const int pairs = kTokenThreads / (dp / 8);
+        const int pairs = kThreads / (dp / 8);
         p.token.heads_per_block = std::min(g.kv_heads, pairs);
         p.token.slots = pairs / p.token.heads_per_block;
         p.token.kv_blocks = (g.kv_heads + p.token.heads_per_block - 1) / p.token.heads_per_block;
@@ -533,22 +540,22 @@ Plan forward_plan(const AttnCall &a, DType dt, bool may_split = true)
         p.blocks = 1;
         // (biases of a work-group's heads for a chunk of keys fill the LDS array)
         p.token.chunk = kTokenBias / (p.token.heads_per_block * p.grp);
-        // up to four rounds of keys in one work-group; beyond that, or where
-        // the chip has room, two rounds at least to each of several
+        // up to four rounds of keys in one work-group (40 x 483 keys: 15 us,
+        // 22 with two launches); beyond that, where the chip has room, two at
+        // least to each of several (64 x 400 keys: 12.6 + 3.6 us, 29.6 in one;
+        // 4 x 65536: 27 + 4, 3100 in one)
         const int64_t groups = int64_t(g.n) * p.token.kv_blocks * p.token.group_blocks;
         const int rounds = (g.lk() + kTokenUnroll * p.token.slots - 1) / (kTokenUnroll * p.token.slots);
         const int64_t room = 1024 / groups;
         p.splits = may_split && rounds > 4 ? int(std::max<int64_t>(1, std::min<int64_t>(room, (rounds + 1) / 2))) : 1;
         return p;
     }
-    // half work-groups where whole ones would leave half of their queries empty
-    p.waves = (lq + 63) / 64 % 2 == 1 && lq <= 320 ? 2 : 4;
-    const int queries = 32 * p.waves;
-    p.blocks = (lq + queries - 1) / queries;
+    p.blocks = (lq + kQueries - 1) / kQueries;
     const int64_t groups = int64_t(g.n) * g.heads * p.blocks;
     const int tiles = (g.lk() + tile - 1) / tile;
-    // fewer work-groups than two rounds of the chip: the keys are dealt out too,
-    // four tiles at least to each
+    // fewer work-groups than compute units: the keys are dealt out too, four
+    // tiles at least to each (one image of 40 x 40, 4 heads of 64: 23 us and 7 of
+    // joining, 58 in one piece)
     p.splits = 1;
     if (groups < 256 && may_split)
         p.splits = int(std::max<int64_t>(1, std::min<int64_t>(512 / groups, tiles / 4)));
@@ -558,7 +565,7 @@ Plan forward_plan(const AttnCall &a, DType dt, bool may_split = true)
     if (a.bias.table != nullptr) {
         const Offsets o = make_offsets(g);
         // the widest range of offsets that a tile of queries and one of keys have
-        const int span_q = std::min(queries, lq) - 1 + std::min((queries - 1) / g.wq + 1, g.hq - 1) * o.skip_q;
+        const int span_q = std::min(kQueries, lq) - 1 + std::min((kQueries - 1) / g.wq + 1, g.hq - 1) * o.skip_q;
         const int span_k = tile + ((tile - 1) / g.wk + 1) * (g.hk > 1 ? o.skip_k : 0);
         const int window = span_q + span_k + 5;
         p.cap = 1024;
@@ -577,15 +584,10 @@ hipError_t forward_launch(const Forward &f, const Plan &p, hipStream_t s)
     const AttnGeom &g = f.a.g;
     const unsigned grid = xcd_grid(int64_t(g.n) * g.heads * p.splits * p.blocks);
     constexpr int kParts = sizeof(T) == 2 ? 3 : 1;
-    const bool train = f.rest != nullptr;
-    if (p.waves == 4 && train)
-        attention_forward_kernel<T, DQP, MODE, 4, kParts><<<grid, 256, p.lds, s>>>(f);
-    else if (p.waves == 4)
-        attention_forward_kernel<T, DQP, MODE, 4, 1><<<grid, 256, p.lds, s>>>(f);
-    else if (train)
-        attention_forward_kernel<T, DQP, MODE, 2, kParts><<<grid, 128, p.lds, s>>>(f);
+    if (f.rest != nullptr)
+        attention_forward_kernel<T, DQP, MODE, kParts><<<grid, kThreads, p.lds, s>>>(f);
     else
-        attention_forward_kernel<T, DQP, MODE, 2, 1><<<grid, 128, p.lds, s>>>(f);
+        attention_forward_kernel<T, DQP, MODE, 1><<<grid, kThreads, p.lds, s>>>(f);
     if (hipError_t e = hipGetLastError())
         return e;
     if (p.splits > 1) {
@@ -598,9 +600,9 @@ template <typename T, int DQP, int GRP> hipError_t token_launch(const Forward &f
     const AttnGeom &g = f.a.g;
     const unsigned grid = unsigned(int64_t(g.n) * p.token.kv_blocks * p.token.group_blocks * p.splits);
     if (f.a.bias.table != nullptr)
-        attention_token_kernel<T, DQP, GRP, true><<<grid, kTokenThreads, 0, s>>>(f, p.token);
+        attention_token_kernel<T, DQP, GRP, true><<<grid, kThreads, 0, s>>>(f, p.token);
     else
-        attention_token_kernel<T, DQP, GRP, false><<<grid, kTokenThreads, 0, s>>>(f, p.token);
+        attention_token_kernel<T, DQP, GRP, false><<<grid, kThreads, 0, s>>>(f, p.token);
     if (hipError_t e = hipGetLastError())
         return e;
     if (p.splits > 1) {
@@ -615,6 +617,8 @@ template <typename T, int DQP> hipError_t forward_mode(const Forward &f, const P
                           : p.grp == 2 ? token_launch<T, DQP, 2>(f, p, s) : token_launch<T, DQP, 4>(f, p, s);
     if (f.a.bias.table == nullptr)
         return forward_launch<T, DQP, 0>(f, p, s);
+    // (four keys of a row have biases side by side: 275 us for 16 x 40 x 40, 283
+    // key by key; 302 and 322 for 2 x 80 x 80 with 128 reals a head)
     if (f.a.g.hk == 1 || f.a.g.wk % 4 == 0)
         return forward_launch<T, DQP, 1>(f, p, s);
     return forward_launch<T, DQP, 2>(f, p, s);

@@ -109,8 +109,11 @@ __device__ __forceinline__ void store_part(float *dst, const f32x16 (&v)[DP / 32
 }
 
 // The launch of the queries' side.  Sums of dS by offset are gathered over the
-// segment whose biases are staged; as the walk leaves it they go, over the
-// waves, to the work-group's own row of `offsets`.
+// segment whose biases are staged; as the walk leaves it they go to the
+// work-group's own row of `offsets`.  Bound by the instructions to LDS, an
+// addition and a quarter of a bias per pair above all: 16 images of 40 x 40, 8
+// heads of 64 reals, 340 us, 370 TFLOP/s of its three products (190 without a
+// bias); 32 of 14 x 14, 16 heads, 65 us (a tile of 64 keys in four has 4).
 template <typename T, int DQP, int MODE>
 __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kernel(Backward f)
 {
@@ -376,7 +379,9 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
     }
 }
 
-// The launch of the keys' side: lanes hold keys, registers queries.
+// The launch of the keys' side: lanes hold keys, registers queries.  Bound as the
+// forward pass is: 16 images of 40 x 40, 8 heads of 64 reals, 325 us, 520 TFLOP/s
+// of its four products; 32 of 14 x 14, 16 heads, 47 us.
 constexpr int kNoSegment = -(1 << 30);
 // A value of each row of a tile, as accumulators have them.
 __device__ __forceinline__ f32x16 row_values(const float *values, int first, int sub)
@@ -583,22 +588,28 @@ template <typename T, int DQP> __global__ void __launch_bounds__(256) gradient_j
     }
 }
 
-// Sum over images slice, slice + slices, .. and their work-groups of what offset
-// `a` has in them, in a fixed order.
-__device__ __forceinline__ double offset_sum(const Backward &f, int head, int a, int slice, int slices, int last_k)
+// Sum over images slice, slice + slices, .., blocks b0, b0 + step, .. and their
+// work-groups of what offset `a` has in them, in a fixed order.
+__device__ __forceinline__ double offset_sum(const Backward &f, int head, int a, int slice, int slices, int b0, int step,
+                                             int last_k)
 {
     const AttnGeom &g = f.a.g;
     const int lq = g.lq();
     const int64_t image = int64_t(g.heads) * f.blocks * f.q_splits * f.range;
     double s = 0.0;
-    for (int b = 0; b < f.blocks; ++b) {
+    for (int b = b0; b < f.blocks; b += step) {
         const int low = f.o.origin - place_q(f.o, min((b + 1) * kQueries, lq) - 1);
         const int past = f.o.origin - place_q(f.o, b * kQueries) + last_k + 1;
         if (a < low || a >= past)
             continue;
-        for (int sp = 0; sp < f.q_splits; ++sp) {
-            const float *p = f.offsets + ((int64_t(head) * f.blocks + b) * f.q_splits + sp) * f.range + (a - low);
-#pragma unroll 4
+        const float *p = f.offsets + (int64_t(head) * f.blocks + b) * f.q_splits * f.range + (a - low);
+        if (f.q_splits > 1) {  // (few images then)
+            for (int img = slice; img < g.n; img += slices)
+#pragma unroll 8
+                for (int sp = 0; sp < f.q_splits; ++sp)
+                    s += double(p[img * image + int64_t(sp) * f.range]);
+        } else {
+#pragma unroll 8
             for (int img = slice; img < g.n; img += slices)
                 s += double(p[img * image]);
         }
@@ -607,14 +618,31 @@ __device__ __forceinline__ double offset_sum(const Backward &f, int head, int a,
 }
 
 // Sums by offset of each slice of the images, in fp64: out [slices][heads][total].
-__global__ void __launch_bounds__(256) offset_sums_kernel(Backward f, int slices, double *__restrict__ out)
+// A lane per offset, the blocks and, where they are few, the images shared out
+// among the waves: what bounds it are the chains of loads (one image of 1600
+// queries, 4 heads: 9 us; 22 where a wave takes all of its offsets' blocks).
+constexpr int kSumWaves = 4;
+__global__ void __launch_bounds__(64 * kSumWaves) offset_sums_kernel(Backward f, int slices, double *__restrict__ out)
 {
-    const int a = blockIdx.x * 256 + threadIdx.x, head = blockIdx.y;
-    if (a >= f.o.total)
-        return;
+    __shared__ double parts[kSumWaves][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int a = blockIdx.x * 64 + lane, head = blockIdx.y;
     const int last_k = place_k(f.o, f.a.g.lk() - 1);
-    for (int slice = blockIdx.z; slice < slices; slice += gridDim.z)
-        out[(int64_t(slice) * f.a.g.heads + head) * f.o.total + a] = offset_sum(f, head, a, slice, slices, last_k);
+    const int step = f.blocks >= 4 ? 4 : f.blocks >= 2 ? 2 : 1;
+    static_assert(kSumWaves % 4 == 0, "waves share blocks and images evenly");
+    for (int slice = blockIdx.z; slice < slices; slice += gridDim.z) {
+        parts[wave][lane] = a < f.o.total ? offset_sum(f, head, a, slice + slices * (wave / step), slices * (kSumWaves / step),
+                                                       wave % step, step, last_k)
+                                          : 0.0;
+        __syncthreads();
+        if (wave == 0 && a < f.o.total) {
+            double s = 0.0;
+            for (int w = 0; w < kSumWaves; ++w)
+                s += parts[w][lane];
+            out[(int64_t(slice) * f.a.g.heads + head) * f.o.total + a] = s;
+        }
+        __syncthreads();
+    }
 }
 
 // dtable from the sums by offset: a work-group per row of buckets (head, by),
@@ -670,7 +698,7 @@ table_gradient_kernel(Backward f, int rows, int slices, const double *__restrict
                     for (int c = 0; c < kCols; ++c) {
                         const int x = x0 + 64 * c + lane, a = (y0 + taken[r]) * o.pitch + x;
                         if (x < o.pitch)
-                            s[c] += DIRECT ? offset_sum(f, head, a, sl, slices, last_k)
+                            s[c] += DIRECT ? offset_sum(f, head, a, sl, slices, 0, 1, last_k)
                                            : sums[(int64_t(sl) * heads + head) * o.total + a];
                     }
                 }
@@ -729,7 +757,9 @@ size_t round_up(size_t bytes)
 }
 
 // Work-groups that share a walk of `tiles` where there are only `groups` walks
-// for 256 compute units: two rounds of the chip, four tiles at least to each.
+// for 256 compute units: two rounds of the chip, four tiles at least to each (one
+// image of 40 x 40, 4 heads of 64 reals: 32 and 24 us and 6 of joining, 89 and 65
+// with a work-group to a walk).
 int share(int64_t groups, int tiles)
 {
     return groups >= 256 ? 1 : int(std::max<int64_t>(1, std::min<int64_t>(512 / groups, tiles / 4)));
@@ -781,11 +811,12 @@ Plan backward_plan(const AttnCall &a, DType dt, const AttnGradients &gr)
         if (table) {
             p.range = block_q + host_place(lk - 1, g.wk, o.skip_k) + 1;
             p.offset_bytes = round_up(size_t(std::max<int64_t>(q_groups, q_walk >= 8 ? 512 : 0)) * p.range * sizeof(float));
-            // few sums are taken to their buckets directly; images whose queries
+            // few sums are taken to their buckets directly (2 images of 16 x 16, 2
+            // heads: 6.5 us, 4.7 + 4.5 in two launches); images whose queries
             // have places of their own have slices of their own
             p.direct = int64_t(g.n) * p.blocks * p.q_splits <= 16;
             p.slices = a.pos != nullptr ? g.n : p.direct ? 1
-                     : std::min(g.n, std::max(1, 1024 / std::max(1, (o.total + 255) / 256 * g.heads)));
+                     : std::min(g.n, std::max(1, 2048 / std::max(1, (o.total + 63) / 64 * g.heads)));
             p.sum_bytes = round_up(size_t(p.slices) * g.heads * o.total * sizeof(double));
         }
     }
@@ -821,6 +852,8 @@ template <typename T, int DQP> hipError_t launch_mode(const Backward &f, const P
     if (f.a.bias.table == nullptr)
         return launch<T, DQP, 0, 0>(f, p, s);
     const bool k4 = g.hk == 1 || g.wk % 4 == 0, q4 = g.hq == 1 || g.wq % 4 == 0;
+    // (four pixels of a row have biases and sums side by side: 341 and 328 us for
+    // 16 x 40 x 40, 426 and 343 pixel by pixel)
     if (k4 && q4)
         return launch<T, DQP, 1, 1>(f, p, s);
     return launch<T, DQP, 2, 2>(f, p, s);
@@ -908,7 +941,8 @@ hipError_t attention_backward_run(const AttnCall &a, DType dt, const AttnGradien
         table_gradient_kernel<true><<<groups, kTableThreads, 0, s>>>(f, rows, p.slices, nullptr, gr.dtable);
         return hipGetLastError();
     }
-    offset_sums_kernel<<<dim3((f.o.total + 255) / 256, g.heads, std::min(p.slices, 65535)), 256, 0, s>>>(f, p.slices, sums);
+    offset_sums_kernel<<<dim3((f.o.total + 63) / 64, g.heads, std::min(p.slices, 65535)), 64 * kSumWaves, 0, s>>>(
+        f, p.slices, sums);
     if (hipError_t e = hipGetLastError())
         return e;
     table_gradient_kernel<false><<<groups, kTableThreads, 0, s>>>(f, rows, p.slices, sums, gr.dtable);

@@ -210,9 +210,10 @@ struct Lane {
 
 // ------------------------------------------------------------------- forward
 
-// Bound by HBM: two maps read and two written, 8 bytes per real in bf16.  The
+// Bound by HBM: two maps read and two written, 8 bytes per real in bf16 (64 x 56
+// x 56, 64 channels: 411 MB in 93 us, 4.4 TB/s where a large copy has 5.3).  The
 // work-groups walk over the rows side by side, so that at any time few DRAM
-// pages are in use, and what they write goes past the caches.
+// pages are in use, and what they write goes past the caches (116 us before).
 template <typename T, bool BLOCK, bool HAS_Y, bool HAS_H>
 __global__ void __launch_bounds__(BLOCK ? kBlockThreads : kThreads)
 residual_forward_kernel(int64_t rows, FastDiv by_hw, int reals, int lpr, bool whole, ResidualForward a, Drop drop,
@@ -295,7 +296,8 @@ struct Deal {
 //   dx = G,  u = G m scale gate gamma,  dy = (u - yhat mean(u yhat)) / rms(y),
 //   Q[image] = sum over rows of G m yhat,  N = sum over rows of dh out / rms(out);
 // Q carries the gradients of gate, scale and gamma, N that of next_gamma.
-// Bound by HBM: four maps read and two written, 12 bytes per real in bf16.
+// Bound by HBM: four maps read and two written, 12 bytes per real in bf16 (64 x
+// 56 x 56, 64 channels: 617 MB in 134 us, 4.6 TB/s, and 10 us for the sums).
 template <typename T, bool BLOCK, bool HAS_Y, bool HAS_H>
 __global__ void __launch_bounds__(BLOCK ? kBlockThreads : kThreads)
 residual_backward_kernel(Deal deal, int reals, int lpr, bool whole, ResidualBackward a, Drop drop, float eps,
@@ -481,8 +483,8 @@ param_gradient_kernel(const S *__restrict__ sums, int64_t entries, int reals, Re
 
 // ------------------------------------------------------------------- dropout
 
-// Bound by HBM where the mask is cheap enough: one product of 32 x 32 bits per
-// 4/7 of a real (14 per chunk of 8).
+// Bound by HBM, the mask being cheap enough: 14 products of 32 x 32 bits per
+// chunk of 8 reals (128 x 32 x 32, 16 channels: 34 MB in 6.9 us, 4.9 TB/s).
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 dropout_kernel(int64_t rows, int reals, int lpr, bool whole, const T *__restrict__ x, T *__restrict__ out, Drop drop)
