@@ -620,8 +620,9 @@ QUAN_API int quan_relpos_buckets(int32_t radius, int32_t buckets, int32_t *map);
  *
  * rest and stats are what quan_attention_backward takes.  With a bias, maps of
  * more than one row may be 1792 pixels wide.  out may overlap no input; it may
- * be a slice of a map that holds inputs in other channels.  Probabilities are
- * rounded to dtype before they meet v; everything else is fp32.  Calls with
+ * be a slice of a map that holds inputs in other channels.  Probabilities of
+ * bf16 maps are rounded to bf16 before they meet v (with rest they are split in
+ * three such numbers, so that their 24 bits count); everything else is fp32.  Calls with
  * few queries split the keys over work-groups where a workspace can be had
  * (at most 64 MiB); a captured call that cannot have it sums them in one piece,
  * and so may differ in rounding.
