@@ -553,12 +553,12 @@ Plan forward_plan(const AttnCall &a, DType dt, bool may_split = true)
     p.blocks = (lq + kQueries - 1) / kQueries;
     const int64_t groups = int64_t(g.n) * g.heads * p.blocks;
     const int tiles = (g.lk() + tile - 1) / tile;
-    // fewer work-groups than compute units: the keys are dealt out too, four
-    // tiles at least to each (one image of 40 x 40, 4 heads of 64: 23 us and 7 of
-    // joining, 58 in one piece)
+    // fewer work-groups than compute units: the keys are dealt out too, two tiles
+    // at least to each (one image of 40 x 40, 4 heads of 64: 20 us and 7 of joining,
+    // 58 in one piece; 2 of 20 x 20: 12.5 and 4.5, 22 in one)
     p.splits = 1;
     if (groups < 256 && may_split)
-        p.splits = int(std::max<int64_t>(1, std::min<int64_t>(512 / groups, tiles / 4)));
+        p.splits = int(std::max<int64_t>(1, std::min<int64_t>(512 / groups, tiles / 2)));
     p.tiles_per_split = (tiles + p.splits - 1) / p.splits;
     p.splits = (tiles + p.tiles_per_split - 1) / p.tiles_per_split;
     p.cap = 0;

@@ -757,12 +757,14 @@ size_t round_up(size_t bytes)
 }
 
 // Work-groups that share a walk of `tiles` where there are only `groups` walks
-// for 256 compute units: two rounds of the chip, four tiles at least to each (one
-// image of 40 x 40, 4 heads of 64 reals: 32 and 24 us and 6 of joining, 89 and 65
-// with a work-group to a walk).
+// for 256 compute units: two rounds of the chip, two tiles at least to each (one
+// image of 40 x 40, 4 heads of 64 reals: 28 and 21 us and 9 of joining, 89 and 65
+// with a work-group to a walk; 32, 24 and 7 with four tiles at least, and 2 of 20 x
+// 20 then 30 and 23 where they take 21, 15 and 5).
+constexpr int kLeastTiles = 2;
 int share(int64_t groups, int tiles)
 {
-    return groups >= 256 ? 1 : int(std::max<int64_t>(1, std::min<int64_t>(512 / groups, tiles / 4)));
+    return groups >= 256 ? 1 : int(std::max<int64_t>(1, std::min<int64_t>(512 / groups, tiles / kLeastTiles)));
 }
 
 Plan backward_plan(const AttnCall &a, DType dt, const AttnGradients &gr)
@@ -788,9 +790,10 @@ Plan backward_plan(const AttnCall &a, DType dt, const AttnGradients &gr)
     p.k_tiles = (k_walk + p.k_splits - 1) / p.k_splits;
     p.k_splits = (k_walk + p.k_tiles - 1) / p.k_tiles;
     // (room for what smaller batches share: at most 512 work-groups)
-    if (q_walk >= 8)
+    const bool q_shared = q_walk >= 2 * kLeastTiles, k_shared = k_walk >= 2 * kLeastTiles;
+    if (q_shared)
         p.part_q = round_up(size_t(512) * kQueries * dp * sizeof(float));
-    if (k_walk >= 8)
+    if (k_shared)
         p.part_k = round_up(size_t(512) * kQueries * dp * sizeof(float));
     p.slices = 1;
     p.delta_bytes = round_up(size_t(g.n) * g.heads * lq * sizeof(float));
@@ -810,9 +813,10 @@ Plan backward_plan(const AttnCall &a, DType dt, const AttnGradients &gr)
         p.k_cap = cap(block_k + span(tile, g.wq, g.hq, o.skip_q) + 8);
         if (table) {
             p.range = block_q + host_place(lk - 1, g.wk, o.skip_k) + 1;
-            p.offset_bytes = round_up(size_t(std::max<int64_t>(q_groups, q_walk >= 8 ? 512 : 0)) * p.range * sizeof(float));
+            p.offset_bytes = round_up(size_t(std::max<int64_t>(q_groups, q_shared ? 512 : 0)) * p.range * sizeof(float));
             // few sums are taken to their buckets directly (2 images of 16 x 16, 2
-            // heads: 6.5 us, 4.7 + 4.5 in two launches); images whose queries
+            // heads: 6.5 us from four, 10.7 from sixteen, 4.7 + 4.5 and a launch's
+            // distance in two); images whose queries
             // have places of their own have slices of their own
             p.direct = int64_t(g.n) * p.blocks * p.q_splits <= 16;
             p.slices = a.pos != nullptr ? g.n : p.direct ? 1
