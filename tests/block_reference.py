@@ -6,7 +6,7 @@ probabilities P (before they meet v or dout), dS (before k or q) and every
 stored result; sums are fp32.  So, with B_i = sum_j P_ij |v_j|,
 
   |out error|   <= u (|out| + B)                     (inference)
-                   u |out| + u^2 B                   (a training step: P in two parts)
+                   u |out| + u^2 B                   (a training step: P in parts)
   |delta error| <= eps_i = u^2 sum |dout| B          (rows' sums of dout out)
   |dv error|    <= u (|dv| + P^T |dout|)
   |dq error|    <= u (|dq| + scale |dS| |k|) + scale P eps |k|, dk likewise
