@@ -285,8 +285,13 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
             const int lo = low_q + place_k(f.o, j0), hi = high_q + place_k(f.o, min(j0 + KT, lk) - 1) + 3;
             if (hi >= segment + f.o.cap) {
                 __syncthreads();  // the last segment has been read and added to
-                if (offsets != nullptr)
+                if (offsets != nullptr) {
                     flush();
+                    if (lo > done) {  // (a row of keys ended: offsets that the block has to none)
+                        clear(done, lo);
+                        done = lo;
+                    }
+                }
                 __syncthreads();
                 start_segment(lo);
             }
