@@ -175,10 +175,11 @@ __device__ __forceinline__ void row_sums(float (&s)[N], int lpr, float *lds)
     }
 }
 
-// 1 / sqrt(x) of x > 0.
+// 1 / sqrt(x) of x > 0 (of the smallest normal number for smaller ones, which the
+// instruction takes as 0); NaN stays NaN (fmaxf would take the number).
 __device__ __forceinline__ float inv_sqrt(float x)
 {
-    return __builtin_amdgcn_rsqf(fmaxf(x, 1.17549435e-38f));
+    return __builtin_amdgcn_rsqf(x < 1.17549435e-38f ? 1.17549435e-38f : x);
 }
 
 // The three sums of a gradient's row, those of absent parts left out.
