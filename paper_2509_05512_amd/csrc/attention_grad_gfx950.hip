@@ -37,9 +37,10 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves, kQueries = 32 * kWaves;
 // Sums of dS by offset in 64-bit fixed point: integer additions in LDS take 7
 // clocks a wave where those of floats take 194 (measured), and their order
 // changes nothing, so that the waves share one array.  Its units 2^-k follow
-// from a bound of the terms known before they are: |dS| <= |dP - delta| <=
-// |dO| |v| + |delta|, with the work-group's largest |dO| and |delta| and the
-// tile's largest element of v.  k = kSumBits - e for a bound below 2^e: an
+// from a bound of the terms known before they are: |dS| <= |dP - delta| <= (sum of
+// |dO|'s elements) max |v| + |delta|, with the largest such sum and |delta| of the
+// work-group's rows and the tile's largest element of v (no squares: they leave
+// fp32 long before dO does).  k = kSumBits - e for a bound below 2^e: an
 // offset's terms (one per query, 128) stay below 2^50, and a term's last place
 // is 2^-42 of the bound.  A tile with a larger bound takes the array to coarser
 // units.  What NaN or infinity is in the work-group's rows or in v gives NaN.
@@ -209,19 +210,19 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
     };
     if (MODE != 0 && begin < end)
         start_segment(low_q + place_k(f.o, begin));
-    // the bound's parts from the work-group's rows: |dO| and |delta|; a row whose
-    // sum is no number has NaN
+    // the bound's parts from the work-group's rows: the sum of |dO| and |delta|; a
+    // row whose sum of probabilities is no number has NaN
     float top_go = 0.0f, top_delta = 0.0f;
     if (MODE != 0 && offsets != nullptr) {
-        float n2 = 0.0f;
+        float n1 = 0.0f;
 #pragma unroll
         for (int i = 0; i < DP / 16; ++i) {
             const f32x8 w = to_f32(go[i]);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                n2 = fmaf(w[e], w[e], n2);
+                n1 += fabsf(w[e]);
         }
-        top_go = wave_top(sum <= -kLowest ? sqrtf(half_sum(n2)) : NAN);
+        top_go = wave_top(sum <= -kLowest ? half_sum(n1) : NAN);
         top_delta = wave_top(delta);
         if (lane == 0) {
             tops[wave] = top_go;
@@ -233,7 +234,6 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
             top_go = bits_max(top_go, tops[w]);
             top_delta = bits_max(top_delta, tops[kWaves + w]);
         }
-        top_go *= sqrtf(float(DP));
         __syncthreads();
     }
     int units = kNoUnits;  // k of the array's units 2^-k
