@@ -94,8 +94,8 @@ __global__ void __launch_bounds__(kThreads, 2) attention_forward_kernel(Forward 
     const float *table = nullptr;
     if (MODE != 0) {
         if (f.a.pos != nullptr) {
-            pos_y = f.a.pos[2 * img];
-            pos_x = f.a.pos[2 * img + 1];
+            pos_y = query_pos(f.a.pos[2 * img]);
+            pos_x = query_pos(f.a.pos[2 * img + 1]);
         }
         table = f.a.bias.table + int64_t(head) * f.a.bias.ny * f.a.bias.nx;
         low_q = f.o.origin - place_q(f.o, min(q0 + kQueries, lq) - 1);
@@ -386,8 +386,8 @@ __global__ void __launch_bounds__(kThreads) attention_token_kernel(Forward f, To
     const int valid = active ? km.valid(d, 8) : 0;
     int pos_y = 0, pos_x = 0;
     if (BIAS && f.a.pos != nullptr) {
-        pos_y = f.a.pos[2 * img];
-        pos_x = f.a.pos[2 * img + 1];
+        pos_y = query_pos(f.a.pos[2 * img]);
+        pos_x = query_pos(f.a.pos[2 * img + 1]);
     }
     const int nb = f.a.bias.ny * f.a.bias.nx;
     const int chunk = BIAS ? tk.chunk : max(end - first, 1);

@@ -188,8 +188,8 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
     float *offsets = nullptr;
     if (MODE != 0) {
         if (f.a.pos != nullptr) {
-            pos_y = f.a.pos[2 * img];
-            pos_x = f.a.pos[2 * img + 1];
+            pos_y = query_pos(f.a.pos[2 * img]);
+            pos_x = query_pos(f.a.pos[2 * img + 1]);
         }
         table = f.a.bias.table + int64_t(head) * f.a.bias.ny * f.a.bias.nx;
         low_q = f.o.origin - place_q(f.o, min(q0 + kQueries, lq) - 1);
@@ -449,8 +449,8 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) attention_dkv_ker
     int pos_y = 0, pos_x = 0, lane_at = 0, low_k = 0, high_k = 0;
     if (MODE != 0) {
         if (f.a.pos != nullptr) {
-            pos_y = f.a.pos[2 * img];
-            pos_x = f.a.pos[2 * img + 1];
+            pos_y = query_pos(f.a.pos[2 * img]);
+            pos_x = query_pos(f.a.pos[2 * img + 1]);
         }
         low_k = f.o.origin + place_k(f.o, k0);
         high_k = f.o.origin + place_k(f.o, min(k0 + kQueries, lk) - 1);
@@ -676,7 +676,8 @@ table_gradient_kernel(Backward f, int rows, int slices, const double *__restrict
         tot[x] = 0.0;
     const int groups = pos != nullptr ? slices : 1, per = slices / groups;
     for (int group = 0; group < groups; ++group) {
-        const int pos_y = pos != nullptr ? pos[2 * group] : 0, pos_x = pos != nullptr ? pos[2 * group + 1] : 0;
+        const int pos_y = pos != nullptr ? query_pos(pos[2 * group]) : 0;
+        const int pos_x = pos != nullptr ? query_pos(pos[2 * group + 1]) : 0;
         for (int x0 = 0; x0 < o.pitch; x0 += kTableCols) {
             double s[kCols] = {};
             for (int y0 = 0; y0 < rows; y0 += kTableThreads) {
