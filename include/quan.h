@@ -619,7 +619,16 @@ QUAN_API int quan_relpos_buckets(int32_t radius, int32_t buckets, int32_t *map);
  *              key) and the sum of 2^(score - maximum).
  *
  * rest and stats are what quan_attention_backward takes.  With a bias, maps of
- * more than one row may be 1792 pixels wide.  out may overlap no input; it may
+ * more than one row may be 1792 pixels wide, and unless queries and keys are
+ * maps of one width (or there is one query, in this call), the offsets between
+ * a block of 128 pixels of one and a tile of 64 (fp32: 32) of the other have to
+ * fit in a work-group's 160 KiB, at 4 bytes each (12 in the queries' part of the
+ * backward pass with dtable) beside 16 to 66 KiB of tiles.  About (128 / width)
+ * * (width of the other map) of them belong to a block: queries of 8 x 8 on
+ * keys 512 wide fit everywhere, queries of 16 x 4 on keys 1024 wide have no
+ * backward pass with dtable.  What does not fit returns QUAN_ERR_UNSUPPORTED
+ * before anything is launched, a call with stats also where its backward pass
+ * would not fit without dtable.  out may overlap no input; it may
  * be a slice of a map that holds inputs in other channels.  Probabilities of
  * bf16 maps are rounded to bf16 before they meet v (with rest they are split in
  * three such numbers, so that their 24 bits count); everything else is fp32.  Calls with

@@ -561,20 +561,18 @@ Plan forward_plan(const AttnCall &a, DType dt, bool may_split = true)
         p.splits = int(std::max<int64_t>(1, std::min<int64_t>(512 / groups, tiles / 2)));
     p.tiles_per_split = (tiles + p.splits - 1) / p.splits;
     p.splits = (tiles + p.tiles_per_split - 1) / p.tiles_per_split;
+    const size_t tiles_bytes = size_t(4) * tile * (dp + (es == 2 ? 0 : 4)) * es + size_t(2) * tile * 4;
     p.cap = 0;
     if (a.bias.table != nullptr) {
         const Offsets o = make_offsets(g);
         // the widest range of offsets that a tile of queries and one of keys have
-        const int span_q = std::min(kQueries, lq) - 1 + std::min((kQueries - 1) / g.wq + 1, g.hq - 1) * o.skip_q;
-        const int span_k = tile + ((tile - 1) / g.wk + 1) * (g.hk > 1 ? o.skip_k : 0);
-        const int window = span_q + span_k + 5;
-        p.cap = 1024;
-        while (p.cap < window)
-            p.cap *= 2;
+        const int window = place_span(std::min(kQueries, lq), g.wq, g.hq, o.skip_q) +
+                           place_span(tile, g.wk, g.hk, o.skip_k) + 8;
+        p.cap = segment_cap(window, tiles_bytes, 4);
         if (p.cap < o.total && p.cap < 2048)
             p.cap = 2048;
     }
-    p.lds = size_t(4) * tile * (dp + (es == 2 ? 0 : 4)) * es + size_t(2) * tile * 4 + size_t(p.cap) * 4;
+    p.lds = tiles_bytes + size_t(p.cap) * 4;
     return p;
 }
 
@@ -709,6 +707,11 @@ size_t attention_forward_extra_bytes(const AttnCall &a, DType dt)
         return 0;
     const size_t rows = size_t(a.g.n) * a.g.heads * a.g.lq();
     return size_t(p.splits) * rows * (4 * padded_dq(a.g.dq) + 2) * sizeof(float);
+}
+
+bool attention_forward_fits(const AttnCall &a, DType dt)
+{
+    return forward_plan(a, dt).lds <= kLdsLimit;
 }
 
 hipError_t attention_forward_run(const AttnCall &a, DType dt, const AttnMap &out, void *rest, float *stats, void *work,

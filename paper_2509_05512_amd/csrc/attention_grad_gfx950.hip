@@ -801,22 +801,18 @@ Plan backward_plan(const AttnCall &a, DType dt, const AttnGradients &gr)
         p.part_q = round_up(size_t(512) * kQueries * dp * sizeof(float));
     if (k_shared)
         p.part_k = round_up(size_t(512) * kQueries * dp * sizeof(float));
+    p.q_lds = size_t(4) * tile * (dp + (es == 2 ? 0 : 4)) * es + size_t(2) * tile * 4;
+    p.k_lds = p.q_lds + size_t(6) * tile * 4;
+    const int q_entry = table ? 12 : 4;  // bytes: a bias, and a sum
     p.slices = 1;
     p.delta_bytes = round_up(size_t(g.n) * g.heads * lq * sizeof(float));
     if (a.bias.table != nullptr) {
         const Offsets o = make_offsets(g);
-        auto span = [](int count, int w, int h, int skip) { return count + std::min((count - 1) / w + 1, h - 1) * skip; };
         // a segment holds the widest tile's offsets
-        auto cap = [&](int window) {
-            int c = 1024;
-            while (c < window)
-                c *= 2;
-            return c;
-        };
-        const int block_q = span(std::min(kQueries, lq), g.wq, g.hq, o.skip_q);
-        const int block_k = span(std::min(kQueries, lk), g.wk, g.hk, o.skip_k);
-        p.q_cap = cap(block_q + span(tile, g.wk, g.hk, o.skip_k) + 8);
-        p.k_cap = cap(block_k + span(tile, g.wq, g.hq, o.skip_q) + 8);
+        const int block_q = place_span(std::min(kQueries, lq), g.wq, g.hq, o.skip_q);
+        const int block_k = place_span(std::min(kQueries, lk), g.wk, g.hk, o.skip_k);
+        p.q_cap = segment_cap(block_q + place_span(tile, g.wk, g.hk, o.skip_k) + 8, p.q_lds, q_entry);
+        p.k_cap = segment_cap(block_k + place_span(tile, g.wq, g.hq, o.skip_q) + 8, p.k_lds, 4);
         if (table) {
             p.range = block_q + host_place(lk - 1, g.wk, o.skip_k) + 1;
             p.offset_bytes = round_up(size_t(std::max<int64_t>(q_groups, q_shared ? 512 : 0)) * p.range * sizeof(float));
@@ -830,9 +826,8 @@ Plan backward_plan(const AttnCall &a, DType dt, const AttnGradients &gr)
             p.sum_bytes = round_up(size_t(p.slices) * g.heads * o.total * sizeof(double));
         }
     }
-    const size_t tiles = size_t(4) * tile * (dp + (es == 2 ? 0 : 4)) * es + size_t(2) * tile * 4;
-    p.q_lds = tiles + size_t(p.q_cap) * 4 * (table ? 3 : 1);
-    p.k_lds = tiles + size_t(6) * tile * 4 + size_t(p.k_cap) * 4;
+    p.q_lds += size_t(p.q_cap) * q_entry;
+    p.k_lds += size_t(p.k_cap) * 4;
     return p;
 }
 
@@ -881,6 +876,12 @@ template <typename T> hipError_t launch_dq(const Backward &f, const Plan &p, hip
 }
 
 }  // namespace
+
+bool attention_backward_fits(const AttnCall &a, DType dt, const AttnGradients &gr)
+{
+    const Plan p = backward_plan(a, dt, gr);
+    return std::max(p.q_lds, p.k_lds) <= kLdsLimit;
+}
 
 size_t attention_backward_work_bytes(const AttnCall &a, DType dt, const AttnGradients &gr)
 {

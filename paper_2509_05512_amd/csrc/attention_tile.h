@@ -20,6 +20,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "gfx950_dma.h"
 #include "quan_block.h"
 
@@ -383,6 +385,23 @@ struct Offsets {
     int skip_q, skip_k;  // pitch - wq, pitch - wk
     int cap;             // entries of a segment
 };
+// Tokens side by side, from any one on: the range of their places.
+inline int place_span(int count, int w, int h, int skip)
+{
+    return count + std::min((count - 1) / w + 1, h - 1) * skip;
+}
+// What a work-group may have of a compute unit's 160 KiB, static arrays aside.
+constexpr size_t kLdsLimit = 160 * 1024 - 512;
+// Entries of a segment that holds a tile's `window` of offsets at `bytes` each
+// beside `fixed` bytes of LDS: a power of two, or where that does not fit the
+// window alone (which may not fit either).
+inline int segment_cap(int window, size_t fixed, int bytes)
+{
+    int c = 1024;
+    while (c < window)
+        c *= 2;
+    return fixed + size_t(c) * bytes <= kLdsLimit ? c : (window + 3) / 4 * 4;
+}
 inline Offsets make_offsets(const AttnGeom &g)
 {
     Offsets o;

@@ -90,7 +90,7 @@ struct AttnGeom {
     constexpr int lk() const { return hk * wk; }
 };
 constexpr int kAttnMaxDq = 32;       // quaternion channels of a head
-constexpr int kAttnMaxWidth = 1792;  // of maps with more than one row: a tile's offsets fit in LDS
+constexpr int kAttnMaxWidth = 1792;  // of maps with more than one row, with a bias
 constexpr int kAttnMaxBuckets = 1024;  // per axis
 struct AttnCall {
     AttnGeom g;
@@ -116,6 +116,9 @@ hipError_t attention_pack_run(const AttnPack &p, int n, int dq, DType dt, hipStr
 // stats [n][heads][lq][2]: the row's maximum in units of log 2 and the sum of
 // 2^(score - maximum).  `work` holds the copies that the call needs, `extra`
 // (or NULL) partial results of a call with few queries.
+// _fits: whether a tile's offsets fit in LDS (without a bias, and for maps as
+// wide as each other, always).
+bool attention_forward_fits(const AttnCall &a, DType dt);
 size_t attention_forward_work_bytes(const AttnCall &a, DType dt);
 size_t attention_forward_extra_bytes(const AttnCall &a, DType dt);
 hipError_t attention_forward_run(const AttnCall &a, DType dt, const AttnMap &out, void *rest, float *stats, void *work,
@@ -127,6 +130,7 @@ struct AttnGradients {
     const float *stats;
     float *dtable;
 };
+bool attention_backward_fits(const AttnCall &a, DType dt, const AttnGradients &g);
 size_t attention_backward_work_bytes(const AttnCall &a, DType dt, const AttnGradients &g);
 hipError_t attention_backward_run(const AttnCall &a, DType dt, const AttnGradients &g, void *work, hipStream_t stream);
 

@@ -298,6 +298,17 @@ int check_call(const char *fn, const quan_tensor *q, const quan_tensor *k, const
     return QUAN_OK;
 }
 
+// A tile's offsets have to fit in LDS: narrow maps against wide ones have many.
+int check_offsets(const char *fn, bool fits, const char *of)
+{
+    if (!fits)
+        return report(QUAN_ERR_UNSUPPORTED,
+                      "%s: the offsets between 128 pixels of one map and a tile of the other do not fit in a "
+                      "work-group's memory%s",
+                      fn, of);
+    return QUAN_OK;
+}
+
 struct ForwardCall {
     quan::AttnCall a;
     quan::DType dt;
@@ -380,6 +391,12 @@ QUAN_API int quan_attention_forward(const quan_tensor *q, const quan_tensor *k, 
         return report(QUAN_ERR_ALIGN, "%s: rest must be 16-byte aligned", fn);
     if (misaligned(stats, 4))
         return report(QUAN_ERR_ALIGN, "%s: stats must be 4-byte aligned", fn);
+    c.dt = to_dt(q->dtype);
+    if (int rc = check_offsets(fn, quan::attention_forward_fits(c.a, c.dt), ""))
+        return rc;
+    if (stats != nullptr)
+        if (int rc = check_offsets(fn, quan::attention_backward_fits(c.a, c.dt, {}), " (of its backward pass)"))
+            return rc;
     const Span rest_span{"rest", rest, dense_bytes(q)};
     const Span stats_span{"stats", stats, size_t(c.a.g.n) * heads * c.a.g.lq() * 8};
     for (const Span &o : {out_span, rest_span, stats_span})
@@ -390,7 +407,6 @@ QUAN_API int quan_attention_forward(const quan_tensor *q, const quan_tensor *k, 
     if (int rc = check_alias(fn, rest_span, {stats_span}))
         return rc;
     for_heads(&c.out, c.a.g.dq);
-    c.dt = to_dt(q->dtype);
     c.rest = rest;
     c.stats = stats;
     const size_t bytes = quan::attention_forward_work_bytes(c.a, c.dt);
@@ -436,6 +452,10 @@ QUAN_API int quan_attention_backward(const quan_tensor *q, const quan_tensor *k,
     const Span rest_span{"rest", rest, dense_bytes(q)};
     const Span stats_span{"stats", stats, size_t(c.a.g.n) * heads * c.a.g.lq() * 8};
     const Span dtable_span{"dtable", dtable, s.table.bytes};
+    c.dt = to_dt(q->dtype);
+    c.g.dtable = dtable;
+    if (int rc = check_offsets(fn, quan::attention_backward_fits(c.a, c.dt, c.g), dtable != nullptr ? " (with dtable)" : ""))
+        return rc;
     for (const Span &o : {dq_span, dk_span, dv_span, dtable_span})
         if (int rc = check_alias(fn, o, {s.q, s.k, s.v, s.table, s.by, s.bx, s.kv_len, s.pos, out_span, rest_span,
                                          stats_span, dout_span}))
@@ -448,10 +468,8 @@ QUAN_API int quan_attention_backward(const quan_tensor *q, const quan_tensor *k,
         return rc;
     for (quan::AttnMap *m : {&c.g.out, &c.g.dout, &c.g.dq, &c.g.dk, &c.g.dv})
         for_heads(m, c.a.g.dq);
-    c.dt = to_dt(q->dtype);
     c.g.rest = rest;
     c.g.stats = stats;
-    c.g.dtable = dtable;
     return quan::run_on_stream(stream, quan::attention_backward_work_bytes(c.a, c.dt, c.g), 0, run_backward, &c, fn);
 }
 
