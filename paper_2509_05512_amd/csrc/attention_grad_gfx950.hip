@@ -922,10 +922,11 @@ hipError_t attention_backward_run(const AttnCall &a, DType dt, const AttnGradien
             pack.src[i] = *m;
             // (rest is dense and aligned, but its rows may not be whole chunks)
             pack.src[i].vec = m->vec && g.dq % 8 == 0;
+            pack.kv_len[i] = keys ? a.kv_len : nullptr;
             pack.heads[i] = keys ? g.kv_heads : g.heads;
             pack.tokens[i] = keys ? g.lk() : g.lq();
             pack.dst[i] = take(keys ? p.k_copy : p.q_copy);
-            *m = {pack.dst[i], pack.heads[i] * pack.tokens[i] * d, d, d / 4, true, pack.tokens[i] * d};
+            *m = {pack.dst[i], int64_t(pack.heads[i]) * pack.tokens[i] * d, d, d / 4, true, pack.tokens[i] * d};
         }
         if (hipError_t e = attention_pack_run(pack, g.n, g.dq, dt, s))
             return e;

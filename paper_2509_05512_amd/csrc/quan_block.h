@@ -101,11 +101,13 @@ struct AttnCall {
 };
 // Heads are read as 16-byte chunks of whole rows of D = 4 * padded_dq reals;
 // maps that do not lie so (unaligned slices, other dq) are copied first, head by
-// head ([n][head][token][D], zeros in the added channels).
+// head ([n][head][token][D], zeros in the added channels; of keys those that the
+// image has).
 constexpr int padded_dq(int dq) { return dq <= 8 ? 8 : dq <= 16 ? 16 : 32; }
 struct AttnPack {
     static constexpr int kMaps = 6;
     AttnMap src[kMaps];
+    const int32_t *kv_len[kMaps];  // [n], NULL: all tokens
     int heads[kMaps], tokens[kMaps];
     void *dst[kMaps];
     int maps;
