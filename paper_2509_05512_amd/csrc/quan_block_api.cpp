@@ -61,6 +61,9 @@ quan::DType to_dt(int32_t dtype)
 }
 
 constexpr int64_t kMaxPixels = (int64_t(1) << 31) - 1, kMaxImagePixels = int64_t(1) << 24;
+// Work-groups of 256 lanes (in eights) that a launch may have: a grid's axis holds
+// less than 2^32 lanes.
+constexpr int64_t kMaxLanes = (int64_t(1) << 32) - 1, kMaxGroups = kMaxLanes / 256 / 8 * 8;
 
 // ------------------------------------------------------------------ the rows
 
@@ -261,9 +264,9 @@ int check_call(const char *fn, const quan_tensor *q, const quan_tensor *k, const
     quan::AttnGeom &g = a->g;
     g = {int(q->shape[0]), heads,           int(ckv / dq),    int(dq), int(q->shape[3]),
          int(q->shape[4]), int(k->shape[3]), int(k->shape[4]), scale};
-    // work-groups of 64 queries or keys, and of one query's splits
+    // a work-group takes 128 queries of a head and image, or a part of one's keys
     const int64_t blocks = (std::max(g.lq(), g.lk()) + 63) / 64;
-    if (blocks * g.n > kMaxPixels / 2 / heads)
+    if (blocks * g.n > kMaxPixels / 2 / heads || (g.lq() + 127) / 128 * int64_t(g.n) * heads > kMaxGroups)
         return report(QUAN_ERR_UNSUPPORTED, "%s: too many work-groups", fn);
     for (quan::AttnMap *m : {&a->q, &a->k, &a->v})
         for_heads(m, g.dq);
@@ -447,6 +450,13 @@ QUAN_API int quan_attention_backward(const quan_tensor *q, const quan_tensor *k,
         return report(QUAN_ERR_DTYPE, "%s: rest is for bf16 maps", fn);
     if (misaligned(rest, 16))
         return report(QUAN_ERR_ALIGN, "%s: rest must be 16-byte aligned", fn);
+    const quan::AttnGeom &g = c.a.g;
+    if ((g.lk() + 127) / 128 * int64_t(g.n) * g.kv_heads > kMaxGroups)
+        return report(QUAN_ERR_UNSUPPORTED, "%s: too many work-groups", fn);
+    // (4 lanes per offset, 512 per row of buckets)
+    if (dtable != nullptr && (int64_t(g.hk + g.hq) * (g.wk + g.wq) > kMaxLanes / 4 - 64 ||
+                              int64_t(heads) * relpos->buckets_y > kMaxLanes / 512))
+        return report(QUAN_ERR_UNSUPPORTED, "%s: too many offsets or buckets for dtable", fn);
     if (misaligned(stats, 4) || misaligned(dtable, 4))
         return report(QUAN_ERR_ALIGN, "%s: stats and dtable must be 4-byte aligned", fn);
     const Span rest_span{"rest", rest, dense_bytes(q)};

@@ -25,9 +25,9 @@ def addr(i):
     return 0x1000000000 * (i + 1)
 
 
-def desc(i, c, hw, dtype):
+def desc(i, c, hw, dtype, n=1):
     h, w = hw
-    return quan.QuanTensor(addr(i), dtype, 5, (ctypes.c_int64 * 5)(1, 4, c, h, w),
+    return quan.QuanTensor(addr(i), dtype, 5, (ctypes.c_int64 * 5)(n, 4, c, h, w),
                            (ctypes.c_int64 * 5)(h * w * 4 * c, c, 1, w * 4 * c, 4 * c))
 
 
@@ -37,19 +37,19 @@ class QuanRelpos(ctypes.Structure):
         + [(m, ctypes.c_int32) for m in ("buckets_y", "buckets_x", "radius_y", "radius_x")]
 
 
-def call(lib, q_hw, k_hw, dq, dtype, what):
+def call(lib, q_hw, k_hw, dq, dtype, what, n=1, heads=1, buckets=4):
     """what: "forward", "save", "backward" (without dtable) or "dtable"; the
     outputs lie on q."""
-    q, k, v, out, dout = (desc(i, dq, hw, dtype) for i, hw in enumerate((q_hw, k_hw, k_hw, q_hw, q_hw)))
-    rp = QuanRelpos(addr(20), addr(21), addr(22), 4, 4, 8, 8)
+    q, k, v, out, dout = (desc(i, heads * dq, hw, dtype, n) for i, hw in enumerate((q_hw, k_hw, k_hw, q_hw, q_hw)))
+    rp = QuanRelpos(addr(20), addr(21), addr(22), buckets, 4, 8, 8)
 
     def ref(d):
         return ctypes.byref(d)
-    first = [ref(q), ref(k), ref(v), ref(rp), None, None, 0.1, 1]
+    first = [ref(q), ref(k), ref(v), ref(rp), None, None, 0.1, heads]
     if what in ("forward", "save"):
-        return lib.quan_attention_forward(*first, ref(desc(0, dq, q_hw, dtype)), None, addr(10) if what == "save" else None,
+        return lib.quan_attention_forward(*first, ref(desc(0, heads * dq, q_hw, dtype, n)), None, addr(10) if what == "save" else None,
                                           None)
-    grads = [ref(desc(0, dq, q_hw, dtype)), ref(desc(11, dq, k_hw, dtype)), ref(desc(12, dq, k_hw, dtype))]
+    grads = [ref(desc(0, heads * dq, q_hw, dtype, n)), ref(desc(11, heads * dq, k_hw, dtype, n)), ref(desc(12, heads * dq, k_hw, dtype, n))]
     return lib.quan_attention_backward(*first, ref(out), None, addr(10), ref(dout), *grads,
                                        addr(13) if what == "dtable" else None, None)
 
@@ -125,3 +125,17 @@ def test_examples(lib, q_hw, k_hw, dq, what):
     assert rc == (E_UNSUP if need(q_hw, k_hw, dq, BF, what) + 3000 > LDS else E_ALIAS), need(q_hw, k_hw, dq, BF, what)
     assert call(lib, (8, 8), (64, 512), 32, BF, "dtable") == E_ALIAS
     assert call(lib, (16, 4), (16, 1024), 16, BF, "dtable") == E_UNSUP
+
+
+# (n, heads, queries, keys, buckets): a launch's axis has less than 2^32 lanes, 256
+# to a work-group of 128 queries or keys of a head and image
+@pytest.mark.parametrize("what", WHAT)
+@pytest.mark.parametrize("n,heads,q_hw,k_hw,buckets,limited", [
+    (16777208, 1, (1, 1), (1, 1), 4, ()), (16777209, 1, (1, 1), (1, 1), 4, WHAT),
+    (2097151, 8, (1, 128), (1, 128), 4, ()), (2097151, 8, (1, 129), (1, 129), 4, WHAT),
+    (2097151, 8, (1, 1), (1, 129), 4, ("backward", "dtable")),
+    (1, 1, (1, 1), (1, 16777216), 4, ()),
+    (1, 8191, (1, 2), (1, 2), 1024, ()), (1, 8192, (1, 2), (1, 2), 1024, ("dtable",))])
+def test_launches_of_too_many_work_groups(lib, n, heads, q_hw, k_hw, buckets, limited, what):
+    rc = call(lib, q_hw, k_hw, 2, BF, what, n, heads, buckets)
+    assert rc == (E_UNSUP if what in limited else E_ALIAS), lib.quan_last_error()
