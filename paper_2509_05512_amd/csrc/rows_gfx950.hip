@@ -485,10 +485,11 @@ param_gradient_kernel(const S *__restrict__ sums, int64_t entries, int reals, Re
 // ------------------------------------------------------------------- dropout
 
 // Bound by HBM, the mask being cheap enough: 14 products of 32 x 32 bits per
-// chunk of 8 reals (128 x 32 x 32, 16 channels: 34 MB in 6.9 us, 4.9 TB/s).
+// chunk of 8 reals (128 x 32 x 32, 16 channels: 34 MB in 6.9 us, 4.9 TB/s).  out
+// may be x: a chunk is read and written by one lane, in that order.
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
-dropout_kernel(int64_t rows, int reals, int lpr, bool whole, const T *__restrict__ x, T *__restrict__ out, Drop drop)
+dropout_kernel(int64_t rows, int reals, int lpr, bool whole, const T *x, T *out, Drop drop)
 {
     const int first = threadIdx.x & (lpr - 1);
     const int per = kThreads / lpr, chunks = (reals + 7) / 8;
