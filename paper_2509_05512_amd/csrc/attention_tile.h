@@ -433,10 +433,11 @@ __device__ __forceinline__ int place_k(const Offsets &o, int t)
 
 // A coordinate of a query's place.  Maps and radii are at most 2^24, so that
 // offsets from 2^26 on are beyond any radius; closer to the ends of the type
-// their differences would wrap.
+// their differences would wrap.  (One for all lanes, and kept as that: in vector
+// registers it cost the queries' gradient two more spilled ones, 341 us for 327.)
 __device__ __forceinline__ int query_pos(int p)
 {
-    return min(max(p, -(1 << 26)), 1 << 26);
+    return __builtin_amdgcn_readfirstlane(min(max(p, -(1 << 26)), 1 << 26));
 }
 // Bucket (by * nx + bx) of offset A for an image whose queries start at (y, x).
 __device__ __forceinline__ int bucket_of(const Offsets &o, const AttnBias &b, int a, int y, int x)
