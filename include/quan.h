@@ -656,9 +656,13 @@ QUAN_API int quan_attention_forward(const quan_tensor *q, const quan_tensor *k, 
  *   dtable     fp32 [heads][buckets_y * buckets_x], or NULL.
  * Every other argument is the forward's.  Sums have a fixed order (dtable's are
  * whole numbers of 2^-42 of a bound of their terms within a block of 128
- * queries, fp64 beyond): deterministic.  Uses a
- * workspace per (device, stream), with dtable of about 4 * N * heads *
- * (Hq*Wq / 128) * (offsets of a map) bytes.
+ * queries, fp64 beyond): deterministic.  Uses a workspace per (device, stream),
+ * a quarter larger than the call asks for, that smaller batches of the same maps
+ * fit into: the maps' copies where they need any; 4 * N * heads * Hq*Wq bytes; up
+ * to 26 MB (heads of 8 channels) or 100 MB (of 32) for the parts of walks that
+ * work-groups share; and with dtable about 4 * N * heads * (Hq*Wq / 128) *
+ * (offsets of a map) bytes and 8 * heads * (offsets of a map), with pos N times
+ * that.
  */
 QUAN_API int quan_attention_backward(const quan_tensor *q, const quan_tensor *k, const quan_tensor *v,
                                      const quan_relpos *relpos, const int32_t *kv_len, const int32_t *pos,

@@ -25,10 +25,14 @@ struct Backward {
     AttnMap out, rest, dout, dq, dk, dv;  // (rest.data may be NULL)
     const float *stats;
     float *delta;    // [n][heads][lq]
-    float *offsets;  // [n * heads * blocks][q_splits][range] sums of dS by offset, NULL: none asked for
+    // sums of dS by offset, [n * heads * blocks][q_splits][range]: a work-group's
+    // entries are those between its queries and its share of the keys, from the
+    // lowest on; NULL: none asked for
+    float *offsets;
     int blocks, range;
     // work-groups that share a block of queries, of keys; the tiles of each
     int q_splits, k_splits, q_tiles, k_tiles;
+    int q_span;  // tokens of q_tiles
     float *part_q, *part_k, *part_v;  // [split][row][D] where shared
 };
 
@@ -146,7 +150,7 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
     const int q0 = block * kQueries, query = q0 + 32 * wave + (lane & 31);
     const bool q_here = query < lq;
     const int len = f.a.kv_len != nullptr ? min(max(f.a.kv_len[img], 0), lk) : lk;
-    const int begin = split * f.q_tiles * KT, end = min(len, begin + f.q_tiles * KT);
+    const int begin = split * f.q_span, end = min(len, begin + f.q_span);
     const int64_t row = (int64_t(img) * g.heads + head) * lq + query;
 
     const WholeMap<T, DQP> qm(f.a.q, img, head), km(f.a.k, img, kv_head), vm(f.a.v, img, kv_head);
@@ -195,11 +199,12 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
         low_q = f.o.origin - place_q(f.o, min(q0 + kQueries, lq) - 1);
         high_q = f.o.origin - place_q(f.o, q0);
         lane_at = f.o.origin - place_q(f.o, min(query, lq - 1));
+        done = low_q + place_k(f.o, begin);
         if (f.offsets != nullptr)
-            offsets = f.offsets + (((int64_t(img) * g.heads + head) * f.blocks + block) * f.q_splits + split) * f.range - low_q;
-        done = low_q;
+            offsets = f.offsets + (((int64_t(img) * g.heads + head) * f.blocks + block) * f.q_splits + split) * f.range - done;
     }
-    const int past = MODE != 0 ? high_q + place_k(f.o, lk - 1) + 1 : 0;  // past the last offset
+    // past the last offset to this work-group's keys
+    const int past = MODE != 0 ? high_q + place_k(f.o, min(begin + f.q_span, lk) - 1) + 1 : 0;
     auto start_segment = [&](int lo) {
         segment = lo;
         const int count = min(f.o.cap, past + 3 - segment);  // (a quad may pass the last offset)
@@ -258,11 +263,6 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
         }
         done = max(done, last);
     };
-    // (entries of the keys before this work-group's)
-    if (MODE != 0 && offsets != nullptr && begin > 0) {
-        done = begin < end ? low_q + place_k(f.o, begin) : past;
-        clear(low_q, done);
-    }
 
     f32x16 dq[DP / 32];
 #pragma unroll
@@ -380,7 +380,7 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
             __syncthreads();
             flush();
         }
-        clear(done, past);  // entries of keys that this work-group has not
+        clear(done, past);  // entries of keys that the image has not
     }
 }
 
@@ -593,6 +593,19 @@ template <typename T, int DQP> __global__ void __launch_bounds__(256) gradient_j
     }
 }
 
+// The last key whose place is at most `place` >= 0, and the first whose place is
+// at least that.
+__device__ __forceinline__ int last_key(const Offsets &o, int place, int lk)
+{
+    const int w = o.pitch - o.skip_k, row = fast_div(place, o.by_pitch);
+    return min(row * w + min(place - row * o.pitch, w - 1), lk - 1);
+}
+__device__ __forceinline__ int first_key(const Offsets &o, int place)
+{
+    const int w = o.pitch - o.skip_k, row = fast_div(max(place, 0), o.by_pitch);
+    return row * w + min(max(place, 0) - row * o.pitch, w);
+}
+
 // Sum over images slice, slice + slices, .., blocks b0, b0 + step, .. and their
 // work-groups of what offset `a` has in them, in a fixed order.
 __device__ __forceinline__ double offset_sum(const Backward &f, int head, int a, int slice, int slices, int b0, int step,
@@ -604,15 +617,16 @@ __device__ __forceinline__ double offset_sum(const Backward &f, int head, int a,
     double s = 0.0;
     for (int b = b0; b < f.blocks; b += step) {
         const int low = f.o.origin - place_q(f.o, min((b + 1) * kQueries, lq) - 1);
-        const int past = f.o.origin - place_q(f.o, b * kQueries) + last_k + 1;
-        if (a < low || a >= past)
+        const int high = f.o.origin - place_q(f.o, b * kQueries);
+        if (a < low || a > high + last_k)
             continue;
         const float *p = f.offsets + (int64_t(head) * f.blocks + b) * f.q_splits * f.range + (a - low);
-        if (f.q_splits > 1) {  // (few images then)
+        if (f.q_splits > 1) {  // (few images then; those that have the offset to one of their keys)
+            const int sp0 = first_key(f.o, a - high) / f.q_span, sp1 = last_key(f.o, a - low, g.lk()) / f.q_span;
             for (int img = slice; img < g.n; img += slices)
 #pragma unroll 8
-                for (int sp = 0; sp < f.q_splits; ++sp)
-                    s += double(p[img * image + int64_t(sp) * f.range]);
+                for (int sp = sp0; sp <= sp1; ++sp)
+                    s += double(p[img * image + int64_t(sp) * f.range - place_k(f.o, sp * f.q_span)]);
         } else {
 #pragma unroll 8
             for (int img = slice; img < g.n; img += slices)
@@ -773,6 +787,23 @@ int share(int64_t groups, int tiles)
     return groups >= 256 ? 1 : int(std::max<int64_t>(1, std::min<int64_t>(512 / groups, tiles / kLeastTiles)));
 }
 
+// That, in whole tiles.
+struct Walk {
+    int splits, tiles;  // tiles of each
+    Walk(int64_t groups, int walk)
+    {
+        tiles = (walk + share(groups, walk) - 1) / share(groups, walk);
+        splits = (walk + tiles - 1) / tiles;
+    }
+};
+
+// Entries of a work-group's sums by offset.
+int offset_range(const AttnGeom &g, const Offsets &o, int keys)
+{
+    return place_span(std::min(kQueries, g.lq()), g.wq, g.hq, o.skip_q) +
+           place_span(std::min(keys, g.lk()), g.wk, g.hk, o.skip_k);
+}
+
 Plan backward_plan(const AttnCall &a, DType dt, const AttnGradients &gr)
 {
     const AttnGeom &g = a.g;
@@ -789,12 +820,11 @@ Plan backward_plan(const AttnCall &a, DType dt, const AttnGradients &gr)
     const int key_blocks = (lk + kQueries - 1) / kQueries;
     const int q_walk = (lk + tile - 1) / tile, k_walk = (lq + tile - 1) / tile * (g.heads / g.kv_heads);
     const int64_t q_groups = int64_t(g.n) * g.heads * p.blocks, k_groups = int64_t(g.n) * g.kv_heads * key_blocks;
-    p.q_splits = share(q_groups, q_walk);
-    p.q_tiles = (q_walk + p.q_splits - 1) / p.q_splits;
-    p.q_splits = (q_walk + p.q_tiles - 1) / p.q_tiles;
-    p.k_splits = share(k_groups, k_walk);
-    p.k_tiles = (k_walk + p.k_splits - 1) / p.k_splits;
-    p.k_splits = (k_walk + p.k_tiles - 1) / p.k_tiles;
+    const Walk qw(q_groups, q_walk), kw(k_groups, k_walk);
+    p.q_splits = qw.splits;
+    p.q_tiles = qw.tiles;
+    p.k_splits = kw.splits;
+    p.k_tiles = kw.tiles;
     // (room for what smaller batches share: at most 512 work-groups)
     const bool q_shared = q_walk >= 2 * kLeastTiles, k_shared = k_walk >= 2 * kLeastTiles;
     if (q_shared)
@@ -814,15 +844,15 @@ Plan backward_plan(const AttnCall &a, DType dt, const AttnGradients &gr)
         p.q_cap = segment_cap(block_q + place_span(tile, g.wk, g.hk, o.skip_k) + 8, p.q_lds, q_entry);
         p.k_cap = segment_cap(block_k + place_span(tile, g.wq, g.hq, o.skip_q) + 8, p.k_lds, 4);
         if (table) {
-            p.range = block_q + host_place(lk - 1, g.wk, o.skip_k) + 1;
-            p.offset_bytes = round_up(size_t(std::max<int64_t>(q_groups, q_shared ? 512 : 0)) * p.range * sizeof(float));
+            p.range = offset_range(g, o, p.q_tiles * tile);
+            p.offset_bytes = round_up(size_t(q_groups) * p.q_splits * p.range * sizeof(float));
             // few sums are taken to their buckets directly (2 images of 16 x 16, 2
             // heads: 6.5 us from four, 10.7 from sixteen, 4.7 + 4.5 and a launch's
             // distance in two); images whose queries
             // have places of their own have slices of their own
             p.direct = int64_t(g.n) * p.blocks * p.q_splits <= 16;
             p.slices = a.pos != nullptr ? g.n : p.direct ? 1
-                     : std::min(g.n, std::max(1, 2048 / std::max(1, (o.total + 63) / 64 * g.heads)));
+                     : std::min(g.n, std::max(1, int(2048 / std::max<int64_t>(1, (o.total + 63) / 64 * int64_t(g.heads)))));
             p.sum_bytes = round_up(size_t(p.slices) * g.heads * o.total * sizeof(double));
         }
     }
@@ -886,7 +916,19 @@ bool attention_backward_fits(const AttnCall &a, DType dt, const AttnGradients &g
 size_t attention_backward_work_bytes(const AttnCall &a, DType dt, const AttnGradients &gr)
 {
     const Plan p = backward_plan(a, dt, gr);
-    return 4 * p.q_copy + 2 * p.k_copy + p.delta_bytes + p.offset_bytes + p.sum_bytes + p.part_q + 2 * p.part_k;
+    size_t offset_bytes = p.offset_bytes;
+    if (offset_bytes > 0 && p.part_q > 0) {
+        // (smaller batches are shared by more work-groups, whose entries overlap)
+        const Offsets o = make_offsets(a.g);
+        const int tile = dt == DType::BF16 ? 64 : 32, walk = (a.g.lk() + tile - 1) / tile;
+        const int64_t image = int64_t(a.g.heads) * p.blocks;
+        for (int64_t groups = image; groups < std::min<int64_t>(256, image * a.g.n); groups += image) {
+            const Walk w(groups, walk);
+            offset_bytes = std::max(offset_bytes, round_up(size_t(groups) * w.splits * offset_range(a.g, o, w.tiles * tile) *
+                                                           sizeof(float)));
+        }
+    }
+    return 4 * p.q_copy + 2 * p.k_copy + p.delta_bytes + offset_bytes + p.sum_bytes + p.part_q + 2 * p.part_k;
 }
 
 hipError_t attention_backward_run(const AttnCall &a, DType dt, const AttnGradients &gr, void *work, hipStream_t s)
@@ -944,6 +986,7 @@ hipError_t attention_backward_run(const AttnCall &a, DType dt, const AttnGradien
     f.k_splits = p.k_splits;
     f.q_tiles = p.q_tiles;
     f.k_tiles = p.k_tiles;
+    f.q_span = p.q_tiles * (dt == DType::BF16 ? 64 : 32);
     if (hipError_t e = dt == DType::BF16 ? launch_dq<__bf16>(f, p, s) : launch_dq<float>(f, p, s))
         return e;
     if (!table)

@@ -418,10 +418,6 @@ inline Offsets make_offsets(const AttnGeom &g)
     o.cap = 0;
     return o;
 }
-__device__ __host__ __forceinline__ int host_place(int t, int w, int skip)
-{
-    return t + t / w * skip;
-}
 __device__ __forceinline__ int place_q(const Offsets &o, int t)
 {
     return t + fast_div(t, o.by_wq) * o.skip_q;
