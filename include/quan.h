@@ -660,9 +660,9 @@ QUAN_API int quan_attention_forward(const quan_tensor *q, const quan_tensor *k, 
  * a quarter larger than the call asks for, that smaller batches of the same maps
  * fit into: the maps' copies where they need any; 4 * N * heads * Hq*Wq bytes; up
  * to 26 MB (heads of 8 channels) or 100 MB (of 32) for the parts of walks that
- * work-groups share; and with dtable about 4 * N * heads * (Hq*Wq / 128) *
- * (offsets of a map) bytes and 8 * heads * (offsets of a map), with pos N times
- * that.
+ * work-groups share; and with dtable the lesser of 2 GiB and about 4 * N * heads
+ * * (Hq*Wq / 128) * (offsets of a map) bytes, and 8 * heads * (offsets of a map),
+ * up to N times that with pos or few offsets.
  */
 QUAN_API int quan_attention_backward(const quan_tensor *q, const quan_tensor *k, const quan_tensor *v,
                                      const quan_relpos *relpos, const int32_t *kv_len, const int32_t *pos,

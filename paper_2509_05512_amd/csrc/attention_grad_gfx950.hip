@@ -9,7 +9,9 @@
 // dS by offset), the second blocks of keys and walks over the queries of the
 // heads that share them (dK, dV).  Where there are few blocks, several
 // work-groups share a block's walk, and a third launch adds up their results.
-// One or two more bring the sums by offset to buckets, in fp64.
+// One or two more bring the sums by offset to buckets, in fp64; where the sums of
+// all blocks of queries would take too much memory, the first launch and theirs
+// come in turns.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -25,11 +27,13 @@ struct Backward {
     AttnMap out, rest, dout, dq, dk, dv;  // (rest.data may be NULL)
     const float *stats;
     float *delta;    // [n][heads][lq]
-    // sums of dS by offset, [n * heads * blocks][q_splits][range]: a work-group's
-    // entries are those between its queries and its share of the keys, from the
-    // lowest on; NULL: none asked for
+    // sums of dS by offset, [rows][q_splits][range]: a work-group's entries are those
+    // between its queries and its share of the keys, from the lowest on; NULL: none
+    // asked for
     float *offsets;
     int blocks, range;
+    // the launch's blocks of queries, counted by image, head and block
+    int first_row, rows;
     // work-groups that share a block of queries, of keys; the tiles of each
     int q_splits, k_splits, q_tiles, k_tiles;
     int q_span;  // tokens of q_tiles
@@ -135,10 +139,11 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
 
     const AttnGeom &g = f.a.g;
     const int lq = g.lq(), lk = g.lk();
-    const int total = g.n * g.heads * f.blocks * f.q_splits;
+    const int total = f.rows * f.q_splits;
     int id = xcd_order(total);
     if (id >= total)
         return;
+    id += f.first_row;  // (0 with several splits)
     const int block = id % f.blocks;
     id /= f.blocks;
     const int split = id % f.q_splits;
@@ -201,7 +206,7 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
         lane_at = f.o.origin - place_q(f.o, min(query, lq - 1));
         done = low_q + place_k(f.o, begin);
         if (f.offsets != nullptr)
-            offsets = f.offsets + (((int64_t(img) * g.heads + head) * f.blocks + block) * f.q_splits + split) * f.range - done;
+            offsets = f.offsets + (int64_t((img * g.heads + head) * f.blocks + block - f.first_row) * f.q_splits + split) * f.range - done;
     }
     // past the last offset to this work-group's keys
     const int past = MODE != 0 ? high_q + place_k(f.o, min(begin + f.q_span, lk) - 1) + 1 : 0;
@@ -607,7 +612,8 @@ __device__ __forceinline__ int first_key(const Offsets &o, int place)
 }
 
 // Sum over images slice, slice + slices, .., blocks b0, b0 + step, .. and their
-// work-groups of what offset `a` has in them, in a fixed order.
+// work-groups of what offset `a` has in them, in a fixed order.  (Of those whose
+// blocks the launch before has taken.)
 __device__ __forceinline__ double offset_sum(const Backward &f, int head, int a, int slice, int slices, int b0, int step,
                                              int last_k)
 {
@@ -620,7 +626,8 @@ __device__ __forceinline__ double offset_sum(const Backward &f, int head, int a,
         const int high = f.o.origin - place_q(f.o, b * kQueries);
         if (a < low || a > high + last_k)
             continue;
-        const float *p = f.offsets + (int64_t(head) * f.blocks + b) * f.q_splits * f.range + (a - low);
+        const int row = head * f.blocks + b, per_image = g.heads * f.blocks;  // of image 0
+        const float *p = f.offsets + int64_t(row - f.first_row) * f.q_splits * f.range + (a - low);
         if (f.q_splits > 1) {  // (few images then; those that have the offset to one of their keys)
             const int sp0 = first_key(f.o, a - high) / f.q_span, sp1 = last_key(f.o, a - low, g.lk()) / f.q_span;
             for (int img = slice; img < g.n; img += slices)
@@ -628,20 +635,27 @@ __device__ __forceinline__ double offset_sum(const Backward &f, int head, int a,
                 for (int sp = sp0; sp <= sp1; ++sp)
                     s += double(p[img * image + int64_t(sp) * f.range - place_k(f.o, sp * f.q_span)]);
         } else {
+            int img = slice, end = g.n;
+            if (f.rows < g.n * per_image) {  // images that have the block in the launch
+                const int first = max((f.first_row - row + per_image - 1) / per_image, 0);
+                end = min(max((f.first_row + f.rows - row + per_image - 1) / per_image, 0), end);
+                img += (max(first - slice, 0) + slices - 1) / slices * slices;
+            }
 #pragma unroll 8
-            for (int img = slice; img < g.n; img += slices)
+            for (; img < end; img += slices)
                 s += double(p[img * image]);
         }
     }
     return s;
 }
 
-// Sums by offset of each slice of the images, in fp64: out [slices][heads][total].
+// Sums by offset of each slice of the images, in fp64: out [slices][heads][total],
+// added to what is there where `more`.
 // A lane per offset, the blocks and, where they are few, the images shared out
 // among the waves: what bounds it are the chains of loads (one image of 1600
 // queries, 4 heads: 9 us; 22 where a wave takes all of its offsets' blocks).
 constexpr int kSumWaves = 4;
-__global__ void __launch_bounds__(64 * kSumWaves) offset_sums_kernel(Backward f, int slices, double *__restrict__ out)
+__global__ void __launch_bounds__(64 * kSumWaves) offset_sums_kernel(Backward f, int slices, bool more, double *__restrict__ out)
 {
     __shared__ double parts[kSumWaves][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -658,7 +672,8 @@ __global__ void __launch_bounds__(64 * kSumWaves) offset_sums_kernel(Backward f,
             double s = 0.0;
             for (int w = 0; w < kSumWaves; ++w)
                 s += parts[w][lane];
-            out[(int64_t(slice) * f.a.g.heads + head) * f.o.total + a] = s;
+            double *to = out + (int64_t(slice) * f.a.g.heads + head) * f.o.total + a;
+            *to = more ? *to + s : s;
         }
         __syncthreads();
     }
@@ -763,6 +778,7 @@ table_gradient_kernel(Backward f, int rows, int slices, const double *__restrict
 
 struct Plan {
     int blocks, range, slices, q_cap, k_cap;
+    int rows;  // blocks of queries whose sums by offset are held at a time
     int q_splits, k_splits, q_tiles, k_tiles;
     bool copies, direct;
     size_t q_lds, k_lds;
@@ -796,6 +812,12 @@ struct Walk {
         splits = (walk + tiles - 1) / tiles;
     }
 };
+
+// What sums by offset may take: they grow with the square of a map's pixels, so
+// that beyond this the queries' launch and the sums over its blocks come in turns
+// (backward pass of 64 and 96 heads of 160 x 160, 32 reals each, 2.6 and 3.9 GB of
+// sums: 70.0 and 102.4 ms, 69.2 and 102.7 with all of them held).
+constexpr size_t kOffsetBytes = size_t(2) << 30;
 
 // Entries of a work-group's sums by offset.
 int offset_range(const AttnGeom &g, const Offsets &o, int keys)
@@ -835,6 +857,7 @@ Plan backward_plan(const AttnCall &a, DType dt, const AttnGradients &gr)
     p.k_lds = p.q_lds + size_t(6) * tile * 4;
     const int q_entry = table ? 12 : 4;  // bytes: a bias, and a sum
     p.slices = 1;
+    p.rows = int(q_groups);
     p.delta_bytes = round_up(size_t(g.n) * g.heads * lq * sizeof(float));
     if (a.bias.table != nullptr) {
         const Offsets o = make_offsets(g);
@@ -845,12 +868,15 @@ Plan backward_plan(const AttnCall &a, DType dt, const AttnGradients &gr)
         p.k_cap = segment_cap(block_k + place_span(tile, g.wq, g.hq, o.skip_q) + 8, p.k_lds, 4);
         if (table) {
             p.range = offset_range(g, o, p.q_tiles * tile);
-            p.offset_bytes = round_up(size_t(q_groups) * p.q_splits * p.range * sizeof(float));
+            // (shared walks are few, and their sums no more than the maps)
+            if (p.q_splits == 1)
+                p.rows = int(std::min<int64_t>(q_groups, std::max<int64_t>(1, kOffsetBytes / (size_t(p.range) * sizeof(float)))));
+            p.offset_bytes = round_up(size_t(p.rows) * p.q_splits * p.range * sizeof(float));
             // few sums are taken to their buckets directly (2 images of 16 x 16, 2
             // heads: 6.5 us from four, 10.7 from sixteen, 4.7 + 4.5 and a launch's
             // distance in two); images whose queries
             // have places of their own have slices of their own
-            p.direct = int64_t(g.n) * p.blocks * p.q_splits <= 16;
+            p.direct = int64_t(g.n) * p.blocks * p.q_splits <= 16 && p.rows == q_groups;
             p.slices = a.pos != nullptr ? g.n : p.direct ? 1
                      : std::min(g.n, std::max(1, int(2048 / std::max<int64_t>(1, (o.total + 63) / 64 * int64_t(g.heads)))));
             p.sum_bytes = round_up(size_t(p.slices) * g.heads * o.total * sizeof(double));
@@ -861,14 +887,23 @@ Plan backward_plan(const AttnCall &a, DType dt, const AttnGradients &gr)
     return p;
 }
 
-template <typename T, int DQP, int QMODE, int KMODE> hipError_t launch(Backward f, const Plan &p, hipStream_t s)
+template <typename T, int DQP, int QMODE, int KMODE> hipError_t launch(Backward f, const Plan &p, double *sums, hipStream_t s)
 {
     const AttnGeom &g = f.a.g;
     f.o.cap = p.q_cap;
-    attention_dq_kernel<T, DQP, QMODE>
-        <<<xcd_grid(int64_t(g.n) * g.heads * p.blocks * p.q_splits), kThreads, p.q_lds, s>>>(f);
-    if (hipError_t e = hipGetLastError())
-        return e;
+    const int rows = g.n * g.heads * p.blocks;
+    for (f.first_row = 0; f.first_row < rows; f.first_row += p.rows) {
+        f.rows = std::min(p.rows, rows - f.first_row);
+        attention_dq_kernel<T, DQP, QMODE><<<xcd_grid(int64_t(f.rows) * p.q_splits), kThreads, p.q_lds, s>>>(f);
+        if (hipError_t e = hipGetLastError())
+            return e;
+        if (f.offsets == nullptr || p.direct)
+            continue;
+        offset_sums_kernel<<<dim3((f.o.total + 63) / 64, g.heads, std::min(p.slices, 65535)), 64 * kSumWaves, 0, s>>>(
+            f, p.slices, f.first_row > 0, sums);
+        if (hipError_t e = hipGetLastError())
+            return e;
+    }
     f.o.cap = p.k_cap;
     const int64_t blocks = (g.lk() + kQueries - 1) / kQueries;
     attention_dkv_kernel<T, DQP, KMODE>
@@ -881,27 +916,27 @@ template <typename T, int DQP, int QMODE, int KMODE> hipError_t launch(Backward 
         gradient_join_kernel<T, DQP><<<unsigned((quads + 255) / 256), 256, 0, s>>>(f);
     return hipGetLastError();
 }
-template <typename T, int DQP> hipError_t launch_mode(const Backward &f, const Plan &p, hipStream_t s)
+template <typename T, int DQP> hipError_t launch_mode(const Backward &f, const Plan &p, double *sums, hipStream_t s)
 {
     const AttnGeom &g = f.a.g;
     if (f.a.bias.table == nullptr)
-        return launch<T, DQP, 0, 0>(f, p, s);
+        return launch<T, DQP, 0, 0>(f, p, sums, s);
     const bool k4 = g.hk == 1 || g.wk % 4 == 0, q4 = g.hq == 1 || g.wq % 4 == 0;
     // (four pixels of a row have biases and sums side by side: 341 and 328 us for
     // 16 x 40 x 40, 426 and 343 pixel by pixel)
     if (k4 && q4)
-        return launch<T, DQP, 1, 1>(f, p, s);
-    return launch<T, DQP, 2, 2>(f, p, s);
+        return launch<T, DQP, 1, 1>(f, p, sums, s);
+    return launch<T, DQP, 2, 2>(f, p, sums, s);
 }
-template <typename T> hipError_t launch_dq(const Backward &f, const Plan &p, hipStream_t s)
+template <typename T> hipError_t launch_dq(const Backward &f, const Plan &p, double *sums, hipStream_t s)
 {
     switch (padded_dq(f.a.g.dq)) {
     case 8:
-        return launch_mode<T, 8>(f, p, s);
+        return launch_mode<T, 8>(f, p, sums, s);
     case 16:
-        return launch_mode<T, 16>(f, p, s);
+        return launch_mode<T, 16>(f, p, sums, s);
     default:
-        return launch_mode<T, 32>(f, p, s);
+        return launch_mode<T, 32>(f, p, sums, s);
     }
 }
 
@@ -987,20 +1022,17 @@ hipError_t attention_backward_run(const AttnCall &a, DType dt, const AttnGradien
     f.q_tiles = p.q_tiles;
     f.k_tiles = p.k_tiles;
     f.q_span = p.q_tiles * (dt == DType::BF16 ? 64 : 32);
-    if (hipError_t e = dt == DType::BF16 ? launch_dq<__bf16>(f, p, s) : launch_dq<float>(f, p, s))
+    if (hipError_t e = dt == DType::BF16 ? launch_dq<__bf16>(f, p, sums, s) : launch_dq<float>(f, p, sums, s))
         return e;
     if (!table)
         return hipSuccess;
     const int rows = g.hk + g.hq - 1, groups = g.heads * a.bias.ny;
-    if (p.direct) {
+    f.first_row = 0;
+    f.rows = p.rows;
+    if (p.direct)
         table_gradient_kernel<true><<<groups, kTableThreads, 0, s>>>(f, rows, p.slices, nullptr, gr.dtable);
-        return hipGetLastError();
-    }
-    offset_sums_kernel<<<dim3((f.o.total + 63) / 64, g.heads, std::min(p.slices, 65535)), 64 * kSumWaves, 0, s>>>(
-        f, p.slices, sums);
-    if (hipError_t e = hipGetLastError())
-        return e;
-    table_gradient_kernel<false><<<groups, kTableThreads, 0, s>>>(f, rows, p.slices, sums, gr.dtable);
+    else
+        table_gradient_kernel<false><<<groups, kTableThreads, 0, s>>>(f, rows, p.slices, sums, gr.dtable);
     return hipGetLastError();
 }
 

@@ -81,3 +81,38 @@ def test_captured_smaller_batches(hq, wq, hk, wk, heads, dtype):
                 want = gradients(n, saved[n])
             torch.cuda.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(held, want)), n
+
+
+def test_large_maps_in_turns():
+    """96 heads of 160 x 160, whose sums by offset would take 3.9 GB: they are
+    taken in turns, and the results are those of the images one by one."""
+    say("sums by offset in turns")
+    n, heads, h, w, dq = 3, 32, 160, 160, 8
+    q, k, v, do = (rand_map(s, n, heads * dq, h, w, BF) for s in (1, 2, 3, 4))
+    b = quan.quan_relpos_buckets(159, 16, "cuda")
+    relpos = (torch.randn((heads, 16, 16), generator=torch.Generator().manual_seed(5)).cuda(), b, b)
+
+    def step(i0, i1):
+        q_, k_, v_, do_ = (t[i0:i1] for t in (q, k, v, do))
+        out, stats, rest = quan.quan_attention_forward(q_, k_, v_, heads, relpos=relpos, save=True)
+        grads = dict(zip(("dq", "dk", "dv"), (torch.empty_like(t) for t in (q_, k_, v_))))
+        return lambda: quan.quan_attention_backward(q_, k_, v_, out, stats, rest, do_, heads, relpos=relpos, **grads)
+    one = [step(i, i + 1)() for i in range(n)]
+    call = step(0, n)
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    before = torch.cuda.mem_get_info()[0]
+    with torch.cuda.stream(st):
+        got = call()
+    torch.cuda.synchronize()
+    held = before - torch.cuda.mem_get_info()[0]
+    say(f"{held / 1e6:.1f} MB")
+    # 2 GiB, 26 MB of sums, 25 of parts, 10 of rows, and a quarter of all; torch's small blocks
+    assert held <= 2.85e9
+    for i, each in enumerate(one):
+        for name, a, e in zip(("dq", "dk", "dv"), got, each):
+            assert torch.equal(a[i:i + 1], e), (name, i)
+    parts = torch.stack([e[3] for e in one]).double()
+    # (each rounded once to fp32, from sums that differ by fp64's rounding)
+    off = (got[3].double() - parts.sum(0)).abs()
+    assert bool((off <= 2.0 ** -23 * (parts.abs().sum(0) + got[3].double().abs())).all())
