@@ -175,11 +175,10 @@ __device__ __forceinline__ void row_sums(float (&s)[N], int lpr, float *lds)
     }
 }
 
-// 1 / sqrt(x) of x > 0 (of the smallest normal number for smaller ones, which the
-// instruction takes as 0); NaN stays NaN (fmaxf would take the number).
+// 1 / sqrt(x) of a normal number x > 0; NaN stays NaN.
 __device__ __forceinline__ float inv_sqrt(float x)
 {
-    return __builtin_amdgcn_rsqf(x < 1.17549435e-38f ? 1.17549435e-38f : x);
+    return __builtin_amdgcn_rsqf(x);
 }
 
 // The three sums of a gradient's row, those of absent parts left out.
@@ -551,6 +550,14 @@ Deal deal_rows(const RowsGeom &g, bool by_image)
     return d;
 }
 
+// The smallest eps that is added: the root takes smaller numbers as 0.  (Here, not
+// at each root: a comparison there that lets NaN through, which fmaxf does not, took
+// the gradients of 64 x 56 x 56, 64 channels, from 143 to 205 us.)
+float normal_eps(float eps)
+{
+    return std::max(eps, 1.17549435e-38f);
+}
+
 template <typename T, bool HAS_Y, bool HAS_H>
 hipError_t forward_launch(const RowsGeom &g, const ResidualForward &a, const Drop &drop, float eps, hipStream_t s)
 {
@@ -605,6 +612,7 @@ hipError_t residual_forward_run(const RowsGeom &g, DType dt, const ResidualForwa
                                 hipStream_t s)
 {
     const bool has_y = a.y != nullptr, has_h = a.h != nullptr;
+    eps = normal_eps(eps);
     if (dt == DType::BF16)
         return has_y ? has_h ? forward_launch<__bf16, true, true>(g, a, drop, eps, s)
                              : forward_launch<__bf16, true, false>(g, a, drop, eps, s)
@@ -627,6 +635,7 @@ hipError_t residual_backward_run(const RowsGeom &g, DType dt, const ResidualBack
                                  void *work, hipStream_t s)
 {
     const bool has_y = a.y != nullptr, has_h = a.dh != nullptr;
+    eps = normal_eps(eps);
     if (dt == DType::BF16)
         return has_y ? has_h ? backward_launch<__bf16, true, true>(g, a, drop, eps, work, s)
                              : backward_launch<__bf16, true, false>(g, a, drop, eps, work, s)
