@@ -633,12 +633,16 @@ template <typename T> hipError_t forward_dq(const Forward &f, const Plan &p, hip
     }
 }
 
-// The maps that are copied: a map per z, its images' heads along y (several to a
-// work-group where they have few tokens: `threads` take one, a power of two), 8
-// reals of a token per thread along x.  Of keys and values only what the images have is
-// read (64 tokens in a cache of 4 million, heads of 10 channels: 1336 us for the
-// call when all of it was, 40 now).
-template <typename T, int DQP> __global__ void __launch_bounds__(256) attention_pack_kernel(AttnPack p, int n, int dq, int threads)
+// The maps that are copied: a map per z, its images along y (several to a
+// work-group where they are small: `threads` take one, a power of two), and along x
+// 8 reals of a head's row per thread, the heads of a token side by side as they lie
+// in the map.  (16 images of 40 x 40, 8 heads of 12 channels: 42 us, 76 head by
+// head.)  Of keys and values only what the images have is read: 64 tokens in a
+// cache of 4 million, heads of 10 channels, 35 us for the call, 1336 when all of
+// it was.  (An image's rows of all heads are less than 2^31: their copy would be
+// larger than the memory.)
+template <typename T, int DQP>
+__global__ void __launch_bounds__(256) attention_pack_kernel(AttnPack p, int n, int dq, int threads)
 {
     constexpr int DP = 4 * DQP, kChunks = DP / 8;
     const int d = 8 * int(threadIdx.x % kChunks), per = 256 / threads;
@@ -648,14 +652,17 @@ template <typename T, int DQP> __global__ void __launch_bounds__(256) attention_
     for (int m = 0; m < AttnPack::kMaps; ++m) {
         if (m != int(blockIdx.z))
             continue;
-        const int64_t pairs = int64_t(n) * p.heads[m];
-        for (int64_t pair = int64_t(blockIdx.y) * per + threadIdx.x / threads; pair < pairs; pair += int64_t(gridDim.y) * per) {
-            const int64_t img = pair / p.heads[m];
-            const HeadMap<T, DQP> src(p.src[m], img, int(pair % p.heads[m]), dq);
-            T *dst = static_cast<T *>(p.dst[m]) + pair * p.tokens[m] * DP + d;
+        const int heads = p.heads[m];
+        for (int img = int(blockIdx.y) * per + int(threadIdx.x) / threads; img < n; img += int(gridDim.y) * per) {
+            T *dst = static_cast<T *>(p.dst[m]) + int64_t(img) * heads * p.tokens[m] * DP + d;
             const int tokens = p.kv_len[m] != nullptr ? min(max(p.kv_len[m][img], 0), p.tokens[m]) : p.tokens[m];
-            for (int token = first; token < tokens; token += step)
-                *reinterpret_cast<typename Elem<T>::frag *>(dst + int64_t(token) * DP) = src.load(token, d, true);
+            const int64_t rows = int64_t(tokens) * heads;
+            for (int64_t row = first; row < rows; row += step) {
+                const int token = fast_div(int(row), p.by_heads[m]), head = int(row) - token * heads;
+                const HeadMap<T, DQP> src(p.src[m], img, head, dq);
+                *reinterpret_cast<typename Elem<T>::frag *>(dst + (int64_t(head) * p.tokens[m] + token) * DP) =
+                    src.load(token, d, true);
+            }
         }
     }
 }
@@ -675,19 +682,15 @@ bool whole_maps(const AttnCall &a)
 hipError_t attention_pack_run(const AttnPack &p, int n, int dq, DType dt, hipStream_t s)
 {
     const int dqp = padded_dq(dq);
-    int64_t pairs = 1;
-    int tokens = 1;
-    for (int m = 0; m < p.maps; ++m) {
-        pairs = std::max(pairs, int64_t(n) * p.heads[m]);
-        tokens = std::max(tokens, p.tokens[m]);
-    }
-    const int64_t chunks = int64_t(tokens) * (dqp / 2);
+    int64_t chunks = 1;
+    for (int m = 0; m < p.maps; ++m)
+        chunks = std::max(chunks, int64_t(p.heads[m]) * p.tokens[m] * (dqp / 2));
     int threads = dqp / 2;
     while (threads < 256 && threads < chunks)
         threads *= 2;
     // (work-groups for several rounds of the chip, each with as many turns as it takes)
-    const dim3 grid(unsigned(std::min((chunks + 255) / 256, std::max<int64_t>(1, 24576 / (pairs * p.maps)))),
-                    unsigned(std::min<int64_t>((pairs * threads + 255) / 256, 65535)), unsigned(p.maps));
+    const dim3 grid(unsigned(std::min((chunks + 255) / 256, std::max<int64_t>(1, 24576 / (int64_t(n) * p.maps)))),
+                    unsigned(std::min<int64_t>((int64_t(n) * threads + 255) / 256, 65535)), unsigned(p.maps));
     if (dt == DType::BF16) {
         if (dqp == 8)
             attention_pack_kernel<__bf16, 8><<<grid, 256, 0, s>>>(p, n, dq, threads);
@@ -745,6 +748,7 @@ hipError_t attention_forward_run(const AttnCall &a, DType dt, const AttnMap &out
             pack.src[i] = *m;
             pack.kv_len[i] = q ? nullptr : a.kv_len;
             pack.heads[i] = q ? g.heads : g.kv_heads;
+            pack.by_heads[i] = FastDiv(pack.heads[i]);
             pack.tokens[i] = q ? g.lq() : g.lk();
             pack.dst[i] = at;
             const int64_t d = 4 * padded_dq(g.dq);

@@ -1001,6 +1001,7 @@ hipError_t attention_backward_run(const AttnCall &a, DType dt, const AttnGradien
             pack.src[i].vec = m->vec && g.dq % 8 == 0;
             pack.kv_len[i] = keys ? a.kv_len : nullptr;
             pack.heads[i] = keys ? g.kv_heads : g.heads;
+            pack.by_heads[i] = FastDiv(pack.heads[i]);
             pack.tokens[i] = keys ? g.lk() : g.lq();
             pack.dst[i] = take(keys ? p.k_copy : p.q_copy);
             *m = {pack.dst[i], int64_t(pack.heads[i]) * pack.tokens[i] * d, d, d / 4, true, pack.tokens[i] * d};

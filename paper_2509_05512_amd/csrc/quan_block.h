@@ -109,6 +109,7 @@ struct AttnPack {
     AttnMap src[kMaps];
     const int32_t *kv_len[kMaps];  // [n], NULL: all tokens
     int heads[kMaps], tokens[kMaps];
+    FastDiv by_heads[kMaps];
     void *dst[kMaps];
     int maps;
 };
