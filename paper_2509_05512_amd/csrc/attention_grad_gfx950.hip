@@ -872,11 +872,15 @@ Plan backward_plan(const AttnCall &a, DType dt, const AttnGradients &gr)
             if (p.q_splits == 1)
                 p.rows = int(std::min<int64_t>(q_groups, std::max<int64_t>(1, kOffsetBytes / (size_t(p.range) * sizeof(float)))));
             p.offset_bytes = round_up(size_t(p.rows) * p.q_splits * p.range * sizeof(float));
-            // few sums are taken to their buckets directly (2 images of 16 x 16, 2
-            // heads: 6.5 us from four, 10.7 from sixteen, 4.7 + 4.5 and a launch's
-            // distance in two); images whose queries
-            // have places of their own have slices of their own
-            p.direct = int64_t(g.n) * p.blocks * p.q_splits <= 16 && p.rows == q_groups;
+            // few sums are taken to their buckets directly: `entries` that an offset
+            // has, 16 at most, and 8192 of them in all (backward pass of 16 images
+            // of 8 x 8, 16 heads: 22.7 us, 24.8 in two launches; 8 of 14 x 9, 2 heads:
+            // 28.1, 30.5; one of 30 x 30 and 2 of 32 x 32, 32 heads: no difference;
+            // 4 of 20 x 20, 64 heads: 119.5, 112.8; one of 1 x 2000, 64 heads: 1089,
+            // 473); images whose queries have places of their own have slices of
+            // their own
+            const int64_t entries = int64_t(g.n) * p.blocks * p.q_splits;
+            p.direct = entries <= 16 && entries * o.total <= 8192 && p.rows == q_groups;
             p.slices = a.pos != nullptr ? g.n : p.direct ? 1
                      : std::min(g.n, std::max(1, int(2048 / std::max<int64_t>(1, (o.total + 63) / 64 * int64_t(g.heads)))));
             p.sum_bytes = round_up(size_t(p.slices) * g.heads * o.total * sizeof(double));
