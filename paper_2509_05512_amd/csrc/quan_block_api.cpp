@@ -60,6 +60,7 @@ quan::DType to_dt(int32_t dtype)
     return dtype == QUAN_BF16 ? quan::DType::BF16 : quan::DType::F32;
 }
 
+constexpr int64_t kMaxSpan = int64_t(1) << 48;  // elements from a map's first to its last
 constexpr int64_t kMaxPixels = (int64_t(1) << 31) - 1, kMaxImagePixels = int64_t(1) << 24;
 // Work-groups of 256 lanes (in eights) that a launch may have: a grid's axis holds
 // less than 2^32 lanes.
@@ -192,8 +193,11 @@ int check_map(const char *fn, const char *what, const quan_tensor *t, int32_t dt
         if (t->shape[i] > 1 && (t->strides[i] < 1 || t->strides[i] > int64_t(1) << 40))
             return report(QUAN_ERR_LAYOUT, "%s: %s has stride %lld on axis %d", fn, what, (long long)t->strides[i], i);
     const int64_t s_p = t->strides[1];
-    int64_t s_t = w > 1 ? t->strides[4] : h > 1 ? t->strides[3] : 4 * s_p;
-    int64_t s_n = n > 1 ? t->strides[0] : h * w * s_t;
+    const int64_t s_t = w > 1 ? t->strides[4] : h > 1 ? t->strides[3] : 4 * s_p;
+    // (nothing below leaves 64 bits)
+    if (s_t > kMaxSpan / (h * w) || (n > 1 && t->strides[0] > kMaxSpan / n))
+        return report(QUAN_ERR_UNSUPPORTED, "%s: %s spans more than 2^48 elements", fn, what);
+    const int64_t s_n = n > 1 ? t->strides[0] : h * w * s_t;
     if ((c > 1 && t->strides[2] != 1) || (h > 1 && w > 1 && t->strides[3] != w * s_t) || s_p < c ||
         s_t < 3 * s_p + c || s_n < (h * w - 1) * s_t + 3 * s_p + c)
         return report(QUAN_ERR_LAYOUT,

@@ -139,3 +139,29 @@ def test_examples(lib, q_hw, k_hw, dq, what):
 def test_launches_of_too_many_work_groups(lib, n, heads, q_hw, k_hw, buckets, limited, what):
     rc = call(lib, q_hw, k_hw, 2, BF, what, n, heads, buckets)
     assert rc == (E_UNSUP if what in limited else E_ALIAS), lib.quan_last_error()
+
+
+@pytest.mark.parametrize("what", ["forward", "dtable"])
+@pytest.mark.parametrize("shape,strides", [
+    ((1, 4, 8, 1, 1 << 24), (1 << 60, 8, 1, 1 << 60, 1 << 40)),     # pixels of an image: 2^64 elements
+    ((1 << 15, 4, 8, 1, 1 << 12), (1 << 40, 8, 1, 1 << 30, 32)),    # images: 2^55
+    ((1, 4, 8, 1 << 12, 1 << 12), (1 << 60, 8, 1, 1 << 40, 1 << 28)),
+    ((1, 4, 8, 1, 1 << 20), (1 << 60, 1 << 38, 1, 1 << 60, 1 << 40))])
+def test_strides_beyond_any_memory(lib, shape, strides, what):
+    """What they span does not fit in 64 bits, or in any memory: refused, with
+    nothing computed from it."""
+    n, _, c, h, w = shape
+    dense = (h * w * 4 * c, c, 1, w * 4 * c, 4 * c)
+
+    def t(i, s):
+        return quan.QuanTensor(addr(i) * 1000, BF, 5, (ctypes.c_int64 * 5)(*shape), (ctypes.c_int64 * 5)(*s))
+    for wide in ("q", "k", "out"):
+        q, k, v, out, dout, dq, dk, dv = (t(i, strides if name == wide else dense) for i, name in
+                                          enumerate(("q", "k", "v", "out", "dout", "dq", "dk", "dv")))
+        first = [ctypes.byref(q), ctypes.byref(k), ctypes.byref(v), None, None, None, 0.1, 1]
+        if what == "forward":
+            rc = lib.quan_attention_forward(*first, ctypes.byref(out), None, 2, None)
+        else:
+            rc = lib.quan_attention_backward(*first, ctypes.byref(out), None, 2, ctypes.byref(dout), ctypes.byref(dq),
+                                             ctypes.byref(dk), ctypes.byref(dv), None, None)
+        assert rc == E_UNSUP and b"2^48" in lib.quan_last_error(), (wide, rc, lib.quan_last_error())
