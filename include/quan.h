@@ -628,13 +628,14 @@ QUAN_API int quan_relpos_buckets(int32_t radius, int32_t buckets, int32_t *map);
  * keys 512 wide fit everywhere, queries of 16 x 4 on keys 1024 wide have no
  * backward pass with dtable.  What does not fit returns QUAN_ERR_UNSUPPORTED
  * before anything is launched, a call with stats also where its backward pass
- * would not fit without dtable.  out may overlap no input; it may
- * be a slice of a map that holds inputs in other channels.  Probabilities of
- * bf16 maps are rounded to bf16 before they meet v (with rest they are split in
- * three such numbers, so that their 24 bits count); everything else is fp32.  Calls with
- * few queries split the keys over work-groups where a workspace can be had
- * (at most 64 MiB); a captured call that cannot have it sums them in one piece,
- * and so may differ in rounding.
+ * would not fit without dtable.
+ * out may overlap no input; it may be a slice of a map that holds inputs in other
+ * channels.  Probabilities of bf16 maps are rounded to bf16 before they meet v
+ * (with rest they are split in three such numbers, so that their 24 bits count),
+ * a single query's are not; everything else is fp32.  Calls with few queries
+ * split the keys over work-groups where a workspace can be had (at most 64 MiB);
+ * a captured call that cannot have it sums them in one piece, and so may differ
+ * in rounding.
  */
 QUAN_API int quan_attention_forward(const quan_tensor *q, const quan_tensor *k, const quan_tensor *v,
                                     const quan_relpos *relpos, const int32_t *kv_len, const int32_t *pos,
@@ -649,7 +650,9 @@ QUAN_API int quan_attention_forward(const quan_tensor *q, const quan_tensor *k, 
  *   dq = scale dS k,  dk = scale dS^T q,
  *   dtable[h][b] = sum of dS over the images and pairs of pixels in bucket b.
  *
- *   rest       the forward's, or NULL: row sums then take the rounded out.
+ *   rest       the forward's, or NULL: row sums then take the rounded out.  With
+ *              bf16 maps P is rounded to bf16 before it meets dout, and dS before it
+ *              meets k and q; row sums and dtable take neither.
  *   dq, dk, dv descriptors like q, k, v (strides of their own; slices of one
  *              map may be passed), overlapping nothing else.  dk and dv are
  *              sums over the heads that share them, and zero behind kv_len.
@@ -680,8 +683,9 @@ QUAN_API int quan_rmsnorm_forward(const void *x, const float *gamma, float eps, 
 
 /* Its gradients for dL/dout = dout: dx = dres + r (gamma dout - xhat
  * mean(gamma dout xhat)), r = 1 / sqrt(mean(x^2) + eps), xhat = r x, and dgamma
- * = sum of dout xhat over pixels ([4, c] fp32, added up in fp64 in a fixed
- * order).  dres, like x, is a gradient that reaches x past the norm, or NULL;
+ * = sum of dout xhat over pixels ([4, c] fp32, added up in a fixed order, in fp32
+ * over the pixels that a work-group takes and in fp64 beyond).  dres, like x, is a
+ * gradient that reaches x past the norm, or NULL;
  * dx may be dres or dout but may not otherwise overlap an input. */
 QUAN_API int quan_rmsnorm_backward(const void *x, const void *dout, const float *gamma, const void *dres,
                                    float eps, void *dx, float *dgamma, int32_t n, int32_t c, int32_t h,
@@ -720,8 +724,8 @@ QUAN_API int quan_residual_forward(const void *x, const void *y, const void *gat
  *
  * dgate (dtype), dgamma, dscale and dnext_gamma (fp32 [4, c]) are NULL exactly
  * where their parameter is.  dx may be dout or dh, dy may be y; other overlaps
- * are refused.  Sums are added in fp64 in a fixed order: deterministic.  Uses
- * a workspace per (device, stream).
+ * are refused.  Sums have a fixed order, in fp32 over the pixels that a work-group
+ * takes and in fp64 beyond: deterministic.  Uses a workspace per (device, stream).
  */
 QUAN_API int quan_residual_backward(const void *y, const void *dout, const void *out, const void *dh,
                                     const void *gate, const float *gamma, const float *scale,

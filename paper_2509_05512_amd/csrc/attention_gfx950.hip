@@ -5,10 +5,13 @@
 // wave holds its 32 queries' rows, and the transposed scores S^T = K Q^T leave a
 // query's scores in two lanes (see attention_tile.h), so that maxima and sums
 // are taken in registers and the probabilities are the next product's operand.
-// What bounds it is what a wave issues between two products: 16 exponentials,
-// sums and biases of a lane's scores, and the tiles' way out of LDS.  2 images of
-// 80 x 80, 4 heads of 128 reals: 255 us, 660 TFLOP/s; 16 of 40 x 40, 8 heads of
-// 64, in training 271 us, 620 TFLOP/s (matrix units busy 25 and 29 % of the time).
+// What bounds it is what a wave issues between two products, 16 exponentials, sums
+// and biases of a lane's scores: 16 images of 40 x 40, 8 heads of 64 reals, in
+// training 276 us, 300 TFLOP/s of its two products (it makes four, see PARTS), with
+// the SIMDs at vector instructions 65 % of the time, the matrix units 29 %, LDS 24 %.
+// Where there are few work-groups it is that: 2 of 80 x 80, 4 heads of 128, 255 us,
+// 660 TFLOP/s, 400 of them, 1.3 waves a SIMD that wait 38 % of their time (vector
+// instructions 35 %, matrix units 25 %, LDS 28 %).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -32,7 +35,9 @@ struct Forward {
 };
 
 // PARTS (3 in a training step in bf16, else 1): bf16 numbers that a probability
-// meets v in, each what the ones before leave of it.  The gradient of the bias,
+// meets v in, each what the ones before leave of it.  At inference one will do: it
+// is off by 2^-8 of a term at most, as out is of the sum once it is rounded (all in
+// all 2.3e-3 of out's norm, 1.7e-3 from out's own rounding).  The gradient of the bias,
 // which is fp32, goes by the rows' sums of dout out: with probabilities of 8 bits
 // 3e-4 of its norm was wrong, of 16 bits 1e-6 to 7e-6, of 24 bits what fp32
 // leaves, 1e-7 to 4e-7.  The third part is 45 us of the 270 at 1600 queries and
@@ -216,20 +221,21 @@ __global__ void __launch_bounds__(kThreads, 2) attention_forward_kernel(Forward 
         o[i] *= inv;
         om.store(query, i, half, o[i], q_here);
     }
-    if constexpr (sizeof(T) == 2)
+    if constexpr (sizeof(T) == 2) {
         if (f.rest != nullptr) {
-        const int64_t c_all = int64_t(g.heads) * g.dq;
-        const AttnMap dense{f.rest, lq * 4 * c_all, 4 * c_all, c_all, g.dq % 8 == 0, g.dq};
-        const HeadMap<T, DQP> rm(dense, img, head, g.dq);
+            const int64_t c_all = int64_t(g.heads) * g.dq;
+            const AttnMap dense{f.rest, lq * 4 * c_all, 4 * c_all, c_all, g.dq % 8 == 0, g.dq};
+            const HeadMap<T, DQP> rm(dense, img, head, g.dq);
 #pragma unroll
-        for (int i = 0; i < DP / 32; ++i)
+            for (int i = 0; i < DP / 32; ++i)
 #pragma unroll
-            for (int gq = 0; gq < 4; ++gq) {
-                const int d = 32 * i + 8 * gq + 4 * half;
-                const f32x4 v = {o[i][4 * gq], o[i][4 * gq + 1], o[i][4 * gq + 2], o[i][4 * gq + 3]};
-                if (q_here)
-                    store_rest(rm.at(query, d), v, rm.valid(d, 4), rm.vec);
-            }
+                for (int gq = 0; gq < 4; ++gq) {
+                    const int d = 32 * i + 8 * gq + 4 * half;
+                    const f32x4 v = {o[i][4 * gq], o[i][4 * gq + 1], o[i][4 * gq + 2], o[i][4 * gq + 3]};
+                    if (q_here)
+                        store_rest(rm.at(query, d), v, rm.valid(d, 4), rm.vec);
+                }
+        }
     }
     if (f.stats != nullptr && half == 0 && q_here) {
         f.stats[2 * row] = top == -INFINITY ? 0.0f : top;
@@ -250,11 +256,12 @@ __device__ __forceinline__ void finish_real(const Forward &f, int64_t row, int r
     if (om.valid(real, 1) > 0) {
         const T rounded = T(value);
         *om.at(query, real) = rounded;
-        if constexpr (sizeof(T) == 2)
+        if constexpr (sizeof(T) == 2) {
             if (f.rest != nullptr) {
-            const int64_t c_all = int64_t(g.heads) * g.dq;
-            static_cast<short *>(f.rest)[((img * lq + query) * 4 + real / DQP) * c_all + int64_t(head) * g.dq + real % DQP] =
-                rest_of(value, rounded);
+                const int64_t c_all = int64_t(g.heads) * g.dq;
+                static_cast<short *>(f.rest)[((img * lq + query) * 4 + real / DQP) * c_all + int64_t(head) * g.dq + real % DQP] =
+                    rest_of(value, rounded);
+            }
         }
     }
     if (f.stats != nullptr && real == 0) {
@@ -318,10 +325,11 @@ __global__ void __launch_bounds__(256) attention_join_kernel(Forward f)
 // map.  Each such set of lanes walks over every `slots`-th key with a softmax
 // of its own; they are joined in LDS, and those of several splits of an image's
 // keys (equal shares of what the image has) by attention_join_kernel.  Biases of
-// a chunk of keys are looked up into LDS at a time.  Bound by reading keys and
-// values once, and below that by a first key's way from memory: a cache of 4 x
-// 65536 keys (half of them there), 8 heads of 64 reals on 2 of keys: 27 us, 2.5
-// TB/s, and 4 us of joining; 64 maps of 20 x 20, 4 heads of 64: 12 and 3 us.
+// a chunk of keys are looked up into LDS at a time.  Probabilities stay in fp32.
+// Bound by the way of keys and values from memory, read once: a cache of 4 x 65536
+// keys (half of them there), 8 heads of 64 reals on 2 of keys: 27 us, 2.5 TB/s, 1.9
+// waves a SIMD that wait 53 % of their time, and 4 us of joining; 64 maps of 20 x 20,
+// 4 heads of 64: 12 and 3 us, 0.9 waves, 73 %.
 struct Token {
     int heads_per_block, slots, kv_blocks, group_blocks, chunk;
 };

@@ -51,7 +51,8 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves, kQueries = 32 * kWaves;
 // fp32 long before dO does).  k = kSumBits - e for a bound below 2^e: an
 // offset's terms (one per query, 128) stay below 2^50, and a term's last place
 // is 2^-42 of the bound.  A tile with a larger bound takes the array to coarser
-// units.  What NaN or infinity is in the work-group's rows or in v gives NaN.
+// units.  What NaN or infinity is in the work-group's rows or in v, and a bound
+// beyond fp32, gives NaN.
 //
 // Adding 1.5 * 2^52 to a term brings it, rounded, to the low bits of a double;
 // those bits are added as they are, the constant with them: it is a multiple of
@@ -119,10 +120,14 @@ __device__ __forceinline__ void store_part(float *dst, const f32x16 (&v)[DP / 32
 
 // The launch of the queries' side.  Sums of dS by offset are gathered over the
 // segment whose biases are staged; as the walk leaves it they go to the
-// work-group's own row of `offsets`.  Bound by the instructions to LDS, an
-// addition and a quarter of a bias per pair above all: 16 images of 40 x 40, 8
-// heads of 64 reals, 340 us, 370 TFLOP/s of its three products (190 without a
-// bias); 32 of 14 x 14, 16 heads, 65 us (a tile of 64 keys in four has 4).
+// work-group's own row of `offsets`.  16 images of 40 x 40, 8 heads of 64 reals:
+// 343 us, 370 TFLOP/s of its three products, 190 us without a bias: an addition and
+// a quarter of a bias in LDS per pair are the rest.  2.2 waves a SIMD wait 49 % of
+// their time (vector instructions 43 %, LDS 38 %, matrix units 17 %).  32 of 14 x
+// 14, 16 heads: 66 us (a tile of 64 keys in four has 4; 1.7 waves, 60 %).  Three
+// waves a SIMD spill 7 registers a lane, 16 where places are looked up one by one;
+// two, which spill none, take 380 us for the first (56 for the second).  dS meets k
+// rounded to bf16, off by 2^-8 of a term at most, as dq is once it is rounded.
 template <typename T, int DQP, int MODE>
 __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kernel(Backward f)
 {
@@ -389,9 +394,12 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) attention_dq_kern
     }
 }
 
-// The launch of the keys' side: lanes hold keys, registers queries.  Bound as the
-// forward pass is: 16 images of 40 x 40, 8 heads of 64 reals, 325 us, 520 TFLOP/s
-// of its four products; 32 of 14 x 14, 16 heads, 47 us.
+// The launch of the keys' side: lanes hold keys, registers queries.  Bound by what
+// two waves a SIMD, all that its accumulators leave room for, wait for: 16 images of
+// 40 x 40, 8 heads of 64 reals, 330 us, 510 TFLOP/s of its four products (45 % of
+// 1.6 waves' time; vector instructions and LDS 34 %, matrix units 23 %); 32 of 14 x
+// 14, 16 heads, 47 us.  P meets dout and dS meets q rounded to bf16, off by 2^-8 of a
+// term at most, as dv and dk are once they are rounded.
 constexpr int kNoSegment = -(1 << 30);
 // A value of each row of a tile, as accumulators have them.
 __device__ __forceinline__ f32x16 row_values(const float *values, int first, int sub)

@@ -211,7 +211,8 @@ struct Lane {
 // ------------------------------------------------------------------- forward
 
 // Bound by HBM: two maps read and two written, 8 bytes per real in bf16 (64 x 56
-// x 56, 64 channels: 411 MB in 93 us, 4.4 TB/s where a large copy has 5.3).  The
+// x 56, 64 channels: 411 MB in 93 us, 4.4 TB/s where a large copy has 5.3; 108 us
+// where every pass has maps of its own, none of them left in the last cache).  The
 // work-groups walk over the rows side by side, so that at any time few DRAM
 // pages are in use, and what they write goes past the caches (116 us before).
 template <typename T, bool BLOCK, bool HAS_Y, bool HAS_H>
@@ -295,7 +296,8 @@ struct Deal {
 // factors and yhat = y / rms(y) (or y):
 //   dx = G,  u = G m scale gate gamma,  dy = (u - yhat mean(u yhat)) / rms(y),
 //   Q[image] = sum over rows of G m yhat,  N = sum over rows of dh out / rms(out);
-// Q carries the gradients of gate, scale and gamma, N that of next_gamma.
+// Q carries the gradients of gate, scale and gamma, N that of next_gamma; a lane
+// adds up its rows in fp32, what lies beyond a work-group's sums is fp64.
 // Bound by HBM: four maps read and two written, 12 bytes per real in bf16 (64 x
 // 56 x 56, 64 channels: 617 MB in 134 us, 4.6 TB/s, and 10 us for the sums).
 template <typename T, bool BLOCK, bool HAS_Y, bool HAS_H>
