@@ -889,9 +889,12 @@ Plan backward_plan(const AttnCall &a, DType dt, const AttnGradients &gr)
             // their own
             const int64_t entries = int64_t(g.n) * p.blocks * p.q_splits;
             p.direct = entries <= 16 && entries * o.total <= 8192 && p.rows == q_groups;
-            p.slices = a.pos != nullptr ? g.n : p.direct ? 1
-                     : std::min(g.n, std::max(1, int(2048 / std::max<int64_t>(1, (o.total + 63) / 64 * int64_t(g.heads)))));
-            p.sum_bytes = round_up(size_t(p.slices) * g.heads * o.total * sizeof(double));
+            const int most = a.pos != nullptr
+                                 ? g.n
+                                 : std::min(g.n, std::max(1, int(2048 / std::max<int64_t>(1, (o.total + 63) / 64 * int64_t(g.heads)))));
+            p.slices = p.direct && a.pos == nullptr ? 1 : most;
+            // (a smaller batch's may go through slices where this one's do not)
+            p.sum_bytes = round_up(size_t(most) * g.heads * o.total * sizeof(double));
         }
     }
     p.q_lds += size_t(p.q_cap) * q_entry;

@@ -83,6 +83,38 @@ def test_captured_smaller_batches(hq, wq, hk, wk, heads, dtype):
             assert all(torch.equal(a, b) for a, b in zip(held, want)), n
 
 
+def test_captured_smaller_batch_in_slices():
+    """16 images whose sums go to their buckets directly, then 15, dealt out to
+    twice the work-groups, whose sums go through slices of the images."""
+    say("smaller batch in slices")
+    most, n, heads, dq, h, w = 16, 15, 16, 8, 8, 16
+    q, k, v, do = (rand_map(s, most, heads * dq, h, w, F32) for s in (1, 2, 3, 4))
+    by, bx = (quan.quan_relpos_buckets(r - 1, 9, "cuda") for r in (h, w))
+    relpos = (torch.randn((heads, 9, 9), generator=torch.Generator().manual_seed(5)).cuda(), by, bx)
+    saved = [quan.quan_attention_forward(q[:m], k[:m], v[:m], heads, relpos=relpos, save=True) for m in (most, n)]
+
+    def gradients(m, kept):
+        return quan.quan_attention_backward(q[:m], k[:m], v[:m], *kept, do[:m], heads, relpos=relpos)
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        gradients(most, saved[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        held = gradients(n, saved[1])
+    for rep in range(3):
+        do.copy_(rand_map(10 + rep, most, heads * dq, h, w, F32))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(st):
+            gradients(most, saved[0])
+            want = gradients(n, saved[1])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, want))
+
+
 def test_large_maps_in_turns():
     """96 heads of 160 x 160, whose sums by offset would take 3.9 GB: they are
     taken in turns, and the results are those of the images one by one."""
