@@ -579,8 +579,9 @@ typedef struct quan_relpos {
  * A bucket map for quan_relpos, written to host memory: one bucket per offset
  * where buckets >= 2*radius + 1; else buckets/2 for each sign (an offset of 0
  * counts as negative), the nearer half of them one per distance and the others
- * in steps that widen by a constant factor up to `radius`.  map holds 2*radius
- * + 1 entries.
+ * in steps that widen by a constant factor up to `radius` (C. Raffel et al.,
+ * "Exploring the limits of transfer learning with a unified text-to-text
+ * transformer", JMLR 21, 2020).  map holds 2*radius + 1 entries.
  */
 QUAN_API int quan_relpos_buckets(int32_t radius, int32_t buckets, int32_t *map);
 
