@@ -751,6 +751,164 @@ QUAN_API int quan_residual_backward(const void *y, const void *dout, const void 
 QUAN_API int quan_dropout(const void *x, float p, const uint64_t *rng, void *out, int32_t n, int32_t c,
                           int32_t h, int32_t w, int32_t dtype, void *stream);
 
+/*
+ * Sequences of pixels
+ * -------------------
+ * The attention block where maps come pixel after pixel, in raster order, and
+ * a pixel sees those before it: whole prompts packed one behind another, a
+ * cache of their keys and values in pages, and one new pixel per sequence
+ * against that cache.
+ *
+ * The maps of these entry points hold sequences of tokens (pixels) in one of two
+ * ways.  With first = NULL, sequence i is image i, all of its pixels in row
+ * order.  With first, an int32 array [sequences + 1] on the device that ascends
+ * from 0 or more to at most the map's pixels, the map is one image (N = 1) and
+ * sequence i its pixels first[i] .. first[i + 1] - 1; sequences may be empty,
+ * and what lies before the first and behind the last one is neither read nor
+ * written.  (Values out of order or range are clamped: their sequences are cut,
+ * no memory outside the maps is touched.)
+ */
+
+/* What a cache holds: the maps' own type, or 8-bit floats (e4m3: 4 bits of
+ * exponent, 3 of fraction, no infinities) with a power of two for every token
+ * and head. */
+enum quan_cache_format { QUAN_CACHE_F32 = 0, QUAN_CACHE_BF16 = 1, QUAN_CACHE_E4M3 = 2 };
+
+/*
+ * A cache of keys and values in pages of page_tokens tokens, on the device.
+ *
+ *   keys, values  [pages][heads][page_tokens] rows of quan_cache_row_bytes(dq,
+ *                 format) bytes, 16-byte aligned: a head's 4*dq reals,
+ *                 component-major, zeros behind them.
+ *   key_exp, value_exp   QUAN_CACHE_E4M3: [pages][heads][page_tokens] bytes e +
+ *                 127; a row's reals are its elements times 2^e.  NULL otherwise.
+ *   table         int32 [sequences][table_pages]: the page of positions
+ *                 p * page_tokens .. of each sequence.  Several entries may name
+ *                 one page (a common beginning).  An entry outside 0..pages-1
+ *                 is no page: what would be written there is dropped, what
+ *                 would be read is zero, its tokens take no part in attention.
+ *
+ * pages * heads * page_tokens and table_pages * page_tokens stay below 2^31,
+ * sequences * table_pages too; heads <= 65535, dq <= 32, page_tokens <= 2^24.
+ */
+typedef struct quan_cache {
+    void *keys, *values;
+    uint8_t *key_exp, *value_exp;
+    const int32_t *table;
+    int32_t format, pages, page_tokens, heads, dq, sequences, table_pages;
+} quan_cache;
+
+/* Bytes of a cache's row (see quan_cache), or a negative QUAN_ERR_* code. */
+QUAN_API int64_t quan_cache_row_bytes(int32_t dq, int32_t format);
+
+/*
+ * Keys and values of new tokens into a cache: token j of sequence i goes to
+ * position start[i] + j.
+ *
+ *   k, v      descriptors [N, 4, heads*dq, H, W] as quan_attention_forward takes
+ *             them (channel slices of wider maps); QUAN_F32 or QUAN_BF16, the
+ *             cache's own type or any of the two with QUAN_CACHE_E4M3.
+ *   first     see above; the sequences are the cache's.
+ *   start     int32 [sequences] on the device, or NULL for 0.
+ *   kv_len    int32 [sequences] on the device, or NULL: positions from kv_len[i]
+ *             on are left alone (the end of a padded batch), as are those below
+ *             0 or beyond the table.
+ *
+ * QUAN_CACHE_E4M3: with a the largest magnitude of a row's 4*dq reals, e is the
+ * least whole number >= -117 with a <= 448 * 2^e, and every real is divided by 2^e
+ * and rounded once, to nearest even (but with e = 120 to at most 240, as 256 * 2^120
+ * is no fp32 number); it is off by at most 2^-4 of its magnitude or 2^(e - 10).  A row with an infinity or NaN is kept as NaN, its byte 255.
+ * Two tokens that go to one slot leave it undefined.
+ */
+QUAN_API int quan_cache_write(const quan_tensor *k, const quan_tensor *v, const int32_t *first,
+                              const int32_t *start, const int32_t *kv_len, const quan_cache *cache,
+                              void *stream);
+
+/* The same tokens back into maps k, v: positions start[i] + j below kv_len[i],
+ * zeros for the others, the products with 2^e rounded once to the maps' dtype.
+ * Arguments as quan_cache_write's; k and v may be slices of one map. */
+QUAN_API int quan_cache_read(const quan_cache *cache, const int32_t *first, const int32_t *start,
+                             const int32_t *kv_len, quan_tensor *k, quan_tensor *v, void *stream);
+
+/*
+ * Attention of one new token per sequence over a cache:
+ *
+ *   s_j = scale * Re(sum_c conj(q_c) k_jc) + bias[h][bucket(j)],  out = sum_j P_j v_j,
+ *   P_j = exp(s_j) / sum_j exp(s_j),   over the positions j < kv_len[i],
+ *
+ * as quan_attention_forward's with one query; keys and values are what
+ * quan_cache_read gives in fp32.
+ *
+ *   q, out    descriptors [sequences, 4, heads*dq, 1, 1]; heads is a multiple of
+ *             the cache's, query head h reading its head h / (heads / its heads).
+ *             The dtype is the cache's, or any with QUAN_CACHE_E4M3.
+ *   kv_len    int32 [sequences], or NULL for the whole table (clamped to it).
+ *   relpos    the bias or NULL: position j stands at (j / width, j % width) of a
+ *             map `width` >= 1 pixels wide, the query at pos, int32 [sequences][2]
+ *             (y, x), NULL for (0, 0).
+ *   scale     finite.
+ *
+ * A sequence without a token (or with every bias -infinity) has out 0.  bf16
+ * queries meet bf16 keys as they are (8-bit elements are bf16 numbers);
+ * probabilities keep 16 bits with bf16 queries, 24 with fp32 ones, sums are fp32.
+ * Long sequences are dealt out to work-groups where a workspace can be had (at
+ * most 64 MiB); a captured call that cannot have it may differ in rounding.
+ */
+QUAN_API int quan_cache_attention(const quan_tensor *q, const quan_cache *cache, const quan_relpos *relpos,
+                                  int32_t width, const int32_t *kv_len, const int32_t *pos, float scale,
+                                  int32_t heads, quan_tensor *out, void *stream);
+
+/*
+ * Attention inside sequences, the queries being the last tokens of the keys':
+ * with lq queries and lk keys in a sequence, query i sees
+ *
+ *   keys j <= i + lk - lq   (causal = 1)   or all of them   (causal = 0),
+ *
+ * and out_i = sum_j P_ij v_j as in quan_attention_forward, without a bias.  A
+ * query that sees no key has out 0.
+ *
+ *   q, out     descriptors [N, 4, heads*dq, Hq, Wq]; k, v [N, 4, kv_heads*dq, Hk,
+ *              Wk], kv_heads dividing heads: channel slices of wider maps, as
+ *              quan_attention_forward takes them.
+ *   q_first, k_first   the sequences of the queries' and of the keys' map (see
+ *              above), of `sequences` each; k_first NULL with q_first: the
+ *              same as q_first, the maps being of one size.  Both NULL: the
+ *              images, and sequences is N.
+ *   stats      NULL, or fp32 [heads][N*Hq*Wq][2] for the backward pass: each
+ *              query's maximum in units of log 2 and the sum of 2^(score -
+ *              maximum).
+ *
+ * Probabilities of bf16 maps are rounded to bf16 before they meet v; everything
+ * else is fp32.  out may overlap no input; it may be a slice of a map that holds
+ * inputs in other channels.  Few queries have their keys dealt out to work-groups
+ * where a workspace can be had (at most 64 MiB); a captured call that cannot have
+ * it may differ in rounding.
+ */
+QUAN_API int quan_packed_attention_forward(const quan_tensor *q, const quan_tensor *k, const quan_tensor *v,
+                                           const int32_t *q_first, const int32_t *k_first, int32_t sequences,
+                                           int32_t causal, float scale, int32_t heads, quan_tensor *out,
+                                           float *stats, void *stream);
+
+/*
+ * Its gradients for dL/dout = dout, from what it was given and gave:
+ *
+ *   dP = dout v^T,  dS = P (dP - rowsum(dout out)),  dv = P^T dout,
+ *   dq = scale dS k,  dk = scale dS^T q.
+ *
+ * dq, dk, dv are descriptors like q, k, v (slices of one map may be passed),
+ * overlapping nothing else; dk and dv are sums over the heads that share them, zero
+ * for keys that no query sees.  With bf16 maps P is rounded to bf16 before it meets
+ * dout, and dS before it meets k and q.  Sums have a fixed order: deterministic.
+ * Uses a workspace per (device, stream): the maps' copies where they are no whole
+ * aligned chunks, 4 * heads * N*Hq*Wq bytes, and up to 200 MB for the parts of walks
+ * that work-groups share.
+ */
+QUAN_API int quan_packed_attention_backward(const quan_tensor *q, const quan_tensor *k, const quan_tensor *v,
+                                            const int32_t *q_first, const int32_t *k_first, int32_t sequences,
+                                            int32_t causal, float scale, int32_t heads, const quan_tensor *out,
+                                            const float *stats, const quan_tensor *dout, quan_tensor *dq,
+                                            quan_tensor *dk, quan_tensor *dv, void *stream);
+
 /* Message describing the last failure of a quan_* call on this thread
  * ("" if none).  The pointer stays valid until the next call on the thread. */
 QUAN_API const char *quan_last_error(void);

@@ -15,8 +15,9 @@ LIB = os.path.join(PKG, "libquan.so")
 SOURCES = ["qconv2d_gfx950.hip", "qconv2d_pointwise_gfx950.hip", "qconv2d_wgrad_gfx950.hip",
            "qconv2d_wgrad_rows_gfx950.hip", "stem_gfx950.hip", "iqbn_gfx950.hip",
            "poincare_gfx950.hip", "rows_gfx950.hip",
-           "attention_gfx950.hip", "attention_grad_gfx950.hip", "quan_noalloc.hip", "quan_api.cpp",
-           "quan_block_api.cpp"]
+           "attention_gfx950.hip", "attention_grad_gfx950.hip", "cache_gfx950.hip", "cache_attention_gfx950.hip",
+           "packed_attention_gfx950.hip", "packed_attention_grad_gfx950.hip", "quan_noalloc.hip", "quan_api.cpp",
+           "quan_block_api.cpp", "quan_sequence_api.cpp"]
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -1,0 +1,233 @@
+// Causal attention of packed sequences on gfx950, forward.
+//
+// As in the attention between all pixels of a map, a work-group of four waves
+// takes 128 queries of one head and sequence and walks over the keys in tiles of LDS
+// with the running maximum and sum of a softmax; the transposed scores S^T = K Q^T
+// leave a query's scores in two lanes.  The walk ends with the keys that the block's
+// last query sees.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "packed_tile.h"
+
+namespace quan {
+namespace {
+
+struct Forward {
+    PackedCall c;
+    AttnMap out;
+    float *stats;
+    int blocks;
+};
+
+template <typename T, int DQP>
+__global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(Forward f)
+{
+    constexpr int DP = 4 * DQP;
+    typedef Stage<T, DP, kThreads> Tile;
+    typedef typename Elem<T>::frag frag;
+    constexpr int KT = Tile::kTokens, SUBS = KT / 32;
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
+    __shared__ int counts[kWaves], flags[2 * KT];
+    T *k_lds = reinterpret_cast<T *>(lds_raw), *v_lds = k_lds + 2 * Tile::kElems;
+
+    const PackedCall &c = f.c;
+    // heads side by side, so that each of 8 (or a divisor) stays on an XCD; the
+    // blocks that see most keys first
+    const int head = blockIdx.x % c.heads, kv_head = head / (c.heads / c.kv_heads);
+    const Block b = locate(c.qs, f.blocks - 1 - int(blockIdx.x / c.heads), counts);
+    const Tokens qt = tokens_of(c.qs, c.qs.first, b.seq), kt = tokens_of(c.ks, c.ks.first, b.seq);
+    if (b.at >= qt.len)
+        return;
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int half_at = KT / 2 * half;  // the lane's half of a tile
+    const int query = b.at + 32 * wave + (lane & 31);
+    const bool q_here = query < qt.len;
+    // keys that a query sees: those below query + shift
+    const int shift = c.causal ? kt.len - qt.len + 1 : 0;
+    const int end = c.causal ? min(kt.len, min(b.at + kBlock, qt.len) - 1 + shift) : kt.len;
+    const int wave_end = b.at + 32 * wave >= qt.len ? 0 : c.causal ? min(end, b.at + 32 * wave + 31 + shift) : end;
+    const int seen = c.causal ? query + shift : kt.len;
+
+    const WholeMap<T, DQP> qm(c.q, qt.img, head), km(c.k, kt.img, kv_head), vm(c.v, kt.img, kv_head);
+    Tile k_tile, v_tile;
+    if (end > 0) {
+        k_tile.fetch(km, kt.at, kt.at + end);
+        v_tile.fetch(vm, kt.at, kt.at + end);
+    }
+    frag q[DP / 16];
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i)
+        q[i] = qm.load(qt.at + query, 16 * i + 8 * half, q_here);
+
+    f32x16 o[DP / 32];
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i)
+        o[i] = 0.0f;
+    float top = -INFINITY, sum = 0.0f;
+    const float scale = c.scale * kLog2e;
+
+    int buf = 0;
+    for (int j0 = 0; j0 < end; j0 += KT, buf ^= 1) {
+        T *kb = k_lds + buf * Tile::kElems, *vb = v_lds + buf * Tile::kElems;
+        // whether a query of the block does not see all of the tile
+        const bool edge = c.causal && j0 + KT > b.at + shift;
+        if (edge)
+            zero_not_finite(v_tile, v_tile, flags + buf * KT);
+        k_tile.put(kb);
+        v_tile.put(vb);
+        __syncthreads();
+        if (j0 + KT < end) {
+            k_tile.fetch(km, kt.at + j0 + KT, kt.at + end);
+            v_tile.fetch(vm, kt.at + j0 + KT, kt.at + end);
+        }
+        if (j0 >= wave_end)
+            continue;  // (none of the wave's queries sees the tile)
+        f32x16 s[SUBS];
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub) {
+            s[sub] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < DP / 16; ++i)
+                s[sub] = mma(row_frag<T, DP>(kb, sub, i), q[i], s[sub]);
+        }
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub)
+            s[sub] *= scale;
+        // tiles that reach past what the wave's first query sees
+        if (j0 + KT > min(end, c.causal ? b.at + 32 * wave + shift : end)) {
+#pragma unroll
+            for (int sub = 0; sub < SUBS; ++sub)
+                clear_behind(s[sub], min(seen, end) - j0 - half_at, sub, -INFINITY);
+        }
+        float t = s[0][0];
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                t = fmaxf(t, s[sub][r]);
+        t = half_max(t);
+        if (__any(t > top)) {
+            const float now = fmaxf(top, t);
+            const float back = exp2_fast(top - (now == -INFINITY ? 0.0f : now));
+            top = now;
+            sum *= back;
+#pragma unroll
+            for (int i = 0; i < DP / 32; ++i)
+                o[i] *= back;
+        }
+        const float m = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[sub][r] = exp2_fast(s[sub][r] - m);
+                sum += s[sub][r];
+            }
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                const frag p = acc_frag<T>(s[sub], st);
+#pragma unroll
+                for (int i = 0; i < DP / 32; ++i)
+                    o[i] = mma(col_frag<DP>(vb, sub, st, i), p, o[i]);
+            }
+        for (auto bad = edge ? flagged(flags + buf * KT, KT) : 0; bad != 0; bad &= bad - 1) {
+            const int j = j0 + __builtin_ctzll(bad);
+            const float p = exp2_fast(row_dot(km, kt.at + j, q) * scale - m);
+            row_add(o, vm, kt.at + j, p, j < seen);
+        }
+    }
+    sum = half_sum(sum);
+
+    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+    const HeadMap<T, DQP> om(f.out, qt.img, head, c.dq);
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i) {
+        o[i] *= inv;
+        om.store(qt.at + query, i, half, o[i], q_here);
+    }
+    if (f.stats != nullptr && half == 0 && q_here) {
+        float *st = f.stats + 2 * (head * c.q_tokens() + int64_t(qt.img) * c.qs.tokens + qt.at + query);
+        st[0] = top == -INFINITY ? 0.0f : top;
+        st[1] = sum;
+    }
+}
+
+template <typename T, int DQP> hipError_t launch(const Forward &f, hipStream_t s)
+{
+    constexpr int kTile = Elem<T>::kTile;
+    const size_t lds = size_t(4) * kTile * Lds<T, 4 * DQP>::kRow * sizeof(T);
+    packed_forward_kernel<T, DQP><<<unsigned(int64_t(f.blocks) * f.c.heads), kThreads, lds, s>>>(f);
+    return hipGetLastError();
+}
+template <typename T> hipError_t launch_dq(const Forward &f, hipStream_t s)
+{
+    switch (padded_dq(f.c.dq)) {
+    case 8:
+        return launch<T, 8>(f, s);
+    case 16:
+        return launch<T, 16>(f, s);
+    default:
+        return launch<T, 32>(f, s);
+    }
+}
+
+}  // namespace
+
+size_t packed_copy_bytes(int64_t tokens, int heads, int dq, DType dt)
+{
+    return (size_t(tokens) * heads * 4 * padded_dq(dq) * (dt == DType::BF16 ? 2 : 4) + 255) & ~size_t(255);
+}
+
+void packed_copy_add(AttnPack &pack, AttnMap &m, int images, int tokens, int heads, int dq, DType dt, unsigned char *&at)
+{
+    const int i = pack.maps++;
+    const int64_t d = 4 * padded_dq(dq);
+    pack.src[i] = m;
+    pack.kv_len[i] = nullptr;
+    pack.heads[i] = heads;
+    pack.by_heads[i] = FastDiv(heads);
+    pack.tokens[i] = tokens;
+    pack.dst[i] = at;
+    m = {at, int64_t(heads) * tokens * d, d, d / 4, true, tokens * d};
+    at += packed_copy_bytes(int64_t(images) * tokens, heads, dq, dt);
+}
+
+size_t packed_forward_work_bytes(const PackedCall &c, DType dt)
+{
+    if (c.q.vec && c.k.vec && c.v.vec && padded_dq(c.dq) == c.dq)
+        return 0;
+    return packed_copy_bytes(c.q_tokens(), c.heads, c.dq, dt) + 2 * packed_copy_bytes(c.k_tokens(), c.kv_heads, c.dq, dt);
+}
+
+size_t packed_forward_extra_bytes(const PackedCall &, DType)
+{
+    return 0;
+}
+
+hipError_t packed_forward_run(const PackedCall &c, DType dt, const AttnMap &out, float *stats, void *work, void *,
+                              hipStream_t s)
+{
+    Forward f;
+    f.c = c;
+    f.out = out;
+    f.stats = stats;
+    f.blocks = int(packed_blocks(c.qs));
+    if (work != nullptr) {
+        AttnPack pack;
+        pack.maps = 0;
+        unsigned char *at = static_cast<unsigned char *>(work);
+        packed_copy_add(pack, f.c.q, c.images, c.qs.tokens, c.heads, c.dq, dt, at);
+        packed_copy_add(pack, f.c.k, c.images, c.ks.tokens, c.kv_heads, c.dq, dt, at);
+        packed_copy_add(pack, f.c.v, c.images, c.ks.tokens, c.kv_heads, c.dq, dt, at);
+        if (hipError_t e = attention_pack_run(pack, c.images, c.dq, dt, s))
+            return e;
+    }
+    return dt == DType::BF16 ? launch_dq<__bf16>(f, s) : launch_dq<float>(f, s);
+}
+
+}  // namespace quan

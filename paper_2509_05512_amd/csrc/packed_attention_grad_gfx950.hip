@@ -1,0 +1,389 @@
+// The gradients of causal attention of packed sequences on gfx950.
+//
+// With P the probabilities, recomputed from the rows' saved maxima and sums,
+//   dP = dO V^T,  delta_i = dO_i . O_i,  dS = P (dP - delta),
+//   dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO.
+// Two launches, so that every sum has one owner and a fixed order: the first takes
+// blocks of queries and walks over the keys that they see (dQ, delta), the second
+// blocks of keys and walks over the queries that see them, head by head of those
+// that share them (dK, dV).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "packed_tile.h"
+
+namespace quan {
+namespace {
+
+struct Backward {
+    PackedCall c;
+    AttnMap out, dout, dq, dk, dv;
+    const float *stats;
+    float *delta;  // [heads][q_tokens]
+    int q_blocks, k_blocks;
+};
+
+template <typename T, int DQP>
+__global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) packed_dq_kernel(Backward f)
+{
+    constexpr int DP = 4 * DQP;
+    typedef Stage<T, DP, kThreads> Tile;
+    typedef typename Elem<T>::frag frag;
+    constexpr int KT = Tile::kTokens, SUBS = KT / 32;
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
+    __shared__ int counts[kWaves], flags[2 * KT];
+    T *k_lds = reinterpret_cast<T *>(lds_raw), *v_lds = k_lds + 2 * Tile::kElems;
+
+    const PackedCall &c = f.c;
+    const int head = blockIdx.x % c.heads, kv_head = head / (c.heads / c.kv_heads);
+    const Block b = locate(c.qs, f.q_blocks - 1 - int(blockIdx.x / c.heads), counts);
+    const Tokens qt = tokens_of(c.qs, c.qs.first, b.seq), kt = tokens_of(c.ks, c.ks.first, b.seq);
+    if (b.at >= qt.len)
+        return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int half_at = KT / 2 * half;  // the lane's half of a tile
+    const int query = b.at + 32 * wave + (lane & 31);
+    const bool q_here = query < qt.len;
+    const int shift = c.causal ? kt.len - qt.len + 1 : 0;
+    const int end = c.causal ? min(kt.len, min(b.at + kBlock, qt.len) - 1 + shift) : kt.len;
+    const int wave_end = b.at + 32 * wave >= qt.len ? 0 : c.causal ? min(end, b.at + 32 * wave + 31 + shift) : end;
+    const int seen = min(c.causal ? query + shift : kt.len, end);
+
+    const WholeMap<T, DQP> qm(c.q, qt.img, head), km(c.k, kt.img, kv_head), vm(c.v, kt.img, kv_head);
+    Tile k_tile, v_tile;
+    if (end > 0) {
+        k_tile.fetch(km, kt.at, kt.at + end);
+        v_tile.fetch(vm, kt.at, kt.at + end);
+    }
+    const int64_t row = head * c.q_tokens() + int64_t(qt.img) * c.qs.tokens + qt.at + query;
+    frag q[DP / 16], go[DP / 16];
+    float delta = 0.0f;
+    {
+        const WholeMap<T, DQP> gm(f.dout, qt.img, head), om(f.out, qt.img, head);
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) {
+            const int d = 16 * i + 8 * half;
+            q[i] = qm.load(qt.at + query, d, q_here);
+            go[i] = gm.load(qt.at + query, d, q_here);
+            const f32x8 o = to_f32(om.load(qt.at + query, d, q_here)), w = to_f32(go[i]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                delta = fmaf(w[e], o[e], delta);
+        }
+        delta = half_sum(delta);
+        if (q_here && half == 0)
+            f.delta[row] = delta;
+    }
+    // P = 2^(s - top) inv; rows without a key, and none, have P = 0
+    const float sum = q_here ? f.stats[2 * row + 1] : 0.0f;
+    const bool empty = sum == 0.0f;
+    const float top = empty ? INFINITY : f.stats[2 * row];
+    const float inv = empty ? 0.0f : 1.0f / sum;
+    const float minus = empty ? 0.0f : -delta * inv;
+    const float scale = c.scale * kLog2e;
+
+    f32x16 dq[DP / 32];
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i)
+        dq[i] = 0.0f;
+    int buf = 0;
+    for (int j0 = 0; j0 < end; j0 += KT, buf ^= 1) {
+        T *kb = k_lds + buf * Tile::kElems, *vb = v_lds + buf * Tile::kElems;
+        // whether a query of the block does not see all of the tile
+        const bool edge = c.causal && j0 + KT > b.at + shift;
+        if (edge)
+            zero_not_finite(k_tile, k_tile, flags + buf * KT);
+        k_tile.put(kb);
+        v_tile.put(vb);
+        __syncthreads();
+        if (j0 + KT < end) {
+            k_tile.fetch(km, kt.at + j0 + KT, kt.at + end);
+            v_tile.fetch(vm, kt.at + j0 + KT, kt.at + end);
+        }
+        if (j0 >= wave_end)
+            continue;  // (none of the wave's queries sees the tile)
+        const auto bad = edge ? flagged(flags + buf * KT, KT) : 0;
+        const bool whole = j0 + KT <= min(end, c.causal ? b.at + 32 * wave + shift : end);
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub) {
+            f32x16 s = 0.0f, dp = 0.0f;
+#pragma unroll
+            for (int i = 0; i < DP / 16; ++i) {
+                s = mma(row_frag<T, DP>(kb, sub, i), q[i], s);
+                dp = mma(row_frag<T, DP>(vb, sub, i), go[i], dp);
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                s[r] = exp2_fast(fmaf(s[r], scale, -top)) * fmaf(dp[r], inv, minus);
+            if (!whole)
+                clear_behind(s, seen - j0 - half_at, sub, 0.0f);
+            if (bad != 0)
+                clear_flagged<KT>(s, bad, sub);
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                const frag p = acc_frag<T>(s, st);
+#pragma unroll
+                for (int i = 0; i < DP / 32; ++i)
+                    dq[i] = mma(col_frag<DP>(kb, sub, st, i), p, dq[i]);
+            }
+        }
+        for (auto rest = bad; rest != 0; rest &= rest - 1) {
+            const int j = j0 + __builtin_ctzll(rest);
+            const float p = exp2_fast(fmaf(row_dot(km, kt.at + j, q), scale, -top));
+            row_add(dq, km, kt.at + j, p * fmaf(row_dot(vm, kt.at + j, go), inv, minus), j < seen);
+        }
+    }
+    const HeadMap<T, DQP> om(f.dq, qt.img, head, c.dq);
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i) {
+        dq[i] *= c.scale;
+        om.store(qt.at + query, i, half, dq[i], q_here);
+    }
+}
+
+// A value of each row of a tile, as accumulators have them.
+__device__ __forceinline__ f32x16 row_values(const float *values, int first, int sub)
+{
+    f32x16 v;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const f32x4 t = *reinterpret_cast<const f32x4 *>(values + first + 16 * sub + 4 * g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            v[4 * g + e] = t[e];
+    }
+    return v;
+}
+// `value` in the accumulators of part `sub` whose tokens are before `from` of the
+// lane's half of the tile.
+__device__ __forceinline__ void clear_before(f32x16 &s, int from, int sub, float value)
+{
+    asm volatile("" : "+v"(from));
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+        s[r] = 16 * sub + r < from ? value : s[r];
+}
+
+// The launch of the keys' side: lanes hold keys, registers queries.
+template <typename T, int DQP>
+__global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) packed_dkv_kernel(Backward f)
+{
+    constexpr int DP = 4 * DQP;
+    typedef Stage<T, DP, kThreads> Tile;
+    typedef typename Elem<T>::frag frag;
+    constexpr int QT = Tile::kTokens, SUBS = QT / 32;
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
+    __shared__ int counts[kWaves], flags[2 * QT];
+    float *rows = reinterpret_cast<float *>(lds_raw);  // [2][top, inv, -delta][QT]
+    T *q_lds = reinterpret_cast<T *>(rows + 6 * QT), *g_lds = q_lds + 2 * Tile::kElems;
+
+    const PackedCall &c = f.c;
+    const int group = c.heads / c.kv_heads, kv_head = blockIdx.x % c.kv_heads;
+    // (of causal sequences the first blocks of keys are seen by most queries)
+    const Block b = locate(c.ks, int(blockIdx.x / c.kv_heads), counts);
+    const Tokens qt = tokens_of(c.qs, c.qs.first, b.seq), kt = tokens_of(c.ks, c.ks.first, b.seq);
+    if (b.at >= kt.len)
+        return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int half_at = QT / 2 * half;  // the lane's half of a tile
+    const int key = b.at + 32 * wave + (lane & 31);
+    const bool k_here = key < kt.len;
+    // the first query that sees a key: key - back
+    const int back = c.causal ? kt.len - qt.len : 0;
+
+    const WholeMap<T, DQP> km(c.k, kt.img, kv_head), vm(c.v, kt.img, kv_head);
+    frag k[DP / 16], v[DP / 16];
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) {
+        k[i] = km.load(kt.at + key, 16 * i + 8 * half, k_here);
+        v[i] = vm.load(kt.at + key, 16 * i + 8 * half, k_here);
+    }
+    f32x16 dk[DP / 32], dv[DP / 32];
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i) {
+        dk[i] = 0.0f;
+        dv[i] = 0.0f;
+    }
+    const float scale = c.scale * kLog2e;
+    // tiles of queries, from the first that sees one of the block's keys
+    const int from = c.causal ? max(0, b.at - back) / QT : 0, tiles = max(0, (qt.len + QT - 1) / QT - from);
+    const int last = group * tiles;
+    Tile q_tile, g_tile;
+    float row_top = 0.0f, row_sum = 0.0f, row_delta = 0.0f;  // of thread t < QT's query of a tile
+    auto fetch = [&](int head, int i0) {
+        q_tile.fetch(WholeMap<T, DQP>(c.q, qt.img, head), qt.at + i0, qt.at + qt.len);
+        g_tile.fetch(WholeMap<T, DQP>(f.dout, qt.img, head), qt.at + i0, qt.at + qt.len);
+        if (threadIdx.x < QT) {
+            const int i = i0 + threadIdx.x;
+            const int64_t row = head * c.q_tokens() + int64_t(qt.img) * c.qs.tokens + qt.at + min(i, qt.len - 1);
+            row_top = f.stats[2 * row];
+            row_sum = i < qt.len ? f.stats[2 * row + 1] : 0.0f;
+            row_delta = f.delta[row];
+        }
+    };
+    int head = kv_head * group, tile = from;
+    if (last > 0)
+        fetch(head, tile * QT);
+    int buf = 0;
+    for (int item = 0; item < last; ++item, buf ^= 1) {
+        const int i0 = tile * QT;
+        T *qb = q_lds + buf * Tile::kElems, *gb = g_lds + buf * Tile::kElems;
+        float *rw = rows + buf * 3 * QT;
+        // whether a key of the block is not seen by all of the tile
+        const bool edge = c.causal && i0 < b.at + kBlock - 1 - back;
+        if (edge)
+            zero_not_finite(q_tile, g_tile, flags + buf * QT);
+        q_tile.put(qb);
+        g_tile.put(gb);
+        if (threadIdx.x < QT) {
+            const bool empty = row_sum == 0.0f;
+            rw[threadIdx.x] = empty ? INFINITY : row_top;
+            rw[QT + threadIdx.x] = empty ? 0.0f : 1.0f / row_sum;
+            rw[2 * QT + threadIdx.x] = empty ? 0.0f : -row_delta;
+        }
+        __syncthreads();
+        const int this_head = head;
+        if (++tile == from + tiles) {
+            tile = from;
+            ++head;
+        }
+        if (item + 1 < last)
+            fetch(head, tile * QT);
+        // (a wave whose keys are not there, or that no query of the tile sees)
+        if (b.at + 32 * wave >= kt.len || (c.causal && i0 + QT <= b.at + 32 * wave - back))
+            continue;
+        f32x16 s[SUBS], dp[SUBS];
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub) {
+            s[sub] = 0.0f;
+            dp[sub] = row_values(rw + 2 * QT, half_at, sub);  // dP - delta starts from -delta
+        }
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i)
+#pragma unroll
+            for (int sub = 0; sub < SUBS; ++sub) {
+                s[sub] = mma(row_frag<T, DP>(qb, sub, i), k[i], s[sub]);
+                dp[sub] = mma(row_frag<T, DP>(gb, sub, i), v[i], dp[sub]);
+            }
+        const auto bad = edge ? flagged(flags + buf * QT, QT) : 0;
+        const bool whole = !c.causal || i0 >= b.at + 32 * wave + 31 - back;
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub) {
+            const f32x16 top = row_values(rw, half_at, sub), inv = row_values(rw + QT, half_at, sub);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[sub][r] = exp2_fast(fmaf(s[sub][r], scale, -top[r])) * inv[r];
+                dp[sub][r] *= s[sub][r];
+            }
+            if (!whole) {
+                clear_before(s[sub], key - back - i0 - half_at, sub, 0.0f);
+                clear_before(dp[sub], key - back - i0 - half_at, sub, 0.0f);
+            }
+            if (bad != 0) {
+                clear_flagged<QT>(s[sub], bad, sub);
+                clear_flagged<QT>(dp[sub], bad, sub);
+            }
+        }
+#pragma unroll
+        for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                const frag p = acc_frag<T>(s[sub], st), ds = acc_frag<T>(dp[sub], st);
+#pragma unroll
+                for (int i = 0; i < DP / 32; ++i) {
+                    dv[i] = mma(col_frag<DP>(gb, sub, st, i), p, dv[i]);
+                    dk[i] = mma(col_frag<DP>(qb, sub, st, i), ds, dk[i]);
+                }
+            }
+        for (auto rest = bad; rest != 0; rest &= rest - 1) {
+            const int at = __builtin_ctzll(rest);
+            const WholeMap<T, DQP> qm(c.q, qt.img, this_head), gm(f.dout, qt.img, this_head);
+            const int64_t token = qt.at + i0 + at;
+            const float p = exp2_fast(fmaf(row_dot(qm, token, k), scale, -rw[at])) * rw[QT + at];
+            const bool sees = i0 + at >= key - back;
+            row_add(dv, gm, token, p, sees);
+            row_add(dk, qm, token, p * (row_dot(gm, token, v) + rw[2 * QT + at]), sees);
+        }
+    }
+    const HeadMap<T, DQP> okm(f.dk, kt.img, kv_head, c.dq), ovm(f.dv, kt.img, kv_head, c.dq);
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i) {
+        dk[i] *= c.scale;
+        okm.store(kt.at + key, i, half, dk[i], k_here);
+        ovm.store(kt.at + key, i, half, dv[i], k_here);
+    }
+}
+
+template <typename T, int DQP> hipError_t launch(const Backward &f, hipStream_t s)
+{
+    constexpr int kTile = Elem<T>::kTile;
+    const size_t lds = size_t(4) * kTile * Lds<T, 4 * DQP>::kRow * sizeof(T);
+    packed_dq_kernel<T, DQP><<<unsigned(int64_t(f.q_blocks) * f.c.heads), kThreads, lds, s>>>(f);
+    if (hipError_t e = hipGetLastError())
+        return e;
+    packed_dkv_kernel<T, DQP>
+        <<<unsigned(int64_t(f.k_blocks) * f.c.kv_heads), kThreads, lds + 6 * kTile * sizeof(float), s>>>(f);
+    return hipGetLastError();
+}
+template <typename T> hipError_t launch_dq(const Backward &f, hipStream_t s)
+{
+    switch (padded_dq(f.c.dq)) {
+    case 8:
+        return launch<T, 8>(f, s);
+    case 16:
+        return launch<T, 16>(f, s);
+    default:
+        return launch<T, 32>(f, s);
+    }
+}
+
+bool copies(const PackedCall &c, const PackedGradients &g)
+{
+    return !(c.q.vec && c.k.vec && c.v.vec && g.out.vec && g.dout.vec) || padded_dq(c.dq) != c.dq;
+}
+size_t delta_bytes(const PackedCall &c)
+{
+    return (size_t(c.heads) * c.q_tokens() * sizeof(float) + 255) & ~size_t(255);
+}
+
+}  // namespace
+
+size_t packed_backward_work_bytes(const PackedCall &c, DType dt, const PackedGradients &g)
+{
+    size_t bytes = delta_bytes(c);
+    if (copies(c, g))
+        bytes += 3 * packed_copy_bytes(c.q_tokens(), c.heads, c.dq, dt) +
+                 2 * packed_copy_bytes(c.k_tokens(), c.kv_heads, c.dq, dt);
+    return bytes;
+}
+
+hipError_t packed_backward_run(const PackedCall &c, DType dt, const PackedGradients &g, void *work, hipStream_t s)
+{
+    Backward f;
+    f.c = c;
+    f.out = g.out;
+    f.dout = g.dout;
+    f.dq = g.dq;
+    f.dk = g.dk;
+    f.dv = g.dv;
+    f.stats = g.stats;
+    f.q_blocks = int(packed_blocks(c.qs));
+    f.k_blocks = int(packed_blocks(c.ks));
+    unsigned char *at = static_cast<unsigned char *>(work);
+    f.delta = reinterpret_cast<float *>(at);
+    at += delta_bytes(c);
+    if (copies(c, g)) {
+        AttnPack pack;
+        pack.maps = 0;
+        for (AttnMap *m : {&f.c.q, &f.out, &f.dout})
+            packed_copy_add(pack, *m, c.images, c.qs.tokens, c.heads, c.dq, dt, at);
+        for (AttnMap *m : {&f.c.k, &f.c.v})
+            packed_copy_add(pack, *m, c.images, c.ks.tokens, c.kv_heads, c.dq, dt, at);
+        if (hipError_t e = attention_pack_run(pack, c.images, c.dq, dt, s))
+            return e;
+    }
+    return dt == DType::BF16 ? launch_dq<__bf16>(f, s) : launch_dq<float>(f, s);
+}
+
+}  // namespace quan

@@ -86,6 +86,12 @@ SIGNATURES = {
     "quan_residual_forward": (ctypes.c_int, [_vp] * 6 + [_f32, _vp, _f32] + [_vp] * 2 + [_i32] * 5 + [_vp]),
     "quan_residual_backward": (ctypes.c_int, [_vp] * 8 + [_f32, _vp, _f32] + [_vp] * 6 + [_i32] * 5 + [_vp]),
     "quan_dropout": (ctypes.c_int, [_vp, _f32, _vp, _vp] + [_i32] * 5 + [_vp]),
+    "quan_cache_row_bytes": (ctypes.c_int64, [_i32] * 2),
+    "quan_cache_write": (ctypes.c_int, [_vp] * 7),
+    "quan_cache_read": (ctypes.c_int, [_vp] * 7),
+    "quan_cache_attention": (ctypes.c_int, [_vp] * 3 + [_i32] + [_vp] * 2 + [_f32, _i32] + [_vp] * 2),
+    "quan_packed_attention_forward": (ctypes.c_int, [_vp] * 5 + [_i32, _i32, _f32, _i32] + [_vp] * 3),
+    "quan_packed_attention_backward": (ctypes.c_int, [_vp] * 5 + [_i32, _i32, _f32, _i32] + [_vp] * 7),
     "quan_last_error": (ctypes.c_char_p, []),
     "quan_release": (ctypes.c_int, []),
     "quan_version": (ctypes.c_char_p, []),
@@ -936,6 +942,227 @@ def quan_dropout(x, p, rng=None, out=None):
         rc = lib.quan_dropout(_ptr(x), float(p), _ptr(rng), _ptr(out), n, c, h, w, _dtype_code(x), _stream(x.device))
     _check(rc)
     return out
+
+
+# ------------------------------------------------------ sequences of pixels
+
+QUAN_CACHE_F32, QUAN_CACHE_BF16, QUAN_CACHE_E4M3 = 0, 1, 2
+_FORMATS = {torch.float32: QUAN_CACHE_F32, torch.bfloat16: QUAN_CACHE_BF16, torch.float8_e4m3fn: QUAN_CACHE_E4M3}
+_PACK_CACHE = struct.Struct("@PPPPPiiiiiii4x").pack  # struct quan_cache
+
+
+class Cache(NamedTuple):
+    """A cache of keys and values in pages (struct quan_cache): keys and values
+    [pages, heads, page_tokens, row], row a head's 4 dq reals and zeros up to
+    whole 16 bytes; with float8_e4m3fn elements key_exp and value_exp, uint8
+    [pages, heads, page_tokens], hold e + 127 of a row's factor 2^e (None
+    otherwise).  table: int32 [sequences, pages of each], the page of every
+    page_tokens positions; -1 (or any number that is no page): none."""
+    keys: torch.Tensor
+    values: torch.Tensor
+    key_exp: Optional[torch.Tensor]
+    value_exp: Optional[torch.Tensor]
+    table: torch.Tensor
+    dq: int
+
+    @property
+    def heads(self):
+        return self.keys.shape[1]
+
+    @property
+    def page_tokens(self):
+        return self.keys.shape[2]
+
+
+def quan_cache_row_bytes(dq, dtype=torch.float8_e4m3fn):
+    """Bytes of a cache's row of heads of dq quaternion channels."""
+    got = load_library().quan_cache_row_bytes(int(dq), _FORMATS.get(dtype, -1))
+    _check(min(got, 0))
+    return got
+
+
+def empty_cache(pages, page_tokens, heads, dq, table, dtype=torch.float8_e4m3fn):
+    """A Cache of `pages` pages on the table's device, none written yet."""
+    shape = (int(pages), int(heads), int(page_tokens))
+    row = quan_cache_row_bytes(dq, dtype) // dtype.itemsize
+    keys, values = (torch.empty((*shape, row), dtype=dtype, device=table.device) for _ in range(2))
+    exps = (None, None)
+    if dtype == torch.float8_e4m3fn:
+        exps = tuple(torch.empty(shape, dtype=torch.uint8, device=table.device) for _ in range(2))
+    return Cache(keys, values, *exps, table, int(dq))
+
+
+def _cache(c, device):
+    """struct quan_cache of a Cache."""
+    form = _FORMATS.get(c.keys.dtype)
+    if form is None:
+        raise TypeError(f"unsupported dtype {c.keys.dtype} of a cache; expected float8_e4m3fn, bfloat16 or float32")
+    if c.keys.dim() != 4 or c.values.shape != c.keys.shape or c.values.dtype != c.keys.dtype \
+            or not c.keys.is_contiguous() or not c.values.is_contiguous():
+        raise ValueError("a cache's keys and values must be contiguous [pages, heads, page_tokens, row] tensors alike")
+    pages, heads, page_tokens, row = c.keys.shape
+    size = c.keys.element_size()
+    if not 0 < c.dq <= 32 or row != -(-4 * c.dq * size // 16) * 16 // size:
+        raise ValueError("a cache's rows must hold 4 dq reals up to whole 16 bytes")
+    for t in (c.key_exp, c.value_exp):
+        if (t is None) != (form != QUAN_CACHE_E4M3) or (t is not None and (
+                t.dtype != torch.uint8 or t.shape != c.keys.shape[:3] or not t.is_contiguous())):
+            raise ValueError("an 8-bit cache has key_exp and value_exp, contiguous uint8 [pages, heads, page_tokens]")
+    if c.table.dim() != 2 or c.table.dtype != torch.int32 or not c.table.is_contiguous():
+        raise ValueError("a cache's table must be a contiguous int32 [sequences, pages] tensor")
+    for t in (c.keys, c.values, c.key_exp, c.value_exp, c.table):
+        if t is not None and t.device != device:
+            raise ValueError("a cache must lie on the maps' device")
+    return _PACK_CACHE(c.keys.data_ptr(), c.values.data_ptr(), _ptr(c.key_exp) or 0, _ptr(c.value_exp) or 0,
+                       c.table.data_ptr(), form, pages, page_tokens, heads, c.dq, *c.table.shape)
+
+
+def _ints(name, t, shape, device):
+    """Pointer of a contiguous int32 tensor, None without one."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype != torch.int32 or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name} must be a contiguous int32 {list(shape)} tensor on the maps' device")
+    return t.data_ptr()
+
+
+def _copy_args(cache, k, v, start, first, kv_len):
+    if k.dim() != 5 or v.dim() != 5:
+        raise ValueError("k and v must be [N, 4, C, H, W]")
+    dev, n = k.device, cache.table.shape[0]
+    if v.device != dev:
+        raise ValueError("all tensors must be on k's device")
+    return (_cache(cache, dev), _map_desc(k), _map_desc(v), _ints("first", first, (n + 1,), dev),
+            _ints("start", start, (n,), dev), _ints("kv_len", kv_len, (n,), dev))
+
+
+def quan_cache_write(cache, k, v, start=None, first=None, kv_len=None):
+    """Keys and values of new tokens into a Cache, rounded to its 8 bits or as
+    they are: token j of sequence i goes to position start[i] + j.
+
+    k, v: [N, 4, heads dq, H, W], channel slices of wider maps are taken as they
+    are; a sequence per image, or with first, int32 [sequences + 1], the pixels
+    first[i] .. first[i + 1] - 1 of the one image.  start: int32 [sequences], 0
+    without one.  kv_len: int32 [sequences], positions from kv_len[i] on are left
+    alone (padding)."""
+    lib = load_library()
+    held, kd, vd, first, start, kv_len = _copy_args(cache, k, v, start, first, kv_len)
+    with _on(k.device):
+        rc = lib.quan_cache_write(kd, vd, first, start, kv_len, held, _stream(k.device))
+    if rc:
+        _check(rc)
+
+
+def quan_cache_read(cache, k, v, start=None, first=None, kv_len=None):
+    """Positions start[i] + j of a Cache back into maps k, v, arguments as
+    quan_cache_write's; zeros from kv_len[i] on and where there is no page.
+    Returns (k, v)."""
+    lib = load_library()
+    held, kd, vd, first, start, kv_len = _copy_args(cache, k, v, start, first, kv_len)
+    with _on(k.device):
+        rc = lib.quan_cache_read(held, first, start, kv_len, kd, vd, _stream(k.device))
+    if rc:
+        _check(rc)
+    return k, v
+
+
+def quan_cache_attention(q, cache, kv_len, heads, relpos=None, pos=None, width=None, scale=None, out=None):
+    """Attention of one new token per sequence over the first kv_len (int32
+    [sequences], None: all) positions of a Cache.
+
+    q: [sequences, 4, C, 1, 1], C / heads the cache's dq, heads a multiple of its
+    heads.  relpos: (table, bucket_y, bucket_x) as quan_attention_forward's, for
+    positions that are the pixels of a map `width` wide; pos: int32
+    [sequences, 2], the query's (y, x) there.  scale: 1 / sqrt(4 C / heads) by
+    default.  Returns out, like q."""
+    lib = load_library()
+    if q.dim() != 5:
+        raise ValueError("q must be [N, 4, C, 1, 1]")
+    dev, heads = q.device, int(heads)
+    n, _, c, h, w = q.shape
+    if relpos is not None and width is None:
+        raise ValueError("relpos needs the width of the map whose pixels the positions are")
+    if out is None:
+        out = empty_qmap(n, c, h, w, q.dtype, dev)
+    elif out.dim() != 5 or out.device != dev:
+        raise ValueError("out must be [N, 4, C, 1, 1] on q's device")
+    held, bias = _cache(cache, dev), None if relpos is None else _relpos(relpos, heads, dev)
+    seqs = cache.table.shape[0]
+    if scale is None:
+        scale = 0.5 / math.sqrt(cache.dq)
+    lens, at = _ints("kv_len", kv_len, (seqs,), dev), _ints("pos", pos, (seqs, 2), dev)
+    with _on(dev):
+        rc = lib.quan_cache_attention(_map_desc(q), held, bias, 1 if width is None else int(width), lens, at,
+                                      float(scale), heads, _map_desc(out), _stream(dev))
+    if rc:
+        _check(rc)
+    return out
+
+
+def _packed_args(q, k, v, first, heads, k_first, causal, scale):
+    if q.dim() != 5 or k.dim() != 5 or v.dim() != 5:
+        raise ValueError("q, k and v must be [N, 4, C, H, W]")
+    dev, heads = q.device, int(heads)
+    if k.device != dev or v.device != dev:
+        raise ValueError("all tensors must be on q's device")
+    n = q.shape[0] if first is None else first.numel() - 1
+    if scale is None:
+        scale = 1.0 / math.sqrt(max(1, 4 * (q.shape[2] // heads))) if heads > 0 else 1.0
+    return (_map_desc(q), _map_desc(k), _map_desc(v), _ints("first", first, (n + 1,), dev),
+            _ints("k_first", k_first, (n + 1,), dev), n, int(bool(causal)), float(scale), heads)
+
+
+def quan_packed_attention_forward(q, k, v, first, heads, k_first=None, causal=True, scale=None, out=None, save=False):
+    """Causal attention inside sequences of pixels.
+
+    q: [1, 4, C, H, W] whose pixels first[i] .. first[i + 1] - 1 are sequence i
+    (first: int32 [sequences + 1]), or with first None [N, 4, C, H, W], a
+    sequence per image.  k, v: [.., 4, Ckv, Hk, Wk], their sequences by k_first
+    (None: as first); heads may share keys as in quan_attention_forward.  A
+    sequence's queries are the last of its keys' tokens: query i of lq sees keys j
+    <= i + lk - lq, or all of them with causal=False.  Pixels of no sequence are
+    neither read nor written.  Returns out, or with save (out, stats) for
+    quan_packed_attention_backward."""
+    lib = load_library()
+    args = _packed_args(q, k, v, first, heads, k_first, causal, scale)
+    n, _, c, h, w = q.shape
+    dev = q.device
+    if out is None:
+        out = empty_qmap(n, c, h, w, q.dtype, dev)
+    elif out.dim() != 5 or out.device != dev:
+        raise ValueError("out must be [N, 4, C, H, W] on q's device")
+    stats = torch.empty((args[-1], n * h * w, 2), dtype=torch.float32, device=dev) if save else None
+    with _on(dev):
+        rc = lib.quan_packed_attention_forward(*args, _map_desc(out), _ptr(stats), _stream(dev))
+    if rc:
+        _check(rc)
+    return (out, stats) if save else out
+
+
+def quan_packed_attention_backward(q, k, v, out, stats, dout, first, heads, k_first=None, causal=True, scale=None,
+                                   dq=None, dk=None, dv=None):
+    """Gradients of quan_packed_attention_forward for dL/dout = dout, with what it
+    saved.  dq, dk, dv may be slices of one map.  Returns (dq, dk, dv)."""
+    lib = load_library()
+    args = _packed_args(q, k, v, first, heads, k_first, causal, scale)
+    n, _, _, h, w = q.shape
+    dev = q.device
+    if stats is None or stats.shape != (args[-1], n * h * w, 2) or stats.dtype != torch.float32 \
+            or not stats.is_contiguous():
+        raise ValueError("stats must be the forward's, float32 [heads, N H W, 2]")
+    dq, dk, dv = (_like_map(like) if t is None else t for t, like in ((dq, q), (dk, k), (dv, v)))
+    for t in (out, stats, dout, dq, dk, dv):
+        if t.device != dev:
+            raise ValueError("all tensors must be on q's device")
+    for t in (out, dout, dq, dk, dv):
+        if t.dim() != 5:
+            raise ValueError("out, dout and the gradients must be [N, 4, C, H, W]")
+    with _on(dev):
+        rc = lib.quan_packed_attention_backward(*args, _map_desc(out), stats.data_ptr(), _map_desc(dout), _map_desc(dq),
+                                                _map_desc(dk), _map_desc(dv), _stream(dev))
+    if rc:
+        _check(rc)
+    return dq, dk, dv
 
 
 def quan_last_error() -> str:

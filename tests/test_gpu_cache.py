@@ -1,0 +1,235 @@
+"""A paged cache on the GPU: new tokens in 8 bits or as they are, and back."""
+import numpy as np
+import pytest
+import torch
+
+import sequence_reference as ref
+from parity import say
+from paper_2509_05512_amd import quan
+
+pytestmark = pytest.mark.gpu
+BF, F32, E4M3 = torch.bfloat16, torch.float32, torch.float8_e4m3fn
+DEV = "cuda"
+
+
+def rand_map(seed, n, c, h, w, dtype, spread=0):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn((n, h, w, 4, c), generator=g)
+    if spread:
+        x = x * torch.exp2(torch.randint(-spread, spread + 1, (n, h, w, 1, 1), generator=g).float())
+    return x.to(dtype).to(DEV).permute(0, 3, 4, 1, 2)
+
+
+def ints(v):
+    return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+def make_table(rng, lens, page, extra=2):
+    """Pages in any order, -1 behind the last that a sequence needs."""
+    need = [-(-v // page) for v in lens]
+    pages = sum(need) + extra
+    order, at = rng.permutation(pages), 0
+    table = np.full((len(lens), max(1, max(need))), -1, np.int32)
+    for i, m in enumerate(need):
+        table[i, :m] = order[at:at + m]
+        at += m
+    return ints(table.tolist()), pages
+
+
+def held(cache):
+    """(elements' values [pages, heads, slots, row], bytes or None) on the host."""
+    t = [x.float().cpu().numpy().astype(np.float64) for x in (cache.keys, cache.values)]
+    e = [None if x is None else x.cpu().numpy() for x in (cache.key_exp, cache.value_exp)]
+    return t, e
+
+
+def clear(cache):
+    for t in (cache.keys, cache.values):
+        t.view(torch.uint8).fill_(0x2a)
+    for t in (cache.key_exp, cache.value_exp):
+        if t is not None:
+            t.fill_(7)
+    return cache
+
+
+def expected(cache, rows, table, where):
+    """What the cache must hold: rows [tokens, heads, d] at (sequence, position)
+    or None, elsewhere what clear() put there."""
+    fresh = clear(quan.empty_cache(cache.keys.shape[0], cache.page_tokens, cache.heads, cache.dq, cache.table, cache.keys.dtype))
+    (keys, values), (ke, ve) = held(fresh)
+    table = table.cpu().numpy()
+    for which, (dst, exp) in enumerate(((keys, ke), (values, ve))):
+        for x, at in zip(rows[which], where):
+            if at is None:
+                continue
+            seq, position = at
+            if position < 0 or position >= table.shape[1] * cache.page_tokens:
+                continue
+            page = table[seq, position // cache.page_tokens]
+            if page < 0 or page >= keys.shape[0]:
+                continue
+            slot = position % cache.page_tokens
+            dst[page, :, slot] = 0.0
+            if exp is None:
+                dst[page, :, slot, :x.shape[1]] = x
+            else:
+                dst[page, :, slot, :x.shape[1]], exp[page, :, slot] = ref.quantise(x)
+    return (keys, values), (ke, ve)
+
+
+def same(got, want):
+    for g, w in zip(got[0] + got[1], want[0] + want[1]):
+        if g is not None:
+            assert np.array_equal(g, w, equal_nan=True), int((g != w).sum())
+
+
+FORMS = [(BF, E4M3), (F32, E4M3), (BF, BF), (F32, F32)]
+
+
+@pytest.mark.parametrize("dtype,form", FORMS, ids=["bf16-e4m3", "fp32-e4m3", "bf16", "fp32"])
+@pytest.mark.parametrize("dq,heads,page", [(16, 2, 16), (8, 3, 7), (32, 1, 64), (5, 2, 1), (12, 4, 5), (1, 1, 3), (24, 2, 33)])
+def test_write_and_read(dtype, form, dq, heads, page):
+    """Packed sequences of any length, one of them empty, behind tokens that were
+    there; slices of one map; every byte of the pool looked at."""
+    say(f"cache copy {dtype} {form} dq {dq} heads {heads} page {page}")
+    rng = np.random.default_rng(dq * 100 + page)
+    lens, past = [5, 0, 1, 70, 17], [0, 3, 9, 2, 40]
+    table, pages = make_table(rng, [a + b for a, b in zip(lens, past)], page)
+    cache = clear(quan.empty_cache(pages, page, heads, dq, table, form))
+    c, tokens = heads * dq, sum(lens) + 4  # two tokens before the first sequence, two behind the last
+    kv = rand_map(7, 1, 2 * c, 1, tokens, dtype, spread=6)
+    k, v = kv[:, :, :c], kv[:, :, c:]
+    first = ref.starts(lens) + 2
+    quan.quan_cache_write(cache, k, v, ints(past), first=ints(first.tolist()))
+    rows = [ref.rows_of(t.float().cpu().numpy().astype(np.float64), heads) for t in (k, v)]
+    where = [None] * tokens
+    for i, n in enumerate(lens):
+        for j in range(n):
+            where[first[i] + j] = (i, past[i] + j)
+    want = expected(cache, rows, table, where)
+    same(held(cache), want)
+    back = torch.full_like(kv, 3.0)
+    kb, vb = quan.quan_cache_read(cache, back[:, :, :c], back[:, :, c:], ints(past), first=ints(first.tolist()))
+    for which, got in enumerate((kb, vb)):
+        got = ref.rows_of(got.float().cpu().numpy().astype(np.float64), heads)
+        for t, at in enumerate(where):
+            if at is None:
+                assert np.all(got[t] == 3.0)
+                continue
+            x = rows[which][t]
+            if form == E4M3:
+                y, e = ref.quantise(x)
+                x = y * 2.0 ** (e - 127.0)[:, None]  # (4 bits of fraction: exact in bf16)
+            assert np.array_equal(got[t], x)
+
+
+def test_values_of_all_kinds():
+    """Ties, the largest values and their neighbours, fp32's ends, zeros, infinities
+    and NaN in rows of their own."""
+    say("cache values of all kinds")
+    dq = 8
+    x = np.zeros((64, 4 * dq), np.float32)
+    rng = np.random.default_rng(3)
+    for i in range(20):  # 448 2^e, and what is just above and below
+        big = np.float32(448 * 2.0 ** (i - 10))
+        x[3 * i % 60] = rng.standard_normal(4 * dq) * big / 8
+        x[3 * i % 60, 0] = [big, np.nextafter(big, np.float32(np.inf)), np.nextafter(big, np.float32(0))][i % 3]
+    x[1, :9] = [1.0, 1.0625, 1.1875, 2.0 ** -9, 2.0 ** -10, 1.5 * 2.0 ** -9, 2.5 * 2.0 ** -9, 240, 448]  # ties
+    x[2] = 2.0 ** -149
+    x[4] = np.finfo(np.float32).max
+    x[5, 3] = np.inf
+    x[7, 9] = -np.inf
+    x[8, 31] = np.nan
+    x[10] = -2.0 ** -126
+    x[11] = rng.standard_normal(4 * dq) * 2.0 ** -120
+    t = torch.from_numpy(x.reshape(1, 1, 64, 4, dq)).to(DEV).permute(0, 3, 4, 1, 2)
+    cache = clear(quan.empty_cache(4, 16, 1, dq, ints([[3, 1, 0, 2]])))
+    quan.quan_cache_write(cache, t, t)
+    rows = ref.rows_of(t.cpu().numpy().astype(np.float64), 1)
+    same(held(cache), expected(cache, (rows, rows), cache.table, [(0, j) for j in range(64)]))
+    k, v = quan.quan_cache_read(cache, torch.zeros_like(t), torch.zeros_like(t))
+    y, e = ref.quantise(rows)
+    want = np.where((e == 255)[..., None], np.nan, y * 2.0 ** (e - 127.0)[..., None])
+    for got in (k, v):
+        assert np.array_equal(ref.rows_of(got.cpu().numpy().astype(np.float64), 1), want, equal_nan=True)
+
+
+def test_images_and_padding():
+    """A sequence per image; kv_len keeps padding out; bad pages, positions below 0
+    and beyond the table are dropped and read as zeros."""
+    say("cache images and padding")
+    n, heads, dq, page = 5, 2, 16, 8
+    table = ints([[0, 1, 2], [3, -1, 4], [5, 99, 6], [7, -2147483648, 8], [9, 10, 11]])
+    start, kv_len = [0, 2, 0, -3, 20], [9, 24, 24, 24, 2147483647]
+    for dtype in (BF, F32):
+        cache = clear(quan.empty_cache(12, page, heads, dq, table))
+        kv = rand_map(4, n, 2 * heads * dq, 3, 7, dtype)
+        k, v = kv[:, :, :heads * dq], kv[:, :, heads * dq:]
+        quan.quan_cache_write(cache, k, v, ints(start), kv_len=ints(kv_len))
+        rows = [ref.rows_of(t.float().cpu().numpy().astype(np.float64), heads) for t in (k, v)]
+        where = [(i, start[i] + j) if start[i] + j < kv_len[i] else None for i in range(n) for j in range(21)]
+        same(held(cache), expected(cache, rows, table, where))
+        kb, vb = quan.quan_cache_read(cache, torch.full_like(k, 3.0), torch.full_like(v, 3.0), ints(start), kv_len=ints(kv_len))
+        tab = table.cpu().numpy()
+        for got, x in zip((kb, vb), rows):
+            got = ref.rows_of(got.float().cpu().numpy().astype(np.float64), heads)
+            for t, at in enumerate(where):
+                there = at is not None and 0 <= at[1] < 24 and 0 <= tab[at[0], at[1] // page] < 12
+                y, e = ref.quantise(x[t])
+                assert np.array_equal(got[t], y * 2.0 ** (e - 127.0)[:, None] if there else np.zeros_like(y))
+
+
+@pytest.mark.parametrize("count", [1, 63, 64, 65, 700, 2047, 2048, 5000])
+def test_many_sequences(count):
+    """Single tokens of many sequences, some of them with none."""
+    say(f"cache of {count} sequences")
+    rng = np.random.default_rng(count)
+    lens = rng.integers(0, 3, count).tolist()
+    lens[-1] = 1
+    table = ints(rng.permutation(count)[:, None].tolist())
+    cache = clear(quan.empty_cache(count, 4, 1, 4, table, F32))
+    k = rand_map(1, 1, 4, 1, sum(lens), F32)
+    past = rng.integers(0, 3, count).tolist()
+    quan.quan_cache_write(cache, k, k, ints(past), first=ints(ref.starts(lens).tolist()))
+    rows = ref.rows_of(k.cpu().numpy().astype(np.float64), 1)
+    where = [(i, past[i] + j) for i in range(count) for j in range(lens[i])]
+    same(held(cache), expected(cache, (rows, rows), table, where))
+
+
+def test_sequences_out_of_order():
+    """Values of `first` beyond the map or descending reach no other memory: what is
+    outside the pool's and the maps' own tensors keeps its bytes."""
+    say("cache, sequences out of order")
+    pool = torch.full((3, 8, 1, 8, 16), 0x2a, dtype=torch.uint8, device=DEV)
+    exps = torch.full((3, 8, 1, 8), 7, dtype=torch.uint8, device=DEV)
+    c = quan.Cache(pool[1].view(E4M3), pool[1].clone().view(E4M3), exps[1], exps[1].clone(),
+                   ints([[0, 1], [2, 3], [4, 5]]), 4)
+    room = torch.full((1, 1, 60, 4, 4), 3.0, device=DEV)
+    k = room[:, :, 20:40].permute(0, 3, 4, 1, 2)
+    for first in ([9, 2, 30, 5], [-5, 100, 3, 2147483647], [-2147483648, 7, 7, 20], [21, 22, 23, 24]):
+        quan.quan_cache_write(c, k, k.clone(), first=ints(first))
+        quan.quan_cache_read(c, k, k.clone(), first=ints(first))
+    torch.cuda.synchronize()
+    assert bool((pool[0] == 0x2a).all()) and bool((pool[2] == 0x2a).all())
+    assert bool((exps[0] == 7).all()) and bool((exps[2] == 7).all())
+    assert bool((room[:, :, :20] == 3.0).all()) and bool((room[:, :, 40:] == 3.0).all())
+
+
+def test_unaligned_and_wide_maps():
+    """Slices that begin at any channel, components and pixels of any strides."""
+    say("cache, maps of any strides")
+    heads, dq, tokens = 2, 8, 21
+    table, pages = make_table(np.random.default_rng(0), [tokens], 4)
+    for dtype in (BF, F32):
+        wide = rand_map(2, 1, 37, 1, tokens, dtype)
+        k, v = wide[:, :, 3:3 + 16], wide[:, :, 21:]
+        cache = clear(quan.empty_cache(pages, 4, heads, dq, table))
+        quan.quan_cache_write(cache, k, v)
+        rows = [ref.rows_of(t.float().cpu().numpy().astype(np.float64), heads) for t in (k, v)]
+        same(held(cache), expected(cache, rows, table, [(0, j) for j in range(tokens)]))
+        to = torch.full_like(wide, 3.0)
+        kb, vb = quan.quan_cache_read(cache, to[:, :, 3:19], to[:, :, 21:])
+        for got, x in zip((kb, vb), rows):
+            y, e = ref.quantise(x)
+            assert np.array_equal(ref.rows_of(got.float().cpu().numpy().astype(np.float64), heads), y * 2.0 ** (e - 127.0)[..., None])
+        assert bool((to[:, :, :3] == 3.0).all()) and bool((to[:, :, 19:21] == 3.0).all())

@@ -1,0 +1,199 @@
+"""Causal attention of packed sequences on the GPU, forward and backward."""
+import numpy as np
+import pytest
+import torch
+
+import sequence_reference as ref
+from parity import say
+from paper_2509_05512_amd import quan
+from test_gpu_cache import BF, DEV, F32, ints, rand_map
+
+pytestmark = pytest.mark.gpu
+
+
+def rows(t, heads):
+    return ref.rows_of(t.float().cpu().numpy().astype(np.float64), heads)
+
+
+def step(q, k, v, do, first, heads, **kw):
+    out, stats = quan.quan_packed_attention_forward(q, k, v, first, heads, save=True, **kw)
+    grads = quan.quan_packed_attention_backward(q, k, v, out, stats, do, first, heads, **kw)
+    return (out, stats, *grads)
+
+
+def compare(q, k, v, do, lq, lk, heads, got, what, causal=True, scale=None, q0=0, k0=0):
+    """Against the reference; tokens of no sequence are not looked at."""
+    dq = q.shape[2] // heads
+    kvh = k.shape[2] // dq
+    z, y = slice(q0, q0 + sum(lq)), slice(k0, k0 + sum(lk))
+    want, err = ref.packed(rows(q, heads)[z], rows(k, kvh)[y], rows(v, kvh)[y], lq, lk, causal, scale, rows(do, heads)[z])
+    out, stats, dqs, dks, dvs = got
+    bf = q.dtype == BF
+    ref.check(rows(out, heads)[z], want["out"], err["out"], bf, what + " out")
+    top, total = (stats[:, z, i].double().cpu().numpy().T for i in range(2))
+    with np.errstate(divide="ignore"):
+        lse = np.log(2) * top + np.log(total)
+    there = np.isfinite(want["lse"])
+    assert np.array_equal(np.isfinite(lse), there), what
+    assert np.all(np.abs(lse[there] - want["lse"][there]) <= 1e-4), what
+    ref.check(rows(dqs, heads)[z], want["dq"], err["dq"], bf, what + " dq")
+    ref.check(rows(dks, kvh)[y], want["dk"], err["dk"], bf, what + " dk")
+    ref.check(rows(dvs, kvh)[y], want["dv"], err["dv"], bf, what + " dv")
+
+
+LENS = {
+    "mixed": ([0, 1, 2, 31, 0, 33, 64, 65, 127, 0], None),
+    "long": ([300, 129, 128], None),
+    "one": ([1], None),
+    "past": ([3, 70, 1, 130, 0], [40, 200, 129, 131, 7]),
+    "less": ([70, 5, 200, 3], [3, 0, 150, 3]),
+}
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("lens", LENS)
+@pytest.mark.parametrize("dq,heads,kv_heads", [(16, 4, 2), (8, 3, 3), (32, 2, 1), (5, 2, 2), (12, 8, 1), (1, 1, 1)])
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "all"])
+def test_packed(dtype, lens, dq, heads, kv_heads, causal):
+    say(f"packed {dtype} {lens} dq {dq} heads {heads}/{kv_heads} causal {causal}")
+    lq, lk = LENS[lens]
+    same = lk is None
+    lk = lq if same else lk
+    c, ckv = heads * dq, kv_heads * dq
+    if same:  # slices of one map
+        qkv = rand_map(1, 1, c + 2 * ckv, 1, sum(lq), dtype)
+        q, k, v = qkv[:, :, :c], qkv[:, :, c:c + ckv], qkv[:, :, c + ckv:]
+    else:
+        q = rand_map(1, 1, c, 1, sum(lq), dtype)
+        k, v = (rand_map(s, 1, ckv, 1, max(1, sum(lk)), dtype) for s in (2, 3))
+    do = rand_map(4, 1, c, 1, sum(lq), dtype)
+    kw = dict(k_first=None if same else ints(ref.starts(lk).tolist()), causal=causal)
+    got = step(q, k, v, do, ints(ref.starts(lq).tolist()), heads, **kw)
+    compare(q, k, v, do, lq, lk, heads, got, lens, causal)
+    again = step(q, k, v, do, ints(ref.starts(lq).tolist()), heads, **kw)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+def test_images(dtype):
+    """A sequence per image, pixels in row order; a scale of the caller's."""
+    say(f"packed images {dtype}")
+    n, heads, dq = 3, 2, 16
+    q, k, v, do = (rand_map(s, n, heads * dq, 9, 15, dtype) for s in range(4))
+    got = step(q, k, v, do, None, heads, scale=0.2)
+    compare(q, k, v, do, [135] * n, [135] * n, heads, got, "images", scale=0.2)
+    q, do = (rand_map(s, n, heads * dq, 1, 10, dtype) for s in (5, 6))
+    got = step(q, k, v, do, None, heads)
+    compare(q, k, v, do, [10] * n, [135] * n, heads, got, "images, few queries")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+def test_long_sequences(dtype):
+    """Walks that work-groups share, beside short ones."""
+    say(f"packed, long walks {dtype}")
+    heads, dq = 2, 16
+    for lq, lk in (([130, 3], [2000, 900]), ([1100, 40], [1100, 40])):
+        q, do = (rand_map(s, 1, heads * dq, 1, sum(lq), dtype) for s in (1, 2))
+        k, v = (rand_map(s, 1, dq, 1, sum(lk), dtype) for s in (3, 4))
+        first, k_first = (ints(ref.starts(t).tolist()) for t in (lq, lk))
+        compare(q, k, v, do, lq, lk, heads, step(q, k, v, do, first, heads, k_first=k_first), f"{lq} on {lk}")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("dq", [16, 12])
+def test_tokens_of_no_sequence(dtype, dq):
+    """Before the first and behind the last sequence: NaN there is not read, and
+    what is there in the results stays."""
+    say(f"packed, tokens of no sequence {dtype} {dq}")
+    heads, lens, before, behind = 2, [70, 0, 130], 5, 9
+    total = before + sum(lens) + behind
+    q, k, v, do = (rand_map(s, 1, heads * dq, 1, total, dtype) for s in range(4))
+    for t in (q, k, v, do):
+        t[..., :before] = float("nan")
+        t[..., before + sum(lens):] = float("nan")
+    first = ints((ref.starts(lens) + before).tolist())
+    out, g = (torch.full_like(q, 3.0) for _ in range(2))
+    grads = [torch.full_like(q, 3.0) for _ in range(3)]
+    out, stats = quan.quan_packed_attention_forward(q, k, v, first, heads, out=out, save=True)
+    quan.quan_packed_attention_backward(q, k, v, out, stats, do, first, heads, dq=grads[0], dk=grads[1], dv=grads[2])
+    compare(q, k, v, do, lens, lens, heads, (out, stats, *grads), "inside", q0=before, k0=before)
+    for t in (out, *grads):
+        assert bool((t[..., :before] == 3.0).all()) and bool((t[..., before + sum(lens):] == 3.0).all())
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_masked_infinities_and_nan(dtype, bad):
+    """What a query does not see changes nothing of its result and gradient, nor
+    what a key is not seen by of its gradients: not one bit."""
+    say(f"packed, masked {bad} {dtype}")
+    heads, dq, lens, at = 2, 16, [200, 40], 77
+    q, k, v, do = (rand_map(s, 1, heads * dq, 1, sum(lens), dtype) for s in range(4))
+    first = ints(ref.starts(lens).tolist())
+    clean = step(q, k, v, do, first, heads)
+    for which in range(4):
+        maps = [t.clone(memory_format=torch.preserve_format) for t in (q, k, v, do)]
+        maps[which][0, 1, 3, 0, at] = bad
+        got = step(*maps, first, heads)
+        if which in (1, 2):  # a key or value: later queries see it
+            for i in (0, 2):
+                assert torch.equal(got[i][..., :at], clean[i][..., :at]), (which, i)
+            if which == 2:
+                assert not bool(torch.isfinite(got[0][0, 1, 3, 0, at:200]).any())
+        else:  # a query or its gradient: reaches its own row and the keys before it
+            for i in (0, 2):
+                assert torch.equal(got[i][..., :at], clean[i][..., :at]), (which, i)
+                assert torch.equal(got[i][..., at + 1:], clean[i][..., at + 1:]), (which, i)
+            for i in (3, 4):
+                assert torch.equal(got[i][..., at + 1:], clean[i][..., at + 1:]), (which, i)
+        for i in (0, 2, 3, 4):
+            assert torch.equal(got[i][..., 200:], clean[i][..., 200:]), (which, i)
+
+
+def test_sequences_out_of_order():
+    """Values that descend or lie beyond the map reach no other memory."""
+    say("packed, sequences out of order")
+    heads, dq, total = 2, 8, 300
+    room = torch.full((5, 3 * total, 4, heads * dq), 3.0, dtype=BF, device=DEV)
+    q, k, v, do = (rand_map(s, 1, heads * dq, 1, total, BF) for s in range(4))
+    out, a, b, c = (room[i, total:2 * total][None, None].permute(0, 3, 4, 1, 2) for i in range(4))
+    for first in ([200, 100, 300, 0], [-7, 1000, 3, 2147483647], [-2147483648, 128, 128, 300], [301, 302, 400, 500]):
+        out, stats = quan.quan_packed_attention_forward(q, k, v, ints(first), heads, out=out, save=True)
+        quan.quan_packed_attention_backward(q, k, v, out, stats.zero_(), do, ints(first), heads, k_first=ints(first[::-1]),
+                                            dq=a, dk=b, dv=c)
+    torch.cuda.synchronize()
+    assert bool((room[:, :total] == 3.0).all()) and bool((room[:, 2 * total:] == 3.0).all())
+
+
+@pytest.mark.parametrize("count", [3, 64, 65, 256, 257, 1000])
+def test_many_sequences(count):
+    say(f"packed, {count} sequences")
+    rng = np.random.default_rng(count)
+    lens = rng.integers(0, 9, count).tolist()
+    lens[count // 2] = 140
+    heads, dq = 1, 8
+    q, k, v, do = (rand_map(s, 1, heads * dq, 1, sum(lens), BF) for s in range(4))
+    compare(q, k, v, do, lens, lens, heads, step(q, k, v, do, ints(ref.starts(lens).tolist()), heads), "many")
+
+
+def test_gradients_against_differences():
+    """In fp32, along random directions: central differences of the sum of dout out
+    are off by the third derivative's h^2 / 6 (1e-6 for h = 2^-6, terms of order 1)
+    and by fp32's rounding of the sums, 2^-24 sqrt(terms) / h: 1e-3 of the sums of
+    a hundred products leaves room for both."""
+    say("packed, differences")
+    heads, dq, lens = 2, 5, [9, 21]
+    maps = [rand_map(s, 1, heads * dq, 1, sum(lens), F32) for s in range(4)]
+    first = ints(ref.starts(lens).tolist())
+    grads = step(*maps, first, heads)[2:]
+    h = 2.0 ** -6
+    for i in range(3):
+        way = rand_map(10 + i, 1, heads * dq, 1, sum(lens), F32)
+
+        def at(s):
+            moved = [t + s * h * way if j == i else t for j, t in enumerate(maps[:3])]
+            return (quan.quan_packed_attention_forward(*moved, first, heads).double() * maps[3].double()).sum()
+        slope = float((at(1) - at(-1)) / (2 * h))
+        want = float((grads[i].double() * way.double()).sum())
+        size = float((grads[i].double() * way.double()).abs().sum())
+        assert abs(slope - want) <= 1e-3 * size, (i, slope, want)
