@@ -317,7 +317,7 @@ QUAN_API int quan_cache_attention(const quan_tensor *q, const quan_cache *cache,
         return rc;
     if (!std::isfinite(scale))
         return report(QUAN_ERR_SHAPE, "%s: scale must be finite", fn);
-    if (int64_t(cache->sequences) * heads > kMaxGroups)
+    if (int64_t(cache->sequences) * heads > kMaxLanes / 512)  // (work-groups of 512 lanes)
         return report(QUAN_ERR_UNSUPPORTED, "%s: too many work-groups", fn);
     const Span len_span{"kv_len", kv_len, size_t(cache->sequences) * 4};
     const Span pos_span{"pos", pos, size_t(cache->sequences) * 8};
