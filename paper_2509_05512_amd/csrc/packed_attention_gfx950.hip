@@ -18,8 +18,15 @@ struct Forward {
     PackedCall c;
     AttnMap out;
     float *stats;
-    int blocks;
+    int blocks, splits;
+    float *part, *part_stats;  // [split][head][token][D], [split][head][token][2]; splits > 1
 };
+
+// Keys that a block's queries see, all of them together.
+__device__ __forceinline__ int keys_of(const PackedCall &c, const Tokens &q, const Tokens &k, int at)
+{
+    return c.causal ? min(k.len, min(at + kBlock, q.len) + k.len - q.len) : k.len;
+}
 
 template <typename T, int DQP>
 __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(Forward f)
@@ -36,10 +43,16 @@ __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(Forward f)
     // heads side by side, so that each of 8 (or a divisor) stays on an XCD; the
     // blocks that see most keys first
     const int head = blockIdx.x % c.heads, kv_head = head / (c.heads / c.kv_heads);
-    const Block b = locate(c.qs, f.blocks - 1 - int(blockIdx.x / c.heads), counts);
+    const int split = blockIdx.x / c.heads % f.splits;
+    const Block b = locate(c.qs, f.blocks - 1 - int(blockIdx.x / (c.heads * f.splits)), counts);
     const Tokens qt = tokens_of(c.qs, c.qs.first, b.seq), kt = tokens_of(c.ks, c.ks.first, b.seq);
     if (b.at >= qt.len)
         return;
+    const int all = keys_of(c, qt, kt, b.at);
+    const Walk walk = walk_of((kt.len + KT - 1) / KT, (all + KT - 1) / KT, f.splits);
+    if (split >= walk.count)
+        return;
+    const int begin = split * walk.per * KT, end = min(all, begin + walk.per * KT);
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
     const int half_at = KT / 2 * half;  // the lane's half of a tile
@@ -47,30 +60,34 @@ __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(Forward f)
     const bool q_here = query < qt.len;
     // keys that a query sees: those below query + shift
     const int shift = c.causal ? kt.len - qt.len + 1 : 0;
-    const int end = c.causal ? min(kt.len, min(b.at + kBlock, qt.len) - 1 + shift) : kt.len;
     const int wave_end = b.at + 32 * wave >= qt.len ? 0 : c.causal ? min(end, b.at + 32 * wave + 31 + shift) : end;
     const int seen = c.causal ? query + shift : kt.len;
 
     const WholeMap<T, DQP> qm(c.q, qt.img, head), km(c.k, kt.img, kv_head), vm(c.v, kt.img, kv_head);
     Tile k_tile, v_tile;
-    if (end > 0) {
-        k_tile.fetch(km, kt.at, kt.at + end);
-        v_tile.fetch(vm, kt.at, kt.at + end);
+    if (begin < end) {
+        k_tile.fetch(km, kt.at + begin, kt.at + end);
+        v_tile.fetch(vm, kt.at + begin, kt.at + end);
     }
+    // scores are taken with the scale's magnitude, its sign goes to q (0: q is 0)
+    const float sign = c.scale < 0.0f ? -1.0f : c.scale > 0.0f ? 1.0f : 0.0f;
+    const float scale = c.scale != 0.0f ? fabsf(c.scale) * kLog2e : 1.0f;
     frag q[DP / 16];
 #pragma unroll
-    for (int i = 0; i < DP / 16; ++i)
+    for (int i = 0; i < DP / 16; ++i) {
         q[i] = qm.load(qt.at + query, 16 * i + 8 * half, q_here);
+        if (sign != 1.0f)
+            q[i] = to_frag<T>(to_f32(q[i]) * sign);
+    }
 
     f32x16 o[DP / 32];
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i)
         o[i] = 0.0f;
     float top = -INFINITY, sum = 0.0f;
-    const float scale = c.scale * kLog2e;
 
     int buf = 0;
-    for (int j0 = 0; j0 < end; j0 += KT, buf ^= 1) {
+    for (int j0 = begin; j0 < end; j0 += KT, buf ^= 1) {
         T *kb = k_lds + buf * Tile::kElems, *vb = v_lds + buf * Tile::kElems;
         // whether a query of the block does not see all of the tile
         const bool edge = c.causal && j0 + KT > b.at + shift;
@@ -93,9 +110,6 @@ __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(Forward f)
             for (int i = 0; i < DP / 16; ++i)
                 s[sub] = mma(row_frag<T, DP>(kb, sub, i), q[i], s[sub]);
         }
-#pragma unroll
-        for (int sub = 0; sub < SUBS; ++sub)
-            s[sub] *= scale;
         // tiles that reach past what the wave's first query sees
         if (j0 + KT > min(end, c.causal ? b.at + 32 * wave + shift : end)) {
 #pragma unroll
@@ -106,9 +120,9 @@ __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(Forward f)
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                t = fmaxf(t, s[sub][r]);
-        t = half_max(t);
+            for (int r = 0; r < 16; r += 2)
+                t = fmaxf(t, fmaxf(s[sub][r], s[sub][r + 1]));
+        t = half_max(t) * scale;
         if (__any(t > top)) {
             const float now = fmaxf(top, t);
             const float back = exp2_fast(top - (now == -INFINITY ? 0.0f : now));
@@ -123,7 +137,7 @@ __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(Forward f)
         for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                s[sub][r] = exp2_fast(s[sub][r] - m);
+                s[sub][r] = exp2_fast(fmaf(s[sub][r], scale, -m));
                 sum += s[sub][r];
             }
 #pragma unroll
@@ -143,6 +157,16 @@ __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(Forward f)
     }
     sum = half_sum(sum);
 
+    const int64_t row = head * c.q_tokens() + int64_t(qt.img) * c.qs.tokens + qt.at + query;
+    if (walk.count > 1) {
+        const int64_t at = split * (c.heads * c.q_tokens()) + row;
+        store_part<DP>(f.part + at * DP, o, q_here);
+        if (half == 0 && q_here) {
+            f.part_stats[2 * at] = top;
+            f.part_stats[2 * at + 1] = sum;
+        }
+        return;
+    }
     const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
     const HeadMap<T, DQP> om(f.out, qt.img, head, c.dq);
 #pragma unroll
@@ -151,17 +175,70 @@ __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(Forward f)
         om.store(qt.at + query, i, half, o[i], q_here);
     }
     if (f.stats != nullptr && half == 0 && q_here) {
-        float *st = f.stats + 2 * (head * c.q_tokens() + int64_t(qt.img) * c.qs.tokens + qt.at + query);
-        st[0] = top == -INFINITY ? 0.0f : top;
-        st[1] = sum;
+        f.stats[2 * row] = top == -INFINITY ? 0.0f : top;
+        f.stats[2 * row + 1] = sum;
     }
+}
+
+// The results of work-groups that shared a block's keys, joined: D / 4 lanes for a
+// query, 4 reals each.
+template <typename T, int DQP> __global__ void __launch_bounds__(kThreads) packed_join_kernel(Forward f)
+{
+    constexpr int DP = 4 * DQP, KT = Elem<T>::kTile, kLanes = DP / 4, kGroups = join_groups(DP);
+    __shared__ int counts[kWaves];
+    const PackedCall &c = f.c;
+    const int head = blockIdx.x % c.heads, id = blockIdx.x / c.heads;
+    const Block b = locate(c.qs, id / kGroups, counts);
+    const Tokens qt = tokens_of(c.qs, c.qs.first, b.seq), kt = tokens_of(c.ks, c.ks.first, b.seq);
+    const int query = b.at + id % kGroups * (kThreads / kLanes) + threadIdx.x / kLanes, d = 4 * (threadIdx.x % kLanes);
+    if (query >= qt.len)
+        return;
+    const Walk walk = walk_of((kt.len + KT - 1) / KT, (keys_of(c, qt, kt, b.at) + KT - 1) / KT, f.splits);
+    if (walk.count == 1)
+        return;
+    const int64_t row = head * c.q_tokens() + int64_t(qt.img) * c.qs.tokens + qt.at + query;
+    float top = -INFINITY, sum = 0.0f;
+    f32x4 o = 0.0f;
+#pragma unroll 4
+    for (int s = 0; s < walk.count; ++s) {
+        const int64_t at = s * (c.heads * c.q_tokens()) + row;
+        const float t = f.part_stats[2 * at], l = f.part_stats[2 * at + 1];
+        const f32x4 v = *reinterpret_cast<const f32x4 *>(f.part + at * DP + d);
+        const float now = fmaxf(top, t), m = now == -INFINITY ? 0.0f : now;
+        const float back = exp2_fast(top - m), w = exp2_fast(t - m);
+        top = now;
+        sum = sum * back + l * w;
+        o = o * back + v * w;
+    }
+    o *= sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+    const HeadMap<T, DQP> om(f.out, qt.img, head, c.dq);
+    store_quad(om.at(qt.at + query, d), o, om.valid(d, 4), om.vec);
+    if (f.stats != nullptr && d == 0) {
+        f.stats[2 * row] = top == -INFINITY ? 0.0f : top;
+        f.stats[2 * row + 1] = sum;
+    }
+}
+
+// Work-groups that share a block's walk where there are few blocks.
+int forward_splits(const PackedCall &c, DType dt, bool may_split)
+{
+    const int64_t groups = packed_blocks(c.qs) * c.heads;
+    const int tiles = (c.ks.tokens + (dt == DType::BF16 ? 63 : 31)) / (dt == DType::BF16 ? 64 : 32);
+    if (!may_split || groups >= 512)
+        return 1;
+    return int(std::max<int64_t>(1, std::min<int64_t>((1024 + groups - 1) / groups, tiles / 4)));
 }
 
 template <typename T, int DQP> hipError_t launch(const Forward &f, hipStream_t s)
 {
     constexpr int kTile = Elem<T>::kTile;
     const size_t lds = size_t(4) * kTile * Lds<T, 4 * DQP>::kRow * sizeof(T);
-    packed_forward_kernel<T, DQP><<<unsigned(int64_t(f.blocks) * f.c.heads), kThreads, lds, s>>>(f);
+    const unsigned groups = unsigned(int64_t(f.blocks) * f.c.heads);
+    packed_forward_kernel<T, DQP><<<groups * f.splits, kThreads, lds, s>>>(f);
+    if (hipError_t e = hipGetLastError())
+        return e;
+    if (f.splits > 1)
+        packed_join_kernel<T, DQP><<<groups * join_groups(4 * DQP), kThreads, 0, s>>>(f);
     return hipGetLastError();
 }
 template <typename T> hipError_t launch_dq(const Forward &f, hipStream_t s)
@@ -204,12 +281,13 @@ size_t packed_forward_work_bytes(const PackedCall &c, DType dt)
     return packed_copy_bytes(c.q_tokens(), c.heads, c.dq, dt) + 2 * packed_copy_bytes(c.k_tokens(), c.kv_heads, c.dq, dt);
 }
 
-size_t packed_forward_extra_bytes(const PackedCall &, DType)
+size_t packed_forward_extra_bytes(const PackedCall &c, DType dt)
 {
-    return 0;
+    const int splits = forward_splits(c, dt, true);
+    return splits == 1 ? 0 : size_t(splits) * c.heads * c.q_tokens() * (4 * padded_dq(c.dq) + 2) * sizeof(float);
 }
 
-hipError_t packed_forward_run(const PackedCall &c, DType dt, const AttnMap &out, float *stats, void *work, void *,
+hipError_t packed_forward_run(const PackedCall &c, DType dt, const AttnMap &out, float *stats, void *work, void *extra,
                               hipStream_t s)
 {
     Forward f;
@@ -217,6 +295,9 @@ hipError_t packed_forward_run(const PackedCall &c, DType dt, const AttnMap &out,
     f.out = out;
     f.stats = stats;
     f.blocks = int(packed_blocks(c.qs));
+    f.splits = forward_splits(c, dt, extra != nullptr);
+    f.part = static_cast<float *>(extra);
+    f.part_stats = f.part + (f.splits > 1 ? size_t(f.splits) * c.heads * c.q_tokens() * 4 * padded_dq(c.dq) : 0);
     if (work != nullptr) {
         AttnPack pack;
         pack.maps = 0;

@@ -10,6 +10,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <utility>
 
 #include "packed_tile.h"
 
@@ -21,8 +22,25 @@ struct Backward {
     AttnMap out, dout, dq, dk, dv;
     const float *stats;
     float *delta;  // [heads][q_tokens]
-    int q_blocks, k_blocks;
+    int q_blocks, k_blocks, q_splits, k_splits;
+    float *part_q, *part_k, *part_v;  // [split][head][token][D] where walks are shared
 };
+
+// Tiles of keys that a block's queries see.
+__device__ __forceinline__ int key_tiles(const PackedCall &c, const Tokens &q, const Tokens &k, int at, int tile)
+{
+    const int keys = c.causal ? min(k.len, min(at + kBlock, q.len) + k.len - q.len) : k.len;
+    return (keys + tile - 1) / tile;
+}
+// The first tile of queries that sees one of a block's keys, and how many from it on.
+struct Span {
+    int from, count;
+};
+__device__ __forceinline__ Span query_tiles(const PackedCall &c, const Tokens &q, const Tokens &k, int at, int tile)
+{
+    const int from = c.causal ? max(0, at - (k.len - q.len)) / tile : 0;
+    return {from, max(0, (q.len + tile - 1) / tile - from)};
+}
 
 template <typename T, int DQP>
 __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) packed_dq_kernel(Backward f)
@@ -37,24 +55,29 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) packed_dq_kernel(
 
     const PackedCall &c = f.c;
     const int head = blockIdx.x % c.heads, kv_head = head / (c.heads / c.kv_heads);
-    const Block b = locate(c.qs, f.q_blocks - 1 - int(blockIdx.x / c.heads), counts);
+    const int split = blockIdx.x / c.heads % f.q_splits;
+    const Block b = locate(c.qs, f.q_blocks - 1 - int(blockIdx.x / (c.heads * f.q_splits)), counts);
     const Tokens qt = tokens_of(c.qs, c.qs.first, b.seq), kt = tokens_of(c.ks, c.ks.first, b.seq);
     if (b.at >= qt.len)
+        return;
+    const Walk walk = walk_of((kt.len + KT - 1) / KT, key_tiles(c, qt, kt, b.at, KT), f.q_splits);
+    if (split >= walk.count)
         return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
     const int half_at = KT / 2 * half;  // the lane's half of a tile
     const int query = b.at + 32 * wave + (lane & 31);
     const bool q_here = query < qt.len;
     const int shift = c.causal ? kt.len - qt.len + 1 : 0;
-    const int end = c.causal ? min(kt.len, min(b.at + kBlock, qt.len) - 1 + shift) : kt.len;
+    const int all = c.causal ? min(kt.len, min(b.at + kBlock, qt.len) - 1 + shift) : kt.len;
+    const int begin = split * walk.per * KT, end = min(all, begin + walk.per * KT);
     const int wave_end = b.at + 32 * wave >= qt.len ? 0 : c.causal ? min(end, b.at + 32 * wave + 31 + shift) : end;
     const int seen = min(c.causal ? query + shift : kt.len, end);
 
     const WholeMap<T, DQP> qm(c.q, qt.img, head), km(c.k, kt.img, kv_head), vm(c.v, kt.img, kv_head);
     Tile k_tile, v_tile;
-    if (end > 0) {
-        k_tile.fetch(km, kt.at, kt.at + end);
-        v_tile.fetch(vm, kt.at, kt.at + end);
+    if (begin < end) {
+        k_tile.fetch(km, kt.at + begin, kt.at + end);
+        v_tile.fetch(vm, kt.at + begin, kt.at + end);
     }
     const int64_t row = head * c.q_tokens() + int64_t(qt.img) * c.qs.tokens + qt.at + query;
     frag q[DP / 16], go[DP / 16];
@@ -72,7 +95,7 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) packed_dq_kernel(
                 delta = fmaf(w[e], o[e], delta);
         }
         delta = half_sum(delta);
-        if (q_here && half == 0)
+        if (q_here && half == 0 && split == 0)
             f.delta[row] = delta;
     }
     // P = 2^(s - top) inv; rows without a key, and none, have P = 0
@@ -88,7 +111,7 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) packed_dq_kernel(
     for (int i = 0; i < DP / 32; ++i)
         dq[i] = 0.0f;
     int buf = 0;
-    for (int j0 = 0; j0 < end; j0 += KT, buf ^= 1) {
+    for (int j0 = begin; j0 < end; j0 += KT, buf ^= 1) {
         T *kb = k_lds + buf * Tile::kElems, *vb = v_lds + buf * Tile::kElems;
         // whether a query of the block does not see all of the tile
         const bool edge = c.causal && j0 + KT > b.at + shift;
@@ -133,6 +156,10 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) packed_dq_kernel(
             const float p = exp2_fast(fmaf(row_dot(km, kt.at + j, q), scale, -top));
             row_add(dq, km, kt.at + j, p * fmaf(row_dot(vm, kt.at + j, go), inv, minus), j < seen);
         }
+    }
+    if (walk.count > 1) {
+        store_part<DP>(f.part_q + (split * (c.heads * c.q_tokens()) + row) * DP, dq, q_here);
+        return;
     }
     const HeadMap<T, DQP> om(f.dq, qt.img, head, c.dq);
 #pragma unroll
@@ -179,12 +206,18 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) packed_dkv_kernel
     T *q_lds = reinterpret_cast<T *>(rows + 6 * QT), *g_lds = q_lds + 2 * Tile::kElems;
 
     const PackedCall &c = f.c;
-    const int group = c.heads / c.kv_heads, kv_head = blockIdx.x % c.kv_heads;
+    const int group = c.heads / c.kv_heads, kv_head = blockIdx.x % c.kv_heads, split = blockIdx.x / c.kv_heads % f.k_splits;
     // (of causal sequences the first blocks of keys are seen by most queries)
-    const Block b = locate(c.ks, int(blockIdx.x / c.kv_heads), counts);
+    const Block b = locate(c.ks, int(blockIdx.x / (c.kv_heads * f.k_splits)), counts);
     const Tokens qt = tokens_of(c.qs, c.qs.first, b.seq), kt = tokens_of(c.ks, c.ks.first, b.seq);
     if (b.at >= kt.len)
         return;
+    // the walk: tiles of queries, head by head
+    const Span tiles = query_tiles(c, qt, kt, b.at, QT);
+    const Walk walk = walk_of(group * ((qt.len + QT - 1) / QT), group * tiles.count, f.k_splits);
+    if (split >= walk.count)
+        return;
+    const int first = split * walk.per, last = min(group * tiles.count, first + walk.per);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
     const int half_at = QT / 2 * half;  // the lane's half of a tile
     const int key = b.at + 32 * wave + (lane & 31);
@@ -206,9 +239,6 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) packed_dkv_kernel
         dv[i] = 0.0f;
     }
     const float scale = c.scale * kLog2e;
-    // tiles of queries, from the first that sees one of the block's keys
-    const int from = c.causal ? max(0, b.at - back) / QT : 0, tiles = max(0, (qt.len + QT - 1) / QT - from);
-    const int last = group * tiles;
     Tile q_tile, g_tile;
     float row_top = 0.0f, row_sum = 0.0f, row_delta = 0.0f;  // of thread t < QT's query of a tile
     auto fetch = [&](int head, int i0) {
@@ -222,11 +252,14 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) packed_dkv_kernel
             row_delta = f.delta[row];
         }
     };
-    int head = kv_head * group, tile = from;
-    if (last > 0)
+    int head = kv_head * group, tile = tiles.from;
+    if (first < last) {
+        head += first / tiles.count;
+        tile += first % tiles.count;
         fetch(head, tile * QT);
+    }
     int buf = 0;
-    for (int item = 0; item < last; ++item, buf ^= 1) {
+    for (int item = first; item < last; ++item, buf ^= 1) {
         const int i0 = tile * QT;
         T *qb = q_lds + buf * Tile::kElems, *gb = g_lds + buf * Tile::kElems;
         float *rw = rows + buf * 3 * QT;
@@ -244,8 +277,8 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) packed_dkv_kernel
         }
         __syncthreads();
         const int this_head = head;
-        if (++tile == from + tiles) {
-            tile = from;
+        if (++tile == tiles.from + tiles.count) {
+            tile = tiles.from;
             ++head;
         }
         if (item + 1 < last)
@@ -306,6 +339,13 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) packed_dkv_kernel
             row_add(dk, qm, token, p * (row_dot(gm, token, v) + rw[2 * QT + at]), sees);
         }
     }
+    if (walk.count > 1) {
+        const int64_t row = kv_head * c.k_tokens() + int64_t(kt.img) * c.ks.tokens + kt.at + key;
+        const int64_t at = (split * (c.kv_heads * c.k_tokens()) + row) * DP;
+        store_part<DP>(f.part_k + at, dk, k_here);
+        store_part<DP>(f.part_v + at, dv, k_here);
+        return;
+    }
     const HeadMap<T, DQP> okm(f.dk, kt.img, kv_head, c.dq), ovm(f.dv, kt.img, kv_head, c.dq);
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i) {
@@ -315,15 +355,59 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) packed_dkv_kernel
     }
 }
 
+// The results of work-groups that shared a block, added up in order: D / 4 lanes for
+// a token, 4 reals each.  First the blocks of queries, then those of keys.
+template <typename T, int DQP> __global__ void __launch_bounds__(kThreads) packed_sum_kernel(Backward f, int of_queries)
+{
+    constexpr int DP = 4 * DQP, TILE = Elem<T>::kTile, kLanes = DP / 4, kGroups = join_groups(DP);
+    __shared__ int counts[kWaves];
+    const PackedCall &c = f.c;
+    const bool keys = int(blockIdx.x) >= of_queries;
+    const int heads = keys ? c.kv_heads : c.heads, group = c.heads / c.kv_heads;
+    const int head = (blockIdx.x - (keys ? of_queries : 0)) % heads, id = (blockIdx.x - (keys ? of_queries : 0)) / heads;
+    const Sequences &mine = keys ? c.ks : c.qs;
+    const Block b = locate(mine, id / kGroups, counts);
+    const Tokens qt = tokens_of(c.qs, c.qs.first, b.seq), kt = tokens_of(c.ks, c.ks.first, b.seq), t = keys ? kt : qt;
+    const int token = b.at + id % kGroups * (kThreads / kLanes) + threadIdx.x / kLanes, d = 4 * (threadIdx.x % kLanes);
+    if (token >= t.len)
+        return;
+    const Walk walk = keys ? walk_of(group * ((qt.len + TILE - 1) / TILE), group * query_tiles(c, qt, kt, b.at, TILE).count, f.k_splits)
+                           : walk_of((kt.len + TILE - 1) / TILE, key_tiles(c, qt, kt, b.at, TILE), f.q_splits);
+    if (walk.count == 1)
+        return;
+    const int64_t all = heads * (keys ? c.k_tokens() : c.q_tokens());
+    const int64_t row = head * (keys ? c.k_tokens() : c.q_tokens()) + int64_t(t.img) * mine.tokens + t.at + token;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        if (which == 1 && !keys)
+            break;
+        const float *p = (keys ? which == 0 ? f.part_k : f.part_v : f.part_q) + row * DP + d;
+        f32x4 s = 0.0f;
+#pragma unroll 4
+        for (int i = 0; i < walk.count; ++i)
+            s += *reinterpret_cast<const f32x4 *>(p + i * all * DP);
+        if (which == 0)
+            s *= c.scale;
+        const HeadMap<T, DQP> m(keys ? which == 0 ? f.dk : f.dv : f.dq, t.img, head, c.dq);
+        store_quad(m.at(t.at + token, d), s, m.valid(d, 4), m.vec);
+    }
+}
+
 template <typename T, int DQP> hipError_t launch(const Backward &f, hipStream_t s)
 {
     constexpr int kTile = Elem<T>::kTile;
     const size_t lds = size_t(4) * kTile * Lds<T, 4 * DQP>::kRow * sizeof(T);
-    packed_dq_kernel<T, DQP><<<unsigned(int64_t(f.q_blocks) * f.c.heads), kThreads, lds, s>>>(f);
+    const unsigned q_groups = unsigned(int64_t(f.q_blocks) * f.c.heads), k_groups = unsigned(int64_t(f.k_blocks) * f.c.kv_heads);
+    packed_dq_kernel<T, DQP><<<q_groups * f.q_splits, kThreads, lds, s>>>(f);
     if (hipError_t e = hipGetLastError())
         return e;
-    packed_dkv_kernel<T, DQP>
-        <<<unsigned(int64_t(f.k_blocks) * f.c.kv_heads), kThreads, lds + 6 * kTile * sizeof(float), s>>>(f);
+    packed_dkv_kernel<T, DQP><<<k_groups * f.k_splits, kThreads, lds + 6 * kTile * sizeof(float), s>>>(f);
+    if (hipError_t e = hipGetLastError())
+        return e;
+    const unsigned of_queries = f.q_splits > 1 ? q_groups * join_groups(4 * DQP) : 0;
+    const unsigned of_keys = f.k_splits > 1 ? k_groups * join_groups(4 * DQP) : 0;
+    if (of_queries + of_keys > 0)
+        packed_sum_kernel<T, DQP><<<of_queries + of_keys, kThreads, 0, s>>>(f, int(of_queries));
     return hipGetLastError();
 }
 template <typename T> hipError_t launch_dq(const Backward &f, hipStream_t s)
@@ -342,16 +426,45 @@ bool copies(const PackedCall &c, const PackedGradients &g)
 {
     return !(c.q.vec && c.k.vec && c.v.vec && g.out.vec && g.dout.vec) || padded_dq(c.dq) != c.dq;
 }
+size_t round_up(size_t bytes)
+{
+    return (bytes + 255) & ~size_t(255);
+}
 size_t delta_bytes(const PackedCall &c)
 {
-    return (size_t(c.heads) * c.q_tokens() * sizeof(float) + 255) & ~size_t(255);
+    return round_up(size_t(c.heads) * c.q_tokens() * sizeof(float));
+}
+
+// Work-groups that share a walk of at most `tiles` where there are few walks.
+int splits_of(int64_t groups, int64_t tiles)
+{
+    if (groups >= 1024)
+        return 1;
+    return int(std::max<int64_t>(1, std::min<int64_t>((1024 + groups - 1) / groups, tiles / 4)));
+}
+struct Plan {
+    int q_splits, k_splits;
+    size_t part_q, part_k;
+};
+Plan plan(const PackedCall &c, DType dt)
+{
+    const int tile = dt == DType::BF16 ? 64 : 32, dp = 4 * padded_dq(c.dq);
+    Plan p{};
+    p.q_splits = splits_of(packed_blocks(c.qs) * c.heads, (c.ks.tokens + tile - 1) / tile);
+    p.k_splits = splits_of(packed_blocks(c.ks) * c.kv_heads, int64_t(c.heads / c.kv_heads) * ((c.qs.tokens + tile - 1) / tile));
+    if (p.q_splits > 1)
+        p.part_q = round_up(size_t(p.q_splits) * c.heads * c.q_tokens() * dp * sizeof(float));
+    if (p.k_splits > 1)
+        p.part_k = round_up(size_t(p.k_splits) * c.kv_heads * c.k_tokens() * dp * sizeof(float));
+    return p;
 }
 
 }  // namespace
 
 size_t packed_backward_work_bytes(const PackedCall &c, DType dt, const PackedGradients &g)
 {
-    size_t bytes = delta_bytes(c);
+    const Plan p = plan(c, dt);
+    size_t bytes = delta_bytes(c) + p.part_q + 2 * p.part_k;
     if (copies(c, g))
         bytes += 3 * packed_copy_bytes(c.q_tokens(), c.heads, c.dq, dt) +
                  2 * packed_copy_bytes(c.k_tokens(), c.kv_heads, c.dq, dt);
@@ -373,6 +486,13 @@ hipError_t packed_backward_run(const PackedCall &c, DType dt, const PackedGradie
     unsigned char *at = static_cast<unsigned char *>(work);
     f.delta = reinterpret_cast<float *>(at);
     at += delta_bytes(c);
+    const Plan p = plan(c, dt);
+    f.q_splits = p.q_splits;
+    f.k_splits = p.k_splits;
+    for (auto [part, bytes] : {std::pair{&f.part_q, p.part_q}, {&f.part_k, p.part_k}, {&f.part_v, p.part_k}}) {
+        *part = reinterpret_cast<float *>(at);
+        at += bytes;
+    }
     if (copies(c, g)) {
         AttnPack pack;
         pack.maps = 0;

@@ -46,6 +46,19 @@ __device__ __forceinline__ Block locate(const Sequences &s, int id, int *lds)
     return {seq, block < 0 || block > s.tokens / kBlock ? s.tokens : block * kBlock};
 }
 
+// A block's walk over `mine` tiles, dealt out to work-groups: `count` of them take
+// `per` tiles each, the last the rest, where the sequence's longest walk has `longest`
+// tiles and `splits` work-groups, so that all take about as many.  (Two tiles at
+// least.)
+struct Walk {
+    int per, count;
+};
+__device__ __forceinline__ Walk walk_of(int longest, int mine, int splits)
+{
+    const int per = max(2, (longest + splits - 1) / splits);
+    return {per, max(1, (mine + per - 1) / per)};
+}
+
 // Infinities and NaN in rows of a tile that not all of the work-group's lanes see:
 // a product's masked factor 0 would make NaN of them.  Such rows (rare, and looked
 // for in the tiles at a walk's edge alone) are zeroed on their way to LDS and added
@@ -121,6 +134,23 @@ __device__ __forceinline__ void row_add(f32x16 (&acc)[DQP / 8], const WholeMap<T
                 acc[i][4 * g + t] = sees ? fmaf(by, float(p[t]), acc[i][4 * g + t]) : acc[i][4 * g + t];
         }
 }
+
+// A D x 32 tile of accumulators, transposed, to a row of fp32.
+template <int DP> __device__ __forceinline__ void store_part(float *dst, const f32x16 (&v)[DP / 32], bool here)
+{
+    if (!here)
+        return;
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32x4 t = {v[i][4 * g], v[i][4 * g + 1], v[i][4 * g + 2], v[i][4 * g + 3]};
+            *reinterpret_cast<f32x4 *>(dst + 32 * i + 8 * g + 4 * ((threadIdx.x & 63) >> 5)) = t;
+        }
+}
+
+// Work-groups of a launch that joins: each takes 1024 / D rows of a block.
+constexpr int join_groups(int dp) { return kBlock * dp / 1024; }
 
 }  // namespace
 }  // namespace quan
