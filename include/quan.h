@@ -874,9 +874,9 @@ QUAN_API int quan_cache_attention(const quan_tensor *q, const quan_cache *cache,
  *              above), of `sequences` each; k_first NULL with q_first: the
  *              same as q_first, the maps being of one size.  Both NULL: the
  *              images, and sequences is N.
- *   stats      NULL, or fp32 [heads][N*Hq*Wq][2] for the backward pass: each
- *              query's maximum in units of log 2 and the sum of 2^(score -
- *              maximum).
+ *   stats      NULL, or fp32 [heads][N*Hq*Wq][2] for the backward pass: for each
+ *              query a number m in units of log 2, within 8 of its largest score
+ *              (0 for a query without a key), and the sum of 2^(score - m).
  *
  * Probabilities of bf16 maps are rounded to bf16 before they meet v; everything
  * else is fp32.  out may overlap no input; it may be a slice of a map that holds

@@ -14,6 +14,8 @@
 namespace quan {
 namespace {
 
+constexpr float kAhead = 8.0f;  // probabilities of 2^8 at most
+
 struct Forward {
     PackedCall c;
     AttnMap out;
@@ -22,21 +24,22 @@ struct Forward {
     float *part, *part_stats;  // [split][head][token][D], [split][head][token][2]; splits > 1
 };
 
-// Keys that a block's queries see, all of them together.
-__device__ __forceinline__ int keys_of(const PackedCall &c, const Tokens &q, const Tokens &k, int at)
+// Keys that the queries of a block of `size` see, all of them together.
+__device__ __forceinline__ int keys_of(const PackedCall &c, const Tokens &q, const Tokens &k, int at, int size)
 {
-    return c.causal ? min(k.len, min(at + kBlock, q.len) + k.len - q.len) : k.len;
+    return c.causal ? min(k.len, min(at + size, q.len) + k.len - q.len) : k.len;
 }
 
-template <typename T, int DQP>
+// QN: sets of 32 queries that a wave holds.
+template <typename T, int DQP, int QN>
 __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(Forward f)
 {
     constexpr int DP = 4 * DQP;
     typedef Stage<T, DP, kThreads> Tile;
     typedef typename Elem<T>::frag frag;
-    constexpr int KT = Tile::kTokens, SUBS = KT / 32;
+    constexpr int KT = Tile::kTokens, SUBS = KT / 32, SIZE = kBlock * QN;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
-    __shared__ int counts[kWaves], flags[2 * KT];
+    __shared__ int flags[2 * kWaves];
     T *k_lds = reinterpret_cast<T *>(lds_raw), *v_lds = k_lds + 2 * Tile::kElems;
 
     const PackedCall &c = f.c;
@@ -44,11 +47,11 @@ __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(Forward f)
     // blocks that see most keys first
     const int head = blockIdx.x % c.heads, kv_head = head / (c.heads / c.kv_heads);
     const int split = blockIdx.x / c.heads % f.splits;
-    const Block b = locate(c.qs, f.blocks - 1 - int(blockIdx.x / (c.heads * f.splits)), counts);
+    const Block b = locate_longest<SIZE>(c.qs, int(blockIdx.x / (c.heads * f.splits)), false);
     const Tokens qt = tokens_of(c.qs, c.qs.first, b.seq), kt = tokens_of(c.ks, c.ks.first, b.seq);
     if (b.at >= qt.len)
         return;
-    const int all = keys_of(c, qt, kt, b.at);
+    const int all = keys_of(c, qt, kt, b.at, SIZE);
     const Walk walk = walk_of((kt.len + KT - 1) / KT, (all + KT - 1) / KT, f.splits);
     if (split >= walk.count)
         return;
@@ -56,12 +59,10 @@ __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(Forward f)
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
     const int half_at = KT / 2 * half;  // the lane's half of a tile
-    const int query = b.at + 32 * wave + (lane & 31);
-    const bool q_here = query < qt.len;
+    const int wave_at = b.at + 32 * QN * wave, query = wave_at + (lane & 31);  // the first of the lane's queries
     // keys that a query sees: those below query + shift
     const int shift = c.causal ? kt.len - qt.len + 1 : 0;
-    const int wave_end = b.at + 32 * wave >= qt.len ? 0 : c.causal ? min(end, b.at + 32 * wave + 31 + shift) : end;
-    const int seen = c.causal ? query + shift : kt.len;
+    const int wave_end = wave_at >= qt.len ? 0 : c.causal ? min(end, wave_at + 32 * QN - 1 + shift) : end;
 
     const WholeMap<T, DQP> qm(c.q, qt.img, head), km(c.k, kt.img, kv_head), vm(c.v, kt.img, kv_head);
     Tile k_tile, v_tile;
@@ -72,27 +73,35 @@ __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(Forward f)
     // scores are taken with the scale's magnitude, its sign goes to q (0: q is 0)
     const float sign = c.scale < 0.0f ? -1.0f : c.scale > 0.0f ? 1.0f : 0.0f;
     const float scale = c.scale != 0.0f ? fabsf(c.scale) * kLog2e : 1.0f;
-    frag q[DP / 16];
+    frag q[QN][DP / 16];
 #pragma unroll
-    for (int i = 0; i < DP / 16; ++i) {
-        q[i] = qm.load(qt.at + query, 16 * i + 8 * half, q_here);
-        if (sign != 1.0f)
-            q[i] = to_frag<T>(to_f32(q[i]) * sign);
+    for (int n = 0; n < QN; ++n)
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) {
+            q[n][i] = qm.load(qt.at + query + 32 * n, 16 * i + 8 * half, query + 32 * n < qt.len);
+            if (sign != 1.0f)
+                q[n][i] = to_frag<T>(to_f32(q[n][i]) * sign);
+        }
+
+    f32x16 o[QN][DP / 32];
+    float base[QN], ahead[QN], sum[QN];
+#pragma unroll
+    for (int n = 0; n < QN; ++n) {
+#pragma unroll
+        for (int i = 0; i < DP / 32; ++i)
+            o[n][i] = 0.0f;
+        base[n] = sum[n] = 0.0f;
+        ahead[n] = -INFINITY;
     }
 
-    f32x16 o[DP / 32];
-#pragma unroll
-    for (int i = 0; i < DP / 32; ++i)
-        o[i] = 0.0f;
-    float top = -INFINITY, sum = 0.0f;
-
+    // tiles from here on are not seen by all of the block's queries
+    const int edge = c.causal ? max(0, b.at + shift) / KT * KT : all;
+    bool left = false;
     int buf = 0;
     for (int j0 = begin; j0 < end; j0 += KT, buf ^= 1) {
         T *kb = k_lds + buf * Tile::kElems, *vb = v_lds + buf * Tile::kElems;
-        // whether a query of the block does not see all of the tile
-        const bool edge = c.causal && j0 + KT > b.at + shift;
-        if (edge)
-            zero_not_finite(v_tile, v_tile, flags + buf * KT);
+        if (j0 >= edge)
+            flag_wave(flags + buf * kWaves, staged_not_finite(v_tile));
         k_tile.put(kb);
         v_tile.put(vb);
         __syncthreads();
@@ -100,83 +109,134 @@ __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(Forward f)
             k_tile.fetch(km, kt.at + j0 + KT, kt.at + end);
             v_tile.fetch(vm, kt.at + j0 + KT, kt.at + end);
         }
+        if (j0 >= edge && flagged<kWaves>(flags + buf * kWaves)) {
+            left = true;
+            continue;
+        }
         if (j0 >= wave_end)
             continue;  // (none of the wave's queries sees the tile)
-        f32x16 s[SUBS];
+        f32x16 s[QN][SUBS];
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub) {
-            s[sub] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < DP / 16; ++i)
-                s[sub] = mma(row_frag<T, DP>(kb, sub, i), q[i], s[sub]);
+            for (int n = 0; n < QN; ++n)
+                s[n][sub] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < DP / 16; ++i) {
+                const frag row = row_frag<T, DP>(kb, sub, i);
+#pragma unroll
+                for (int n = 0; n < QN; ++n)
+                    s[n][sub] = mma(row, q[n][i], s[n][sub]);
+            }
         }
-        // tiles that reach past what the wave's first query sees
-        if (j0 + KT > min(end, c.causal ? b.at + 32 * wave + shift : end)) {
+#pragma unroll
+        for (int n = 0; n < QN; ++n) {
+            // tiles that reach past what the first of the queries sees
+            if (j0 + KT > min(end, c.causal ? wave_at + 32 * n + shift : end)) {
+                const int seen = c.causal ? min(query + 32 * n + shift, end) : end;
+#pragma unroll
+                for (int sub = 0; sub < SUBS; ++sub)
+                    clear_behind(s[n][sub], seen - j0 - half_at, sub, -INFINITY);
+            }
+            // in units of log 2 from `base`, which follows the row's maximum where that
+            // is kAhead above it (and first of all)
+            float most = -INFINITY;
 #pragma unroll
             for (int sub = 0; sub < SUBS; ++sub)
-                clear_behind(s[sub], min(seen, end) - j0 - half_at, sub, -INFINITY);
-        }
-        float t = s[0][0];
 #pragma unroll
-        for (int sub = 0; sub < SUBS; ++sub)
+                for (int r = 0; r < 16; r += 2) {
+                    s[n][sub][r] = fmaf(s[n][sub][r], scale, -base[n]);
+                    s[n][sub][r + 1] = fmaf(s[n][sub][r + 1], scale, -base[n]);
+                    most = fmaxf(most, fmaxf(s[n][sub][r], s[n][sub][r + 1]));
+                }
+            most = half_max(most);
+            if (__any(most > ahead[n])) {
+                const float up = most > ahead[n] ? most : 0.0f;
+                const float back = ahead[n] == -INFINITY ? 0.0f : exp2_fast(-up);  // (nothing before)
+                base[n] += up;
+                ahead[n] = most > ahead[n] ? kAhead : ahead[n];
+                sum[n] *= back;
 #pragma unroll
-            for (int r = 0; r < 16; r += 2)
-                t = fmaxf(t, fmaxf(s[sub][r], s[sub][r + 1]));
-        t = half_max(t) * scale;
-        if (__any(t > top)) {
-            const float now = fmaxf(top, t);
-            const float back = exp2_fast(top - (now == -INFINITY ? 0.0f : now));
-            top = now;
-            sum *= back;
+                for (int i = 0; i < DP / 32; ++i)
+                    o[n][i] *= back;
 #pragma unroll
-            for (int i = 0; i < DP / 32; ++i)
-                o[i] *= back;
-        }
-        const float m = top == -INFINITY ? 0.0f : top;
-#pragma unroll
-        for (int sub = 0; sub < SUBS; ++sub)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[sub][r] = exp2_fast(fmaf(s[sub][r], scale, -m));
-                sum += s[sub][r];
+                for (int sub = 0; sub < SUBS; ++sub)
+                    s[n][sub] -= up;
             }
+#pragma unroll
+            for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[n][sub][r] = exp2_fast(s[n][sub][r]);
+                    sum[n] += s[n][sub][r];
+                }
+        }
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
-                const frag p = acc_frag<T>(s[sub], st);
+                frag p[QN];
 #pragma unroll
-                for (int i = 0; i < DP / 32; ++i)
-                    o[i] = mma(col_frag<DP>(vb, sub, st, i), p, o[i]);
+                for (int n = 0; n < QN; ++n)
+                    p[n] = acc_frag<T>(s[n][sub], st);
+#pragma unroll
+                for (int i = 0; i < DP / 32; ++i) {
+                    const frag column = col_frag<DP>(vb, sub, st, i);
+#pragma unroll
+                    for (int n = 0; n < QN; ++n)
+                        o[n][i] = mma(column, p[n], o[n][i]);
+                }
             }
-        for (auto bad = edge ? flagged(flags + buf * KT, KT) : 0; bad != 0; bad &= bad - 1) {
-            const int j = j0 + __builtin_ctzll(bad);
-            const float p = exp2_fast(row_dot(km, kt.at + j, q) * scale - m);
-            row_add(o, vm, kt.at + j, p, j < seen);
-        }
     }
-    sum = half_sum(sum);
-
-    const int64_t row = head * c.q_tokens() + int64_t(qt.img) * c.qs.tokens + qt.at + query;
-    if (walk.count > 1) {
-        const int64_t at = split * (c.heads * c.q_tokens()) + row;
-        store_part<DP>(f.part + at * DP, o, q_here);
-        if (half == 0 && q_here) {
-            f.part_stats[2 * at] = top;
-            f.part_stats[2 * at + 1] = sum;
+#pragma unroll
+    for (int n = 0; n < QN; ++n)
+        sum[n] = half_sum(sum[n]);
+    if (left)
+        for (int j0 = max(begin, edge); j0 < end; j0 += KT) {
+            if (!rows_not_finite(vm, kt.at + j0, kt.at + min(j0 + KT, end)))
+                continue;
+            for (int j = j0; j < min(j0 + KT, end); ++j)
+#pragma unroll
+                for (int n = 0; n < QN; ++n) {
+                    const bool sees = j < query + 32 * n + shift;
+                    const float t = row_dot(km, kt.at + j, q[n]) * scale;
+                    const bool up = sees && t > base[n] + ahead[n];
+                    const float back = !up ? 1.0f : ahead[n] == -INFINITY ? 0.0f : exp2_fast(base[n] - t);
+                    base[n] = up ? t : base[n];
+                    ahead[n] = up ? kAhead : ahead[n];
+                    const float p = exp2_fast(t - base[n]);
+                    sum[n] = sees ? fmaf(sum[n], back, p) : sum[n];
+#pragma unroll
+                    for (int i = 0; i < DP / 32; ++i)
+                        o[n][i] *= back;
+                    row_add(o[n], vm, kt.at + j, p, sees);
+                }
         }
-        return;
-    }
-    const float inv = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
     const HeadMap<T, DQP> om(f.out, qt.img, head, c.dq);
 #pragma unroll
-    for (int i = 0; i < DP / 32; ++i) {
-        o[i] *= inv;
-        om.store(qt.at + query, i, half, o[i], q_here);
-    }
-    if (f.stats != nullptr && half == 0 && q_here) {
-        f.stats[2 * row] = top == -INFINITY ? 0.0f : top;
-        f.stats[2 * row + 1] = sum;
+    for (int n = 0; n < QN; ++n) {
+        const int token = qt.at + query + 32 * n;
+        const bool here = query + 32 * n < qt.len;
+        const int64_t row = head * c.q_tokens() + int64_t(qt.img) * c.qs.tokens + token;
+        if (walk.count > 1) {
+            const int64_t at = split * (c.heads * c.q_tokens()) + row;
+            store_part<DP>(f.part + at * DP, o[n], here);
+            if (half == 0 && here) {
+                f.part_stats[2 * at] = ahead[n] == -INFINITY ? -INFINITY : base[n];
+                f.part_stats[2 * at + 1] = sum[n];
+            }
+            continue;
+        }
+        const float inv = sum[n] > 0.0f || sum[n] != sum[n] ? 1.0f / sum[n] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < DP / 32; ++i) {
+            o[n][i] *= inv;
+            om.store(token, i, half, o[n][i], here);
+        }
+        if (f.stats != nullptr && half == 0 && here) {
+            f.stats[2 * row] = base[n];
+            f.stats[2 * row + 1] = sum[n];
+        }
     }
 }
 
@@ -193,7 +253,7 @@ template <typename T, int DQP> __global__ void __launch_bounds__(kThreads) packe
     const int query = b.at + id % kGroups * (kThreads / kLanes) + threadIdx.x / kLanes, d = 4 * (threadIdx.x % kLanes);
     if (query >= qt.len)
         return;
-    const Walk walk = walk_of((kt.len + KT - 1) / KT, (keys_of(c, qt, kt, b.at) + KT - 1) / KT, f.splits);
+    const Walk walk = walk_of((kt.len + KT - 1) / KT, (keys_of(c, qt, kt, b.at, kBlock) + KT - 1) / KT, f.splits);
     if (walk.count == 1)
         return;
     const int64_t row = head * c.q_tokens() + int64_t(qt.img) * c.qs.tokens + qt.at + query;
@@ -226,15 +286,25 @@ int forward_splits(const PackedCall &c, DType dt, bool may_split)
     const int tiles = (c.ks.tokens + (dt == DType::BF16 ? 63 : 31)) / (dt == DType::BF16 ? 64 : 32);
     if (!may_split || groups >= 512)
         return 1;
-    return int(std::max<int64_t>(1, std::min<int64_t>((1024 + groups - 1) / groups, tiles / 4)));
+    return int(std::max<int64_t>(1, std::min<int64_t>((512 + groups - 1) / groups, tiles / 4)));
 }
 
-template <typename T, int DQP> hipError_t launch(const Forward &f, hipStream_t s)
+template <typename T, int DQP> hipError_t launch(Forward f, hipStream_t s)
 {
     constexpr int kTile = Elem<T>::kTile;
     const size_t lds = size_t(4) * kTile * Lds<T, 4 * DQP>::kRow * sizeof(T);
+    // blocks twice as large where there are enough of them
+    constexpr bool kWide = sizeof(T) == 2 && DQP <= 16;
+    if constexpr (kWide) {
+        const int64_t wide = packed_blocks(f.c.qs, 2 * kBlock);
+        if (f.splits == 1 && wide * f.c.heads >= 512) {
+            f.blocks = int(wide);
+            packed_forward_kernel<T, DQP, 2><<<unsigned(wide * f.c.heads), kThreads, lds, s>>>(f);
+            return hipGetLastError();
+        }
+    }
     const unsigned groups = unsigned(int64_t(f.blocks) * f.c.heads);
-    packed_forward_kernel<T, DQP><<<groups * f.splits, kThreads, lds, s>>>(f);
+    packed_forward_kernel<T, DQP, 1><<<groups * f.splits, kThreads, lds, s>>>(f);
     if (hipError_t e = hipGetLastError())
         return e;
     if (f.splits > 1)

@@ -43,20 +43,20 @@ __device__ __forceinline__ Span query_tiles(const PackedCall &c, const Tokens &q
 }
 
 template <typename T, int DQP>
-__global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) packed_dq_kernel(Backward f)
+__global__ void __launch_bounds__(kThreads, 2) packed_dq_kernel(Backward f)
 {
     constexpr int DP = 4 * DQP;
     typedef Stage<T, DP, kThreads> Tile;
     typedef typename Elem<T>::frag frag;
     constexpr int KT = Tile::kTokens, SUBS = KT / 32;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
-    __shared__ int counts[kWaves], flags[2 * KT];
+    __shared__ int flags[2 * kWaves];
     T *k_lds = reinterpret_cast<T *>(lds_raw), *v_lds = k_lds + 2 * Tile::kElems;
 
     const PackedCall &c = f.c;
     const int head = blockIdx.x % c.heads, kv_head = head / (c.heads / c.kv_heads);
     const int split = blockIdx.x / c.heads % f.q_splits;
-    const Block b = locate(c.qs, f.q_blocks - 1 - int(blockIdx.x / (c.heads * f.q_splits)), counts);
+    const Block b = locate_longest<kBlock>(c.qs, int(blockIdx.x / (c.heads * f.q_splits)), false);
     const Tokens qt = tokens_of(c.qs, c.qs.first, b.seq), kt = tokens_of(c.ks, c.ks.first, b.seq);
     if (b.at >= qt.len)
         return;
@@ -110,13 +110,14 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) packed_dq_kernel(
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i)
         dq[i] = 0.0f;
+    // tiles from here on are not seen by all of the block's queries
+    const int edge = c.causal ? max(0, b.at + shift) / KT * KT : all;
+    bool left = false;
     int buf = 0;
     for (int j0 = begin; j0 < end; j0 += KT, buf ^= 1) {
         T *kb = k_lds + buf * Tile::kElems, *vb = v_lds + buf * Tile::kElems;
-        // whether a query of the block does not see all of the tile
-        const bool edge = c.causal && j0 + KT > b.at + shift;
-        if (edge)
-            zero_not_finite(k_tile, k_tile, flags + buf * KT);
+        if (j0 >= edge)
+            flag_wave(flags + buf * kWaves, staged_not_finite(k_tile));
         k_tile.put(kb);
         v_tile.put(vb);
         __syncthreads();
@@ -124,9 +125,12 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) packed_dq_kernel(
             k_tile.fetch(km, kt.at + j0 + KT, kt.at + end);
             v_tile.fetch(vm, kt.at + j0 + KT, kt.at + end);
         }
+        if (j0 >= edge && flagged<kWaves>(flags + buf * kWaves)) {
+            left = true;
+            continue;
+        }
         if (j0 >= wave_end)
             continue;  // (none of the wave's queries sees the tile)
-        const auto bad = edge ? flagged(flags + buf * KT, KT) : 0;
         const bool whole = j0 + KT <= min(end, c.causal ? b.at + 32 * wave + shift : end);
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub) {
@@ -141,8 +145,6 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) packed_dq_kernel(
                 s[r] = exp2_fast(fmaf(s[r], scale, -top)) * fmaf(dp[r], inv, minus);
             if (!whole)
                 clear_behind(s, seen - j0 - half_at, sub, 0.0f);
-            if (bad != 0)
-                clear_flagged<KT>(s, bad, sub);
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
                 const frag p = acc_frag<T>(s, st);
@@ -151,12 +153,16 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 3 : 1) packed_dq_kernel(
                     dq[i] = mma(col_frag<DP>(kb, sub, st, i), p, dq[i]);
             }
         }
-        for (auto rest = bad; rest != 0; rest &= rest - 1) {
-            const int j = j0 + __builtin_ctzll(rest);
-            const float p = exp2_fast(fmaf(row_dot(km, kt.at + j, q), scale, -top));
-            row_add(dq, km, kt.at + j, p * fmaf(row_dot(vm, kt.at + j, go), inv, minus), j < seen);
-        }
     }
+    if (left)
+        for (int j0 = max(begin, edge); j0 < end; j0 += KT) {
+            if (!rows_not_finite(km, kt.at + j0, kt.at + min(j0 + KT, end)))
+                continue;
+            for (int j = j0; j < min(j0 + KT, end); ++j) {
+                const float p = exp2_fast(fmaf(row_dot(km, kt.at + j, q), scale, -top));
+                row_add(dq, km, kt.at + j, p * fmaf(row_dot(vm, kt.at + j, go), inv, minus), j < seen);
+            }
+        }
     if (walk.count > 1) {
         store_part<DP>(f.part_q + (split * (c.heads * c.q_tokens()) + row) * DP, dq, q_here);
         return;
@@ -193,22 +199,24 @@ __device__ __forceinline__ void clear_before(f32x16 &s, int from, int sub, float
 }
 
 // The launch of the keys' side: lanes hold keys, registers queries.
-template <typename T, int DQP>
-__global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) packed_dkv_kernel(Backward f)
+// With 8 waves two take each 32 keys, half of every tile's queries each, and their
+// sums meet in LDS at the end: accumulators of 128 reals leave room for no more.
+template <typename T, int DQP, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, 2) packed_dkv_kernel(Backward f)
 {
     constexpr int DP = 4 * DQP;
-    typedef Stage<T, DP, kThreads> Tile;
+    typedef Stage<T, DP, 64 * WAVES> Tile;
     typedef typename Elem<T>::frag frag;
-    constexpr int QT = Tile::kTokens, SUBS = QT / 32;
+    constexpr int QT = Tile::kTokens, SUBS = QT * kWaves / (32 * WAVES);  // parts of a tile that a wave takes
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
-    __shared__ int counts[kWaves], flags[2 * QT];
+    __shared__ int flags[2 * WAVES];
     float *rows = reinterpret_cast<float *>(lds_raw);  // [2][top, inv, -delta][QT]
     T *q_lds = reinterpret_cast<T *>(rows + 6 * QT), *g_lds = q_lds + 2 * Tile::kElems;
 
     const PackedCall &c = f.c;
     const int group = c.heads / c.kv_heads, kv_head = blockIdx.x % c.kv_heads, split = blockIdx.x / c.kv_heads % f.k_splits;
     // (of causal sequences the first blocks of keys are seen by most queries)
-    const Block b = locate(c.ks, int(blockIdx.x / (c.kv_heads * f.k_splits)), counts);
+    const Block b = locate_longest<kBlock>(c.ks, int(blockIdx.x / (c.kv_heads * f.k_splits)), true);
     const Tokens qt = tokens_of(c.qs, c.qs.first, b.seq), kt = tokens_of(c.ks, c.ks.first, b.seq);
     if (b.at >= kt.len)
         return;
@@ -218,8 +226,9 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) packed_dkv_kernel
     if (split >= walk.count)
         return;
     const int first = split * walk.per, last = min(group * tiles.count, first + walk.per);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = (threadIdx.x >> 6) % kWaves, half = lane >> 5;
     const int half_at = QT / 2 * half;  // the lane's half of a tile
+    const int sub0 = threadIdx.x >> 6 >= kWaves;  // the first of the wave's parts
     const int key = b.at + 32 * wave + (lane & 31);
     const bool k_here = key < kt.len;
     // the first query that sees a key: key - back
@@ -258,15 +267,15 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) packed_dkv_kernel
         tile += first % tiles.count;
         fetch(head, tile * QT);
     }
+    bool left = false;
     int buf = 0;
     for (int item = first; item < last; ++item, buf ^= 1) {
         const int i0 = tile * QT;
         T *qb = q_lds + buf * Tile::kElems, *gb = g_lds + buf * Tile::kElems;
         float *rw = rows + buf * 3 * QT;
-        // whether a key of the block is not seen by all of the tile
-        const bool edge = c.causal && i0 < b.at + kBlock - 1 - back;
+        const bool edge = c.causal && i0 < b.at + kBlock - 1 - back;  // (a key is not seen by all of the tile)
         if (edge)
-            zero_not_finite(q_tile, g_tile, flags + buf * QT);
+            flag_wave(flags + buf * WAVES, staged_not_finite(q_tile) || staged_not_finite(g_tile));
         q_tile.put(qb);
         g_tile.put(gb);
         if (threadIdx.x < QT) {
@@ -276,13 +285,16 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) packed_dkv_kernel
             rw[2 * QT + threadIdx.x] = empty ? 0.0f : -row_delta;
         }
         __syncthreads();
-        const int this_head = head;
         if (++tile == tiles.from + tiles.count) {
             tile = tiles.from;
             ++head;
         }
         if (item + 1 < last)
             fetch(head, tile * QT);
+        if (edge && flagged<WAVES>(flags + buf * WAVES)) {
+            left = true;
+            continue;
+        }
         // (a wave whose keys are not there, or that no query of the tile sees)
         if (b.at + 32 * wave >= kt.len || (c.causal && i0 + QT <= b.at + 32 * wave - back))
             continue;
@@ -290,32 +302,27 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) packed_dkv_kernel
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub) {
             s[sub] = 0.0f;
-            dp[sub] = row_values(rw + 2 * QT, half_at, sub);  // dP - delta starts from -delta
+            dp[sub] = row_values(rw + 2 * QT, half_at, sub0 + sub);  // dP - delta starts from -delta
         }
 #pragma unroll
         for (int i = 0; i < DP / 16; ++i)
 #pragma unroll
             for (int sub = 0; sub < SUBS; ++sub) {
-                s[sub] = mma(row_frag<T, DP>(qb, sub, i), k[i], s[sub]);
-                dp[sub] = mma(row_frag<T, DP>(gb, sub, i), v[i], dp[sub]);
+                s[sub] = mma(row_frag<T, DP>(qb, sub0 + sub, i), k[i], s[sub]);
+                dp[sub] = mma(row_frag<T, DP>(gb, sub0 + sub, i), v[i], dp[sub]);
             }
-        const auto bad = edge ? flagged(flags + buf * QT, QT) : 0;
         const bool whole = !c.causal || i0 >= b.at + 32 * wave + 31 - back;
 #pragma unroll
         for (int sub = 0; sub < SUBS; ++sub) {
-            const f32x16 top = row_values(rw, half_at, sub), inv = row_values(rw + QT, half_at, sub);
+            const f32x16 top = row_values(rw, half_at, sub0 + sub), inv = row_values(rw + QT, half_at, sub0 + sub);
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 s[sub][r] = exp2_fast(fmaf(s[sub][r], scale, -top[r])) * inv[r];
                 dp[sub][r] *= s[sub][r];
             }
             if (!whole) {
-                clear_before(s[sub], key - back - i0 - half_at, sub, 0.0f);
-                clear_before(dp[sub], key - back - i0 - half_at, sub, 0.0f);
-            }
-            if (bad != 0) {
-                clear_flagged<QT>(s[sub], bad, sub);
-                clear_flagged<QT>(dp[sub], bad, sub);
+                clear_before(s[sub], key - back - i0 - half_at - 16 * sub0, sub, 0.0f);
+                clear_before(dp[sub], key - back - i0 - half_at - 16 * sub0, sub, 0.0f);
             }
         }
 #pragma unroll
@@ -325,19 +332,53 @@ __global__ void __launch_bounds__(kThreads, DQP <= 16 ? 2 : 1) packed_dkv_kernel
                 const frag p = acc_frag<T>(s[sub], st), ds = acc_frag<T>(dp[sub], st);
 #pragma unroll
                 for (int i = 0; i < DP / 32; ++i) {
-                    dv[i] = mma(col_frag<DP>(gb, sub, st, i), p, dv[i]);
-                    dk[i] = mma(col_frag<DP>(qb, sub, st, i), ds, dk[i]);
+                    dv[i] = mma(col_frag<DP>(gb, sub0 + sub, st, i), p, dv[i]);
+                    dk[i] = mma(col_frag<DP>(qb, sub0 + sub, st, i), ds, dk[i]);
                 }
             }
-        for (auto rest = bad; rest != 0; rest &= rest - 1) {
-            const int at = __builtin_ctzll(rest);
-            const WholeMap<T, DQP> qm(c.q, qt.img, this_head), gm(f.dout, qt.img, this_head);
-            const int64_t token = qt.at + i0 + at;
-            const float p = exp2_fast(fmaf(row_dot(qm, token, k), scale, -rw[at])) * rw[QT + at];
-            const bool sees = i0 + at >= key - back;
-            row_add(dv, gm, token, p, sees);
-            row_add(dk, qm, token, p * (row_dot(gm, token, v) + rw[2 * QT + at]), sees);
+    }
+    if (left)
+        for (int item = first; item < last; ++item) {
+            const int h = kv_head * group + item / tiles.count, i0 = (tiles.from + item % tiles.count) * QT;
+            const WholeMap<T, DQP> qm(c.q, qt.img, h), gm(f.dout, qt.img, h);
+            const int end = min(i0 + QT, qt.len);
+            if (i0 >= b.at + kBlock - 1 - back || (!rows_not_finite(qm, qt.at + i0, qt.at + end) &&
+                                                   !rows_not_finite(gm, qt.at + i0, qt.at + end)))
+                continue;
+            for (int i = i0 + sub0; i < end; i += WAVES / kWaves) {
+                const int64_t row = h * c.q_tokens() + int64_t(qt.img) * c.qs.tokens + qt.at + i;
+                const float sum = f.stats[2 * row + 1], inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+                const float top = sum == 0.0f ? INFINITY : f.stats[2 * row], delta = sum == 0.0f ? 0.0f : f.delta[row];
+                const float p = exp2_fast(fmaf(row_dot(qm, qt.at + i, k), scale, -top)) * inv;
+                const bool sees = i >= key - back;
+                row_add(dv, gm, qt.at + i, p, sees);
+                row_add(dk, qm, qt.at + i, p * (row_dot(gm, qt.at + i, v) - delta), sees);
+            }
         }
+    if constexpr (WAVES > kWaves) {
+        // the second wave's sums to the first
+        static_assert(4 * Tile::kElems * sizeof(T) >= kWaves * 32 * DP * sizeof(float), "the tiles' room holds them");
+        float *sums = reinterpret_cast<float *>(q_lds) + wave * 32 * DP + lane;
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            f32x16(&x)[DP / 32] = which == 0 ? dk : dv;
+            __syncthreads();
+            if (sub0 > 0)
+#pragma unroll
+                for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        sums[(16 * i + r) * 64] = x[i][r];
+            __syncthreads();
+            if (sub0 == 0)
+#pragma unroll
+                for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        x[i][r] += sums[(16 * i + r) * 64];
+        }
+        if (sub0 > 0)
+            return;
     }
     if (walk.count > 1) {
         const int64_t row = kv_head * c.k_tokens() + int64_t(kt.img) * c.ks.tokens + kt.at + key;
@@ -401,7 +442,9 @@ template <typename T, int DQP> hipError_t launch(const Backward &f, hipStream_t 
     packed_dq_kernel<T, DQP><<<q_groups * f.q_splits, kThreads, lds, s>>>(f);
     if (hipError_t e = hipGetLastError())
         return e;
-    packed_dkv_kernel<T, DQP><<<k_groups * f.k_splits, kThreads, lds + 6 * kTile * sizeof(float), s>>>(f);
+    constexpr int kDkvWaves = sizeof(T) == 2 && DQP == 32 ? 8 : 4;
+    packed_dkv_kernel<T, DQP, kDkvWaves>
+        <<<k_groups * f.k_splits, 64 * kDkvWaves, lds + 6 * kTile * sizeof(float), s>>>(f);
     if (hipError_t e = hipGetLastError())
         return e;
     const unsigned of_queries = f.q_splits > 1 ? q_groups * join_groups(4 * DQP) : 0;

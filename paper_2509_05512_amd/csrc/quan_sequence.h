@@ -86,11 +86,12 @@ hipError_t packed_backward_run(const PackedCall &c, DType dt, const PackedGradie
 // bytes of a copy, and one more map of a launch, which `m` is afterwards.
 size_t packed_copy_bytes(int64_t tokens, int heads, int dq, DType dt);
 void packed_copy_add(AttnPack &pack, AttnMap &m, int images, int tokens, int heads, int dq, DType dt, unsigned char *&at);
-// Blocks of 128 tokens that the sequences have at most (see locate() in
+// Blocks of `size` tokens that the sequences have at most (see locate() in
 // packed_tile.h).
-inline int64_t packed_blocks(const Sequences &s)
+inline int64_t packed_blocks(const Sequences &s, int size = 128)
 {
-    return s.first != nullptr ? int64_t(s.tokens) / 128 + s.count : int64_t(s.count) * ((int64_t(s.tokens) + 127) / 128);
+    return s.first != nullptr ? int64_t(s.tokens) / size + s.count
+                              : int64_t(s.count) * ((int64_t(s.tokens) + size - 1) / size);
 }
 
 }  // namespace quan

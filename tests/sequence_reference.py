@@ -126,7 +126,7 @@ def packed(q, k, v, lq, lk, causal=True, scale=None, dout=None):
             dp = go @ vh.T
             ds = p * (dp - (p * dp).sum(1, keepdims=True))
             pe = p * (np.abs(go) * U * (np.abs(out) + B)).sum(1, keepdims=True)
-            off = scale * (U * np.abs(ds) + pe)
+            off = abs(scale) * (U * np.abs(ds) + pe)
             terms = p * (np.abs(go) @ np.abs(vh).T + (np.abs(go) * B).sum(1, keepdims=True))
             res["dq"][a:a + nq, h] = scale * ds @ kh
             res["dk"][b:b + nk, g] += scale * ds.T @ qh
@@ -134,8 +134,8 @@ def packed(q, k, v, lq, lk, causal=True, scale=None, dout=None):
             err["dq"][a:a + nq, h] = off @ np.abs(kh)
             err["dk"][b:b + nk, g] += off.T @ np.abs(qh)
             err["dv"][b:b + nk, g] += U * p.T @ np.abs(go)
-            size["dq"] = max(size["dq"], float((scale * terms @ np.abs(kh)).max()))
-            terms_k["dk"][b:b + nk, g] += scale * terms.T @ np.abs(qh)
+            size["dq"] = max(size["dq"], float((abs(scale) * terms @ np.abs(kh)).max()))
+            terms_k["dk"][b:b + nk, g] += abs(scale) * terms.T @ np.abs(qh)
             terms_k["dv"][b:b + nk, g] += p.T @ np.abs(go)
     for m in ("dq", "dk", "dv"):
         if m in res:
