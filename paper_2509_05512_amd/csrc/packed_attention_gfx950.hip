@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(Forward f)
         const int64_t row = head * c.q_tokens() + int64_t(qt.img) * c.qs.tokens + token;
         if (walk.count > 1) {
             const int64_t at = split * (c.heads * c.q_tokens()) + row;
-            store_part<DP>(f.part + at * DP, o[n], here);
+            store_part<DP / 32>(f.part + at * DP, o[n], here);
             if (half == 0 && here) {
                 f.part_stats[2 * at] = ahead[n] == -INFINITY ? -INFINITY : base[n];
                 f.part_stats[2 * at + 1] = sum[n];

@@ -42,15 +42,21 @@ __device__ __forceinline__ Span query_tiles(const PackedCall &c, const Tokens &q
     return {from, max(0, (q.len + tile - 1) / tile - from)};
 }
 
-template <typename T, int DQP>
-__global__ void __launch_bounds__(kThreads, 2) packed_dq_kernel(Backward f)
+// Heads of more than 64 bf16 reals have two waves for 32 tokens, each with one of the
+// two parts of every tile, so that what a wave holds fits in half of a SIMD's
+// registers; what they make of their parts they exchange through LDS.
+template <typename T, int DQP> constexpr int kPair = sizeof(T) == 2 && DQP > 16 ? 2 : 1;
+
+template <typename T, int DQP, int PAIR = kPair<T, DQP>>
+__global__ void __launch_bounds__(64 * kWaves * PAIR, DQP <= 16 || PAIR == 2 ? 2 : 1) packed_dq_kernel(Backward f)
 {
-    constexpr int DP = 4 * DQP;
-    typedef Stage<T, DP, kThreads> Tile;
+    constexpr int DP = 4 * DQP, WAVES = kWaves * PAIR;
+    typedef Stage<T, DP, 64 * WAVES> Tile;
     typedef typename Elem<T>::frag frag;
-    constexpr int KT = Tile::kTokens, SUBS = KT / 32;
+    constexpr int KT = Tile::kTokens, SUBS = KT / 32 / PAIR, MINE = DP / 32 / PAIR;  // parts, and sums' tiles, of a wave
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
-    __shared__ int flags[2 * kWaves];
+    __shared__ int flags[2 * WAVES];
+    __shared__ frag swap[PAIR == 2 ? WAVES * 2 * 64 : 1];
     T *k_lds = reinterpret_cast<T *>(lds_raw), *v_lds = k_lds + 2 * Tile::kElems;
 
     const PackedCall &c = f.c;
@@ -63,7 +69,8 @@ __global__ void __launch_bounds__(kThreads, 2) packed_dq_kernel(Backward f)
     const Walk walk = walk_of((kt.len + KT - 1) / KT, key_tiles(c, qt, kt, b.at, KT), f.q_splits);
     if (split >= walk.count)
         return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = (threadIdx.x >> 6) % kWaves, half = lane >> 5;
+    const int second = (threadIdx.x >> 6) / kWaves;  // of a pair: the part that it takes, and the half of the sums
     const int half_at = KT / 2 * half;  // the lane's half of a tile
     const int query = b.at + 32 * wave + (lane & 31);
     const bool q_here = query < qt.len;
@@ -95,7 +102,7 @@ __global__ void __launch_bounds__(kThreads, 2) packed_dq_kernel(Backward f)
                 delta = fmaf(w[e], o[e], delta);
         }
         delta = half_sum(delta);
-        if (q_here && half == 0 && split == 0)
+        if (q_here && half == 0 && second == 0 && split == 0)
             f.delta[row] = delta;
     }
     // P = 2^(s - top) inv; rows without a key, and none, have P = 0
@@ -106,9 +113,9 @@ __global__ void __launch_bounds__(kThreads, 2) packed_dq_kernel(Backward f)
     const float minus = empty ? 0.0f : -delta * inv;
     const float scale = c.scale * kLog2e;
 
-    f32x16 dq[DP / 32];
+    f32x16 dq[MINE];
 #pragma unroll
-    for (int i = 0; i < DP / 32; ++i)
+    for (int i = 0; i < MINE; ++i)
         dq[i] = 0.0f;
     // tiles from here on are not seen by all of the block's queries
     const int edge = c.causal ? max(0, b.at + shift) / KT * KT : all;
@@ -117,7 +124,7 @@ __global__ void __launch_bounds__(kThreads, 2) packed_dq_kernel(Backward f)
     for (int j0 = begin; j0 < end; j0 += KT, buf ^= 1) {
         T *kb = k_lds + buf * Tile::kElems, *vb = v_lds + buf * Tile::kElems;
         if (j0 >= edge)
-            flag_wave(flags + buf * kWaves, staged_not_finite(k_tile));
+            flag_wave(flags + buf * WAVES, staged_not_finite(k_tile));
         k_tile.put(kb);
         v_tile.put(vb);
         __syncthreads();
@@ -125,32 +132,60 @@ __global__ void __launch_bounds__(kThreads, 2) packed_dq_kernel(Backward f)
             k_tile.fetch(km, kt.at + j0 + KT, kt.at + end);
             v_tile.fetch(vm, kt.at + j0 + KT, kt.at + end);
         }
-        if (j0 >= edge && flagged<kWaves>(flags + buf * kWaves)) {
+        if (j0 >= edge && flagged<WAVES>(flags + buf * WAVES)) {
             left = true;
             continue;
         }
-        if (j0 >= wave_end)
-            continue;  // (none of the wave's queries sees the tile)
+        const bool idle = j0 >= wave_end;  // (none of the wave's queries sees the tile, nor its partner's)
         const bool whole = j0 + KT <= min(end, c.causal ? b.at + 32 * wave + shift : end);
 #pragma unroll
-        for (int sub = 0; sub < SUBS; ++sub) {
-            f32x16 s = 0.0f, dp = 0.0f;
+        for (int n = 0; n < SUBS; ++n) {
+            const int sub = PAIR == 2 ? second : n;
+            frag ds[2];
+            if (!idle) {
+                f32x16 s = 0.0f, dp = 0.0f;
 #pragma unroll
-            for (int i = 0; i < DP / 16; ++i) {
-                s = mma(row_frag<T, DP>(kb, sub, i), q[i], s);
-                dp = mma(row_frag<T, DP>(vb, sub, i), go[i], dp);
+                for (int i = 0; i < DP / 16; ++i) {
+                    s = mma(row_frag<T, DP>(kb, sub, i), q[i], s);
+                    dp = mma(row_frag<T, DP>(vb, sub, i), go[i], dp);
+                }
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    s[r] = exp2_fast(fmaf(s[r], scale, -top)) * fmaf(dp[r], inv, minus);
+                if (!whole)
+                    clear_behind(s, seen - j0 - half_at - 16 * sub, 0, 0.0f);
+#pragma unroll
+                for (int st = 0; st < 2; ++st)
+                    ds[st] = acc_frag<T>(s, st);
             }
+            if constexpr (PAIR == 2) {
+                frag *at = swap + lane;
+                const int self = threadIdx.x >> 6, partner = (self + kWaves) % WAVES;
+                if (!idle)
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                s[r] = exp2_fast(fmaf(s[r], scale, -top)) * fmaf(dp[r], inv, minus);
-            if (!whole)
-                clear_behind(s, seen - j0 - half_at, sub, 0.0f);
+                    for (int st = 0; st < 2; ++st)
+                        at[(2 * self + st) * 64] = ds[st];
+                __syncthreads();
+                if (idle)
+                    continue;
 #pragma unroll
-            for (int st = 0; st < 2; ++st) {
-                const frag p = acc_frag<T>(s, st);
+                for (int st = 0; st < 2; ++st)
 #pragma unroll
-                for (int i = 0; i < DP / 32; ++i)
-                    dq[i] = mma(col_frag<DP>(kb, sub, st, i), p, dq[i]);
+                    for (int i = 0; i < MINE; ++i)
+                        dq[i] = mma(col_frag<DP>(kb, sub, st, second * MINE + i), ds[st], dq[i]);
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    const frag other = at[(2 * partner + st) * 64];
+#pragma unroll
+                    for (int i = 0; i < MINE; ++i)
+                        dq[i] = mma(col_frag<DP>(kb, sub ^ 1, st, second * MINE + i), other, dq[i]);
+                }
+            } else if (!idle) {
+#pragma unroll
+                for (int st = 0; st < 2; ++st)
+#pragma unroll
+                    for (int i = 0; i < MINE; ++i)
+                        dq[i] = mma(col_frag<DP>(kb, sub, st, i), ds[st], dq[i]);
             }
         }
     }
@@ -160,18 +195,18 @@ __global__ void __launch_bounds__(kThreads, 2) packed_dq_kernel(Backward f)
                 continue;
             for (int j = j0; j < min(j0 + KT, end); ++j) {
                 const float p = exp2_fast(fmaf(row_dot(km, kt.at + j, q), scale, -top));
-                row_add(dq, km, kt.at + j, p * fmaf(row_dot(vm, kt.at + j, go), inv, minus), j < seen);
+                row_add(dq, km, kt.at + j, p * fmaf(row_dot(vm, kt.at + j, go), inv, minus), j < seen, second * MINE);
             }
         }
     if (walk.count > 1) {
-        store_part<DP>(f.part_q + (split * (c.heads * c.q_tokens()) + row) * DP, dq, q_here);
+        store_part<MINE>(f.part_q + (split * (c.heads * c.q_tokens()) + row) * DP + 32 * second * MINE, dq, q_here);
         return;
     }
     const HeadMap<T, DQP> om(f.dq, qt.img, head, c.dq);
 #pragma unroll
-    for (int i = 0; i < DP / 32; ++i) {
+    for (int i = 0; i < MINE; ++i) {
         dq[i] *= c.scale;
-        om.store(qt.at + query, i, half, dq[i], q_here);
+        om.store(qt.at + query, second * MINE + i, half, dq[i], q_here);
     }
 }
 
@@ -198,18 +233,18 @@ __device__ __forceinline__ void clear_before(f32x16 &s, int from, int sub, float
         s[r] = 16 * sub + r < from ? value : s[r];
 }
 
-// The launch of the keys' side: lanes hold keys, registers queries.
-// With 8 waves two take each 32 keys, half of every tile's queries each, and their
-// sums meet in LDS at the end: accumulators of 128 reals leave room for no more.
-template <typename T, int DQP, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, 2) packed_dkv_kernel(Backward f)
+// The launch of the keys' side: lanes hold keys, registers queries.  Of a pair of
+// waves one gathers dV, the other dK, each from its own and its partner's part.
+template <typename T, int DQP, int PAIR = kPair<T, DQP>>
+__global__ void __launch_bounds__(64 * kWaves * PAIR, DQP <= 16 || PAIR == 2 ? 2 : 1) packed_dkv_kernel(Backward f)
 {
-    constexpr int DP = 4 * DQP;
+    constexpr int DP = 4 * DQP, WAVES = kWaves * PAIR;
     typedef Stage<T, DP, 64 * WAVES> Tile;
     typedef typename Elem<T>::frag frag;
-    constexpr int QT = Tile::kTokens, SUBS = QT * kWaves / (32 * WAVES);  // parts of a tile that a wave takes
+    constexpr int QT = Tile::kTokens, SUBS = QT / 32 / PAIR;  // parts of a tile that a wave takes
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
     __shared__ int flags[2 * WAVES];
+    __shared__ frag swap[PAIR == 2 ? WAVES * 2 * 64 : 1];
     float *rows = reinterpret_cast<float *>(lds_raw);  // [2][top, inv, -delta][QT]
     T *q_lds = reinterpret_cast<T *>(rows + 6 * QT), *g_lds = q_lds + 2 * Tile::kElems;
 
@@ -226,10 +261,10 @@ __global__ void __launch_bounds__(64 * WAVES, 2) packed_dkv_kernel(Backward f)
     if (split >= walk.count)
         return;
     const int first = split * walk.per, last = min(group * tiles.count, first + walk.per);
-    const int lane = threadIdx.x & 63, wave = (threadIdx.x >> 6) % kWaves, half = lane >> 5;
+    const int lane = threadIdx.x & 63, all_wave = threadIdx.x >> 6, wave = all_wave % kWaves, half = lane >> 5;
+    const int second = all_wave / kWaves;  // of a pair: the part that it takes; the first gathers dV, the second dK
     const int half_at = QT / 2 * half;  // the lane's half of a tile
-    const int sub0 = threadIdx.x >> 6 >= kWaves;  // the first of the wave's parts
-    const int key = b.at + 32 * wave + (lane & 31);
+    const int wave_at = b.at + 32 * wave, key = wave_at + (lane & 31);
     const bool k_here = key < kt.len;
     // the first query that sees a key: key - back
     const int back = c.causal ? kt.len - qt.len : 0;
@@ -241,12 +276,12 @@ __global__ void __launch_bounds__(64 * WAVES, 2) packed_dkv_kernel(Backward f)
         k[i] = km.load(kt.at + key, 16 * i + 8 * half, k_here);
         v[i] = vm.load(kt.at + key, 16 * i + 8 * half, k_here);
     }
-    f32x16 dk[DP / 32], dv[DP / 32];
+    f32x16 sums[3 - PAIR][DP / 32];  // dV, dK or the wave's one of them
 #pragma unroll
-    for (int i = 0; i < DP / 32; ++i) {
-        dk[i] = 0.0f;
-        dv[i] = 0.0f;
-    }
+    for (int which = 0; which < 3 - PAIR; ++which)
+#pragma unroll
+        for (int i = 0; i < DP / 32; ++i)
+            sums[which][i] = 0.0f;
     const float scale = c.scale * kLog2e;
     Tile q_tile, g_tile;
     float row_top = 0.0f, row_sum = 0.0f, row_delta = 0.0f;  // of thread t < QT's query of a tile
@@ -295,47 +330,71 @@ __global__ void __launch_bounds__(64 * WAVES, 2) packed_dkv_kernel(Backward f)
             left = true;
             continue;
         }
-        // (a wave whose keys are not there, or that no query of the tile sees)
-        if (b.at + 32 * wave >= kt.len || (c.causal && i0 + QT <= b.at + 32 * wave - back))
-            continue;
-        f32x16 s[SUBS], dp[SUBS];
+        // (a wave whose keys are not there, or that no query of the tile sees; its
+        // partner has the same)
+        const bool idle = wave_at >= kt.len || (c.causal && i0 + QT <= wave_at - back);
 #pragma unroll
-        for (int sub = 0; sub < SUBS; ++sub) {
-            s[sub] = 0.0f;
-            dp[sub] = row_values(rw + 2 * QT, half_at, sub0 + sub);  // dP - delta starts from -delta
-        }
+        for (int n = 0; n < SUBS; ++n) {
+            const int sub = PAIR == 2 ? second : n;
+            frag p[2], ds[2];
+            if (!idle) {
+                f32x16 s = 0.0f, dp = row_values(rw + 2 * QT, half_at, sub);  // dP - delta starts from -delta
 #pragma unroll
-        for (int i = 0; i < DP / 16; ++i)
+                for (int i = 0; i < DP / 16; ++i) {
+                    s = mma(row_frag<T, DP>(qb, sub, i), k[i], s);
+                    dp = mma(row_frag<T, DP>(gb, sub, i), v[i], dp);
+                }
+                const f32x16 top = row_values(rw, half_at, sub), inv = row_values(rw + QT, half_at, sub);
 #pragma unroll
-            for (int sub = 0; sub < SUBS; ++sub) {
-                s[sub] = mma(row_frag<T, DP>(qb, sub0 + sub, i), k[i], s[sub]);
-                dp[sub] = mma(row_frag<T, DP>(gb, sub0 + sub, i), v[i], dp[sub]);
-            }
-        const bool whole = !c.causal || i0 >= b.at + 32 * wave + 31 - back;
+                for (int r = 0; r < 16; ++r) {
+                    s[r] = exp2_fast(fmaf(s[r], scale, -top[r])) * inv[r];
+                    dp[r] *= s[r];
+                }
+                if (c.causal && i0 < wave_at + 31 - back) {
+                    clear_before(s, key - back - i0 - half_at - 16 * sub, 0, 0.0f);
+                    clear_before(dp, key - back - i0 - half_at - 16 * sub, 0, 0.0f);
+                }
 #pragma unroll
-        for (int sub = 0; sub < SUBS; ++sub) {
-            const f32x16 top = row_values(rw, half_at, sub0 + sub), inv = row_values(rw + QT, half_at, sub0 + sub);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[sub][r] = exp2_fast(fmaf(s[sub][r], scale, -top[r])) * inv[r];
-                dp[sub][r] *= s[sub][r];
-            }
-            if (!whole) {
-                clear_before(s[sub], key - back - i0 - half_at - 16 * sub0, sub, 0.0f);
-                clear_before(dp[sub], key - back - i0 - half_at - 16 * sub0, sub, 0.0f);
-            }
-        }
-#pragma unroll
-        for (int sub = 0; sub < SUBS; ++sub)
-#pragma unroll
-            for (int st = 0; st < 2; ++st) {
-                const frag p = acc_frag<T>(s[sub], st), ds = acc_frag<T>(dp[sub], st);
-#pragma unroll
-                for (int i = 0; i < DP / 32; ++i) {
-                    dv[i] = mma(col_frag<DP>(gb, sub0 + sub, st, i), p, dv[i]);
-                    dk[i] = mma(col_frag<DP>(qb, sub0 + sub, st, i), ds, dk[i]);
+                for (int st = 0; st < 2; ++st) {
+                    p[st] = acc_frag<T>(s, st);
+                    ds[st] = acc_frag<T>(dp, st);
                 }
             }
+            if constexpr (PAIR == 2) {
+                frag *at = swap + lane;
+                if (!idle)
+#pragma unroll
+                    for (int st = 0; st < 2; ++st)
+                        at[(2 * all_wave + st) * 64] = second == 0 ? ds[st] : p[st];
+                __syncthreads();
+                if (idle)
+                    continue;
+                const T *from = second == 0 ? gb : qb;
+                const int partner = (all_wave + kWaves) % WAVES;
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    const frag mine = second == 0 ? p[st] : ds[st];
+#pragma unroll
+                    for (int i = 0; i < DP / 32; ++i)
+                        sums[0][i] = mma(col_frag<DP>(from, sub, st, i), mine, sums[0][i]);
+                }
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    const frag other = at[(2 * partner + st) * 64];
+#pragma unroll
+                    for (int i = 0; i < DP / 32; ++i)
+                        sums[0][i] = mma(col_frag<DP>(from, sub ^ 1, st, i), other, sums[0][i]);
+                }
+            } else if (!idle) {
+#pragma unroll
+                for (int st = 0; st < 2; ++st)
+#pragma unroll
+                    for (int i = 0; i < DP / 32; ++i) {
+                        sums[0][i] = mma(col_frag<DP>(gb, sub, st, i), p[st], sums[0][i]);
+                        sums[2 - PAIR][i] = mma(col_frag<DP>(qb, sub, st, i), ds[st], sums[2 - PAIR][i]);
+                    }
+            }
+        }
     }
     if (left)
         for (int item = first; item < last; ++item) {
@@ -345,54 +404,35 @@ __global__ void __launch_bounds__(64 * WAVES, 2) packed_dkv_kernel(Backward f)
             if (i0 >= b.at + kBlock - 1 - back || (!rows_not_finite(qm, qt.at + i0, qt.at + end) &&
                                                    !rows_not_finite(gm, qt.at + i0, qt.at + end)))
                 continue;
-            for (int i = i0 + sub0; i < end; i += WAVES / kWaves) {
+            for (int i = i0; i < end; ++i) {
                 const int64_t row = h * c.q_tokens() + int64_t(qt.img) * c.qs.tokens + qt.at + i;
                 const float sum = f.stats[2 * row + 1], inv = sum == 0.0f ? 0.0f : 1.0f / sum;
                 const float top = sum == 0.0f ? INFINITY : f.stats[2 * row], delta = sum == 0.0f ? 0.0f : f.delta[row];
                 const float p = exp2_fast(fmaf(row_dot(qm, qt.at + i, k), scale, -top)) * inv;
                 const bool sees = i >= key - back;
-                row_add(dv, gm, qt.at + i, p, sees);
-                row_add(dk, qm, qt.at + i, p * (row_dot(gm, qt.at + i, v) - delta), sees);
+                if (second == 0)
+                    row_add(sums[0], gm, qt.at + i, p, sees);
+                if (second == 1 || PAIR == 1)
+                    row_add(sums[2 - PAIR], qm, qt.at + i, p * (row_dot(gm, qt.at + i, v) - delta), sees);
             }
         }
-    if constexpr (WAVES > kWaves) {
-        // the second wave's sums to the first
-        static_assert(4 * Tile::kElems * sizeof(T) >= kWaves * 32 * DP * sizeof(float), "the tiles' room holds them");
-        float *sums = reinterpret_cast<float *>(q_lds) + wave * 32 * DP + lane;
 #pragma unroll
-        for (int which = 0; which < 2; ++which) {
-            f32x16(&x)[DP / 32] = which == 0 ? dk : dv;
-            __syncthreads();
-            if (sub0 > 0)
-#pragma unroll
-                for (int i = 0; i < DP / 32; ++i)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        sums[(16 * i + r) * 64] = x[i][r];
-            __syncthreads();
-            if (sub0 == 0)
-#pragma unroll
-                for (int i = 0; i < DP / 32; ++i)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        x[i][r] += sums[(16 * i + r) * 64];
+    for (int which = 0; which < 2; ++which) {
+        if (PAIR == 2 && which != second)
+            continue;
+        f32x16(&x)[DP / 32] = sums[PAIR == 2 ? 0 : which];
+        if (walk.count > 1) {
+            const int64_t row = kv_head * c.k_tokens() + int64_t(kt.img) * c.ks.tokens + kt.at + key;
+            store_part<DP / 32>((which == 0 ? f.part_v : f.part_k) + (split * (c.kv_heads * c.k_tokens()) + row) * DP, x, k_here);
+            continue;
         }
-        if (sub0 > 0)
-            return;
-    }
-    if (walk.count > 1) {
-        const int64_t row = kv_head * c.k_tokens() + int64_t(kt.img) * c.ks.tokens + kt.at + key;
-        const int64_t at = (split * (c.kv_heads * c.k_tokens()) + row) * DP;
-        store_part<DP>(f.part_k + at, dk, k_here);
-        store_part<DP>(f.part_v + at, dv, k_here);
-        return;
-    }
-    const HeadMap<T, DQP> okm(f.dk, kt.img, kv_head, c.dq), ovm(f.dv, kt.img, kv_head, c.dq);
+        const HeadMap<T, DQP> om(which == 0 ? f.dv : f.dk, kt.img, kv_head, c.dq);
 #pragma unroll
-    for (int i = 0; i < DP / 32; ++i) {
-        dk[i] *= c.scale;
-        okm.store(kt.at + key, i, half, dk[i], k_here);
-        ovm.store(kt.at + key, i, half, dv[i], k_here);
+        for (int i = 0; i < DP / 32; ++i) {
+            if (which == 1)
+                x[i] *= c.scale;
+            om.store(kt.at + key, i, half, x[i], k_here);
+        }
     }
 }
 
@@ -439,12 +479,11 @@ template <typename T, int DQP> hipError_t launch(const Backward &f, hipStream_t 
     constexpr int kTile = Elem<T>::kTile;
     const size_t lds = size_t(4) * kTile * Lds<T, 4 * DQP>::kRow * sizeof(T);
     const unsigned q_groups = unsigned(int64_t(f.q_blocks) * f.c.heads), k_groups = unsigned(int64_t(f.k_blocks) * f.c.kv_heads);
-    packed_dq_kernel<T, DQP><<<q_groups * f.q_splits, kThreads, lds, s>>>(f);
+    packed_dq_kernel<T, DQP><<<q_groups * f.q_splits, 64 * kWaves * kPair<T, DQP>, lds, s>>>(f);
     if (hipError_t e = hipGetLastError())
         return e;
-    constexpr int kDkvWaves = sizeof(T) == 2 && DQP == 32 ? 8 : 4;
-    packed_dkv_kernel<T, DQP, kDkvWaves>
-        <<<k_groups * f.k_splits, 64 * kDkvWaves, lds + 6 * kTile * sizeof(float), s>>>(f);
+    packed_dkv_kernel<T, DQP>
+        <<<k_groups * f.k_splits, 64 * kWaves * kPair<T, DQP>, lds + 6 * kTile * sizeof(float), s>>>(f);
     if (hipError_t e = hipGetLastError())
         return e;
     const unsigned of_queries = f.q_splits > 1 ? q_groups * join_groups(4 * DQP) : 0;

@@ -187,15 +187,17 @@ __device__ __forceinline__ float row_dot(const WholeMap<T, DQP> &m, int64_t toke
     }
     return half_sum(s);
 }
-// A row times `by`, added to the accumulators of the lanes that see it.
-template <typename T, int DQP>
-__device__ __forceinline__ void row_add(f32x16 (&acc)[DQP / 8], const WholeMap<T, DQP> &m, int64_t token, float by, bool sees)
+// A row times `by`, added to the accumulators (from the row's tile `first` on) of the
+// lanes that see it.
+template <typename T, int DQP, int N>
+__device__ __forceinline__ void row_add(f32x16 (&acc)[N], const WholeMap<T, DQP> &m, int64_t token, float by, bool sees,
+                                        int first = 0)
 {
 #pragma unroll
-    for (int i = 0; i < DQP / 8; ++i)
+    for (int i = 0; i < N; ++i)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            const T *p = m.at(token, 32 * i + 8 * g + 4 * ((threadIdx.x & 63) >> 5));
+            const T *p = m.at(token, 32 * (first + i) + 8 * g + 4 * ((threadIdx.x & 63) >> 5));
 #pragma unroll
             for (int t = 0; t < 4; ++t)
                 acc[i][4 * g + t] = sees ? fmaf(by, float(p[t]), acc[i][4 * g + t]) : acc[i][4 * g + t];
@@ -203,12 +205,12 @@ __device__ __forceinline__ void row_add(f32x16 (&acc)[DQP / 8], const WholeMap<T
 }
 
 // A D x 32 tile of accumulators, transposed, to a row of fp32.
-template <int DP> __device__ __forceinline__ void store_part(float *dst, const f32x16 (&v)[DP / 32], bool here)
+template <int N> __device__ __forceinline__ void store_part(float *dst, const f32x16 (&v)[N], bool here)
 {
     if (!here)
         return;
 #pragma unroll
-    for (int i = 0; i < DP / 32; ++i)
+    for (int i = 0; i < N; ++i)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const f32x4 t = {v[i][4 * g], v[i][4 * g + 1], v[i][4 * g + 2], v[i][4 * g + 3]};
