@@ -24,12 +24,6 @@ struct Forward {
     float *part, *part_stats;  // [split][head][token][D], [split][head][token][2]; splits > 1
 };
 
-// Keys that the queries of a block of `size` see, all of them together.
-__device__ __forceinline__ int keys_of(const PackedCall &c, const Tokens &q, const Tokens &k, int at, int size)
-{
-    return c.causal ? min(k.len, min(at + size, q.len) + k.len - q.len) : k.len;
-}
-
 // QN: sets of 32 queries that a wave holds.
 template <typename T, int DQP, int QN>
 __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(Forward f)
@@ -46,15 +40,15 @@ __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(Forward f)
     // heads side by side, so that each of 8 (or a divisor) stays on an XCD; the
     // blocks that see most keys first
     const int head = blockIdx.x % c.heads, kv_head = head / (c.heads / c.kv_heads);
-    const int split = blockIdx.x / c.heads % f.splits;
-    const Block b = locate_longest<SIZE>(c.qs, int(blockIdx.x / (c.heads * f.splits)), false);
-    const Tokens qt = tokens_of(c.qs, c.qs.first, b.seq), kt = tokens_of(c.ks, c.ks.first, b.seq);
-    if (b.at >= qt.len)
+    // (of the shares of walks all first ones, then all second ones: in between, those
+    // that are none would leave the same compute units idle)
+    const int id = blockIdx.x / c.heads, split = id / f.blocks;
+    const Place b = place_of<SIZE, KT, false>(c, id - split * f.blocks, f.splits);
+    const Tokens &qt = b.q, &kt = b.k;
+    const Walk &walk = b.walk;
+    if (b.at >= qt.len || split >= walk.count)
         return;
-    const int all = keys_of(c, qt, kt, b.at, SIZE);
-    const Walk walk = walk_of((kt.len + KT - 1) / KT, (all + KT - 1) / KT, f.splits);
-    if (split >= walk.count)
-        return;
+    const int all = c.causal ? min(kt.len, min(b.at + SIZE, qt.len) + kt.len - qt.len) : kt.len;
     const int begin = split * walk.per * KT, end = min(all, begin + walk.per * KT);
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
@@ -251,10 +245,9 @@ template <typename T, int DQP> __global__ void __launch_bounds__(kThreads) packe
     const Block b = locate(c.qs, id / kGroups, counts);
     const Tokens qt = tokens_of(c.qs, c.qs.first, b.seq), kt = tokens_of(c.ks, c.ks.first, b.seq);
     const int query = b.at + id % kGroups * (kThreads / kLanes) + threadIdx.x / kLanes, d = 4 * (threadIdx.x % kLanes);
-    if (query >= qt.len)
-        return;
-    const Walk walk = walk_of((kt.len + KT - 1) / KT, (keys_of(c, qt, kt, b.at, kBlock) + KT - 1) / KT, f.splits);
-    if (walk.count == 1)
+    const int tiles = key_tiles<KT>(c.causal, qt.len, kt.len, b.at + kBlock);
+    const Walk walk = walk_of<KT, false>(c, qt.len, kt.len, tiles, f.splits, all_walks<kBlock, KT, false>(c));
+    if (walk.count == 1 || query >= qt.len)
         return;
     const int64_t row = head * c.q_tokens() + int64_t(qt.img) * c.qs.tokens + qt.at + query;
     float top = -INFINITY, sum = 0.0f;
@@ -279,14 +272,17 @@ template <typename T, int DQP> __global__ void __launch_bounds__(kThreads) packe
     }
 }
 
+constexpr int64_t kMaxExtra = int64_t(64) << 20;
+
 // Work-groups that share a block's walk where there are few blocks.
 int forward_splits(const PackedCall &c, DType dt, bool may_split)
 {
     const int64_t groups = packed_blocks(c.qs) * c.heads;
     const int tiles = (c.ks.tokens + (dt == DType::BF16 ? 63 : 31)) / (dt == DType::BF16 ? 64 : 32);
-    if (!may_split || groups >= 512)
+    if (!may_split || groups >= kSlots)
         return 1;
-    return int(std::max<int64_t>(1, std::min<int64_t>((512 + groups - 1) / groups, tiles / 4)));
+    const int64_t room = kMaxExtra / (c.heads * c.q_tokens() * (4 * padded_dq(c.dq) + 2) * int64_t(sizeof(float)));
+    return int(std::max<int64_t>(1, std::min({(2 * kSlots + groups - 1) / groups, int64_t(tiles) / 4, room})));
 }
 
 template <typename T, int DQP> hipError_t launch(Forward f, hipStream_t s)

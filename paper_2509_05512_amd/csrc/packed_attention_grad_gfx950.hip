@@ -26,22 +26,6 @@ struct Backward {
     float *part_q, *part_k, *part_v;  // [split][head][token][D] where walks are shared
 };
 
-// Tiles of keys that a block's queries see.
-__device__ __forceinline__ int key_tiles(const PackedCall &c, const Tokens &q, const Tokens &k, int at, int tile)
-{
-    const int keys = c.causal ? min(k.len, min(at + kBlock, q.len) + k.len - q.len) : k.len;
-    return (keys + tile - 1) / tile;
-}
-// The first tile of queries that sees one of a block's keys, and how many from it on.
-struct Span {
-    int from, count;
-};
-__device__ __forceinline__ Span query_tiles(const PackedCall &c, const Tokens &q, const Tokens &k, int at, int tile)
-{
-    const int from = c.causal ? max(0, at - (k.len - q.len)) / tile : 0;
-    return {from, max(0, (q.len + tile - 1) / tile - from)};
-}
-
 // Heads of more than 64 bf16 reals have two waves for 32 tokens, each with one of the
 // two parts of every tile, so that what a wave holds fits in half of a SIMD's
 // registers; what they make of their parts they exchange through LDS.
@@ -61,13 +45,11 @@ __global__ void __launch_bounds__(64 * kWaves * PAIR, DQP <= 16 || PAIR == 2 ? 2
 
     const PackedCall &c = f.c;
     const int head = blockIdx.x % c.heads, kv_head = head / (c.heads / c.kv_heads);
-    const int split = blockIdx.x / c.heads % f.q_splits;
-    const Block b = locate_longest<kBlock>(c.qs, int(blockIdx.x / (c.heads * f.q_splits)), false);
-    const Tokens qt = tokens_of(c.qs, c.qs.first, b.seq), kt = tokens_of(c.ks, c.ks.first, b.seq);
-    if (b.at >= qt.len)
-        return;
-    const Walk walk = walk_of((kt.len + KT - 1) / KT, key_tiles(c, qt, kt, b.at, KT), f.q_splits);
-    if (split >= walk.count)
+    const int id = blockIdx.x / c.heads, split = id / f.q_blocks;
+    const Place b = place_of<kBlock, KT, false>(c, id - split * f.q_blocks, f.q_splits);
+    const Tokens &qt = b.q, &kt = b.k;
+    const Walk &walk = b.walk;
+    if (b.at >= qt.len || split >= walk.count)
         return;
     const int lane = threadIdx.x & 63, wave = (threadIdx.x >> 6) % kWaves, half = lane >> 5;
     const int second = (threadIdx.x >> 6) / kWaves;  // of a pair: the part that it takes, and the half of the sums
@@ -249,17 +231,15 @@ __global__ void __launch_bounds__(64 * kWaves * PAIR, DQP <= 16 || PAIR == 2 ? 2
     T *q_lds = reinterpret_cast<T *>(rows + 6 * QT), *g_lds = q_lds + 2 * Tile::kElems;
 
     const PackedCall &c = f.c;
-    const int group = c.heads / c.kv_heads, kv_head = blockIdx.x % c.kv_heads, split = blockIdx.x / c.kv_heads % f.k_splits;
-    // (of causal sequences the first blocks of keys are seen by most queries)
-    const Block b = locate_longest<kBlock>(c.ks, int(blockIdx.x / (c.kv_heads * f.k_splits)), true);
-    const Tokens qt = tokens_of(c.qs, c.qs.first, b.seq), kt = tokens_of(c.ks, c.ks.first, b.seq);
-    if (b.at >= kt.len)
+    const int group = c.heads / c.kv_heads, kv_head = blockIdx.x % c.kv_heads;
+    const int id = blockIdx.x / c.kv_heads, split = id / f.k_blocks;
+    const Place b = place_of<kBlock, QT, true>(c, id - split * f.k_blocks, f.k_splits);
+    const Tokens &qt = b.q, &kt = b.k;
+    const Walk &walk = b.walk;
+    if (b.at >= kt.len || split >= walk.count)
         return;
     // the walk: tiles of queries, head by head
-    const Span tiles = query_tiles(c, qt, kt, b.at, QT);
-    const Walk walk = walk_of(group * ((qt.len + QT - 1) / QT), group * tiles.count, f.k_splits);
-    if (split >= walk.count)
-        return;
+    const Span tiles = query_tiles<QT>(c.causal, qt.len, kt.len, b.at);
     const int first = split * walk.per, last = min(group * tiles.count, first + walk.per);
     const int lane = threadIdx.x & 63, all_wave = threadIdx.x >> 6, wave = all_wave % kWaves, half = lane >> 5;
     const int second = all_wave / kWaves;  // of a pair: the part that it takes; the first gathers dV, the second dK
@@ -444,17 +424,17 @@ template <typename T, int DQP> __global__ void __launch_bounds__(kThreads) packe
     __shared__ int counts[kWaves];
     const PackedCall &c = f.c;
     const bool keys = int(blockIdx.x) >= of_queries;
-    const int heads = keys ? c.kv_heads : c.heads, group = c.heads / c.kv_heads;
+    const int heads = keys ? c.kv_heads : c.heads;
     const int head = (blockIdx.x - (keys ? of_queries : 0)) % heads, id = (blockIdx.x - (keys ? of_queries : 0)) / heads;
     const Sequences &mine = keys ? c.ks : c.qs;
     const Block b = locate(mine, id / kGroups, counts);
     const Tokens qt = tokens_of(c.qs, c.qs.first, b.seq), kt = tokens_of(c.ks, c.ks.first, b.seq), t = keys ? kt : qt;
     const int token = b.at + id % kGroups * (kThreads / kLanes) + threadIdx.x / kLanes, d = 4 * (threadIdx.x % kLanes);
-    if (token >= t.len)
-        return;
-    const Walk walk = keys ? walk_of(group * ((qt.len + TILE - 1) / TILE), group * query_tiles(c, qt, kt, b.at, TILE).count, f.k_splits)
-                           : walk_of((kt.len + TILE - 1) / TILE, key_tiles(c, qt, kt, b.at, TILE), f.q_splits);
-    if (walk.count == 1)
+    const int q_tiles = query_tiles<TILE>(c.causal, qt.len, kt.len, b.at).count;
+    const int k_tiles = key_tiles<TILE>(c.causal, qt.len, kt.len, b.at + kBlock);
+    const Walk walk = keys ? walk_of<TILE, true>(c, qt.len, kt.len, q_tiles, f.k_splits, all_walks<kBlock, TILE, true>(c))
+                           : walk_of<TILE, false>(c, qt.len, kt.len, k_tiles, f.q_splits, all_walks<kBlock, TILE, false>(c));
+    if (walk.count == 1 || token >= t.len)
         return;
     const int64_t all = heads * (keys ? c.k_tokens() : c.q_tokens());
     const int64_t row = head * (keys ? c.k_tokens() : c.q_tokens()) + int64_t(t.img) * mine.tokens + t.at + token;
@@ -520,9 +500,9 @@ size_t delta_bytes(const PackedCall &c)
 // Work-groups that share a walk of at most `tiles` where there are few walks.
 int splits_of(int64_t groups, int64_t tiles)
 {
-    if (groups >= 1024)
+    if (groups >= kSlots)
         return 1;
-    return int(std::max<int64_t>(1, std::min<int64_t>((1024 + groups - 1) / groups, tiles / 4)));
+    return int(std::max<int64_t>(1, std::min<int64_t>((2 * kSlots + groups - 1) / groups, tiles / 4)));
 }
 struct Plan {
     int q_splits, k_splits;

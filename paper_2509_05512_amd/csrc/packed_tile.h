@@ -48,9 +48,19 @@ template <int SIZE = kBlock> __device__ __forceinline__ Block locate(const Seque
 }
 
 // Sum and maximum over a wave.
+#define QUAN_DPP(v, ctrl) __builtin_amdgcn_update_dpp(0, v, ctrl, 0xf, 0xf, false)
+__device__ __forceinline__ float wave_sum(float x)
+{
+    x += __int_as_float(QUAN_DPP(__float_as_int(x), 0xB1));
+    x += __int_as_float(QUAN_DPP(__float_as_int(x), 0x4E));
+    x += __int_as_float(QUAN_DPP(__float_as_int(x), 0x141));
+    x += __int_as_float(QUAN_DPP(__float_as_int(x), 0x140));
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = half_sum(__uint_as_float(a[0]) + __uint_as_float(a[1]));
+    return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x)));
+}
 __device__ __forceinline__ int wave_sum(int x)
 {
-#define QUAN_DPP(v, ctrl) __builtin_amdgcn_update_dpp(0, v, ctrl, 0xf, 0xf, false)
     x += QUAN_DPP(x, 0xB1);   // lane ^ 1
     x += QUAN_DPP(x, 0x4E);   // lane ^ 2
     x += QUAN_DPP(x, 0x141);  // 7 - lane of 8
@@ -73,58 +83,143 @@ __device__ __forceinline__ int wave_max(int x)
     return __builtin_amdgcn_readfirstlane(max(int(b[0]), int(b[1])));
 }
 
-// The blocks in an order that begins with the longest walks: of 64 sequences at a
-// time, first the blocks that are `level` from their sequence's one end, then those
-// that are one less, down to 0 (whose walks are the shortest).  at is SIZE * level,
-// or with from_end the block that many before the last.
-template <int SIZE> __device__ __forceinline__ Block locate_longest(const Sequences &s, int id, bool from_end)
+// Tiles of keys that queries up to `last` (counted from 1) of a sequence see.
+template <int TILE> __device__ __forceinline__ int key_tiles(bool causal, int lq, int lk, int last)
 {
-    const int lane = threadIdx.x & 63;
-    if (s.first == nullptr) {
-        const int per = (s.tokens + SIZE - 1) / SIZE, down = id / s.count;  // (equal lengths)
-        return {id - down * s.count, (from_end ? down : per - 1 - down) * SIZE};
-    }
-    // the 64 sequences, counted as in locate()
-    int set = 0;
-    for (int i0 = 0; i0 + 64 < s.count; i0 += 64 * 64) {
-        const int i = i0 + 64 * lane + 64;
-        set += __popcll(__ballot(i < s.count && min(max(s.first[min(i, s.count)], 0), s.tokens) / SIZE + i <= id));
-    }
-    set *= 64;
-    const int at0 = min(max(s.first[set], 0), s.tokens), rank = id - (at0 / SIZE + set);
-    const int seq = min(set + lane, s.count - 1);
-    const int a = min(max(s.first[seq], 0), s.tokens), len = min(max(s.first[seq + 1], a), s.tokens) - a;
-    const int blocks = set + lane < s.count ? (len + SIZE - 1) / SIZE : 0;
-    // the largest level with more than `rank` blocks at or above it
-    int low = 0, high = wave_max(blocks);
-    if (rank < 0 || rank >= wave_sum(blocks))
-        return {0, s.tokens};
-    while (high - low > 1) {
-        const int mid = (low + high) >> 1;
-        if (wave_sum(max(0, blocks - mid)) > rank)
-            low = mid;
-        else
-            high = mid;
-    }
-    const int skip = rank - wave_sum(max(0, blocks - low - 1));
-    const auto here = __ballot(blocks > low);
-    const auto mine = __ballot(blocks > low && __popcll(here & ((1ull << lane) - 1)) == skip);
-    const int l = mine != 0 ? __builtin_ctzll(mine) : 0;
-    const int of = __builtin_amdgcn_readlane(blocks, l);
-    return {min(set + l, s.count - 1), (from_end ? of - 1 - low : low) * SIZE};
+    return (max(0, causal ? min(lk, min(last, lq) + lk - lq) : lk) + TILE - 1) / TILE;
+}
+// The first tile of queries that sees a key at `at` or behind it, and how many from
+// it on.
+struct Span {
+    int from, count;
+};
+template <int TILE> __device__ __forceinline__ Span query_tiles(bool causal, int lq, int lk, int at)
+{
+    const int from = causal ? max(0, at - (lk - lq)) / TILE : 0;
+    return {from, max(0, (lq + TILE - 1) / TILE - from)};
 }
 
-// A block's walk over `mine` tiles, dealt out to work-groups: `count` of them take
-// `per` tiles each, the last the rest, where the sequence's longest walk has `longest`
-// tiles and `splits` work-groups, so that all take about as many.  (Two tiles at
-// least.)
+// A walk is dealt out to `count` work-groups, `per` tiles to each (the last has the
+// rest).
 struct Walk {
     int per, count;
 };
-__device__ __forceinline__ Walk walk_of(int longest, int mine, int splits)
+// Tiles of all walks of a sequence, KEYS: of blocks of keys over the queries that see
+// them, else of blocks of queries over their keys.  (A rule of thumb: halves of the
+// first and the last.)
+template <int SIZE, int TILE, bool KEYS> __device__ __forceinline__ float walks_of(bool causal, int lq, int lk)
 {
-    const int per = max(2, (longest + splits - 1) / splits);
-    return {per, max(1, (mine + per - 1) / per)};
+    const int blocks = ((KEYS ? lk : lq) + SIZE - 1) / SIZE;
+    const int first = KEYS ? query_tiles<TILE>(causal, lq, lk, 0).count : key_tiles<TILE>(causal, lq, lk, SIZE);
+    const int last = KEYS ? query_tiles<TILE>(causal, lq, lk, max(0, lk - 1)).count : key_tiles<TILE>(causal, lq, lk, lq);
+    return 0.5f * float(blocks) * float(first + last);
+}
+// That of a block with `mine` tiles in its sequence (`times`: walks over the heads of
+// a group one after another): to as many as have the share of one of kSlots
+// work-groups of all walks, and what it costs to start one, each, where the
+// sequence's longest walk is more than twice that; to `splits` at most, which is what
+// the launch has.  (One sequence of 6400 tokens, 4 heads of 128 reals, a training
+// step: 368 us, 384 with shares of 1 / 400, 409 of 1 / 300, 405 with starts of 3 tiles
+// at 1 / 512; without shares 1569.)  all: the sum of walks_of() over the lanes' sequences.
+constexpr int kSlots = 512;                                           // two to a compute unit
+constexpr int start_of(int tile) { return tile == 64 ? 4 : 1; }  // tiles' worth: bf16, fp32
+template <int TILE, bool KEYS>
+__device__ __forceinline__ Walk walk_of(const PackedCall &c, int lq, int lk, int mine, int splits, float all)
+{
+    const int times = KEYS ? c.heads / c.kv_heads : 1;
+    const int longest = times * (((KEYS ? lq : lk) + TILE - 1) / TILE);
+    const int share = int(fminf(wave_sum(all) * float(c.heads) / kSlots, 1e9f)) + start_of(TILE);
+    if (longest <= 2 * share)
+        return {max(1, times * mine), 1};
+    const int per = max(share, (longest + splits - 1) / splits);
+    return {per, max(1, (times * mine + per - 1) / per)};
+}
+template <int SIZE, int TILE, bool KEYS> __device__ __forceinline__ float all_walks(const PackedCall &c)
+{
+    float all = 0.0f;
+    for (int i0 = 0; i0 < c.qs.count; i0 += 64) {
+        const int seq = i0 + int(threadIdx.x & 63), at = min(seq, c.qs.count - 1);
+        const float w = walks_of<SIZE, TILE, KEYS>(c.causal, tokens_of(c.qs, c.qs.first, at).len, tokens_of(c.ks, c.ks.first, at).len);
+        all += seq < c.qs.count ? w : 0.0f;
+    }
+    return all;
+}
+
+// Block `id` of a launch, its sequence and its walk.  The blocks come in an order that
+// begins with the longest walks: of 64 sequences at a time, first the blocks that are
+// `level` from their sequence's one end, then those one less, down to 0 (whose walks
+// are the shortest); queries' blocks from the last, of keys from the first.  at >= the
+// sequence's length: none.  (What a wave needs it reads at once: a work-group has
+// little to do before its first tile but to wait for memory.)
+struct Place {
+    Tokens q, k;
+    int at;
+    Walk walk;
+};
+template <int SIZE, int TILE, bool KEYS> __device__ __forceinline__ Place place_of(const PackedCall &c, int id, int splits)
+{
+    const int lane = threadIdx.x & 63;
+    const Sequences &mine = KEYS ? c.ks : c.qs;
+    Place p;
+    float all = 0.0f;
+    if (mine.first == nullptr) {
+        const int per = (mine.tokens + SIZE - 1) / SIZE, down = id / mine.count;  // (equal lengths)
+        const int seq = id - down * mine.count;
+        p.q = {seq, 0, c.qs.tokens};
+        p.k = {seq, 0, c.ks.tokens};
+        p.at = (KEYS ? down : per - 1 - down) * SIZE;
+        if (splits > 1)
+            all = lane == 0 ? float(mine.count) * walks_of<SIZE, TILE, KEYS>(c.causal, p.q.len, p.k.len) : 0.0f;
+    } else {
+        const int n = mine.count;
+        auto clamp = [&](int v, const Sequences &s) { return min(max(v, 0), s.tokens); };
+        // the 64 sequences, counted as in locate()
+        int set = 0;
+        for (int i0 = 0; i0 + 64 < n; i0 += 64 * 64) {
+            const int i = i0 + 64 * lane + 64;
+            set += __popcll(__ballot(i < n && clamp(mine.first[min(i, n)], mine) / SIZE + i <= id));
+        }
+        set *= 64;
+        const int seq = min(set + lane, n - 1);
+        const int qa = clamp(c.qs.first[seq], c.qs), q_len = max(clamp(c.qs.first[seq + 1], c.qs) - qa, 0);
+        int ka = qa, k_len = q_len;
+        if (c.ks.first != c.qs.first) {
+            ka = clamp(c.ks.first[seq], c.ks);
+            k_len = max(clamp(c.ks.first[seq + 1], c.ks) - ka, 0);
+        }
+        const int blocks = set + lane < n ? ((KEYS ? k_len : q_len) + SIZE - 1) / SIZE : 0;
+        const int rank = id - (__builtin_amdgcn_readfirstlane(KEYS ? ka : qa) / SIZE + set);
+        // the largest level with more than `rank` blocks at or above it
+        int low = 0, high = wave_max(blocks);
+        if (rank < 0 || rank >= wave_sum(blocks))
+            return {{0, 0, 0}, {0, 0, 0}, 0, {1, 1}};
+        while (high - low > 1) {
+            const int mid = (low + high) >> 1;
+            if (wave_sum(max(0, blocks - mid)) > rank)
+                low = mid;
+            else
+                high = mid;
+        }
+        const int skip = rank - wave_sum(max(0, blocks - low - 1));
+        const auto here = __ballot(blocks > low);
+        const auto one = __ballot(blocks > low && __popcll(here & ((1ull << lane) - 1)) == skip);
+        const int l = one != 0 ? __builtin_ctzll(one) : 0;
+        p.q = {0, __builtin_amdgcn_readlane(qa, l), __builtin_amdgcn_readlane(q_len, l)};
+        p.k = {0, __builtin_amdgcn_readlane(ka, l), __builtin_amdgcn_readlane(k_len, l)};
+        const int of = ((KEYS ? p.k.len : p.q.len) + SIZE - 1) / SIZE;
+        p.at = (KEYS ? of - 1 - low : low) * SIZE;
+        if (splits > 1 && n > 64)
+            all = all_walks<SIZE, TILE, KEYS>(c);
+        else if (splits > 1)
+            all = set + lane < n ? walks_of<SIZE, TILE, KEYS>(c.causal, q_len, k_len) : 0.0f;
+    }
+    const int tiles = KEYS ? query_tiles<TILE>(c.causal, p.q.len, p.k.len, p.at).count
+                           : key_tiles<TILE>(c.causal, p.q.len, p.k.len, p.at + SIZE);
+    if (splits > 1)
+        p.walk = walk_of<TILE, KEYS>(c, p.q.len, p.k.len, tiles, splits, all);
+    else
+        p.walk = {max(1, (KEYS ? c.heads / c.kv_heads : 1) * tiles), 1};
+    return p;
 }
 
 // Infinities and NaN in rows of a tile that not all of the work-group's lanes see:
