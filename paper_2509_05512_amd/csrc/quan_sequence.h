@@ -42,6 +42,7 @@ struct CacheCopy {
     AttnMap k, v;
     const int32_t *start, *kv_len;  // [sequences]; NULL: 0, the table's end
 };
+int64_t cache_copy_groups(const CacheCopy &c);  // work-groups of 256 lanes
 hipError_t cache_write_run(const CacheCopy &c, DType dt, hipStream_t stream);
 hipError_t cache_read_run(const CacheCopy &c, DType dt, hipStream_t stream);
 

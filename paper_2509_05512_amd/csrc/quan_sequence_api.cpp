@@ -136,7 +136,10 @@ int check_copy(const char *fn, const quan_tensor *k, const quan_tensor *v, const
         return rc;
     c->start = start;
     c->kv_len = kv_len;
-    c->k.s_h = c->v.s_h = cache->dq;
+    for_heads(&c->k, cache->dq);
+    for_heads(&c->v, cache->dq);
+    if (quan::cache_copy_groups(*c) > kMaxGroups)
+        return report(QUAN_ERR_UNSUPPORTED, "%s: too many work-groups", fn);
     *dt = to_dt(k->dtype);
     return QUAN_OK;
 }

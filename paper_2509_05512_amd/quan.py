@@ -992,29 +992,39 @@ def empty_cache(pages, page_tokens, heads, dq, table, dtype=torch.float8_e4m3fn)
     return Cache(keys, values, *exps, table, int(dq))
 
 
+# elements of a row by (dq, format): 4 dq up to whole 16 bytes
+_ROWS = {(dq, f): -(-4 * dq // per) * per for dq in range(1, 33) for f, per in (
+    (QUAN_CACHE_F32, 4), (QUAN_CACHE_BF16, 8), (QUAN_CACHE_E4M3, 16))}
+
+
 def _cache(c, device):
     """struct quan_cache of a Cache."""
-    form = _FORMATS.get(c.keys.dtype)
+    keys, values, key_exp, value_exp, table, dq = c
+    form = _FORMATS.get(keys.dtype)
     if form is None:
-        raise TypeError(f"unsupported dtype {c.keys.dtype} of a cache; expected float8_e4m3fn, bfloat16 or float32")
-    if c.keys.dim() != 4 or c.values.shape != c.keys.shape or c.values.dtype != c.keys.dtype \
-            or not c.keys.is_contiguous() or not c.values.is_contiguous():
+        raise TypeError(f"unsupported dtype {keys.dtype} of a cache; expected float8_e4m3fn, bfloat16 or float32")
+    shape, places = keys.shape, table.shape
+    if len(shape) != 4 or values.shape != shape or values.dtype != keys.dtype or not keys.is_contiguous() \
+            or not values.is_contiguous():
         raise ValueError("a cache's keys and values must be contiguous [pages, heads, page_tokens, row] tensors alike")
-    pages, heads, page_tokens, row = c.keys.shape
-    size = c.keys.element_size()
-    if not 0 < c.dq <= 32 or row != -(-4 * c.dq * size // 16) * 16 // size:
+    pages, heads, page_tokens, row = shape
+    if row != _ROWS.get((dq, form)):
         raise ValueError("a cache's rows must hold 4 dq reals up to whole 16 bytes")
-    for t in (c.key_exp, c.value_exp):
-        if (t is None) != (form != QUAN_CACHE_E4M3) or (t is not None and (
-                t.dtype != torch.uint8 or t.shape != c.keys.shape[:3] or not t.is_contiguous())):
-            raise ValueError("an 8-bit cache has key_exp and value_exp, contiguous uint8 [pages, heads, page_tokens]")
-    if c.table.dim() != 2 or c.table.dtype != torch.int32 or not c.table.is_contiguous():
+    if len(places) != 2 or table.dtype != torch.int32 or not table.is_contiguous():
         raise ValueError("a cache's table must be a contiguous int32 [sequences, pages] tensor")
-    for t in (c.keys, c.values, c.key_exp, c.value_exp, c.table):
-        if t is not None and t.device != device:
-            raise ValueError("a cache must lie on the maps' device")
-    return _PACK_CACHE(c.keys.data_ptr(), c.values.data_ptr(), _ptr(c.key_exp) or 0, _ptr(c.value_exp) or 0,
-                       c.table.data_ptr(), form, pages, page_tokens, heads, c.dq, *c.table.shape)
+    if not keys.device == values.device == table.device == device:
+        raise ValueError("a cache must lie on the maps' device")
+    ke = ve = 0
+    if form == QUAN_CACHE_E4M3:
+        for t in (key_exp, value_exp):
+            if t is None or t.dtype != torch.uint8 or t.shape != shape[:3] or not t.is_contiguous() or t.device != device:
+                raise ValueError("an 8-bit cache has key_exp and value_exp, contiguous uint8 [pages, heads, page_tokens] "
+                                 "on its device")
+        ke, ve = key_exp.data_ptr(), value_exp.data_ptr()
+    elif key_exp is not None or value_exp is not None:
+        raise ValueError("key_exp and value_exp are for an 8-bit cache")
+    return _PACK_CACHE(keys.data_ptr(), values.data_ptr(), ke, ve, table.data_ptr(), form, pages, page_tokens, heads, dq,
+                       *places)
 
 
 def _ints(name, t, shape, device):
