@@ -788,8 +788,8 @@ enum quan_cache_format { QUAN_CACHE_F32 = 0, QUAN_CACHE_BF16 = 1, QUAN_CACHE_E4M
  *                 is no page: what would be written there is dropped, what
  *                 would be read is zero, its tokens take no part in attention.
  *
- * pages * heads * page_tokens and table_pages * page_tokens stay below 2^31,
- * sequences * table_pages too; heads <= 65535, dq <= 32, page_tokens <= 2^24.
+ * pages * heads * page_tokens and sequences * table_pages stay below 2^31,
+ * table_pages * page_tokens <= 2^30; heads <= 65535, dq <= 32, page_tokens <= 2^24.
  */
 typedef struct quan_cache {
     void *keys, *values;

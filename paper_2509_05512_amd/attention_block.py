@@ -14,7 +14,12 @@ or a residual sum of its own.
 
 ``cache`` and ``query`` are the form for single pixels: keys and values of a map
 that arrives row by row are written once, and a query at any place reads the
-first ``kv_len`` of them.
+first ``kv_len`` of them.  ``pages`` is the same cache in pages, in 8 bits unless
+asked for otherwise.
+
+With ``causal`` the block works in raster order: a pixel sees those before it and
+itself, without a bias.  ``extend`` takes the next pixels of sequences whose
+earlier ones lie in a cache of pages, as many as there are, and ``query`` one.
 
     python -m paper_2509_05512_amd.attention_block
 
@@ -32,12 +37,12 @@ class AttentionBlock:
     packs the kernels that the convolutions read after a change to them."""
 
     def __init__(self, c, heads, kv_heads=None, radius=8, buckets=17, p=0.0, last=False, dtype=torch.bfloat16,
-                 device="cuda", seed=0):
+                 device="cuda", seed=0, causal=False):
         kv_heads = heads if kv_heads is None else kv_heads
         if c % heads or heads % kv_heads:
             raise ValueError("c must be a multiple of heads, heads of kv_heads")
         self.c, self.heads, self.kv = c, heads, c // heads * kv_heads
-        self.p, self.dtype = p, dtype
+        self.p, self.dtype, self.causal = p, dtype, causal
         self.bucket = quan.quan_relpos_buckets(radius, buckets, device)
         draw = torch.Generator().manual_seed(seed)
         # a quaternion kernel sums 4 c products
@@ -45,13 +50,13 @@ class AttentionBlock:
         self.params = {
             "qkv": torch.randn((4, wide, c, 1, 1), generator=draw) / math.sqrt(4 * c),
             "proj": torch.randn((4, c, c, 1, 1), generator=draw) / math.sqrt(4 * c),
-            "table": 0.1 * torch.randn((heads, buckets, buckets), generator=draw),
+            "table": None if causal else 0.1 * torch.randn((heads, buckets, buckets), generator=draw),
             "gamma": torch.ones((4, c)),
             "scale": torch.full((4, c), 0.1),
         }
         if not last:
             self.params["next_gamma"] = torch.ones((4, c))
-        self.params = {name: t.to(device) for name, t in self.params.items()}
+        self.params = {name: t.to(device) for name, t in self.params.items() if t is not None}
         self.load()
 
     def load(self):
@@ -66,7 +71,14 @@ class AttentionBlock:
         return qkv[:, :, :self.c], qkv[:, :, self.c:self.c + self.kv], qkv[:, :, self.c + self.kv:]
 
     def _relpos(self):
-        return self.params["table"], self.bucket, self.bucket
+        return None if self.causal else (self.params["table"], self.bucket, self.bucket)
+
+    def _attend(self, qkv, save):
+        parts = self._parts(qkv)
+        if self.causal:
+            got = quan.quan_packed_attention_forward(*parts, None, self.heads, save=save)
+            return (*got, None) if save else got
+        return quan.quan_attention_forward(*parts, self.heads, relpos=self._relpos(), save=save)
 
     def _step(self):
         at = self.params
@@ -77,7 +89,7 @@ class AttentionBlock:
         saved) for backward.  Dropout is on where rng is given."""
         p = 0.0 if rng is None else self.p
         qkv = self._conv("qkv", h)
-        attended = quan.quan_attention_forward(*self._parts(qkv), self.heads, relpos=self._relpos(), save=save)
+        attended = self._attend(qkv, save)
         a, stats, rest = attended if save else (attended, None, None)
         y = self._conv("proj", a)
         out, h_out = quan.quan_residual_forward(x, y, gate=gate, p=p, rng=rng, **self._step())
@@ -98,8 +110,11 @@ class AttentionBlock:
         da = self._conv_backward("proj", a, res.dy, grads)
         dqkv = torch.empty_like(qkv)
         dq, dk, dv = self._parts(dqkv)
-        grads["table"] = quan.quan_attention_backward(*self._parts(qkv), a, stats, rest, da, self.heads,
-                                                      relpos=self._relpos(), dq=dq, dk=dk, dv=dv)[3]
+        if self.causal:
+            quan.quan_packed_attention_backward(*self._parts(qkv), a, stats, da, None, self.heads, dq=dq, dk=dk, dv=dv)
+        else:
+            grads["table"] = quan.quan_attention_backward(*self._parts(qkv), a, stats, rest, da, self.heads,
+                                                          relpos=self._relpos(), dq=dq, dk=dk, dv=dv)[3]
         dh = self._conv_backward("qkv", h, dqkv, grads)
         return res.dx, dh, res.dgate, grads
 
@@ -113,19 +128,59 @@ class AttentionBlock:
         device = self.bucket.device
         return tuple(quan.empty_qmap(n, self.kv, height, width, self.dtype, device) for _ in range(2))
 
+    def pages(self, n, height, width, page_tokens=64, dtype=torch.float8_e4m3fn):
+        """The same in pages (quan.Cache), the pages of a map one after another."""
+        per, dq = -(-height * width // page_tokens), self.c // self.heads
+        table = torch.arange(n * per, dtype=torch.int32, device=self.bucket.device).view(n, per)
+        return quan.empty_cache(n * per, page_tokens, self.kv // dq, dq, table, dtype)
+
     def write(self, cache, h, row):
         """Keys and values of the rows that h holds, from `row` on."""
         _, k, v = self._parts(self._conv("qkv", h))
+        if isinstance(cache, quan.Cache):
+            start = torch.full((h.shape[0],), row * h.shape[4], dtype=torch.int32, device=h.device)
+            quan.quan_cache_write(cache, k, v, start)
+            return
         for held, new in zip(cache, (k, v)):
             held[:, :, :, row:row + h.shape[3]].copy_(new)
 
-    def query(self, cache, x, h, pos, kv_len=None, gate=None):
+    def query(self, cache, x, h, pos, kv_len=None, gate=None, width=None):
         """(out, h_out) of one pixel per image, x and h [N, 4, C, 1, 1], at pos
         int32 [N, 2] (y, x) of a cache whose first kv_len int32 [N] pixels are
-        there."""
+        there; a cache of pages holds maps `width` wide (pos and width are for the
+        bias, a causal block has none)."""
         q, _, _ = self._parts(self._conv("qkv", h))
-        a = quan.quan_attention_forward(q, *cache, self.heads, relpos=self._relpos(), kv_len=kv_len, pos=pos)
+        if isinstance(cache, quan.Cache):
+            a = quan.quan_cache_attention(q, cache, kv_len, self.heads, relpos=self._relpos(), pos=pos, width=width)
+        else:
+            a = quan.quan_attention_forward(q, *cache, self.heads, relpos=self._relpos(), kv_len=kv_len, pos=pos)
         return quan.quan_residual_forward(x, self._conv("proj", a), gate=gate, **self._step())
+
+    def extend(self, cache, x, h, past, gate=None):
+        """(out, h_out) of the next pixels of a causal block's sequences, x and h
+        [N, 4, C, H, W] in raster order behind the past[i] (integers) that the cache
+        of pages holds of sequence i; theirs are written to it."""
+        if not self.causal:
+            raise ValueError("extend is for a causal block")
+        n, new, dev = x.shape[0], x.shape[3] * x.shape[4], x.device
+        q, k, v = self._parts(self._conv("qkv", h))
+        quan.quan_cache_write(cache, k, v, torch.tensor(past, dtype=torch.int32, device=dev))
+        lens = [p + new for p in past]
+        first, k_first = (torch.tensor([sum(t[:i]) for i in range(n + 1)], dtype=torch.int32, device=dev)
+                          for t in ([new] * n, lens))
+        held = quan.empty_qmap(1, 2 * self.kv, 1, sum(lens), self.dtype, dev)
+        keys, values = quan.quan_cache_read(cache, held[:, :, :self.kv], held[:, :, self.kv:], first=k_first)
+        one = _in_a_row(q)
+        a = quan.quan_packed_attention_forward(one, keys, values, first, self.heads, k_first=k_first)
+        y = self._conv("proj", a.permute(0, 3, 4, 1, 2).reshape(n, *x.shape[3:], 4, self.c).permute(0, 3, 4, 1, 2))
+        return quan.quan_residual_forward(x, y, gate=gate, **self._step())
+
+
+def _in_a_row(t):
+    """Maps [N, 4, C, H, W] whose pixels lie at one stride as one image of N H W."""
+    n, _, c, h, w = t.shape
+    _, s_p, s_c, _, s_t = t.stride()
+    return t.as_strided((1, 4, c, 1, n * h * w), (n * h * w * s_t, s_p, s_c, n * h * w * s_t, s_t))
 
 
 class Stack:

@@ -265,19 +265,22 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 && D < 128 ? 4 : 2) c
     const bool partial = c.row_bytes != R::kBytes;  // the rows are shorter than D reals
     const int chunks = c.row_bytes / 16;
 
+    // a position's page is read a round ahead, a position's factors with its rows
+    const int32_t *pages = c.table + int64_t(seq) * c.table_pages;
+    auto page_of = [&](int j) { return j < share.end ? pages[fast_div(j, c.by_page)] : -1; };
+    int page = page_of(share.begin + wave * kChunk + lane);
     for (int j0 = share.begin + wave * kChunk; j0 < share.end; j0 += kRound) {
         // the chunk's rows, a position per lane
         const int j = j0 + lane;
-        Slot slot{-1, 0};
-        if (j < share.end)
-            slot = slot_of(c, seq, j);
-        const bool here = slot.row >= 0;
-        const int row = here ? slot.row + kv_head * page_rows + slot.slot : 0;
+        const bool here = page >= 0 && page < c.pages;
+        const int row = here ? (page * c.heads + kv_head) * page_rows + j - fast_div(j, c.by_page) * page_rows : 0;
         const auto ok = __ballot(here);
+        page = page_of(j + kRound);
         rows[lane] = row;
+        unsigned key_exp = 0, value_exp = 0;
         if (E4M3) {
-            key_by[lane] = here ? scale * factor_of(c.key_exp[row]) : 0.0f;
-            value_by[lane] = here ? factor_of(c.value_exp[row]) : 0.0f;
+            key_exp = c.key_exp[row];
+            value_exp = c.value_exp[row];
         }
         if (BIAS != 0) {
             const int y = fast_div(j, a.by_width), x = j - y * a.width;
@@ -322,6 +325,13 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 && D < 128 ? 4 : 2) c
                                                                 partial ? c.row_bytes : R::kBytes);
                     }
                 }
+            if (E4M3 && sub == 0) {
+                key_by[lane] = here ? scale * factor_of(key_exp) : 0.0f;
+                value_by[lane] = here ? factor_of(value_exp) : 0.0f;
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            }
             if (partial && !E4M3) {
                 // (an 8-bit row that is not finite is so as a whole)
 #pragma unroll
@@ -572,12 +582,13 @@ Token plan(const CacheAttention &a, bool may_split)
     t.group = a.heads / a.cache.heads;
     t.group_blocks = (t.group + kQueries - 1) / kQueries;
     t.units = a.cache.heads * t.group_blocks;
-    // spans beyond one for each sequence, where the chip has room for them: two
-    // work-groups per compute unit
+    // spans beyond one for each sequence, where there is not a work-group for each
+    // compute unit: so many that there is (4 x 65536 tokens: 18.9 us, 20.8 with two, 22.3
+    // with four)
     const int64_t groups = int64_t(a.n) * t.units;
-    if (may_split && groups < 512 && a.cache.capacity() > kRound) {
+    if (may_split && groups < 256 && a.cache.capacity() > kRound) {
         const int64_t rounds = (int64_t(a.cache.capacity()) + kRound - 1) / kRound * a.n;
-        t.spans = int(std::min<int64_t>(a.n + (512 + t.units - 1) / t.units, a.n + rounds));
+        t.spans = int(std::min<int64_t>(a.n + (256 + t.units - 1) / t.units, a.n + rounds));
     }
     return t;
 }

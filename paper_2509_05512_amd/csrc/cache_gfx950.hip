@@ -233,6 +233,8 @@ Copy copy_plan(const CacheCopy &c)
     // so many tokens that each lane has kAhead rows
     const int rows = kAhead * kThreads / p.lanes;
     p.tokens = std::max(1, std::min(kTokens, rows / (2 * c.cache.heads)));
+    // (few tokens: over the chip)
+    p.tokens = int(std::min<int64_t>(p.tokens, (p.pixels + 255) / 256));
     return p;
 }
 

@@ -48,9 +48,11 @@ int check_cache(const char *fn, const quan_cache *c, int32_t dtype, quan::Cache 
         return report(QUAN_ERR_UNSUPPORTED, "%s: at most 65535 heads and 2^24 tokens of a page", fn);
     // (65535 * 2^24 leaves room for the comparison)
     const int64_t page_rows = int64_t(c->heads) * c->page_tokens;
-    if (page_rows > kMaxInt || page_rows * c->pages > kMaxInt || int64_t(c->table_pages) * c->page_tokens > kMaxInt ||
-        int64_t(c->sequences) * c->table_pages > kMaxInt)
-        return report(QUAN_ERR_UNSUPPORTED, "%s: the cache has 2^31 or more rows, positions or entries of its table", fn);
+    if (page_rows > kMaxInt || page_rows * c->pages > kMaxInt || int64_t(c->sequences) * c->table_pages > kMaxInt)
+        return report(QUAN_ERR_UNSUPPORTED, "%s: the cache has 2^31 or more rows or entries of its table", fn);
+    // (what a work-group adds to a position stays an int)
+    if (int64_t(c->table_pages) * c->page_tokens > int64_t(1) << 30)
+        return report(QUAN_ERR_UNSUPPORTED, "%s: a sequence has more than 2^30 positions", fn);
     if (misaligned(c->keys, 16) || misaligned(c->values, 16))
         return report(QUAN_ERR_ALIGN, "%s: the cache's keys and values must be 16-byte aligned", fn);
     if (misaligned(c->table, 4))

@@ -60,7 +60,7 @@ CACHE = [
     (dict(cache=cache(sequences=0)), E_SHAPE), (dict(cache=cache(table_pages=0)), E_SHAPE),
     (dict(cache=cache(dq=33)), E_UNSUP), (dict(cache=cache(heads=65536)), E_UNSUP),
     (dict(cache=cache(page_tokens=(1 << 24) + 1)), E_UNSUP), (dict(cache=cache(pages=1 << 27)), E_UNSUP),
-    (dict(cache=cache(table_pages=1 << 27)), E_UNSUP), (dict(cache=cache(heads=65535, page_tokens=1 << 24)), E_UNSUP),
+    (dict(cache=cache(table_pages=1 << 27)), E_UNSUP), (dict(cache=cache(table_pages=(1 << 26) + 1)), E_UNSUP), (dict(cache=cache(heads=65535, page_tokens=1 << 24)), E_UNSUP),
     (dict(cache=cache(sequences=1 << 16, table_pages=1 << 15)), E_UNSUP),
     (dict(cache=cache(keys=addr(30) + 8)), E_ALIGN), (dict(cache=cache(values=addr(31) + 4)), E_ALIGN),
     (dict(cache=cache(table=addr(34) + 2)), E_ALIGN),
