@@ -874,12 +874,15 @@ QUAN_API int quan_cache_attention(const quan_tensor *q, const quan_cache *cache,
  *              above), of `sequences` each; k_first NULL with q_first: the
  *              same as q_first, the maps being of one size.  Both NULL: the
  *              images, and sequences is N.
+ *   rest       NULL, or (bf16) a 16-byte aligned dense map like out's that
+ *              receives, for the backward pass, what the rounding of out left (16
+ *              bits a real).
  *   stats      NULL, or fp32 [heads][N*Hq*Wq][2] for the backward pass: for each
  *              query a number m in units of log 2, within 8 of its largest score
  *              (0 for a query without a key), and the sum of 2^(score - m).
  *
- * Probabilities of bf16 maps are rounded to bf16 before they meet v; everything
- * else is fp32.  out may overlap no input; it may be a slice of a map that holds
+ * Probabilities of bf16 maps are rounded to bf16 before they meet v (with rest they
+ * are split in two such numbers, so that 16 bits count); everything else is fp32.  out may overlap no input; it may be a slice of a map that holds
  * inputs in other channels.  Few queries have their keys dealt out to work-groups
  * where a workspace can be had (at most 64 MiB); a captured call that cannot have
  * it may differ in rounding.
@@ -887,7 +890,7 @@ QUAN_API int quan_cache_attention(const quan_tensor *q, const quan_cache *cache,
 QUAN_API int quan_packed_attention_forward(const quan_tensor *q, const quan_tensor *k, const quan_tensor *v,
                                            const int32_t *q_first, const int32_t *k_first, int32_t sequences,
                                            int32_t causal, float scale, int32_t heads, quan_tensor *out,
-                                           float *stats, void *stream);
+                                           void *rest, float *stats, void *stream);
 
 /*
  * Its gradients for dL/dout = dout, from what it was given and gave:
@@ -895,9 +898,10 @@ QUAN_API int quan_packed_attention_forward(const quan_tensor *q, const quan_tens
  *   dP = dout v^T,  dS = P (dP - rowsum(dout out)),  dv = P^T dout,
  *   dq = scale dS k,  dk = scale dS^T q.
  *
- * dq, dk, dv are descriptors like q, k, v (slices of one map may be passed),
- * overlapping nothing else; dk and dv are sums over the heads that share them, zero
- * for keys that no query sees.  With bf16 maps P is rounded to bf16 before it meets
+ * rest is the forward's, or NULL: row sums then take the rounded out.  dq, dk, dv are
+ * descriptors like q, k, v (slices of one map may be passed), overlapping nothing
+ * else; dk and dv are sums over the heads that share them, zero for keys that no
+ * query sees.  With bf16 maps P is rounded to bf16 before it meets
  * dout, and dS before it meets k and q.  Sums have a fixed order: deterministic.
  * Uses a workspace per (device, stream): the maps' copies where they are no whole
  * aligned chunks, 4 * heads * N*Hq*Wq bytes, and up to 200 MB for the parts of walks
@@ -906,8 +910,8 @@ QUAN_API int quan_packed_attention_forward(const quan_tensor *q, const quan_tens
 QUAN_API int quan_packed_attention_backward(const quan_tensor *q, const quan_tensor *k, const quan_tensor *v,
                                             const int32_t *q_first, const int32_t *k_first, int32_t sequences,
                                             int32_t causal, float scale, int32_t heads, const quan_tensor *out,
-                                            const float *stats, const quan_tensor *dout, quan_tensor *dq,
-                                            quan_tensor *dk, quan_tensor *dv, void *stream);
+                                            const void *rest, const float *stats, const quan_tensor *dout,
+                                            quan_tensor *dq, quan_tensor *dk, quan_tensor *dv, void *stream);
 
 /* Message describing the last failure of a quan_* call on this thread
  * ("" if none).  The pointer stays valid until the next call on the thread. */

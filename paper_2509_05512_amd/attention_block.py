@@ -77,7 +77,7 @@ class AttentionBlock:
         parts = self._parts(qkv)
         if self.causal:
             got = quan.quan_packed_attention_forward(*parts, None, self.heads, save=save)
-            return (*got, None) if save else got
+            return (got[0], *got[1]) if save else got
         return quan.quan_attention_forward(*parts, self.heads, relpos=self._relpos(), save=save)
 
     def _step(self):
@@ -111,7 +111,7 @@ class AttentionBlock:
         dqkv = torch.empty_like(qkv)
         dq, dk, dv = self._parts(dqkv)
         if self.causal:
-            quan.quan_packed_attention_backward(*self._parts(qkv), a, stats, da, None, self.heads, dq=dq, dk=dk, dv=dv)
+            quan.quan_packed_attention_backward(*self._parts(qkv), a, (stats, rest), da, None, self.heads, dq=dq, dk=dk, dv=dv)
         else:
             grads["table"] = quan.quan_attention_backward(*self._parts(qkv), a, stats, rest, da, self.heads,
                                                           relpos=self._relpos(), dq=dq, dk=dk, dv=dv)[3]

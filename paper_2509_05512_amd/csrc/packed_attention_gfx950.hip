@@ -18,14 +18,20 @@ constexpr float kAhead = 8.0f;  // probabilities of 2^8 at most
 
 struct Forward {
     PackedCall c;
-    AttnMap out;
+    AttnMap out, rest;  // (rest.data may be NULL)
     float *stats;
     int blocks, splits;
     float *part, *part_stats;  // [split][head][token][D], [split][head][token][2]; splits > 1
 };
 
-// QN: sets of 32 queries that a wave holds.
-template <typename T, int DQP, int QN>
+// QN: sets of 32 queries that a wave holds.  PARTS: bf16 numbers that a probability
+// meets v in, the second what the first leaves of it.  At inference one will do: it is
+// off by 2^-8 of a term at most, as out is of the sum once it is rounded.  In a
+// training step (with rest) there are two: the rows' sums of dout out go into every
+// dS, and with probabilities of 8 bits and the rounded out the queries' gradient was
+// 0.0025 to 0.005 of its norm off (sequences of 1600 and of 2 tokens; bf16's own
+// rounding is 0.0017).
+template <typename T, int DQP, int QN, int PARTS>
 __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(Forward f)
 {
     constexpr int DP = 4 * DQP;
@@ -169,16 +175,23 @@ __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(Forward f)
         for (int sub = 0; sub < SUBS; ++sub)
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
-                frag p[QN];
+                frag p[QN][PARTS];
 #pragma unroll
                 for (int n = 0; n < QN; ++n)
-                    p[n] = acc_frag<T>(s[n][sub], st);
+#pragma unroll
+                    for (int part = 0; part < PARTS; ++part) {
+                        if (part > 0)
+                            take_from(s[n][sub], st, p[n][part - 1]);
+                        p[n][part] = acc_frag<T>(s[n][sub], st);
+                    }
 #pragma unroll
                 for (int i = 0; i < DP / 32; ++i) {
                     const frag column = col_frag<DP>(vb, sub, st, i);
 #pragma unroll
                     for (int n = 0; n < QN; ++n)
-                        o[n][i] = mma(column, p[n], o[n][i]);
+#pragma unroll
+                        for (int part = 0; part < PARTS; ++part)
+                            o[n][i] = mma(column, p[n][part], o[n][i]);
                 }
             }
     }
@@ -227,6 +240,18 @@ __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(Forward f)
             o[n][i] *= inv;
             om.store(token, i, half, o[n][i], here);
         }
+        if constexpr (PARTS > 1) {
+            const HeadMap<T, DQP> rm(f.rest, qt.img, head, c.dq);
+#pragma unroll
+            for (int i = 0; i < DP / 32; ++i)
+#pragma unroll
+                for (int gq = 0; gq < 4; ++gq) {
+                    const int d = 32 * i + 8 * gq + 4 * half;
+                    const f32x4 v = {o[n][i][4 * gq], o[n][i][4 * gq + 1], o[n][i][4 * gq + 2], o[n][i][4 * gq + 3]};
+                    if (here)
+                        store_rest(rm.at(token, d), v, rm.valid(d, 4), rm.vec);
+                }
+        }
         if (f.stats != nullptr && half == 0 && here) {
             f.stats[2 * row] = base[n];
             f.stats[2 * row + 1] = sum[n];
@@ -266,6 +291,12 @@ template <typename T, int DQP> __global__ void __launch_bounds__(kThreads) packe
     o *= sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
     const HeadMap<T, DQP> om(f.out, qt.img, head, c.dq);
     store_quad(om.at(qt.at + query, d), o, om.valid(d, 4), om.vec);
+    if constexpr (sizeof(T) == 2) {
+        if (f.rest.data != nullptr) {
+            const HeadMap<T, DQP> rm(f.rest, qt.img, head, c.dq);
+            store_rest(rm.at(qt.at + query, d), o, rm.valid(d, 4), rm.vec);
+        }
+    }
     if (f.stats != nullptr && d == 0) {
         f.stats[2 * row] = top == -INFINITY ? 0.0f : top;
         f.stats[2 * row + 1] = sum;
@@ -285,7 +316,7 @@ int forward_splits(const PackedCall &c, DType dt, bool may_split)
     return int(std::max<int64_t>(1, std::min({(2 * kSlots + groups - 1) / groups, int64_t(tiles) / 4, room})));
 }
 
-template <typename T, int DQP> hipError_t launch(Forward f, hipStream_t s)
+template <typename T, int DQP, int PARTS> hipError_t launch(Forward f, hipStream_t s)
 {
     constexpr int kTile = Elem<T>::kTile;
     const size_t lds = size_t(4) * kTile * Lds<T, 4 * DQP>::kRow * sizeof(T);
@@ -295,27 +326,34 @@ template <typename T, int DQP> hipError_t launch(Forward f, hipStream_t s)
         const int64_t wide = packed_blocks(f.c.qs, 2 * kBlock);
         if (f.splits == 1 && wide * f.c.heads >= 512) {
             f.blocks = int(wide);
-            packed_forward_kernel<T, DQP, 2><<<unsigned(wide * f.c.heads), kThreads, lds, s>>>(f);
+            packed_forward_kernel<T, DQP, 2, PARTS><<<unsigned(wide * f.c.heads), kThreads, lds, s>>>(f);
             return hipGetLastError();
         }
     }
     const unsigned groups = unsigned(int64_t(f.blocks) * f.c.heads);
-    packed_forward_kernel<T, DQP, 1><<<groups * f.splits, kThreads, lds, s>>>(f);
+    packed_forward_kernel<T, DQP, 1, PARTS><<<groups * f.splits, kThreads, lds, s>>>(f);
     if (hipError_t e = hipGetLastError())
         return e;
     if (f.splits > 1)
         packed_join_kernel<T, DQP><<<groups * join_groups(4 * DQP), kThreads, 0, s>>>(f);
     return hipGetLastError();
 }
+template <typename T, int DQP> hipError_t launch_parts(const Forward &f, hipStream_t s)
+{
+    if constexpr (sizeof(T) == 2)
+        if (f.rest.data != nullptr)
+            return launch<T, DQP, 2>(f, s);
+    return launch<T, DQP, 1>(f, s);
+}
 template <typename T> hipError_t launch_dq(const Forward &f, hipStream_t s)
 {
     switch (padded_dq(f.c.dq)) {
     case 8:
-        return launch<T, 8>(f, s);
+        return launch_parts<T, 8>(f, s);
     case 16:
-        return launch<T, 16>(f, s);
+        return launch_parts<T, 16>(f, s);
     default:
-        return launch<T, 32>(f, s);
+        return launch_parts<T, 32>(f, s);
     }
 }
 
@@ -353,12 +391,13 @@ size_t packed_forward_extra_bytes(const PackedCall &c, DType dt)
     return splits == 1 ? 0 : size_t(splits) * c.heads * c.q_tokens() * (4 * padded_dq(c.dq) + 2) * sizeof(float);
 }
 
-hipError_t packed_forward_run(const PackedCall &c, DType dt, const AttnMap &out, float *stats, void *work, void *extra,
-                              hipStream_t s)
+hipError_t packed_forward_run(const PackedCall &c, DType dt, const AttnMap &out, void *rest, float *stats, void *work,
+                              void *extra, hipStream_t s)
 {
     Forward f;
     f.c = c;
     f.out = out;
+    f.rest = packed_dense(c, rest);
     f.stats = stats;
     f.blocks = int(packed_blocks(c.qs));
     f.splits = forward_splits(c, dt, extra != nullptr);

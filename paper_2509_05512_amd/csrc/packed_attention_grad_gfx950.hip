@@ -19,7 +19,7 @@ namespace {
 
 struct Backward {
     PackedCall c;
-    AttnMap out, dout, dq, dk, dv;
+    AttnMap out, rest, dout, dq, dk, dv;  // (rest.data may be NULL)
     const float *stats;
     float *delta;  // [heads][q_tokens]
     int q_blocks, k_blocks, q_splits, k_splits;
@@ -72,13 +72,15 @@ __global__ void __launch_bounds__(64 * kWaves * PAIR, DQP <= 16 || PAIR == 2 ? 2
     frag q[DP / 16], go[DP / 16];
     float delta = 0.0f;
     {
-        const WholeMap<T, DQP> gm(f.dout, qt.img, head), om(f.out, qt.img, head);
+        const WholeMap<T, DQP> gm(f.dout, qt.img, head), om(f.out, qt.img, head), rm(f.rest, qt.img, head);
 #pragma unroll
         for (int i = 0; i < DP / 16; ++i) {
             const int d = 16 * i + 8 * half;
             q[i] = qm.load(qt.at + query, d, q_here);
             go[i] = gm.load(qt.at + query, d, q_here);
-            const f32x8 o = to_f32(om.load(qt.at + query, d, q_here)), w = to_f32(go[i]);
+            const frag rounded = om.load(qt.at + query, d, q_here);
+            const f32x8 o = f.rest.data != nullptr ? with_rest(rounded, rm.load(qt.at + query, d, q_here)) : to_f32(rounded);
+            const f32x8 w = to_f32(go[i]);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 delta = fmaf(w[e], o[e], delta);
@@ -528,7 +530,7 @@ size_t packed_backward_work_bytes(const PackedCall &c, DType dt, const PackedGra
     const Plan p = plan(c, dt);
     size_t bytes = delta_bytes(c) + p.part_q + 2 * p.part_k;
     if (copies(c, g))
-        bytes += 3 * packed_copy_bytes(c.q_tokens(), c.heads, c.dq, dt) +
+        bytes += (g.rest != nullptr ? 4 : 3) * packed_copy_bytes(c.q_tokens(), c.heads, c.dq, dt) +
                  2 * packed_copy_bytes(c.k_tokens(), c.kv_heads, c.dq, dt);
     return bytes;
 }
@@ -538,6 +540,7 @@ hipError_t packed_backward_run(const PackedCall &c, DType dt, const PackedGradie
     Backward f;
     f.c = c;
     f.out = g.out;
+    f.rest = packed_dense(c, g.rest);
     f.dout = g.dout;
     f.dq = g.dq;
     f.dk = g.dk;
@@ -558,8 +561,9 @@ hipError_t packed_backward_run(const PackedCall &c, DType dt, const PackedGradie
     if (copies(c, g)) {
         AttnPack pack;
         pack.maps = 0;
-        for (AttnMap *m : {&f.c.q, &f.out, &f.dout})
-            packed_copy_add(pack, *m, c.images, c.qs.tokens, c.heads, c.dq, dt, at);
+        for (AttnMap *m : {&f.c.q, &f.out, &f.dout, &f.rest})
+            if (m->data != nullptr)
+                packed_copy_add(pack, *m, c.images, c.qs.tokens, c.heads, c.dq, dt, at);
         for (AttnMap *m : {&f.c.k, &f.c.v})
             packed_copy_add(pack, *m, c.images, c.ks.tokens, c.kv_heads, c.dq, dt, at);
         if (hipError_t e = attention_pack_run(pack, c.images, c.dq, dt, s))

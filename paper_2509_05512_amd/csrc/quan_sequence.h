@@ -72,15 +72,23 @@ struct PackedCall {
     constexpr int64_t q_tokens() const { return int64_t(images) * qs.tokens; }
     constexpr int64_t k_tokens() const { return int64_t(images) * ks.tokens; }
 };
-// stats [heads][q_tokens][2] or NULL, as quan_attention_forward's.
+// stats [heads][q_tokens][2] or NULL; rest (bf16) the remainder of out to 16 more
+// bits, dense like it, or NULL.
 size_t packed_forward_work_bytes(const PackedCall &c, DType dt);
 size_t packed_forward_extra_bytes(const PackedCall &c, DType dt);
-hipError_t packed_forward_run(const PackedCall &c, DType dt, const AttnMap &out, float *stats, void *work, void *extra,
-                              hipStream_t stream);
+hipError_t packed_forward_run(const PackedCall &c, DType dt, const AttnMap &out, void *rest, float *stats, void *work,
+                              void *extra, hipStream_t stream);
 struct PackedGradients {
     AttnMap out, dout, dq, dk, dv;
+    const void *rest;
     const float *stats;
 };
+// A dense map like q's.
+inline AttnMap packed_dense(const PackedCall &c, const void *data)
+{
+    const int64_t all = int64_t(c.heads) * c.dq;
+    return {data, c.qs.tokens * 4 * all, 4 * all, all, c.dq % 8 == 0, c.dq};
+}
 size_t packed_backward_work_bytes(const PackedCall &c, DType dt, const PackedGradients &g);
 hipError_t packed_backward_run(const PackedCall &c, DType dt, const PackedGradients &g, void *work, hipStream_t stream);
 // Maps that do not lie in whole aligned chunks are copied first (see AttnPack):

@@ -219,16 +219,32 @@ int check_packed(const char *fn, const quan_tensor *q, const quan_tensor *k, con
     return QUAN_OK;
 }
 
+// What the forward pass keeps for the backward one.
+int check_saved(const char *fn, const quan_tensor *q, const void *rest, const float *stats, int32_t heads,
+                const quan::PackedCall &c, Span *rest_span, Span *stats_span)
+{
+    if (rest != nullptr && q->dtype != QUAN_BF16)
+        return report(QUAN_ERR_DTYPE, "%s: rest is for bf16 maps", fn);
+    if (misaligned(rest, 16))
+        return report(QUAN_ERR_ALIGN, "%s: rest must be 16-byte aligned", fn);
+    if (misaligned(stats, 4))
+        return report(QUAN_ERR_ALIGN, "%s: stats must be 4-byte aligned", fn);
+    *rest_span = {"rest", rest, size_t(c.q_tokens()) * 4 * q->shape[2] * 2};
+    *stats_span = {"stats", stats, size_t(heads) * c.q_tokens() * 8};
+    return QUAN_OK;
+}
+
 struct PackedForward {
     quan::PackedCall c;
     quan::DType dt;
     quan::AttnMap out;
+    void *rest;
     float *stats;
 };
 hipError_t run_packed_forward(void *args, void *work, void *extra, hipStream_t s)
 {
     const PackedForward &p = *static_cast<PackedForward *>(args);
-    return quan::packed_forward_run(p.c, p.dt, p.out, p.stats, work, extra, s);
+    return quan::packed_forward_run(p.c, p.dt, p.out, p.rest, p.stats, work, extra, s);
 }
 
 struct PackedBackward {
@@ -358,8 +374,8 @@ QUAN_API int quan_cache_attention(const quan_tensor *q, const quan_cache *cache,
 
 QUAN_API int quan_packed_attention_forward(const quan_tensor *q, const quan_tensor *k, const quan_tensor *v,
                                            const int32_t *q_first, const int32_t *k_first, int32_t sequences,
-                                           int32_t causal, float scale, int32_t heads, quan_tensor *out, float *stats,
-                                           void *stream)
+                                           int32_t causal, float scale, int32_t heads, quan_tensor *out, void *rest,
+                                           float *stats, void *stream)
 {
     const char *fn = "packed_attention_forward";
     quan::clear_error();
@@ -370,15 +386,18 @@ QUAN_API int quan_packed_attention_forward(const quan_tensor *q, const quan_tens
     Span out_span;
     if (int rc = check_map(fn, "out", out, q->dtype, q->shape, &p.out, &out_span))
         return rc;
-    const Span stats_span{"stats", stats, size_t(heads) * p.c.q_tokens() * 8};
-    if (misaligned(stats, 4))
-        return report(QUAN_ERR_ALIGN, "%s: stats must be 4-byte aligned", fn);
-    for (const Span &o : {out_span, stats_span})
+    Span rest_span, stats_span;
+    if (int rc = check_saved(fn, q, rest, stats, heads, p.c, &rest_span, &stats_span))
+        return rc;
+    for (const Span &o : {out_span, rest_span, stats_span})
         if (int rc = check_alias(fn, o, {s.q, s.k, s.v, s.q_first, s.k_first}))
             return rc;
-    if (int rc = check_alias(fn, out_span, {stats_span}))
+    if (int rc = check_alias(fn, out_span, {rest_span, stats_span}))
+        return rc;
+    if (int rc = check_alias(fn, rest_span, {stats_span}))
         return rc;
     for_heads(&p.out, p.c.dq);
+    p.rest = rest;
     p.stats = stats;
     const size_t bytes = quan::packed_forward_work_bytes(p.c, p.dt), extra = quan::packed_forward_extra_bytes(p.c, p.dt);
     if (bytes == 0 && extra == 0)
@@ -389,8 +408,8 @@ QUAN_API int quan_packed_attention_forward(const quan_tensor *q, const quan_tens
 QUAN_API int quan_packed_attention_backward(const quan_tensor *q, const quan_tensor *k, const quan_tensor *v,
                                             const int32_t *q_first, const int32_t *k_first, int32_t sequences,
                                             int32_t causal, float scale, int32_t heads, const quan_tensor *out,
-                                            const float *stats, const quan_tensor *dout, quan_tensor *dq, quan_tensor *dk,
-                                            quan_tensor *dv, void *stream)
+                                            const void *rest, const float *stats, const quan_tensor *dout, quan_tensor *dq,
+                                            quan_tensor *dk, quan_tensor *dv, void *stream)
 {
     const char *fn = "packed_attention_backward";
     quan::clear_error();
@@ -411,11 +430,11 @@ QUAN_API int quan_packed_attention_backward(const quan_tensor *q, const quan_ten
         return rc;
     if (stats == nullptr)
         return report(QUAN_ERR_NULL, "%s: stats must be non-NULL", fn);
-    if (misaligned(stats, 4))
-        return report(QUAN_ERR_ALIGN, "%s: stats must be 4-byte aligned", fn);
-    const Span stats_span{"stats", stats, size_t(heads) * p.c.q_tokens() * 8};
+    Span rest_span, stats_span;
+    if (int rc = check_saved(fn, q, rest, stats, heads, p.c, &rest_span, &stats_span))
+        return rc;
     for (const Span &o : {dq_span, dk_span, dv_span})
-        if (int rc = check_alias(fn, o, {s.q, s.k, s.v, s.q_first, s.k_first, out_span, stats_span, dout_span}))
+        if (int rc = check_alias(fn, o, {s.q, s.k, s.v, s.q_first, s.k_first, out_span, rest_span, stats_span, dout_span}))
             return rc;
     if (int rc = check_alias(fn, dq_span, {dk_span, dv_span}))
         return rc;
@@ -423,6 +442,7 @@ QUAN_API int quan_packed_attention_backward(const quan_tensor *q, const quan_ten
         return rc;
     for (quan::AttnMap *m : {&p.g.out, &p.g.dout, &p.g.dq, &p.g.dk, &p.g.dv})
         for_heads(m, p.c.dq);
+    p.g.rest = rest;
     p.g.stats = stats;
     return quan::run_on_stream(stream, quan::packed_backward_work_bytes(p.c, p.dt, p.g), 0, run_packed_backward, &p, fn);
 }

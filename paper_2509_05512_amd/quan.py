@@ -90,8 +90,8 @@ SIGNATURES = {
     "quan_cache_write": (ctypes.c_int, [_vp] * 7),
     "quan_cache_read": (ctypes.c_int, [_vp] * 7),
     "quan_cache_attention": (ctypes.c_int, [_vp] * 3 + [_i32] + [_vp] * 2 + [_f32, _i32] + [_vp] * 2),
-    "quan_packed_attention_forward": (ctypes.c_int, [_vp] * 5 + [_i32, _i32, _f32, _i32] + [_vp] * 3),
-    "quan_packed_attention_backward": (ctypes.c_int, [_vp] * 5 + [_i32, _i32, _f32, _i32] + [_vp] * 7),
+    "quan_packed_attention_forward": (ctypes.c_int, [_vp] * 5 + [_i32, _i32, _f32, _i32] + [_vp] * 4),
+    "quan_packed_attention_backward": (ctypes.c_int, [_vp] * 5 + [_i32, _i32, _f32, _i32] + [_vp] * 8),
     "quan_last_error": (ctypes.c_char_p, []),
     "quan_release": (ctypes.c_int, []),
     "quan_version": (ctypes.c_char_p, []),
@@ -1122,6 +1122,14 @@ def _packed_args(q, k, v, first, heads, k_first, causal, scale):
             _ints("k_first", k_first, (n + 1,), dev), n, int(bool(causal)), float(scale), heads)
 
 
+class PackedSaved(NamedTuple):
+    """What quan_packed_attention_forward keeps for its backward pass: each query's
+    softmax statistics, float32 [heads, N H W, 2], and with bf16 maps what the
+    rounding of out left, a map like it."""
+    stats: torch.Tensor
+    rest: Optional[torch.Tensor]
+
+
 def quan_packed_attention_forward(q, k, v, first, heads, k_first=None, causal=True, scale=None, out=None, save=False):
     """Causal attention inside sequences of pixels.
 
@@ -1131,7 +1139,7 @@ def quan_packed_attention_forward(q, k, v, first, heads, k_first=None, causal=Tr
     (None: as first); heads may share keys as in quan_attention_forward.  A
     sequence's queries are the last of its keys' tokens: query i of lq sees keys j
     <= i + lk - lq, or all of them with causal=False.  Pixels of no sequence are
-    neither read nor written.  Returns out, or with save (out, stats) for
+    neither read nor written.  Returns out, or with save (out, PackedSaved) for
     quan_packed_attention_backward."""
     lib = load_library()
     args = _packed_args(q, k, v, first, heads, k_first, causal, scale)
@@ -1141,35 +1149,42 @@ def quan_packed_attention_forward(q, k, v, first, heads, k_first=None, causal=Tr
         out = empty_qmap(n, c, h, w, q.dtype, dev)
     elif out.dim() != 5 or out.device != dev:
         raise ValueError("out must be [N, 4, C, H, W] on q's device")
-    stats = torch.empty((args[-1], n * h * w, 2), dtype=torch.float32, device=dev) if save else None
+    stats = rest = None
+    if save:
+        stats = torch.empty((args[-1], n * h * w, 2), dtype=torch.float32, device=dev)
+        if q.dtype == torch.bfloat16:
+            rest = empty_qmap(n, c, h, w, q.dtype, dev)
     with _on(dev):
-        rc = lib.quan_packed_attention_forward(*args, _map_desc(out), _ptr(stats), _stream(dev))
+        rc = lib.quan_packed_attention_forward(*args, _map_desc(out), _ptr(rest), _ptr(stats), _stream(dev))
     if rc:
         _check(rc)
-    return (out, stats) if save else out
+    return (out, PackedSaved(stats, rest)) if save else out
 
 
-def quan_packed_attention_backward(q, k, v, out, stats, dout, first, heads, k_first=None, causal=True, scale=None,
+def quan_packed_attention_backward(q, k, v, out, saved, dout, first, heads, k_first=None, causal=True, scale=None,
                                    dq=None, dk=None, dv=None):
     """Gradients of quan_packed_attention_forward for dL/dout = dout, with what it
     saved.  dq, dk, dv may be slices of one map.  Returns (dq, dk, dv)."""
     lib = load_library()
+    stats, rest = saved
     args = _packed_args(q, k, v, first, heads, k_first, causal, scale)
     n, _, _, h, w = q.shape
     dev = q.device
     if stats is None or stats.shape != (args[-1], n * h * w, 2) or stats.dtype != torch.float32 \
             or not stats.is_contiguous():
         raise ValueError("stats must be the forward's, float32 [heads, N H W, 2]")
+    if rest is not None and (rest.shape != q.shape or rest.dtype != q.dtype or not is_device_layout(rest)):
+        raise ValueError("rest must be the forward's, in device layout like out")
     dq, dk, dv = (_like_map(like) if t is None else t for t, like in ((dq, q), (dk, k), (dv, v)))
-    for t in (out, stats, dout, dq, dk, dv):
-        if t.device != dev:
+    for t in (out, stats, rest, dout, dq, dk, dv):
+        if t is not None and t.device != dev:
             raise ValueError("all tensors must be on q's device")
     for t in (out, dout, dq, dk, dv):
         if t.dim() != 5:
             raise ValueError("out, dout and the gradients must be [N, 4, C, H, W]")
     with _on(dev):
-        rc = lib.quan_packed_attention_backward(*args, _map_desc(out), stats.data_ptr(), _map_desc(dout), _map_desc(dq),
-                                                _map_desc(dk), _map_desc(dv), _stream(dev))
+        rc = lib.quan_packed_attention_backward(*args, _map_desc(out), _ptr(rest), stats.data_ptr(), _map_desc(dout),
+                                                _map_desc(dq), _map_desc(dk), _map_desc(dv), _stream(dev))
     if rc:
         _check(rc)
     return dq, dk, dv

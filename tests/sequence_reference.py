@@ -5,9 +5,11 @@ u = 2^-8 is the unit roundoff of bf16.  With bf16 maps, B_i = sum_j P_ij |v_j|:
 
 cache attention (probabilities keep 16 bits: u^2 of each)
   |out error|   <= u |out| + u^2 B
-packed attention (probabilities and dS rounded to bf16 before a product)
-  |out error|   <= u (|out| + B)
-  |delta error| <= eps_i = sum |dout| u (|out| + B)     (rows' sums of dout out)
+packed attention (probabilities and dS rounded to bf16 before a product, but in a
+training step's forward pass probabilities keep 16 bits too)
+  |out error|   <= u (|out| + B)                        (inference)
+                   u |out| + u^2 B                      (a training step)
+  |delta error| <= eps_i = u^2 sum |dout| B             (rows' sums of dout out)
   |dv error|    <= u (|dv| + P^T |dout|)
   |dq error|    <= u (|dq| + scale |dS| |k|) + scale P eps |k|, dk likewise
 
@@ -118,14 +120,14 @@ def packed(q, k, v, lq, lk, causal=True, scale=None, dout=None):
             p = p / np.where(tot == 0, 1, tot)
             out, B = p @ vh, p @ np.abs(vh)
             res["out"][a:a + nq, h] = out
-            err["out"][a:a + nq, h] = U * (np.abs(out) + B)
+            err["out"][a:a + nq, h] = U * (np.abs(out) + (1.0 if dout is None else U) * B)
             size["out"] = max(size["out"], float(B.max()))
             if dout is None:
                 continue
             go = dout[a:a + nq, h]
             dp = go @ vh.T
             ds = p * (dp - (p * dp).sum(1, keepdims=True))
-            pe = p * (np.abs(go) * U * (np.abs(out) + B)).sum(1, keepdims=True)
+            pe = p * (np.abs(go) * U * U * B).sum(1, keepdims=True)
             off = abs(scale) * (U * np.abs(ds) + pe)
             terms = p * (np.abs(go) @ np.abs(vh).T + (np.abs(go) * B).sum(1, keepdims=True))
             res["dq"][a:a + nq, h] = scale * ds @ kh

@@ -16,9 +16,9 @@ def rows(t, heads):
 
 
 def step(q, k, v, do, first, heads, **kw):
-    out, stats = quan.quan_packed_attention_forward(q, k, v, first, heads, save=True, **kw)
-    grads = quan.quan_packed_attention_backward(q, k, v, out, stats, do, first, heads, **kw)
-    return (out, stats, *grads)
+    out, saved = quan.quan_packed_attention_forward(q, k, v, first, heads, save=True, **kw)
+    grads = quan.quan_packed_attention_backward(q, k, v, out, saved, do, first, heads, **kw)
+    return (out, saved.stats, *grads)
 
 
 def compare(q, k, v, do, lq, lk, heads, got, what, causal=True, scale=None, q0=0, k0=0, score=0.0):
@@ -116,9 +116,9 @@ def test_tokens_of_no_sequence(dtype, dq):
     first = ints((ref.starts(lens) + before).tolist())
     out, g = (torch.full_like(q, 3.0) for _ in range(2))
     grads = [torch.full_like(q, 3.0) for _ in range(3)]
-    out, stats = quan.quan_packed_attention_forward(q, k, v, first, heads, out=out, save=True)
-    quan.quan_packed_attention_backward(q, k, v, out, stats, do, first, heads, dq=grads[0], dk=grads[1], dv=grads[2])
-    compare(q, k, v, do, lens, lens, heads, (out, stats, *grads), "inside", q0=before, k0=before)
+    out, saved = quan.quan_packed_attention_forward(q, k, v, first, heads, out=out, save=True)
+    quan.quan_packed_attention_backward(q, k, v, out, saved, do, first, heads, dq=grads[0], dk=grads[1], dv=grads[2])
+    compare(q, k, v, do, lens, lens, heads, (out, saved.stats, *grads), "inside", q0=before, k0=before)
     for t in (out, *grads):
         assert bool((t[..., :before] == 3.0).all()) and bool((t[..., before + sum(lens):] == 3.0).all())
 
@@ -168,8 +168,9 @@ def test_sequences_out_of_order():
     q, k, v, do = (rand_map(s, 1, heads * dq, 1, total, BF) for s in range(4))
     out, a, b, c = (room[i, total:2 * total][None, None].permute(0, 3, 4, 1, 2) for i in range(4))
     for first in ([200, 100, 300, 0], [-7, 1000, 3, 2147483647], [-2147483648, 128, 128, 300], [301, 302, 400, 500]):
-        out, stats = quan.quan_packed_attention_forward(q, k, v, ints(first), heads, out=out, save=True)
-        quan.quan_packed_attention_backward(q, k, v, out, stats.zero_(), do, ints(first), heads, k_first=ints(first[::-1]),
+        out, saved = quan.quan_packed_attention_forward(q, k, v, ints(first), heads, out=out, save=True)
+        saved.stats.zero_()
+        quan.quan_packed_attention_backward(q, k, v, out, saved, do, ints(first), heads, k_first=ints(first[::-1]),
                                             dq=a, dk=b, dv=c)
     torch.cuda.synchronize()
     assert bool((room[:, :total] == 3.0).all()) and bool((room[:, 2 * total:] == 3.0).all())
@@ -224,3 +225,57 @@ def test_scores_of_any_size(dtype, scale, sign):
     got = step(q, k, v, do, ints(ref.starts(lens).tolist()), heads, scale=scale)
     most = max(float((rows(q, heads)[:, h] @ rows(k, heads)[:, h].T * scale).__abs__().max()) for h in range(heads))
     compare(q, k, v, do, lens, lens, heads, got, "scores", scale=scale, score=4 * dq * 2.0 ** -24 * most)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("dq", [16, 5])
+def test_inference_and_no_rest(dtype, dq):
+    """Without save the bound of one bf16 number per probability; gradients without
+    the rounding's rest have delta off by 2^-8 of the sums of |dout out| more."""
+    say(f"packed, inference {dtype} {dq}")
+    heads, lens = 2, [5, 300, 64]
+    q, k, v, do = (rand_map(s, 1, heads * dq, 1, sum(lens), dtype) for s in range(4))
+    first = ints(ref.starts(lens).tolist())
+    out = quan.quan_packed_attention_forward(q, k, v, first, heads)
+    want, err = ref.packed(*(rows(t, heads) for t in (q, k, v)), lens, lens)
+    ref.check(rows(out, heads), want["out"], err["out"], dtype == BF, "inference")
+    out, saved = quan.quan_packed_attention_forward(q, k, v, first, heads, save=True)
+    grads = quan.quan_packed_attention_backward(q, k, v, out, saved._replace(rest=None), do, first, heads)
+    again = quan.quan_packed_attention_backward(q, k, v, out, saved, do, first, heads)
+    assert torch.equal(grads[2], again[2])  # (dv knows nothing of delta)
+    if dtype == F32:
+        assert all(torch.equal(a, b) for a, b in zip(grads, again))
+        return
+    # dq's change is scale sum_j P_ij k_j times delta's, |delta's| <= 2^-8 sum |dout out|,
+    # and the two roundings of dS and of dq beside it
+    off = (np.abs(rows(do, heads)) * np.abs(want["out"])).sum(2, keepdims=True) * ref.U
+    res, bound = ref.packed(*(rows(t, heads) for t in (q, k, v)), lens, lens, dout=rows(do, heads))
+    most = off * np.abs(rows(k, heads)).max() / np.sqrt(4 * dq)
+    assert np.all(np.abs(rows(grads[0], heads) - res["dq"]) <= 1.01 * bound["dq"][0] + bound["dq"][1] + most)
+
+
+@pytest.mark.parametrize("dq", [16, 12, 8])
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "all"])
+def test_many_heads(dq, causal):
+    """Enough blocks for 64 queries to a wave, long ones and odd ones among them, with
+    and without what a backward pass needs; a NaN key of the last sequence's middle
+    reaches the queries behind it and no other."""
+    say(f"packed, many heads {dq} causal {causal}")
+    heads, kvh, lens = 56, 8, [600, 0, 1, 257, 700, 33]
+    total = sum(lens)
+    q, do = (rand_map(s, 1, heads * dq, 1, total, BF) for s in (1, 2))
+    k, v = (rand_map(s, 1, kvh * dq, 1, total, BF) for s in (3, 4))
+    first = ints(ref.starts(lens).tolist())
+    got = step(q, k, v, do, first, heads, causal=causal)
+    compare(q, k, v, do, lens, lens, heads, got, "many heads", causal)
+    out = quan.quan_packed_attention_forward(q, k, v, first, heads, causal=causal)
+    want, err = ref.packed(rows(q, heads), rows(k, kvh), rows(v, kvh), lens, lens, causal)
+    ref.check(rows(out, heads), want["out"], err["out"], True, "many heads, inference")
+    k = k.clone(memory_format=torch.preserve_format)
+    k[0, :, :, 0, total - 17] = float("nan")
+    hit = slice(total - 17, total) if causal else slice(total - 33, total)
+    for t in (quan.quan_packed_attention_forward(q, k, v, first, heads, causal=causal),
+              step(q, k, v, do, first, heads, causal=causal)[0]):
+        assert not bool(torch.isfinite(t[..., hit]).any())
+        assert bool(torch.isfinite(t[..., :hit.start]).all())
+        ref.check(rows(t, heads)[:hit.start], want["out"][:hit.start], (err["out"][0][:hit.start], err["out"][1]), True, "rest")

@@ -181,8 +181,8 @@ def calls(seed=0, dtype=BF):
         one = quan.quan_cache_attention(q1, cache, after, heads)
         back = torch.zeros_like(kv)
         k, v = quan.quan_cache_read(cache, back[:, :, :ckv], back[:, :, ckv:], first=first)
-        out, stats = quan.quan_packed_attention_forward(qp, k, v, first, heads, save=True)
-        return (one, back, out, *quan.quan_packed_attention_backward(qp, k, v, out, stats, do, first, heads))
+        out, saved = quan.quan_packed_attention_forward(qp, k, v, first, heads, save=True)
+        return (one, back, out, *quan.quan_packed_attention_backward(qp, k, v, out, saved, do, first, heads))
     return run
 
 

@@ -136,10 +136,10 @@ def test_cache_attention_refuses(lib, kw, code):
 
 def packed(lib, back=False, **kw):
     a = dict(q=desc(addr(0)), k=desc(addr(1)), v=desc(addr(2)), q_first=None, k_first=None, sequences=2, causal=1, scale=0.125,
-             heads=2, out=desc(addr(3)), stats=addr(5), dout=desc(addr(6)), dq=desc(addr(7)), dk=desc(addr(8)), dv=desc(addr(9)))
+             heads=2, out=desc(addr(3)), rest=addr(4), stats=addr(5), dout=desc(addr(6)), dq=desc(addr(7)), dk=desc(addr(8)), dv=desc(addr(9)))
     a.update(kw)
     first = [ref_of(a["q"]), ref_of(a["k"]), ref_of(a["v"]), a["q_first"], a["k_first"], a["sequences"], a["causal"], a["scale"],
-             a["heads"], ref_of(a["out"]), a["stats"]]
+             a["heads"], ref_of(a["out"]), a["rest"], a["stats"]]
     if back:
         rc = lib.quan_packed_attention_backward(*first, *(ref_of(a[m]) for m in ("dout", "dq", "dk", "dv")), None)
     else:
@@ -164,7 +164,9 @@ PACKED = [
     (one(k=desc(addr(1), n=1, w=7), v=desc(addr(2), n=1, w=7)), E_SHAPE), (one() | dict(q_first=addr(23) + 2), E_ALIGN),
     (one(k_first=addr(24) + 1), E_ALIGN), (one(sequences=1 << 25), E_UNSUP),
     (dict(q=desc(addr(0), strides=(1536, 384, 24, 6, 1))), E_LAYOUT), (dict(q=desc(addr(0) + 1)), E_ALIGN),
-    (dict(stats=addr(5) + 2), E_ALIGN),
+    (dict(stats=addr(5) + 2), E_ALIGN), (dict(rest=addr(4) + 8), E_ALIGN),
+    ({m: desc(addr(i), dtype=0) for i, m in ((0, "q"), (1, "k"), (2, "v"), (3, "out"), (6, "dout"), (7, "dq"), (8, "dk"),
+                                             (9, "dv"))}, E_DTYPE),
 ]
 
 
@@ -177,6 +179,7 @@ def test_packed_attention_refuses(lib, kw, code, back):
 
 @pytest.mark.parametrize("back,kw,code", [
     (False, dict(out=desc(addr(0))), E_ALIAS), (False, dict(out=desc(addr(2) + 64)), E_ALIAS), (False, dict(stats=addr(3)), E_ALIAS),
+    (False, dict(rest=addr(1)), E_ALIAS), (False, dict(rest=addr(3)), E_ALIAS), (True, dict(dk=desc(addr(4))), E_ALIAS),
     (False, one() | dict(out=desc(addr(23), n=1)), E_ALIAS),
     (False, dict(q=desc(addr(0), c_all=64), out=desc(addr(0) + 2 * 8, c_all=64)), E_ALIAS),
     (True, dict(dout=None), E_NULL), (True, dict(dq=None), E_NULL), (True, dict(dk=None), E_NULL), (True, dict(dv=None), E_NULL),
@@ -225,7 +228,7 @@ def test_binding_refuses():
         with pytest.raises(ValueError):
             quan.quan_packed_attention_forward(k, k, k, heads=2, **kw)
     with pytest.raises(ValueError):
-        quan.quan_packed_attention_backward(k, k, k, k, torch.zeros(2, 5, 2), k, None, 2)
+        quan.quan_packed_attention_backward(k, k, k, k, quan.PackedSaved(torch.zeros(2, 5, 2), None), k, None, 2)
 
 
 def test_reference_quantises():
