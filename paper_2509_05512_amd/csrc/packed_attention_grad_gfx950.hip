@@ -30,12 +30,16 @@ struct Backward {
 // two parts of every tile, so that what a wave holds fits in half of a SIMD's
 // registers; what they make of their parts they exchange through LDS.
 template <typename T, int DQP> constexpr int kPair = sizeof(T) == 2 && DQP > 16 ? 2 : 1;
+// Operands of a chain of products that are read together.  (Four of 64 reals against
+// one at a time: a training step of 7200 tokens in nine sequences, 52 us for the
+// queries' gradient and 63 for the others, 57 and 67; of 128 there are no registers.)
+template <typename T, int DP> constexpr int kBatch = sizeof(T) == 4 || DP == 32 ? 2 : DP == 64 ? 4 : 1;
 
 template <typename T, int DQP, int PAIR = kPair<T, DQP>>
 __global__ void __launch_bounds__(64 * kWaves * PAIR, DQP <= 16 || PAIR == 2 ? 2 : 1) packed_dq_kernel(Backward f)
 {
     constexpr int DP = 4 * DQP, WAVES = kWaves * PAIR;
-    typedef Stage<T, DP, 64 * WAVES> Tile;
+        typedef Stage<T, DP, 64 * WAVES> Tile;
     typedef typename Elem<T>::frag frag;
     constexpr int KT = Tile::kTokens, SUBS = KT / 32 / PAIR, MINE = DP / 32 / PAIR;  // parts, and sums' tiles, of a wave
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
@@ -72,18 +76,30 @@ __global__ void __launch_bounds__(64 * kWaves * PAIR, DQP <= 16 || PAIR == 2 ? 2
     frag q[DP / 16], go[DP / 16];
     float delta = 0.0f;
     {
-        const WholeMap<T, DQP> gm(f.dout, qt.img, head), om(f.out, qt.img, head), rm(f.rest, qt.img, head);
+        // (without a rest the map itself is read in its place, and not used)
+        const bool rest = sizeof(T) == 2 && f.rest.data != nullptr;
+        const WholeMap<T, DQP> gm(f.dout, qt.img, head), om(f.out, qt.img, head), rm(rest ? f.rest : f.out, qt.img, head);
+        frag o[DP / 16], o_rest[DP / 16];
 #pragma unroll
         for (int i = 0; i < DP / 16; ++i) {
             const int d = 16 * i + 8 * half;
             q[i] = qm.load(qt.at + query, d, q_here);
             go[i] = gm.load(qt.at + query, d, q_here);
-            const frag rounded = om.load(qt.at + query, d, q_here);
-            const f32x8 o = f.rest.data != nullptr ? with_rest(rounded, rm.load(qt.at + query, d, q_here)) : to_f32(rounded);
+            o[i] = om.load(qt.at + query, d, q_here);
+            if constexpr (sizeof(T) == 2)
+                o_rest[i] = rm.load(qt.at + query, d, q_here);
+        }
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) {
+            f32x8 x = to_f32(o[i]);
+            if constexpr (sizeof(T) == 2) {
+                const f32x8 full = with_rest(o[i], o_rest[i]);
+                x = rest ? full : x;
+            }
             const f32x8 w = to_f32(go[i]);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                delta = fmaf(w[e], o[e], delta);
+                delta = fmaf(w[e], x[e], delta);
         }
         delta = half_sum(delta);
         if (q_here && half == 0 && second == 0 && split == 0)
@@ -92,10 +108,13 @@ __global__ void __launch_bounds__(64 * kWaves * PAIR, DQP <= 16 || PAIR == 2 ? 2
     // P = 2^(s - top) inv; rows without a key, and none, have P = 0
     const float sum = q_here ? f.stats[2 * row + 1] : 0.0f;
     const bool empty = sum == 0.0f;
-    const float top = empty ? INFINITY : f.stats[2 * row];
+    float top = q_here ? f.stats[2 * row] : 0.0f;
+    top = empty ? INFINITY : top;
     const float inv = empty ? 0.0f : 1.0f / sum;
     const float minus = empty ? 0.0f : -delta * inv;
     const float scale = c.scale * kLog2e;
+    // (waited for here, or each tile of the walk would wait for the loads before it)
+    asm volatile("" : "+v"(top));
 
     f32x16 dq[MINE];
 #pragma unroll
@@ -129,9 +148,18 @@ __global__ void __launch_bounds__(64 * kWaves * PAIR, DQP <= 16 || PAIR == 2 ? 2
             if (!idle) {
                 f32x16 s = 0.0f, dp = 0.0f;
 #pragma unroll
-                for (int i = 0; i < DP / 16; ++i) {
-                    s = mma(row_frag<T, DP>(kb, sub, i), q[i], s);
-                    dp = mma(row_frag<T, DP>(vb, sub, i), go[i], dp);
+                for (int i0 = 0; i0 < DP / 16; i0 += kBatch<T, DP>) {
+                    frag kr[kBatch<T, DP>], vr[kBatch<T, DP>];
+#pragma unroll
+                    for (int i = 0; i < kBatch<T, DP>; ++i) {
+                        kr[i] = row_frag<T, DP>(kb, sub, i0 + i);
+                        vr[i] = row_frag<T, DP>(vb, sub, i0 + i);
+                    }
+#pragma unroll
+                    for (int i = 0; i < kBatch<T, DP>; ++i) {
+                        s = mma(kr[i], q[i0 + i], s);
+                        dp = mma(vr[i], go[i0 + i], dp);
+                    }
                 }
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
@@ -165,11 +193,17 @@ __global__ void __launch_bounds__(64 * kWaves * PAIR, DQP <= 16 || PAIR == 2 ? 2
                         dq[i] = mma(col_frag<DP>(kb, sub ^ 1, st, second * MINE + i), other, dq[i]);
                 }
             } else if (!idle) {
+                frag kc[2][MINE];
 #pragma unroll
                 for (int st = 0; st < 2; ++st)
 #pragma unroll
                     for (int i = 0; i < MINE; ++i)
-                        dq[i] = mma(col_frag<DP>(kb, sub, st, i), ds[st], dq[i]);
+                        kc[st][i] = col_frag<DP>(kb, sub, st, i);
+#pragma unroll
+                for (int st = 0; st < 2; ++st)
+#pragma unroll
+                    for (int i = 0; i < MINE; ++i)
+                        dq[i] = mma(kc[st][i], ds[st], dq[i]);
             }
         }
     }
@@ -223,7 +257,7 @@ template <typename T, int DQP, int PAIR = kPair<T, DQP>>
 __global__ void __launch_bounds__(64 * kWaves * PAIR, DQP <= 16 || PAIR == 2 ? 2 : 1) packed_dkv_kernel(Backward f)
 {
     constexpr int DP = 4 * DQP, WAVES = kWaves * PAIR;
-    typedef Stage<T, DP, 64 * WAVES> Tile;
+        typedef Stage<T, DP, 64 * WAVES> Tile;
     typedef typename Elem<T>::frag frag;
     constexpr int QT = Tile::kTokens, SUBS = QT / 32 / PAIR;  // parts of a tile that a wave takes
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
@@ -322,9 +356,18 @@ __global__ void __launch_bounds__(64 * kWaves * PAIR, DQP <= 16 || PAIR == 2 ? 2
             if (!idle) {
                 f32x16 s = 0.0f, dp = row_values(rw + 2 * QT, half_at, sub);  // dP - delta starts from -delta
 #pragma unroll
-                for (int i = 0; i < DP / 16; ++i) {
-                    s = mma(row_frag<T, DP>(qb, sub, i), k[i], s);
-                    dp = mma(row_frag<T, DP>(gb, sub, i), v[i], dp);
+                for (int j0 = 0; j0 < DP / 16; j0 += kBatch<T, DP>) {
+                    frag qr[kBatch<T, DP>], gr[kBatch<T, DP>];
+#pragma unroll
+                    for (int i = 0; i < kBatch<T, DP>; ++i) {
+                        qr[i] = row_frag<T, DP>(qb, sub, j0 + i);
+                        gr[i] = row_frag<T, DP>(gb, sub, j0 + i);
+                    }
+#pragma unroll
+                    for (int i = 0; i < kBatch<T, DP>; ++i) {
+                        s = mma(qr[i], k[j0 + i], s);
+                        dp = mma(gr[i], v[j0 + i], dp);
+                    }
                 }
                 const f32x16 top = row_values(rw, half_at, sub), inv = row_values(rw + QT, half_at, sub);
 #pragma unroll
@@ -369,12 +412,19 @@ __global__ void __launch_bounds__(64 * kWaves * PAIR, DQP <= 16 || PAIR == 2 ? 2
                 }
             } else if (!idle) {
 #pragma unroll
-                for (int st = 0; st < 2; ++st)
+                for (int st = 0; st < 2; ++st) {
+                    frag gc[DP / 32], qc[DP / 32];
 #pragma unroll
                     for (int i = 0; i < DP / 32; ++i) {
-                        sums[0][i] = mma(col_frag<DP>(gb, sub, st, i), p[st], sums[0][i]);
-                        sums[2 - PAIR][i] = mma(col_frag<DP>(qb, sub, st, i), ds[st], sums[2 - PAIR][i]);
+                        gc[i] = col_frag<DP>(gb, sub, st, i);
+                        qc[i] = col_frag<DP>(qb, sub, st, i);
                     }
+#pragma unroll
+                    for (int i = 0; i < DP / 32; ++i) {
+                        sums[0][i] = mma(gc[i], p[st], sums[0][i]);
+                        sums[2 - PAIR][i] = mma(qc[i], ds[st], sums[2 - PAIR][i]);
+                    }
+                }
             }
         }
     }
