@@ -817,8 +817,9 @@ QUAN_API int64_t quan_cache_row_bytes(int32_t dq, int32_t format);
  * QUAN_CACHE_E4M3: with a the largest magnitude of a row's 4*dq reals, e is the
  * least whole number >= -117 with a <= 448 * 2^e, and every real is divided by 2^e
  * and rounded once, to nearest even (but with e = 120 to at most 240, as 256 * 2^120
- * is no fp32 number); it is off by at most 2^-4 of its magnitude or 2^(e - 10).  A row with an infinity or NaN is kept as NaN, its byte 255.
- * Two tokens that go to one slot leave it undefined.
+ * is no fp32 number); it is off by at most 2^-4 of its magnitude or 2^(e - 10).  A
+ * row with an infinity or NaN is kept as NaN, its byte 255.  Two tokens that go to
+ * one slot leave it undefined.
  */
 QUAN_API int quan_cache_write(const quan_tensor *k, const quan_tensor *v, const int32_t *first,
                               const int32_t *start, const int32_t *kv_len, const quan_cache *cache,
@@ -882,10 +883,11 @@ QUAN_API int quan_cache_attention(const quan_tensor *q, const quan_cache *cache,
  *              (0 for a query without a key), and the sum of 2^(score - m).
  *
  * Probabilities of bf16 maps are rounded to bf16 before they meet v (with rest they
- * are split in two such numbers, so that 16 bits count); everything else is fp32.  out may overlap no input; it may be a slice of a map that holds
- * inputs in other channels.  Few queries have their keys dealt out to work-groups
- * where a workspace can be had (at most 64 MiB); a captured call that cannot have
- * it may differ in rounding.
+ * are split in two such numbers, so that 16 bits count); everything else is fp32.
+ * out may overlap no input; it may be a slice of a map that holds inputs in other
+ * channels.  Few queries have their keys dealt out to work-groups where a workspace
+ * can be had (at most 64 MiB); a captured call that cannot have it may differ in
+ * rounding.
  */
 QUAN_API int quan_packed_attention_forward(const quan_tensor *q, const quan_tensor *k, const quan_tensor *v,
                                            const int32_t *q_first, const int32_t *k_first, int32_t sequences,
@@ -901,11 +903,11 @@ QUAN_API int quan_packed_attention_forward(const quan_tensor *q, const quan_tens
  * rest is the forward's, or NULL: row sums then take the rounded out.  dq, dk, dv are
  * descriptors like q, k, v (slices of one map may be passed), overlapping nothing
  * else; dk and dv are sums over the heads that share them, zero for keys that no
- * query sees.  With bf16 maps P is rounded to bf16 before it meets
- * dout, and dS before it meets k and q.  Sums have a fixed order: deterministic.
- * Uses a workspace per (device, stream): the maps' copies where they are no whole
- * aligned chunks, 4 * heads * N*Hq*Wq bytes, and up to 200 MB for the parts of walks
- * that work-groups share.
+ * query sees.  With bf16 maps P is rounded to bf16 before it meets dout, and dS
+ * before it meets k and q.  Sums have a fixed order: deterministic.  Uses a
+ * workspace per (device, stream): the maps' copies where they are no whole aligned
+ * chunks, 4 * heads * N*Hq*Wq bytes, and up to 300 MB for the parts of walks that
+ * work-groups share.
  */
 QUAN_API int quan_packed_attention_backward(const quan_tensor *q, const quan_tensor *k, const quan_tensor *v,
                                             const int32_t *q_first, const int32_t *k_first, int32_t sequences,

@@ -6,6 +6,12 @@
 // many as a power of two, the row, neighbouring rows being a token's heads, which lie
 // side by side in the maps; a lane has 4 rows in flight.  The largest magnitude of a
 // row is found in its lanes' registers.
+//
+// Bound by HBM and, writing 8 bits, by the vector instructions on the way (58 % busy;
+// 2.9 waves a SIMD, waiting 52 % of their time): 16 x 1600 tokens of 8 heads of 64 bf16
+// reals written in 23.5 us, 8 sequences of up to 6400 tokens of 4 heads of 128 read in
+// 18.6, 79 MB each, of which a large copy takes 14.5 us; with one row in flight 28.6
+// and 24.4.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
