@@ -29,7 +29,7 @@ struct Forward {
     PackedCall c;
     AttnMap out, rest;  // (rest.data may be NULL)
     float *stats;
-    int blocks, splits;
+    int blocks, splits, near;
     float *part, *part_stats;  // [split][head][token][D], [split][head][token][2]; splits > 1
 };
 
@@ -52,12 +52,13 @@ __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(Forward f)
     T *k_lds = reinterpret_cast<T *>(lds_raw), *v_lds = k_lds + 2 * Tile::kElems;
 
     const PackedCall &c = f.c;
-    // heads side by side, so that each of 8 (or a divisor) stays on an XCD; the
-    // blocks that see most keys first
-    const int head = blockIdx.x % c.heads, kv_head = head / (c.heads / c.kv_heads);
-    // (of the shares of walks all first ones, then all second ones: in between, those
-    // that are none would leave the same compute units idle)
-    const int id = blockIdx.x / c.heads, split = id / f.blocks;
+    // the blocks that see most keys first; of the shares of walks all first ones, then
+    // all second ones: in between, those that are none would leave the same compute
+    // units idle
+    const auto [head, id] = unit_of(blockIdx.x, c.heads, f.near);
+    const int kv_head = head / (c.heads / c.kv_heads), split = id / f.blocks;
+    if (split >= f.splits)
+        return;
     const Place b = place_of<SIZE, KT, false>(c, id - split * f.blocks, f.splits);
     const Tokens &qt = b.q, &kt = b.k;
     const Walk &walk = b.walk;
@@ -275,7 +276,9 @@ template <typename T, int DQP> __global__ void __launch_bounds__(kThreads) packe
     constexpr int DP = 4 * DQP, KT = Elem<T>::kTile, kLanes = DP / 4, kGroups = join_groups(DP);
     __shared__ int counts[kWaves];
     const PackedCall &c = f.c;
-    const int head = blockIdx.x % c.heads, id = blockIdx.x / c.heads;
+    const auto [head, id] = unit_of(blockIdx.x, c.heads, f.near);
+    if (id >= f.blocks * kGroups)
+        return;
     const Block b = locate(c.qs, id / kGroups, counts);
     const Tokens qt = tokens_of(c.qs, c.qs.first, b.seq), kt = tokens_of(c.ks, c.ks.first, b.seq);
     const int query = b.at + id % kGroups * (kThreads / kLanes) + threadIdx.x / kLanes, d = 4 * (threadIdx.x % kLanes);
@@ -335,16 +338,16 @@ template <typename T, int DQP, int PARTS> hipError_t launch(Forward f, hipStream
         const int64_t wide = packed_blocks(f.c.qs, 2 * kBlock);
         if (f.splits == 1 && wide * f.c.heads >= 512) {
             f.blocks = int(wide);
-            packed_forward_kernel<T, DQP, 2, PARTS><<<unsigned(wide * f.c.heads), kThreads, lds, s>>>(f);
+            packed_forward_kernel<T, DQP, 2, PARTS><<<unsigned(unit_blocks(wide, f.c.heads, f.near)), kThreads, lds, s>>>(f);
             return hipGetLastError();
         }
     }
-    const unsigned groups = unsigned(int64_t(f.blocks) * f.c.heads);
-    packed_forward_kernel<T, DQP, 1, PARTS><<<groups * f.splits, kThreads, lds, s>>>(f);
+    const auto grid = [&](int64_t ids) { return unsigned(unit_blocks(ids, f.c.heads, f.near)); };
+    packed_forward_kernel<T, DQP, 1, PARTS><<<grid(int64_t(f.blocks) * f.splits), kThreads, lds, s>>>(f);
     if (hipError_t e = hipGetLastError())
         return e;
     if (f.splits > 1)
-        packed_join_kernel<T, DQP><<<groups * join_groups(4 * DQP), kThreads, 0, s>>>(f);
+        packed_join_kernel<T, DQP><<<grid(int64_t(f.blocks) * join_groups(4 * DQP)), kThreads, 0, s>>>(f);
     return hipGetLastError();
 }
 template <typename T, int DQP> hipError_t launch_parts(const Forward &f, hipStream_t s)
@@ -422,6 +425,7 @@ hipError_t packed_forward_run(const PackedCall &c, DType dt, const AttnMap &out,
         if (hipError_t e = attention_pack_run(pack, c.images, c.dq, dt, s))
             return e;
     }
+    f.near = near_heads(f.c.q, c.heads, c.dq, dt == DType::BF16 ? 2 : 4);
     return dt == DType::BF16 ? launch_dq<__bf16>(f, s) : launch_dq<float>(f, s);
 }
 

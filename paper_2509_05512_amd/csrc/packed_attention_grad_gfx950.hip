@@ -28,7 +28,7 @@ struct Backward {
     AttnMap out, rest, dout, dq, dk, dv;  // (rest.data may be NULL)
     const float *stats;
     float *delta;  // [heads][q_tokens]
-    int q_blocks, k_blocks, q_splits, k_splits;
+    int q_blocks, k_blocks, q_splits, k_splits, q_near, k_near;
     float *part_q, *part_k, *part_v;  // [split][head][token][D] where walks are shared
 };
 
@@ -54,8 +54,10 @@ __global__ void __launch_bounds__(64 * kWaves * PAIR, DQP <= 16 || PAIR == 2 ? 2
     T *k_lds = reinterpret_cast<T *>(lds_raw), *v_lds = k_lds + 2 * Tile::kElems;
 
     const PackedCall &c = f.c;
-    const int head = blockIdx.x % c.heads, kv_head = head / (c.heads / c.kv_heads);
-    const int id = blockIdx.x / c.heads, split = id / f.q_blocks;
+    const auto [head, id] = unit_of(blockIdx.x, c.heads, f.q_near);
+    const int kv_head = head / (c.heads / c.kv_heads), split = id / f.q_blocks;
+    if (split >= f.q_splits)
+        return;
     const Place b = place_of<kBlock, KT, false>(c, id - split * f.q_blocks, f.q_splits);
     const Tokens &qt = b.q, &kt = b.k;
     const Walk &walk = b.walk;
@@ -273,8 +275,10 @@ __global__ void __launch_bounds__(64 * kWaves * PAIR, DQP <= 16 || PAIR == 2 ? 2
     T *q_lds = reinterpret_cast<T *>(rows + 6 * QT), *g_lds = q_lds + 2 * Tile::kElems;
 
     const PackedCall &c = f.c;
-    const int group = c.heads / c.kv_heads, kv_head = blockIdx.x % c.kv_heads;
-    const int id = blockIdx.x / c.kv_heads, split = id / f.k_blocks;
+    const auto [kv_head, id] = unit_of(blockIdx.x, c.kv_heads, f.k_near);
+    const int group = c.heads / c.kv_heads, split = id / f.k_blocks;
+    if (split >= f.k_splits)
+        return;
     const Place b = place_of<kBlock, QT, true>(c, id - split * f.k_blocks, f.k_splits);
     const Tokens &qt = b.q, &kt = b.k;
     const Walk &walk = b.walk;
@@ -483,7 +487,9 @@ template <typename T, int DQP> __global__ void __launch_bounds__(kThreads) packe
     const PackedCall &c = f.c;
     const bool keys = int(blockIdx.x) >= of_queries;
     const int heads = keys ? c.kv_heads : c.heads;
-    const int head = (blockIdx.x - (keys ? of_queries : 0)) % heads, id = (blockIdx.x - (keys ? of_queries : 0)) / heads;
+    const auto [head, id] = unit_of(blockIdx.x - (keys ? of_queries : 0), heads, keys ? f.k_near : f.q_near);
+    if (id >= (keys ? f.k_blocks : f.q_blocks) * kGroups)
+        return;
     const Sequences &mine = keys ? c.ks : c.qs;
     const Block b = locate(mine, id / kGroups, counts);
     const Tokens qt = tokens_of(c.qs, c.qs.first, b.seq), kt = tokens_of(c.ks, c.ks.first, b.seq), t = keys ? kt : qt;
@@ -516,16 +522,17 @@ template <typename T, int DQP> hipError_t launch(const Backward &f, hipStream_t 
 {
     constexpr int kTile = Elem<T>::kTile;
     const size_t lds = size_t(4) * kTile * Lds<T, 4 * DQP>::kRow * sizeof(T);
-    const unsigned q_groups = unsigned(int64_t(f.q_blocks) * f.c.heads), k_groups = unsigned(int64_t(f.k_blocks) * f.c.kv_heads);
-    packed_dq_kernel<T, DQP><<<q_groups * f.q_splits, 64 * kWaves * kPair<T, DQP>, lds, s>>>(f);
+    const auto q_grid = [&](int64_t each) { return unsigned(unit_blocks(each * f.q_blocks, f.c.heads, f.q_near)); };
+    const auto k_grid = [&](int64_t each) { return unsigned(unit_blocks(each * f.k_blocks, f.c.kv_heads, f.k_near)); };
+    packed_dq_kernel<T, DQP><<<q_grid(f.q_splits), 64 * kWaves * kPair<T, DQP>, lds, s>>>(f);
     if (hipError_t e = hipGetLastError())
         return e;
     packed_dkv_kernel<T, DQP>
-        <<<k_groups * f.k_splits, 64 * kWaves * kPair<T, DQP>, lds + 6 * kTile * sizeof(float), s>>>(f);
+        <<<k_grid(f.k_splits), 64 * kWaves * kPair<T, DQP>, lds + 6 * kTile * sizeof(float), s>>>(f);
     if (hipError_t e = hipGetLastError())
         return e;
-    const unsigned of_queries = f.q_splits > 1 ? q_groups * join_groups(4 * DQP) : 0;
-    const unsigned of_keys = f.k_splits > 1 ? k_groups * join_groups(4 * DQP) : 0;
+    const unsigned of_queries = f.q_splits > 1 ? q_grid(join_groups(4 * DQP)) : 0;
+    const unsigned of_keys = f.k_splits > 1 ? k_grid(join_groups(4 * DQP)) : 0;
     if (of_queries + of_keys > 0)
         packed_sum_kernel<T, DQP><<<of_queries + of_keys, kThreads, 0, s>>>(f, int(of_queries));
     return hipGetLastError();
@@ -625,6 +632,8 @@ hipError_t packed_backward_run(const PackedCall &c, DType dt, const PackedGradie
         if (hipError_t e = attention_pack_run(pack, c.images, c.dq, dt, s))
             return e;
     }
+    f.q_near = near_heads(f.c.q, c.heads, c.dq, dt == DType::BF16 ? 2 : 4);
+    f.k_near = near_heads(f.c.k, c.kv_heads, c.dq, dt == DType::BF16 ? 2 : 4);
     return dt == DType::BF16 ? launch_dq<__bf16>(f, s) : launch_dq<float>(f, s);
 }
 

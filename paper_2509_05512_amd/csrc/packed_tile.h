@@ -47,6 +47,35 @@ template <int SIZE = kBlock> __device__ __forceinline__ Block locate(const Seque
     return {seq, block < 0 || block > s.tokens / SIZE ? s.tokens : block * SIZE};
 }
 
+// The work-group's head and its number among that head's.  Work-groups go round the
+// 8 XCDs, and each XCD has an L2 of its own with lines of 128 bytes, in which a map has
+// the same component of up to 4 or 8 heads side by side: `near` such heads go one after
+// another to one XCD, other heads and other blocks to others.  (7200 tokens in nine
+// sequences, 8 heads of 64 bf16 reals: 41 and 50 us for the queries' and the keys'
+// gradient, 50 and 62 with every head on an XCD of its own, which read 186 and 247 MB
+// from beyond its L2 for maps of 30.)
+struct Unit {
+    int head, id;
+};
+__device__ __forceinline__ Unit unit_of(int block, int heads, int near)
+{
+    const int turn = block / 8, set = turn / near * 8 + block % 8, sets = heads / near;
+    return {set % sets * near + turn % near, set / sets};
+}
+// Work-groups of a launch with `ids` numbers; some at the end have larger ones.
+inline int64_t unit_blocks(int64_t ids, int heads, int near)
+{
+    return (ids * (heads / near) + 7) / 8 * 8 * near;
+}
+// Heads that share lines of a map whose elements have `size` bytes.
+inline int near_heads(const AttnMap &m, int heads, int dq, int size)
+{
+    int near = 1;
+    while (m.s_h == dq && heads % (2 * near) == 0 && 2 * near * dq * size <= 128)
+        near *= 2;
+    return near;
+}
+
 // Sum and maximum over a wave.
 #define QUAN_DPP(v, ctrl) __builtin_amdgcn_update_dpp(0, v, ctrl, 0xf, 0xf, false)
 __device__ __forceinline__ float wave_sum(float x)

@@ -210,7 +210,9 @@ int check_packed(const char *fn, const quan_tensor *q, const quan_tensor *k, con
     c->dq = int(dq);
     c->causal = causal == 1;
     c->scale = scale;
-    if (quan::packed_blocks(c->qs) > kMaxGroups / heads || quan::packed_blocks(c->ks) > kMaxGroups / c->kv_heads ||
+    // (work-groups of 512 lanes, in whole turns of the XCDs)
+    constexpr int64_t kMost = kMaxLanes / 512 - 128;
+    if (quan::packed_blocks(c->qs) > kMost / heads || quan::packed_blocks(c->ks) > kMost / c->kv_heads ||
         c->q_tokens() > kMaxInt * 4 / heads)
         return report(QUAN_ERR_UNSUPPORTED, "%s: too many work-groups", fn);
     for (quan::AttnMap *m : {&c->q, &c->k, &c->v})

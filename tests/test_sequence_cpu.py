@@ -162,7 +162,7 @@ PACKED = [
     (dict(scale=math.nan), E_SHAPE), (dict(causal=2), E_SHAPE), (dict(causal=-1), E_SHAPE), (dict(sequences=0), E_SHAPE),
     (dict(sequences=3), E_SHAPE), (dict(q_first=addr(23)), E_SHAPE), (dict(k_first=addr(23)), E_NULL),
     (one(k=desc(addr(1), n=1, w=7), v=desc(addr(2), n=1, w=7)), E_SHAPE), (one() | dict(q_first=addr(23) + 2), E_ALIGN),
-    (one(k_first=addr(24) + 1), E_ALIGN), (one(sequences=1 << 25), E_UNSUP),
+    (one(k_first=addr(24) + 1), E_ALIGN), (one(sequences=1 << 25), E_UNSUP), (one(sequences=1 << 22), E_UNSUP),
     (dict(q=desc(addr(0), strides=(1536, 384, 24, 6, 1))), E_LAYOUT), (dict(q=desc(addr(0) + 1)), E_ALIGN),
     (dict(stats=addr(5) + 2), E_ALIGN), (dict(rest=addr(4) + 8), E_ALIGN),
     ({m: desc(addr(i), dtype=0) for i, m in ((0, "q"), (1, "k"), (2, "v"), (3, "out"), (6, "dout"), (7, "dq"), (8, "dk"),
