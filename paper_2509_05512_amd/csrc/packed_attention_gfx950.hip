@@ -8,9 +8,9 @@
 //
 // Where there are 512 blocks of 256 queries, a wave has 64: a tile's operands are read
 // from LDS once for two products.  (Nine sequences of up to 6400 tokens, 8 heads of 64
-// reals on 2: 187 us, 717 TFLOP/s, 245 with 32 queries a wave and the blocks in order.)
-// Its SIMDs are then 30 % of the time in matrix instructions and 46 to 56 % in vector
-// ones, with two waves each that overlap little.  No faster, each on its own: scores
+// reals on 2: 183 us, 731 TFLOP/s, 245 with 32 queries a wave and the blocks in order.)
+// Its SIMDs are then 31 % of the time in matrix instructions and 54 % in vector
+// ones, with two waves each that overlap little (waiting 29 %).  No faster, each on its own: scores
 // without the running maximum where a tile's sum shows that none is far ahead (a fifth
 // fewer vector instructions), raised wave priorities for either half of a tile, walks
 // that begin in different places, tiles dealt to two sets of waves in a work-group.

@@ -8,11 +8,11 @@
 // blocks of keys and walks over the queries that see them, head by head of those
 // that share them (dK, dV).
 //
-// 7200 tokens in nine sequences, 8 heads of 64 reals: 50 us and 62; one of 6400, 4 heads
-// of 128 on 2: 121 and 131, and 21 to sum the parts of shared walks, with matrix units
-// 23 % busy.  Their waves, two a SIMD, wait 41 to 67 % of their time, for LDS and for
-// each other at a tile's barrier, and longest where a work-group starts and ends (8 us
-// for a walk of one tile).
+// 7200 tokens in nine sequences, 8 heads of 64 reals: 41 us and 50; one of 6400, 4 heads
+// of 128 on 2: 118 and 130, and 21 to sum the parts of shared walks, with matrix units
+// 20 and 24 % busy.  Their waves, one to two a SIMD, wait 36 to 44 % of their time, for
+// LDS and for each other at a tile's barrier; a walk of one tile takes 8 us, and the
+// longest walks of the nine sequences three times the mean.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -37,8 +37,8 @@ struct Backward {
 // registers; what they make of their parts they exchange through LDS.
 template <typename T, int DQP> constexpr int kPair = sizeof(T) == 2 && DQP > 16 ? 2 : 1;
 // Operands of a chain of products that are read together.  (Four of 64 reals against
-// one at a time: a training step of 7200 tokens in nine sequences, 52 us for the
-// queries' gradient and 63 for the others, 57 and 67; of 128 there are no registers.)
+// one at a time, 7200 tokens in nine sequences: the keys' gradient 62 us and 66; of 128
+// there are no registers.)
 template <typename T, int DP> constexpr int kBatch = sizeof(T) == 4 || DP == 32 ? 2 : DP == 64 ? 4 : 1;
 
 template <typename T, int DQP, int PAIR = kPair<T, DQP>>
