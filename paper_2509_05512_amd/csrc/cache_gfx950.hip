@@ -34,6 +34,18 @@ struct Copy {
 };
 constexpr int kNoSequence = -2, kNoSlot = -1;
 
+// The largest of neighbouring lanes' numbers, 1, 2, 4, 8 or 16 of them (an 8-bit row has
+// 16 at most).
+__device__ __forceinline__ unsigned lanes_max(unsigned x, int lanes)
+{
+    const auto step = [&](unsigned y, int of) { x = lanes > of ? max(x, y) : x; };
+    step(__builtin_amdgcn_update_dpp(0, int(x), 0xB1, 0xf, 0xf, false), 1);   // lane ^ 1
+    step(__builtin_amdgcn_update_dpp(0, int(x), 0x4E, 0xf, 0xf, false), 2);   // lane ^ 2
+    step(__builtin_amdgcn_update_dpp(0, int(x), 0x141, 0xf, 0xf, false), 4);  // 7 - lane of 8
+    step(__builtin_amdgcn_update_dpp(0, int(x), 0x140, 0xf, 0xf, false), 8);  // 15 - lane of 16
+    return x;
+}
+
 // The sequence of pixel `token` of a packed map: the last that starts at or
 // before it.
 __device__ __forceinline__ int find_sequence(const int32_t *first, int count, int token)
@@ -198,13 +210,12 @@ __global__ void __launch_bounds__(kThreads) cache_copy_kernel(Copy p)
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
                         top = max(top, __float_as_uint(v[u][e]) & 0x7fffffffu);
-                    for (int l = 1; l < p.lanes; l *= 2)
-                        top = max(top, unsigned(__shfl_xor(int(top), l, 64)));
+                    top = lanes_max(top, p.lanes);
                     const unsigned byte = factor_byte(top);
                     const float by = inverse_of(byte), most = byte == kLastByte ? 240.0f : 448.0f;
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        v[u][e] = fminf(fmaxf(v[u][e] * by, -most), most);
+                        v[u][e] = __builtin_amdgcn_fmed3f(v[u][e] * by, -most, most);
                     u32x2 d = {unsigned(to_e4m3(v[u][0], v[u][1], v[u][2], v[u][3])),
                                unsigned(to_e4m3(v[u][4], v[u][5], v[u][6], v[u][7]))};
                     if (byte == 255u)
