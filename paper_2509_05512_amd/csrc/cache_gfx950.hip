@@ -7,10 +7,10 @@
 // side by side in the maps; a lane has 4 rows in flight.  The largest magnitude of a
 // row is found in its lanes' registers.
 //
-// Bound by HBM and, writing 8 bits, by the vector instructions on the way (58 % busy;
-// 2.9 waves a SIMD, waiting 52 % of their time): 16 x 1600 tokens of 8 heads of 64 bf16
-// reals written in 23.5 us, 8 sequences of up to 6400 tokens of 4 heads of 128 read in
-// 18.6, 79 MB each, of which a large copy takes 14.5 us; with one row in flight 28.6
+// Bound by HBM and, writing 8 bits, by the vector instructions on the way (51 % busy;
+// 2.3 waves a SIMD, waiting 48 % of their time): 16 x 1600 tokens of 8 heads of 64 bf16
+// reals written in 21.0 us, 8 sequences of up to 6400 tokens of 4 heads of 128 read in
+// 18.3, 79 MB each, of which a large copy takes 14.5 us; with one row in flight 28.6
 // and 24.4.
 #include <hip/hip_runtime.h>
 
@@ -247,9 +247,13 @@ Copy copy_plan(const CacheCopy &c)
     p.lanes = 1;
     while (p.lanes * 8 * cache_elem_size(c.cache.form) < c.cache.row_bytes)
         p.lanes *= 2;
-    // so many tokens that each lane has kAhead rows
+    // so many tokens that each lane has kAhead rows, or twice as many where that leaves
+    // four work-groups to a compute unit (16 x 1600 tokens of 8 heads written: 22.3 us
+    // against 23.2, 24.2 with four times as many; 25600 of 4 heads read: 19.1, 19.7, 20.1)
     const int rows = kAhead * kThreads / p.lanes;
     p.tokens = std::max(1, std::min(kTokens, rows / (2 * c.cache.heads)));
+    if (2 * p.tokens <= kTokens && p.pixels / (2 * p.tokens) >= 1024)
+        p.tokens *= 2;
     // (few tokens: over the chip)
     p.tokens = int(std::min<int64_t>(p.tokens, (p.pixels + 255) / 256));
     return p;
