@@ -1,16 +1,17 @@
 // A paged cache of keys and values on gfx950: new tokens into its pages, in 8 bits
 // with a power of two per row or as they are, and back.
 //
-// A work-group takes some tokens and finds their slots first, a thread for each.  Then
+// A work-group takes some tokens and finds their slots first, and where they lie in the
+// maps, a thread for each.  Then
 // a lane takes 8 reals of a row (a token's head of k or v) and neighbouring lanes, as
 // many as a power of two, the row, neighbouring rows being a token's heads, which lie
 // side by side in the maps; a lane has 4 rows in flight.  The largest magnitude of a
 // row is found in its lanes' registers.
 //
-// Bound by HBM and, writing 8 bits, by the vector instructions on the way (51 % busy;
-// 2.3 waves a SIMD, waiting 48 % of their time): 16 x 1600 tokens of 8 heads of 64 bf16
-// reals written in 21.0 us, 8 sequences of up to 6400 tokens of 4 heads of 128 read in
-// 18.3, 79 MB each, of which a large copy takes 14.5 us; with one row in flight 28.6
+// Bound by HBM and, writing 8 bits, by the vector instructions on the way (45 % busy;
+// 2.2 waves a SIMD, waiting 54 % of their time): 16 x 1600 tokens of 8 heads of 64 bf16
+// reals written in 19.2 us, 8 sequences of up to 6400 tokens of 4 heads of 128 read in
+// 16.2, 79 MB each, of which a large copy takes 14.5 us; with one row in flight 28.6
 // and 24.4.
 #include <hip/hip_runtime.h>
 
@@ -82,6 +83,7 @@ __global__ void __launch_bounds__(kThreads) cache_copy_kernel(Copy p)
     constexpr bool E4M3 = F == CacheForm::E4M3;
     typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
     __shared__ int firsts[kFirsts], slots[kTokens];
+    __shared__ T *maps[kTokens][2];  // where a token's keys and values lie
     const CacheCopy &c = p.c;
     const Cache &cache = c.cache;
     const int32_t *first = c.seq.first;
@@ -117,6 +119,11 @@ __global__ void __launch_bounds__(kThreads) cache_copy_kernel(Copy p)
             }
         }
         slots[threadIdx.x] = some ? slot : kNoSequence;
+        const int img = first == nullptr ? seq : 0, in_map = pixel - img * c.seq.tokens;
+        for (int side = 0; side < 2; ++side) {
+            const AttnMap &m = side ? c.v : c.k;
+            maps[threadIdx.x][side] = static_cast<T *>(const_cast<void *>(m.data)) + img * m.s_n + in_map * m.s_t;
+        }
     }
     __syncthreads();
 
@@ -124,13 +131,15 @@ __global__ void __launch_bounds__(kThreads) cache_copy_kernel(Copy p)
     const int rows = count * 2 * cache.heads, real = 8 * lane;
     const bool here = real < 4 * cache.dq;
     const int comp = here ? real / cache.dq : 0, ch = here ? real - comp * cache.dq : 0;
+    const int64_t in_k = comp * c.k.s_p + ch, in_v = comp * c.v.s_p + ch;  // the lane's reals of a token's head
     const bool whole = c.k.vec && c.v.vec && cache.dq % 8 == 0;  // 8 reals lie side by side, aligned
     // bytes of the lane's 8 elements in a row, and how many of them it has
     constexpr int kBytes = 8 * cache_elem_size(F);
     const int at_byte = lane * kBytes;
+    const auto row_at = [&](int i) { return uint64_t(unsigned(i)) * unsigned(cache.row_bytes) + at_byte; };
     for (int r0 = threadIdx.x / p.lanes; r0 < rows; r0 += per * kAhead) {
         T *x[kAhead];
-        int64_t at[kAhead];
+        int at[kAhead];  // (a cache has fewer than 2^31 rows)
         bool value[kAhead];
         int slot[kAhead];
 #pragma unroll
@@ -139,11 +148,8 @@ __global__ void __launch_bounds__(kThreads) cache_copy_kernel(Copy p)
             const int side = fast_div(row, p.by_heads), head = row - side * cache.heads;  // token * 2 + (1 for v)
             value[u] = side & 1;
             slot[u] = r0 + u * per < rows ? slots[side >> 1] : kNoSequence;
-            at[u] = int64_t(slot[u]) + int64_t(head) * cache.page_tokens;
-            const int pixel = pixel0 + (side >> 1), img = first == nullptr ? fast_div(pixel, p.by_tokens) : 0;
-            const AttnMap &m = value[u] ? c.v : c.k;
-            x[u] = static_cast<T *>(const_cast<void *>(m.data)) + img * m.s_n + int64_t(pixel - img * c.seq.tokens) * m.s_t +
-                   int64_t(head) * cache.dq;
+            at[u] = max(slot[u], 0) + head * cache.page_tokens;
+            x[u] = maps[side >> 1][side & 1] + head * cache.dq;
         }
         f32x8 v[kAhead];
         if constexpr (READ) {
@@ -158,7 +164,7 @@ __global__ void __launch_bounds__(kThreads) cache_copy_kernel(Copy p)
                 f[u] = frag{};
                 if (slot[u] < 0)
                     continue;
-                const unsigned char *row = (value[u] ? cache.values : cache.keys) + at[u] * cache.row_bytes + at_byte;
+                const unsigned char *row = (value[u] ? cache.values : cache.keys) + row_at(at[u]);
                 if constexpr (E4M3) {
                     if (at_byte < cache.row_bytes)
                         d[u] = *reinterpret_cast<const u32x2 *>(row);
@@ -182,7 +188,7 @@ __global__ void __launch_bounds__(kThreads) cache_copy_kernel(Copy p)
                 if (slot[u] == kNoSequence)
                     continue;
                 if (whole) {
-                    store_chunk<T>(x[u] + comp * (value[u] ? c.v : c.k).s_p + ch, v[u], here ? 8 : 0, true);
+                    store_chunk<T>(x[u] + (value[u] ? in_v : in_k), v[u], here ? 8 : 0, true);
                 } else {
                     for_reals(value[u] ? c.v : c.k, cache.dq, real, [&](int e, int64_t off) {
                         if (off >= 0)
@@ -194,7 +200,7 @@ __global__ void __launch_bounds__(kThreads) cache_copy_kernel(Copy p)
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 if (whole) {
-                    v[u] = to_f32(load_chunk<T>(x[u] + comp * (value[u] ? c.v : c.k).s_p + ch, here ? 8 : 0, true));
+                    v[u] = to_f32(load_chunk<T>(x[u] + (value[u] ? in_v : in_k), here ? 8 : 0, true));
                 } else {
                     for_reals(value[u] ? c.v : c.k, cache.dq, real, [&](int e, int64_t off) {
                         const float t = float(x[u][off >= 0 ? off : 0]);
@@ -204,7 +210,7 @@ __global__ void __launch_bounds__(kThreads) cache_copy_kernel(Copy p)
             }
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                unsigned char *row = (value[u] ? cache.values : cache.keys) + at[u] * cache.row_bytes + at_byte;
+                unsigned char *row = (value[u] ? cache.values : cache.keys) + row_at(at[u]);
                 if constexpr (E4M3) {
                     unsigned top = 0;
 #pragma unroll
