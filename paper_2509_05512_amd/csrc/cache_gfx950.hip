@@ -2,11 +2,10 @@
 // with a power of two per row or as they are, and back.
 //
 // A work-group takes some tokens and finds their slots first, and where they lie in the
-// maps, a thread for each.  Then
-// a lane takes 8 reals of a row (a token's head of k or v) and neighbouring lanes, as
-// many as a power of two, the row, neighbouring rows being a token's heads, which lie
-// side by side in the maps; a lane has 4 rows in flight.  The largest magnitude of a
-// row is found in its lanes' registers.
+// maps, a thread for each.  Then a lane takes 8 reals of a row (a token's head of k or
+// v) and neighbouring lanes, as many as a power of two, the row, neighbouring rows being
+// a token's heads, which lie side by side in the maps; a lane has 4 rows in flight.  The
+// largest magnitude of a row is found in its lanes' registers.
 //
 // Bound by HBM and, writing 8 bits, by the vector instructions on the way (45 % busy;
 // 2.2 waves a SIMD, waiting 54 % of their time): 16 x 1600 tokens of 8 heads of 64 bf16
