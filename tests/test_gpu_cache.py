@@ -233,3 +233,32 @@ def test_unaligned_and_wide_maps():
             y, e = ref.quantise(x)
             assert np.array_equal(ref.rows_of(got.float().cpu().numpy().astype(np.float64), heads), y * 2.0 ** (e - 127.0)[..., None])
         assert bool((to[:, :, :3] == 3.0).all()) and bool((to[:, :, 19:21] == 3.0).all())
+
+
+@pytest.mark.parametrize("dtype,form", [(BF, E4M3), (BF, BF), (F32, E4M3)], ids=["bf16-e4m3", "bf16", "fp32-e4m3"])
+@pytest.mark.parametrize("dq,heads", [(16, 8), (24, 5)])
+def test_many_tokens(dtype, form, dq, heads):
+    """More tokens than go to a work-group of few: a call leaves what calls for 900 of
+    its tokens at a time leave, bit for bit, written and read, as tokens do not
+    depend on each other; sequences, pages and the last work-group end anywhere."""
+    say(f"cache, many tokens {dtype} {form} {dq} {heads}")
+    lens, page = [9001, 0, 5003, 13, 2600, 7777, 4001, 4999], 24
+    table, pages = make_table(np.random.default_rng(5), lens, page)
+    first = ref.starts(lens).tolist()
+    k, v = (rand_map(s, 1, heads * dq, 1, sum(lens), dtype, spread=20) for s in (1, 2))
+    whole, pieces = (clear(quan.empty_cache(pages, page, heads, dq, table, form)) for _ in range(2))
+    quan.quan_cache_write(whole, k, v, first=ints(first))
+    back = [quan.empty_qmap(1, heads * dq, 1, sum(lens), dtype, torch.device("cuda", 0)) for _ in range(2)]
+    quan.quan_cache_read(whole, *back, first=ints(first))
+    for a in range(0, sum(lens), 900):
+        b = min(a + 900, sum(lens))
+        part = [min(max(f, a), b) - a for f in first]
+        start = ints([max(a - f, 0) for f in first[:-1]])
+        quan.quan_cache_write(pieces, k[..., a:b], v[..., a:b], start, first=ints(part))
+        got = [quan.empty_qmap(1, heads * dq, 1, b - a, dtype, torch.device("cuda", 0)) for _ in range(2)]
+        quan.quan_cache_read(whole, *got, start, first=ints(part))
+        assert all(torch.equal(x, y[..., a:b]) for x, y in zip(got, back)), a
+    for x, y in zip(whole[:4], pieces[:4]):
+        assert x is None or torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+    if form == dtype:
+        assert torch.equal(back[0], k) and torch.equal(back[1], v)

@@ -279,3 +279,15 @@ def test_many_heads(dq, causal):
         assert not bool(torch.isfinite(t[..., hit]).any())
         assert bool(torch.isfinite(t[..., :hit.start]).all())
         ref.check(rows(t, heads)[:hit.start], want["out"][:hit.start], (err["out"][0][:hit.start], err["out"][1]), True, "rest")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("dq,heads,kv_heads", [(16, 6, 2), (16, 12, 12), (8, 24, 8), (32, 6, 6), (16, 7, 7)])
+def test_heads_in_cache_lines(dtype, dq, heads, kv_heads):
+    """Heads that share lines of 128 bytes by twos, fours and eights, in three such sets
+    or none: every head and block is there once, with walks shared and whole."""
+    say(f"packed, heads in lines {dtype} {dq} {heads}/{kv_heads}")
+    lens = [400, 129, 0, 33]
+    q, do = (rand_map(s, 1, heads * dq, 1, sum(lens), dtype) for s in (1, 2))
+    k, v = (rand_map(s, 1, kv_heads * dq, 1, sum(lens), dtype) for s in (3, 4))
+    compare(q, k, v, do, lens, lens, heads, step(q, k, v, do, ints(ref.starts(lens).tolist()), heads), "lines")
