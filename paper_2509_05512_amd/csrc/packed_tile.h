@@ -211,8 +211,9 @@ template <int SIZE, int TILE, bool KEYS> __device__ __forceinline__ Place place_
         set *= 64;
         const int seq = min(set + lane, n - 1);
         const int qa = clamp(c.qs.first[seq], c.qs), q_len = max(clamp(c.qs.first[seq + 1], c.qs) - qa, 0);
+        // (one array for maps of two sizes: each map's tokens end with it)
         int ka = qa, k_len = q_len;
-        if (c.ks.first != c.qs.first) {
+        if (c.ks.first != c.qs.first || c.ks.tokens != c.qs.tokens) {
             ka = clamp(c.ks.first[seq], c.ks);
             k_len = max(clamp(c.ks.first[seq + 1], c.ks) - ka, 0);
         }

@@ -291,3 +291,38 @@ def test_heads_in_cache_lines(dtype, dq, heads, kv_heads):
     q, do = (rand_map(s, 1, heads * dq, 1, sum(lens), dtype) for s in (1, 2))
     k, v = (rand_map(s, 1, kv_heads * dq, 1, sum(lens), dtype) for s in (3, 4))
     compare(q, k, v, do, lens, lens, heads, step(q, k, v, do, ints(ref.starts(lens).tolist()), heads), "lines")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("dq", [16, 32])
+@pytest.mark.parametrize("q_tokens,k_tokens,first,lq,lk", [
+    (300, 200, [0, 300], [300], [200]), (200, 300, [0, 300], [200], [300]),
+    (300, 200, [0, 130, 260, 300], [130, 130, 40], [130, 70, 0]), (200, 2100, [0, 90, 2100], [90, 110], [90, 2010]),
+    (2100, 200, [0, 90, 2100], [90, 2010], [90, 110])])
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "all"])
+def test_one_array_for_maps_of_two_sizes(dtype, dq, q_tokens, k_tokens, first, lq, lk, causal):
+    """Offsets beyond the smaller map, given for both as one tensor: its sequences end
+    with it, as they do with an array of their own; NaN behind the keys is not read,
+    and what lies around the results stays."""
+    say(f"packed, one array {dtype} dq {dq} {q_tokens} on {k_tokens} of {first} causal {causal}")
+    heads, spare = 2, 400
+
+    def room(value, tokens):
+        all_of = torch.full((spare + tokens + spare, 4, heads * dq), value, dtype=dtype, device=DEV)
+        return all_of, all_of[spare:spare + tokens][None, None].permute(0, 3, 4, 1, 2)
+    q, do = (rand_map(s, 1, heads * dq, 1, q_tokens, dtype) for s in (1, 2))
+    k, v = (room(float("nan"), k_tokens)[1].copy_(rand_map(s, 1, heads * dq, 1, k_tokens, dtype)) for s in (3, 4))
+    first = ints(first)
+
+    def run(k_first):
+        rooms = [room(3.0, t) for t in (q_tokens, q_tokens, k_tokens, k_tokens)]
+        out, dqs, dks, dvs = (view for _, view in rooms)
+        _, saved = quan.quan_packed_attention_forward(q, k, v, first, heads, k_first=k_first, causal=causal, out=out, save=True)
+        quan.quan_packed_attention_backward(q, k, v, out, saved, do, first, heads, k_first=k_first, causal=causal, dq=dqs,
+                                            dk=dks, dv=dvs)
+        for all_of, _ in rooms:
+            assert bool((all_of[:spare] == 3.0).all()) and bool((all_of[-spare:] == 3.0).all())
+        return out, saved.stats, dqs, dks, dvs
+    got = run(first)
+    compare(q, k, v, do, lq, lk, heads, got, "one array", causal)
+    assert all(torch.equal(a, b) for a, b in zip(got, run(first.clone())))
