@@ -32,6 +32,17 @@ import torch
 from . import quan
 
 
+class Pages(quan.Cache):
+    """A cache of pages that holds maps of `tokens` pixels; the slots behind them on
+    a map's last page hold nothing."""
+    tokens = None
+
+    def _replace(self, **fields):
+        got = super()._replace(**fields)
+        got.tokens = self.tokens
+        return got
+
+
 class AttentionBlock:
     """params: float32 tensors by name, for an optimizer; ``load`` casts and
     packs the kernels that the convolutions read after a change to them."""
@@ -129,10 +140,12 @@ class AttentionBlock:
         return tuple(quan.empty_qmap(n, self.kv, height, width, self.dtype, device) for _ in range(2))
 
     def pages(self, n, height, width, page_tokens=64, dtype=torch.float8_e4m3fn):
-        """The same in pages (quan.Cache), the pages of a map one after another."""
+        """The same in pages (a quan.Cache), the pages of a map one after another."""
         per, dq = -(-height * width // page_tokens), self.c // self.heads
         table = torch.arange(n * per, dtype=torch.int32, device=self.bucket.device).view(n, per)
-        return quan.empty_cache(n * per, page_tokens, self.kv // dq, dq, table, dtype)
+        pages = Pages(*quan.empty_cache(n * per, page_tokens, self.kv // dq, dq, table, dtype))
+        pages.tokens = height * width
+        return pages
 
     def write(self, cache, h, row):
         """Keys and values of the rows that h holds, from `row` on."""
@@ -147,10 +160,13 @@ class AttentionBlock:
     def query(self, cache, x, h, pos, kv_len=None, gate=None, width=None):
         """(out, h_out) of one pixel per image, x and h [N, 4, C, 1, 1], at pos
         int32 [N, 2] (y, x) of a cache whose first kv_len int32 [N] pixels are
-        there; a cache of pages holds maps `width` wide (pos and width are for the
-        bias, a causal block has none)."""
+        there, None: all of its maps'; a cache of pages holds maps `width` wide (pos
+        and width are for the bias, a causal block has none).  (A quan.Cache that
+        `pages` has not made has as many as its table.)"""
         q, _, _ = self._parts(self._conv("qkv", h))
         if isinstance(cache, quan.Cache):
+            if kv_len is None and getattr(cache, "tokens", None) is not None:
+                kv_len = torch.full((h.shape[0],), cache.tokens, dtype=torch.int32, device=h.device)
             a = quan.quan_cache_attention(q, cache, kv_len, self.heads, relpos=self._relpos(), pos=pos, width=width)
         else:
             a = quan.quan_attention_forward(q, *cache, self.heads, relpos=self._relpos(), kv_len=kv_len, pos=pos)

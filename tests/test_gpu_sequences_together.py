@@ -262,3 +262,30 @@ def test_long_packed_backward_against_one_sequence():
     for i, a in enumerate(ref.starts(lens)[:-1]):
         alone = [quan.to_device_layout(t[..., a:a + lens[i]]) for t in maps]
         compare(*alone, [lens[i]], [lens[i]], heads, step(*alone, ints([0, lens[i]]), heads), f"alone {i}")
+
+
+@pytest.mark.parametrize("dtype", [None, BF], ids=["e4m3", "bf16"])
+@pytest.mark.parametrize("side,page", [(20, 64), (8, 6), (8, 16)])
+def test_pages_of_whole_maps(dtype, side, page):
+    """Without lengths a query reads a map's pixels, as from the cache of maps, and
+    not the slots behind them on the last page, which are NaN here: a bf16 step of the
+    largest value from the same keys and values in maps (8-bit ones are bf16 numbers)."""
+    say(f"block, pages of whole maps {dtype} {side} {page}")
+    n, c, heads = 3, 32, 4
+    block = AttentionBlock(c, heads, kv_heads=2, radius=side - 1, buckets=9, seed=4)
+    x, h = rand_map(1, n, c, side, side, BF), rand_map(2, n, c, side, side, BF)
+    pages = block.pages(n, side, side, page_tokens=page, **({} if dtype is None else {"dtype": dtype}))
+    for t in pages[:4]:
+        if t is not None:
+            t.view(torch.uint8).fill_(0x7f if t.dtype == E4M3 else 0xff)
+    block.write(pages, h, 0)
+    maps = block.cache(n, side, side)
+    quan.quan_cache_read(pages, *maps)
+    pos = ints([[2, 3], [5, 0], [7, 7]])
+    px, ph = (quan.to_device_layout(t[..., 2:3, 3:4]) for t in (x, h))
+    want = block.query(maps, px, ph, pos)
+    whole = torch.full((n,), side * side, dtype=torch.int32, device=DEV)
+    for got in (block.query(pages, px, ph, pos, width=side), block.query(pages, px, ph, pos, kv_len=whole, width=side),
+                block.query(pages._replace(table=pages.table.clone()), px, ph, pos, width=side)):
+        for p, q in zip(want, got):
+            assert float((p.float() - q.float()).abs().max()) <= 2.0 ** -7 * float(p.float().abs().max())
