@@ -175,10 +175,14 @@ class AttentionBlock:
     def extend(self, cache, x, h, past, gate=None):
         """(out, h_out) of the next pixels of a causal block's sequences, x and h
         [N, 4, C, H, W] in raster order behind the past[i] (integers) that the cache
-        of pages holds of sequence i; theirs are written to it."""
+        of pages holds of sequence i; theirs are written to it, which has to have
+        room for them."""
         if not self.causal:
             raise ValueError("extend is for a causal block")
         n, new, dev = x.shape[0], x.shape[3] * x.shape[4], x.device
+        room = cache.table.shape[1] * cache.page_tokens
+        if len(past) != n or any(p < 0 or p + new > room for p in past):
+            raise ValueError(f"past must be {n} lengths that leave room for {new} of a sequence's {room} positions")
         q, k, v = self._parts(self._conv("qkv", h))
         quan.quan_cache_write(cache, k, v, torch.tensor(past, dtype=torch.int32, device=dev))
         lens = [p + new for p in past]

@@ -10,6 +10,7 @@ import torch
 
 import sequence_reference as ref
 from paper_2509_05512_amd import quan
+from paper_2509_05512_amd.attention_block import AttentionBlock
 from test_block_cpu import QuanRelpos, addr, desc, relpos
 
 E_NULL, E_SHAPE, E_DTYPE, E_ALIGN, E_ALIAS, E_UNSUP, E_LAYOUT = -1, -2, -3, -4, -5, -6, -9
@@ -266,3 +267,21 @@ def test_reference_attends():
         assert np.allclose(res["out"], out.detach().numpy(), atol=1e-12)
         for name, x in zip(("dq", "dk", "dv"), t):
             assert np.allclose(res[name], np.nan_to_num(x.grad.numpy()), atol=1e-12), name
+
+
+def bare_block(c=8, heads=2):
+    """A block without parameters: what its checks look at."""
+    block = AttentionBlock.__new__(AttentionBlock)
+    block.c, block.heads, block.kv, block.causal, block.dtype = c, heads, c, True, torch.bfloat16
+    return block
+
+
+@pytest.mark.parametrize("past", [[5], [5, 5, 5], [-1, 5], [5, 19], [18, 0], [1 << 31, 0]])
+def test_extend_refuses(past):
+    """Pixels behind what the cache has room for, or a number of lengths that is not the
+    maps'; nothing has been computed by then."""
+    block, table = bare_block(), torch.zeros((2, 3), dtype=torch.int32)
+    cache = quan.empty_cache(4, 8, 2, 4, table)  # 24 positions
+    x = quan.empty_qmap(2, 8, 2, 4, torch.bfloat16, "cpu")
+    with pytest.raises(ValueError, match="past"):
+        block.extend(cache, x, x, past)
