@@ -149,6 +149,10 @@ class AttentionBlock:
 
     def write(self, cache, h, row):
         """Keys and values of the rows that h holds, from `row` on."""
+        if isinstance(cache, quan.Cache):
+            room = cache.table.shape[1] * cache.page_tokens
+            if row < 0 or (row + h.shape[3]) * h.shape[4] > room:
+                raise ValueError(f"rows {row} to {row + h.shape[3] - 1} are not among a sequence's {room} positions")
         _, k, v = self._parts(self._conv("qkv", h))
         if isinstance(cache, quan.Cache):
             start = torch.full((h.shape[0],), row * h.shape[4], dtype=torch.int32, device=h.device)

@@ -285,3 +285,14 @@ def test_extend_refuses(past):
     x = quan.empty_qmap(2, 8, 2, 4, torch.bfloat16, "cpu")
     with pytest.raises(ValueError, match="past"):
         block.extend(cache, x, x, past)
+
+
+@pytest.mark.parametrize("rows,row", [(3, 4), (7, 0), (1, 6), (1, -1)])
+def test_write_refuses(rows, row):
+    """Rows behind what a cache of pages has room for, or before its first; nothing has
+    been computed by then."""
+    block, table = bare_block(), torch.zeros((2, 3), dtype=torch.int32)
+    cache = quan.empty_cache(4, 8, 2, 4, table)  # 24 positions, 6 rows of 4
+    h = quan.empty_qmap(2, 8, rows, 4, torch.bfloat16, "cpu")
+    with pytest.raises(ValueError, match="rows"):
+        block.write(cache, h, row)
