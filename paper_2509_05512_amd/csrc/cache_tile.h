@@ -60,6 +60,26 @@ __device__ __forceinline__ f32x4 from_e4m3(int v)
     return f32x4{a[0], a[1], b[0], b[1]};
 }
 
+// 8 probabilities as bf16 numbers, and in their place what those leave, for a second
+// such operand.  They are cut, not rounded, so that neither part is negative, and what
+// is left has 2^-23 of the number added, so that it is not 0 either: an infinity of v
+// times both is that infinity twice.  (Rounded, it was NaN where the rest was 0 or
+// below.  A rest below 2^-7 of the number's binade is rounded to 8 bits: off by 2^-16
+// of the number at most, the half of which it would be between two rounded parts.)
+__device__ __forceinline__ bf16x8 cut(f32x8 &v)
+{
+    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+    u32x4 high;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const unsigned a = __float_as_uint(v[2 * e]), b = __float_as_uint(v[2 * e + 1]);
+        high[e] = __builtin_amdgcn_perm(b, a, 0x07060302);
+        v[2 * e] = fmaf(v[2 * e], 1.0f + 0x1p-23f, -__uint_as_float(a & 0xffff0000u));
+        v[2 * e + 1] = fmaf(v[2 * e + 1], 1.0f + 0x1p-23f, -__uint_as_float(b & 0xffff0000u));
+    }
+    return __builtin_bit_cast(bf16x8, high);
+}
+
 // Tokens of a sequence: of image `img`, from `at` on.
 struct Tokens {
     int img, at, len;

@@ -187,13 +187,18 @@ __global__ void __launch_bounds__(kThreads, 2) packed_forward_kernel(Forward f)
             for (int st = 0; st < 2; ++st) {
                 frag p[QN][PARTS];
 #pragma unroll
-                for (int n = 0; n < QN; ++n)
+                for (int n = 0; n < QN; ++n) {
+                    if constexpr (PARTS == 2) {
+                        f32x8 t;
 #pragma unroll
-                    for (int part = 0; part < PARTS; ++part) {
-                        if (part > 0)
-                            take_from(s[n][sub], st, p[n][part - 1]);
-                        p[n][part] = acc_frag<T>(s[n][sub], st);
+                        for (int e = 0; e < 8; ++e)
+                            t[e] = s[n][sub][8 * st + e];
+                        p[n][0] = cut(t);
+                        p[n][1] = to_frag<T>(t);
+                    } else {
+                        p[n][0] = acc_frag<T>(s[n][sub], st);
                     }
+                }
 #pragma unroll
                 for (int i = 0; i < DP / 32; ++i) {
                     const frag column = col_frag<DP>(vb, sub, st, i);

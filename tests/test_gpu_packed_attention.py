@@ -326,3 +326,42 @@ def test_one_array_for_maps_of_two_sizes(dtype, dq, q_tokens, k_tokens, first, l
     got = run(first)
     compare(q, k, v, do, lq, lk, heads, got, "one array", causal)
     assert all(torch.equal(a, b) for a, b in zip(got, run(first.clone())))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("save", [False, True], ids=["inference", "training"])
+@pytest.mark.parametrize("heads,kv_heads,dq,lq,lk", [
+    (2, 1, 16, [300, 40], None), (2, 2, 32, [300, 40], None), (2, 2, 5, [70], [200]), (1, 1, 16, [130], [2000]),
+    (56, 8, 16, [600, 300], None)])
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "all"])
+def test_infinite_values(dtype, save, heads, kv_heads, dq, lq, lk, causal):
+    """An infinity in v that a query sees is its result's, both signs in one place are
+    NaN, as is a NaN: in the walk and at its edge, at inference and in training.  The
+    other reals keep their bounds."""
+    say(f"packed, infinite values {dtype} save {save} heads {heads}/{kv_heads} dq {dq} {lq} {lk} causal {causal}")
+    lk = lk or lq
+    q = rand_map(1, 1, heads * dq, 1, sum(lq), dtype)
+    k, v = (rand_map(s, 1, kv_heads * dq, 1, sum(lk), dtype) for s in (2, 3))
+    first, k_first = (ints(ref.starts(t).tolist()) for t in (lq, lk))
+    # (component, channel, token, value) of the first head of keys in the first sequence
+    odd = [(0, 0, 3, np.inf), (1, 2, 3, -np.inf), (1, 3, 65, np.inf), (2, 1, 10, np.inf), (2, 1, lk[0] - 2, -np.inf),
+           (3, 4, 69, np.nan), (3, 0, 20, np.inf), (3, 0, 66, np.nan), (3, 0, 67, np.inf)]
+    zeros = v.clone(memory_format=torch.preserve_format)
+    for comp, ch, token, value in odd:
+        v[0, comp, ch, 0, token] = value
+        zeros[0, comp, ch, 0, token] = 0.0
+    got = quan.quan_packed_attention_forward(q, k, v, first, heads, k_first=k_first, causal=causal, save=save)
+    got = rows(got[0] if save else got, heads)
+    # (with dout the bounds are those of a training step)
+    want, err = ref.packed(rows(q, heads), rows(k, kv_heads), rows(zeros, kv_heads), lq, lk, causal,
+                           dout=np.zeros_like(got) if save else None)
+    want, bound = want["out"], err["out"]
+    extra = np.zeros_like(want)
+    for comp, ch, token, value in odd:
+        sees = np.arange(lq[0]) >= (token - (lk[0] - lq[0]) if causal else 0)
+        with np.errstate(invalid="ignore"):
+            extra[:lq[0], :heads // kv_heads, comp * dq + ch] += np.where(sees, value, 0.0)[:, None]
+    hit = ~np.isfinite(extra)
+    assert hit.any() and np.array_equal(got[hit], extra[hit], equal_nan=True)
+    fixed = np.where(hit, want, got)
+    ref.check(fixed, want, (bound[0], bound[1]), dtype == BF, "the others")
