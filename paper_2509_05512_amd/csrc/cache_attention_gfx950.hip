@@ -436,7 +436,12 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 2 && D < 128 ? 4 : 2) c
                         }
                 } else {
                     bf16x8 pf[PP];
-                    split<PP>(p, pf);
+                    if constexpr (F == CacheForm::BF16) {  // (whose values may be infinite)
+                        pf[0] = cut(p);
+                        pf[1] = __builtin_convertvector(p, bf16x8);
+                    } else {
+                        split<PP>(p, pf);
+                    }
 #pragma unroll
                     for (int m = 0; m < kMine; ++m) {
                         // element m of the 8 rows

@@ -192,3 +192,31 @@ def test_read_back_attention_is_the_same():
     a = quan.quan_cache_attention(q, cache, ints(lens), heads)
     b = quan.quan_attention_forward(q, k, v, heads, kv_len=ints(lens))
     assert float((a.float() - b.float()).abs().max()) <= 2.0 ** -7 * float(b.float().abs().max())
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("dq,heads,kv_heads", [(16, 4, 2), (8, 3, 3), (32, 16, 1), (5, 2, 1)])
+@pytest.mark.parametrize("lens", [[100, 1, 65], [5000, 70, 0]], ids=["short", "long"])
+def test_infinite_values(dtype, dq, heads, kv_heads, lens):
+    """An infinity in a value is the result's, both signs in one place are NaN, as is a
+    NaN; the other reals keep their bounds."""
+    say(f"cache attention, infinite values {dtype} dq {dq} heads {heads}/{kv_heads} {lens}")
+    cache = fill(21, lens, 16, kv_heads, dq, dtype, dtype)
+    q = rand_map(3, len(lens), heads * dq, 1, 1, dtype)
+    odd = [(0, 3, np.inf), (1, 7, -np.inf), (2, 9, np.inf), (2, lens[0] - 1, -np.inf), (3, 40, np.nan), (4 * dq - 1, 64, np.inf),
+           (4 * dq - 2, 5, np.inf), (4 * dq - 2, 50, np.nan), (4 * dq - 2, 51, np.inf)]
+    zeros = cache._replace(values=cache.values.clone())
+    extra = np.zeros((len(lens), heads, 4 * dq))
+    for real, token, value in odd:
+        page = int(cache.table[0, token // 16])
+        cache.values[page, 0, token % 16, real] = value
+        zeros.values[page, 0, token % 16, real] = 0.0
+        with np.errstate(invalid="ignore"):
+            extra[0, :heads // kv_heads, real] += value
+    got = ref.rows_of(quan.quan_cache_attention(q, cache, ints(lens), heads).float().cpu().numpy().astype(np.float64), heads)
+    keys, values = values_of(zeros)
+    rows = ref.rows_of(q.float().cpu().numpy().astype(np.float64), heads)
+    want, err, size = ref.cache_attention(rows, keys, values, lens, heads)
+    hit = ~np.isfinite(extra)
+    assert np.array_equal(got[hit], extra[hit], equal_nan=True)
+    ref.check(np.where(hit, want, got), want, (err, ref.F32 * max(size, 1e-30)), dtype == BF, "the others")
