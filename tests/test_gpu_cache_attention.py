@@ -220,3 +220,31 @@ def test_infinite_values(dtype, dq, heads, kv_heads, lens):
     hit = ~np.isfinite(extra)
     assert np.array_equal(got[hit], extra[hit], equal_nan=True)
     ref.check(np.where(hit, want, got), want, (err, ref.F32 * max(size, 1e-30)), dtype == BF, "the others")
+
+
+@pytest.mark.parametrize("dtype,form", FORMS, ids=["bf16-e4m3", "fp32-e4m3", "bf16", "fp32"])
+@pytest.mark.parametrize("count", [65, 129, 200])
+def test_many_sequences_dealt_out(dtype, form, count):
+    """Sequences in several sets of 64, empty ones among them, with long ones behind the
+    first set that work-groups share."""
+    say(f"cache attention of {count} sequences, dealt out {dtype} {form}")
+    lens = np.random.default_rng(count).integers(0, 60, count).tolist()
+    lens[3], lens[64], lens[count - 1] = 0, 3000, 5001
+    lens[count // 2 + 20] = 1
+    cache = fill(count, lens, 64, 1, 8, dtype, form)
+    run(cache, rand_map(1, count, 8, 1, 1, dtype), lens, 1, what="out")
+
+
+@pytest.mark.parametrize("dtype,form", FORMS, ids=["bf16-e4m3", "fp32-e4m3", "bf16", "fp32"])
+@pytest.mark.parametrize("dq,heads,kv_heads", [(32, 16, 1), (24, 32, 2), (20, 33, 1)])
+def test_many_wide_heads_of_a_key(dtype, form, dq, heads, kv_heads):
+    """16 query heads and more than 64 reals to a head of keys, whose results take more
+    than 64 KiB where the waves' are joined."""
+    say(f"cache attention {dtype} {form} dq {dq} heads {heads}/{kv_heads}")
+    lens = [0, 1, 70, 700]
+    cache = fill(31, lens, 16, kv_heads, dq, dtype, form)
+    q = rand_map(4, len(lens), heads * dq, 1, 1, dtype)
+    run(cache, q, lens, heads, what="out")
+    g = torch.Generator().manual_seed(6)
+    table = torch.randn((heads, 1, 9), generator=g).to(DEV)
+    run(cache, q, lens, heads, (table, None, quan.quan_relpos_buckets(30, 9, DEV)), [[0, 5]] * 4, 50, what="out with a bias")

@@ -365,3 +365,31 @@ def test_infinite_values(dtype, save, heads, kv_heads, dq, lq, lk, causal):
     assert hit.any() and np.array_equal(got[hit], extra[hit], equal_nan=True)
     fixed = np.where(hit, want, got)
     ref.check(fixed, want, (bound[0], bound[1]), dtype == BF, "the others")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("count", [65, 100, 200])
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "all"])
+def test_many_sequences_with_shared_walks(dtype, count, causal):
+    """Sequences in several sets of 64, the long ones behind the first set with walks
+    that work-groups share (one head leaves fewer blocks than are wanted)."""
+    say(f"packed, {count} sequences with shared walks {dtype} causal {causal}")
+    lens = np.random.default_rng(count).integers(0, 9, count).tolist()
+    lens[0], lens[64], lens[count - 1] = 0, 700, 2000
+    heads, dq = 1, 8
+    q, k, v, do = (rand_map(s, 1, heads * dq, 1, sum(lens), dtype) for s in range(4))
+    first = ints(ref.starts(lens).tolist())
+    got = step(q, k, v, do, first, heads, causal=causal)
+    compare(q, k, v, do, lens, lens, heads, got, "many", causal)
+    assert all(torch.equal(a, b) for a, b in zip(got, step(q, k, v, do, first, heads, causal=causal)))
+
+
+@pytest.mark.parametrize("count", [4096, 4097, 5000])
+def test_thousands_of_sequences(count):
+    """More sets of 64 sequences than a wave has lanes, longer ones in the last of them."""
+    say(f"packed, {count} sequences")
+    lens = np.random.default_rng(count).integers(0, 4, count).tolist()
+    lens[0], lens[70], lens[count - 3], lens[count - 1] = 0, 300, 200, 129
+    heads, dq = 1, 8
+    q, k, v, do = (rand_map(s, 1, heads * dq, 1, sum(lens), BF) for s in range(4))
+    compare(q, k, v, do, lens, lens, heads, step(q, k, v, do, ints(ref.starts(lens).tolist()), heads), "thousands")
