@@ -764,9 +764,10 @@ QUAN_API int quan_dropout(const void *x, float p, const uint64_t *rng, void *out
  * order.  With first, an int32 array [sequences + 1] on the device that ascends
  * from 0 or more to at most the map's pixels, the map is one image (N = 1) and
  * sequence i its pixels first[i] .. first[i + 1] - 1; sequences may be empty,
- * and what lies before the first and behind the last one is neither read nor
- * written.  (Values out of order or range are clamped: their sequences are cut,
- * no memory outside the maps is touched.)
+ * and what lies before the first and behind the last one goes into no result and
+ * is not written (it may be read, as memory of the maps).  (Values out of order or
+ * range are clamped: their sequences are cut, no memory outside the maps is
+ * touched.  One array may stand for maps of two sizes, each map ending its own.)
  */
 
 /* What a cache holds: the maps' own type, or 8-bit floats (e4m3: 4 bits of
@@ -849,8 +850,8 @@ QUAN_API int quan_cache_read(const quan_cache *cache, const int32_t *first, cons
  *             (y, x), NULL for (0, 0).
  *   scale     finite.
  *
- * A sequence without a token (or with every bias -infinity) has out 0.  bf16
- * queries meet bf16 keys as they are (8-bit elements are bf16 numbers);
+ * A sequence without a token (or with every bias -infinity) has out 0; an infinity
+ * in a value is the result's.  bf16 queries meet bf16 keys as they are (8-bit elements are bf16 numbers);
  * probabilities keep 16 bits with bf16 queries, 24 with fp32 ones, sums are fp32.
  * Long sequences are dealt out to work-groups where a workspace can be had (at
  * most 64 MiB); a captured call that cannot have it may differ in rounding.
@@ -866,7 +867,7 @@ QUAN_API int quan_cache_attention(const quan_tensor *q, const quan_cache *cache,
  *   keys j <= i + lk - lq   (causal = 1)   or all of them   (causal = 0),
  *
  * and out_i = sum_j P_ij v_j as in quan_attention_forward, without a bias.  A
- * query that sees no key has out 0.
+ * query that sees no key has out 0, and an infinity in v that it sees is its out's.
  *
  *   q, out     descriptors [N, 4, heads*dq, Hq, Wq]; k, v [N, 4, kv_heads*dq, Hk,
  *              Wk], kv_heads dividing heads: channel slices of wider maps, as

@@ -1138,8 +1138,8 @@ def quan_packed_attention_forward(q, k, v, first, heads, k_first=None, causal=Tr
     sequence per image.  k, v: [.., 4, Ckv, Hk, Wk], their sequences by k_first
     (None: as first); heads may share keys as in quan_attention_forward.  A
     sequence's queries are the last of its keys' tokens: query i of lq sees keys j
-    <= i + lk - lq, or all of them with causal=False.  Pixels of no sequence are
-    neither read nor written.  Returns out, or with save (out, PackedSaved) for
+    <= i + lk - lq, or all of them with causal=False.  Pixels of no sequence go into
+    no result and are not written.  Returns out, or with save (out, PackedSaved) for
     quan_packed_attention_backward."""
     lib = load_library()
     args = _packed_args(q, k, v, first, heads, k_first, causal, scale)
