@@ -851,8 +851,9 @@ QUAN_API int quan_cache_read(const quan_cache *cache, const int32_t *first, cons
  *   scale     finite.
  *
  * A sequence without a token (or with every bias -infinity) has out 0; an infinity
- * in a value is the result's.  bf16 queries meet bf16 keys as they are (8-bit elements are bf16 numbers);
- * probabilities keep 16 bits with bf16 queries, 24 with fp32 ones, sums are fp32.
+ * in a value is the result's.  bf16 queries meet bf16 keys as they are (8-bit
+ * elements are bf16 numbers); probabilities keep 16 bits with bf16 queries, 24 with
+ * fp32 ones, sums are fp32.
  * Long sequences are dealt out to work-groups where a workspace can be had (at
  * most 64 MiB); a captured call that cannot have it may differ in rounding.
  */

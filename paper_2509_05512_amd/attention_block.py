@@ -180,7 +180,8 @@ class AttentionBlock:
         """(out, h_out) of the next pixels of a causal block's sequences, x and h
         [N, 4, C, H, W] in raster order behind the past[i] (integers) that the cache
         of pages holds of sequence i; theirs are written to it, which has to have
-        room for them."""
+        room for them.  (All that it holds of them is read back into maps, and the
+        lengths go from the host to the device: a graph cannot capture the call.)"""
         if not self.causal:
             raise ValueError("extend is for a causal block")
         n, new, dev = x.shape[0], x.shape[3] * x.shape[4], x.device

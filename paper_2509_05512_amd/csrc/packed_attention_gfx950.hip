@@ -8,9 +8,10 @@
 //
 // Where there are 512 blocks of 256 queries, a wave has 64: a tile's operands are read
 // from LDS once for two products.  (Nine sequences of up to 6400 tokens, 8 heads of 64
-// reals on 2: 183 us, 731 TFLOP/s, 245 with 32 queries a wave and the blocks in order.)
-// Its SIMDs are then 31 % of the time in matrix instructions and 54 % in vector
-// ones, with two waves each that overlap little (waiting 29 %).  No faster, each on its own: scores
+// reals on 2: 179 to 183 us on one card, 740 TFLOP/s, 245 with 32 queries a wave and the
+// blocks in order; 213 on another card.)  Its SIMDs are then 31 % of the time in matrix
+// instructions and 53 % in vector ones, with two waves each that overlap little
+// (waiting 29 %).  No faster, each on its own: scores
 // without the running maximum where a tile's sum shows that none is far ahead (a fifth
 // fewer vector instructions), raised wave priorities for either half of a tile, walks
 // that begin in different places, tiles dealt to two sets of waves in a work-group.
@@ -34,7 +35,7 @@ struct Forward {
 };
 
 // QN: sets of 32 queries that a wave holds.  PARTS: bf16 numbers that a probability
-// meets v in, the second what the first leaves of it.  At inference one will do: it is
+// meets v in, the second what the first leaves of it (see cut()).  At inference one will do: it is
 // off by 2^-8 of a term at most, as out is of the sum once it is rounded.  In a
 // training step (with rest) there are two: the rows' sums of dout out go into every
 // dS, and with probabilities of 8 bits and the rounded out the queries' gradient was

@@ -8,11 +8,11 @@
 // blocks of keys and walks over the queries that see them, head by head of those
 // that share them (dK, dV).
 //
-// 7200 tokens in nine sequences, 8 heads of 64 reals: 41 us and 50; one of 6400, 4 heads
-// of 128 on 2: 118 and 130, and 21 to sum the parts of shared walks, with matrix units
-// 20 and 24 % busy.  Their waves, one to two a SIMD, wait 36 to 44 % of their time, for
-// LDS and for each other at a tile's barrier; a walk of one tile takes 8 us, and the
-// longest walks of the nine sequences three times the mean.
+// 7200 tokens in nine sequences, 8 heads of 64 reals: 41 to 43 us and 50 to 54; one of
+// 6400, 4 heads of 128 on 2: 118 to 123 and 130 to 139, and 21 to sum the parts of shared
+// walks, with matrix units 20 and 24 % busy.  Their waves, one to two a SIMD, wait 36 to
+// 44 % of their time, for LDS and for each other at a tile's barrier; a walk of one tile
+// takes 8 us, and the longest walks of the nine sequences three times the mean.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -45,7 +45,7 @@ template <typename T, int DQP, int PAIR = kPair<T, DQP>>
 __global__ void __launch_bounds__(64 * kWaves * PAIR, DQP <= 16 || PAIR == 2 ? 2 : 1) packed_dq_kernel(Backward f)
 {
     constexpr int DP = 4 * DQP, WAVES = kWaves * PAIR;
-        typedef Stage<T, DP, 64 * WAVES> Tile;
+    typedef Stage<T, DP, 64 * WAVES> Tile;
     typedef typename Elem<T>::frag frag;
     constexpr int KT = Tile::kTokens, SUBS = KT / 32 / PAIR, MINE = DP / 32 / PAIR;  // parts, and sums' tiles, of a wave
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];
@@ -265,7 +265,7 @@ template <typename T, int DQP, int PAIR = kPair<T, DQP>>
 __global__ void __launch_bounds__(64 * kWaves * PAIR, DQP <= 16 || PAIR == 2 ? 2 : 1) packed_dkv_kernel(Backward f)
 {
     constexpr int DP = 4 * DQP, WAVES = kWaves * PAIR;
-        typedef Stage<T, DP, 64 * WAVES> Tile;
+    typedef Stage<T, DP, 64 * WAVES> Tile;
     typedef typename Elem<T>::frag frag;
     constexpr int QT = Tile::kTokens, SUBS = QT / 32 / PAIR;  // parts of a tile that a wave takes
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_raw[];

@@ -150,7 +150,10 @@ template <int SIZE, int TILE, bool KEYS> __device__ __forceinline__ float walks_
 // the launch has.  (One sequence of 6400 tokens, 4 heads of 128 reals, a training
 // step: 368 us, 384 with shares of 1 / 400, 409 of 1 / 300, 405 with starts of 3 tiles
 // at 1 / 512; without shares 1569.)  all: the sum of walks_of() over the lanes' sequences.
-constexpr int kSlots = 512;                                           // two to a compute unit
+// (Two to a compute unit, which is what heads of up to 64 bf16 reals and the wide
+// forward pass have; registers and LDS leave the wide gradients one, so that there it
+// is a share of what runs in two turns.)
+constexpr int kSlots = 512;
 constexpr int start_of(int tile) { return tile == 64 ? 4 : 1; }  // tiles' worth: bf16, fp32
 template <int TILE, bool KEYS>
 __device__ __forceinline__ Walk walk_of(const PackedCall &c, int lq, int lk, int mine, int splits, float all)
