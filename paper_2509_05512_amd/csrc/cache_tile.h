@@ -64,8 +64,8 @@ __device__ __forceinline__ f32x4 from_e4m3(int v)
 // such operand.  They are cut, not rounded, so that neither part is negative, and what
 // is left has 2^-23 of the number added, so that it is not 0 either: an infinity of v
 // times both is that infinity twice.  (Rounded, it was NaN where the rest was 0 or
-// below.  A rest below 2^-7 of the number's binade is rounded to 8 bits: off by 2^-16
-// of the number at most, the half of which it would be between two rounded parts.)
+// below.  The rest is under 2^-7 of the number's binade and rounded to 8 bits: off by
+// 2^-16 of the number at most, twice what two rounded parts are off by.)
 __device__ __forceinline__ bf16x8 cut(f32x8 &v)
 {
     typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
